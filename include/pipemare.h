@@ -383,6 +383,95 @@ pm_status pm_update_flat_static(const pm_arenas* arenas, const uint64_t* stage_o
                                 const int32_t* tau_bkwd, int32_t n_stages, const pm_config* cfg,
                                 int64_t k, void* stream);
 
+/* ---- operators for programs with their own forward and backward pass ------------------------ */
+
+/* The calls below stand beside pm_update_flat: a program that computes its gradients itself takes its attention over
+ * packed sequences, its loss and the clipping of its gradients from here and hands the gradient arena to pm_update_flat.
+ * They keep nothing between calls, allocate nothing, are asynchronous on `stream` (whose device must be the current
+ * one), copy nothing between host and device and can be captured into a CUDA graph.  Two calls may run at the same time
+ * as long as neither writes what the other uses, workspaces included.  Sums, softmax statistics and norms are held in
+ * 32 bits or more; no result depends on the order in which blocks run.  pm_last_error(NULL) gives the message of a
+ * refused call (of the calling thread). */
+
+/* A [tokens, heads, head_dim] tensor: the last dimension contiguous, the others at any stride (elements, >= 0; outputs
+ * without overlap), so that q, k and v can be views of one projection's output. */
+typedef struct {
+  void* data;                    /* device */
+  int64_t token_stride, head_stride;
+} pm_head_view;
+
+/* Attention over sequences of different lengths laid end to end.  Sequence b is tokens cu_seqlens[b] ..
+ * cu_seqlens[b + 1] - 1 (device array of n_seqs + 1 ascending entries within 0 .. n_tokens; empty sequences are allowed,
+ * tokens before the first and behind the last belong to none and are neither used nor written).  Query head h reads
+ * key/value head h / (n_heads / n_kv_heads).
+ *   s_ij = scale q_i . k_j for the keys of i's sequence (causal: those with j <= i),  lse_i = log sum_j exp(s_ij),
+ *   o_i = sum_j exp(s_ij - lse_i) v_j
+ * dtype is the type of every tensor but lse (PM_BF16: products of bf16 values with fp32 sums; the probabilities are
+ * rounded to bf16 before they multiply v).  head_dim: 1 to 128.  A value that is not finite spreads over the results of
+ * its own sequence (in the backward pass, and through v, to positions before it, too) and to no other.  Entries of
+ * cu_seqlens outside 0 .. n_tokens are clipped to that range; if they do not ascend, the results of the sequences concerned
+ * are undefined, and no tensor is touched outside its rows. */
+typedef struct {
+  int32_t dtype;                 /* PM_F32 | PM_BF16 */
+  int32_t n_heads, n_kv_heads;   /* n_heads a multiple of n_kv_heads */
+  int32_t head_dim;
+  int32_t n_seqs;
+  int32_t causal;
+  int64_t n_tokens;              /* rows of every tensor */
+  float scale;                   /* positive; 1 / sqrt(head_dim) as a rule */
+} pm_attention_desc;
+
+/* lse: [n_heads][n_tokens] float, or NULL where no backward pass follows.  o must not overlap q, k or v. */
+pm_status pm_attention_packed_forward(const pm_attention_desc* desc, const pm_head_view* q, const pm_head_view* k,
+                                      const pm_head_view* v, const int32_t* cu_seqlens, const pm_head_view* o, float* lse,
+                                      void* stream);
+/* Gradients of q, k, v from d_o and the forward pass's o and lse; dk and dv are summed over the query heads that share
+ * them.  dq, dk, dv overlap neither each other nor the inputs.  workspace: at least
+ * pm_attention_packed_workspace_bytes(desc) bytes of device memory, 16-byte aligned. */
+uint64_t pm_attention_packed_workspace_bytes(const pm_attention_desc* desc);
+pm_status pm_attention_packed_backward(const pm_attention_desc* desc, const pm_head_view* q, const pm_head_view* k,
+                                       const pm_head_view* v, const pm_head_view* o, const float* lse,
+                                       const pm_head_view* d_o, const int32_t* cu_seqlens, const pm_head_view* dq,
+                                       const pm_head_view* dk, const pm_head_view* dv, void* workspace,
+                                       uint64_t workspace_bytes, void* stream);
+
+/* Per row of logits [rows, vocab] (row_stride elements apart, dtype PM_F32 | PM_BF16):
+ *   lse = log sum_j exp(x_j);  logprob = x_y - lse for the target y;  entropy = lse - sum_j p_j x_j;  the top_k largest
+ *   logits' ids, in descending order (equal logits: the lower id first), and their log probabilities.
+ * targets and logprob [rows] go together (both NULL: not wanted); a target < 0 is padding (logprob 0, no gradient
+ * through it), one >= vocab gives NaN.  entropy, lse: [rows] or NULL.  top_logprob, top_ids: [rows, top_k], top_k 0 to 32.
+ * Logits of -infinity have probability 0; a row of nothing else has lse and log probabilities -infinity, entropy 0 and no
+ * gradient.  A row that holds a NaN or +infinity has no distribution: its float results are NaN, its ids -1. */
+pm_status pm_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t vocab, int64_t row_stride,
+                            const int32_t* targets, float* logprob, float* entropy, float* lse, int32_t top_k,
+                            float* top_logprob, int32_t* top_ids, void* stream);
+/* d_logits [rows, vocab] (dtype as logits, grad_stride elements apart) from the gradients of logprob and of the entropy
+ * (either may be NULL), with lse and (for d_entropy) entropy as the forward call wrote them:
+ *   d_logits_j = d_logprob ([j = y] - p_j) - d_entropy p_j (log p_j + entropy).
+ * p_j = exp(x_j - lse); in rows with |lse| > 4096, where a rounded lse no longer resolves p, it is taken from the logits.
+ * d_logits may be logits itself (same strides); otherwise the two do not overlap. */
+pm_status pm_token_logprobs_backward(const void* logits, int32_t dtype, int64_t rows, int32_t vocab, int64_t row_stride,
+                                     const int32_t* targets, const float* lse, const float* entropy,
+                                     const float* d_logprob, const float* d_entropy, void* d_logits, int64_t grad_stride,
+                                     void* stream);
+
+/* Clipping by the global norm over many tensors:
+ *   norm = sqrt(sum of the squares of every src element),  scale = min(1, max_norm / norm),  dst = scale * src
+ * norm and scale: one device float each.  dst may be src itself (clipping in place, same type), or another tensor of
+ * either type, such as a slice of the gradient arena; otherwise sources and destinations do not overlap.  The squares are
+ * summed in 64 bits, so none leaves the range.  A norm that is infinite or NaN is reported as it is and scales nothing
+ * (scale 1).  tensors: host array, read during the call; empty tensors are allowed.  max_norm: positive, infinity to
+ * measure the norm alone.  workspace: device, at least pm_clip_gradients_workspace_bytes(n_tensors) bytes. */
+typedef struct {
+  const void* src;               /* device */
+  void* dst;                     /* device */
+  uint64_t count;                /* elements */
+  int32_t src_dtype, dst_dtype;  /* PM_F32 | PM_BF16 */
+} pm_tensor_pair;
+uint64_t pm_clip_gradients_workspace_bytes(int32_t n_tensors);
+pm_status pm_clip_gradients(const pm_tensor_pair* tensors, int32_t n_tensors, double max_norm, float* norm, float* scale,
+                            void* workspace, uint64_t workspace_bytes, void* stream);
+
 const char* pm_status_string(pm_status s);
 
 #ifdef __cplusplus

@@ -51,6 +51,19 @@ class pm_arenas(C.Structure):
                 ("grad", C.c_void_p), ("w_lp", C.c_void_p), ("count", C.c_uint64)]
 
 
+class pm_head_view(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class pm_attention_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("n_seqs", C.c_int32), ("causal", C.c_int32), ("n_tokens", C.c_int64), ("scale", C.c_float)]
+
+
+class pm_tensor_pair(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("count", C.c_uint64), ("src_dtype", C.c_int32), ("dst_dtype", C.c_int32)]
+
+
 class PipeMareError(RuntimeError):
     def __init__(self, status, message):
         super().__init__(f"{status}: {message}")
@@ -102,6 +115,16 @@ def lib():
                                         C.c_int32, C.POINTER(pm_config), C.c_int64, vp]
     L.pm_update_flat_static_max_stages.restype = C.c_int32
     L.pm_update_flat_static_last_error.restype = C.c_char_p
+    i32, i64, u64, view, desc = C.c_int32, C.c_int64, C.c_uint64, C.POINTER(pm_head_view), C.POINTER(pm_attention_desc)
+    L.pm_attention_packed_forward.argtypes = [desc, view, view, view, vp, view, vp, vp]
+    L.pm_attention_packed_workspace_bytes.argtypes = [desc]
+    L.pm_attention_packed_workspace_bytes.restype = u64
+    L.pm_attention_packed_backward.argtypes = [desc, view, view, view, view, vp, view, vp, view, view, view, vp, u64, vp]
+    L.pm_token_logprobs.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp, vp, i32, vp, vp, vp]
+    L.pm_token_logprobs_backward.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.pm_clip_gradients_workspace_bytes.argtypes = [i32]
+    L.pm_clip_gradients_workspace_bytes.restype = u64
+    L.pm_clip_gradients.argtypes = [C.POINTER(pm_tensor_pair), i32, C.c_double, vp, vp, vp, u64, vp]
     _lib = L
     return L
 

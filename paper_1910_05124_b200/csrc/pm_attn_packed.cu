@@ -1,0 +1,377 @@
+// Attention over packed sequences with shared key/value heads, forward and backward, on the CUDA cores: fp32, and bf16 head widths
+// or layouts that the tensor-core kernels do not take.
+//
+//   s_ij = scale q_i . k_j (j <= i where causal),  lse_i = log sum_j e^(s_ij),  o_i = sum_j e^(s_ij - lse_i) v_j
+//   p_ij = e^(s_ij - lse_i),  ds_ij = p_ij (do_i . v_j - do_i . o_i)
+//   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_{h, i} ds_ij q_i,   dv_j = sum_{h, i} p_ij do_i    (h: the heads that share k, v)
+//
+// Tiles of 64 x 64 scores by 256 threads, a thread holds 4 x 4 of them; operands are fp32 in shared memory whatever their type
+// (exact for bf16), all sums fp32.  Forward: one block per 64 query rows and head, one pass over the keys with the running
+// maximum and sum.  Backward: one kernel owns query rows (dq), one owns key rows (dk, dv) and walks the query tiles of every
+// head of its group, so each gradient is summed by one block in a fixed order, without atomics, at the price of forming the
+// scores twice.
+#include <atomic>
+
+#include "pm_attn_packed.cuh"
+
+namespace pm {
+
+constexpr int PK_T = 64, PK_LDP = PK_T + 4, PK_THREADS = 256;
+
+template <int DP> constexpr int kPkLd = DP + 4;
+template <int DP> constexpr int pk_smem(int tiles, int squares) { return (tiles * PK_T * kPkLd<DP> + squares * PK_T * PK_LDP) * 4; }
+
+// rows row0 .. row0 + 63 of a head into a tile, zeros outside the sequence and behind the head's width
+template <typename T, int DP>
+__device__ __forceinline__ void pk_load(float* tile, const HeadView& x, const SeqTile& s, int row0, int head, int dim) {
+  for (int i = threadIdx.x; i < PK_T * DP; i += PK_THREADS) {
+    const int r = i / DP, c = i % DP;
+    tile[r * kPkLd<DP> + c] = (row0 + r < s.len && c < dim) ? to_f<T>(head_row<T>(x, s.begin + row0 + r, head)[c]) : 0.f;
+  }
+}
+
+// acc[i][j] += A[4 ty + i] . B[tx + 16 j]
+template <int DP> __device__ __forceinline__ void pk_abt(float (&acc)[4][4], const float* A, const float* B) {
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+#pragma unroll 4
+  for (int d = 0; d < DP; d += 4) {
+    float4 a[4], b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(A + (4 * ty + i) * kPkLd<DP> + d);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = *reinterpret_cast<const float4*>(B + (tx + 16 * j) * kPkLd<DP> + d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(a[i].w, b[j].w, fmaf(a[i].z, b[j].z, fmaf(a[i].y, b[j].y, fmaf(a[i].x, b[j].x, acc[i][j]))));
+  }
+}
+// the thread's columns of a DP-wide row: 2 tx, 2 tx + 1 (DP = 32), else 4 tx .. 4 tx + 3 of every 64
+template <int DP> __device__ __forceinline__ int pk_col(int c) {
+  const int tx = threadIdx.x & 15;
+  return DP == 32 ? 2 * tx + c : (c >> 2) * 64 + 4 * tx + (c & 3);
+}
+// acc[i][c] += sum_k P[4 ty + i][k] B[k][column c]
+template <int DP> __device__ __forceinline__ void pk_pb(float (&acc)[4][DP / 16], const float* P, const float* B) {
+  const int ty = threadIdx.x >> 4;
+#pragma unroll 2
+  for (int k = 0; k < PK_T; k += 4) {
+    float p[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 v = *reinterpret_cast<const float4*>(P + (4 * ty + i) * PK_LDP + k);
+      p[i][0] = v.x; p[i][1] = v.y; p[i][2] = v.z; p[i][3] = v.w;
+    }
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      float b[DP / 16];
+      const float* row = B + (k + kk) * kPkLd<DP>;
+      if constexpr (DP == 32) {
+        const float2 v = *reinterpret_cast<const float2*>(row + pk_col<DP>(0));
+        b[0] = v.x; b[1] = v.y;
+      } else {
+#pragma unroll
+        for (int g = 0; g < DP / 64; ++g) {
+          const float4 v = *reinterpret_cast<const float4*>(row + pk_col<DP>(4 * g));
+          b[4 * g] = v.x; b[4 * g + 1] = v.y; b[4 * g + 2] = v.z; b[4 * g + 3] = v.w;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) acc[i][c] = fmaf(p[i][kk], b[c], acc[i][c]);
+    }
+  }
+}
+template <typename T, int DP>
+__device__ __forceinline__ void pk_store(const HeadView& x, const SeqTile& s, int row0, int head, int dim, const float (&acc)[4][DP / 16], const float (&f)[4]) {
+  const int ty = threadIdx.x >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = row0 + 4 * ty + i;
+    if (r >= s.len) continue;
+    T* out = head_row_out<T>(x, s.begin + r, head);
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) if (pk_col<DP>(c) < dim) out[pk_col<DP>(c)] = from_f<T>(acc[i][c] * f[i]);
+  }
+}
+__device__ __forceinline__ SeqTile pk_tile(const PackedArgs& a) { return find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x, PK_T); }
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(PK_THREADS) attn_packed_fwd_kernel(PackedArgs a) {
+  const SeqTile s = pk_tile(a);
+  if (s.tile < 0) return;
+  extern __shared__ float sm[];
+  float *sQ = sm, *sK = sQ + PK_T * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sP = sV + PK_T * kPkLd<DP>;
+  const int h = blockIdx.y, hk = h / a.group, q0 = s.tile * PK_T;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  pk_load<T, DP>(sQ, a.q, s, q0, h, a.dim);
+  float o[4][DP / 16] = {}, m[4], l[4] = {};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m[i] = -INFINITY;
+  const int end = a.causal ? min(s.len, q0 + PK_T) : s.len;
+  for (int k0 = 0; k0 < end; k0 += PK_T) {
+    __syncthreads();
+    pk_load<T, DP>(sK, a.k, s, k0, hk, a.dim);
+    pk_load<T, DP>(sV, a.v, s, k0, hk, a.dim);
+    __syncthreads();
+    float acc[4][4] = {};
+    pk_abt<DP>(acc, sQ, sK);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = q0 + 4 * ty + i;
+      float mx = m[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int c = k0 + tx + 16 * j;
+        acc[i][j] = c < s.len && (!a.causal || c <= r) ? acc[i][j] * a.scale : -INFINITY;
+        mx = max_nan(mx, acc[i][j]);
+      }
+#pragma unroll
+      for (int x = 8; x > 0; x >>= 1) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+      // the first tile holds key 0, which every row sees: mx is above -infinity unless the scores are
+      const float base = mx == -INFINITY ? 0.f : mx, f = ex2((m[i] - base) * kLog2e);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float e = ex2((acc[i][j] - base) * kLog2e);
+        sum += e;
+        sP[(4 * ty + i) * PK_LDP + tx + 16 * j] = e;
+      }
+#pragma unroll
+      for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+      l[i] = l[i] * f + sum;
+      m[i] = mx;
+#pragma unroll
+      for (int c = 0; c < DP / 16; ++c) o[i][c] *= f;
+    }
+    __syncthreads();
+    pk_pb<DP>(o, sP, sV);
+  }
+  float inv[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    inv[i] = 1.f / l[i];
+    const int r = q0 + 4 * ty + i;
+    if (a.lse && tx == 0 && r < s.len) a.lse[(int64_t)h * a.tokens + s.begin + r] = m[i] + logf(l[i]);
+  }
+  pk_store<T, DP>(a.o, s, q0, h, a.dim, o, inv);
+}
+
+// delta_i = do_i . o_i, one warp per row and head; rows outside the sequences get a value that nothing reads
+template <typename T>
+__global__ void __launch_bounds__(256) attn_packed_delta_kernel(PackedArgs a) {
+  const int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (i < a.tokens * a.heads) {
+    const int64_t token = i / a.heads;
+    const int h = (int)(i - token * a.heads);
+    const T *x = head_row<T>(a.o, token, h), *y = head_row<T>(a.d_o, token, h);
+    float sum = 0.f;
+    for (int c = lane; c < a.dim; c += 32) sum = fmaf(to_f<T>(x[c]), to_f<T>(y[c]), sum);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) a.delta[(int64_t)h * a.tokens + token] = sum;
+  }
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(PK_THREADS) attn_packed_dq_kernel(PackedArgs a) {
+  const SeqTile s = pk_tile(a);
+  if (s.tile < 0) return;
+  extern __shared__ float sm[];
+  float *sQ = sm, *sO = sQ + PK_T * kPkLd<DP>, *sK = sO + PK_T * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sS = sV + PK_T * kPkLd<DP>;
+  const int h = blockIdx.y, hk = h / a.group, q0 = s.tile * PK_T;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  pk_load<T, DP>(sQ, a.q, s, q0, h, a.dim);
+  pk_load<T, DP>(sO, a.d_o, s, q0, h, a.dim);
+  float lse[4], delta[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = q0 + 4 * ty + i;
+    lse[i] = r < s.len ? a.lse[(int64_t)h * a.tokens + s.begin + r] : 0.f;
+    delta[i] = r < s.len ? a.delta[(int64_t)h * a.tokens + s.begin + r] : 0.f;
+  }
+  float dq[4][DP / 16] = {};
+  const int end = a.causal ? min(s.len, q0 + PK_T) : s.len;
+  for (int k0 = 0; k0 < end; k0 += PK_T) {
+    __syncthreads();
+    pk_load<T, DP>(sK, a.k, s, k0, hk, a.dim);
+    pk_load<T, DP>(sV, a.v, s, k0, hk, a.dim);
+    __syncthreads();
+    float acc[4][4] = {}, dp[4][4] = {};
+    pk_abt<DP>(acc, sQ, sK);
+    pk_abt<DP>(dp, sO, sV);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int c = k0 + tx + 16 * j, r = q0 + 4 * ty + i;
+        const float p = ex2((acc[i][j] * a.scale - lse[i]) * kLog2e);
+        sS[(4 * ty + i) * PK_LDP + tx + 16 * j] = c < s.len && r < s.len && (!a.causal || c <= r) ? p * (dp[i][j] - delta[i]) : 0.f;
+      }
+    __syncthreads();
+    pk_pb<DP>(dq, sS, sK);
+  }
+  const float f[4] = {a.scale, a.scale, a.scale, a.scale};
+  pk_store<T, DP>(a.dq, s, q0, h, a.dim, dq, f);
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(PK_THREADS) attn_packed_dkv_kernel(PackedArgs a) {
+  const SeqTile s = pk_tile(a);
+  if (s.tile < 0) return;
+  extern __shared__ float sm[];
+  float *sK = sm, *sV = sK + PK_T * kPkLd<DP>, *sQ = sV + PK_T * kPkLd<DP>, *sO = sQ + PK_T * kPkLd<DP>, *sP = sO + PK_T * kPkLd<DP>,
+        *sS = sP + PK_T * PK_LDP;
+  const int hk = blockIdx.y, k0 = s.tile * PK_T;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  pk_load<T, DP>(sK, a.k, s, k0, hk, a.dim);
+  pk_load<T, DP>(sV, a.v, s, k0, hk, a.dim);
+  float dk[4][DP / 16] = {}, dv[4][DP / 16] = {};
+  for (int h = hk * a.group; h < (hk + 1) * a.group; ++h)
+    for (int q0 = a.causal ? k0 : 0; q0 < s.len; q0 += PK_T) {
+      __syncthreads();
+      pk_load<T, DP>(sQ, a.q, s, q0, h, a.dim);
+      pk_load<T, DP>(sO, a.d_o, s, q0, h, a.dim);
+      __syncthreads();
+      float acc[4][4] = {}, dp[4][4] = {};
+      pk_abt<DP>(acc, sK, sQ);                    // rows: keys, columns: queries
+      pk_abt<DP>(dp, sV, sO);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int r = q0 + tx + 16 * j;
+        const int64_t at = (int64_t)h * a.tokens + s.begin + r;
+        const float lse = r < s.len ? a.lse[at] : 0.f, delta = r < s.len ? a.delta[at] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int c = k0 + 4 * ty + i;
+          const bool in = c < s.len && r < s.len && (!a.causal || c <= r);
+          const float p = in ? ex2((acc[i][j] * a.scale - lse) * kLog2e) : 0.f;
+          sP[(4 * ty + i) * PK_LDP + tx + 16 * j] = p;
+          sS[(4 * ty + i) * PK_LDP + tx + 16 * j] = in ? p * (dp[i][j] - delta) : 0.f;
+        }
+      }
+      __syncthreads();
+      pk_pb<DP>(dv, sP, sO);
+      pk_pb<DP>(dk, sS, sQ);
+    }
+  const float f[4] = {a.scale, a.scale, a.scale, a.scale}, one[4] = {1.f, 1.f, 1.f, 1.f};
+  pk_store<T, DP>(a.dk, s, k0, hk, a.dim, dk, f);
+  pk_store<T, DP>(a.dv, s, k0, hk, a.dim, dv, one);
+}
+
+// raises a kernel's shared-memory limit once per device
+template <typename K> static cudaError_t pk_allow(K kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || dev > 63 || !(done.load(std::memory_order_relaxed) >> dev & 1)) {
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev <= 63) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  return e;
+}
+
+template <typename T, int DP> static cudaError_t pk_forward(const PackedArgs& a, cudaStream_t st) {
+  static std::atomic<uint64_t> done{0};
+  constexpr int smem = pk_smem<DP>(3, 1);
+  const cudaError_t e = pk_allow(attn_packed_fwd_kernel<T, DP>, smem, done);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(attn_packed_fwd_kernel<T, DP>, dim3((unsigned)most_tiles(a.tokens, a.n_seqs, PK_T), a.heads), dim3(PK_THREADS), smem, st, false, a);
+}
+template <typename T, int DP> static cudaError_t pk_backward(const PackedArgs& a, cudaStream_t st) {
+  static std::atomic<uint64_t> done[2];
+  cudaError_t e = pk_allow(attn_packed_dq_kernel<T, DP>, pk_smem<DP>(4, 1), done[0]);
+  if (e == cudaSuccess) e = pk_allow(attn_packed_dkv_kernel<T, DP>, pk_smem<DP>(4, 2), done[1]);
+  const unsigned tiles = (unsigned)most_tiles(a.tokens, a.n_seqs, PK_T);
+  if (e == cudaSuccess) e = launch_pdl(attn_packed_delta_kernel<T>, dim3((unsigned)((a.tokens * a.heads + 7) / 8)), dim3(256), 0, st, false, a);
+  if (e == cudaSuccess) e = launch_pdl(attn_packed_dkv_kernel<T, DP>, dim3(tiles, a.kv_heads), dim3(PK_THREADS), pk_smem<DP>(4, 2), st, false, a);
+  if (e == cudaSuccess) e = launch_pdl(attn_packed_dq_kernel<T, DP>, dim3(tiles, a.heads), dim3(PK_THREADS), pk_smem<DP>(4, 1), st, false, a);
+  return e;
+}
+template <typename T> static cudaError_t pk_run(const PackedArgs& a, bool backward, cudaStream_t st) {
+  if (a.dim <= 32) return backward ? pk_backward<T, 32>(a, st) : pk_forward<T, 32>(a, st);
+  if (a.dim <= 64) return backward ? pk_backward<T, 64>(a, st) : pk_forward<T, 64>(a, st);
+  return backward ? pk_backward<T, 128>(a, st) : pk_forward<T, 128>(a, st);
+}
+
+static pm_status pk_check(const pm_attention_desc* d) {
+  if (!d) return ops_fail(PM_ERR_INVALID_ARG, "null argument");
+  if (d->dtype != PM_F32 && d->dtype != PM_BF16) return ops_fail(PM_ERR_INVALID_ARG, "unknown element type");
+  if (d->n_heads < 1 || d->n_kv_heads < 1 || d->n_heads % d->n_kv_heads) return ops_fail(PM_ERR_INVALID_ARG, "n_heads must be a positive multiple of n_kv_heads");
+  if (d->n_heads > 65535) return ops_fail(PM_ERR_SHAPE, "at most 65535 heads");
+  if (d->head_dim < 1) return ops_fail(PM_ERR_INVALID_ARG, "head_dim must be positive");
+  if (d->head_dim > 128) return ops_fail(PM_ERR_UNSUPPORTED, "heads wider than 128");
+  if (d->n_seqs < 0 || d->n_tokens < 0) return ops_fail(PM_ERR_INVALID_ARG, "negative size");
+  if (d->n_tokens > 0x7fffffff - 128 || d->n_seqs > (1 << 24) || d->n_tokens * d->n_heads > ((int64_t)1 << 33))
+    return ops_fail(PM_ERR_SHAPE, "too many tokens, sequences or rows");
+  if (!(d->scale > 0) || d->scale > 3e38f) return ops_fail(PM_ERR_INVALID_ARG, "scale must be positive and finite");
+  return PM_OK;
+}
+static pm_status pk_view(HeadView& out, const pm_head_view* v, const char* name, int size) {
+  if (!v || !v->data) return ops_fail(PM_ERR_INVALID_ARG, "%s: null pointer", name);
+  if (!aligned_to(v->data, size)) return ops_fail(PM_ERR_INVALID_ARG, "%s: pointer not aligned to its element type", name);
+  if (v->token_stride < 0 || v->head_stride < 0) return ops_fail(PM_ERR_INVALID_ARG, "%s: negative stride", name);
+  out = HeadView{v->data, v->token_stride, v->head_stride};
+  return PM_OK;
+}
+static PackedArgs pk_args(const pm_attention_desc* d, const int32_t* cu, float* lse) {
+  PackedArgs a{};
+  a.cu = cu; a.lse = lse; a.tokens = d->n_tokens; a.n_seqs = d->n_seqs; a.heads = d->n_heads; a.kv_heads = d->n_kv_heads;
+  a.group = d->n_heads / d->n_kv_heads; a.dim = d->head_dim; a.causal = d->causal != 0; a.scale = d->scale;
+  return a;
+}
+
+}  // namespace pm
+
+using namespace pm;
+
+extern "C" {
+
+pm_status pm_attention_packed_forward(const pm_attention_desc* d, const pm_head_view* q, const pm_head_view* k, const pm_head_view* v,
+                                      const int32_t* cu_seqlens, const pm_head_view* o, float* lse, void* stream) {
+  if (const pm_status s = pk_check(d)) return s;
+  if (d->n_tokens == 0 || d->n_seqs == 0) return PM_OK;
+  if (!cu_seqlens) return ops_fail(PM_ERR_INVALID_ARG, "null cu_seqlens");
+  PackedArgs a = pk_args(d, cu_seqlens, lse);
+  const int size = d->dtype == PM_BF16 ? 2 : 4;
+  if (const pm_status s = pk_view(a.q, q, "q", size)) return s;
+  if (const pm_status s = pk_view(a.k, k, "k", size)) return s;
+  if (const pm_status s = pk_view(a.v, v, "v", size)) return s;
+  if (const pm_status s = pk_view(a.o, o, "o", size)) return s;
+  const cudaStream_t st = (cudaStream_t)stream;
+  const cudaError_t e = d->dtype == PM_BF16 ? pk_run<__nv_bfloat16>(a, false, st) : pk_run<float>(a, false, st);
+  return ops_cuda(e, "packed attention");
+}
+
+uint64_t pm_attention_packed_workspace_bytes(const pm_attention_desc* d) {
+  return !d || d->n_heads < 1 || d->n_tokens < 0 ? 0 : (uint64_t)d->n_heads * (uint64_t)d->n_tokens * sizeof(float);
+}
+
+pm_status pm_attention_packed_backward(const pm_attention_desc* d, const pm_head_view* q, const pm_head_view* k, const pm_head_view* v,
+                                       const pm_head_view* o, const float* lse, const pm_head_view* d_o, const int32_t* cu_seqlens,
+                                       const pm_head_view* dq, const pm_head_view* dk, const pm_head_view* dv, void* workspace,
+                                       uint64_t workspace_bytes, void* stream) {
+  if (const pm_status s = pk_check(d)) return s;
+  if (d->n_tokens == 0 || d->n_seqs == 0) return PM_OK;
+  if (!cu_seqlens || !lse) return ops_fail(PM_ERR_INVALID_ARG, "null cu_seqlens or lse");
+  PackedArgs a = pk_args(d, cu_seqlens, const_cast<float*>(lse));
+  const int size = d->dtype == PM_BF16 ? 2 : 4;
+  if (const pm_status s = pk_view(a.q, q, "q", size)) return s;
+  if (const pm_status s = pk_view(a.k, k, "k", size)) return s;
+  if (const pm_status s = pk_view(a.v, v, "v", size)) return s;
+  if (const pm_status s = pk_view(a.o, o, "o", size)) return s;
+  if (const pm_status s = pk_view(a.d_o, d_o, "d_o", size)) return s;
+  if (const pm_status s = pk_view(a.dq, dq, "dq", size)) return s;
+  if (const pm_status s = pk_view(a.dk, dk, "dk", size)) return s;
+  if (const pm_status s = pk_view(a.dv, dv, "dv", size)) return s;
+  const uint64_t need = pm_attention_packed_workspace_bytes(d);
+  if (!workspace || workspace_bytes < need) return ops_fail(PM_ERR_NOMEM, "workspace too small: need %llu bytes", (unsigned long long)need);
+  if (!aligned_to(workspace, 4)) return ops_fail(PM_ERR_INVALID_ARG, "workspace must be 4-byte aligned");
+  a.delta = static_cast<float*>(workspace);
+  const cudaStream_t st = (cudaStream_t)stream;
+  const cudaError_t e = d->dtype == PM_BF16 ? pk_run<__nv_bfloat16>(a, true, st) : pk_run<float>(a, true, st);
+  return ops_cuda(e, "packed attention backward");
+}
+
+}  // extern "C"

@@ -1,0 +1,82 @@
+// Attention over packed sequences: arguments and the map from a block to its tile of a sequence.
+#pragma once
+#include "pm_ops.cuh"
+
+namespace pm {
+
+struct HeadView {
+  const void* data;
+  int64_t token, head;                            // strides in elements
+};
+struct PackedArgs {
+  HeadView q, k, v, o, d_o, dq, dk, dv;           // o is written by the forward pass, dq, dk, dv by the backward pass
+  const int32_t* cu;                              // [n_seqs + 1]
+  float *lse, *delta;                             // [heads][tokens]
+  int64_t tokens;
+  int n_seqs, heads, kv_heads, group, dim, causal;
+  float scale;
+};
+
+template <typename T> __device__ __forceinline__ const T* head_row(const HeadView& x, int64_t token, int head) {
+  return static_cast<const T*>(x.data) + token * x.token + (int64_t)head * x.head;
+}
+template <typename T> __device__ __forceinline__ T* head_row_out(const HeadView& x, int64_t token, int head) {
+  return const_cast<T*>(head_row<T>(x, token, head));
+}
+
+struct SeqTile {
+  int64_t begin;                                  // first token of the sequence
+  int len, tile;                                  // its length; the tile's index inside it (-1: no such tile)
+};
+
+// The index-th tile of `rows` rows, counted through the sequences; called by a whole warp, same result in every lane.  A lane takes
+// eight consecutive sequences, so up to 256 cost one round of loads.  Starts are clipped to 0 .. tokens and a sequence that
+// would end before it starts is empty: whatever the array holds, no tile reaches outside the tensors.
+__device__ __forceinline__ SeqTile find_tile(const int32_t* cu, int n_seqs, int64_t tokens, int index, int rows) {
+  const int lane = threadIdx.x & 31;
+  int before = 0;
+  for (int base = 0; base < n_seqs; base += 256) {
+    int64_t start[9];
+    int tiles[8], mine = 0;
+#pragma unroll
+    for (int i = 0; i < 9; ++i) {
+      const int at = min(base + lane * 8 + i, n_seqs);
+      const int64_t c = cu[at];
+      start[i] = c < 0 ? 0 : c > tokens ? tokens : c;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t len = start[i + 1] - start[i];
+      tiles[i] = len > 0 ? (int)((len + rows - 1) / rows) : 0;
+      mine += tiles[i];
+    }
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) { const int v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
+    const int first = before + upto - mine;
+    const unsigned has = __ballot_sync(0xffffffffu, index >= first && index < first + mine);
+    if (has) {
+      int at = first, tile = -1, len = 0;
+      int64_t begin = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (tile < 0 && index >= at && index < at + tiles[i]) { tile = index - at; begin = start[i]; len = (int)(start[i + 1] - start[i]); }
+        at += tiles[i];
+      }
+      const int who = __ffs(has) - 1;
+      return SeqTile{__shfl_sync(0xffffffffu, begin, who), __shfl_sync(0xffffffffu, len, who), __shfl_sync(0xffffffffu, tile, who)};
+    }
+    before += __shfl_sync(0xffffffffu, upto, 31);
+  }
+  return SeqTile{0, 0, -1};
+}
+
+// tiles of `rows` rows that sequences of `tokens` tokens in all can have at most
+inline int64_t most_tiles(int64_t tokens, int n_seqs, int rows) { return tokens / rows + n_seqs; }
+
+// launchers of the tensor-core kernels
+bool attn_packed_tc_takes(const PackedArgs& a, int dtype, bool backward);
+cudaError_t attn_packed_tc_forward(const PackedArgs& a, cudaStream_t st);
+cudaError_t attn_packed_tc_backward(const PackedArgs& a, cudaStream_t st);
+
+}  // namespace pm

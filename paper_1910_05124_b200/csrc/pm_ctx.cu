@@ -1,6 +1,7 @@
 // Host side of the C ABI: layout arithmetic, context set-up, and the launch sequence of a tick.
 #include <functional>
 #include <cmath>
+#include <cstdarg>
 #include <cstdio>
 #include <cstring>
 #include <string>
@@ -9,6 +10,7 @@
 #include "pm_tick.cuh"
 #include "pm_update.cuh"
 #include "pm_umma.cuh"
+#include "pm_ops.cuh"
 
 namespace pm {
 pm_status attn_plan_create(AttnPlan** out, const TickArgs& t, const std::vector<StageDev>& st, void* ws_region, cudaStream_t stream, std::string& err);
@@ -587,6 +589,18 @@ pm_status cuda_fail(pm_ctx* ctx, cudaError_t e, const char* what) {
   return fail(ctx, PM_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
 }
 }  // namespace
+
+namespace pm {
+pm_status ops_fail(pm_status s, const char* format, ...) noexcept {
+  char text[256];
+  va_list args;
+  va_start(args, format);
+  vsnprintf(text, sizeof(text), format, args);
+  va_end(args);
+  try { g_error = text; } catch (...) {}                 // out of memory: the status alone tells
+  return s;
+}
+}  // namespace pm
 
 extern "C" {
 

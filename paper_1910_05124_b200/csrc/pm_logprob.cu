@@ -1,0 +1,462 @@
+// Log probabilities of given tokens, the distribution's entropy and its most likely alternatives, and their gradient.
+//
+//   lse = m + log sum e^(x - m),   logprob = x_y - lse,   H = log sum e^(x - m) - sum (x - m) e^(x - m) / sum e^(x - m)
+//   dx_j = g_l ([j = y] - p_j) - g_H p_j (log p_j + H),   p_j = e^(x_j - lse)
+//
+// Forward: one pass over the logits.  A thread keeps the running maximum of its elements and the two sums relative to it; the
+// threads' triples are joined at the end.  A row belongs to a cluster of 1, 2, 4 or 8 blocks that join through distributed shared
+// memory, so that a few long rows still occupy the GPU and nothing needs a workspace.  Bound by memory (one read).
+//
+// The alternatives cost one comparison per element, the maximum that the softmax needs anyway: the k-th largest of 32 maxima
+// over disjoint parts of the segment is a value that at least k elements reach, so only threads whose own maximum reaches it read
+// their elements again (from L2) and list those that do; the list, a few dozen entries, is ranked by counting.  Rows with so many
+// equal values that the list overflows take k passes over the segment instead.
+#include <cfloat>
+
+#include <cooperative_groups.h>
+
+#include "pm_ops.cuh"
+
+namespace pm {
+namespace cg = cooperative_groups;
+
+constexpr int kLpThreads = 256;
+constexpr int kLpWarps = kLpThreads / 32;
+constexpr int kLpMaxK = 32;
+constexpr int kLpList = 512;                      // candidates; about k (1 + log(32 / (32 - k))) are expected, 130 for k = 32
+constexpr int kLpMaxCluster = 8;
+
+struct LogprobArgs {
+  const void* logits;
+  int64_t rows, row_stride;
+  int vocab, top_k;
+  const int32_t* targets;
+  float *logprob, *entropy, *lse, *top_logprob;
+  int32_t* top_ids;
+};
+
+template <typename T> struct Vec { static constexpr int n = 16 / sizeof(T); };
+
+__device__ __forceinline__ void unpack16(const uint4& q, float (&v)[4]) {
+  v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y); v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
+}
+__device__ __forceinline__ void unpack16(const uint4& q, float (&v)[8]) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+}
+
+// A row as 16-byte vectors at 16-byte boundaries: vector j holds elements j * n - shift ...; the first and the last may reach over the
+// row's ends, where they are put together from single elements (-infinity outside).
+template <typename T> struct RowVectors {
+  const T* row;
+  int vocab, shift, count;
+  __device__ __forceinline__ RowVectors(const T* r, int v) : row(r), vocab(v) {
+    shift = (int)((reinterpret_cast<uintptr_t>(r) & 15) / sizeof(T));
+    count = (v + shift + Vec<T>::n - 1) / Vec<T>::n;
+  }
+  __device__ __forceinline__ int first(int j) const { return j * Vec<T>::n - shift; }
+  __device__ __forceinline__ bool whole(int j) const { return first(j) >= 0 && first(j) + Vec<T>::n <= vocab; }
+  __device__ __forceinline__ uint4 load(int j) const { return *reinterpret_cast<const uint4*>(row + first(j)); }
+  __device__ __forceinline__ void get(int j, float (&v)[Vec<T>::n]) const {
+    if (whole(j)) { unpack16(load(j), v); return; }
+#pragma unroll
+    for (int i = 0; i < Vec<T>::n; ++i) { const int at = first(j) + i; v[i] = at >= 0 && at < vocab ? to_f<T>(row[at]) : -INFINITY; }
+  }
+};
+
+struct Sums { float m, s, t; };
+// the sums relative to another maximum (never below the own one); a maximum of -infinity has empty sums
+__device__ __forceinline__ void rebase(Sums& a, float m) {
+  if (a.m == m || a.m == -INFINITY) { a.m = m; return; }
+  const float d = fmaxf(a.m - m, -200.f), f = ex2(d * kLog2e);
+  a.t = f * (a.t + d * a.s);                      // sum (x - m') e^(x - m') from sum (x - m) e^(x - m)
+  a.s *= f;
+  a.m = m;
+}
+__device__ __forceinline__ Sums join(Sums a, Sums b) {
+  const float m = max_nan(a.m, b.m);
+  rebase(a, m); rebase(b, m);
+  return Sums{m, a.s + b.s, a.t + b.t};
+}
+__device__ __forceinline__ bool beats(float v, int id, float w, int other) { return v > w || (v == w && id < other); }
+
+struct LpShared {
+  Sums warp[kLpWarps];
+  Sums block;                                     // read by the cluster
+  float lane_max[kLpWarps][32];
+  float threshold;
+  int n_list;
+  float list_v[kLpList];
+  int list_id[kLpList];
+  float top_v[kLpMaxK];                           // this block's best, in order; read by the cluster
+  int top_id[kLpMaxK];
+  float all_v[kLpMaxCluster * kLpMaxK];
+  int all_id[kLpMaxCluster * kLpMaxK];
+};
+
+// The k best of the block's vectors [j0, j1) in order into sh.top_*: value descending, then index ascending.  `mine` is the largest
+// value of the thread's own vectors j0 + threadIdx.x, + kLpThreads, ...  Missing entries are (-infinity, vocab).
+template <typename T> __device__ void block_top(LpShared& sh, const RowVectors<T>& x, int j0, int j1, int k, float mine) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  sh.lane_max[warp][lane] = mine;
+  if (tid == 0) sh.n_list = 0;
+  if (tid < kLpMaxK) { sh.top_v[tid] = -INFINITY; sh.top_id[tid] = x.vocab; }
+  __syncthreads();
+  if (warp == 0) {
+    float v = sh.lane_max[0][lane];
+#pragma unroll
+    for (int w = 1; w < kLpWarps; ++w) v = fmaxf(v, sh.lane_max[w][lane]);
+    // bitonic sort over the lanes, descending
+#pragma unroll
+    for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+      for (int step = size / 2; step > 0; step /= 2) {
+        const float o = __shfl_xor_sync(0xffffffffu, v, step);
+        const bool down = (lane & size) == 0, low = (lane & step) == 0;
+        v = down == low ? fmaxf(v, o) : fminf(v, o);
+      }
+    const float th = __shfl_sync(0xffffffffu, v, k - 1);
+    if (lane == 0) sh.threshold = th;
+  }
+  __syncthreads();
+  const float th = sh.threshold;
+  // the vectors of each thread that reaches the threshold, read again by its whole warp
+  unsigned hit = __ballot_sync(0xffffffffu, mine >= th);
+  while (hit) {
+    const int who = __ffs(hit) - 1;
+    hit &= hit - 1;
+    for (int j = j0 + warp * 32 + who + lane * kLpThreads; j < j1; j += 32 * kLpThreads) {
+      float v[Vec<T>::n];
+      x.get(j, v);
+#pragma unroll
+      for (int i = 0; i < Vec<T>::n; ++i) {
+        const int id = x.first(j) + i;
+        if (v[i] >= th && id >= 0 && id < x.vocab) {
+          const int at = atomicAdd(&sh.n_list, 1);
+          if (at < kLpList) { sh.list_v[at] = v[i]; sh.list_id[at] = id; }
+        }
+      }
+    }
+  }
+  __syncthreads();
+  const int n = sh.n_list;
+  if (n <= kLpList) {
+    for (int a = tid; a < n; a += kLpThreads) {
+      const float v = sh.list_v[a];
+      const int id = sh.list_id[a];
+      int rank = 0;
+      for (int b = 0; b < n; ++b) rank += beats(sh.list_v[b], sh.list_id[b], v, id);
+      if (rank < k) { sh.top_v[rank] = v; sh.top_id[rank] = id; }
+    }
+    __syncthreads();
+    return;
+  }
+  float last_v = INFINITY;
+  int last_id = -1;
+  for (int r = 0; r < k; ++r) {                    // the best of what comes after the last one found
+    float bv = -INFINITY;
+    int bid = x.vocab;
+    for (int j = j0 + tid; j < j1; j += kLpThreads) {
+      float v[Vec<T>::n];
+      x.get(j, v);
+#pragma unroll
+      for (int i = 0; i < Vec<T>::n; ++i) {
+        const int id = x.first(j) + i;
+        if (id >= 0 && id < x.vocab && beats(last_v, last_id, v[i], id) && beats(v[i], id, bv, bid)) { bv = v[i]; bid = id; }
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const float ov = __shfl_xor_sync(0xffffffffu, bv, o);
+      const int oid = __shfl_xor_sync(0xffffffffu, bid, o);
+      if (beats(ov, oid, bv, bid)) { bv = ov; bid = oid; }
+    }
+    if (lane == 0) { sh.list_v[warp] = bv; sh.list_id[warp] = bid; }
+    __syncthreads();
+    bv = sh.list_v[0]; bid = sh.list_id[0];
+    for (int w = 1; w < kLpWarps; ++w) if (beats(sh.list_v[w], sh.list_id[w], bv, bid)) { bv = sh.list_v[w]; bid = sh.list_id[w]; }
+    if (tid == 0) { sh.top_v[r] = bv; sh.top_id[r] = bid; }
+    last_v = bv; last_id = bid;
+    __syncthreads();
+  }
+}
+
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(kLpThreads, 4) logprob_kernel(LogprobArgs a) {
+  __shared__ LpShared sh;
+  constexpr int N = Vec<T>::n, kUnroll = 4;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
+  const int64_t row = blockIdx.x / parts;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const RowVectors<T> x(static_cast<const T*>(a.logits) + row * a.row_stride, a.vocab);
+  const int j0 = (int)((int64_t)x.count * part / parts), j1 = (int)((int64_t)x.count * (part + 1) / parts);
+
+  Sums st{-INFINITY, 0.f, 0.f};
+  auto take = [&](const float* v, int n) {
+    float m = st.m;
+    for (int i = 0; i < n; ++i) m = max_nan(m, v[i]);
+    if (m != st.m) rebase(st, m);
+    const float base = m == -INFINITY ? 0.f : m;
+    for (int i = 0; i < n; ++i) {
+      const float d = fmaxf(v[i] - base, -200.f), e = ex2(d * kLog2e);   // at -200 the exponential is zero and the product too
+      st.s += e;
+      st.t = fmaf(e, d, st.t);
+    }
+  };
+  int j = j0 + tid;
+  for (; j + (kUnroll - 1) * kLpThreads < j1 && x.whole(j) && x.whole(j + (kUnroll - 1) * kLpThreads); j += kUnroll * kLpThreads) {
+    uint4 q[kUnroll];
+    float v[kUnroll][N];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) q[u] = x.load(j + u * kLpThreads);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) unpack16(q[u], v[u]);
+    float m = st.m;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int i = 0; i < N; ++i) m = max_nan(m, v[u][i]);
+    if (m != st.m) rebase(st, m);
+    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float d = fmaxf(v[u][i] - base, -200.f), e = ex2(d * kLog2e);   // at -200 the exponential is zero and the product too
+        st.s += e;
+        st.t = fmaf(e, d, st.t);
+      }
+  }
+  for (; j < j1; j += kLpThreads) {
+    float v[N];
+    x.get(j, v);
+    take(v, N);
+  }
+  const float mine = st.m;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    Sums b{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), __shfl_xor_sync(0xffffffffu, st.t, o)};
+    st = lane & o ? join(b, st) : join(st, b);
+  }
+  if (lane == 0) sh.warp[tid >> 5] = st;
+  __syncthreads();
+  if (tid == 0) {
+    st = sh.warp[0];
+    for (int w = 1; w < kLpWarps; ++w) st = join(st, sh.warp[w]);
+    sh.block = st;
+  }
+  if (TOP) block_top(sh, x, j0, j1, a.top_k, mine);
+  if (parts > 1) cluster.sync(); else __syncthreads();
+  if (part == 0) {
+    st = sh.block;
+    for (int c = 1; c < parts; ++c) st = join(st, *cluster.map_shared_rank(&sh.block, c));
+    const bool none = !(st.m < INFINITY);         // a NaN or +infinity in the row: no distribution
+    const bool empty = st.m == -INFINITY;         // nothing but -infinity
+    const float log_s = logf(st.s);
+    if (tid == 0) {
+      if (a.lse) a.lse[row] = none ? NAN : empty ? -INFINITY : st.m + log_s;
+      if (a.entropy) a.entropy[row] = none ? NAN : empty ? 0.f : log_s - st.t / st.s;
+      if (a.targets) {
+        const int y = a.targets[row];
+        float lp = 0.f;
+        if (y >= a.vocab) lp = NAN;
+        else if (y >= 0) lp = none ? NAN : empty ? -INFINITY : (to_f<T>(x.row[y]) - st.m) - log_s;
+        a.logprob[row] = lp;
+      }
+    }
+    if (TOP) {
+      const int k = a.top_k, n = parts * k;
+      const float* bv = sh.top_v;
+      const int* bid = sh.top_id;
+      if (parts > 1) {
+        for (int i = tid; i < n; i += kLpThreads) {
+          sh.all_v[i] = cluster.map_shared_rank(sh.top_v, i / k)[i % k];
+          sh.all_id[i] = cluster.map_shared_rank(sh.top_id, i / k)[i % k];
+        }
+        __syncthreads();
+        bv = sh.all_v; bid = sh.all_id;
+      }
+      for (int i = tid; i < n; i += kLpThreads) {
+        int rank = 0;
+        // entries of blocks with fewer than k elements are equal among themselves and come behind every element
+        for (int b = 0; b < n; ++b) rank += beats(bv[b], bid[b], bv[i], bid[i]);
+        if (!none && rank < k && bid[i] < a.vocab) {
+          a.top_logprob[row * k + rank] = empty ? -INFINITY : (bv[i] - st.m) - log_s;
+          a.top_ids[row * k + rank] = bid[i];
+        }
+      }
+      if (none && tid < k) { a.top_logprob[row * k + tid] = NAN; a.top_ids[row * k + tid] = -1; }
+    }
+  }
+  if (parts > 1) cluster.sync();                  // the first block has read the others' shared memory
+}
+
+struct LogprobBwdArgs {
+  const void* logits;
+  int64_t row_stride, grad_stride;
+  int vocab, per_row;                             // blocks per row
+  const int32_t* targets;
+  const float *lse, *entropy, *d_logprob, *d_entropy;
+  void* d_logits;
+};
+
+constexpr int kLbVectors = 4;                     // 16-byte vectors per thread
+
+// An lse beyond this magnitude no longer resolves log p (its rounding alone is 2^-13 and more), as in a row whose every logit is a
+// mask's lowest value.  Such a row is left to one block, which takes the maximum and the sum from the logits again.
+constexpr float kLseCoarse = 4096.f;
+
+__device__ __forceinline__ float logit_grad(float lp, float gl, float gh, float h) {
+  lp = max_nan(lp, -200.f);                       // where p underflows the product below is zero
+  return -ex2(lp * kLog2e) * fmaf(gh, lp + h, gl);
+}
+
+template <typename T> __device__ __noinline__ void coarse_row(const T* in, T* out, int vocab, int y, float gl, float gh, float h) {
+  __shared__ Sums warp_sums[kLpWarps];
+  Sums st{-INFINITY, 0.f, 0.f};
+  for (int i = threadIdx.x; i < vocab; i += kLpThreads) st = join(st, Sums{to_f<T>(in[i]), 1.f, 0.f});
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const Sums b{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), 0.f};
+    st = threadIdx.x & o ? join(b, st) : join(st, b);
+  }
+  if ((threadIdx.x & 31) == 0) warp_sums[threadIdx.x >> 5] = st;
+  __syncthreads();
+  st = warp_sums[0];
+  for (int w = 1; w < kLpWarps; ++w) st = join(st, warp_sums[w]);
+  const float log_s = logf(st.s);
+  for (int i = threadIdx.x; i < vocab; i += kLpThreads)
+    out[i] = from_f<T>(logit_grad((to_f<T>(in[i]) - st.m) - log_s, gl, gh, h) + (i == y ? gl : 0.f));
+}
+
+// One read, one write: dx_j = -p_j (g_l + g_H (log p_j + H)), plus g_l at the target.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kLpThreads) logprob_bwd_kernel(LogprobBwdArgs a) {
+  constexpr int N = Vec<T>::n;
+  const int64_t row = blockIdx.x / a.per_row;
+  const int part = (int)(blockIdx.x - row * a.per_row);
+  const T* in = static_cast<const T*>(a.logits) + row * a.row_stride;
+  T* out = static_cast<T*>(a.d_logits) + row * a.grad_stride;
+  const float lse = a.lse[row];
+  const int y = a.targets ? a.targets[row] : -1;
+  float gl = a.d_logprob && y >= 0 ? a.d_logprob[row] : 0.f;
+  if (a.d_logprob && y >= a.vocab) gl = NAN;
+  const float gh = a.d_entropy ? a.d_entropy[row] : 0.f, h = a.d_entropy ? a.entropy[row] : 0.f;
+  const bool empty = lse == -INFINITY;
+  if (fabsf(lse) > kLseCoarse && !empty) {
+    if (part == 0) coarse_row(in, out, a.vocab, y, gl, gh, h);
+    return;
+  }
+  auto grad = [&](float v, int at) { return empty ? 0.f : logit_grad(v - lse, gl, gh, h) + (at == y ? gl : 0.f); };
+  if (VEC) {
+    const RowVectors<T> x(in, a.vocab);
+    const int j0 = part * kLbVectors * kLpThreads + threadIdx.x;
+    uint4 q[kLbVectors];
+#pragma unroll
+    for (int u = 0; u < kLbVectors; ++u) {
+      const int j = j0 + u * kLpThreads;
+      if (j < x.count && x.whole(j)) q[u] = x.load(j);
+    }
+#pragma unroll
+    for (int u = 0; u < kLbVectors; ++u) {
+      const int j = j0 + u * kLpThreads;
+      if (j >= x.count) break;
+      const int at = x.first(j);
+      if (x.whole(j)) {
+        float v[N];
+        unpack16(q[u], v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = grad(v[i], at + i);
+        uint4 w;
+        if constexpr (N == 4) {
+          w = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        } else {
+          uint32_t p[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            p[i] = *reinterpret_cast<const uint32_t*>(&b);
+          }
+          w = make_uint4(p[0], p[1], p[2], p[3]);
+        }
+        *reinterpret_cast<uint4*>(out + at) = w;
+      } else {
+        for (int i = 0; i < N; ++i)
+          if (at + i >= 0 && at + i < a.vocab) out[at + i] = from_f<T>(grad(to_f<T>(in[at + i]), at + i));
+      }
+    }
+  } else {
+    const int e1 = min(a.vocab, (part + 1) * kLbVectors * kLpThreads * N);
+    for (int i = part * kLbVectors * kLpThreads * N + threadIdx.x; i < e1; i += kLpThreads) out[i] = from_f<T>(grad(to_f<T>(in[i]), i));
+  }
+}
+
+template <typename T> static cudaError_t logprob_launch(const LogprobArgs& a, int parts, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(a.rows * parts)); cfg.blockDim = dim3(kLpThreads); cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return a.top_k ? cudaLaunchKernelEx(&cfg, logprob_kernel<T, true>, a) : cudaLaunchKernelEx(&cfg, logprob_kernel<T, false>, a);
+}
+
+static pm_status logprob_shape(int32_t dtype, int64_t rows, int32_t vocab, int64_t row_stride, const void* logits) {
+  if (dtype != PM_F32 && dtype != PM_BF16) return ops_fail(PM_ERR_INVALID_ARG, "unknown element type");
+  if (rows < 0 || vocab < 1) return ops_fail(PM_ERR_INVALID_ARG, "rows must be >= 0 and vocab positive");
+  if (rows > (1 << 24) || vocab > (1 << 24)) return ops_fail(PM_ERR_SHAPE, "at most 2^24 rows and 2^24 tokens of vocabulary");
+  if (row_stride < vocab) return ops_fail(PM_ERR_INVALID_ARG, "row stride below the vocabulary size");
+  if (!aligned_to(logits, dtype == PM_BF16 ? 2 : 4)) return ops_fail(PM_ERR_INVALID_ARG, "pointer not aligned to its element type");
+  return PM_OK;
+}
+
+}  // namespace pm
+
+using namespace pm;
+
+extern "C" {
+
+pm_status pm_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t vocab, int64_t row_stride, const int32_t* targets,
+                            float* logprob, float* entropy, float* lse, int32_t top_k, float* top_logprob, int32_t* top_ids, void* stream) {
+  if (const pm_status s = logprob_shape(dtype, rows, vocab, row_stride, logits)) return s;
+  if (rows == 0) return PM_OK;
+  if (!logits) return ops_fail(PM_ERR_INVALID_ARG, "null logits");
+  if ((targets == nullptr) != (logprob == nullptr)) return ops_fail(PM_ERR_INVALID_ARG, "targets and logprob are given together or not at all");
+  if (top_k < 0 || top_k > kLpMaxK || top_k > vocab) return ops_fail(PM_ERR_INVALID_ARG, "top_k must be 0 to 32 and at most the vocabulary size");
+  if (top_k > 0 && (!top_logprob || !top_ids)) return ops_fail(PM_ERR_INVALID_ARG, "top_k without a place for the alternatives");
+  // A cluster per row once the rows leave SMs without work, as long as each block keeps some vectors per thread.
+  const int vectors = vocab / (dtype == PM_BF16 ? 8 : 4);
+  int parts = 1;
+  while (parts < kLpMaxCluster && rows * parts * 2 <= 2 * kSms && vectors / (parts * 2) >= 2 * kLpThreads) parts *= 2;
+  const LogprobArgs a{logits, rows, row_stride, vocab, top_k, targets, logprob, entropy, lse, top_logprob, top_ids};
+  const cudaError_t e = dtype == PM_BF16 ? logprob_launch<__nv_bfloat16>(a, parts, (cudaStream_t)stream) : logprob_launch<float>(a, parts, (cudaStream_t)stream);
+  return ops_cuda(e, "token log probabilities");
+}
+
+pm_status pm_token_logprobs_backward(const void* logits, int32_t dtype, int64_t rows, int32_t vocab, int64_t row_stride, const int32_t* targets,
+                                     const float* lse, const float* entropy, const float* d_logprob, const float* d_entropy, void* d_logits,
+                                     int64_t grad_stride, void* stream) {
+  if (const pm_status s = logprob_shape(dtype, rows, vocab, row_stride, logits)) return s;
+  if (const pm_status s = logprob_shape(dtype, rows, vocab, grad_stride, d_logits)) return s;
+  if (!d_logprob && !d_entropy) return ops_fail(PM_ERR_INVALID_ARG, "neither a gradient of logprob nor one of the entropy");
+  if (rows == 0) return PM_OK;
+  if (!logits || !lse || !d_logits) return ops_fail(PM_ERR_INVALID_ARG, "null argument");
+  if (d_logprob && !targets) return ops_fail(PM_ERR_INVALID_ARG, "a gradient of logprob needs the targets");
+  if (d_entropy && !entropy) return ops_fail(PM_ERR_INVALID_ARG, "a gradient of the entropy needs the entropy");
+  const int size = dtype == PM_BF16 ? 2 : 4, per_block = kLbVectors * kLpThreads * 16 / size;
+  // both rows at the same place within their 16-byte blocks, in every row: vectors; else single elements
+  const bool vec = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(d_logits)) & 15) == 0 &&
+                   ((row_stride - grad_stride) * size) % 16 == 0;
+  const int per_row = (vocab + 16 / size - 1 + per_block - 1) / per_block;
+  const LogprobBwdArgs a{logits, row_stride, grad_stride, vocab, per_row, d_logprob ? targets : nullptr, lse, entropy, d_logprob, d_entropy, d_logits};
+  const dim3 grid((unsigned)(rows * per_row)), block(kLpThreads);
+  if ((int64_t)rows * per_row > 0x7fffffff) return ops_fail(PM_ERR_SHAPE, "more than 2^31 blocks");
+  void (*kernel)(LogprobBwdArgs) = dtype == PM_BF16 ? (vec ? logprob_bwd_kernel<__nv_bfloat16, true> : logprob_bwd_kernel<__nv_bfloat16, false>)
+                                                    : (vec ? logprob_bwd_kernel<float, true> : logprob_bwd_kernel<float, false>);
+  return ops_cuda(launch_pdl(kernel, grid, block, 0, (cudaStream_t)stream, false, a), "gradient of the log probabilities");
+}
+
+}  // extern "C"

@@ -1,0 +1,263 @@
+"""Operators for programs with their own forward and backward pass, next to `FlatUpdate`: attention over packed sequences,
+log probabilities of given tokens, and gradient clipping.  Argument checks and marshalling only; the tensors belong to the
+caller, outputs included.
+
+Every call is asynchronous on `stream` (default: the current stream of the tensors' device) and may be captured into a CUDA
+graph.  As with any CUDA call, a tensor that another stream still writes has to be waited for by the caller.  Refused
+arguments raise PipeMareError.
+"""
+import ctypes as C
+import math
+
+import torch
+
+from .binding import (PM_BF16, PM_F32, PipeMareError, _check, lib, pm_attention_desc, pm_head_view, pm_tensor_pair)
+
+_DTYPES = {torch.float32: PM_F32, torch.bfloat16: PM_BF16}
+
+
+def _refuse(message, status="PM_ERR_INVALID_ARG"):
+    raise PipeMareError(status, message)
+
+
+def _tensor(name, t, dtype, device, shape=None):
+    if not isinstance(t, torch.Tensor):
+        _refuse(f"{name} must be a tensor")
+    if t.device != device:
+        _refuse(f"{name} is on {t.device}, expected {device}")
+    if t.dtype != dtype:
+        _refuse(f"{name} is {t.dtype}, expected {dtype}")
+    if shape is not None and tuple(t.shape) != shape:
+        _refuse(f"{name} has shape {tuple(t.shape)}, expected {shape}", "PM_ERR_SHAPE")
+    return t
+
+
+def _flat(name, t, dtype, device, shape):
+    """Data pointer of a contiguous tensor; None for None."""
+    if t is None:
+        return None
+    if not _tensor(name, t, dtype, device, shape).is_contiguous():
+        _refuse(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _compute_device(name, t):
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        _refuse(f"{name} must be a CUDA tensor")
+    if t.dtype not in _DTYPES:
+        _refuse(f"{name} is {t.dtype}; float32 and bfloat16 are supported", "PM_ERR_UNSUPPORTED")
+    return t.device
+
+
+class _Launch:
+    """The stream of a call, with its device current while the call lasts."""
+
+    def __init__(self, device, stream):
+        if stream is not None and stream.device != device:
+            _refuse(f"the stream belongs to {stream.device}, the tensors to {device}")
+        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
+        self.other = device.index != torch.cuda.current_device()
+        self.guard = torch.cuda.device(device) if self.other else None
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return C.c_void_p(self.stream.cuda_stream)
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+    def workspace(self, n_bytes, device):
+        """Device scratch of this call alone: from the allocator's pool of the launching stream, so that the memory is reused only
+        by work queued behind the call (or, under capture, stays with the graph)."""
+        if self.stream == torch.cuda.current_stream(device):
+            return torch.empty(max(n_bytes, 16), dtype=torch.uint8, device=device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(max(n_bytes, 16), dtype=torch.uint8, device=device)
+
+
+class PackedAttention:
+    """Attention over sequences of different lengths laid end to end, with shared key/value heads.
+
+    q, o: [tokens, n_heads, head_dim]; k, v: [tokens, n_kv_heads, head_dim]; all float32 or all bfloat16, the last dimension
+    contiguous, the others at any stride (q, k and v may be views of one projection's output).  cu_seqlens: int32
+    [sequences + 1] on the device, ascending; sequence b is tokens cu_seqlens[b] to cu_seqlens[b + 1] - 1, and tokens outside
+    all sequences are neither used nor written.  lse: float32 [n_heads, tokens].  head_dim up to 128.
+    """
+
+    def __init__(self, n_heads, n_kv_heads, head_dim, *, causal=True, scale=None):
+        if n_heads < 1 or n_kv_heads < 1 or n_heads % n_kv_heads:
+            _refuse("n_heads must be a positive multiple of n_kv_heads")
+        if head_dim < 1:
+            _refuse("head_dim must be positive")
+        if head_dim > 128:
+            _refuse("heads wider than 128", "PM_ERR_UNSUPPORTED")
+        scale = head_dim ** -0.5 if scale is None else float(scale)
+        if not 0 < scale < 3e38:
+            _refuse("scale must be positive and finite")
+        self.n_heads, self.n_kv_heads, self.head_dim, self.causal, self.scale = n_heads, n_kv_heads, head_dim, bool(causal), scale
+        self.L = lib()
+
+    def _desc(self, q, cu_seqlens):
+        device = _compute_device("q", q)
+        if q.dim() != 3:
+            _refuse(f"q has shape {tuple(q.shape)}, expected [tokens, {self.n_heads}, {self.head_dim}]", "PM_ERR_SHAPE")
+        if not isinstance(cu_seqlens, torch.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.numel() < 1:
+            _refuse("cu_seqlens must be a one-dimensional tensor of sequences + 1 entries", "PM_ERR_SHAPE")
+        cu = _flat("cu_seqlens", cu_seqlens, torch.int32, device, tuple(cu_seqlens.shape))
+        d = pm_attention_desc(_DTYPES[q.dtype], self.n_heads, self.n_kv_heads, self.head_dim, cu_seqlens.numel() - 1, int(self.causal),
+                              q.shape[0], self.scale)
+        return device, d, cu
+
+    def _view(self, name, t, q, heads, written=False):
+        _tensor(name, t, q.dtype, q.device, (q.shape[0], heads, self.head_dim))
+        token, head, one = t.stride()
+        if one != 1 and self.head_dim > 1:
+            _refuse(f"the last dimension of {name} must be contiguous")
+        if written and t.numel() > 0:
+            # rows of one head, or heads of one row, must not share elements
+            a, b = sorted(((token, t.shape[0]), (head, heads)))
+            a, b = [s for s, n in (a, b) if n > 1] or [self.head_dim], (b, a)
+            if a[0] < self.head_dim or (len(a) > 1 and a[1] < a[0] * (b[1][1] - 1) + self.head_dim):
+                _refuse(f"{name} overlaps itself")
+        return pm_head_view(t.data_ptr(), token, head)
+
+    def pm_attention_packed_forward(self, q, k, v, cu_seqlens, o, lse=None, stream=None):
+        """Writes o and, for a backward pass, lse."""
+        device, d, cu = self._desc(q, cu_seqlens)
+        views = [C.byref(self._view(n, t, q, h)) for n, t, h in (("q", q, self.n_heads), ("k", k, self.n_kv_heads), ("v", v, self.n_kv_heads))]
+        out = self._view("o", o, q, self.n_heads, written=True)
+        p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, q.shape[0]))
+        with _Launch(device, stream) as st:
+            _check(self.L.pm_attention_packed_forward(C.byref(d), *views, cu, C.byref(out), p_lse, st))
+
+    def pm_attention_packed_backward(self, q, k, v, o, lse, d_o, cu_seqlens, dq, dk, dv, stream=None):
+        """Writes dq, dk and dv from d_o and what the forward call wrote."""
+        device, d, cu = self._desc(q, cu_seqlens)
+        H, K = self.n_heads, self.n_kv_heads
+        vq, vk, vv, vo, vdo = (C.byref(self._view(n, t, q, h)) for n, t, h in (("q", q, H), ("k", k, K), ("v", v, K), ("o", o, H), ("d_o", d_o, H)))
+        wq, wk, wv = (C.byref(self._view(n, t, q, h, written=True)) for n, t, h in (("dq", dq, H), ("dk", dk, K), ("dv", dv, K)))
+        if lse is None:
+            _refuse("lse must be a tensor")
+        p_lse = _flat("lse", lse, torch.float32, device, (H, q.shape[0]))
+        need = self.L.pm_attention_packed_workspace_bytes(C.byref(d))
+        launch = _Launch(device, stream)
+        with launch as st:
+            ws = launch.workspace(need, device)
+            _check(self.L.pm_attention_packed_backward(C.byref(d), vq, vk, vv, vo, p_lse, vdo, cu, wq, wk, wv, ws.data_ptr(), need, st))
+
+
+class TokenLogProbs:
+    """Log probabilities of given tokens under rows of logits [rows, vocab] (float32 or bfloat16, contiguous rows at any stride),
+    the entropy of each row, its logsumexp, and its top_k most likely tokens.
+
+    targets: int32 [rows], negative = padding.  logprob, entropy, lse: float32 [rows]; top_logprob: float32 [rows, top_k];
+    top_ids: int32 [rows, top_k], equal logits in ascending order of their ids.
+    """
+
+    def __init__(self, vocab, top_k=0):
+        if vocab < 1 or vocab > 1 << 24:
+            _refuse("vocab must be 1 to 2^24")
+        if not 0 <= top_k <= min(32, vocab):
+            _refuse("top_k must be 0 to 32 and at most the vocabulary size")
+        self.vocab, self.top_k = vocab, top_k
+        self.L = lib()
+
+    def _rows(self, name, t, like=None):
+        device = _compute_device(name, t)
+        if like is not None:
+            _tensor(name, t, like.dtype, like.device, tuple(like.shape))
+        if t.dim() != 2 or t.shape[1] != self.vocab:
+            _refuse(f"{name} has shape {tuple(t.shape)}, expected [rows, {self.vocab}]", "PM_ERR_SHAPE")
+        if self.vocab > 1 and t.stride(1) != 1:
+            _refuse(f"the rows of {name} must be contiguous")
+        stride = t.stride(0) if t.shape[0] > 1 else self.vocab
+        if stride < self.vocab:
+            _refuse(f"the rows of {name} overlap")
+        return device, stride
+
+    def pm_token_logprobs(self, logits, targets, logprob, entropy=None, lse=None, top_logprob=None, top_ids=None, stream=None):
+        """Writes logprob (targets and logprob may both be None) and whichever of the others are given."""
+        device, stride = self._rows("logits", logits)
+        n, k = logits.shape[0], self.top_k
+        if k and (top_logprob is None or top_ids is None):
+            _refuse("top_logprob and top_ids must be given with top_k")
+        f32, i32 = torch.float32, torch.int32
+        with _Launch(device, stream) as st:
+            _check(self.L.pm_token_logprobs(
+                logits.data_ptr(), _DTYPES[logits.dtype], n, self.vocab, stride, _flat("targets", targets, i32, device, (n,)),
+                _flat("logprob", logprob, f32, device, (n,)), _flat("entropy", entropy, f32, device, (n,)), _flat("lse", lse, f32, device, (n,)),
+                k, _flat("top_logprob", top_logprob, f32, device, (n, k)), _flat("top_ids", top_ids, i32, device, (n, k)), st))
+
+    def pm_token_logprobs_backward(self, logits, targets, lse, d_logits, d_logprob=None, entropy=None, d_entropy=None, stream=None):
+        """Writes d_logits (logits itself is allowed) from the gradients of logprob and / or of the entropy."""
+        device, stride = self._rows("logits", logits)
+        _, grad_stride = self._rows("d_logits", d_logits, logits)
+        n, f32 = logits.shape[0], torch.float32
+        if lse is None:
+            _refuse("lse must be a tensor")
+        if logits.data_ptr() == d_logits.data_ptr() and stride != grad_stride:
+            _refuse("d_logits shares the memory of logits at other strides")
+        with _Launch(device, stream) as st:
+            _check(self.L.pm_token_logprobs_backward(
+                logits.data_ptr(), _DTYPES[logits.dtype], n, self.vocab, stride, _flat("targets", targets, torch.int32, device, (n,)),
+                _flat("lse", lse, f32, device, (n,)), _flat("entropy", entropy, f32, device, (n,)),
+                _flat("d_logprob", d_logprob, f32, device, (n,)), _flat("d_entropy", d_entropy, f32, device, (n,)),
+                d_logits.data_ptr(), grad_stride, st))
+
+
+class GradClip:
+    """Clipping of a list of gradient tensors by their global norm, into `outs` (None: in place).
+
+    Holds the two lists (and so the tensors' memory) for calls to come; a program whose gradients move to other tensors makes a new one.
+    Tensors are contiguous, float32 or bfloat16 in any mixture, on one device; outs[i] has as many elements as grads[i] and may be a
+    slice of the gradient arena.
+    """
+
+    def __init__(self, grads, outs=None):
+        grads = list(grads)
+        outs = grads if outs is None else list(outs)
+        if not grads:
+            _refuse("no tensors")
+        if len(outs) != len(grads):
+            _refuse(f"{len(grads)} gradients, {len(outs)} destinations")
+        self.device = _compute_device("grads[0]", grads[0])
+        self.L = lib()
+        self.grads, self.outs = grads, outs
+        self.tensors = (pm_tensor_pair * len(grads))()
+        spans = []
+        for i, (g, o) in enumerate(zip(grads, outs)):
+            for name, t in ((f"grads[{i}]", g), (f"outs[{i}]", o)):
+                _compute_device(name, t)
+                _tensor(name, t, t.dtype, self.device)
+                if not t.is_contiguous():
+                    _refuse(f"{name} must be contiguous")
+            if g.numel() != o.numel():
+                _refuse(f"grads[{i}] has {g.numel()} elements, outs[{i}] {o.numel()}", "PM_ERR_SHAPE")
+            self.tensors[i] = pm_tensor_pair(g.data_ptr(), o.data_ptr(), g.numel(), _DTYPES[g.dtype], _DTYPES[o.dtype])
+            if g.numel() == 0:
+                continue
+            in_place = g.data_ptr() == o.data_ptr() and g.dtype == o.dtype
+            spans.append((o.data_ptr(), o.data_ptr() + o.numel() * o.element_size(), True, f"outs[{i}]"))
+            if not in_place:
+                spans.append((g.data_ptr(), g.data_ptr() + g.numel() * g.element_size(), False, f"grads[{i}]"))
+        end = {True: (0, ""), False: (0, "")}                # the furthest end so far of what is written, and of what is read
+        for a, b, written, name in sorted(spans):
+            for other in (True, False) if written else (True,):
+                if a < end[other][0]:
+                    _refuse(f"{name} overlaps {end[other][1]}")
+            end[written] = max(end[written], (b, name))
+        self.ws_bytes = self.L.pm_clip_gradients_workspace_bytes(len(grads))
+
+    def pm_clip_gradients(self, max_norm, norm, scale, stream=None):
+        """Writes outs, the norm before clipping, and the factor (float32 tensors of one element)."""
+        max_norm = float(max_norm)
+        if not max_norm > 0 or math.isnan(max_norm):
+            _refuse("max_norm must be positive")
+        p_norm, p_scale = (_flat(n, t, torch.float32, self.device, tuple(t.shape) if isinstance(t, torch.Tensor) and t.numel() == 1 else (1,))
+                           for n, t in (("norm", norm), ("scale", scale)))
+        launch = _Launch(self.device, stream)
+        with launch as st:
+            ws = launch.workspace(self.ws_bytes, self.device)
+            _check(self.L.pm_clip_gradients(self.tensors, len(self.tensors), max_norm, p_norm, p_scale, ws.data_ptr(), self.ws_bytes, st))
