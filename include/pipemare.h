@@ -435,6 +435,10 @@ pm_status pm_attention_packed_backward(const pm_attention_desc* desc, const pm_h
                                        const pm_head_view* dk, const pm_head_view* dv, void* workspace,
                                        uint64_t workspace_bytes, void* stream);
 
+/* Every wait inside the tensor-core kernels is bounded (about one second).  One that runs out is a defect: the rows
+ * concerned are NaN, and this call, which synchronises the stream, returns PM_ERR_TIMEOUT once. */
+pm_status pm_attention_packed_status(void* stream);
+
 /* Per row of logits [rows, vocab] (row_stride elements apart, dtype PM_F32 | PM_BF16):
  *   lse = log sum_j exp(x_j);  logprob = x_y - lse for the target y;  entropy = lse - sum_j p_j x_j;  the top_k largest
  *   logits' ids, in descending order (equal logits: the lower id first), and their log probabilities.

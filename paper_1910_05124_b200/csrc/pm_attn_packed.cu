@@ -340,7 +340,8 @@ pm_status pm_attention_packed_forward(const pm_attention_desc* d, const pm_head_
   if (const pm_status s = pk_view(a.v, v, "v", size)) return s;
   if (const pm_status s = pk_view(a.o, o, "o", size)) return s;
   const cudaStream_t st = (cudaStream_t)stream;
-  const cudaError_t e = d->dtype == PM_BF16 ? pk_run<__nv_bfloat16>(a, false, st) : pk_run<float>(a, false, st);
+  const cudaError_t e = attn_packed_tc_takes(a, d->dtype, false) ? attn_packed_tc_forward(a, st)
+                        : d->dtype == PM_BF16 ? pk_run<__nv_bfloat16>(a, false, st) : pk_run<float>(a, false, st);
   return ops_cuda(e, "packed attention");
 }
 
@@ -370,8 +371,15 @@ pm_status pm_attention_packed_backward(const pm_attention_desc* d, const pm_head
   if (!aligned_to(workspace, 4)) return ops_fail(PM_ERR_INVALID_ARG, "workspace must be 4-byte aligned");
   a.delta = static_cast<float*>(workspace);
   const cudaStream_t st = (cudaStream_t)stream;
-  const cudaError_t e = d->dtype == PM_BF16 ? pk_run<__nv_bfloat16>(a, true, st) : pk_run<float>(a, true, st);
+  const cudaError_t e = attn_packed_tc_takes(a, d->dtype, true) ? attn_packed_tc_backward(a, st)
+                        : d->dtype == PM_BF16 ? pk_run<__nv_bfloat16>(a, true, st) : pk_run<float>(a, true, st);
   return ops_cuda(e, "packed attention backward");
+}
+
+pm_status pm_attention_packed_status(void* stream) {
+  int code = 0;
+  if (const pm_status s = ops_cuda(attn_packed_status(&code, (cudaStream_t)stream), "packed attention status")) return s;
+  return code ? ops_fail(PM_ERR_TIMEOUT, "packed attention: device-side wait %d ran out", code) : PM_OK;
 }
 
 }  // extern "C"

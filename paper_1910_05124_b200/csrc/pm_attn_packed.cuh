@@ -78,5 +78,7 @@ inline int64_t most_tiles(int64_t tokens, int n_seqs, int rows) { return tokens 
 bool attn_packed_tc_takes(const PackedArgs& a, int dtype, bool backward);
 cudaError_t attn_packed_tc_forward(const PackedArgs& a, cudaStream_t st);
 cudaError_t attn_packed_tc_backward(const PackedArgs& a, cudaStream_t st);
+// the code of a device-side wait that ran out since the last call (0: none); synchronises the stream
+cudaError_t attn_packed_status(int* code, cudaStream_t st);
 
 }  // namespace pm

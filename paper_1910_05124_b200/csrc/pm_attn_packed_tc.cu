@@ -1,0 +1,416 @@
+// Attention over packed sequences on the tensor cores (tcgen05, TMEM, TMA): bf16, heads of up to 128 in steps of 8 (zero-filled to a
+// tile of 64 or 128 by the copies).  The mathematics is that of pm_attn_packed.cu.
+//
+// Forward.  A block owns NT query tiles of 128 rows: two heads that share keys and values, or two consecutive tiles of one head; every
+// key/value tile it copies serves both.  Four warps per query tile (thread = row = tensor-memory lane) do the softmax, one warp
+// copies, one issues the products:
+//   S = Q K^T (128 x 128 x D, operands in shared memory) -> p = 2^(c s - m) in fp32 -> bf16 P over S's columns in tensor memory
+//   -> O += P V (A = P from tensor memory).
+// While the softmax of one tile runs, the products of the other do.  The running maximum m is raised, and O and the row sum rescaled,
+// only when a row of the warp outgrows it by 2^8: P then reaches at most 256, which bf16 holds as exactly as 1, and most key tiles
+// leave O alone.
+//
+// Products that read P are issued before the product that overwrites it, and products complete in the order of their issue, so a
+// commit behind S(j + 1) also says that O holds tile j.
+#include <atomic>
+#include <mutex>
+
+#include "pm_attn_packed.cuh"
+#include "pm_ptx.cuh"
+
+namespace pm {
+
+// A bounded wait that ran out (a defect): its code, kept until pm_attention_packed_status reads it.
+__device__ int g_attn_packed_status;
+
+constexpr int TC_ROWS = 128;                      // rows of a tile, of queries and of keys
+constexpr int FWD_P = 64;                         // first column of P within S's 128
+constexpr int TC_SUB = TC_ROWS * 128;             // bytes of a [128 x 64] bf16 sub-tile, 128-byte swizzle
+
+template <int DT, int NT> struct FwdShape {
+  static constexpr int kSub = DT / 64;            // sub-tiles of a tile
+  static constexpr int kTile = kSub * TC_SUB;
+  static constexpr int kStages = NT == 1 ? (DT == 64 ? 2 : 1) : (DT == 64 ? 4 : 2);
+  static constexpr int kThreads = NT * 128 + 64;
+  static constexpr int kBlocks = NT == 1 ? 2 : 1; // per SM
+  static constexpr int kCols = NT * 256;          // tensor-memory columns: S (128 each), then O (DT each)
+  static constexpr int kBars = 1 + 4 * kStages + 3 * NT;
+  static constexpr int kSmem = NT * kTile + 2 * kStages * kTile + 1024 + kBars * 8 + 16;
+};
+
+struct TcMaps { CUtensorMap q, k, v; };
+
+// 128 x N x DT product of two K-major tiles
+template <int DT> __device__ __forceinline__ void mma_abt(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+  const uint64_t base = desc_base(16, 1024);
+#pragma unroll
+  for (int k = 0; k < DT / 16; ++k) {
+    const uint32_t off = (k >> 2) * TC_SUB + (k & 3) * 32;
+    tc_mma_bf16(d, desc_at(base, a + off), desc_at(base, b + off), idesc, k > 0);
+  }
+}
+// 128 x DT x 128 product of A in tensor memory and a tile whose rows run along the depth
+template <int DT> __device__ __forceinline__ void mma_ab(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
+  const uint64_t base = desc_base(TC_SUB, 1024);
+#pragma unroll
+  for (int k = 0; k < TC_ROWS / 16; ++k) tc_mma_bf16_ta(d, a + k * 8, desc_at(base, b + k * 2048), idesc, accumulate || k > 0);
+}
+
+template <int DT> __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int64_t token) {
+#pragma unroll
+  for (int i = 0; i < DT / 64; ++i) tma_load_3d(dst + i * TC_SUB, map, bar, i * 64, head, (int)token);
+}
+
+// c s - m for two values at a time
+__device__ __forceinline__ float2 fma_f32x2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+
+template <int DT, int NT>
+__global__ void __launch_bounds__(FwdShape<DT, NT>::kThreads, FwdShape<DT, NT>::kBlocks)
+attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcMaps maps, int units, int pair_heads) {
+  using S = FwdShape<DT, NT>;
+  const int rows = pair_heads ? TC_ROWS : NT * TC_ROWS;
+  const int unit = blockIdx.x % units;
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / units, rows);
+  if (s.tile < 0) return;
+  // the last tiles of a sequence see the most keys: they come first
+  const int tile = (s.len + rows - 1) / rows - 1 - s.tile;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto head_of = [&](int t) { return pair_heads ? unit * 2 + t : unit; };
+  auto first_of = [&](int t) { return pair_heads ? tile * TC_ROWS : (tile * NT + t) * TC_ROWS; };
+  auto keys_of = [&](int t) {                     // key tiles that query tile t sees
+    const int q0 = first_of(t);
+    return q0 >= s.len ? 0 : ((a.causal ? min(s.len, q0 + TC_ROWS) : s.len) + TC_ROWS - 1) / TC_ROWS;
+  };
+  const int hk = head_of(0) / a.group;
+  int n_keys = keys_of(0);
+  if (NT == 2) n_keys = max(n_keys, keys_of(1));
+
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  uint8_t* const sptr = smem_raw + (base - raw);
+  const uint32_t sQ = base, sK = sQ + NT * S::kTile, sV = sK + S::kStages * S::kTile, bars = sV + S::kStages * S::kTile;
+  const uint32_t bar_q = bars;
+  auto k_full = [&](int i) { return bars + 8 * (1 + i); };
+  auto k_empty = [&](int i) { return bars + 8 * (1 + S::kStages + i); };
+  auto v_full = [&](int i) { return bars + 8 * (1 + 2 * S::kStages + i); };
+  auto v_empty = [&](int i) { return bars + 8 * (1 + 3 * S::kStages + i); };
+  auto s_full = [&](int t) { return bars + 8 * (1 + 4 * S::kStages + t); };
+  auto p_full = [&](int t) { return bars + 8 * (1 + 4 * S::kStages + NT + t); };
+  auto o_full = [&](int t) { return bars + 8 * (1 + 4 * S::kStages + 2 * NT + t); };
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(sptr + (bars - base) + 8 * S::kBars);
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* const status = &g_attn_packed_status;
+
+  if (threadIdx.x == 0) {
+    mbar_init(bar_q, 1);
+    for (int i = 0; i < S::kStages; ++i) { mbar_init(k_full(i), 1); mbar_init(k_empty(i), 1); mbar_init(v_full(i), 1); mbar_init(v_empty(i), 1); }
+    for (int t = 0; t < NT; ++t) { mbar_init(s_full(t), 1); mbar_init(p_full(t), 128); mbar_init(o_full(t), 1); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == NT * 4 + 1) {
+    tmem_alloc(smem_u32(tmem_slot), S::kCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  auto col_s = [&](int t) { return tmem + t * 128; };
+  auto col_o = [&](int t) { return tmem + NT * 128 + t * DT; };
+
+  if (warp == NT * 4) {                           // ---- copies
+    int armed_k = 0, armed_v = 0;
+    bool ok = true;
+    if (elect_one()) {
+      int bytes = 0;
+      for (int t = 0; t < NT; ++t) if (keys_of(t)) bytes += S::kTile;
+      mbar_arrive_expect_tx(bar_q, bytes);
+      for (int t = 0; t < NT; ++t)
+        if (keys_of(t)) load_tile<DT>(sQ + t * S::kTile, &maps.q, bar_q, head_of(t), s.begin + first_of(t));
+    }
+    __syncwarp();
+    for (int j = 0; j < n_keys && ok; ++j) {
+      const int st = j % S::kStages;
+      const uint32_t ph = (j / S::kStages - 1) & 1;
+      if (j >= S::kStages) ok = mbar_wait(k_empty(st), ph, abort_flag, status, 31);
+      if (!ok) break;
+      if (elect_one()) { mbar_arrive_expect_tx(k_full(st), S::kTile); load_tile<DT>(sK + st * S::kTile, &maps.k, k_full(st), hk, s.begin + j * TC_ROWS); }
+      __syncwarp();
+      ++armed_k;
+      if (j >= S::kStages) ok = mbar_wait(v_empty(st), ph, abort_flag, status, 32);
+      if (!ok) break;
+      if (elect_one()) { mbar_arrive_expect_tx(v_full(st), S::kTile); load_tile<DT>(sV + st * S::kTile, &maps.v, v_full(st), hk, s.begin + j * TC_ROWS); }
+      __syncwarp();
+      ++armed_v;
+    }
+    if (*abort_flag) {                            // nothing may be in flight when the block ends
+      volatile int never = 0;
+      mbar_wait(bar_q, 0, &never, status, 33);
+      for (int j = max(0, armed_k - S::kStages); j < armed_k; ++j) mbar_wait(k_full(j % S::kStages), (j / S::kStages) & 1, &never, status, 33);
+      for (int j = max(0, armed_v - S::kStages); j < armed_v; ++j) mbar_wait(v_full(j % S::kStages), (j / S::kStages) & 1, &never, status, 33);
+    }
+  } else if (warp == NT * 4 + 1) {                // ---- products
+    const uint32_t id_s = make_idesc_mn(128, 128, 0, 0), id_o = make_idesc_mn(128, DT, 0, 1);
+    bool ok = mbar_wait(bar_q, 0, abort_flag, status, 34) && mbar_wait(k_full(0), 0, abort_flag, status, 35);
+    if (ok) {
+      tc_fence_after();
+      if (elect_one()) {
+        for (int t = 0; t < NT; ++t)
+          if (keys_of(t)) { mma_abt<DT>(col_s(t), sQ + t * S::kTile, sK, id_s); tc_commit(s_full(t)); }
+        tc_commit(k_empty(0));
+      }
+      __syncwarp();
+    }
+    for (int j = 0; j < n_keys && ok; ++j) {
+      const int st = j % S::kStages, nx = (j + 1) % S::kStages;
+      ok = mbar_wait(v_full(st), (j / S::kStages) & 1, abort_flag, status, 36);
+      if (ok && j + 1 < n_keys && S::kStages > 1) ok = mbar_wait(k_full(nx), ((j + 1) / S::kStages) & 1, abort_flag, status, 37);
+      if (!ok) break;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int n = keys_of(t);
+        if (j >= n) continue;
+        ok = mbar_wait(p_full(t), j & 1, abort_flag, status, 38);
+        // with one stage the next keys are copied only now, behind the previous product's commit
+        if (ok && S::kStages == 1 && j + 1 < n) ok = mbar_wait(k_full(0), (j + 1) & 1, abort_flag, status, 37);
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) {
+          mma_ab<DT>(col_o(t), col_s(t) + FWD_P, sV + st * S::kTile, id_o, j > 0);
+          if (j + 1 < n) { mma_abt<DT>(col_s(t), sQ + t * S::kTile, sK + nx * S::kTile, id_s); tc_commit(s_full(t)); }
+          else tc_commit(o_full(t));
+        }
+        __syncwarp();
+      }
+      if (!ok) break;
+      if (elect_one()) {
+        tc_commit(v_empty(st));
+        if (j + 1 < n_keys) tc_commit(k_empty(nx));
+      }
+      __syncwarp();
+    }
+  } else {                                        // ---- softmax: thread = row
+    const int t = warp >> 2, r = threadIdx.x & 127;
+    const int n = keys_of(t), q0 = first_of(t), row = q0 + r;
+    if (n > 0) {
+      const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+      const uint32_t ts = col_s(t) + lanes, to = col_o(t) + lanes;
+      const float c = a.scale * kLog2e;
+      const int limit = a.causal ? min(s.len, row + 1) : s.len;      // keys this row sees
+      float m = -INFINITY, l = 0.f;               // m: the maximum in use, times c
+      bool ok = true;
+      for (int j = 0; j < n; ++j) {
+        ok = mbar_wait(s_full(t), j & 1, abort_flag, status, 39);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        const int k0 = j * TC_ROWS;
+        const bool edge = k0 + TC_ROWS > s.len || (a.causal && k0 + TC_ROWS > q0 + 1);
+        auto mask = [&](uint32_t (&x)[32], int q) {
+          if (edge)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (k0 + q * 32 + i >= limit) x[i] = 0xFF800000u;
+        };
+        // the maximum over the row; its upper half stays in registers, the lower one is read again
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        auto maximum = [&](const uint32_t (&x)[32]) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(x[i]));
+        };
+        uint32_t v[2][32];
+        tmem_ld32(ts, v[0]);
+        tmem_ld32(ts + 32, v[1]);
+        tmem_ld_wait();
+        mask(v[0], 0); mask(v[1], 1);
+        maximum(v[0]); maximum(v[1]);
+        tmem_ld32(ts + 64, v[0]);
+        tmem_ld32(ts + 96, v[1]);
+        tmem_ld_wait();
+        mask(v[0], 2); mask(v[1], 3);
+        maximum(v[0]); maximum(v[1]);
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+        if (j == 0) {
+          m = top;
+        } else if (__any_sync(0xffffffffu, top > m + 8.f)) {
+          const float up = fmaxf(m, top), f = ex2(m - up);
+          m = up;
+          l *= f;
+#pragma unroll
+          for (int q = 0; q < DT / 32; ++q) {
+            uint32_t o[32];
+            tmem_ld32(to + q * 32, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_st32(to + q * 32, o);
+          }
+        }
+        float2 sum = make_float2(0.f, 0.f);
+        const float2 cc = make_float2(c, c), mm = make_float2(-m, -m);
+        auto probabilities = [&](const uint32_t (&x)[32], int q) {
+          uint32_t p[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float2 e = fma_f32x2(make_float2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), cc, mm);
+            e.x = ex2(e.x); e.y = ex2(e.y);
+            sum = add_f32x2(sum, e);
+            p[i] = pack_bf16(e.x, e.y);
+          }
+          tmem_st16(ts + FWD_P + q * 16, p);
+        };
+        probabilities(v[0], 2);                   // P's columns 96 .. 127 overwrite scores that are in registers ...
+        probabilities(v[1], 3);
+        tmem_ld32(ts, v[0]);
+        tmem_ld32(ts + 32, v[1]);
+        tmem_ld_wait();
+        mask(v[0], 0); mask(v[1], 1);
+        probabilities(v[0], 0);                   // ... and columns 64 .. 95 scores that are done
+        probabilities(v[1], 1);
+        l += sum.x + sum.y;
+        // The rows behind the sequence's end of its last value tile belong to other sequences, or to none: zeros, as p is there, so
+        // that nothing that is not finite meets a zero.  The first query tile that reads the tile clears it.
+        if (k0 + TC_ROWS > s.len && (t == 0 || keys_of(0) <= j)) {
+          const int st = j % S::kStages, valid = s.len - k0;
+          ok = mbar_wait(v_full(st), (j / S::kStages) & 1, abort_flag, status, 40);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          for (int i = valid * 8 + r; i < TC_ROWS * 8; i += 128)
+#pragma unroll
+            for (int q = 0; q < S::kSub; ++q)
+              *reinterpret_cast<uint4*>(sptr + (sV - base) + st * S::kTile + q * TC_SUB + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+          fence_async_smem();
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(p_full(t));
+      }
+      if (ok) ok = mbar_wait(o_full(t), 0, abort_flag, status, 41);
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+      const float inv = ok ? 1.f / l : NAN;
+      const int h = head_of(t);
+      if (a.lse && row < s.len) a.lse[(int64_t)h * a.tokens + s.begin + row] = ok ? (m + log2f(l)) * kLn2 : NAN;
+      __nv_bfloat16* out = head_row_out<__nv_bfloat16>(a.o, s.begin + row, h);
+#pragma unroll
+      for (int q = 0; q < DT / 32; ++q) {
+        uint32_t o[32];
+        tmem_ld32(to + q * 32, o);
+        tmem_ld_wait();
+        if (row < s.len)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            if (q * 32 + g * 8 < a.dim) {
+              float f[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(o[g * 8 + i]) * inv;
+              *reinterpret_cast<uint4*>(out + q * 32 + g * 8) =
+                  make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+            }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == NT * 4 + 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, S::kCols);
+  }
+}
+
+// ---- host side --------------------------------------------------------------------------------------------------
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static EncodeTiledFn encode_fn() {
+  static std::atomic<EncodeTiledFn> cached{nullptr};
+  EncodeTiledFn fn = cached.load(std::memory_order_acquire);
+  if (fn) return fn;
+  void* p = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) return nullptr;
+  fn = reinterpret_cast<EncodeTiledFn>(p);
+  cached.store(fn, std::memory_order_release);
+  return fn;
+}
+
+// [dim, heads, tokens] map with boxes of 64 x 1 x 128; columns behind the head's width and rows behind the last token read as zeros
+static cudaError_t encode_heads(CUtensorMap* map, const HeadView& x, int dim, int heads, int64_t tokens) {
+  const EncodeTiledFn fn = encode_fn();
+  if (!fn) return cudaErrorNotSupported;
+  // a dimension of one entry may come with any stride: give it a valid one
+  const cuuint64_t head = heads > 1 ? (cuuint64_t)x.head * 2 : 256, token = tokens > 1 ? (cuuint64_t)x.token * 2 : 256;
+  const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)tokens}, strides[2] = {head, token};
+  const cuuint32_t box[3] = {64, 1, TC_ROWS}, step[3] = {1, 1, 1};
+  const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(x.data), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+// 16-byte rows and strides, none of them zero
+static bool tc_view(const HeadView& x, int heads, int64_t tokens) {
+  auto stride = [](int64_t s, int64_t n) { return n <= 1 || (s > 0 && s % 8 == 0 && s < ((int64_t)1 << 38)); };
+  return aligned_to(x.data, 16) && stride(x.head, heads) && stride(x.token, tokens);
+}
+
+bool attn_packed_tc_takes(const PackedArgs& a, int dtype, bool backward) {
+  if (backward) return false;
+  return dtype == PM_BF16 && a.dim % 8 == 0 && tc_view(a.q, a.heads, a.tokens) && tc_view(a.k, a.kv_heads, a.tokens) &&
+         tc_view(a.v, a.kv_heads, a.tokens) && tc_view(a.o, a.heads, a.tokens);
+}
+
+template <typename K> static cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev > 63 || !(done.load(std::memory_order_relaxed) >> dev & 1))) {
+    e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev <= 63) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  return e;
+}
+
+template <int DT, int NT> static cudaError_t fwd_launch(const PackedArgs& a, cudaStream_t st) {
+  static std::atomic<uint64_t> done{0};
+  using S = FwdShape<DT, NT>;
+  TcMaps maps;
+  cudaError_t e = allow_smem(attn_packed_fwd_tc_kernel<DT, NT>, S::kSmem, done);
+  if (e == cudaSuccess) e = encode_heads(&maps.q, a.q, a.dim, a.heads, a.tokens);
+  if (e == cudaSuccess) e = encode_heads(&maps.k, a.k, a.dim, a.kv_heads, a.tokens);
+  if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.tokens);
+  if (e != cudaSuccess) return e;
+  const int pair = NT == 2 && a.group % 2 == 0, units = pair ? a.heads / 2 : a.heads;
+  const int64_t blocks = most_tiles(a.tokens, a.n_seqs, pair ? TC_ROWS : NT * TC_ROWS) * units;
+  if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  return launch_pdl(attn_packed_fwd_tc_kernel<DT, NT>, dim3((unsigned)blocks), dim3(S::kThreads), S::kSmem, st, false, a, maps, units, pair);
+}
+
+cudaError_t attn_packed_tc_forward(const PackedArgs& a, cudaStream_t st) {
+  const bool two = a.tokens >= (int64_t)512 * a.n_seqs;
+  if (a.dim <= 64) return two ? fwd_launch<64, 2>(a, st) : fwd_launch<64, 1>(a, st);
+  return two ? fwd_launch<128, 2>(a, st) : fwd_launch<128, 1>(a, st);
+}
+
+cudaError_t attn_packed_tc_backward(const PackedArgs&, cudaStream_t) { return cudaErrorNotSupported; }
+
+cudaError_t attn_packed_status(int* code, cudaStream_t st) {
+  *code = 0;
+  cudaError_t e = cudaMemcpyFromSymbolAsync(code, g_attn_packed_status, sizeof(int), 0, cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e == cudaSuccess && *code) {
+    const int zero = 0;
+    e = cudaMemcpyToSymbolAsync(g_attn_packed_status, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  }
+  return e;
+}
+
+}  // namespace pm

@@ -147,6 +147,14 @@ class PackedAttention:
             ws = launch.workspace(need, device)
             _check(self.L.pm_attention_packed_backward(C.byref(d), vq, vk, vv, vo, p_lse, vdo, cu, wq, wk, wv, ws.data_ptr(), need, st))
 
+    def pm_attention_packed_status(self, device="cuda", stream=None):
+        """Raises if a device-side wait of a tensor-core kernel ran out since the last call (a defect); synchronises the stream."""
+        device = torch.device(device)
+        if device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
+        with _Launch(device, stream) as st:
+            _check(self.L.pm_attention_packed_status(st))
+
 
 class TokenLogProbs:
     """Log probabilities of given tokens under rows of logits [rows, vocab] (float32 or bfloat16, contiguous rows at any stride),

@@ -55,7 +55,7 @@ def check(op, q, k, v, d_o, cu):
         within(got[name], want, bound, name)
 
 
-LENS = [[1], [2, 1, 3], [17, 1, 46], [64], [65, 63], [127, 128, 129], [200, 0, 5, 300], [256, 255, 257, 1], [700, 31]]
+LENS = [[1], [2, 1, 3], [17, 1, 46], [64], [65, 63], [127, 128, 129], [200, 0, 5, 300], [256, 255, 257, 1], [700, 31], [1030], [512, 897, 640]]
 
 
 @pytest.mark.parametrize("causal", [True, False])
@@ -75,6 +75,8 @@ def test_head_widths(cuda_device, D, dtype):
 @pytest.mark.parametrize("H,K", [(1, 1), (3, 1), (8, 2), (5, 5), (16, 1)])
 def test_shared_heads(cuda_device, H, K, dtype):
     check(*make([40, 150], H, K, 128 if H < 8 else 64, dtype, cuda_device, seed=H))
+    if H < 16:
+        check(*make([1100], H, K, 64 if H < 8 else 128, dtype, cuda_device, seed=H))
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
@@ -102,23 +104,24 @@ def test_growing_scores(cuda_device, dtype):
 @pytest.mark.parametrize("dtype", [BF, F])
 def test_rows_outside_the_sequences_stay(cuda_device, dtype):
     """Tokens before the first and behind the last sequence hold NaN in every input and are neither used nor written."""
-    for D in (64, 128, 40):
-        op, q, k, v, d_o, cu = make([90, 39], 4, 2, D, dtype, cuda_device, first=5, tail=70, seed=4)
+    for D, lens, H in ((64, [90, 39], 4), (128, [90, 39], 4), (40, [90, 39], 4), (64, [129], 3), (128, [901], 3), (64, [777], 4)):
+        op, q, k, v, d_o, cu = make(lens, H, H if H == 3 else 2, D, dtype, cuda_device, first=5, tail=70, seed=4)
+        end = 5 + sum(lens)
         clean = [x.clone() for x in (q, k, v, d_o)]
         for x in (q, k, v, d_o):
             x[:5] = math.nan
-            x[134:] = math.inf
+            x[end:] = math.inf
         o, lse = forward(op, q, k, v, cu, fill=3.25)
         for x in (o, lse.t()):
-            assert (x[:5] == 3.25).all() and (x[134:] == 3.25).all()
+            assert (x[:5] == 3.25).all() and (x[end:] == 3.25).all()
         wo, wl, bo, bl = R.attention_forward(*clean[:3], cu, op.scale, True, dtype)
-        within(o[5:134], wo[5:134], bo[5:134], "o")
-        within(lse[:, 5:134], wl[:, 5:134], bl[:, 5:134], "lse")
+        within(o[5:end], wo[5:end], bo[5:end], "o")
+        within(lse[:, 5:end], wl[:, 5:end], bl[:, 5:end], "lse")
         g = backward(op, q, k, v, o, lse, d_o, cu, fill=1.5)
         want = R.attention_backward(*clean[:3], o, lse, clean[3], cu, op.scale, True, dtype)
         for name, x in g.items():
-            assert (x[:5] == 1.5).all() and (x[134:] == 1.5).all(), name
-            within(x[5:134], want[name][0][5:134], want[name][1][5:134], name)
+            assert (x[:5] == 1.5).all() and (x[end:] == 1.5).all(), name
+            within(x[5:end], want[name][0][5:end], want[name][1][5:end], name)
 
 
 @pytest.mark.parametrize("causal", [True, False])
