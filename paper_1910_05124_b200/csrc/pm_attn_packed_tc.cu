@@ -325,6 +325,468 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
   }
 }
 
+// ---- backward ---------------------------------------------------------------------------------------------------
+//
+// Two kernels, as on the CUDA cores: one owns 128 key rows (dk, dv), one owns 128 query rows (dq); every gradient is summed by one
+// block in a fixed order. Seven products a pair of tiles instead of the five that sharing the scores would take, and no atomics,
+// no fp32 copy of dq in memory. Both have the shape  two products -> 128 x 128 values in registers -> bf16 factors in tensor
+// memory -> one or two products that accumulate, and 256 threads for the values: thread = row, two halves of the columns.
+//
+// Keys:     S^T = K Q^T, dP^T = V dO^T;  P^T = 2^(c S^T - lse), dS^T = P^T (dP^T - delta);  dV += P^T dO,  dK += dS^T Q
+//           Transposed, so that P^T and dS^T are what the products take from tensor memory and nothing is written to shared
+//           memory; lse and delta go by column and are read from shared memory.  P^T overwrites S^T and dS^T dP^T, half by half.
+// Queries:  S = Q K^T, dP = dO V^T;  dS as above, by rows;  dQ += dS K.  S is double-buffered; dS overwrites dP.
+
+template <int DT> struct BwdShape {
+  static constexpr int kSub = DT / 64;
+  static constexpr int kTile = kSub * TC_SUB;
+  static constexpr int kStages = DT == 64 ? 4 : 2;
+  static constexpr int kThreads = 320;
+  static constexpr int kBars = 1 + 3 * kStages + 6;
+  static constexpr int kRowBytes = kStages * 2 * TC_ROWS * 4;        // lse and delta of the query tiles in flight
+  static constexpr int kSmem = 2 * kTile + 2 * kStages * kTile + kRowBytes + 1024 + kBars * 8 + 16;
+};
+
+// the same halves of the depth as the 256 threads write: columns 0 .. 31 and 64 .. 95 of the region
+template <int DT> __device__ __forceinline__ void mma_ab_halves(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
+  const uint64_t base = desc_base(TC_SUB, 1024);
+#pragma unroll
+  for (int k = 0; k < TC_ROWS / 16; ++k) tc_mma_bf16_ta(d, a + (k >> 2) * 64 + (k & 3) * 8, desc_at(base, b + k * 2048), idesc, accumulate || k > 0);
+}
+// zeros in rows `valid` .. 127 of a tile, by one warp
+template <int DT> __device__ __forceinline__ void clear_rows(uint8_t* tile, int valid) {
+  for (int i = valid * 8 + (threadIdx.x & 31); i < TC_ROWS * 8; i += 32)
+#pragma unroll
+    for (int q = 0; q < DT / 64; ++q) *reinterpret_cast<uint4*>(tile + q * TC_SUB + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+}
+// half the columns of an accumulator row times f, to bf16 (NaN where a wait ran out)
+template <int DT> __device__ __forceinline__ void store_half(__nv_bfloat16* out, uint32_t taddr, int half, int dim, bool in, float f) {
+#pragma unroll
+  for (int q = 0; q < DT / 64; ++q) {
+    const int c0 = half * (DT / 2) + q * 32;
+    uint32_t o[32];
+    tmem_ld32(taddr + c0, o);
+    tmem_ld_wait();
+    if (in)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        if (c0 + g * 8 < dim) {
+          float v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(o[g * 8 + i]) * f;
+          *reinterpret_cast<uint4*>(out + c0 + g * 8) =
+              make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        }
+  }
+}
+
+struct TcBwdMaps { CUtensorMap q, k, v, d_o; };
+
+template <int DT>
+__global__ void __launch_bounds__(320, 1) attn_packed_dkv_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcBwdMaps maps) {
+  using S = BwdShape<DT>;
+  const int hk = blockIdx.x % a.kv_heads;
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.kv_heads, TC_ROWS);
+  if (s.tile < 0) { pdl_wait(); pdl_trigger(); return; }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int k0 = s.tile * TC_ROWS, i0 = a.causal ? s.tile : 0;
+  const int per_head = (s.len + TC_ROWS - 1) / TC_ROWS - i0, n_it = per_head * a.group;
+  auto head_of = [&](int it) { return hk * a.group + it / per_head; };
+  auto first_of = [&](int it) { return (i0 + it % per_head) * TC_ROWS; };
+
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  uint8_t* const sptr = smem_raw + (base - raw);
+  const uint32_t sK = base, sV = sK + S::kTile, sQ = sV + S::kTile, sO = sQ + S::kStages * S::kTile, srow = sO + S::kStages * S::kTile,
+                 bars = srow + S::kRowBytes;
+  float* const row_values = reinterpret_cast<float*>(sptr + (srow - base));      // [stage][lse, delta][128]
+  const uint32_t kv_full = bars;
+  auto full = [&](int i) { return bars + 8 * (1 + i); };
+  auto row_full = [&](int i) { return bars + 8 * (1 + S::kStages + i); };
+  auto empty = [&](int i) { return bars + 8 * (1 + 2 * S::kStages + i); };
+  const uint32_t s_full = bars + 8 * (1 + 3 * S::kStages), dp_full = s_full + 8, p_full = s_full + 16, ds_full = s_full + 24, acc_full = s_full + 32;
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(sptr + (bars - base) + 8 * S::kBars);
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* const status = &g_attn_packed_status;
+
+  if (threadIdx.x == 0) {
+    mbar_init(kv_full, 1);
+    for (int i = 0; i < S::kStages; ++i) { mbar_init(full(i), 1); mbar_init(row_full(i), 32); mbar_init(empty(i), 1); }
+    mbar_init(s_full, 1); mbar_init(dp_full, 1); mbar_init(p_full, 256); mbar_init(ds_full, 256); mbar_init(acc_full, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 9) {
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_wait();                                     // delta
+  pdl_trigger();
+  const uint32_t tmem = *tmem_slot, col_s = tmem, col_dp = tmem + 128, col_dv = tmem + 256, col_dk = tmem + 256 + DT;
+
+  if (warp == 8) {                                // ---- copies
+    int armed = 0;
+    bool ok = true;
+    if (elect_one()) {
+      mbar_arrive_expect_tx(kv_full, 2 * S::kTile);
+      load_tile<DT>(sK, &maps.k, kv_full, hk, s.begin + k0);
+      load_tile<DT>(sV, &maps.v, kv_full, hk, s.begin + k0);
+    }
+    __syncwarp();
+    for (int it = 0; it < n_it; ++it) {
+      const int st = it % S::kStages, h = head_of(it), q0 = first_of(it);
+      if (it >= S::kStages) ok = mbar_wait(empty(st), (it / S::kStages - 1) & 1, abort_flag, status, 51);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      if (elect_one()) {
+        mbar_arrive_expect_tx(full(st), 2 * S::kTile);
+        load_tile<DT>(sQ + st * S::kTile, &maps.q, full(st), h, s.begin + q0);
+        load_tile<DT>(sO + st * S::kTile, &maps.d_o, full(st), h, s.begin + q0);
+      }
+      __syncwarp();
+      ++armed;
+      float* rows = row_values + st * 2 * TC_ROWS;
+#pragma unroll
+      for (int i = 0; i < TC_ROWS; i += 32) {
+        const int r = q0 + i + lane;
+        const int64_t at = (int64_t)h * a.tokens + s.begin + r;
+        rows[i + lane] = r < s.len ? a.lse[at] * kLog2e : INFINITY;              // no row: probability zero
+        rows[TC_ROWS + i + lane] = r < s.len ? a.delta[at] : 0.f;
+      }
+      if (q0 + TC_ROWS > s.len) {                 // rows of other sequences, or of none: zeros, where P and dS are zero
+        ok = mbar_wait(full(st), (it / S::kStages) & 1, abort_flag, status, 52);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        clear_rows<DT>(sptr + (sQ - base) + st * S::kTile, s.len - q0);
+        clear_rows<DT>(sptr + (sO - base) + st * S::kTile, s.len - q0);
+        fence_async_smem();
+      }
+      mbar_arrive(row_full(st));
+    }
+    if (*abort_flag) {                            // nothing may be in flight when the block ends
+      volatile int never = 0;
+      mbar_wait(kv_full, 0, &never, status, 53);
+      for (int it = max(0, armed - S::kStages); it < armed; ++it) mbar_wait(full(it % S::kStages), (it / S::kStages) & 1, &never, status, 53);
+    }
+  } else if (warp == 9) {                         // ---- products
+    const uint32_t id_s = make_idesc_mn(128, 128, 0, 0), id_d = make_idesc_mn(128, DT, 0, 1);
+    auto ready = [&](int it) {
+      const int st = it % S::kStages;
+      return mbar_wait(full(st), (it / S::kStages) & 1, abort_flag, status, 54) && mbar_wait(row_full(st), (it / S::kStages) & 1, abort_flag, status, 55);
+    };
+    bool ok = mbar_wait(kv_full, 0, abort_flag, status, 56) && ready(0);
+    if (ok) {
+      tc_fence_after();
+      if (elect_one()) {
+        mma_abt<DT>(col_s, sK, sQ, id_s);
+        tc_commit(s_full);
+        mma_abt<DT>(col_dp, sV, sO, id_s);
+        tc_commit(dp_full);
+      }
+      __syncwarp();
+    }
+    for (int it = 0; it < n_it && ok; ++it) {
+      const int st = it % S::kStages, nx = (it + 1) % S::kStages;
+      const bool more = it + 1 < n_it;
+      ok = mbar_wait(p_full, it & 1, abort_flag, status, 57) && (!more || ready(it + 1));
+      if (!ok) break;
+      tc_fence_after();
+      if (elect_one()) {
+        mma_ab_halves<DT>(col_dv, col_s, sO + st * S::kTile, id_d, it > 0);
+        if (more) { mma_abt<DT>(col_s, sK, sQ + nx * S::kTile, id_s); tc_commit(s_full); }
+      }
+      __syncwarp();
+      ok = mbar_wait(ds_full, it & 1, abort_flag, status, 58);
+      if (!ok) break;
+      tc_fence_after();
+      if (elect_one()) {
+        mma_ab_halves<DT>(col_dk, col_dp, sQ + st * S::kTile, id_d, it > 0);
+        tc_commit(empty(st));
+        if (more) { mma_abt<DT>(col_dp, sV, sO + nx * S::kTile, id_s); tc_commit(dp_full); }
+        else tc_commit(acc_full);
+      }
+      __syncwarp();
+    }
+  } else {                                        // ---- values: thread = key row, half of the query columns
+    const int half = warp >> 2, r = threadIdx.x & 127, key = k0 + r;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const float c = a.scale * kLog2e;
+    bool ok = true;
+    for (int it = 0; it < n_it; ++it) {
+      const int st = it % S::kStages, q0 = first_of(it);
+      const bool diagonal = a.causal && q0 == k0;
+      const float* rows = row_values + st * 2 * TC_ROWS + half * 64;
+      ok = mbar_wait(row_full(st), (it / S::kStages) & 1, abort_flag, status, 59) && mbar_wait(s_full, it & 1, abort_flag, status, 60);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      float p[64];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        uint32_t v[32], w[16];
+        tmem_ld32(col_s + lanes + half * 64 + q * 32, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+          const float4 l = *reinterpret_cast<const float4*>(rows + q * 32 + i);
+          const float2 x = fma_f32x2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(c, c), make_float2(-l.x, -l.y));
+          const float2 y = fma_f32x2(make_float2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), make_float2(c, c), make_float2(-l.z, -l.w));
+          p[q * 32 + i] = ex2(x.x); p[q * 32 + i + 1] = ex2(x.y); p[q * 32 + i + 2] = ex2(y.x); p[q * 32 + i + 3] = ex2(y.y);
+        }
+        if (diagonal)
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (half * 64 + q * 32 + i < r) p[q * 32 + i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = pack_bf16(p[q * 32 + 2 * i], p[q * 32 + 2 * i + 1]);
+        tmem_st16(col_s + lanes + half * 64 + q * 16, w);      // columns of this half that are in registers by now
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      mbar_arrive(p_full);
+      ok = mbar_wait(dp_full, it & 1, abort_flag, status, 61);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        uint32_t v[32], w[16];
+        tmem_ld32(col_dp + lanes + half * 64 + q * 32, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+          const float4 d = *reinterpret_cast<const float4*>(rows + TC_ROWS + q * 32 + i);
+          const float2 x = add_f32x2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(-d.x, -d.y));
+          const float2 y = add_f32x2(make_float2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), make_float2(-d.z, -d.w));
+          w[i / 2] = pack_bf16(p[q * 32 + i] * x.x, p[q * 32 + i + 1] * x.y);
+          w[i / 2 + 1] = pack_bf16(p[q * 32 + i + 2] * y.x, p[q * 32 + i + 3] * y.y);
+        }
+        tmem_st16(col_dp + lanes + half * 64 + q * 16, w);
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      mbar_arrive(ds_full);
+    }
+    if (ok) ok = mbar_wait(acc_full, 0, abort_flag, status, 62);
+    ok = __all_sync(0xffffffffu, ok);
+    tc_fence_after();
+    const bool in = key < s.len;
+    const float bad = ok ? 1.f : NAN;
+    store_half<DT>(head_row_out<__nv_bfloat16>(a.dv, s.begin + key, hk), col_dv + lanes, half, a.dim, in, bad);
+    store_half<DT>(head_row_out<__nv_bfloat16>(a.dk, s.begin + key, hk), col_dk + lanes, half, a.dim, in, a.scale * bad);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(320, 1) attn_packed_dq_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcBwdMaps maps) {
+  using S = BwdShape<DT>;
+  const int h = blockIdx.x % a.heads, hk = h / a.group;
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.heads, TC_ROWS);
+  if (s.tile < 0) { pdl_wait(); return; }
+  const int tile = (s.len + TC_ROWS - 1) / TC_ROWS - 1 - s.tile;                 // the tiles that see the most keys first
+  const int warp = threadIdx.x >> 5;
+  const int q0 = tile * TC_ROWS, n_it = ((a.causal ? min(s.len, q0 + TC_ROWS) : s.len) + TC_ROWS - 1) / TC_ROWS;
+
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  uint8_t* const sptr = smem_raw + (base - raw);
+  const uint32_t sQ = base, sO = sQ + S::kTile, sK = sO + S::kTile, sV = sK + S::kStages * S::kTile, bars = sV + S::kStages * S::kTile;
+  const uint32_t q_full = bars;
+  auto full = [&](int i) { return bars + 8 * (1 + i); };
+  auto cleared = [&](int i) { return bars + 8 * (1 + S::kStages + i); };
+  auto empty = [&](int i) { return bars + 8 * (1 + 2 * S::kStages + i); };
+  const uint32_t s_full = bars + 8 * (1 + 3 * S::kStages), dp_full = s_full + 16, ds_full = s_full + 24, acc_full = s_full + 32;   // s_full: two
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(sptr + (bars - base) + 8 * S::kBars);
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* const status = &g_attn_packed_status;
+
+  if (threadIdx.x == 0) {
+    mbar_init(q_full, 1);
+    for (int i = 0; i < S::kStages; ++i) { mbar_init(full(i), 1); mbar_init(cleared(i), 32); mbar_init(empty(i), 1); }
+    mbar_init(s_full, 1); mbar_init(s_full + 8, 1); mbar_init(dp_full, 1); mbar_init(ds_full, 256); mbar_init(acc_full, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 9) {
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot, col_s = tmem, col_dp = tmem + 256, col_dq = tmem + 384;
+
+  if (warp == 8) {                                // ---- copies
+    int armed = 0;
+    bool ok = true;
+    if (elect_one()) {
+      mbar_arrive_expect_tx(q_full, 2 * S::kTile);
+      load_tile<DT>(sQ, &maps.q, q_full, h, s.begin + q0);
+      load_tile<DT>(sO, &maps.d_o, q_full, h, s.begin + q0);
+    }
+    __syncwarp();
+    for (int it = 0; it < n_it; ++it) {
+      const int st = it % S::kStages, k0 = it * TC_ROWS;
+      if (it >= S::kStages) ok = mbar_wait(empty(st), (it / S::kStages - 1) & 1, abort_flag, status, 71);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      if (elect_one()) {
+        mbar_arrive_expect_tx(full(st), 2 * S::kTile);
+        load_tile<DT>(sK + st * S::kTile, &maps.k, full(st), hk, s.begin + k0);
+        load_tile<DT>(sV + st * S::kTile, &maps.v, full(st), hk, s.begin + k0);
+      }
+      __syncwarp();
+      ++armed;
+      if (k0 + TC_ROWS > s.len) {                 // keys of other sequences, or of none: zeros, where dS is zero
+        ok = mbar_wait(full(st), (it / S::kStages) & 1, abort_flag, status, 72);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        clear_rows<DT>(sptr + (sK - base) + st * S::kTile, s.len - k0);
+        fence_async_smem();
+      }
+      mbar_arrive(cleared(st));
+    }
+    if (*abort_flag) {                            // nothing may be in flight when the block ends
+      volatile int never = 0;
+      mbar_wait(q_full, 0, &never, status, 73);
+      for (int it = max(0, armed - S::kStages); it < armed; ++it) mbar_wait(full(it % S::kStages), (it / S::kStages) & 1, &never, status, 73);
+    }
+  } else if (warp == 9) {                         // ---- products
+    const uint32_t id_s = make_idesc_mn(128, 128, 0, 0), id_d = make_idesc_mn(128, DT, 0, 1);
+    auto ready = [&](int it) {
+      const int st = it % S::kStages;
+      return mbar_wait(full(st), (it / S::kStages) & 1, abort_flag, status, 74) && mbar_wait(cleared(st), (it / S::kStages) & 1, abort_flag, status, 75);
+    };
+    bool ok = mbar_wait(q_full, 0, abort_flag, status, 76) && ready(0) && (n_it < 2 || ready(1));
+    if (ok) {
+      tc_fence_after();
+      if (elect_one()) {
+        mma_abt<DT>(col_s, sQ, sK, id_s);
+        tc_commit(s_full);
+        mma_abt<DT>(col_dp, sO, sV, id_s);
+        tc_commit(dp_full);
+        if (n_it > 1) { mma_abt<DT>(col_s + 128, sQ, sK + (1 % S::kStages) * S::kTile, id_s); tc_commit(s_full + 8); }
+      }
+      __syncwarp();
+    }
+    for (int it = 0; it < n_it && ok; ++it) {
+      const int st = it % S::kStages, nx = (it + 1) % S::kStages, n2 = (it + 2) % S::kStages;
+      ok = mbar_wait(ds_full, it & 1, abort_flag, status, 77);
+      if (!ok) break;
+      tc_fence_after();
+      if (elect_one()) {
+        mma_ab_halves<DT>(col_dq, col_dp, sK + st * S::kTile, id_d, it > 0);
+        tc_commit(empty(st));
+        if (it + 1 < n_it) { mma_abt<DT>(col_dp, sO, sV + nx * S::kTile, id_s); tc_commit(dp_full); }
+        else tc_commit(acc_full);
+      }
+      __syncwarp();
+      if (it + 2 < n_it) {                        // the values of it have left this half of S
+        ok = ready(it + 2);
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) { mma_abt<DT>(col_s + (it & 1) * 128, sQ, sK + n2 * S::kTile, id_s); tc_commit(s_full + 8 * (it & 1)); }
+        __syncwarp();
+      }
+    }
+  } else {                                        // ---- values: thread = query row, half of the key columns
+    const int half = warp >> 2, r = threadIdx.x & 127, row = q0 + r;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const float c = a.scale * kLog2e;
+    const int64_t at = (int64_t)h * a.tokens + s.begin + row;
+    const float lse = row < s.len ? a.lse[at] * kLog2e : INFINITY, delta = row < s.len ? a.delta[at] : 0.f;
+    const int limit = a.causal ? min(s.len, row + 1) : s.len;
+    bool ok = true;
+    for (int it = 0; it < n_it; ++it) {
+      const int k0 = it * TC_ROWS;
+      const bool edge = k0 + TC_ROWS > s.len || (a.causal && k0 + TC_ROWS > q0 + 1);
+      ok = mbar_wait(s_full + 8 * (it & 1), (it >> 1) & 1, abort_flag, status, 78);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      float p[64];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        uint32_t v[32];
+        tmem_ld32(col_s + lanes + (it & 1) * 128 + half * 64 + q * 32, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+          const float2 x = fma_f32x2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(c, c), make_float2(-lse, -lse));
+          p[q * 32 + i] = ex2(x.x); p[q * 32 + i + 1] = ex2(x.y);
+        }
+      }
+      ok = mbar_wait(dp_full, it & 1, abort_flag, status, 79);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        uint32_t v[32], w[16];
+        tmem_ld32(col_dp + lanes + half * 64 + q * 32, v);
+        tmem_ld_wait();
+        float ds[32];
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+          const float2 x = add_f32x2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(-delta, -delta));
+          ds[i] = p[q * 32 + i] * x.x; ds[i + 1] = p[q * 32 + i + 1] * x.y;
+        }
+        if (edge)
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (k0 + half * 64 + q * 32 + i >= limit) ds[i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = pack_bf16(ds[2 * i], ds[2 * i + 1]);
+        tmem_st16(col_dp + lanes + half * 64 + q * 16, w);
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      mbar_arrive(ds_full);
+    }
+    if (ok) ok = mbar_wait(acc_full, 0, abort_flag, status, 80);
+    ok = __all_sync(0xffffffffu, ok);
+    tc_fence_after();
+    store_half<DT>(head_row_out<__nv_bfloat16>(a.dq, s.begin + row, h), col_dq + lanes, half, a.dim, row < s.len, ok ? a.scale : NAN);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+  pdl_wait();
+}
+
+// delta_i = do_i . o_i: eight lanes a row; rows outside the sequences get a value that nothing reads
+__global__ void __launch_bounds__(256) attn_packed_delta_tc_kernel(const __grid_constant__ PackedArgs a) {
+  const int64_t i = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3);
+  const int part = threadIdx.x & 7;
+  const bool in = i < a.tokens * a.heads;
+  const int64_t token = in ? i / a.heads : 0;
+  const int h = in ? (int)(i - token * a.heads) : 0;
+  const __nv_bfloat16 *x = head_row<__nv_bfloat16>(a.o, token, h), *y = head_row<__nv_bfloat16>(a.d_o, token, h);
+  float sum = 0.f;
+  for (int c = part * 8; c < a.dim; c += 64) {
+    float u[8], w[8];
+    load8(x + c, u);
+    load8(y + c, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fmaf(u[e], w[e], sum);
+  }
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (in && part == 0) a.delta[(int64_t)h * a.tokens + token] = sum;
+}
+
 // ---- host side --------------------------------------------------------------------------------------------------
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -363,9 +825,11 @@ static bool tc_view(const HeadView& x, int heads, int64_t tokens) {
 }
 
 bool attn_packed_tc_takes(const PackedArgs& a, int dtype, bool backward) {
-  if (backward) return false;
-  return dtype == PM_BF16 && a.dim % 8 == 0 && tc_view(a.q, a.heads, a.tokens) && tc_view(a.k, a.kv_heads, a.tokens) &&
-         tc_view(a.v, a.kv_heads, a.tokens) && tc_view(a.o, a.heads, a.tokens);
+  const bool inputs = dtype == PM_BF16 && a.dim % 8 == 0 && tc_view(a.q, a.heads, a.tokens) && tc_view(a.k, a.kv_heads, a.tokens) &&
+                      tc_view(a.v, a.kv_heads, a.tokens) && tc_view(a.o, a.heads, a.tokens);
+  if (!inputs || !backward) return inputs;
+  return tc_view(a.d_o, a.heads, a.tokens) && tc_view(a.dq, a.heads, a.tokens) && tc_view(a.dk, a.kv_heads, a.tokens) &&
+         tc_view(a.dv, a.kv_heads, a.tokens);
 }
 
 template <typename K> static cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>& done) {
@@ -399,7 +863,27 @@ cudaError_t attn_packed_tc_forward(const PackedArgs& a, cudaStream_t st) {
   return two ? fwd_launch<128, 2>(a, st) : fwd_launch<128, 1>(a, st);
 }
 
-cudaError_t attn_packed_tc_backward(const PackedArgs&, cudaStream_t) { return cudaErrorNotSupported; }
+template <int DT> static cudaError_t bwd_launch(const PackedArgs& a, cudaStream_t st) {
+  static std::atomic<uint64_t> done[2];
+  using S = BwdShape<DT>;
+  TcBwdMaps maps;
+  cudaError_t e = allow_smem(attn_packed_dkv_tc_kernel<DT>, S::kSmem, done[0]);
+  if (e == cudaSuccess) e = allow_smem(attn_packed_dq_tc_kernel<DT>, S::kSmem, done[1]);
+  if (e == cudaSuccess) e = encode_heads(&maps.q, a.q, a.dim, a.heads, a.tokens);
+  if (e == cudaSuccess) e = encode_heads(&maps.k, a.k, a.dim, a.kv_heads, a.tokens);
+  if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.tokens);
+  if (e == cudaSuccess) e = encode_heads(&maps.d_o, a.d_o, a.dim, a.heads, a.tokens);
+  if (e != cudaSuccess) return e;
+  const int64_t tiles = most_tiles(a.tokens, a.n_seqs, TC_ROWS);
+  if (tiles * a.heads > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  e = launch_pdl(attn_packed_delta_tc_kernel, dim3((unsigned)((a.tokens * a.heads + 31) / 32)), dim3(256), 0, st, false, a);
+  // The second kernel starts once every block of the first has passed its wait for delta, so its blocks fill the SMs that the first's last
+  // and longest blocks leave; it ends behind the first.
+  if (e == cudaSuccess) e = launch_pdl(attn_packed_dkv_tc_kernel<DT>, dim3((unsigned)(tiles * a.kv_heads)), dim3(S::kThreads), S::kSmem, st, true, a, maps);
+  if (e == cudaSuccess) e = launch_pdl(attn_packed_dq_tc_kernel<DT>, dim3((unsigned)(tiles * a.heads)), dim3(S::kThreads), S::kSmem, st, true, a, maps);
+  return e;
+}
+cudaError_t attn_packed_tc_backward(const PackedArgs& a, cudaStream_t st) { return a.dim <= 64 ? bwd_launch<64>(a, st) : bwd_launch<128>(a, st); }
 
 cudaError_t attn_packed_status(int* code, cudaStream_t st) {
   *code = 0;
