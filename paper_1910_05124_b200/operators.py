@@ -7,7 +7,6 @@ graph.  As with any CUDA call, a tensor that another stream still writes has to 
 arguments raise PipeMareError.
 """
 import ctypes as C
-import math
 
 import torch
 
@@ -20,61 +19,62 @@ def _refuse(message, status="PM_ERR_INVALID_ARG"):
     raise PipeMareError(status, message)
 
 
-def _tensor(name, t, dtype, device, shape=None):
+def _mismatch(name, t, dtype, device, shape):
+    """Refuses a tensor that is not of this type, device and shape."""
     if not isinstance(t, torch.Tensor):
         _refuse(f"{name} must be a tensor")
     if t.device != device:
         _refuse(f"{name} is on {t.device}, expected {device}")
     if t.dtype != dtype:
         _refuse(f"{name} is {t.dtype}, expected {dtype}")
-    if shape is not None and tuple(t.shape) != shape:
+    if tuple(t.shape) != shape:
         _refuse(f"{name} has shape {tuple(t.shape)}, expected {shape}", "PM_ERR_SHAPE")
-    return t
+    _refuse(f"{name} must be contiguous")
 
 
 def _flat(name, t, dtype, device, shape):
     """Data pointer of a contiguous tensor; None for None."""
     if t is None:
         return None
-    if not _tensor(name, t, dtype, device, shape).is_contiguous():
-        _refuse(f"{name} must be contiguous")
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and t.shape == shape and t.is_contiguous()):
+        _mismatch(name, t, dtype, device, shape)
     return t.data_ptr()
 
 
 def _compute_device(name, t):
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
         _refuse(f"{name} must be a CUDA tensor")
     if t.dtype not in _DTYPES:
         _refuse(f"{name} is {t.dtype}; float32 and bfloat16 are supported", "PM_ERR_UNSUPPORTED")
     return t.device
 
 
-class _Launch:
-    """The stream of a call, with its device current while the call lasts."""
+# the handle of the current stream without the object around it, where this torch has the call
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
-    def __init__(self, device, stream):
-        if stream is not None and stream.device != device:
+
+def _launch(call, device, stream, workspace=0):
+    """call(stream handle[, workspace pointer]) with the tensors' device current, and its status checked.
+
+    The workspace is device scratch of this call alone: it comes from the allocator's pool of the launching stream, so the
+    memory is reused only by work queued behind the call (under capture it stays with the graph)."""
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _launch(call, device, stream, workspace)
+    if stream is None:
+        handle = _raw_stream(device.index)
+    else:
+        if stream.device != device:
             _refuse(f"the stream belongs to {stream.device}, the tensors to {device}")
-        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
-        self.other = device.index != torch.cuda.current_device()
-        self.guard = torch.cuda.device(device) if self.other else None
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return C.c_void_p(self.stream.cuda_stream)
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
-
-    def workspace(self, n_bytes, device):
-        """Device scratch of this call alone: from the allocator's pool of the launching stream, so that the memory is reused only
-        by work queued behind the call (or, under capture, stays with the graph)."""
-        if self.stream == torch.cuda.current_stream(device):
-            return torch.empty(max(n_bytes, 16), dtype=torch.uint8, device=device)
-        with torch.cuda.stream(self.stream):
-            return torch.empty(max(n_bytes, 16), dtype=torch.uint8, device=device)
+        handle = stream.cuda_stream
+    if not workspace:
+        return _check(call(handle))
+    if stream is None or handle == _raw_stream(device.index):
+        scratch = torch.empty(workspace, dtype=torch.uint8, device=device)
+    else:
+        with torch.cuda.stream(stream):
+            scratch = torch.empty(workspace, dtype=torch.uint8, device=device)
+    return _check(call(handle, scratch.data_ptr()))
 
 
 class PackedAttention:
@@ -105,55 +105,53 @@ class PackedAttention:
             _refuse(f"q has shape {tuple(q.shape)}, expected [tokens, {self.n_heads}, {self.head_dim}]", "PM_ERR_SHAPE")
         if not isinstance(cu_seqlens, torch.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.numel() < 1:
             _refuse("cu_seqlens must be a one-dimensional tensor of sequences + 1 entries", "PM_ERR_SHAPE")
-        cu = _flat("cu_seqlens", cu_seqlens, torch.int32, device, tuple(cu_seqlens.shape))
-        d = pm_attention_desc(_DTYPES[q.dtype], self.n_heads, self.n_kv_heads, self.head_dim, cu_seqlens.numel() - 1, int(self.causal),
-                              q.shape[0], self.scale)
-        return device, d, cu
+        cu = _flat("cu_seqlens", cu_seqlens, torch.int32, device, cu_seqlens.shape)
+        return device, pm_attention_desc(_DTYPES[q.dtype], self.n_heads, self.n_kv_heads, self.head_dim, cu_seqlens.numel() - 1, self.causal,
+                                         q.shape[0], self.scale), cu
 
     def _view(self, name, t, q, heads, written=False):
-        _tensor(name, t, q.dtype, q.device, (q.shape[0], heads, self.head_dim))
+        shape = (q.shape[0], heads, self.head_dim)
+        if not (isinstance(t, torch.Tensor) and t.dtype is q.dtype and t.device == q.device and t.shape == shape):
+            _mismatch(name, t, q.dtype, q.device, shape)
         token, head, one = t.stride()
         if one != 1 and self.head_dim > 1:
             _refuse(f"the last dimension of {name} must be contiguous")
-        if written and t.numel() > 0:
+        if written and not (head == self.head_dim and token >= heads * head):
             # rows of one head, or heads of one row, must not share elements
-            a, b = sorted(((token, t.shape[0]), (head, heads)))
-            a, b = [s for s, n in (a, b) if n > 1] or [self.head_dim], (b, a)
-            if a[0] < self.head_dim or (len(a) > 1 and a[1] < a[0] * (b[1][1] - 1) + self.head_dim):
-                _refuse(f"{name} overlaps itself")
-        return pm_head_view(t.data_ptr(), token, head)
+            spread = sorted((s, n) for s, n in ((token, shape[0]), (head, heads)) if n > 1)
+            end = self.head_dim
+            for s, n in spread if shape[0] else ():
+                if s < end:
+                    _refuse(f"{name} overlaps itself")
+                end = s * (n - 1) + end
+        return C.byref(pm_head_view(t.data_ptr(), token, head))
 
     def pm_attention_packed_forward(self, q, k, v, cu_seqlens, o, lse=None, stream=None):
         """Writes o and, for a backward pass, lse."""
         device, d, cu = self._desc(q, cu_seqlens)
-        views = [C.byref(self._view(n, t, q, h)) for n, t, h in (("q", q, self.n_heads), ("k", k, self.n_kv_heads), ("v", v, self.n_kv_heads))]
-        out = self._view("o", o, q, self.n_heads, written=True)
-        p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, q.shape[0]))
-        with _Launch(device, stream) as st:
-            _check(self.L.pm_attention_packed_forward(C.byref(d), *views, cu, C.byref(out), p_lse, st))
+        H, K, view = self.n_heads, self.n_kv_heads, self._view
+        args = (C.byref(d), view("q", q, q, H), view("k", k, q, K), view("v", v, q, K), cu, view("o", o, q, H, True),
+                _flat("lse", lse, torch.float32, device, (H, q.shape[0])))
+        _launch(lambda st: self.L.pm_attention_packed_forward(*args, st), device, stream)
 
     def pm_attention_packed_backward(self, q, k, v, o, lse, d_o, cu_seqlens, dq, dk, dv, stream=None):
         """Writes dq, dk and dv from d_o and what the forward call wrote."""
         device, d, cu = self._desc(q, cu_seqlens)
-        H, K = self.n_heads, self.n_kv_heads
-        vq, vk, vv, vo, vdo = (C.byref(self._view(n, t, q, h)) for n, t, h in (("q", q, H), ("k", k, K), ("v", v, K), ("o", o, H), ("d_o", d_o, H)))
-        wq, wk, wv = (C.byref(self._view(n, t, q, h, written=True)) for n, t, h in (("dq", dq, H), ("dk", dk, K), ("dv", dv, K)))
         if lse is None:
             _refuse("lse must be a tensor")
-        p_lse = _flat("lse", lse, torch.float32, device, (H, q.shape[0]))
-        need = self.L.pm_attention_packed_workspace_bytes(C.byref(d))
-        launch = _Launch(device, stream)
-        with launch as st:
-            ws = launch.workspace(need, device)
-            _check(self.L.pm_attention_packed_backward(C.byref(d), vq, vk, vv, vo, p_lse, vdo, cu, wq, wk, wv, ws.data_ptr(), need, st))
+        H, K, view = self.n_heads, self.n_kv_heads, self._view
+        args = (C.byref(d), view("q", q, q, H), view("k", k, q, K), view("v", v, q, K), view("o", o, q, H),
+                _flat("lse", lse, torch.float32, device, (H, q.shape[0])), view("d_o", d_o, q, H), cu,
+                view("dq", dq, q, H, True), view("dk", dk, q, K, True), view("dv", dv, q, K, True))
+        need = self.L.pm_attention_packed_workspace_bytes(args[0])
+        _launch(lambda st, ws=None: self.L.pm_attention_packed_backward(*args, ws, need, st), device, stream, need)
 
     def pm_attention_packed_status(self, device="cuda", stream=None):
         """Raises if a device-side wait of a tensor-core kernel ran out since the last call (a defect); synchronises the stream."""
         device = torch.device(device)
         if device.index is None:
             device = torch.device("cuda", torch.cuda.current_device())
-        with _Launch(device, stream) as st:
-            _check(self.L.pm_attention_packed_status(st))
+        _launch(self.L.pm_attention_packed_status, device, stream)
 
 
 class TokenLogProbs:
@@ -174,13 +172,15 @@ class TokenLogProbs:
 
     def _rows(self, name, t, like=None):
         device = _compute_device(name, t)
-        if like is not None:
-            _tensor(name, t, like.dtype, like.device, tuple(like.shape))
+        if like is not None and not (t.dtype is like.dtype and t.device == like.device and t.shape == like.shape):
+            _mismatch(name, t, like.dtype, like.device, tuple(like.shape))
         if t.dim() != 2 or t.shape[1] != self.vocab:
             _refuse(f"{name} has shape {tuple(t.shape)}, expected [rows, {self.vocab}]", "PM_ERR_SHAPE")
-        if self.vocab > 1 and t.stride(1) != 1:
+        stride, one = t.stride()
+        if one != 1 and self.vocab > 1:
             _refuse(f"the rows of {name} must be contiguous")
-        stride = t.stride(0) if t.shape[0] > 1 else self.vocab
+        if t.shape[0] < 2:
+            stride = self.vocab
         if stride < self.vocab:
             _refuse(f"the rows of {name} overlap")
         return device, stride
@@ -188,15 +188,13 @@ class TokenLogProbs:
     def pm_token_logprobs(self, logits, targets, logprob, entropy=None, lse=None, top_logprob=None, top_ids=None, stream=None):
         """Writes logprob (targets and logprob may both be None) and whichever of the others are given."""
         device, stride = self._rows("logits", logits)
-        n, k = logits.shape[0], self.top_k
+        n, k, f32, i32 = logits.shape[0], self.top_k, torch.float32, torch.int32
         if k and (top_logprob is None or top_ids is None):
             _refuse("top_logprob and top_ids must be given with top_k")
-        f32, i32 = torch.float32, torch.int32
-        with _Launch(device, stream) as st:
-            _check(self.L.pm_token_logprobs(
-                logits.data_ptr(), _DTYPES[logits.dtype], n, self.vocab, stride, _flat("targets", targets, i32, device, (n,)),
+        args = (logits.data_ptr(), _DTYPES[logits.dtype], n, self.vocab, stride, _flat("targets", targets, i32, device, (n,)),
                 _flat("logprob", logprob, f32, device, (n,)), _flat("entropy", entropy, f32, device, (n,)), _flat("lse", lse, f32, device, (n,)),
-                k, _flat("top_logprob", top_logprob, f32, device, (n, k)), _flat("top_ids", top_ids, i32, device, (n, k)), st))
+                k, _flat("top_logprob", top_logprob, f32, device, (n, k)), _flat("top_ids", top_ids, i32, device, (n, k)))
+        _launch(lambda st: self.L.pm_token_logprobs(*args, st), device, stream)
 
     def pm_token_logprobs_backward(self, logits, targets, lse, d_logits, d_logprob=None, entropy=None, d_entropy=None, stream=None):
         """Writes d_logits (logits itself is allowed) from the gradients of logprob and / or of the entropy."""
@@ -207,12 +205,11 @@ class TokenLogProbs:
             _refuse("lse must be a tensor")
         if logits.data_ptr() == d_logits.data_ptr() and stride != grad_stride:
             _refuse("d_logits shares the memory of logits at other strides")
-        with _Launch(device, stream) as st:
-            _check(self.L.pm_token_logprobs_backward(
-                logits.data_ptr(), _DTYPES[logits.dtype], n, self.vocab, stride, _flat("targets", targets, torch.int32, device, (n,)),
+        args = (logits.data_ptr(), _DTYPES[logits.dtype], n, self.vocab, stride, _flat("targets", targets, torch.int32, device, (n,)),
                 _flat("lse", lse, f32, device, (n,)), _flat("entropy", entropy, f32, device, (n,)),
                 _flat("d_logprob", d_logprob, f32, device, (n,)), _flat("d_entropy", d_entropy, f32, device, (n,)),
-                d_logits.data_ptr(), grad_stride, st))
+                d_logits.data_ptr(), grad_stride)
+        _launch(lambda st: self.L.pm_token_logprobs_backward(*args, st), device, stream)
 
 
 class GradClip:
@@ -237,8 +234,8 @@ class GradClip:
         spans = []
         for i, (g, o) in enumerate(zip(grads, outs)):
             for name, t in ((f"grads[{i}]", g), (f"outs[{i}]", o)):
-                _compute_device(name, t)
-                _tensor(name, t, t.dtype, self.device)
+                if _compute_device(name, t) != self.device:
+                    _refuse(f"{name} is on {t.device}, expected {self.device}")
                 if not t.is_contiguous():
                     _refuse(f"{name} must be contiguous")
             if g.numel() != o.numel():
@@ -261,11 +258,13 @@ class GradClip:
     def pm_clip_gradients(self, max_norm, norm, scale, stream=None):
         """Writes outs, the norm before clipping, and the factor (float32 tensors of one element)."""
         max_norm = float(max_norm)
-        if not max_norm > 0 or math.isnan(max_norm):
+        if not max_norm > 0:
             _refuse("max_norm must be positive")
-        p_norm, p_scale = (_flat(n, t, torch.float32, self.device, tuple(t.shape) if isinstance(t, torch.Tensor) and t.numel() == 1 else (1,))
+        p_norm, p_scale = (_flat(n, t, torch.float32, self.device, t.shape if isinstance(t, torch.Tensor) and t.numel() == 1 else (1,))
                            for n, t in (("norm", norm), ("scale", scale)))
-        launch = _Launch(self.device, stream)
-        with launch as st:
-            ws = launch.workspace(self.ws_bytes, self.device)
-            _check(self.L.pm_clip_gradients(self.tensors, len(self.tensors), max_norm, p_norm, p_scale, ws.data_ptr(), self.ws_bytes, st))
+        if p_norm is None or p_scale is None:
+            _refuse("norm and scale must be tensors")
+        if p_norm == p_scale:
+            _refuse("norm and scale share their memory")
+        _launch(lambda st, ws: self.L.pm_clip_gradients(self.tensors, len(self.tensors), max_norm, p_norm, p_scale, ws, self.ws_bytes, st),
+                self.device, stream, self.ws_bytes)
