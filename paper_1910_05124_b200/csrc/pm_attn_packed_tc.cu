@@ -10,8 +10,8 @@
 // only when a row of the warp outgrows it by 2^8: P then reaches at most 256, which bf16 holds as exactly as 1, and most key tiles
 // leave O alone.
 //
-// Products that read P are issued before the product that overwrites it, and products complete in the order of their issue, so a
-// commit behind S(j + 1) also says that O holds tile j.
+// Where P lies over S, products that read P are issued before the product that overwrites it, and products complete in the order of
+// their issue, so a commit behind S(j + 1) also says that O holds tile j.
 #include <atomic>
 #include <mutex>
 
@@ -24,17 +24,37 @@ namespace pm {
 __device__ int g_attn_packed_status;
 
 constexpr int TC_ROWS = 128;                      // rows of a tile, of queries and of keys
-constexpr int FWD_P = 64;                         // first column of P within S's 128
 constexpr int TC_SUB = TC_ROWS * 128;             // bytes of a [128 x 64] bf16 sub-tile, 128-byte swizzle
+
+// A bounded wait in line: a call from a thread that holds a row of scores would have to put them away.
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity)) {
+    if (*abort_flag) return false;
+    if (clock64() - t0 > WAIT_LIMIT_CYCLES) {
+      *abort_flag = 1;
+      atomicCAS(status, 0, code);
+      return false;
+    }
+  }
+  return true;
+}
 
 template <int DT, int NT> struct FwdShape {
   static constexpr int kSub = DT / 64;            // sub-tiles of a tile
   static constexpr int kTile = kSub * TC_SUB;
   static constexpr int kStages = NT == 1 ? (DT == 64 ? 2 : 1) : (DT == 64 ? 4 : 2);
-  static constexpr int kThreads = NT * 128 + 64;
+  static constexpr int kThreads = NT * 128 + 128;
   static constexpr int kBlocks = NT == 1 ? 2 : 1; // per SM
-  static constexpr int kCols = NT * 256;          // tensor-memory columns: S (128 each), then O (DT each)
-  static constexpr int kBars = 1 + 4 * kStages + 3 * NT;
+  // registers: a softmax thread holds a row of 128 scores, the warps that copy and issue need few
+  // (NT = 2: 384 threads at 168, 2 x 128 x 224 + 128 x 48 below that; NT = 1: 256 at 128, 128 x 208 + 128 x 48)
+  static constexpr int kSoftmaxRegs = NT == 1 ? 208 : 224, kOtherRegs = 48;
+  // Tensor-memory columns: S (128 for each tile), O (DT), and for heads of 64 P (64) beside S instead of over it, so that the
+  // next scores are formed while the exponentials of these are.
+  static constexpr int kCols = NT * 256;
+  static constexpr bool kApart = DT == 64;
+  static constexpr int kBars = 1 + 4 * kStages + 5 * NT;
   static constexpr int kSmem = NT * kTile + 2 * kStages * kTile + 1024 + kBars * 8 + 16;
 };
 
@@ -50,10 +70,10 @@ template <int DT> __device__ __forceinline__ void mma_abt(uint32_t d, uint32_t a
   }
 }
 // 128 x DT x 128 product of A in tensor memory and a tile whose rows run along the depth
-template <int DT> __device__ __forceinline__ void mma_ab(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
+template <int DT> __device__ __forceinline__ void mma_ab(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate, int k0, int k1) {
   const uint64_t base = desc_base(TC_SUB, 1024);
 #pragma unroll
-  for (int k = 0; k < TC_ROWS / 16; ++k) tc_mma_bf16_ta(d, a + k * 8, desc_at(base, b + k * 2048), idesc, accumulate || k > 0);
+  for (int k = k0; k < k1; ++k) tc_mma_bf16_ta(d, a + k * 8, desc_at(base, b + k * 2048), idesc, accumulate || k > k0);
 }
 
 template <int DT> __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int64_t token) {
@@ -61,6 +81,11 @@ template <int DT> __device__ __forceinline__ void load_tile(uint32_t dst, const 
   for (int i = 0; i < DT / 64; ++i) tma_load_3d(dst + i * TC_SUB, map, bar, i * 64, head, (int)token);
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 // c s - m for two values at a time
 __device__ __forceinline__ float2 fma_f32x2(float2 a, float2 b, float2 c) {
   float2 r;
@@ -69,6 +94,26 @@ __device__ __forceinline__ float2 fma_f32x2(float2 a, float2 b, float2 c) {
       : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return r;
 }
+
+// 2^x for two values on the FMA units: x = n + f with n the nearest integer, 2^f by the polynomial of degree 4 with the least relative
+// error on [-1/2, 1/2] (2.6e-6, a 700th of bf16's half step; found by iteratively reweighted least squares), n added to the exponent.
+// x is at most 8 here; below -126 the result is 2^-126 where the exponential unit gives zero.
+__device__ __forceinline__ float2 ex2_fma(float2 x) {
+  const float magic = 12582912.f;                 // 1.5 * 2^23: the sum's low bits are the nearest integer
+  x.x = fmaxf(x.x, -126.f); x.y = fmaxf(x.y, -126.f);
+  const float2 t = add_f32x2(x, make_float2(magic, magic)), n = add_f32x2(t, make_float2(-magic, -magic));
+  const float2 f = fma_f32x2(n, make_float2(-1.f, -1.f), x);
+  float2 p = fma_f32x2(make_float2(0.00957010220736f, 0.00957010220736f), f, make_float2(0.0559178628027f, 0.0559178628027f));
+  p = fma_f32x2(p, f, make_float2(0.240247443318f, 0.240247443318f));
+  p = fma_f32x2(p, f, make_float2(0.693121790886f, 0.693121790886f));
+  p = fma_f32x2(p, f, make_float2(0.999999284744f, 0.999999284744f));
+  return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)),
+                     __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+}
+
+// Which of a thread's 16 pairs of a quarter row take the FMA units, as a mask: one in eight.  8192 tokens, 16 heads, causal, us for
+// none / 1/8 / 1/4 / 3/8 / 1/2: heads of 128 230 / 231 / 229 / 235 / 244, heads of 64 211 / 191 / 200 / 198 / 206.
+constexpr uint32_t FWD_FMA = 0x8080;
 
 template <int DT, int NT>
 __global__ void __launch_bounds__(FwdShape<DT, NT>::kThreads, FwdShape<DT, NT>::kBlocks)
@@ -103,6 +148,8 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
   auto s_full = [&](int t) { return bars + 8 * (1 + 4 * S::kStages + t); };
   auto p_full = [&](int t) { return bars + 8 * (1 + 4 * S::kStages + NT + t); };
   auto o_full = [&](int t) { return bars + 8 * (1 + 4 * S::kStages + 2 * NT + t); };
+  auto p_half = [&](int t) { return bars + 8 * (1 + 4 * S::kStages + 3 * NT + t); };
+  auto s_read = [&](int t) { return bars + 8 * (1 + 4 * S::kStages + 4 * NT + t); };
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(sptr + (bars - base) + 8 * S::kBars);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* const status = &g_attn_packed_status;
@@ -110,7 +157,7 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
   if (threadIdx.x == 0) {
     mbar_init(bar_q, 1);
     for (int i = 0; i < S::kStages; ++i) { mbar_init(k_full(i), 1); mbar_init(k_empty(i), 1); mbar_init(v_full(i), 1); mbar_init(v_empty(i), 1); }
-    for (int t = 0; t < NT; ++t) { mbar_init(s_full(t), 1); mbar_init(p_full(t), 128); mbar_init(o_full(t), 1); }
+    for (int t = 0; t < NT; ++t) { mbar_init(s_full(t), 1); mbar_init(s_read(t), 4); mbar_init(p_half(t), 4); mbar_init(p_full(t), 4); mbar_init(o_full(t), 1); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -124,7 +171,10 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
   const uint32_t tmem = *tmem_slot;
   auto col_s = [&](int t) { return tmem + t * 128; };
   auto col_o = [&](int t) { return tmem + NT * 128 + t * DT; };
+  auto col_p = [&](int t) { return S::kApart ? tmem + NT * (128 + DT) + t * 64 : col_s(t); };
 
+  if (warp >= NT * 4) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kOtherRegs));
   if (warp == NT * 4) {                           // ---- copies
     int armed_k = 0, armed_v = 0;
     bool ok = true;
@@ -139,12 +189,12 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
     for (int j = 0; j < n_keys && ok; ++j) {
       const int st = j % S::kStages;
       const uint32_t ph = (j / S::kStages - 1) & 1;
-      if (j >= S::kStages) ok = mbar_wait(k_empty(st), ph, abort_flag, status, 31);
+      if (j >= S::kStages) ok = wait_for(k_empty(st), ph, abort_flag, status, 31);
       if (!ok) break;
       if (elect_one()) { mbar_arrive_expect_tx(k_full(st), S::kTile); load_tile<DT>(sK + st * S::kTile, &maps.k, k_full(st), hk, s.begin + j * TC_ROWS); }
       __syncwarp();
       ++armed_k;
-      if (j >= S::kStages) ok = mbar_wait(v_empty(st), ph, abort_flag, status, 32);
+      if (j >= S::kStages) ok = wait_for(v_empty(st), ph, abort_flag, status, 32);
       if (!ok) break;
       if (elect_one()) { mbar_arrive_expect_tx(v_full(st), S::kTile); load_tile<DT>(sV + st * S::kTile, &maps.v, v_full(st), hk, s.begin + j * TC_ROWS); }
       __syncwarp();
@@ -152,13 +202,13 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
     }
     if (*abort_flag) {                            // nothing may be in flight when the block ends
       volatile int never = 0;
-      mbar_wait(bar_q, 0, &never, status, 33);
-      for (int j = max(0, armed_k - S::kStages); j < armed_k; ++j) mbar_wait(k_full(j % S::kStages), (j / S::kStages) & 1, &never, status, 33);
-      for (int j = max(0, armed_v - S::kStages); j < armed_v; ++j) mbar_wait(v_full(j % S::kStages), (j / S::kStages) & 1, &never, status, 33);
+      wait_for(bar_q, 0, &never, status, 33);
+      for (int j = max(0, armed_k - S::kStages); j < armed_k; ++j) wait_for(k_full(j % S::kStages), (j / S::kStages) & 1, &never, status, 33);
+      for (int j = max(0, armed_v - S::kStages); j < armed_v; ++j) wait_for(v_full(j % S::kStages), (j / S::kStages) & 1, &never, status, 33);
     }
   } else if (warp == NT * 4 + 1) {                // ---- products
     const uint32_t id_s = make_idesc_mn(128, 128, 0, 0), id_o = make_idesc_mn(128, DT, 0, 1);
-    bool ok = mbar_wait(bar_q, 0, abort_flag, status, 34) && mbar_wait(k_full(0), 0, abort_flag, status, 35);
+    bool ok = wait_for(bar_q, 0, abort_flag, status, 34) && wait_for(k_full(0), 0, abort_flag, status, 35);
     if (ok) {
       tc_fence_after();
       if (elect_one()) {
@@ -168,75 +218,132 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
       }
       __syncwarp();
     }
+    auto values = [&](int t, int j) {             // O += P V, the first half of the keys as soon as their probabilities are there
+      const uint32_t v = sV + (j % S::kStages) * S::kTile;
+      if (!wait_for(p_half(t), j & 1, abort_flag, status, 38)) return false;
+      tc_fence_after();
+      if (elect_one()) mma_ab<DT>(col_o(t), col_p(t), v, id_o, j > 0, 0, 4);
+      __syncwarp();
+      if (!wait_for(p_full(t), j & 1, abort_flag, status, 38)) return false;
+      tc_fence_after();
+      if (elect_one()) mma_ab<DT>(col_o(t), col_p(t), v, id_o, true, 4, 8);
+      __syncwarp();
+      return true;
+    };
+    auto scores = [&](int t, int j) {
+      if (elect_one()) { mma_abt<DT>(col_s(t), sQ + t * S::kTile, sK + (j % S::kStages) * S::kTile, id_s); tc_commit(s_full(t)); }
+      __syncwarp();
+    };
+    auto done = [&](uint32_t bar) {
+      if (elect_one()) tc_commit(bar);
+      __syncwarp();
+    };
     for (int j = 0; j < n_keys && ok; ++j) {
       const int st = j % S::kStages, nx = (j + 1) % S::kStages;
-      ok = mbar_wait(v_full(st), (j / S::kStages) & 1, abort_flag, status, 36);
-      if (ok && j + 1 < n_keys && S::kStages > 1) ok = mbar_wait(k_full(nx), ((j + 1) / S::kStages) & 1, abort_flag, status, 37);
-      if (!ok) break;
+      const bool more = j + 1 < n_keys;
+      auto next_keys = [&]() { return wait_for(k_full(nx), ((j + 1) / S::kStages) & 1, abort_flag, status, 37); };
+      if constexpr (S::kApart) {
+        if (more) {
+          ok = next_keys();
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const int n = keys_of(t);
-        if (j >= n) continue;
-        ok = mbar_wait(p_full(t), j & 1, abort_flag, status, 38);
-        // with one stage the next keys are copied only now, behind the previous product's commit
-        if (ok && S::kStages == 1 && j + 1 < n) ok = mbar_wait(k_full(0), (j + 1) & 1, abort_flag, status, 37);
-        if (!ok) break;
-        tc_fence_after();
-        if (elect_one()) {
-          mma_ab<DT>(col_o(t), col_s(t) + FWD_P, sV + st * S::kTile, id_o, j > 0);
-          if (j + 1 < n) { mma_abt<DT>(col_s(t), sQ + t * S::kTile, sK + nx * S::kTile, id_s); tc_commit(s_full(t)); }
-          else tc_commit(o_full(t));
+          for (int t = 0; t < NT; ++t)
+            if (ok && j + 1 < keys_of(t)) {
+              ok = wait_for(s_read(t), j & 1, abort_flag, status, 42);
+              tc_fence_after();
+              if (ok) scores(t, j + 1);
+            }
+          if (!ok) break;
+          done(k_empty(nx));
         }
-        __syncwarp();
+        ok = wait_for(v_full(st), (j / S::kStages) & 1, abort_flag, status, 36);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          if (ok && j < keys_of(t)) {
+            ok = values(t, j);
+            if (ok) done(o_full(t));
+          }
+        if (!ok) break;
+        done(v_empty(st));
+      } else {
+        ok = wait_for(v_full(st), (j / S::kStages) & 1, abort_flag, status, 36);
+        // with one stage the next keys are copied only behind the previous product's commit: waited for below
+        if (ok && more && S::kStages > 1) ok = next_keys();
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const int n = keys_of(t);
+          if (!ok || j >= n) continue;
+          ok = values(t, j);
+          if (ok && S::kStages == 1 && j + 1 < n) ok = next_keys();
+          if (!ok) continue;
+          tc_fence_after();
+          if (j + 1 < n) scores(t, j + 1);
+          else done(o_full(t));
+        }
+        if (!ok) break;
+        done(v_empty(st));
+        if (more) done(k_empty(nx));
       }
-      if (!ok) break;
-      if (elect_one()) {
-        tc_commit(v_empty(st));
-        if (j + 1 < n_keys) tc_commit(k_empty(nx));
-      }
-      __syncwarp();
     }
+  }
   } else {                                        // ---- softmax: thread = row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kSoftmaxRegs));
     const int t = warp >> 2, r = threadIdx.x & 127;
     const int n = keys_of(t), q0 = first_of(t), row = q0 + r;
     if (n > 0) {
       const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-      const uint32_t ts = col_s(t) + lanes, to = col_o(t) + lanes;
+      const uint32_t ts = col_s(t) + lanes, to = col_o(t) + lanes, tp = col_p(t) + lanes;
       const float c = a.scale * kLog2e;
       const int limit = a.causal ? min(s.len, row + 1) : s.len;      // keys this row sees
       float m = -INFINITY, l = 0.f;               // m: the maximum in use, times c
       bool ok = true;
       for (int j = 0; j < n; ++j) {
-        ok = mbar_wait(s_full(t), j & 1, abort_flag, status, 39);
+        ok = wait_for(s_full(t), j & 1, abort_flag, status, 39);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after();
         const int k0 = j * TC_ROWS;
         const bool edge = k0 + TC_ROWS > s.len || (a.causal && k0 + TC_ROWS > q0 + 1);
-        auto mask = [&](uint32_t (&x)[32], int q) {
-          if (edge)
+        // The rows behind the sequence's end of its last value tile belong to other sequences, or to none: zeros, as p is there, so
+        // that nothing that is not finite meets a zero.  The first query tile that reads the tile clears it.
+        if (k0 + TC_ROWS > s.len && (t == 0 || keys_of(0) <= j)) {
+          const int st = j % S::kStages, valid = s.len - k0;
+          ok = wait_for(v_full(st), (j / S::kStages) & 1, abort_flag, status, 40);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          for (int i = valid * 8 + r; i < TC_ROWS * 8; i += 128)
+#pragma unroll
+            for (int q = 0; q < S::kSub; ++q)
+              *reinterpret_cast<uint4*>(sptr + (sV - base) + st * S::kTile + q * TC_SUB + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+          fence_async_smem();
+        }
+        uint32_t v[4][32];
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_ld32(ts + q * 32, v[q]);
+        tmem_ld_wait();
+        if (S::kApart) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(s_read(t));
+        }
+        if (edge) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (k0 + q * 32 + i >= limit) x[i] = 0xFF800000u;
-        };
-        // the maximum over the row; its upper half stays in registers, the lower one is read again
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        auto maximum = [&](const uint32_t (&x)[32]) {
+              if (k0 + q * 32 + i >= limit) v[q][i] = 0xFF800000u;
+        }
 #pragma unroll
-          for (int i = 0; i < 32; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(x[i]));
-        };
-        uint32_t v[2][32];
-        tmem_ld32(ts, v[0]);
-        tmem_ld32(ts + 32, v[1]);
-        tmem_ld_wait();
-        mask(v[0], 0); mask(v[1], 1);
-        maximum(v[0]); maximum(v[1]);
-        tmem_ld32(ts + 64, v[0]);
-        tmem_ld32(ts + 96, v[1]);
-        tmem_ld_wait();
-        mask(v[0], 2); mask(v[1], 3);
-        maximum(v[0]); maximum(v[1]);
+        for (int i = 0; i < 32; i += 2)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) mx[q] = max3(mx[q], __uint_as_float(v[q][i]), __uint_as_float(v[q][i + 1]));
         const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+        if (S::kApart && j > 0) {                 // P's columns are free, and O holds the tiles before this one
+          ok = wait_for(o_full(t), (j - 1) & 1, abort_flag, status, 43);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+        }
         if (j == 0) {
           m = top;
         } else if (__any_sync(0xffffffffu, top > m + 8.f)) {
@@ -260,39 +367,28 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             float2 e = fma_f32x2(make_float2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), cc, mm);
-            e.x = ex2(e.x); e.y = ex2(e.y);
+            if (FWD_FMA >> i & 1) e = ex2_fma(e);
+            else { e.x = ex2(e.x); e.y = ex2(e.y); }
             sum = add_f32x2(sum, e);
             p[i] = pack_bf16(e.x, e.y);
           }
-          tmem_st16(ts + FWD_P + q * 16, p);
+          tmem_st16(tp + q * 16, p);
         };
-        probabilities(v[0], 2);                   // P's columns 96 .. 127 overwrite scores that are in registers ...
-        probabilities(v[1], 3);
-        tmem_ld32(ts, v[0]);
-        tmem_ld32(ts + 32, v[1]);
-        tmem_ld_wait();
-        mask(v[0], 0); mask(v[1], 1);
-        probabilities(v[0], 0);                   // ... and columns 64 .. 95 scores that are done
+        probabilities(v[0], 0);                   // P overwrites scores that are in registers
         probabilities(v[1], 1);
-        l += sum.x + sum.y;
-        // The rows behind the sequence's end of its last value tile belong to other sequences, or to none: zeros, as p is there, so
-        // that nothing that is not finite meets a zero.  The first query tile that reads the tile clears it.
-        if (k0 + TC_ROWS > s.len && (t == 0 || keys_of(0) <= j)) {
-          const int st = j % S::kStages, valid = s.len - k0;
-          ok = mbar_wait(v_full(st), (j / S::kStages) & 1, abort_flag, status, 40);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          for (int i = valid * 8 + r; i < TC_ROWS * 8; i += 128)
-#pragma unroll
-            for (int q = 0; q < S::kSub; ++q)
-              *reinterpret_cast<uint4*>(sptr + (sV - base) + st * S::kTile + q * TC_SUB + i * 16) = make_uint4(0u, 0u, 0u, 0u);
-          fence_async_smem();
-        }
         tmem_st_wait();
         tc_fence_before();
-        mbar_arrive(p_full(t));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_half(t));
+        probabilities(v[2], 2);
+        probabilities(v[3], 3);
+        l += sum.x + sum.y;
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(t));
       }
-      if (ok) ok = mbar_wait(o_full(t), 0, abort_flag, status, 41);
+      if (ok) ok = wait_for(o_full(t), S::kApart ? (n - 1) & 1 : 0, abort_flag, status, 41);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
       const float inv = ok ? 1.f / l : NAN;
@@ -438,7 +534,7 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dkv_tc_kernel(const __grid
     __syncwarp();
     for (int it = 0; it < n_it; ++it) {
       const int st = it % S::kStages, h = head_of(it), q0 = first_of(it);
-      if (it >= S::kStages) ok = mbar_wait(empty(st), (it / S::kStages - 1) & 1, abort_flag, status, 51);
+      if (it >= S::kStages) ok = wait_for(empty(st), (it / S::kStages - 1) & 1, abort_flag, status, 51);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       if (elect_one()) {
@@ -457,7 +553,7 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dkv_tc_kernel(const __grid
         rows[TC_ROWS + i + lane] = r < s.len ? a.delta[at] : 0.f;
       }
       if (q0 + TC_ROWS > s.len) {                 // rows of other sequences, or of none: zeros, where P and dS are zero
-        ok = mbar_wait(full(st), (it / S::kStages) & 1, abort_flag, status, 52);
+        ok = wait_for(full(st), (it / S::kStages) & 1, abort_flag, status, 52);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         clear_rows<DT>(sptr + (sQ - base) + st * S::kTile, s.len - q0);
@@ -468,16 +564,16 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dkv_tc_kernel(const __grid
     }
     if (*abort_flag) {                            // nothing may be in flight when the block ends
       volatile int never = 0;
-      mbar_wait(kv_full, 0, &never, status, 53);
-      for (int it = max(0, armed - S::kStages); it < armed; ++it) mbar_wait(full(it % S::kStages), (it / S::kStages) & 1, &never, status, 53);
+      wait_for(kv_full, 0, &never, status, 53);
+      for (int it = max(0, armed - S::kStages); it < armed; ++it) wait_for(full(it % S::kStages), (it / S::kStages) & 1, &never, status, 53);
     }
   } else if (warp == 9) {                         // ---- products
     const uint32_t id_s = make_idesc_mn(128, 128, 0, 0), id_d = make_idesc_mn(128, DT, 0, 1);
     auto ready = [&](int it) {
       const int st = it % S::kStages;
-      return mbar_wait(full(st), (it / S::kStages) & 1, abort_flag, status, 54) && mbar_wait(row_full(st), (it / S::kStages) & 1, abort_flag, status, 55);
+      return wait_for(full(st), (it / S::kStages) & 1, abort_flag, status, 54) && wait_for(row_full(st), (it / S::kStages) & 1, abort_flag, status, 55);
     };
-    bool ok = mbar_wait(kv_full, 0, abort_flag, status, 56) && ready(0);
+    bool ok = wait_for(kv_full, 0, abort_flag, status, 56) && ready(0);
     if (ok) {
       tc_fence_after();
       if (elect_one()) {
@@ -491,7 +587,7 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dkv_tc_kernel(const __grid
     for (int it = 0; it < n_it && ok; ++it) {
       const int st = it % S::kStages, nx = (it + 1) % S::kStages;
       const bool more = it + 1 < n_it;
-      ok = mbar_wait(p_full, it & 1, abort_flag, status, 57) && (!more || ready(it + 1));
+      ok = wait_for(p_full, it & 1, abort_flag, status, 57) && (!more || ready(it + 1));
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
@@ -499,7 +595,7 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dkv_tc_kernel(const __grid
         if (more) { mma_abt<DT>(col_s, sK, sQ + nx * S::kTile, id_s); tc_commit(s_full); }
       }
       __syncwarp();
-      ok = mbar_wait(ds_full, it & 1, abort_flag, status, 58);
+      ok = wait_for(ds_full, it & 1, abort_flag, status, 58);
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
@@ -519,7 +615,7 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dkv_tc_kernel(const __grid
       const int st = it % S::kStages, q0 = first_of(it);
       const bool diagonal = a.causal && q0 == k0;
       const float* rows = row_values + st * 2 * TC_ROWS + half * 64;
-      ok = mbar_wait(row_full(st), (it / S::kStages) & 1, abort_flag, status, 59) && mbar_wait(s_full, it & 1, abort_flag, status, 60);
+      ok = wait_for(row_full(st), (it / S::kStages) & 1, abort_flag, status, 59) && wait_for(s_full, it & 1, abort_flag, status, 60);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
@@ -547,7 +643,7 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dkv_tc_kernel(const __grid
       tmem_st_wait();
       tc_fence_before();
       mbar_arrive(p_full);
-      ok = mbar_wait(dp_full, it & 1, abort_flag, status, 61);
+      ok = wait_for(dp_full, it & 1, abort_flag, status, 61);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
@@ -570,7 +666,7 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dkv_tc_kernel(const __grid
       tc_fence_before();
       mbar_arrive(ds_full);
     }
-    if (ok) ok = mbar_wait(acc_full, 0, abort_flag, status, 62);
+    if (ok) ok = wait_for(acc_full, 0, abort_flag, status, 62);
     ok = __all_sync(0xffffffffu, ok);
     tc_fence_after();
     const bool in = key < s.len;
@@ -636,7 +732,7 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dq_tc_kernel(const __grid_
     __syncwarp();
     for (int it = 0; it < n_it; ++it) {
       const int st = it % S::kStages, k0 = it * TC_ROWS;
-      if (it >= S::kStages) ok = mbar_wait(empty(st), (it / S::kStages - 1) & 1, abort_flag, status, 71);
+      if (it >= S::kStages) ok = wait_for(empty(st), (it / S::kStages - 1) & 1, abort_flag, status, 71);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       if (elect_one()) {
@@ -647,7 +743,7 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dq_tc_kernel(const __grid_
       __syncwarp();
       ++armed;
       if (k0 + TC_ROWS > s.len) {                 // keys of other sequences, or of none: zeros, where dS is zero
-        ok = mbar_wait(full(st), (it / S::kStages) & 1, abort_flag, status, 72);
+        ok = wait_for(full(st), (it / S::kStages) & 1, abort_flag, status, 72);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         clear_rows<DT>(sptr + (sK - base) + st * S::kTile, s.len - k0);
@@ -657,16 +753,16 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dq_tc_kernel(const __grid_
     }
     if (*abort_flag) {                            // nothing may be in flight when the block ends
       volatile int never = 0;
-      mbar_wait(q_full, 0, &never, status, 73);
-      for (int it = max(0, armed - S::kStages); it < armed; ++it) mbar_wait(full(it % S::kStages), (it / S::kStages) & 1, &never, status, 73);
+      wait_for(q_full, 0, &never, status, 73);
+      for (int it = max(0, armed - S::kStages); it < armed; ++it) wait_for(full(it % S::kStages), (it / S::kStages) & 1, &never, status, 73);
     }
   } else if (warp == 9) {                         // ---- products
     const uint32_t id_s = make_idesc_mn(128, 128, 0, 0), id_d = make_idesc_mn(128, DT, 0, 1);
     auto ready = [&](int it) {
       const int st = it % S::kStages;
-      return mbar_wait(full(st), (it / S::kStages) & 1, abort_flag, status, 74) && mbar_wait(cleared(st), (it / S::kStages) & 1, abort_flag, status, 75);
+      return wait_for(full(st), (it / S::kStages) & 1, abort_flag, status, 74) && wait_for(cleared(st), (it / S::kStages) & 1, abort_flag, status, 75);
     };
-    bool ok = mbar_wait(q_full, 0, abort_flag, status, 76) && ready(0) && (n_it < 2 || ready(1));
+    bool ok = wait_for(q_full, 0, abort_flag, status, 76) && ready(0) && (n_it < 2 || ready(1));
     if (ok) {
       tc_fence_after();
       if (elect_one()) {
@@ -680,7 +776,7 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dq_tc_kernel(const __grid_
     }
     for (int it = 0; it < n_it && ok; ++it) {
       const int st = it % S::kStages, nx = (it + 1) % S::kStages, n2 = (it + 2) % S::kStages;
-      ok = mbar_wait(ds_full, it & 1, abort_flag, status, 77);
+      ok = wait_for(ds_full, it & 1, abort_flag, status, 77);
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
@@ -709,7 +805,7 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dq_tc_kernel(const __grid_
     for (int it = 0; it < n_it; ++it) {
       const int k0 = it * TC_ROWS;
       const bool edge = k0 + TC_ROWS > s.len || (a.causal && k0 + TC_ROWS > q0 + 1);
-      ok = mbar_wait(s_full + 8 * (it & 1), (it >> 1) & 1, abort_flag, status, 78);
+      ok = wait_for(s_full + 8 * (it & 1), (it >> 1) & 1, abort_flag, status, 78);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
@@ -725,7 +821,7 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dq_tc_kernel(const __grid_
           p[q * 32 + i] = ex2(x.x); p[q * 32 + i + 1] = ex2(x.y);
         }
       }
-      ok = mbar_wait(dp_full, it & 1, abort_flag, status, 79);
+      ok = wait_for(dp_full, it & 1, abort_flag, status, 79);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
@@ -752,7 +848,7 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dq_tc_kernel(const __grid_
       tc_fence_before();
       mbar_arrive(ds_full);
     }
-    if (ok) ok = mbar_wait(acc_full, 0, abort_flag, status, 80);
+    if (ok) ok = wait_for(acc_full, 0, abort_flag, status, 80);
     ok = __all_sync(0xffffffffu, ok);
     tc_fence_after();
     store_half<DT>(head_row_out<__nv_bfloat16>(a.dq, s.begin + row, h), col_dq + lanes, half, a.dim, row < s.len, ok ? a.scale : NAN);
