@@ -424,78 +424,103 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
 // ---- backward ---------------------------------------------------------------------------------------------------
 //
 // Two kernels, as on the CUDA cores: one owns 128 key rows (dk, dv), one owns 128 query rows (dq); every gradient is summed by one
-// block in a fixed order. Seven products a pair of tiles instead of the five that sharing the scores would take, and no atomics,
-// no fp32 copy of dq in memory. Both have the shape  two products -> 128 x 128 values in registers -> bf16 factors in tensor
-// memory -> one or two products that accumulate, and 256 threads for the values: thread = row, two halves of the columns.
+// block in a fixed order.  Seven products a pair of tiles instead of the five that sharing the scores would take, and no atomics,
+// no fp32 copy of dq in memory.  Both have the shape  two products -> 128 x BN values in registers -> bf16 factors in tensor
+// memory -> one or two products that accumulate; a thread holds 32 values of one row.
 //
 // Keys:     S^T = K Q^T, dP^T = V dO^T;  P^T = 2^(c S^T - lse), dS^T = P^T (dP^T - delta);  dV += P^T dO,  dK += dS^T Q
 //           Transposed, so that P^T and dS^T are what the products take from tensor memory and nothing is written to shared
-//           memory; lse and delta go by column and are read from shared memory.  P^T overwrites S^T and dS^T dP^T, half by half.
+//           memory; lse and delta go by column and are read from shared memory.  P^T overwrites S^T and dS^T dP^T, each part
+//           of the columns its own.
 // Queries:  S = Q K^T, dP = dO V^T;  dS as above, by rows;  dQ += dS K.  S is double-buffered; dS overwrites dP.
+//
+// Heads of 128: BN = 128, all 512 columns of tensor memory, one block of 18 warps per SM.  Heads of 64: BN = 64 and 256 columns, so
+// that two blocks share an SM and one's copies and epilogue run under the other's work (most of the time of short sequences).
 
 template <int DT> struct BwdShape {
+  static constexpr int kCols = DT == 64 ? 64 : 128;                  // BN: columns of a tile of values
+  static constexpr int kParts = kCols / 32;                          // threads to a row
+  static constexpr int kBlocks = DT == 64 ? 2 : 1;                   // per SM
   static constexpr int kSub = DT / 64;
-  static constexpr int kTile = kSub * TC_SUB;
-  static constexpr int kStages = DT == 64 ? 4 : 2;
-  static constexpr int kThreads = 320;
+  static constexpr int kTile = kSub * TC_SUB;                        // a resident tile: 128 rows
+  static constexpr int kStream = kSub * kCols * 128;                 // a streamed one: BN rows
+  static constexpr int kStages = DT == 64 ? 3 : 2;
+  static constexpr int kThreads = kParts * 128 + 64;
+  static constexpr int kTmem = DT == 64 ? 256 : 512;
   static constexpr int kBars = 1 + 3 * kStages + 6;
-  static constexpr int kRowBytes = kStages * 2 * TC_ROWS * 4;        // lse and delta of the query tiles in flight
-  static constexpr int kSmem = 2 * kTile + 2 * kStages * kTile + kRowBytes + 1024 + kBars * 8 + 16;
+  static constexpr int kRowBytes = kStages * 2 * kCols * 4;          // lse and delta of the query tiles in flight
+  static constexpr int kSmem = 2 * kTile + 2 * kStages * kStream + kRowBytes + 1024 + kBars * 8 + 16;
 };
 
-// the same halves of the depth as the 256 threads write: columns 0 .. 31 and 64 .. 95 of the region
-template <int DT> __device__ __forceinline__ void mma_ab_halves(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
-  const uint64_t base = desc_base(TC_SUB, 1024);
+// Copies of ROWS rows of a head, with boxes of BN rows.
+template <int DT, int ROWS> __device__ __forceinline__ void copy_rows(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int64_t token) {
+  constexpr int kBox = BwdShape<DT>::kCols;
 #pragma unroll
-  for (int k = 0; k < TC_ROWS / 16; ++k) tc_mma_bf16_ta(d, a + (k >> 2) * 64 + (k & 3) * 8, desc_at(base, b + k * 2048), idesc, accumulate || k > 0);
+  for (int i = 0; i < DT / 64; ++i)
+#pragma unroll
+    for (int r = 0; r < ROWS; r += kBox) tma_load_3d(dst + (i * ROWS + r) * 128, map, bar, i * 64, head, (int)token + r);
 }
-// zeros in rows `valid` .. 127 of a tile, by one warp
+// 128 x BN x DT product of a resident and a streamed tile
+template <int DT> __device__ __forceinline__ void mma_scores(uint32_t d, uint32_t a, uint32_t b) {
+  using S = BwdShape<DT>;
+  const uint64_t base = desc_base(16, 1024);
+  const uint32_t idesc = make_idesc_mn(128, S::kCols, 0, 0);
+#pragma unroll
+  for (int k = 0; k < DT / 16; ++k)
+    tc_mma_bf16(d, desc_at(base, a + (k >> 2) * TC_SUB + (k & 3) * 32), desc_at(base, b + (k >> 2) * S::kCols * 128 + (k & 3) * 32), idesc, k > 0);
+}
+// 128 x DT x BN product of factors in tensor memory (16 columns of every 32) and a streamed tile whose rows run along the depth
+template <int DT> __device__ __forceinline__ void mma_gradient(uint32_t d, uint32_t a, uint32_t b, bool accumulate) {
+  using S = BwdShape<DT>;
+  const uint64_t base = desc_base(S::kCols * 128, 1024);
+  const uint32_t idesc = make_idesc_mn(128, DT, 0, 1);
+#pragma unroll
+  for (int k = 0; k < S::kCols / 16; ++k) tc_mma_bf16_ta(d, a + (k >> 1) * 32 + (k & 1) * 8, desc_at(base, b + k * 2048), idesc, accumulate || k > 0);
+}
+// zeros in rows `valid` .. BN - 1 of a streamed tile, by one warp
 template <int DT> __device__ __forceinline__ void clear_rows(uint8_t* tile, int valid) {
-  for (int i = valid * 8 + (threadIdx.x & 31); i < TC_ROWS * 8; i += 32)
+  using S = BwdShape<DT>;
+  for (int i = valid * 8 + (threadIdx.x & 31); i < S::kCols * 8; i += 32)
 #pragma unroll
-    for (int q = 0; q < DT / 64; ++q) *reinterpret_cast<uint4*>(tile + q * TC_SUB + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+    for (int q = 0; q < S::kSub; ++q) *reinterpret_cast<uint4*>(tile + q * S::kCols * 128 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
 }
-// half the columns of an accumulator row times f, to bf16 (NaN where a wait ran out)
-template <int DT> __device__ __forceinline__ void store_half(__nv_bfloat16* out, uint32_t taddr, int half, int dim, bool in, float f) {
+// 32 columns of an accumulator row times f, to bf16 (NaN where a wait ran out)
+__device__ __forceinline__ void store_part(__nv_bfloat16* out, uint32_t taddr, int c0, int dim, bool in, float f) {
+  uint32_t o[32];
+  tmem_ld32(taddr + c0, o);
+  tmem_ld_wait();
+  if (in)
 #pragma unroll
-  for (int q = 0; q < DT / 64; ++q) {
-    const int c0 = half * (DT / 2) + q * 32;
-    uint32_t o[32];
-    tmem_ld32(taddr + c0, o);
-    tmem_ld_wait();
-    if (in)
+    for (int g = 0; g < 4; ++g)
+      if (c0 + g * 8 < dim) {
+        float v[8];
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        if (c0 + g * 8 < dim) {
-          float v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(o[g * 8 + i]) * f;
-          *reinterpret_cast<uint4*>(out + c0 + g * 8) =
-              make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-        }
-  }
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(o[g * 8 + i]) * f;
+        *reinterpret_cast<uint4*>(out + c0 + g * 8) =
+            make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+      }
 }
 
 struct TcBwdMaps { CUtensorMap q, k, v, d_o; };
 
 template <int DT>
-__global__ void __launch_bounds__(320, 1) attn_packed_dkv_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcBwdMaps maps) {
+__global__ void __launch_bounds__(BwdShape<DT>::kThreads, BwdShape<DT>::kBlocks)
+attn_packed_dkv_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcBwdMaps maps) {
   using S = BwdShape<DT>;
+  constexpr int BN = S::kCols, kCopy = S::kParts * 4, kIssue = kCopy + 1;        // the warps that copy and issue
   const int hk = blockIdx.x % a.kv_heads;
   const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.kv_heads, TC_ROWS);
   if (s.tile < 0) { pdl_wait(); pdl_trigger(); return; }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int k0 = s.tile * TC_ROWS, i0 = a.causal ? s.tile : 0;
-  const int per_head = (s.len + TC_ROWS - 1) / TC_ROWS - i0, n_it = per_head * a.group;
-  auto head_of = [&](int it) { return hk * a.group + it / per_head; };
-  auto first_of = [&](int it) { return (i0 + it % per_head) * TC_ROWS; };
+  const int k0 = s.tile * TC_ROWS, first = a.causal ? k0 : 0;
+  const int per_head = (s.len - first + BN - 1) / BN, n_it = per_head * a.group;
 
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const sptr = smem_raw + (base - raw);
-  const uint32_t sK = base, sV = sK + S::kTile, sQ = sV + S::kTile, sO = sQ + S::kStages * S::kTile, srow = sO + S::kStages * S::kTile,
+  const uint32_t sK = base, sV = sK + S::kTile, sQ = sV + S::kTile, sO = sQ + S::kStages * S::kStream, srow = sO + S::kStages * S::kStream,
                  bars = srow + S::kRowBytes;
-  float* const row_values = reinterpret_cast<float*>(sptr + (srow - base));      // [stage][lse, delta][128]
+  float* const row_values = reinterpret_cast<float*>(sptr + (srow - base));      // [stage][lse, delta][BN]
   const uint32_t kv_full = bars;
   auto full = [&](int i) { return bars + 8 * (1 + i); };
   auto row_full = [&](int i) { return bars + 8 * (1 + S::kStages + i); };
@@ -508,12 +533,12 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dkv_tc_kernel(const __grid
   if (threadIdx.x == 0) {
     mbar_init(kv_full, 1);
     for (int i = 0; i < S::kStages; ++i) { mbar_init(full(i), 1); mbar_init(row_full(i), 32); mbar_init(empty(i), 1); }
-    mbar_init(s_full, 1); mbar_init(dp_full, 1); mbar_init(p_full, 256); mbar_init(ds_full, 256); mbar_init(acc_full, 1);
+    mbar_init(s_full, 1); mbar_init(dp_full, 1); mbar_init(p_full, S::kParts * 4); mbar_init(ds_full, S::kParts * 4); mbar_init(acc_full, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 9) {
-    tmem_alloc(smem_u32(tmem_slot), 512);
+  if (warp == kIssue) {
+    tmem_alloc(smem_u32(tmem_slot), S::kTmem);
     tmem_relinquish();
   }
   tc_fence_before();
@@ -521,54 +546,55 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dkv_tc_kernel(const __grid
   tc_fence_after();
   pdl_wait();                                     // delta
   pdl_trigger();
-  const uint32_t tmem = *tmem_slot, col_s = tmem, col_dp = tmem + 128, col_dv = tmem + 256, col_dk = tmem + 256 + DT;
+  const uint32_t tmem = *tmem_slot, col_s = tmem, col_dp = tmem + BN, col_dv = tmem + 2 * BN, col_dk = tmem + 2 * BN + DT;
 
-  if (warp == 8) {                                // ---- copies
-    int armed = 0;
+  if (warp == kCopy) {                            // ---- copies
+    int armed = 0, h = hk * a.group, q0 = first;
     bool ok = true;
     if (elect_one()) {
       mbar_arrive_expect_tx(kv_full, 2 * S::kTile);
-      load_tile<DT>(sK, &maps.k, kv_full, hk, s.begin + k0);
-      load_tile<DT>(sV, &maps.v, kv_full, hk, s.begin + k0);
+      copy_rows<DT, TC_ROWS>(sK, &maps.k, kv_full, hk, s.begin + k0);
+      copy_rows<DT, TC_ROWS>(sV, &maps.v, kv_full, hk, s.begin + k0);
     }
     __syncwarp();
     for (int it = 0; it < n_it; ++it) {
-      const int st = it % S::kStages, h = head_of(it), q0 = first_of(it);
+      const int st = it % S::kStages;
       if (it >= S::kStages) ok = wait_for(empty(st), (it / S::kStages - 1) & 1, abort_flag, status, 51);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       if (elect_one()) {
-        mbar_arrive_expect_tx(full(st), 2 * S::kTile);
-        load_tile<DT>(sQ + st * S::kTile, &maps.q, full(st), h, s.begin + q0);
-        load_tile<DT>(sO + st * S::kTile, &maps.d_o, full(st), h, s.begin + q0);
+        mbar_arrive_expect_tx(full(st), 2 * S::kStream);
+        copy_rows<DT, BN>(sQ + st * S::kStream, &maps.q, full(st), h, s.begin + q0);
+        copy_rows<DT, BN>(sO + st * S::kStream, &maps.d_o, full(st), h, s.begin + q0);
       }
       __syncwarp();
       ++armed;
-      float* rows = row_values + st * 2 * TC_ROWS;
+      float* rows = row_values + st * 2 * BN;
 #pragma unroll
-      for (int i = 0; i < TC_ROWS; i += 32) {
+      for (int i = 0; i < BN; i += 32) {
         const int r = q0 + i + lane;
         const int64_t at = (int64_t)h * a.tokens + s.begin + r;
         rows[i + lane] = r < s.len ? a.lse[at] * kLog2e : INFINITY;              // no row: probability zero
-        rows[TC_ROWS + i + lane] = r < s.len ? a.delta[at] : 0.f;
+        rows[BN + i + lane] = r < s.len ? a.delta[at] : 0.f;
       }
-      if (q0 + TC_ROWS > s.len) {                 // rows of other sequences, or of none: zeros, where P and dS are zero
+      if (q0 + BN > s.len) {                      // rows of other sequences, or of none: zeros, where P and dS are zero
         ok = wait_for(full(st), (it / S::kStages) & 1, abort_flag, status, 52);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        clear_rows<DT>(sptr + (sQ - base) + st * S::kTile, s.len - q0);
-        clear_rows<DT>(sptr + (sO - base) + st * S::kTile, s.len - q0);
+        clear_rows<DT>(sptr + (sQ - base) + st * S::kStream, s.len - q0);
+        clear_rows<DT>(sptr + (sO - base) + st * S::kStream, s.len - q0);
         fence_async_smem();
       }
       mbar_arrive(row_full(st));
+      q0 += BN;
+      if (q0 >= s.len) { q0 = first; ++h; }
     }
     if (*abort_flag) {                            // nothing may be in flight when the block ends
       volatile int never = 0;
       wait_for(kv_full, 0, &never, status, 53);
       for (int it = max(0, armed - S::kStages); it < armed; ++it) wait_for(full(it % S::kStages), (it / S::kStages) & 1, &never, status, 53);
     }
-  } else if (warp == 9) {                         // ---- products
-    const uint32_t id_s = make_idesc_mn(128, 128, 0, 0), id_d = make_idesc_mn(128, DT, 0, 1);
+  } else if (warp == kIssue) {                    // ---- products
     auto ready = [&](int it) {
       const int st = it % S::kStages;
       return wait_for(full(st), (it / S::kStages) & 1, abort_flag, status, 54) && wait_for(row_full(st), (it / S::kStages) & 1, abort_flag, status, 55);
@@ -577,9 +603,9 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dkv_tc_kernel(const __grid
     if (ok) {
       tc_fence_after();
       if (elect_one()) {
-        mma_abt<DT>(col_s, sK, sQ, id_s);
+        mma_scores<DT>(col_s, sK, sQ);
         tc_commit(s_full);
-        mma_abt<DT>(col_dp, sV, sO, id_s);
+        mma_scores<DT>(col_dp, sV, sO);
         tc_commit(dp_full);
       }
       __syncwarp();
@@ -587,115 +613,124 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dkv_tc_kernel(const __grid
     for (int it = 0; it < n_it && ok; ++it) {
       const int st = it % S::kStages, nx = (it + 1) % S::kStages;
       const bool more = it + 1 < n_it;
-      ok = wait_for(p_full, it & 1, abort_flag, status, 57) && (!more || ready(it + 1));
+      ok = wait_for(p_full, it & 1, abort_flag, status, 57);
       if (!ok) break;
       tc_fence_after();
-      if (elect_one()) {
-        mma_ab_halves<DT>(col_dv, col_s, sO + st * S::kTile, id_d, it > 0);
-        if (more) { mma_abt<DT>(col_s, sK, sQ + nx * S::kTile, id_s); tc_commit(s_full); }
-      }
+      if (elect_one()) mma_gradient<DT>(col_dv, col_s, sO + st * S::kStream, it > 0);
       __syncwarp();
+      if (more) {
+        ok = ready(it + 1);
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) { mma_scores<DT>(col_s, sK, sQ + nx * S::kStream); tc_commit(s_full); }
+        __syncwarp();
+      }
       ok = wait_for(ds_full, it & 1, abort_flag, status, 58);
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
-        mma_ab_halves<DT>(col_dk, col_dp, sQ + st * S::kTile, id_d, it > 0);
+        mma_gradient<DT>(col_dk, col_dp, sQ + st * S::kStream, it > 0);
         tc_commit(empty(st));
-        if (more) { mma_abt<DT>(col_dp, sV, sO + nx * S::kTile, id_s); tc_commit(dp_full); }
+        if (more) { mma_scores<DT>(col_dp, sV, sO + nx * S::kStream); tc_commit(dp_full); }
         else tc_commit(acc_full);
       }
       __syncwarp();
     }
-  } else {                                        // ---- values: thread = key row, half of the query columns
-    const int half = warp >> 2, r = threadIdx.x & 127, key = k0 + r;
+  } else {                                        // ---- values: thread = key row, 32 of the query columns
+    const int c0 = (warp >> 2) * 32, key = k0 + (threadIdx.x & 127);
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float c = a.scale * kLog2e;
     bool ok = true;
+    int q0 = first;
     for (int it = 0; it < n_it; ++it) {
-      const int st = it % S::kStages, q0 = first_of(it);
-      const bool diagonal = a.causal && q0 == k0;
-      const float* rows = row_values + st * 2 * TC_ROWS + half * 64;
+      const int st = it % S::kStages;
+      const float* rows = row_values + st * 2 * BN + c0;
       ok = wait_for(row_full(st), (it / S::kStages) & 1, abort_flag, status, 59) && wait_for(s_full, it & 1, abort_flag, status, 60);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      float p[64];
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
+      float p[32];
+      {
         uint32_t v[32], w[16];
-        tmem_ld32(col_s + lanes + half * 64 + q * 32, v);
+        tmem_ld32(col_s + lanes + c0, v);
         tmem_ld_wait();
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
-          const float4 l = *reinterpret_cast<const float4*>(rows + q * 32 + i);
+          const float4 l = *reinterpret_cast<const float4*>(rows + i);
           const float2 x = fma_f32x2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(c, c), make_float2(-l.x, -l.y));
           const float2 y = fma_f32x2(make_float2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), make_float2(c, c), make_float2(-l.z, -l.w));
-          p[q * 32 + i] = ex2(x.x); p[q * 32 + i + 1] = ex2(x.y); p[q * 32 + i + 2] = ex2(y.x); p[q * 32 + i + 3] = ex2(y.y);
+          p[i] = ex2(x.x); p[i + 1] = ex2(x.y); p[i + 2] = ex2(y.x); p[i + 3] = ex2(y.y);
         }
-        if (diagonal)
+        if (a.causal && q0 < k0 + TC_ROWS)
 #pragma unroll
           for (int i = 0; i < 32; ++i)
-            if (half * 64 + q * 32 + i < r) p[q * 32 + i] = 0.f;
+            if (q0 + c0 + i < key) p[i] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) w[i] = pack_bf16(p[q * 32 + 2 * i], p[q * 32 + 2 * i + 1]);
-        tmem_st16(col_s + lanes + half * 64 + q * 16, w);      // columns of this half that are in registers by now
+        for (int i = 0; i < 16; ++i) w[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
+        tmem_st16(col_s + lanes + c0, w);         // columns of this part, which are in registers
       }
       tmem_st_wait();
       tc_fence_before();
-      mbar_arrive(p_full);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_full);
       ok = wait_for(dp_full, it & 1, abort_flag, status, 61);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
+      {
         uint32_t v[32], w[16];
-        tmem_ld32(col_dp + lanes + half * 64 + q * 32, v);
+        tmem_ld32(col_dp + lanes + c0, v);
         tmem_ld_wait();
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
-          const float4 d = *reinterpret_cast<const float4*>(rows + TC_ROWS + q * 32 + i);
+          const float4 d = *reinterpret_cast<const float4*>(rows + BN + i);
           const float2 x = add_f32x2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(-d.x, -d.y));
           const float2 y = add_f32x2(make_float2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), make_float2(-d.z, -d.w));
-          w[i / 2] = pack_bf16(p[q * 32 + i] * x.x, p[q * 32 + i + 1] * x.y);
-          w[i / 2 + 1] = pack_bf16(p[q * 32 + i + 2] * y.x, p[q * 32 + i + 3] * y.y);
+          w[i / 2] = pack_bf16(p[i] * x.x, p[i + 1] * x.y);
+          w[i / 2 + 1] = pack_bf16(p[i + 2] * y.x, p[i + 3] * y.y);
         }
-        tmem_st16(col_dp + lanes + half * 64 + q * 16, w);
+        tmem_st16(col_dp + lanes + c0, w);
       }
       tmem_st_wait();
       tc_fence_before();
-      mbar_arrive(ds_full);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(ds_full);
+      q0 += BN;
+      if (q0 >= s.len) q0 = first;
     }
     if (ok) ok = wait_for(acc_full, 0, abort_flag, status, 62);
     ok = __all_sync(0xffffffffu, ok);
     tc_fence_after();
     const bool in = key < s.len;
     const float bad = ok ? 1.f : NAN;
-    store_half<DT>(head_row_out<__nv_bfloat16>(a.dv, s.begin + key, hk), col_dv + lanes, half, a.dim, in, bad);
-    store_half<DT>(head_row_out<__nv_bfloat16>(a.dk, s.begin + key, hk), col_dk + lanes, half, a.dim, in, a.scale * bad);
+    static_assert(DT == S::kParts * 32, "a part of the threads stores 32 columns of each gradient");
+    store_part(head_row_out<__nv_bfloat16>(a.dv, s.begin + key, hk), col_dv + lanes, c0, a.dim, in, bad);
+    store_part(head_row_out<__nv_bfloat16>(a.dk, s.begin + key, hk), col_dk + lanes, c0, a.dim, in, a.scale * bad);
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kIssue) {
     tc_fence_after();
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc(tmem, S::kTmem);
   }
 }
 
 template <int DT>
-__global__ void __launch_bounds__(320, 1) attn_packed_dq_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcBwdMaps maps) {
+__global__ void __launch_bounds__(BwdShape<DT>::kThreads, BwdShape<DT>::kBlocks)
+attn_packed_dq_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcBwdMaps maps) {
   using S = BwdShape<DT>;
+  constexpr int BN = S::kCols, kCopy = S::kParts * 4, kIssue = kCopy + 1;
   const int h = blockIdx.x % a.heads, hk = h / a.group;
   const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.heads, TC_ROWS);
   if (s.tile < 0) { pdl_wait(); return; }
   const int tile = (s.len + TC_ROWS - 1) / TC_ROWS - 1 - s.tile;                 // the tiles that see the most keys first
-  const int warp = threadIdx.x >> 5;
-  const int q0 = tile * TC_ROWS, n_it = ((a.causal ? min(s.len, q0 + TC_ROWS) : s.len) + TC_ROWS - 1) / TC_ROWS;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int q0 = tile * TC_ROWS, n_it = ((a.causal ? min(s.len, q0 + TC_ROWS) : s.len) + BN - 1) / BN;
 
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const sptr = smem_raw + (base - raw);
-  const uint32_t sQ = base, sO = sQ + S::kTile, sK = sO + S::kTile, sV = sK + S::kStages * S::kTile, bars = sV + S::kStages * S::kTile;
+  const uint32_t sQ = base, sO = sQ + S::kTile, sK = sO + S::kTile, sV = sK + S::kStages * S::kStream, bars = sV + S::kStages * S::kStream;
   const uint32_t q_full = bars;
   auto full = [&](int i) { return bars + 8 * (1 + i); };
   auto cleared = [&](int i) { return bars + 8 * (1 + S::kStages + i); };
@@ -708,45 +743,45 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dq_tc_kernel(const __grid_
   if (threadIdx.x == 0) {
     mbar_init(q_full, 1);
     for (int i = 0; i < S::kStages; ++i) { mbar_init(full(i), 1); mbar_init(cleared(i), 32); mbar_init(empty(i), 1); }
-    mbar_init(s_full, 1); mbar_init(s_full + 8, 1); mbar_init(dp_full, 1); mbar_init(ds_full, 256); mbar_init(acc_full, 1);
+    mbar_init(s_full, 1); mbar_init(s_full + 8, 1); mbar_init(dp_full, 1); mbar_init(ds_full, S::kParts * 4); mbar_init(acc_full, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 9) {
-    tmem_alloc(smem_u32(tmem_slot), 512);
+  if (warp == kIssue) {
+    tmem_alloc(smem_u32(tmem_slot), S::kTmem);
     tmem_relinquish();
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot, col_s = tmem, col_dp = tmem + 256, col_dq = tmem + 384;
+  const uint32_t tmem = *tmem_slot, col_s = tmem, col_dp = tmem + 2 * BN, col_dq = tmem + 3 * BN;
 
-  if (warp == 8) {                                // ---- copies
+  if (warp == kCopy) {                            // ---- copies
     int armed = 0;
     bool ok = true;
     if (elect_one()) {
       mbar_arrive_expect_tx(q_full, 2 * S::kTile);
-      load_tile<DT>(sQ, &maps.q, q_full, h, s.begin + q0);
-      load_tile<DT>(sO, &maps.d_o, q_full, h, s.begin + q0);
+      copy_rows<DT, TC_ROWS>(sQ, &maps.q, q_full, h, s.begin + q0);
+      copy_rows<DT, TC_ROWS>(sO, &maps.d_o, q_full, h, s.begin + q0);
     }
     __syncwarp();
     for (int it = 0; it < n_it; ++it) {
-      const int st = it % S::kStages, k0 = it * TC_ROWS;
+      const int st = it % S::kStages, k0 = it * BN;
       if (it >= S::kStages) ok = wait_for(empty(st), (it / S::kStages - 1) & 1, abort_flag, status, 71);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       if (elect_one()) {
-        mbar_arrive_expect_tx(full(st), 2 * S::kTile);
-        load_tile<DT>(sK + st * S::kTile, &maps.k, full(st), hk, s.begin + k0);
-        load_tile<DT>(sV + st * S::kTile, &maps.v, full(st), hk, s.begin + k0);
+        mbar_arrive_expect_tx(full(st), 2 * S::kStream);
+        copy_rows<DT, BN>(sK + st * S::kStream, &maps.k, full(st), hk, s.begin + k0);
+        copy_rows<DT, BN>(sV + st * S::kStream, &maps.v, full(st), hk, s.begin + k0);
       }
       __syncwarp();
       ++armed;
-      if (k0 + TC_ROWS > s.len) {                 // keys of other sequences, or of none: zeros, where dS is zero
+      if (k0 + BN > s.len) {                      // keys of other sequences, or of none: zeros, where dS is zero
         ok = wait_for(full(st), (it / S::kStages) & 1, abort_flag, status, 72);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        clear_rows<DT>(sptr + (sK - base) + st * S::kTile, s.len - k0);
+        clear_rows<DT>(sptr + (sK - base) + st * S::kStream, s.len - k0);
         fence_async_smem();
       }
       mbar_arrive(cleared(st));
@@ -756,8 +791,7 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dq_tc_kernel(const __grid_
       wait_for(q_full, 0, &never, status, 73);
       for (int it = max(0, armed - S::kStages); it < armed; ++it) wait_for(full(it % S::kStages), (it / S::kStages) & 1, &never, status, 73);
     }
-  } else if (warp == 9) {                         // ---- products
-    const uint32_t id_s = make_idesc_mn(128, 128, 0, 0), id_d = make_idesc_mn(128, DT, 0, 1);
+  } else if (warp == kIssue) {                    // ---- products
     auto ready = [&](int it) {
       const int st = it % S::kStages;
       return wait_for(full(st), (it / S::kStages) & 1, abort_flag, status, 74) && wait_for(cleared(st), (it / S::kStages) & 1, abort_flag, status, 75);
@@ -766,11 +800,11 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dq_tc_kernel(const __grid_
     if (ok) {
       tc_fence_after();
       if (elect_one()) {
-        mma_abt<DT>(col_s, sQ, sK, id_s);
+        mma_scores<DT>(col_s, sQ, sK);
         tc_commit(s_full);
-        mma_abt<DT>(col_dp, sO, sV, id_s);
+        mma_scores<DT>(col_dp, sO, sV);
         tc_commit(dp_full);
-        if (n_it > 1) { mma_abt<DT>(col_s + 128, sQ, sK + (1 % S::kStages) * S::kTile, id_s); tc_commit(s_full + 8); }
+        if (n_it > 1) { mma_scores<DT>(col_s + BN, sQ, sK + S::kStream); tc_commit(s_full + 8); }
       }
       __syncwarp();
     }
@@ -780,9 +814,9 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dq_tc_kernel(const __grid_
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
-        mma_ab_halves<DT>(col_dq, col_dp, sK + st * S::kTile, id_d, it > 0);
+        mma_gradient<DT>(col_dq, col_dp, sK + st * S::kStream, it > 0);
         tc_commit(empty(st));
-        if (it + 1 < n_it) { mma_abt<DT>(col_dp, sO, sV + nx * S::kTile, id_s); tc_commit(dp_full); }
+        if (it + 1 < n_it) { mma_scores<DT>(col_dp, sO, sV + nx * S::kStream); tc_commit(dp_full); }
         else tc_commit(acc_full);
       }
       __syncwarp();
@@ -790,12 +824,12 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dq_tc_kernel(const __grid_
         ok = ready(it + 2);
         if (!ok) break;
         tc_fence_after();
-        if (elect_one()) { mma_abt<DT>(col_s + (it & 1) * 128, sQ, sK + n2 * S::kTile, id_s); tc_commit(s_full + 8 * (it & 1)); }
+        if (elect_one()) { mma_scores<DT>(col_s + (it & 1) * BN, sQ, sK + n2 * S::kStream); tc_commit(s_full + 8 * (it & 1)); }
         __syncwarp();
       }
     }
-  } else {                                        // ---- values: thread = query row, half of the key columns
-    const int half = warp >> 2, r = threadIdx.x & 127, row = q0 + r;
+  } else {                                        // ---- values: thread = query row, 32 of the key columns
+    const int c0 = (warp >> 2) * 32, row = q0 + (threadIdx.x & 127);
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float c = a.scale * kLog2e;
     const int64_t at = (int64_t)h * a.tokens + s.begin + row;
@@ -803,61 +837,53 @@ __global__ void __launch_bounds__(320, 1) attn_packed_dq_tc_kernel(const __grid_
     const int limit = a.causal ? min(s.len, row + 1) : s.len;
     bool ok = true;
     for (int it = 0; it < n_it; ++it) {
-      const int k0 = it * TC_ROWS;
-      const bool edge = k0 + TC_ROWS > s.len || (a.causal && k0 + TC_ROWS > q0 + 1);
+      const int k0 = it * BN;
       ok = wait_for(s_full + 8 * (it & 1), (it >> 1) & 1, abort_flag, status, 78);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      float p[64];
+      float p[32];
+      uint32_t v[32], w[16];
+      tmem_ld32(col_s + lanes + (it & 1) * BN + c0, v);
+      tmem_ld_wait();
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        uint32_t v[32];
-        tmem_ld32(col_s + lanes + (it & 1) * 128 + half * 64 + q * 32, v);
-        tmem_ld_wait();
-#pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-          const float2 x = fma_f32x2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(c, c), make_float2(-lse, -lse));
-          p[q * 32 + i] = ex2(x.x); p[q * 32 + i + 1] = ex2(x.y);
-        }
+      for (int i = 0; i < 32; i += 2) {
+        const float2 x = fma_f32x2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(c, c), make_float2(-lse, -lse));
+        p[i] = ex2(x.x); p[i + 1] = ex2(x.y);
       }
       ok = wait_for(dp_full, it & 1, abort_flag, status, 79);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
+      tmem_ld32(col_dp + lanes + c0, v);
+      tmem_ld_wait();
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        uint32_t v[32], w[16];
-        tmem_ld32(col_dp + lanes + half * 64 + q * 32, v);
-        tmem_ld_wait();
-        float ds[32];
-#pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-          const float2 x = add_f32x2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(-delta, -delta));
-          ds[i] = p[q * 32 + i] * x.x; ds[i + 1] = p[q * 32 + i + 1] * x.y;
-        }
-        if (edge)
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (k0 + half * 64 + q * 32 + i >= limit) ds[i] = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) w[i] = pack_bf16(ds[2 * i], ds[2 * i + 1]);
-        tmem_st16(col_dp + lanes + half * 64 + q * 16, w);
+      for (int i = 0; i < 32; i += 2) {
+        const float2 x = add_f32x2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(-delta, -delta));
+        p[i] *= x.x; p[i + 1] *= x.y;
       }
+      if (k0 + BN > s.len || (a.causal && k0 + BN > q0 + 1))
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (k0 + c0 + i >= limit) p[i] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
+      tmem_st16(col_dp + lanes + c0, w);
       tmem_st_wait();
       tc_fence_before();
-      mbar_arrive(ds_full);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(ds_full);
     }
     if (ok) ok = wait_for(acc_full, 0, abort_flag, status, 80);
     ok = __all_sync(0xffffffffu, ok);
     tc_fence_after();
-    store_half<DT>(head_row_out<__nv_bfloat16>(a.dq, s.begin + row, h), col_dq + lanes, half, a.dim, row < s.len, ok ? a.scale : NAN);
+    store_part(head_row_out<__nv_bfloat16>(a.dq, s.begin + row, h), col_dq + lanes, c0, a.dim, row < s.len, ok ? a.scale : NAN);
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kIssue) {
     tc_fence_after();
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc(tmem, S::kTmem);
   }
   pdl_wait();
 }
@@ -901,14 +927,14 @@ static EncodeTiledFn encode_fn() {
   return fn;
 }
 
-// [dim, heads, tokens] map with boxes of 64 x 1 x 128; columns behind the head's width and rows behind the last token read as zeros
-static cudaError_t encode_heads(CUtensorMap* map, const HeadView& x, int dim, int heads, int64_t tokens) {
+// [dim, heads, tokens] map with boxes of 64 x 1 x rows; columns behind the head's width and rows behind the last token read as zeros
+static cudaError_t encode_heads(CUtensorMap* map, const HeadView& x, int dim, int heads, int64_t tokens, int rows) {
   const EncodeTiledFn fn = encode_fn();
   if (!fn) return cudaErrorNotSupported;
   // a dimension of one entry may come with any stride: give it a valid one
   const cuuint64_t head = heads > 1 ? (cuuint64_t)x.head * 2 : 256, token = tokens > 1 ? (cuuint64_t)x.token * 2 : 256;
   const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)tokens}, strides[2] = {head, token};
-  const cuuint32_t box[3] = {64, 1, TC_ROWS}, step[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {64, 1, (cuuint32_t)rows}, step[3] = {1, 1, 1};
   const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(x.data), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
@@ -943,9 +969,9 @@ template <int DT, int NT> static cudaError_t fwd_launch(const PackedArgs& a, cud
   using S = FwdShape<DT, NT>;
   TcMaps maps;
   cudaError_t e = allow_smem(attn_packed_fwd_tc_kernel<DT, NT>, S::kSmem, done);
-  if (e == cudaSuccess) e = encode_heads(&maps.q, a.q, a.dim, a.heads, a.tokens);
-  if (e == cudaSuccess) e = encode_heads(&maps.k, a.k, a.dim, a.kv_heads, a.tokens);
-  if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.tokens);
+  if (e == cudaSuccess) e = encode_heads(&maps.q, a.q, a.dim, a.heads, a.tokens, TC_ROWS);
+  if (e == cudaSuccess) e = encode_heads(&maps.k, a.k, a.dim, a.kv_heads, a.tokens, TC_ROWS);
+  if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.tokens, TC_ROWS);
   if (e != cudaSuccess) return e;
   const int pair = NT == 2 && a.group % 2 == 0, units = pair ? a.heads / 2 : a.heads;
   const int64_t blocks = most_tiles(a.tokens, a.n_seqs, pair ? TC_ROWS : NT * TC_ROWS) * units;
@@ -965,10 +991,10 @@ template <int DT> static cudaError_t bwd_launch(const PackedArgs& a, cudaStream_
   TcBwdMaps maps;
   cudaError_t e = allow_smem(attn_packed_dkv_tc_kernel<DT>, S::kSmem, done[0]);
   if (e == cudaSuccess) e = allow_smem(attn_packed_dq_tc_kernel<DT>, S::kSmem, done[1]);
-  if (e == cudaSuccess) e = encode_heads(&maps.q, a.q, a.dim, a.heads, a.tokens);
-  if (e == cudaSuccess) e = encode_heads(&maps.k, a.k, a.dim, a.kv_heads, a.tokens);
-  if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.tokens);
-  if (e == cudaSuccess) e = encode_heads(&maps.d_o, a.d_o, a.dim, a.heads, a.tokens);
+  if (e == cudaSuccess) e = encode_heads(&maps.q, a.q, a.dim, a.heads, a.tokens, S::kCols);
+  if (e == cudaSuccess) e = encode_heads(&maps.k, a.k, a.dim, a.kv_heads, a.tokens, S::kCols);
+  if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.tokens, S::kCols);
+  if (e == cudaSuccess) e = encode_heads(&maps.d_o, a.d_o, a.dim, a.heads, a.tokens, S::kCols);
   if (e != cudaSuccess) return e;
   const int64_t tiles = most_tiles(a.tokens, a.n_seqs, TC_ROWS);
   if (tiles * a.heads > 0x7fffffff) return cudaErrorInvalidConfiguration;
