@@ -16,7 +16,7 @@
 
 namespace pm {
 
-constexpr int PK_T = 64, PK_LDP = PK_T + 4, PK_THREADS = 256;
+constexpr int PK_T = 64, PK_LOG_T = 6, PK_LDP = PK_T + 4, PK_THREADS = 256;
 
 template <int DP> constexpr int kPkLd = DP + 4;
 template <int DP> constexpr int pk_smem(int tiles, int squares) { return (tiles * PK_T * kPkLd<DP> + squares * PK_T * PK_LDP) * 4; }
@@ -95,7 +95,7 @@ __device__ __forceinline__ void pk_store(const HeadView& x, const SeqTile& s, in
     for (int c = 0; c < DP / 16; ++c) if (pk_col<DP>(c) < dim) out[pk_col<DP>(c)] = from_f<T>(acc[i][c] * f[i]);
   }
 }
-__device__ __forceinline__ SeqTile pk_tile(const PackedArgs& a) { return find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x, PK_T); }
+__device__ __forceinline__ SeqTile pk_tile(const PackedArgs& a) { return find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x, PK_LOG_T); }
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(PK_THREADS) attn_packed_fwd_kernel(PackedArgs a) {

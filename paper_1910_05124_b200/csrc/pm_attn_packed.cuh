@@ -29,46 +29,50 @@ struct SeqTile {
   int len, tile;                                  // its length; the tile's index inside it (-1: no such tile)
 };
 
-// The index-th tile of `rows` rows, counted through the sequences; called by a whole warp, same result in every lane.  A lane takes
-// eight consecutive sequences, so up to 256 cost one round of loads.  Starts are clipped to 0 .. tokens and a sequence that
-// would end before it starts is empty: whatever the array holds, no tile reaches outside the tensors.
-__device__ __forceinline__ SeqTile find_tile(const int32_t* cu, int n_seqs, int64_t tokens, int index, int rows) {
+// Looks for the index-th tile among sequences base .. base + 32 PER - 1, PER consecutive ones to a lane; `before`: tiles in front of
+// them, on return also those among them.
+template <int PER>
+__device__ __forceinline__ bool find_tile_among(SeqTile& out, const int32_t* cu, int n_seqs, int tokens, int index, int log_rows, int base, int& before) {
   const int lane = threadIdx.x & 31;
-  int before = 0;
-  for (int base = 0; base < n_seqs; base += 256) {
-    int64_t start[9];
-    int tiles[8], mine = 0;
+  int start[PER + 1], tiles[PER], mine = 0;
 #pragma unroll
-    for (int i = 0; i < 9; ++i) {
-      const int at = min(base + lane * 8 + i, n_seqs);
-      const int64_t c = cu[at];
-      start[i] = c < 0 ? 0 : c > tokens ? tokens : c;
-    }
+  for (int i = 0; i <= PER; ++i) start[i] = min(max(cu[min(base + lane * PER + i, n_seqs)], 0), tokens);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t len = start[i + 1] - start[i];
-      tiles[i] = len > 0 ? (int)((len + rows - 1) / rows) : 0;
-      mine += tiles[i];
-    }
-    int upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2) { const int v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
-    const int first = before + upto - mine;
-    const unsigned has = __ballot_sync(0xffffffffu, index >= first && index < first + mine);
-    if (has) {
-      int at = first, tile = -1, len = 0;
-      int64_t begin = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (tile < 0 && index >= at && index < at + tiles[i]) { tile = index - at; begin = start[i]; len = (int)(start[i + 1] - start[i]); }
-        at += tiles[i];
-      }
-      const int who = __ffs(has) - 1;
-      return SeqTile{__shfl_sync(0xffffffffu, begin, who), __shfl_sync(0xffffffffu, len, who), __shfl_sync(0xffffffffu, tile, who)};
-    }
-    before += __shfl_sync(0xffffffffu, upto, 31);
+  for (int i = 0; i < PER; ++i) {
+    tiles[i] = max(start[i + 1] - start[i] + (1 << log_rows) - 1, 0) >> log_rows;
+    mine += tiles[i];
   }
-  return SeqTile{0, 0, -1};
+  int upto = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) { const int v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
+  int at = before + upto - mine;
+  const unsigned has = __ballot_sync(0xffffffffu, index >= at && index < at + mine);
+  before += __shfl_sync(0xffffffffu, upto, 31);
+  if (!has) return false;
+  int tile = 0, len = 0, begin = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (index >= at && index < at + tiles[i]) { tile = index - at; begin = start[i]; len = start[i + 1] - start[i]; }
+    at += tiles[i];
+  }
+  const int who = __ffs(has) - 1;
+  out = SeqTile{__shfl_sync(0xffffffffu, begin, who), __shfl_sync(0xffffffffu, len, who), __shfl_sync(0xffffffffu, tile, who)};
+  return true;
+}
+
+// The index-th tile of 2^log_rows rows, counted through the sequences; called by a whole warp, same result in every lane.  Up to 32
+// sequences, and then every 256, cost one round of loads.  Starts are clipped to 0 .. tokens and a sequence that would end before
+// it starts is empty: whatever the array holds, no tile reaches outside the tensors.
+__device__ __forceinline__ SeqTile find_tile(const int32_t* cu, int n_seqs, int64_t tokens, int index, int log_rows) {
+  SeqTile s{0, 0, -1};
+  int before = 0;
+  if (n_seqs <= 32) {
+    find_tile_among<1>(s, cu, n_seqs, (int)tokens, index, log_rows, 0, before);
+  } else {
+    for (int base = 0; base < n_seqs; base += 256)
+      if (find_tile_among<8>(s, cu, n_seqs, (int)tokens, index, log_rows, base, before)) break;
+  }
+  return s;
 }
 
 // tiles of `rows` rows that sequences of `tokens` tokens in all can have at most

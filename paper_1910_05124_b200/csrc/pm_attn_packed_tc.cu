@@ -23,7 +23,7 @@ namespace pm {
 // A bounded wait that ran out (a defect): its code, kept until pm_attention_packed_status reads it.
 __device__ int g_attn_packed_status;
 
-constexpr int TC_ROWS = 128;                      // rows of a tile, of queries and of keys
+constexpr int TC_ROWS = 128, TC_LOG_ROWS = 7;     // rows of a tile, of queries and of keys
 constexpr int TC_SUB = TC_ROWS * 128;             // bytes of a [128 x 64] bf16 sub-tile, 128-byte swizzle
 
 // A bounded wait in line: a call from a thread that holds a row of scores would have to put them away.
@@ -45,11 +45,13 @@ template <int DT, int NT> struct FwdShape {
   static constexpr int kSub = DT / 64;            // sub-tiles of a tile
   static constexpr int kTile = kSub * TC_SUB;
   static constexpr int kStages = NT == 1 ? (DT == 64 ? 2 : 1) : (DT == 64 ? 4 : 2);
-  static constexpr int kThreads = NT * 128 + 128;
+  static constexpr int kWarps = NT * 4;           // of the softmax: thread = row
+  static constexpr int kThreads = kWarps * 32 + 128;
   static constexpr int kBlocks = NT == 1 ? 2 : 1; // per SM
-  // registers: a softmax thread holds a row of 128 scores, the warps that copy and issue need few
-  // (NT = 2: 384 threads at 168, 2 x 128 x 224 + 128 x 48 below that; NT = 1: 256 at 128, 128 x 208 + 128 x 48)
-  static constexpr int kSoftmaxRegs = NT == 1 ? 208 : 224, kOtherRegs = 48;
+  // Registers: a softmax thread holds a row of 128 scores, the warps that copy and issue need few.  NT = 2: 384 threads are launched
+  // with 168, 256 x 224 + 128 x 56 is no more than that; NT = 1: 256 with 128, 128 x 208 + 128 x 48.
+  // (Two threads to a row, 64 scores each, took 332 us where this takes 295, and 229 where it takes 207: see FWD_FMA's sizes.)
+  static constexpr int kSoftmaxRegs = NT == 1 ? 208 : 224, kOtherRegs = NT == 1 ? 48 : 56;
   // Tensor-memory columns: S (128 for each tile), O (DT), and for heads of 64 P (64) beside S instead of over it, so that the
   // next scores are formed while the exponentials of these are.
   static constexpr int kCols = NT * 256;
@@ -69,11 +71,11 @@ template <int DT> __device__ __forceinline__ void mma_abt(uint32_t d, uint32_t a
     tc_mma_bf16(d, desc_at(base, a + off), desc_at(base, b + off), idesc, k > 0);
   }
 }
-// 128 x DT x 128 product of A in tensor memory and a tile whose rows run along the depth
-template <int DT> __device__ __forceinline__ void mma_ab(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate, int k0, int k1) {
+// 128 x DT x 64 product of half of A in tensor memory and half of a tile whose rows run along the depth
+template <int DT> __device__ __forceinline__ void mma_ab(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate, int half) {
   const uint64_t base = desc_base(TC_SUB, 1024);
 #pragma unroll
-  for (int k = k0; k < k1; ++k) tc_mma_bf16_ta(d, a + k * 8, desc_at(base, b + k * 2048), idesc, accumulate || k > k0);
+  for (int k = 0; k < 4; ++k) tc_mma_bf16_ta(d, a + (half * 4 + k) * 8, desc_at(base, b + (half * 4 + k) * 2048), idesc, accumulate || k > 0);
 }
 
 template <int DT> __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int64_t token) {
@@ -119,23 +121,7 @@ template <int DT, int NT>
 __global__ void __launch_bounds__(FwdShape<DT, NT>::kThreads, FwdShape<DT, NT>::kBlocks)
 attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcMaps maps, int units, int pair_heads) {
   using S = FwdShape<DT, NT>;
-  const int rows = pair_heads ? TC_ROWS : NT * TC_ROWS;
-  const int unit = blockIdx.x % units;
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / units, rows);
-  if (s.tile < 0) return;
-  // the last tiles of a sequence see the most keys: they come first
-  const int tile = (s.len + rows - 1) / rows - 1 - s.tile;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  auto head_of = [&](int t) { return pair_heads ? unit * 2 + t : unit; };
-  auto first_of = [&](int t) { return pair_heads ? tile * TC_ROWS : (tile * NT + t) * TC_ROWS; };
-  auto keys_of = [&](int t) {                     // key tiles that query tile t sees
-    const int q0 = first_of(t);
-    return q0 >= s.len ? 0 : ((a.causal ? min(s.len, q0 + TC_ROWS) : s.len) + TC_ROWS - 1) / TC_ROWS;
-  };
-  const int hk = head_of(0) / a.group;
-  int n_keys = keys_of(0);
-  if (NT == 2) n_keys = max(n_keys, keys_of(1));
-
+  constexpr int kCopy = S::kWarps, kIssue = kCopy + 1;                 // the warps that copy and issue
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const sptr = smem_raw + (base - raw);
@@ -153,17 +139,65 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(sptr + (bars - base) + 8 * S::kBars);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* const status = &g_attn_packed_status;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-  if (threadIdx.x == 0) {
+  // Barriers, tensor memory and the tile's place at the same time; the first copies go out as soon as the copying warp knows its tile.
+  if (warp == kCopy && lane == 0) {
     mbar_init(bar_q, 1);
     for (int i = 0; i < S::kStages; ++i) { mbar_init(k_full(i), 1); mbar_init(k_empty(i), 1); mbar_init(v_full(i), 1); mbar_init(v_empty(i), 1); }
     for (int t = 0; t < NT; ++t) { mbar_init(s_full(t), 1); mbar_init(s_read(t), 4); mbar_init(p_half(t), 4); mbar_init(p_full(t), 4); mbar_init(o_full(t), 1); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    tma_prefetch_desc(&maps.q);
+    tma_prefetch_desc(&maps.k);
+    tma_prefetch_desc(&maps.v);
   }
-  if (warp == NT * 4 + 1) {
+  if (warp == kIssue) {
     tmem_alloc(smem_u32(tmem_slot), S::kCols);
     tmem_relinquish();
+  }
+  const int log_rows = pair_heads ? TC_LOG_ROWS : TC_LOG_ROWS + NT - 1, rows = 1 << log_rows;
+  const int unit = blockIdx.x % units;
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / units, log_rows);
+  if (s.tile < 0) {
+    __syncthreads();
+    if (warp == kIssue) tmem_dealloc(*tmem_slot, S::kCols);
+    return;
+  }
+  // the last tiles of a sequence see the most keys: they come first
+  const int tile = ((s.len + rows - 1) >> log_rows) - 1 - s.tile;
+  auto head_of = [&](int t) { return pair_heads ? unit * 2 + t : unit; };
+  auto first_of = [&](int t) { return pair_heads ? tile * TC_ROWS : (tile * NT + t) * TC_ROWS; };
+  auto keys_of = [&](int t) {                     // key tiles that query tile t sees
+    const int q0 = first_of(t);
+    return q0 >= s.len ? 0 : ((a.causal ? min(s.len, q0 + TC_ROWS) : s.len) + TC_ROWS - 1) / TC_ROWS;
+  };
+  const int hk = head_of(0) / a.group;
+  int n_keys = keys_of(0);
+  if (NT == 2) n_keys = max(n_keys, keys_of(1));
+
+  auto copy_keys = [&](int j) {
+    const int st = j % S::kStages;
+    if (elect_one()) { mbar_arrive_expect_tx(k_full(st), S::kTile); load_tile<DT>(sK + st * S::kTile, &maps.k, k_full(st), hk, s.begin + j * TC_ROWS); }
+    __syncwarp();
+  };
+  auto copy_values = [&](int j) {
+    const int st = j % S::kStages;
+    if (elect_one()) { mbar_arrive_expect_tx(v_full(st), S::kTile); load_tile<DT>(sV + st * S::kTile, &maps.v, v_full(st), hk, s.begin + j * TC_ROWS); }
+    __syncwarp();
+  };
+  if (warp == kCopy) {
+    __syncwarp();
+    if (elect_one()) {
+      int bytes = 0;
+      for (int t = 0; t < NT; ++t) if (keys_of(t)) bytes += S::kTile;
+      mbar_arrive_expect_tx(bar_q, bytes);
+      for (int t = 0; t < NT; ++t)
+        if (keys_of(t)) load_tile<DT>(sQ + t * S::kTile, &maps.q, bar_q, head_of(t), s.begin + first_of(t));
+    }
+    __syncwarp();
+    copy_keys(0);
+    copy_values(0);
   }
   tc_fence_before();
   __syncthreads();
@@ -173,31 +207,23 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
   auto col_o = [&](int t) { return tmem + NT * 128 + t * DT; };
   auto col_p = [&](int t) { return S::kApart ? tmem + NT * (128 + DT) + t * 64 : col_s(t); };
 
-  if (warp >= NT * 4) {
+  if (warp >= S::kWarps) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kOtherRegs));
-  if (warp == NT * 4) {                           // ---- copies
-    int armed_k = 0, armed_v = 0;
+  if (warp == kCopy) {                            // ---- copies
+    int armed_k = 1, armed_v = 1;
     bool ok = true;
-    if (elect_one()) {
-      int bytes = 0;
-      for (int t = 0; t < NT; ++t) if (keys_of(t)) bytes += S::kTile;
-      mbar_arrive_expect_tx(bar_q, bytes);
-      for (int t = 0; t < NT; ++t)
-        if (keys_of(t)) load_tile<DT>(sQ + t * S::kTile, &maps.q, bar_q, head_of(t), s.begin + first_of(t));
-    }
-    __syncwarp();
-    for (int j = 0; j < n_keys && ok; ++j) {
+    for (int j = 1; j < n_keys && ok; ++j) {
       const int st = j % S::kStages;
       const uint32_t ph = (j / S::kStages - 1) & 1;
       if (j >= S::kStages) ok = wait_for(k_empty(st), ph, abort_flag, status, 31);
+      ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      if (elect_one()) { mbar_arrive_expect_tx(k_full(st), S::kTile); load_tile<DT>(sK + st * S::kTile, &maps.k, k_full(st), hk, s.begin + j * TC_ROWS); }
-      __syncwarp();
+      copy_keys(j);
       ++armed_k;
       if (j >= S::kStages) ok = wait_for(v_empty(st), ph, abort_flag, status, 32);
+      ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      if (elect_one()) { mbar_arrive_expect_tx(v_full(st), S::kTile); load_tile<DT>(sV + st * S::kTile, &maps.v, v_full(st), hk, s.begin + j * TC_ROWS); }
-      __syncwarp();
+      copy_values(j);
       ++armed_v;
     }
     if (*abort_flag) {                            // nothing may be in flight when the block ends
@@ -206,7 +232,7 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
       for (int j = max(0, armed_k - S::kStages); j < armed_k; ++j) wait_for(k_full(j % S::kStages), (j / S::kStages) & 1, &never, status, 33);
       for (int j = max(0, armed_v - S::kStages); j < armed_v; ++j) wait_for(v_full(j % S::kStages), (j / S::kStages) & 1, &never, status, 33);
     }
-  } else if (warp == NT * 4 + 1) {                // ---- products
+  } else if (warp == kIssue) {                    // ---- products
     const uint32_t id_s = make_idesc_mn(128, 128, 0, 0), id_o = make_idesc_mn(128, DT, 0, 1);
     bool ok = wait_for(bar_q, 0, abort_flag, status, 34) && wait_for(k_full(0), 0, abort_flag, status, 35);
     if (ok) {
@@ -222,11 +248,11 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
       const uint32_t v = sV + (j % S::kStages) * S::kTile;
       if (!wait_for(p_half(t), j & 1, abort_flag, status, 38)) return false;
       tc_fence_after();
-      if (elect_one()) mma_ab<DT>(col_o(t), col_p(t), v, id_o, j > 0, 0, 4);
+      if (elect_one()) mma_ab<DT>(col_o(t), col_p(t), v, id_o, j > 0, 0);
       __syncwarp();
       if (!wait_for(p_full(t), j & 1, abort_flag, status, 38)) return false;
       tc_fence_after();
-      if (elect_one()) mma_ab<DT>(col_o(t), col_p(t), v, id_o, true, 4, 8);
+      if (elect_one()) mma_ab<DT>(col_o(t), col_p(t), v, id_o, true, 1);
       __syncwarp();
       return true;
     };
@@ -351,13 +377,13 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
           m = up;
           l *= f;
 #pragma unroll
-          for (int q = 0; q < DT / 32; ++q) {
-            uint32_t o[32];
-            tmem_ld32(to + q * 32, o);
+          for (int q = 0; q < DT / 16; ++q) {
+            uint32_t o[16];
+            tmem_ld16(to + q * 16, o);
             tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-            tmem_st32(to + q * 32, o);
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_st16(to + q * 16, o);
           }
         }
         float2 sum = make_float2(0.f, 0.f);
@@ -415,7 +441,7 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == NT * 4 + 1) {
+  if (warp == kIssue) {
     tc_fence_after();
     tmem_dealloc(tmem, S::kCols);
   }
@@ -509,7 +535,7 @@ attn_packed_dkv_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
   using S = BwdShape<DT>;
   constexpr int BN = S::kCols, kCopy = S::kParts * 4, kIssue = kCopy + 1;        // the warps that copy and issue
   const int hk = blockIdx.x % a.kv_heads;
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.kv_heads, TC_ROWS);
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.kv_heads, TC_LOG_ROWS);
   if (s.tile < 0) { pdl_wait(); pdl_trigger(); return; }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int k0 = s.tile * TC_ROWS, first = a.causal ? k0 : 0;
@@ -721,7 +747,7 @@ attn_packed_dq_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_cons
   using S = BwdShape<DT>;
   constexpr int BN = S::kCols, kCopy = S::kParts * 4, kIssue = kCopy + 1;
   const int h = blockIdx.x % a.heads, hk = h / a.group;
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.heads, TC_ROWS);
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.heads, TC_LOG_ROWS);
   if (s.tile < 0) { pdl_wait(); return; }
   const int tile = (s.len + TC_ROWS - 1) / TC_ROWS - 1 - s.tile;                 // the tiles that see the most keys first
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
