@@ -19,16 +19,50 @@ namespace pm {
 constexpr int PK_T = 64, PK_LOG_T = 6, PK_LDP = PK_T + 4, PK_THREADS = 256;
 
 template <int DP> constexpr int kPkLd = DP + 4;
-template <int DP> constexpr int pk_smem(int tiles, int squares) { return (tiles * PK_T * kPkLd<DP> + squares * PK_T * PK_LDP) * 4; }
+template <int DP> constexpr int pk_smem(int tiles, int squares) { return (tiles * PK_T * kPkLd<DP> + squares * PK_T * PK_LDP + 2 * PK_T) * 4; }
 
-// rows row0 .. row0 + 63 of a head into a tile, zeros outside the sequence and behind the head's width
-template <typename T, int DP>
-__device__ __forceinline__ void pk_load(float* tile, const HeadView& x, const SeqTile& s, int row0, int head, int dim) {
-  for (int i = threadIdx.x; i < PK_T * DP; i += PK_THREADS) {
-    const int r = i / DP, c = i % DP;
-    tile[r * kPkLd<DP> + c] = (row0 + r < s.len && c < dim) ? to_f<T>(head_row<T>(x, s.begin + row0 + r, head)[c]) : 0.f;
+// Rows row0 .. row0 + 63 of a head, zeros outside the sequence and behind the head's width: four consecutive values to a register
+// quadruple, all of a thread's loads in flight before the first is put into the tile.  VEC: one load brings the four.
+template <typename T, int DP, bool VEC> struct PkRows {
+  static constexpr int kN = DP / 16;
+  float4 v[kN];
+  __device__ __forceinline__ void fetch(const HeadView& x, const SeqTile& s, int row0, int head, int dim) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int at = i * PK_THREADS + threadIdx.x, r = at / (DP / 4), c = at % (DP / 4) * 4;
+      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (row0 + r >= s.len || c >= dim) continue;
+      const T* p = head_row<T>(x, s.begin + row0 + r, head) + c;
+      if constexpr (VEC && sizeof(T) == 4) {
+        v[i] = *reinterpret_cast<const float4*>(p);
+      } else if constexpr (VEC) {
+        const uint2 q = *reinterpret_cast<const uint2*>(p);
+        v[i] = make_float4(__uint_as_float(q.x << 16), __uint_as_float(q.x & 0xFFFF0000u), __uint_as_float(q.y << 16), __uint_as_float(q.y & 0xFFFF0000u));
+      } else {
+        v[i].x = to_f<T>(p[0]);
+        if (c + 1 < dim) v[i].y = to_f<T>(p[1]);
+        if (c + 2 < dim) v[i].z = to_f<T>(p[2]);
+        if (c + 3 < dim) v[i].w = to_f<T>(p[3]);
+      }
+    }
   }
-}
+  __device__ __forceinline__ void put(float* tile) const {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int at = i * PK_THREADS + threadIdx.x;
+      *reinterpret_cast<float4*>(tile + at / (DP / 4) * kPkLd<DP> + at % (DP / 4) * 4) = v[i];
+    }
+  }
+};
+// A tile of each of two tensors per step.  The next step's are fetched while this one's are worked on, where registers allow.
+template <typename T, int DP, bool VEC> struct PkPair {
+  static constexpr bool kAhead = DP <= 64;
+  PkRows<T, DP, VEC> x, y;
+  __device__ __forceinline__ void fetch(const HeadView& a, const HeadView& b, const SeqTile& s, int row0, int head, int dim) {
+    x.fetch(a, s, row0, head, dim);
+    y.fetch(b, s, row0, head, dim);
+  }
+};
 
 // acc[i][j] += A[4 ty + i] . B[tx + 16 j]
 template <int DP> __device__ __forceinline__ void pk_abt(float (&acc)[4][4], const float* A, const float* B) {
@@ -97,7 +131,7 @@ __device__ __forceinline__ void pk_store(const HeadView& x, const SeqTile& s, in
 }
 __device__ __forceinline__ SeqTile pk_tile(const PackedArgs& a) { return find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x, PK_LOG_T); }
 
-template <typename T, int DP>
+template <typename T, int DP, bool VEC>
 __global__ void __launch_bounds__(PK_THREADS) attn_packed_fwd_kernel(PackedArgs a) {
   const SeqTile s = pk_tile(a);
   if (s.tile < 0) return;
@@ -105,16 +139,24 @@ __global__ void __launch_bounds__(PK_THREADS) attn_packed_fwd_kernel(PackedArgs 
   float *sQ = sm, *sK = sQ + PK_T * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sP = sV + PK_T * kPkLd<DP>;
   const int h = blockIdx.y, hk = h / a.group, q0 = s.tile * PK_T;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  pk_load<T, DP>(sQ, a.q, s, q0, h, a.dim);
+  PkPair<T, DP, VEC> next;
+  {
+    PkRows<T, DP, VEC> q;
+    q.fetch(a.q, s, q0, h, a.dim);
+    if (next.kAhead) next.fetch(a.k, a.v, s, 0, hk, a.dim);
+    q.put(sQ);
+  }
   float o[4][DP / 16] = {}, m[4], l[4] = {};
 #pragma unroll
   for (int i = 0; i < 4; ++i) m[i] = -INFINITY;
   const int end = a.causal ? min(s.len, q0 + PK_T) : s.len;
   for (int k0 = 0; k0 < end; k0 += PK_T) {
+    if (!next.kAhead) next.fetch(a.k, a.v, s, k0, hk, a.dim);
     __syncthreads();
-    pk_load<T, DP>(sK, a.k, s, k0, hk, a.dim);
-    pk_load<T, DP>(sV, a.v, s, k0, hk, a.dim);
+    next.x.put(sK);
+    next.y.put(sV);
     __syncthreads();
+    if (next.kAhead && k0 + PK_T < end) next.fetch(a.k, a.v, s, k0 + PK_T, hk, a.dim);
     float acc[4][4] = {};
     pk_abt<DP>(acc, sQ, sK);
 #pragma unroll
@@ -175,16 +217,22 @@ __global__ void __launch_bounds__(256) attn_packed_delta_kernel(PackedArgs a) {
   }
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool VEC>
 __global__ void __launch_bounds__(PK_THREADS) attn_packed_dq_kernel(PackedArgs a) {
   const SeqTile s = pk_tile(a);
-  if (s.tile < 0) return;
+  if (s.tile < 0) { pdl_wait(); return; }
   extern __shared__ float sm[];
   float *sQ = sm, *sO = sQ + PK_T * kPkLd<DP>, *sK = sO + PK_T * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sS = sV + PK_T * kPkLd<DP>;
   const int h = blockIdx.y, hk = h / a.group, q0 = s.tile * PK_T;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  pk_load<T, DP>(sQ, a.q, s, q0, h, a.dim);
-  pk_load<T, DP>(sO, a.d_o, s, q0, h, a.dim);
+  PkPair<T, DP, VEC> next;
+  {
+    PkPair<T, DP, VEC> own;
+    own.fetch(a.q, a.d_o, s, q0, h, a.dim);
+    if (next.kAhead) next.fetch(a.k, a.v, s, 0, hk, a.dim);
+    own.x.put(sQ);
+    own.y.put(sO);
+  }
   float lse[4], delta[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -195,10 +243,12 @@ __global__ void __launch_bounds__(PK_THREADS) attn_packed_dq_kernel(PackedArgs a
   float dq[4][DP / 16] = {};
   const int end = a.causal ? min(s.len, q0 + PK_T) : s.len;
   for (int k0 = 0; k0 < end; k0 += PK_T) {
+    if (!next.kAhead) next.fetch(a.k, a.v, s, k0, hk, a.dim);
     __syncthreads();
-    pk_load<T, DP>(sK, a.k, s, k0, hk, a.dim);
-    pk_load<T, DP>(sV, a.v, s, k0, hk, a.dim);
+    next.x.put(sK);
+    next.y.put(sV);
     __syncthreads();
+    if (next.kAhead && k0 + PK_T < end) next.fetch(a.k, a.v, s, k0 + PK_T, hk, a.dim);
     float acc[4][4] = {}, dp[4][4] = {};
     pk_abt<DP>(acc, sQ, sK);
     pk_abt<DP>(dp, sO, sV);
@@ -215,47 +265,72 @@ __global__ void __launch_bounds__(PK_THREADS) attn_packed_dq_kernel(PackedArgs a
   }
   const float f[4] = {a.scale, a.scale, a.scale, a.scale};
   pk_store<T, DP>(a.dq, s, q0, h, a.dim, dq, f);
+  pdl_wait();
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool VEC>
 __global__ void __launch_bounds__(PK_THREADS) attn_packed_dkv_kernel(PackedArgs a) {
   const SeqTile s = pk_tile(a);
-  if (s.tile < 0) return;
+  if (s.tile < 0) { pdl_wait(); pdl_trigger(); return; }
   extern __shared__ float sm[];
   float *sK = sm, *sV = sK + PK_T * kPkLd<DP>, *sQ = sV + PK_T * kPkLd<DP>, *sO = sQ + PK_T * kPkLd<DP>, *sP = sO + PK_T * kPkLd<DP>,
-        *sS = sP + PK_T * PK_LDP;
+        *sS = sP + PK_T * PK_LDP, *sR = sS + PK_T * PK_LDP;
   const int hk = blockIdx.y, k0 = s.tile * PK_T;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  pk_load<T, DP>(sK, a.k, s, k0, hk, a.dim);
-  pk_load<T, DP>(sV, a.v, s, k0, hk, a.dim);
+  const int first = a.causal ? k0 : 0, per_head = (s.len - first + PK_T - 1) / PK_T, n_it = per_head * a.group;
+  // a query tile's lse (threads 0 .. 63) and delta (64 .. 127) travel with it
+  auto row_value = [&](int h, int q0) {
+    const int r = q0 + (threadIdx.x & 63);
+    if (threadIdx.x >= 128 || r >= s.len) return 0.f;
+    return (threadIdx.x < 64 ? a.lse : a.delta)[(int64_t)h * a.tokens + s.begin + r];
+  };
+  PkPair<T, DP, VEC> next;
+  {
+    PkPair<T, DP, VEC> own;
+    own.fetch(a.k, a.v, s, k0, hk, a.dim);
+    pdl_wait();                                   // delta
+    pdl_trigger();
+    if (next.kAhead) next.fetch(a.q, a.d_o, s, first, hk * a.group, a.dim);
+    own.x.put(sK);
+    own.y.put(sV);
+  }
+  float next_row = row_value(hk * a.group, first);
   float dk[4][DP / 16] = {}, dv[4][DP / 16] = {};
-  for (int h = hk * a.group; h < (hk + 1) * a.group; ++h)
-    for (int q0 = a.causal ? k0 : 0; q0 < s.len; q0 += PK_T) {
-      __syncthreads();
-      pk_load<T, DP>(sQ, a.q, s, q0, h, a.dim);
-      pk_load<T, DP>(sO, a.d_o, s, q0, h, a.dim);
-      __syncthreads();
-      float acc[4][4] = {}, dp[4][4] = {};
-      pk_abt<DP>(acc, sK, sQ);                    // rows: keys, columns: queries
-      pk_abt<DP>(dp, sV, sO);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int r = q0 + tx + 16 * j;
-        const int64_t at = (int64_t)h * a.tokens + s.begin + r;
-        const float lse = r < s.len ? a.lse[at] : 0.f, delta = r < s.len ? a.delta[at] : 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int c = k0 + 4 * ty + i;
-          const bool in = c < s.len && r < s.len && (!a.causal || c <= r);
-          const float p = in ? ex2((acc[i][j] * a.scale - lse) * kLog2e) : 0.f;
-          sP[(4 * ty + i) * PK_LDP + tx + 16 * j] = p;
-          sS[(4 * ty + i) * PK_LDP + tx + 16 * j] = in ? p * (dp[i][j] - delta) : 0.f;
-        }
-      }
-      __syncthreads();
-      pk_pb<DP>(dv, sP, sO);
-      pk_pb<DP>(dk, sS, sQ);
+  int h = hk * a.group, q0 = first;
+  for (int it = 0; it < n_it; ++it) {
+    if (!next.kAhead) next.fetch(a.q, a.d_o, s, q0, h, a.dim);
+    __syncthreads();
+    next.x.put(sQ);
+    next.y.put(sO);
+    if (threadIdx.x < 128) sR[threadIdx.x] = next_row;
+    __syncthreads();
+    const int r0 = q0;
+    q0 += PK_T;
+    if (q0 >= s.len) { q0 = first; ++h; }
+    if (it + 1 < n_it) {
+      next_row = row_value(h, q0);
+      if (next.kAhead) next.fetch(a.q, a.d_o, s, q0, h, a.dim);
     }
+    float acc[4][4] = {}, dp[4][4] = {};
+    pk_abt<DP>(acc, sK, sQ);                      // rows: keys, columns: queries
+    pk_abt<DP>(dp, sV, sO);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = r0 + tx + 16 * j;
+      const float lse = sR[tx + 16 * j], delta = sR[64 + tx + 16 * j];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = k0 + 4 * ty + i;
+        const bool in = c < s.len && r < s.len && (!a.causal || c <= r);
+        const float p = in ? ex2((acc[i][j] * a.scale - lse) * kLog2e) : 0.f;
+        sP[(4 * ty + i) * PK_LDP + tx + 16 * j] = p;
+        sS[(4 * ty + i) * PK_LDP + tx + 16 * j] = in ? p * (dp[i][j] - delta) : 0.f;
+      }
+    }
+    __syncthreads();
+    pk_pb<DP>(dv, sP, sO);
+    pk_pb<DP>(dk, sS, sQ);
+  }
   const float f[4] = {a.scale, a.scale, a.scale, a.scale}, one[4] = {1.f, 1.f, 1.f, 1.f};
   pk_store<T, DP>(a.dk, s, k0, hk, a.dim, dk, f);
   pk_store<T, DP>(a.dv, s, k0, hk, a.dim, dv, one);
@@ -272,27 +347,35 @@ template <typename K> static cudaError_t pk_allow(K kernel, int bytes, std::atom
   return e;
 }
 
-template <typename T, int DP> static cudaError_t pk_forward(const PackedArgs& a, cudaStream_t st) {
+template <typename T, int DP, bool VEC> static cudaError_t pk_forward(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   constexpr int smem = pk_smem<DP>(3, 1);
-  const cudaError_t e = pk_allow(attn_packed_fwd_kernel<T, DP>, smem, done);
+  const cudaError_t e = pk_allow(attn_packed_fwd_kernel<T, DP, VEC>, smem, done);
   if (e != cudaSuccess) return e;
-  return launch_pdl(attn_packed_fwd_kernel<T, DP>, dim3((unsigned)most_tiles(a.tokens, a.n_seqs, PK_T), a.heads), dim3(PK_THREADS), smem, st, false, a);
+  return launch_pdl(attn_packed_fwd_kernel<T, DP, VEC>, dim3((unsigned)most_tiles(a.tokens, a.n_seqs, PK_T), a.heads), dim3(PK_THREADS), smem, st, false, a);
 }
-template <typename T, int DP> static cudaError_t pk_backward(const PackedArgs& a, cudaStream_t st) {
+template <typename T, int DP, bool VEC> static cudaError_t pk_backward(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done[2];
-  cudaError_t e = pk_allow(attn_packed_dq_kernel<T, DP>, pk_smem<DP>(4, 1), done[0]);
-  if (e == cudaSuccess) e = pk_allow(attn_packed_dkv_kernel<T, DP>, pk_smem<DP>(4, 2), done[1]);
+  cudaError_t e = pk_allow(attn_packed_dq_kernel<T, DP, VEC>, pk_smem<DP>(4, 1), done[0]);
+  if (e == cudaSuccess) e = pk_allow(attn_packed_dkv_kernel<T, DP, VEC>, pk_smem<DP>(4, 2), done[1]);
   const unsigned tiles = (unsigned)most_tiles(a.tokens, a.n_seqs, PK_T);
   if (e == cudaSuccess) e = launch_pdl(attn_packed_delta_kernel<T>, dim3((unsigned)((a.tokens * a.heads + 7) / 8)), dim3(256), 0, st, false, a);
-  if (e == cudaSuccess) e = launch_pdl(attn_packed_dkv_kernel<T, DP>, dim3(tiles, a.kv_heads), dim3(PK_THREADS), pk_smem<DP>(4, 2), st, false, a);
-  if (e == cudaSuccess) e = launch_pdl(attn_packed_dq_kernel<T, DP>, dim3(tiles, a.heads), dim3(PK_THREADS), pk_smem<DP>(4, 1), st, false, a);
+  // dq starts once every block of dk, dv has passed its wait for delta, beside them; it ends behind them
+  if (e == cudaSuccess) e = launch_pdl(attn_packed_dkv_kernel<T, DP, VEC>, dim3(tiles, a.kv_heads), dim3(PK_THREADS), pk_smem<DP>(4, 2), st, true, a);
+  if (e == cudaSuccess) e = launch_pdl(attn_packed_dq_kernel<T, DP, VEC>, dim3(tiles, a.heads), dim3(PK_THREADS), pk_smem<DP>(4, 1), st, true, a);
   return e;
 }
+template <typename T, int DP> static cudaError_t pk_width(const PackedArgs& a, bool backward, cudaStream_t st) {
+  // four elements at a time where every row of the inputs starts at such a boundary
+  const size_t bytes = 4 * sizeof(T);
+  bool vec = a.dim % 4 == 0;
+  for (const HeadView* x : {&a.q, &a.k, &a.v, backward ? &a.d_o : &a.q}) vec = vec && aligned_to(x->data, bytes) && x->token % 4 == 0 && x->head % 4 == 0;
+  if (vec) return backward ? pk_backward<T, DP, true>(a, st) : pk_forward<T, DP, true>(a, st);
+  return backward ? pk_backward<T, DP, false>(a, st) : pk_forward<T, DP, false>(a, st);
+}
 template <typename T> static cudaError_t pk_run(const PackedArgs& a, bool backward, cudaStream_t st) {
-  if (a.dim <= 32) return backward ? pk_backward<T, 32>(a, st) : pk_forward<T, 32>(a, st);
-  if (a.dim <= 64) return backward ? pk_backward<T, 64>(a, st) : pk_forward<T, 64>(a, st);
-  return backward ? pk_backward<T, 128>(a, st) : pk_forward<T, 128>(a, st);
+  if (a.dim <= 32) return pk_width<T, 32>(a, backward, st);
+  return a.dim <= 64 ? pk_width<T, 64>(a, backward, st) : pk_width<T, 128>(a, backward, st);
 }
 
 static pm_status pk_check(const pm_attention_desc* d) {
