@@ -182,10 +182,67 @@ template <typename T> __device__ void block_top(LpShared& sh, const RowVectors<T
   }
 }
 
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(kLpThreads, 4) logprob_kernel(LogprobArgs a) {
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+__device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// the largest value of 16 bytes of logits and what came before
+__device__ __forceinline__ float max_of(const uint4& q, float m, float) {
+  return max_nan(max_nan(m, max_nan(__uint_as_float(q.x), __uint_as_float(q.y))), max_nan(__uint_as_float(q.z), __uint_as_float(q.w)));
+}
+__device__ __forceinline__ float max_of(const uint4& q, float m, __nv_bfloat16) {
+  const uint32_t r = max_nan_bf16x2(max_nan_bf16x2(q.x, q.y), max_nan_bf16x2(q.z, q.w));
+  return max_nan(m, max_nan(__uint_as_float(r << 16), __uint_as_float(r & 0xFFFF0000u)));
+}
+
+// Sums of a thread's vectors.  ENTROPY: with the sum that it needs, and a floor under x - m: at -200 the exponential is zero and its
+// product with the difference too, at -infinity the product would not be.
+template <typename T, bool ENTROPY, int U> __device__ __forceinline__ void take(Sums& st, const uint4 (&q)[U]) {
+  constexpr int N = Vec<T>::n;
+  float m = st.m;
+#pragma unroll
+  for (int u = 0; u < U; ++u) m = max_of(q[u], m, T());
+  if (m != st.m) rebase(st, m);
+  const float base = m == -INFINITY ? 0.f : m;
+  float2 s = make_float2(0.f, 0.f), t = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float v[N];
+    unpack16(q[u], v);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      float2 d = add2(make_float2(v[i], v[i + 1]), make_float2(-base, -base));
+      if (ENTROPY) d = make_float2(fmaxf(d.x, -200.f), fmaxf(d.y, -200.f));
+      const float2 x = fma2(d, make_float2(kLog2e, kLog2e), make_float2(0.f, 0.f));
+      const float2 e = make_float2(ex2(x.x), ex2(x.y));
+      s = add2(s, e);
+      if (ENTROPY) t = fma2(e, d, t);
+    }
+  }
+  st.s += s.x + s.y;
+  if (ENTROPY) st.t += t.x + t.y;
+}
+
+// Six blocks to an SM: the end of a row (joining the sums, ranking the alternatives) is a chain of short steps that the other blocks'
+// loads run beside.
+template <typename T, bool TOP, bool ENTROPY>
+__global__ void __launch_bounds__(kLpThreads, 6) logprob_kernel(LogprobArgs a) {
   __shared__ LpShared sh;
-  constexpr int N = Vec<T>::n, kUnroll = 4;
+  constexpr int U = 4;
   cg::cluster_group cluster = cg::this_cluster();
   const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
   const int64_t row = blockIdx.x / parts;
@@ -194,45 +251,27 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_kernel(LogprobArgs a) {
   const int j0 = (int)((int64_t)x.count * part / parts), j1 = (int)((int64_t)x.count * (part + 1) / parts);
 
   Sums st{-INFINITY, 0.f, 0.f};
-  auto take = [&](const float* v, int n) {
-    float m = st.m;
-    for (int i = 0; i < n; ++i) m = max_nan(m, v[i]);
-    if (m != st.m) rebase(st, m);
-    const float base = m == -INFINITY ? 0.f : m;
-    for (int i = 0; i < n; ++i) {
-      const float d = fmaxf(v[i] - base, -200.f), e = ex2(d * kLog2e);   // at -200 the exponential is zero and the product too
-      st.s += e;
-      st.t = fmaf(e, d, st.t);
+  const uint32_t none2 = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;   // -infinity, or two of them
+  for (int j = j0 + tid; j < j1; j += U * kLpThreads) {
+    uint4 q[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = j + u * kLpThreads;
+      q[u] = at < j1 && x.whole(at) ? x.load(at) : make_uint4(none2, none2, none2, none2);
     }
-  };
-  int j = j0 + tid;
-  for (; j + (kUnroll - 1) * kLpThreads < j1 && x.whole(j) && x.whole(j + (kUnroll - 1) * kLpThreads); j += kUnroll * kLpThreads) {
-    uint4 q[kUnroll];
-    float v[kUnroll][N];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) q[u] = x.load(j + u * kLpThreads);
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) unpack16(q[u], v[u]);
-    float m = st.m;
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-      for (int i = 0; i < N; ++i) m = max_nan(m, v[u][i]);
-    if (m != st.m) rebase(st, m);
-    const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float d = fmaxf(v[u][i] - base, -200.f), e = ex2(d * kLog2e);   // at -200 the exponential is zero and the product too
-        st.s += e;
-        st.t = fmaf(e, d, st.t);
-      }
+    take<T, ENTROPY>(st, q);
   }
-  for (; j < j1; j += kLpThreads) {
-    float v[N];
+  // the vectors that reach over the row's ends, by the threads whose turn they are
+  for (int e = 0; e < 2; ++e) {
+    const int j = e ? x.count - 1 : 0;
+    if (j < j0 || j >= j1 || (j - j0) % kLpThreads != tid || x.whole(j) || (e && x.count == 1)) continue;
+    float v[Vec<T>::n];
     x.get(j, v);
-    take(v, N);
+#pragma unroll
+    for (int i = 0; i < Vec<T>::n; ++i) {
+      const Sums one{v[i], v[i] == -INFINITY ? 0.f : 1.f, 0.f};
+      st = join(st, one);
+    }
   }
   const float mine = st.m;
 #pragma unroll
@@ -401,7 +440,9 @@ template <typename T> static cudaError_t logprob_launch(const LogprobArgs& a, in
   at[0].val.clusterDim.x = parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return a.top_k ? cudaLaunchKernelEx(&cfg, logprob_kernel<T, true>, a) : cudaLaunchKernelEx(&cfg, logprob_kernel<T, false>, a);
+  void (*kernel)(LogprobArgs) = a.top_k ? (a.entropy ? logprob_kernel<T, true, true> : logprob_kernel<T, true, false>)
+                                        : (a.entropy ? logprob_kernel<T, false, true> : logprob_kernel<T, false, false>);
+  return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 static pm_status logprob_shape(int32_t dtype, int64_t rows, int32_t vocab, int64_t row_stride, const void* logits) {
