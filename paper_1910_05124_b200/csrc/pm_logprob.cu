@@ -83,17 +83,73 @@ __device__ __forceinline__ bool beats(float v, int id, float w, int other) { ret
 
 struct LpShared {
   Sums warp[kLpWarps];
-  Sums block;                                     // read by the cluster
+  Sums block[kLpMaxCluster];                      // of the cluster's blocks, in its first
   float lane_max[kLpWarps][32];
   float threshold;
   int n_list;
   float list_v[kLpList];
   int list_id[kLpList];
-  float top_v[kLpMaxK];                           // this block's best, in order; read by the cluster
+  float top_v[kLpMaxK];                           // this block's best, in order
   int top_id[kLpMaxK];
-  float all_v[kLpMaxCluster * kLpMaxK];
+  float all_v[kLpMaxCluster * kLpMaxK];           // the blocks' best, in the cluster's first
   int all_id[kLpMaxCluster * kLpMaxK];
 };
+
+// bitonic sort over the lanes, descending
+__device__ __forceinline__ float sorted_down(float v) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+    for (int step = size / 2; step > 0; step /= 2) {
+      const float o = __shfl_xor_sync(0xffffffffu, v, step);
+      v = ((lane & size) == 0) == ((lane & step) == 0) ? fmaxf(v, o) : fminf(v, o);
+    }
+  return v;
+}
+// the best of vector j's elements that come after (last_v, last_id), and of (bv, bid)
+template <typename T> __device__ __forceinline__ void best_after(const RowVectors<T>& x, int j, float last_v, int last_id, float& bv, int& bid) {
+  float v[Vec<T>::n];
+  x.get(j, v);
+#pragma unroll
+  for (int i = 0; i < Vec<T>::n; ++i) {
+    const int id = x.first(j) + i;
+    if (id >= 0 && id < x.vocab && beats(last_v, last_id, v[i], id) && beats(v[i], id, bv, bid)) { bv = v[i]; bid = id; }
+  }
+}
+__device__ __forceinline__ void warp_best(float& bv, int& bid) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float ov = __shfl_xor_sync(0xffffffffu, bv, o);
+    const int oid = __shfl_xor_sync(0xffffffffu, bid, o);
+    if (beats(ov, oid, bv, bid)) { bv = ov; bid = oid; }
+  }
+}
+
+// What a row's sums say.
+struct RowResult {
+  float m, log_s, entropy;
+  bool none, empty;                               // a NaN or +infinity in the row: no distribution; nothing but -infinity
+  __device__ __forceinline__ explicit RowResult(const Sums& st)
+      : m(st.m), log_s(logf(st.s)), entropy(log_s - st.t / st.s), none(!(st.m < INFINITY)), empty(st.m == -INFINITY) {}
+  __device__ __forceinline__ float log_p(float v) const { return none ? NAN : empty ? -INFINITY : (v - m) - log_s; }
+  template <typename T> __device__ __forceinline__ void write(const LogprobArgs& a, const RowVectors<T>& x, int64_t row) const {
+    if (a.lse) a.lse[row] = none ? NAN : empty ? -INFINITY : m + log_s;
+    if (a.entropy) a.entropy[row] = none ? NAN : empty ? 0.f : entropy;
+    if (a.targets) {
+      const int y = a.targets[row];
+      a.logprob[row] = y >= a.vocab ? NAN : y < 0 ? 0.f : log_p(to_f<T>(x.row[y]));
+    }
+  }
+  __device__ __forceinline__ void write_top(const LogprobArgs& a, int64_t row, int rank, float v, int id) const {
+    a.top_logprob[row * a.top_k + rank] = log_p(v);
+    a.top_ids[row * a.top_k + rank] = none ? -1 : id;
+  }
+};
+
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // The k best of the block's vectors [j0, j1) in order into sh.top_*: value descending, then index ascending.  `mine` is the largest
 // value of the thread's own vectors j0 + threadIdx.x, + kLpThreads, ...  Missing entries are (-infinity, vocab).
@@ -107,16 +163,7 @@ template <typename T> __device__ void block_top(LpShared& sh, const RowVectors<T
     float v = sh.lane_max[0][lane];
 #pragma unroll
     for (int w = 1; w < kLpWarps; ++w) v = fmaxf(v, sh.lane_max[w][lane]);
-    // bitonic sort over the lanes, descending
-#pragma unroll
-    for (int size = 2; size <= 32; size *= 2)
-#pragma unroll
-      for (int step = size / 2; step > 0; step /= 2) {
-        const float o = __shfl_xor_sync(0xffffffffu, v, step);
-        const bool down = (lane & size) == 0, low = (lane & step) == 0;
-        v = down == low ? fmaxf(v, o) : fminf(v, o);
-      }
-    const float th = __shfl_sync(0xffffffffu, v, k - 1);
+    const float th = __shfl_sync(0xffffffffu, sorted_down(v), k - 1);
     if (lane == 0) sh.threshold = th;
   }
   __syncthreads();
@@ -157,21 +204,8 @@ template <typename T> __device__ void block_top(LpShared& sh, const RowVectors<T
   for (int r = 0; r < k; ++r) {                    // the best of what comes after the last one found
     float bv = -INFINITY;
     int bid = x.vocab;
-    for (int j = j0 + tid; j < j1; j += kLpThreads) {
-      float v[Vec<T>::n];
-      x.get(j, v);
-#pragma unroll
-      for (int i = 0; i < Vec<T>::n; ++i) {
-        const int id = x.first(j) + i;
-        if (id >= 0 && id < x.vocab && beats(last_v, last_id, v[i], id) && beats(v[i], id, bv, bid)) { bv = v[i]; bid = id; }
-      }
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const float ov = __shfl_xor_sync(0xffffffffu, bv, o);
-      const int oid = __shfl_xor_sync(0xffffffffu, bid, o);
-      if (beats(ov, oid, bv, bid)) { bv = ov; bid = oid; }
-    }
+    for (int j = j0 + tid; j < j1; j += kLpThreads) best_after(x, j, last_v, last_id, bv, bid);
+    warp_best(bv, bid);
     if (lane == 0) { sh.list_v[warp] = bv; sh.list_id[warp] = bid; }
     __syncthreads();
     bv = sh.list_v[0]; bid = sh.list_id[0];
@@ -247,6 +281,7 @@ __global__ void __launch_bounds__(kLpThreads, 6) logprob_kernel(LogprobArgs a) {
   const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
   const int64_t row = blockIdx.x / parts;
   const int tid = threadIdx.x, lane = tid & 31;
+  if (parts > 1) cluster_arrive_relaxed();        // this block has begun: the others may write to its shared memory
   const RowVectors<T> x(static_cast<const T*>(a.logits) + row * a.row_stride, a.vocab);
   const int j0 = (int)((int64_t)x.count * part / parts), j1 = (int)((int64_t)x.count * (part + 1) / parts);
 
@@ -281,55 +316,140 @@ __global__ void __launch_bounds__(kLpThreads, 6) logprob_kernel(LogprobArgs a) {
   }
   if (lane == 0) sh.warp[tid >> 5] = st;
   __syncthreads();
-  if (tid == 0) {
+  if (TOP) block_top(sh, x, j0, j1, a.top_k, mine);
+  if (parts > 1) {
+    cluster_wait();                               // all blocks have begun
+    if (tid == 0) {
+      st = sh.warp[0];
+      for (int w = 1; w < kLpWarps; ++w) st = join(st, sh.warp[w]);
+      *cluster.map_shared_rank(&sh.block[part], 0) = st;
+    }
+    if (TOP && tid < a.top_k) {
+      cluster.map_shared_rank(sh.all_v, 0)[part * a.top_k + tid] = sh.top_v[tid];
+      cluster.map_shared_rank(sh.all_id, 0)[part * a.top_k + tid] = sh.top_id[tid];
+    }
+    cluster_arrive();
+    cluster_wait();
+    if (part != 0) return;
+    st = sh.block[0];
+    for (int c = 1; c < parts; ++c) st = join(st, sh.block[c]);
+  } else {
     st = sh.warp[0];
     for (int w = 1; w < kLpWarps; ++w) st = join(st, sh.warp[w]);
-    sh.block = st;
   }
-  if (TOP) block_top(sh, x, j0, j1, a.top_k, mine);
-  if (parts > 1) cluster.sync(); else __syncthreads();
-  if (part == 0) {
-    st = sh.block;
-    for (int c = 1; c < parts; ++c) st = join(st, *cluster.map_shared_rank(&sh.block, c));
-    const bool none = !(st.m < INFINITY);         // a NaN or +infinity in the row: no distribution
-    const bool empty = st.m == -INFINITY;         // nothing but -infinity
-    const float log_s = logf(st.s);
-    if (tid == 0) {
-      if (a.lse) a.lse[row] = none ? NAN : empty ? -INFINITY : st.m + log_s;
-      if (a.entropy) a.entropy[row] = none ? NAN : empty ? 0.f : log_s - st.t / st.s;
-      if (a.targets) {
-        const int y = a.targets[row];
-        float lp = 0.f;
-        if (y >= a.vocab) lp = NAN;
-        else if (y >= 0) lp = none ? NAN : empty ? -INFINITY : (to_f<T>(x.row[y]) - st.m) - log_s;
-        a.logprob[row] = lp;
-      }
-    }
-    if (TOP) {
-      const int k = a.top_k, n = parts * k;
-      const float* bv = sh.top_v;
-      const int* bid = sh.top_id;
+  const RowResult r(st);
+  if (tid == 0) r.write<T>(a, x, row);
+  if (TOP) {
+    const int k = a.top_k, n = parts * k;
+    const float* bv = parts > 1 ? sh.all_v : sh.top_v;
+    const int* bid = parts > 1 ? sh.all_id : sh.top_id;
+    for (int i = tid; i < n; i += kLpThreads) {
+      int rank = i;
       if (parts > 1) {
-        for (int i = tid; i < n; i += kLpThreads) {
-          sh.all_v[i] = cluster.map_shared_rank(sh.top_v, i / k)[i % k];
-          sh.all_id[i] = cluster.map_shared_rank(sh.top_id, i / k)[i % k];
-        }
-        __syncthreads();
-        bv = sh.all_v; bid = sh.all_id;
-      }
-      for (int i = tid; i < n; i += kLpThreads) {
-        int rank = 0;
         // entries of blocks with fewer than k elements are equal among themselves and come behind every element
+        rank = 0;
         for (int b = 0; b < n; ++b) rank += beats(bv[b], bid[b], bv[i], bid[i]);
-        if (!none && rank < k && bid[i] < a.vocab) {
-          a.top_logprob[row * k + rank] = empty ? -INFINITY : (bv[i] - st.m) - log_s;
-          a.top_ids[row * k + rank] = bid[i];
+      }
+      if (rank < k && bid[i] < a.vocab) r.write_top(a, row, rank, bv[i], bid[i]);
+    }
+    if (r.none && tid < k) r.write_top(a, row, tid, 0.f, 0);
+  }
+}
+
+// Short rows: a warp to each, nothing shared between warps.
+constexpr int kLpShort = 2048;                    // elements
+constexpr int kLpShortList = 160;
+
+struct LpWarpShared {
+  float v[kLpShortList];
+  int id[kLpShortList];
+};
+
+template <typename T, bool TOP, bool ENTROPY>
+__global__ void __launch_bounds__(kLpThreads) logprob_short_kernel(LogprobArgs a) {
+  __shared__ LpWarpShared shared[TOP ? kLpWarps : 1];
+  constexpr int U = 4, N = Vec<T>::n;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t row = (int64_t)blockIdx.x * kLpWarps + warp;
+  if (row >= a.rows) return;
+  const RowVectors<T> x(static_cast<const T*>(a.logits) + row * a.row_stride, a.vocab);
+  Sums st{-INFINITY, 0.f, 0.f};
+  const uint32_t none2 = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;   // -infinity, or two of them
+  for (int j = lane; j < x.count; j += U * 32) {
+    uint4 q[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = j + u * 32;
+      q[u] = at < x.count && x.whole(at) ? x.load(at) : make_uint4(none2, none2, none2, none2);
+    }
+    take<T, ENTROPY>(st, q);
+  }
+  for (int e = 0; e < 2; ++e) {                   // the vectors that reach over the row's ends
+    const int j = e ? x.count - 1 : 0;
+    if (j % 32 != lane || x.whole(j) || (e && x.count == 1)) continue;
+    float v[N];
+    x.get(j, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) st = join(st, Sums{v[i], v[i] == -INFINITY ? 0.f : 1.f, 0.f});
+  }
+  const float mine = st.m;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const Sums b{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), __shfl_xor_sync(0xffffffffu, st.t, o)};
+    st = lane & o ? join(b, st) : join(st, b);
+  }
+  const RowResult r(st);
+  if (lane == 0) r.write<T>(a, x, row);
+  if constexpr (TOP) {
+    const int k = a.top_k;
+    if (r.none) {
+      if (lane < k) r.write_top(a, row, lane, 0.f, 0);
+      return;
+    }
+    LpWarpShared& sh = shared[warp];
+    const float th = __shfl_sync(0xffffffffu, sorted_down(mine), k - 1);
+    unsigned hit = __ballot_sync(0xffffffffu, mine >= th);
+    int n = 0;
+    while (hit) {                                 // the vectors of each lane that reaches the threshold, by the whole warp
+      const int who = __ffs(hit) - 1;
+      hit &= hit - 1;
+      for (int j = who; j < x.count; j += 32 * 32) {
+        float v[N];
+        const int at = j + lane * 32;
+        if (at < x.count) x.get(at, v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int id = x.first(at) + i;
+          const bool in = at < x.count && id >= 0 && id < x.vocab && v[i] >= th;
+          const unsigned all = __ballot_sync(0xffffffffu, in);
+          const int to = n + __popc(all & ((1u << lane) - 1));
+          if (in && to < kLpShortList) { sh.v[to] = v[i]; sh.id[to] = id; }
+          n += __popc(all);
         }
       }
-      if (none && tid < k) { a.top_logprob[row * k + tid] = NAN; a.top_ids[row * k + tid] = -1; }
+    }
+    __syncwarp();
+    if (n <= kLpShortList) {
+      for (int i = lane; i < n; i += 32) {
+        const float v = sh.v[i];
+        const int id = sh.id[i];
+        int rank = 0;
+        for (int b = 0; b < n; ++b) rank += beats(sh.v[b], sh.id[b], v, id);
+        if (rank < k) r.write_top(a, row, rank, v, id);
+      }
+      return;
+    }
+    float last_v = INFINITY;
+    int last_id = -1;
+    for (int rank = 0; rank < k; ++rank) {        // the best of what comes after the last one found
+      float bv = -INFINITY;
+      int bid = x.vocab;
+      for (int j = lane; j < x.count; j += 32) best_after(x, j, last_v, last_id, bv, bid);
+      warp_best(bv, bid);
+      if (lane == 0) r.write_top(a, row, rank, bv, bid);
+      last_v = bv; last_id = bid;
     }
   }
-  if (parts > 1) cluster.sync();                  // the first block has read the others' shared memory
 }
 
 struct LogprobBwdArgs {
@@ -433,6 +553,11 @@ __global__ void __launch_bounds__(kLpThreads) logprob_bwd_kernel(LogprobBwdArgs 
 }
 
 template <typename T> static cudaError_t logprob_launch(const LogprobArgs& a, int parts, cudaStream_t st) {
+  if (a.vocab <= kLpShort) {
+    void (*kernel)(LogprobArgs) = a.top_k ? (a.entropy ? logprob_short_kernel<T, true, true> : logprob_short_kernel<T, true, false>)
+                                          : (a.entropy ? logprob_short_kernel<T, false, true> : logprob_short_kernel<T, false, false>);
+    return launch_pdl(kernel, dim3((unsigned)((a.rows + kLpWarps - 1) / kLpWarps)), dim3(kLpThreads), 0, st, false, a);
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(a.rows * parts)); cfg.blockDim = dim3(kLpThreads); cfg.stream = st;
   cudaLaunchAttribute at[1];
