@@ -534,13 +534,7 @@ __global__ void __launch_bounds__(BwdShape<DT>::kThreads, BwdShape<DT>::kBlocks)
 attn_packed_dkv_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcBwdMaps maps) {
   using S = BwdShape<DT>;
   constexpr int BN = S::kCols, kCopy = S::kParts * 4, kIssue = kCopy + 1;        // the warps that copy and issue
-  const int hk = blockIdx.x % a.kv_heads;
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.kv_heads, TC_LOG_ROWS);
-  if (s.tile < 0) { pdl_wait(); pdl_trigger(); return; }
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int k0 = s.tile * TC_ROWS, first = a.causal ? k0 : 0;
-  const int per_head = (s.len - first + BN - 1) / BN, n_it = per_head * a.group;
-
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = blockIdx.x % a.kv_heads;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const sptr = smem_raw + (base - raw);
@@ -556,45 +550,67 @@ attn_packed_dkv_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* const status = &g_attn_packed_status;
 
-  if (threadIdx.x == 0) {
+  // barriers, tensor memory and the tile's place at the same time; the first copies go out as soon as the copying warp knows its tile
+  if (warp == kCopy && lane == 0) {
     mbar_init(kv_full, 1);
     for (int i = 0; i < S::kStages; ++i) { mbar_init(full(i), 1); mbar_init(row_full(i), 32); mbar_init(empty(i), 1); }
     mbar_init(s_full, 1); mbar_init(dp_full, 1); mbar_init(p_full, S::kParts * 4); mbar_init(ds_full, S::kParts * 4); mbar_init(acc_full, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    tma_prefetch_desc(&maps.k); tma_prefetch_desc(&maps.v); tma_prefetch_desc(&maps.q); tma_prefetch_desc(&maps.d_o);
   }
   if (warp == kIssue) {
     tmem_alloc(smem_u32(tmem_slot), S::kTmem);
     tmem_relinquish();
   }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  pdl_wait();                                     // delta
-  pdl_trigger();
-  const uint32_t tmem = *tmem_slot, col_s = tmem, col_dp = tmem + BN, col_dv = tmem + 2 * BN, col_dk = tmem + 2 * BN + DT;
-
-  if (warp == kCopy) {                            // ---- copies
-    int armed = 0, h = hk * a.group, q0 = first;
-    bool ok = true;
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.kv_heads, TC_LOG_ROWS);
+  if (s.tile < 0) {
+    __syncthreads();
+    if (warp == kIssue) tmem_dealloc(*tmem_slot, S::kTmem);
+    pdl_wait();
+    pdl_trigger();
+    return;
+  }
+  const int k0 = s.tile * TC_ROWS, first = a.causal ? k0 : 0;
+  const int per_head = (s.len - first + BN - 1) / BN, n_it = per_head * a.group;
+  auto copy_queries = [&](int it, int h, int q0) {
+    const int st = it % S::kStages;
+    if (elect_one()) {
+      mbar_arrive_expect_tx(full(st), 2 * S::kStream);
+      copy_rows<DT, BN>(sQ + st * S::kStream, &maps.q, full(st), h, s.begin + q0);
+      copy_rows<DT, BN>(sO + st * S::kStream, &maps.d_o, full(st), h, s.begin + q0);
+    }
+    __syncwarp();
+  };
+  if (warp == kCopy) {
+    __syncwarp();
     if (elect_one()) {
       mbar_arrive_expect_tx(kv_full, 2 * S::kTile);
       copy_rows<DT, TC_ROWS>(sK, &maps.k, kv_full, hk, s.begin + k0);
       copy_rows<DT, TC_ROWS>(sV, &maps.v, kv_full, hk, s.begin + k0);
     }
     __syncwarp();
+    copy_queries(0, hk * a.group, first);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot, col_s = tmem, col_dp = tmem + BN, col_dv = tmem + 2 * BN, col_dk = tmem + 2 * BN + DT;
+
+  if (warp == kCopy) {                            // ---- copies
+    int armed = 1, h = hk * a.group, q0 = first;
+    bool ok = true;
+    pdl_wait();                                   // delta
+    pdl_trigger();
     for (int it = 0; it < n_it; ++it) {
       const int st = it % S::kStages;
       if (it >= S::kStages) ok = wait_for(empty(st), (it / S::kStages - 1) & 1, abort_flag, status, 51);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      if (elect_one()) {
-        mbar_arrive_expect_tx(full(st), 2 * S::kStream);
-        copy_rows<DT, BN>(sQ + st * S::kStream, &maps.q, full(st), h, s.begin + q0);
-        copy_rows<DT, BN>(sO + st * S::kStream, &maps.d_o, full(st), h, s.begin + q0);
+      if (it > 0) {
+        copy_queries(it, h, q0);
+        ++armed;
       }
-      __syncwarp();
-      ++armed;
       float* rows = row_values + st * 2 * BN;
 #pragma unroll
       for (int i = 0; i < BN; i += 32) {
@@ -746,13 +762,7 @@ __global__ void __launch_bounds__(BwdShape<DT>::kThreads, BwdShape<DT>::kBlocks)
 attn_packed_dq_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcBwdMaps maps) {
   using S = BwdShape<DT>;
   constexpr int BN = S::kCols, kCopy = S::kParts * 4, kIssue = kCopy + 1;
-  const int h = blockIdx.x % a.heads, hk = h / a.group;
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.heads, TC_LOG_ROWS);
-  if (s.tile < 0) { pdl_wait(); return; }
-  const int tile = (s.len + TC_ROWS - 1) / TC_ROWS - 1 - s.tile;                 // the tiles that see the most keys first
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int q0 = tile * TC_ROWS, n_it = ((a.causal ? min(s.len, q0 + TC_ROWS) : s.len) + BN - 1) / BN;
-
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.x % a.heads, hk = h / a.group;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const sptr = smem_raw + (base - raw);
@@ -766,16 +776,45 @@ attn_packed_dq_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_cons
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* const status = &g_attn_packed_status;
 
-  if (threadIdx.x == 0) {
+  if (warp == kCopy && lane == 0) {
     mbar_init(q_full, 1);
     for (int i = 0; i < S::kStages; ++i) { mbar_init(full(i), 1); mbar_init(cleared(i), 32); mbar_init(empty(i), 1); }
     mbar_init(s_full, 1); mbar_init(s_full + 8, 1); mbar_init(dp_full, 1); mbar_init(ds_full, S::kParts * 4); mbar_init(acc_full, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    tma_prefetch_desc(&maps.q); tma_prefetch_desc(&maps.d_o); tma_prefetch_desc(&maps.k); tma_prefetch_desc(&maps.v);
   }
   if (warp == kIssue) {
     tmem_alloc(smem_u32(tmem_slot), S::kTmem);
     tmem_relinquish();
+  }
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.heads, TC_LOG_ROWS);
+  if (s.tile < 0) {
+    __syncthreads();
+    if (warp == kIssue) tmem_dealloc(*tmem_slot, S::kTmem);
+    pdl_wait();
+    return;
+  }
+  const int tile = (s.len + TC_ROWS - 1) / TC_ROWS - 1 - s.tile;                 // the tiles that see the most keys first
+  const int q0 = tile * TC_ROWS, n_it = ((a.causal ? min(s.len, q0 + TC_ROWS) : s.len) + BN - 1) / BN;
+  auto copy_keys = [&](int it) {
+    const int st = it % S::kStages;
+    if (elect_one()) {
+      mbar_arrive_expect_tx(full(st), 2 * S::kStream);
+      copy_rows<DT, BN>(sK + st * S::kStream, &maps.k, full(st), hk, s.begin + it * BN);
+      copy_rows<DT, BN>(sV + st * S::kStream, &maps.v, full(st), hk, s.begin + it * BN);
+    }
+    __syncwarp();
+  };
+  if (warp == kCopy) {
+    __syncwarp();
+    if (elect_one()) {
+      mbar_arrive_expect_tx(q_full, 2 * S::kTile);
+      copy_rows<DT, TC_ROWS>(sQ, &maps.q, q_full, h, s.begin + q0);
+      copy_rows<DT, TC_ROWS>(sO, &maps.d_o, q_full, h, s.begin + q0);
+    }
+    __syncwarp();
+    copy_keys(0);
   }
   tc_fence_before();
   __syncthreads();
@@ -783,26 +822,17 @@ attn_packed_dq_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_cons
   const uint32_t tmem = *tmem_slot, col_s = tmem, col_dp = tmem + 2 * BN, col_dq = tmem + 3 * BN;
 
   if (warp == kCopy) {                            // ---- copies
-    int armed = 0;
+    int armed = 1;
     bool ok = true;
-    if (elect_one()) {
-      mbar_arrive_expect_tx(q_full, 2 * S::kTile);
-      copy_rows<DT, TC_ROWS>(sQ, &maps.q, q_full, h, s.begin + q0);
-      copy_rows<DT, TC_ROWS>(sO, &maps.d_o, q_full, h, s.begin + q0);
-    }
-    __syncwarp();
     for (int it = 0; it < n_it; ++it) {
       const int st = it % S::kStages, k0 = it * BN;
       if (it >= S::kStages) ok = wait_for(empty(st), (it / S::kStages - 1) & 1, abort_flag, status, 71);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      if (elect_one()) {
-        mbar_arrive_expect_tx(full(st), 2 * S::kStream);
-        copy_rows<DT, BN>(sK + st * S::kStream, &maps.k, full(st), hk, s.begin + k0);
-        copy_rows<DT, BN>(sV + st * S::kStream, &maps.v, full(st), hk, s.begin + k0);
+      if (it > 0) {
+        copy_keys(it);
+        ++armed;
       }
-      __syncwarp();
-      ++armed;
       if (k0 + BN > s.len) {                      // keys of other sequences, or of none: zeros, where dS is zero
         ok = wait_for(full(st), (it / S::kStages) & 1, abort_flag, status, 72);
         ok = __all_sync(0xffffffffu, ok);
@@ -914,25 +944,42 @@ attn_packed_dq_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_cons
   pdl_wait();
 }
 
-// delta_i = do_i . o_i: eight lanes a row; rows outside the sequences get a value that nothing reads
+// delta_i = do_i . o_i: eight lanes a row, two rows to each lane with all loads in flight; blockIdx.y is the head.  Rows outside the
+// sequences get a value that nothing reads.
+constexpr int DELTA_R = 2;
 __global__ void __launch_bounds__(256) attn_packed_delta_tc_kernel(const __grid_constant__ PackedArgs a) {
-  const int64_t i = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3);
-  const int part = threadIdx.x & 7;
-  const bool in = i < a.tokens * a.heads;
-  const int64_t token = in ? i / a.heads : 0;
-  const int h = in ? (int)(i - token * a.heads) : 0;
-  const __nv_bfloat16 *x = head_row<__nv_bfloat16>(a.o, token, h), *y = head_row<__nv_bfloat16>(a.d_o, token, h);
-  float sum = 0.f;
-  for (int c = part * 8; c < a.dim; c += 64) {
-    float u[8], w[8];
-    load8(x + c, u);
-    load8(y + c, w);
+  constexpr int R = DELTA_R;
+  pdl_trigger();
+  const int part = threadIdx.x & 7, h = blockIdx.y;
+  const int64_t first = (int64_t)blockIdx.x * 32 * R + (threadIdx.x >> 3);
+  uint4 x[R][2], y[R][2];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum = fmaf(u[e], w[e], sum);
+  for (int r = 0; r < R; ++r) {
+    const int64_t token = min(first + r * 32, a.tokens - 1);
+    const __nv_bfloat16 *o = head_row<__nv_bfloat16>(a.o, token, h), *g = head_row<__nv_bfloat16>(a.d_o, token, h);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int col = part * 8 + c * 64;
+      x[r][c] = col < a.dim ? *reinterpret_cast<const uint4*>(o + col) : make_uint4(0u, 0u, 0u, 0u);
+      y[r][c] = col < a.dim ? *reinterpret_cast<const uint4*>(g + col) : make_uint4(0u, 0u, 0u, 0u);
+    }
   }
 #pragma unroll
-  for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  if (in && part == 0) a.delta[(int64_t)h * a.tokens + token] = sum;
+  for (int r = 0; r < R; ++r) {
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const uint32_t u[4] = {x[r][c].x, x[r][c].y, x[r][c].z, x[r][c].w}, w[4] = {y[r][c].x, y[r][c].y, y[r][c].z, y[r][c].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        sum = fmaf(__uint_as_float(u[e] << 16), __uint_as_float(w[e] << 16), sum);
+        sum = fmaf(__uint_as_float(u[e] & 0xFFFF0000u), __uint_as_float(w[e] & 0xFFFF0000u), sum);
+      }
+    }
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (part == 0 && first + r * 32 < a.tokens) a.delta[(int64_t)h * a.tokens + first + r * 32] = sum;
+  }
 }
 
 // ---- host side --------------------------------------------------------------------------------------------------
@@ -1024,7 +1071,7 @@ template <int DT> static cudaError_t bwd_launch(const PackedArgs& a, cudaStream_
   if (e != cudaSuccess) return e;
   const int64_t tiles = most_tiles(a.tokens, a.n_seqs, TC_ROWS);
   if (tiles * a.heads > 0x7fffffff) return cudaErrorInvalidConfiguration;
-  e = launch_pdl(attn_packed_delta_tc_kernel, dim3((unsigned)((a.tokens * a.heads + 31) / 32)), dim3(256), 0, st, false, a);
+  e = launch_pdl(attn_packed_delta_tc_kernel, dim3((unsigned)((a.tokens + 32 * DELTA_R - 1) / (32 * DELTA_R)), a.heads), dim3(256), 0, st, false, a);
   // The second kernel starts once every block of the first has passed its wait for delta, so its blocks fill the SMs that the first's last
   // and longest blocks leave; it ends behind the first.
   if (e == cudaSuccess) e = launch_pdl(attn_packed_dkv_tc_kernel<DT>, dim3((unsigned)(tiles * a.kv_heads)), dim3(S::kThreads), S::kSmem, st, true, a, maps);

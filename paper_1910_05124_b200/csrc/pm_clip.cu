@@ -18,7 +18,9 @@ namespace pm {
 
 constexpr int kClipThreads = 256;
 constexpr int kChunk = 8192;                      // elements: four (bf16) or eight (fp32) 16-byte loads per thread
-constexpr int kClipBlocks = 4 * kSms;             // four blocks of 256 threads per SM
+// Blocks of 256 threads per SM: the norm keeps eight 16-byte loads a thread in flight and takes the registers of four blocks, the second
+// pass runs with six (185 M bf16 gradients into fp32: 186 us, with four 189).
+constexpr int kNormBlocks = 4 * kSms, kScaleBlocks = 6 * kSms;
 constexpr int kClipCap = 1000;                    // tensors per launch: the parameter space holds 32764 bytes
 
 enum { CF_SRC_BF16 = 1, CF_DST_BF16 = 2, CF_SRC_VEC = 4, CF_DST_VEC = 8, CF_IN_PLACE = 16 };
@@ -45,19 +47,40 @@ template <int CAP> __device__ __forceinline__ uint32_t clip_find(const ClipTable
   return lo;
 }
 
-// Sum of squares of four values.  Squares leave the range of fp32 at 2^64 and lose bits below 2^-63, so four values whose
-// largest lies outside 2^-50 .. 2^60 are squared in 64 bits; among the others what underflows is below 2^-26 of the sum.
+// Sum of squares of eight values.  Squares leave the range of fp32 at 2^64 and lose bits below 2^-63, so eight values whose
+// largest lies outside 2^-50 .. 2^60 are squared in 64 bits; among the others what underflows is below 2^-25 of the sum.
 // (A NaN passes the test with its neighbours or not; either way it reaches the sum.)
-__device__ __forceinline__ double square4(float a, float b, float c, float d) {
-  const float m = fmaxf(fmaxf(fabsf(a), fabsf(b)), fmaxf(fabsf(c), fabsf(d)));
-  if ((m >= 8.8817842e-16f && m <= 1.1529215e18f) || m == 0.f) return (double)((a * a + b * b) + (c * c + d * d));
-  return ((double)a * a + (double)b * b) + ((double)c * c + (double)d * d);
+__device__ __forceinline__ double square8(const float (&v)[8]) {
+  float m = fabsf(v[0]);
+#pragma unroll
+  for (int i = 1; i < 8; ++i) m = fmaxf(m, fabsf(v[i]));
+  if ((m >= 8.8817842e-16f && m <= 1.1529215e18f) || m == 0.f)
+    return (double)(((v[0] * v[0] + v[1] * v[1]) + (v[2] * v[2] + v[3] * v[3])) + ((v[4] * v[4] + v[5] * v[5]) + (v[6] * v[6] + v[7] * v[7])));
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sum += (double)v[i] * v[i];
+  return sum;
 }
 
 __device__ __forceinline__ void unpack8(const uint4& q, float (&v)[8]) {
   const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+}
+
+// the thread's part of the squares of N 16-byte vectors per thread
+template <int N> __device__ __forceinline__ double square_chunk(const __nv_bfloat16* p) {
+  uint4 q[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) q[i] = reinterpret_cast<const uint4*>(p)[i * kClipThreads + threadIdx.x];
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float v[8];
+    unpack8(q[i], v);
+    sum += square8(v);
+  }
+  return sum;
 }
 
 // block-wide sum in a fixed order; valid in thread 0
@@ -87,17 +110,11 @@ __global__ void __launch_bounds__(kClipThreads, 4) clip_norm_kernel(const __grid
       const uint32_t flags = t.e[e].flags;
       if (flags & CF_SRC_BF16) {
         const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(t.e[e].src) + begin;
-        if (n == kChunk && (flags & CF_SRC_VEC)) {
-          uint4 q[kChunk / 8 / kClipThreads];
-#pragma unroll
-          for (int i = 0; i < kChunk / 8 / kClipThreads; ++i) q[i] = reinterpret_cast<const uint4*>(p)[i * kClipThreads + threadIdx.x];
-#pragma unroll
-          for (int i = 0; i < kChunk / 8 / kClipThreads; ++i) {
-            float v[8];
-            unpack8(q[i], v);
-            acc += square4(v[0], v[1], v[2], v[3]);
-            acc += square4(v[4], v[5], v[6], v[7]);
-          }
+        if (c + 1 < c1 && begin + 2 * kChunk <= t.e[e].count && (flags & CF_SRC_VEC)) {
+          acc += square_chunk<kChunk / 4 / kClipThreads>(p);           // two chunks: as many loads in flight as for one of fp32
+          ++c;
+        } else if (n == kChunk && (flags & CF_SRC_VEC)) {
+          acc += square_chunk<kChunk / 8 / kClipThreads>(p);
         } else {
           for (int i = threadIdx.x; i < n; i += kClipThreads) { const double x = __bfloat162float(p[i]); acc += x * x; }
         }
@@ -108,7 +125,8 @@ __global__ void __launch_bounds__(kClipThreads, 4) clip_norm_kernel(const __grid
 #pragma unroll
           for (int i = 0; i < kChunk / 4 / kClipThreads; ++i) q[i] = reinterpret_cast<const float4*>(p)[i * kClipThreads + threadIdx.x];
 #pragma unroll
-          for (int i = 0; i < kChunk / 4 / kClipThreads; ++i) acc += square4(q[i].x, q[i].y, q[i].z, q[i].w);
+          for (int i = 0; i < kChunk / 4 / kClipThreads; i += 2)
+            acc += square8({q[i].x, q[i].y, q[i].z, q[i].w, q[i + 1].x, q[i + 1].y, q[i + 1].z, q[i + 1].w});
         } else {
           for (int i = threadIdx.x; i < n; i += kClipThreads) { const double x = p[i]; acc += x * x; }
         }
@@ -156,7 +174,7 @@ __device__ __forceinline__ void clip_chunk(const S* src, D* dst, int n, bool vec
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(kClipThreads, 4) clip_scale_kernel(const __grid_constant__ ClipTable<CAP> t, const double* partials, int n_partials,
+__global__ void __launch_bounds__(kClipThreads, 6) clip_scale_kernel(const __grid_constant__ ClipTable<CAP> t, const double* partials, int n_partials,
                                                                     double max_norm, float* norm_out, float* scale_out) {
   __shared__ double scratch[kClipThreads / 32];
   __shared__ float s_scale;
@@ -217,26 +235,38 @@ template <int CAP> static int clip_fill(ClipTable<CAP>& t, const pm_tensor_pair*
   return m;
 }
 
+struct ClipCall {
+  double* partials;
+  int n_partials;                                 // of all launches
+  double max_norm;
+  float *norm, *scale;
+  cudaStream_t stream;
+};
+enum { CLIP_NORM = 1, CLIP_SCALE = 2 };           // passes: both where one launch holds all tensors
 template <int CAP>
-static cudaError_t clip_launch(const pm_tensor_pair* tensors, int n, bool scale_pass, double* partials, int n_partials, int blocks, double max_norm,
-                               float* norm, float* scale, cudaStream_t st, bool pdl) {
+static cudaError_t clip_launch(const pm_tensor_pair* tensors, int n, int passes, int first_partial, const ClipCall& c, bool writes) {
   ClipTable<CAP> t;
   clip_fill(t, tensors, n);
-  if (!scale_pass) return launch_pdl(clip_norm_kernel<CAP>, dim3(blocks), dim3(kClipThreads), 0, st, pdl, t, partials);
-  return launch_pdl(clip_scale_kernel<CAP>, dim3(blocks), dim3(kClipThreads), 0, st, pdl, t, partials, n_partials, max_norm, norm, scale);
+  auto blocks = [&](int most) { return t.chunks < 1 ? 1 : t.chunks < (uint32_t)most ? (int)t.chunks : most; };
+  cudaError_t e = cudaSuccess;
+  if (passes & CLIP_NORM) e = launch_pdl(clip_norm_kernel<CAP>, dim3(blocks(kNormBlocks)), dim3(kClipThreads), 0, c.stream, false, t, c.partials + first_partial);
+  if (e == cudaSuccess && (passes & CLIP_SCALE))
+    e = launch_pdl(clip_scale_kernel<CAP>, dim3(blocks(kScaleBlocks)), dim3(kClipThreads), 0, c.stream, writes, t, c.partials, c.n_partials, c.max_norm,
+                   writes ? c.norm : nullptr, writes ? c.scale : nullptr);
+  return e;
 }
 
-static cudaError_t clip_dispatch(const pm_tensor_pair* tensors, int n, bool scale_pass, double* partials, int n_partials, int blocks, double max_norm,
-                                 float* norm, float* scale, cudaStream_t st, bool pdl) {
-  if (n <= 32) return clip_launch<32>(tensors, n, scale_pass, partials, n_partials, blocks, max_norm, norm, scale, st, pdl);
-  if (n <= 256) return clip_launch<256>(tensors, n, scale_pass, partials, n_partials, blocks, max_norm, norm, scale, st, pdl);
-  return clip_launch<kClipCap>(tensors, n, scale_pass, partials, n_partials, blocks, max_norm, norm, scale, st, pdl);
+static cudaError_t clip_dispatch(const pm_tensor_pair* tensors, int n, int passes, int first_partial, const ClipCall& c, bool writes) {
+  if (n <= 64) return clip_launch<64>(tensors, n, passes, first_partial, c, writes);
+  if (n <= 256) return clip_launch<256>(tensors, n, passes, first_partial, c, writes);
+  return clip_launch<kClipCap>(tensors, n, passes, first_partial, c, writes);
 }
 
-static int clip_blocks(const pm_tensor_pair* tensors, int n) {
+// blocks of the first pass over these tensors
+static int clip_partials(const pm_tensor_pair* tensors, int n) {
   uint64_t chunks = 0;
   for (int i = 0; i < n; ++i) chunks += (tensors[i].count + kChunk - 1) / kChunk;
-  return (int)(chunks < 1 ? 1 : chunks < (uint64_t)kClipBlocks ? chunks : (uint64_t)kClipBlocks);
+  return (int)(chunks < 1 ? 1 : chunks < (uint64_t)kNormBlocks ? chunks : (uint64_t)kNormBlocks);
 }
 
 }  // namespace pm
@@ -247,7 +277,7 @@ extern "C" {
 
 uint64_t pm_clip_gradients_workspace_bytes(int32_t n_tensors) {
   if (n_tensors < 1) return 0;
-  return (uint64_t)((n_tensors + kClipCap - 1) / kClipCap) * kClipBlocks * sizeof(double);
+  return (uint64_t)((n_tensors + kClipCap - 1) / kClipCap) * kNormBlocks * sizeof(double);
 }
 
 pm_status pm_clip_gradients(const pm_tensor_pair* tensors, int32_t n_tensors, double max_norm, float* norm, float* scale, void* workspace,
@@ -270,20 +300,20 @@ pm_status pm_clip_gradients(const pm_tensor_pair* tensors, int32_t n_tensors, do
   const uint64_t need = pm_clip_gradients_workspace_bytes(n_tensors);
   if (!workspace || workspace_bytes < need) return ops_fail(PM_ERR_NOMEM, "workspace too small: need %llu bytes", (unsigned long long)need);
   if (!aligned_to(workspace, 8)) return ops_fail(PM_ERR_INVALID_ARG, "workspace must be 8-byte aligned");
-  const cudaStream_t st = (cudaStream_t)stream;
-  double* partials = static_cast<double*>(workspace);
-  int n_partials = 0;
+  ClipCall c{static_cast<double*>(workspace), 0, max_norm, norm, scale, (cudaStream_t)stream};
+  if (n_tensors <= kClipCap) {
+    c.n_partials = clip_partials(tensors, n_tensors);
+    return ops_cuda(clip_dispatch(tensors, n_tensors, CLIP_NORM | CLIP_SCALE, 0, c, true), "gradient clipping");
+  }
+  // several launches a pass: the first of the second pass writes norm and scale
   for (int at = 0; at < n_tensors; at += kClipCap) {
-    const int n = n_tensors - at < kClipCap ? n_tensors - at : kClipCap, blocks = clip_blocks(tensors + at, n);
-    const cudaError_t e = clip_dispatch(tensors + at, n, false, partials + n_partials, 0, blocks, max_norm, nullptr, nullptr, st, false);
-    if (e != cudaSuccess) return ops_cuda(e, "gradient norm");
-    n_partials += blocks;
+    const int n = n_tensors - at < kClipCap ? n_tensors - at : kClipCap;
+    if (const pm_status s = ops_cuda(clip_dispatch(tensors + at, n, CLIP_NORM, c.n_partials, c, false), "gradient norm")) return s;
+    c.n_partials += clip_partials(tensors + at, n);
   }
   for (int at = 0; at < n_tensors; at += kClipCap) {
     const int n = n_tensors - at < kClipCap ? n_tensors - at : kClipCap;
-    const cudaError_t e = clip_dispatch(tensors + at, n, true, partials, n_partials, clip_blocks(tensors + at, n), max_norm, at ? nullptr : norm,
-                                        at ? nullptr : scale, st, at == 0);
-    if (e != cudaSuccess) return ops_cuda(e, "gradient clipping");
+    if (const pm_status s = ops_cuda(clip_dispatch(tensors + at, n, CLIP_SCALE, 0, c, at == 0), "gradient clipping")) return s;
   }
   return PM_OK;
 }

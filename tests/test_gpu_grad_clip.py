@@ -22,7 +22,7 @@ def check(grads, max_norm, outs=None):
     want_norm, want_scale = R.clip(grads, max_norm)
     before = [g.clone() for g in grads]
     norm, scale = run(grads, max_norm, outs)
-    # four squares are added in fp32 (four roundings), the rest in 64 bits; the root halves that; one rounding of the result
+    # eight squares are added in fp32 (four roundings each), the rest in 64 bits; the root halves that; one rounding of the result
     assert abs(norm - want_norm) <= 4 * R.U32 * want_norm, (norm, want_norm)
     assert abs(scale - want_scale) <= 5 * R.U32 * want_scale
     for g, o in zip(before, grads if outs is None else outs):
