@@ -97,6 +97,33 @@ __device__ __forceinline__ float2 fma_f32x2(float2 a, float2 b, float2 c) {
   return r;
 }
 
+// A warp's 32 rows of an accumulator, 32 columns from c0 on, times f, to bf16 rows in memory.  Each lane has a row; through 2 KB of
+// shared memory four lanes come to write 64 bytes of a row, a quarter of the transactions that a lane to a row would make.
+// `rows`: how many of the warp's rows are the sequence's, from the first one on.  NaN where a wait ran out (ok is false).
+__device__ __forceinline__ void store_rows(__nv_bfloat16* out, int64_t stride, int rows, uint32_t taddr, int c0, int dim, float f, bool ok, uint8_t* stage) {
+  const int lane = threadIdx.x & 31;
+  uint32_t o[32];
+  tmem_ld32(taddr + c0, o);
+  tmem_ld_wait();
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(o[g * 8 + i]) * f;
+    *reinterpret_cast<uint4*>(stage + lane * 64 + ((g ^ (lane >> 1 & 3)) << 4)) =
+        make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+  }
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = i * 8 + (lane >> 2), g = lane & 3;
+    uint4 w = *reinterpret_cast<const uint4*>(stage + r * 64 + ((g ^ (r >> 1 & 3)) << 4));
+    if (!ok) w = make_uint4(0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u);
+    if (r < rows && c0 + g * 8 < dim) *reinterpret_cast<uint4*>(out + r * stride + c0 + g * 8) = w;
+  }
+  __syncwarp();
+}
+
 // 2^x for two values on the FMA units: x = n + f with n the nearest integer, 2^f by the polynomial of degree 4 with the least relative
 // error on [-1/2, 1/2] (2.6e-6, a 700th of bf16's half step; found by iteratively reweighted least squares), n added to the exponent.
 // x is at most 8 here; below -126 the result is 2^-126 where the exponential unit gives zero.
@@ -417,26 +444,14 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
       if (ok) ok = wait_for(o_full(t), S::kApart ? (n - 1) & 1 : 0, abort_flag, status, 41);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
-      const float inv = ok ? 1.f / l : NAN;
+      const float inv = 1.f / l;
       const int h = head_of(t);
       if (a.lse && row < s.len) a.lse[(int64_t)h * a.tokens + s.begin + row] = ok ? (m + log2f(l)) * kLn2 : NAN;
-      __nv_bfloat16* out = head_row_out<__nv_bfloat16>(a.o, s.begin + row, h);
+      const int first_row = q0 + (warp & 3) * 32;
 #pragma unroll
-      for (int q = 0; q < DT / 32; ++q) {
-        uint32_t o[32];
-        tmem_ld32(to + q * 32, o);
-        tmem_ld_wait();
-        if (row < s.len)
-#pragma unroll
-          for (int g = 0; g < 4; ++g)
-            if (q * 32 + g * 8 < a.dim) {
-              float f[8];
-#pragma unroll
-              for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(o[g * 8 + i]) * inv;
-              *reinterpret_cast<uint4*>(out + q * 32 + g * 8) =
-                  make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-            }
-      }
+      for (int q = 0; q < DT / 32; ++q)             // Q's tile has been read
+        store_rows(head_row_out<__nv_bfloat16>(a.o, s.begin + first_row, h), a.o.token, s.len - first_row, to, q * 32, a.dim, inv, ok,
+                   sptr + t * S::kTile + (warp & 3) * 2048);
     }
   }
   tc_fence_before();
@@ -510,23 +525,6 @@ template <int DT> __device__ __forceinline__ void clear_rows(uint8_t* tile, int 
 #pragma unroll
     for (int q = 0; q < S::kSub; ++q) *reinterpret_cast<uint4*>(tile + q * S::kCols * 128 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
 }
-// 32 columns of an accumulator row times f, to bf16 (NaN where a wait ran out)
-__device__ __forceinline__ void store_part(__nv_bfloat16* out, uint32_t taddr, int c0, int dim, bool in, float f) {
-  uint32_t o[32];
-  tmem_ld32(taddr + c0, o);
-  tmem_ld_wait();
-  if (in)
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-      if (c0 + g * 8 < dim) {
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(o[g * 8 + i]) * f;
-        *reinterpret_cast<uint4*>(out + c0 + g * 8) =
-            make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-      }
-}
-
 struct TcBwdMaps { CUtensorMap q, k, v, d_o; };
 
 template <int DT>
@@ -743,11 +741,12 @@ attn_packed_dkv_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
     if (ok) ok = wait_for(acc_full, 0, abort_flag, status, 62);
     ok = __all_sync(0xffffffffu, ok);
     tc_fence_after();
-    const bool in = key < s.len;
-    const float bad = ok ? 1.f : NAN;
+    const int first_row = k0 + (warp & 3) * 32;
+    uint8_t* const stage = sptr + (sQ - base) + warp * 2048;           // the streamed tiles have been read
     static_assert(DT == S::kParts * 32, "a part of the threads stores 32 columns of each gradient");
-    store_part(head_row_out<__nv_bfloat16>(a.dv, s.begin + key, hk), col_dv + lanes, c0, a.dim, in, bad);
-    store_part(head_row_out<__nv_bfloat16>(a.dk, s.begin + key, hk), col_dk + lanes, c0, a.dim, in, a.scale * bad);
+    static_assert(S::kParts * 4 * 2048 <= 2 * S::kStages * S::kStream, "staging");
+    store_rows(head_row_out<__nv_bfloat16>(a.dv, s.begin + first_row, hk), a.dv.token, s.len - first_row, col_dv + lanes, c0, a.dim, 1.f, ok, stage);
+    store_rows(head_row_out<__nv_bfloat16>(a.dk, s.begin + first_row, hk), a.dk.token, s.len - first_row, col_dk + lanes, c0, a.dim, a.scale, ok, stage);
   }
   tc_fence_before();
   __syncthreads();
@@ -933,7 +932,9 @@ attn_packed_dq_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_cons
     if (ok) ok = wait_for(acc_full, 0, abort_flag, status, 80);
     ok = __all_sync(0xffffffffu, ok);
     tc_fence_after();
-    store_part(head_row_out<__nv_bfloat16>(a.dq, s.begin + row, h), col_dq + lanes, c0, a.dim, row < s.len, ok ? a.scale : NAN);
+    const int first_row = q0 + (warp & 3) * 32;
+    store_rows(head_row_out<__nv_bfloat16>(a.dq, s.begin + first_row, h), a.dq.token, s.len - first_row, col_dq + lanes, c0, a.dim, a.scale, ok,
+               sptr + (sK - base) + warp * 2048);                      // the streamed tiles have been read
   }
   tc_fence_before();
   __syncthreads();
