@@ -115,7 +115,8 @@ def lib():
                                         C.c_int32, C.POINTER(pm_config), C.c_int64, vp]
     L.pm_update_flat_static_max_stages.restype = C.c_int32
     L.pm_update_flat_static_last_error.restype = C.c_char_p
-    i32, i64, u64, view, desc = C.c_int32, C.c_int64, C.c_uint64, C.POINTER(pm_head_view), C.POINTER(pm_attention_desc)
+    # views by address: a call's views are one array
+    i32, i64, u64, view, desc = C.c_int32, C.c_int64, C.c_uint64, vp, C.POINTER(pm_attention_desc)
     L.pm_attention_packed_forward.argtypes = [desc, view, view, view, vp, view, vp, vp]
     L.pm_attention_packed_workspace_bytes.argtypes = [desc]
     L.pm_attention_packed_workspace_bytes.restype = u64

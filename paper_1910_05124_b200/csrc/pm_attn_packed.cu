@@ -7,8 +7,8 @@
 //
 // Tiles of 64 x 64 scores by 256 threads, a thread holds 4 x 4 of them; operands are fp32 in shared memory whatever their type
 // (exact for bf16), all sums fp32.  Forward: one block per 64 query rows and head, one pass over the keys with the running
-// maximum and sum.  Backward: one kernel owns query rows (dq), one owns key rows (dk, dv) and walks the query tiles of every
-// head of its group, so each gradient is summed by one block in a fixed order, without atomics, at the price of forming the
+// maximum and sum.  Backward: a block owns query rows (dq), or key rows (dk, dv) and walks the query tiles of every head of
+// its group, so each gradient is summed by one block in a fixed order, without atomics, at the price of forming the
 // scores twice.
 #include <atomic>
 
@@ -217,13 +217,12 @@ __global__ void __launch_bounds__(256) attn_packed_delta_kernel(PackedArgs a) {
   }
 }
 
-template <typename T, int DP, bool VEC>
-__global__ void __launch_bounds__(PK_THREADS) attn_packed_dq_kernel(PackedArgs a) {
-  const SeqTile s = pk_tile(a);
+template <typename T, int DP, bool VEC> __device__ __forceinline__ void pk_dq_block(const PackedArgs& a, int block) {
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.heads, PK_LOG_T);
   if (s.tile < 0) { pdl_wait(); return; }
   extern __shared__ float sm[];
   float *sQ = sm, *sO = sQ + PK_T * kPkLd<DP>, *sK = sO + PK_T * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sS = sV + PK_T * kPkLd<DP>;
-  const int h = blockIdx.y, hk = h / a.group, q0 = s.tile * PK_T;
+  const int h = block % a.heads, hk = h / a.group, q0 = s.tile * PK_T;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   PkPair<T, DP, VEC> next;
   {
@@ -233,6 +232,7 @@ __global__ void __launch_bounds__(PK_THREADS) attn_packed_dq_kernel(PackedArgs a
     own.x.put(sQ);
     own.y.put(sO);
   }
+  pdl_wait();                                     // delta
   float lse[4], delta[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -265,17 +265,15 @@ __global__ void __launch_bounds__(PK_THREADS) attn_packed_dq_kernel(PackedArgs a
   }
   const float f[4] = {a.scale, a.scale, a.scale, a.scale};
   pk_store<T, DP>(a.dq, s, q0, h, a.dim, dq, f);
-  pdl_wait();
 }
 
-template <typename T, int DP, bool VEC>
-__global__ void __launch_bounds__(PK_THREADS) attn_packed_dkv_kernel(PackedArgs a) {
-  const SeqTile s = pk_tile(a);
-  if (s.tile < 0) { pdl_wait(); pdl_trigger(); return; }
+template <typename T, int DP, bool VEC> __device__ __forceinline__ void pk_dkv_block(const PackedArgs& a, int block) {
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.kv_heads, PK_LOG_T);
+  if (s.tile < 0) { pdl_wait(); return; }
   extern __shared__ float sm[];
   float *sK = sm, *sV = sK + PK_T * kPkLd<DP>, *sQ = sV + PK_T * kPkLd<DP>, *sO = sQ + PK_T * kPkLd<DP>, *sP = sO + PK_T * kPkLd<DP>,
         *sS = sP + PK_T * PK_LDP, *sR = sS + PK_T * PK_LDP;
-  const int hk = blockIdx.y, k0 = s.tile * PK_T;
+  const int hk = block % a.kv_heads, k0 = s.tile * PK_T;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int first = a.causal ? k0 : 0, per_head = (s.len - first + PK_T - 1) / PK_T, n_it = per_head * a.group;
   // a query tile's lse (threads 0 .. 63) and delta (64 .. 127) travel with it
@@ -289,7 +287,6 @@ __global__ void __launch_bounds__(PK_THREADS) attn_packed_dkv_kernel(PackedArgs 
     PkPair<T, DP, VEC> own;
     own.fetch(a.k, a.v, s, k0, hk, a.dim);
     pdl_wait();                                   // delta
-    pdl_trigger();
     if (next.kAhead) next.fetch(a.q, a.d_o, s, first, hk * a.group, a.dim);
     own.x.put(sK);
     own.y.put(sV);
@@ -336,6 +333,13 @@ __global__ void __launch_bounds__(PK_THREADS) attn_packed_dkv_kernel(PackedArgs 
   pk_store<T, DP>(a.dv, s, k0, hk, a.dim, dv, one);
 }
 
+// The blocks of dk and dv, and behind them those of dq.
+template <typename T, int DP, bool VEC>
+__global__ void __launch_bounds__(PK_THREADS) attn_packed_bwd_kernel(PackedArgs a, int dkv_blocks) {
+  if ((int)blockIdx.x < dkv_blocks) pk_dkv_block<T, DP, VEC>(a, blockIdx.x);
+  else pk_dq_block<T, DP, VEC>(a, blockIdx.x - dkv_blocks);
+}
+
 // raises a kernel's shared-memory limit once per device
 template <typename K> static cudaError_t pk_allow(K kernel, int bytes, std::atomic<uint64_t>& done) {
   int dev = 0;
@@ -355,14 +359,15 @@ template <typename T, int DP, bool VEC> static cudaError_t pk_forward(const Pack
   return launch_pdl(attn_packed_fwd_kernel<T, DP, VEC>, dim3((unsigned)most_tiles(a.tokens, a.n_seqs, PK_T), a.heads), dim3(PK_THREADS), smem, st, false, a);
 }
 template <typename T, int DP, bool VEC> static cudaError_t pk_backward(const PackedArgs& a, cudaStream_t st) {
-  static std::atomic<uint64_t> done[2];
-  cudaError_t e = pk_allow(attn_packed_dq_kernel<T, DP, VEC>, pk_smem<DP>(4, 1), done[0]);
-  if (e == cudaSuccess) e = pk_allow(attn_packed_dkv_kernel<T, DP, VEC>, pk_smem<DP>(4, 2), done[1]);
-  const unsigned tiles = (unsigned)most_tiles(a.tokens, a.n_seqs, PK_T);
+  static std::atomic<uint64_t> done{0};
+  constexpr int smem = pk_smem<DP>(4, 2);
+  cudaError_t e = pk_allow(attn_packed_bwd_kernel<T, DP, VEC>, smem, done);
+  const int64_t tiles = most_tiles(a.tokens, a.n_seqs, PK_T);
+  if (tiles * (a.heads + a.kv_heads) > 0x7fffffff) return cudaErrorInvalidConfiguration;
   if (e == cudaSuccess) e = launch_pdl(attn_packed_delta_kernel<T>, dim3((unsigned)((a.tokens * a.heads + 7) / 8)), dim3(256), 0, st, false, a);
-  // dq starts once every block of dk, dv has passed its wait for delta, beside them; it ends behind them
-  if (e == cudaSuccess) e = launch_pdl(attn_packed_dkv_kernel<T, DP, VEC>, dim3(tiles, a.kv_heads), dim3(PK_THREADS), pk_smem<DP>(4, 2), st, true, a);
-  if (e == cudaSuccess) e = launch_pdl(attn_packed_dq_kernel<T, DP, VEC>, dim3(tiles, a.heads), dim3(PK_THREADS), pk_smem<DP>(4, 1), st, true, a);
+  if (e == cudaSuccess)
+    e = launch_pdl(attn_packed_bwd_kernel<T, DP, VEC>, dim3((unsigned)(tiles * (a.heads + a.kv_heads))), dim3(PK_THREADS), smem, st, true, a,
+                   (int)(tiles * a.kv_heads));
   return e;
 }
 template <typename T, int DP> static cudaError_t pk_width(const PackedArgs& a, bool backward, cudaStream_t st) {

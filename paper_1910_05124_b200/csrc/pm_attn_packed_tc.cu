@@ -464,7 +464,7 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
 
 // ---- backward ---------------------------------------------------------------------------------------------------
 //
-// Two kernels, as on the CUDA cores: one owns 128 key rows (dk, dv), one owns 128 query rows (dq); every gradient is summed by one
+// Two kinds of blocks, as on the CUDA cores: one owns 128 key rows (dk, dv), one 128 query rows (dq); every gradient is summed by one
 // block in a fixed order.  Seven products a pair of tiles instead of the five that sharing the scores would take, and no atomics,
 // no fp32 copy of dq in memory.  Both have the shape  two products -> 128 x BN values in registers -> bf16 factors in tensor
 // memory -> one or two products that accumulate; a thread holds 32 values of one row.
@@ -527,12 +527,10 @@ template <int DT> __device__ __forceinline__ void clear_rows(uint8_t* tile, int 
 }
 struct TcBwdMaps { CUtensorMap q, k, v, d_o; };
 
-template <int DT>
-__global__ void __launch_bounds__(BwdShape<DT>::kThreads, BwdShape<DT>::kBlocks)
-attn_packed_dkv_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcBwdMaps maps) {
+template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a, const TcBwdMaps& maps, int block) {
   using S = BwdShape<DT>;
   constexpr int BN = S::kCols, kCopy = S::kParts * 4, kIssue = kCopy + 1;        // the warps that copy and issue
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = blockIdx.x % a.kv_heads;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = block % a.kv_heads;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const sptr = smem_raw + (base - raw);
@@ -561,12 +559,11 @@ attn_packed_dkv_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
     tmem_alloc(smem_u32(tmem_slot), S::kTmem);
     tmem_relinquish();
   }
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.kv_heads, TC_LOG_ROWS);
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.kv_heads, TC_LOG_ROWS);
   if (s.tile < 0) {
     __syncthreads();
     if (warp == kIssue) tmem_dealloc(*tmem_slot, S::kTmem);
     pdl_wait();
-    pdl_trigger();
     return;
   }
   const int k0 = s.tile * TC_ROWS, first = a.causal ? k0 : 0;
@@ -599,7 +596,6 @@ attn_packed_dkv_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
     int armed = 1, h = hk * a.group, q0 = first;
     bool ok = true;
     pdl_wait();                                   // delta
-    pdl_trigger();
     for (int it = 0; it < n_it; ++it) {
       const int st = it % S::kStages;
       if (it >= S::kStages) ok = wait_for(empty(st), (it / S::kStages - 1) & 1, abort_flag, status, 51);
@@ -756,12 +752,10 @@ attn_packed_dkv_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
   }
 }
 
-template <int DT>
-__global__ void __launch_bounds__(BwdShape<DT>::kThreads, BwdShape<DT>::kBlocks)
-attn_packed_dq_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcBwdMaps maps) {
+template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, const TcBwdMaps& maps, int block) {
   using S = BwdShape<DT>;
   constexpr int BN = S::kCols, kCopy = S::kParts * 4, kIssue = kCopy + 1;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.x % a.heads, hk = h / a.group;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = block % a.heads, hk = h / a.group;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const sptr = smem_raw + (base - raw);
@@ -787,7 +781,7 @@ attn_packed_dq_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_cons
     tmem_alloc(smem_u32(tmem_slot), S::kTmem);
     tmem_relinquish();
   }
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.heads, TC_LOG_ROWS);
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.heads, TC_LOG_ROWS);
   if (s.tile < 0) {
     __syncthreads();
     if (warp == kIssue) tmem_dealloc(*tmem_slot, S::kTmem);
@@ -888,6 +882,7 @@ attn_packed_dq_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_cons
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float c = a.scale * kLog2e;
     const int64_t at = (int64_t)h * a.tokens + s.begin + row;
+    pdl_wait();                                   // delta
     const float lse = row < s.len ? a.lse[at] * kLog2e : INFINITY, delta = row < s.len ? a.delta[at] : 0.f;
     const int limit = a.causal ? min(s.len, row + 1) : s.len;
     bool ok = true;
@@ -942,8 +937,16 @@ attn_packed_dq_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_cons
     tc_fence_after();
     tmem_dealloc(tmem, S::kTmem);
   }
-  pdl_wait();
 }
+
+// The blocks of dk and dv, and behind them, on the SMs that the longest of those leave free, the blocks of dq.
+template <int DT>
+__global__ void __launch_bounds__(BwdShape<DT>::kThreads, BwdShape<DT>::kBlocks)
+attn_packed_bwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcBwdMaps maps, int dkv_blocks) {
+  if ((int)blockIdx.x < dkv_blocks) dkv_block<DT>(a, maps, blockIdx.x);
+  else dq_block<DT>(a, maps, blockIdx.x - dkv_blocks);
+}
+
 
 // delta_i = do_i . o_i: eight lanes a row, two rows to each lane with all loads in flight; blockIdx.y is the head.  Rows outside the
 // sequences get a value that nothing reads.
@@ -1060,23 +1063,22 @@ cudaError_t attn_packed_tc_forward(const PackedArgs& a, cudaStream_t st) {
 }
 
 template <int DT> static cudaError_t bwd_launch(const PackedArgs& a, cudaStream_t st) {
-  static std::atomic<uint64_t> done[2];
+  static std::atomic<uint64_t> done{0};
   using S = BwdShape<DT>;
   TcBwdMaps maps;
-  cudaError_t e = allow_smem(attn_packed_dkv_tc_kernel<DT>, S::kSmem, done[0]);
-  if (e == cudaSuccess) e = allow_smem(attn_packed_dq_tc_kernel<DT>, S::kSmem, done[1]);
+  cudaError_t e = allow_smem(attn_packed_bwd_tc_kernel<DT>, S::kSmem, done);
   if (e == cudaSuccess) e = encode_heads(&maps.q, a.q, a.dim, a.heads, a.tokens, S::kCols);
   if (e == cudaSuccess) e = encode_heads(&maps.k, a.k, a.dim, a.kv_heads, a.tokens, S::kCols);
   if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.tokens, S::kCols);
   if (e == cudaSuccess) e = encode_heads(&maps.d_o, a.d_o, a.dim, a.heads, a.tokens, S::kCols);
   if (e != cudaSuccess) return e;
   const int64_t tiles = most_tiles(a.tokens, a.n_seqs, TC_ROWS);
-  if (tiles * a.heads > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  if (tiles * (a.heads + a.kv_heads) > 0x7fffffff) return cudaErrorInvalidConfiguration;
   e = launch_pdl(attn_packed_delta_tc_kernel, dim3((unsigned)((a.tokens + 32 * DELTA_R - 1) / (32 * DELTA_R)), a.heads), dim3(256), 0, st, false, a);
-  // The second kernel starts once every block of the first has passed its wait for delta, so its blocks fill the SMs that the first's last
-  // and longest blocks leave; it ends behind the first.
-  if (e == cudaSuccess) e = launch_pdl(attn_packed_dkv_tc_kernel<DT>, dim3((unsigned)(tiles * a.kv_heads)), dim3(S::kThreads), S::kSmem, st, true, a, maps);
-  if (e == cudaSuccess) e = launch_pdl(attn_packed_dq_tc_kernel<DT>, dim3((unsigned)(tiles * a.heads)), dim3(S::kThreads), S::kSmem, st, true, a, maps);
+  // starts beside the first's last blocks; its own wait for them before they read delta
+  if (e == cudaSuccess)
+    e = launch_pdl(attn_packed_bwd_tc_kernel<DT>, dim3((unsigned)(tiles * (a.heads + a.kv_heads))), dim3(S::kThreads), S::kSmem, st, true, a, maps,
+                   (int)(tiles * a.kv_heads));
   return e;
 }
 cudaError_t attn_packed_tc_backward(const PackedArgs& a, cudaStream_t st) { return a.dim <= 64 ? bwd_launch<64>(a, st) : bwd_launch<128>(a, st); }

@@ -13,6 +13,7 @@ import torch
 from .binding import (PM_BF16, PM_F32, PipeMareError, _check, lib, pm_attention_desc, pm_head_view, pm_tensor_pair)
 
 _DTYPES = {torch.float32: PM_F32, torch.bfloat16: PM_BF16}
+_VIEW = C.sizeof(pm_head_view)
 
 
 def _refuse(message, status="PM_ERR_INVALID_ARG"):
@@ -106,45 +107,59 @@ class PackedAttention:
         if not isinstance(cu_seqlens, torch.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.numel() < 1:
             _refuse("cu_seqlens must be a one-dimensional tensor of sequences + 1 entries", "PM_ERR_SHAPE")
         cu = _flat("cu_seqlens", cu_seqlens, torch.int32, device, cu_seqlens.shape)
-        return device, pm_attention_desc(_DTYPES[q.dtype], self.n_heads, self.n_kv_heads, self.head_dim, cu_seqlens.numel() - 1, self.causal,
-                                         q.shape[0], self.scale), cu
+        tokens = q.shape[0]
+        return device, tokens, pm_attention_desc(_DTYPES[q.dtype], self.n_heads, self.n_kv_heads, self.head_dim, cu_seqlens.numel() - 1,
+                                                 self.causal, tokens, self.scale), cu
 
-    def _view(self, name, t, q, heads, written=False):
-        shape = (q.shape[0], heads, self.head_dim)
-        if not (isinstance(t, torch.Tensor) and t.dtype is q.dtype and t.device == q.device and t.shape == shape):
-            _mismatch(name, t, q.dtype, q.device, shape)
-        token, head, one = t.stride()
-        if one != 1 and self.head_dim > 1:
-            _refuse(f"the last dimension of {name} must be contiguous")
-        if written and not (head == self.head_dim and token >= heads * head):
-            # rows of one head, or heads of one row, must not share elements
-            spread = sorted((s, n) for s, n in ((token, shape[0]), (head, heads)) if n > 1)
-            end = self.head_dim
-            for s, n in spread if shape[0] else ():
-                if s < end:
-                    _refuse(f"{name} overlaps itself")
-                end = s * (n - 1) + end
-        return C.byref(pm_head_view(t.data_ptr(), token, head))
+    def _views(self, tokens, dtype, device, read, written):
+        """One array of pm_head_view for (name, tensor, heads) triples, checked."""
+        d = self.head_dim
+        flat = []
+        for triples, out in ((read, False), (written, True)):
+            for name, t, heads in triples:
+                if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and t.shape == (tokens, heads, d)):
+                    _mismatch(name, t, dtype, device, (tokens, heads, d))
+                token, head, one = t.stride()
+                if one != 1 and d > 1:
+                    _refuse(f"the last dimension of {name} must be contiguous")
+                if out and not (head == d and token >= heads * d):
+                    self._check_apart(name, ((token, tokens), (head, heads)))
+                flat += (t.data_ptr(), token, head)
+        return (C.c_int64 * len(flat))(*flat)
+
+    def _check_apart(self, name, dims):
+        """Rows of one head, or heads of one row, of a tensor that is written must not share elements."""
+        if min(n for _, n in dims) < 1:
+            return
+        end = self.head_dim
+        for stride, n in sorted((s, n) for s, n in dims if n > 1):
+            if stride < end:
+                _refuse(f"{name} overlaps itself")
+            end += stride * (n - 1)
 
     def pm_attention_packed_forward(self, q, k, v, cu_seqlens, o, lse=None, stream=None):
         """Writes o and, for a backward pass, lse."""
-        device, d, cu = self._desc(q, cu_seqlens)
-        H, K, view = self.n_heads, self.n_kv_heads, self._view
-        args = (C.byref(d), view("q", q, q, H), view("k", k, q, K), view("v", v, q, K), cu, view("o", o, q, H, True),
-                _flat("lse", lse, torch.float32, device, (H, q.shape[0])))
-        _launch(lambda st: self.L.pm_attention_packed_forward(*args, st), device, stream)
+        device, tokens, d, cu = self._desc(q, cu_seqlens)
+        H, K = self.n_heads, self.n_kv_heads
+        views = self._views(tokens, q.dtype, device, (("q", q, H), ("k", k, K), ("v", v, K)), (("o", o, H),))
+        p_lse = _flat("lse", lse, torch.float32, device, (H, tokens))
+        at = C.addressof(views)
+        _launch(lambda st: self.L.pm_attention_packed_forward(C.byref(d), at, at + _VIEW, at + 2 * _VIEW, cu, at + 3 * _VIEW, p_lse, st), device, stream)
 
     def pm_attention_packed_backward(self, q, k, v, o, lse, d_o, cu_seqlens, dq, dk, dv, stream=None):
         """Writes dq, dk and dv from d_o and what the forward call wrote."""
-        device, d, cu = self._desc(q, cu_seqlens)
+        device, tokens, d, cu = self._desc(q, cu_seqlens)
         if lse is None:
             _refuse("lse must be a tensor")
-        H, K, view = self.n_heads, self.n_kv_heads, self._view
-        args = (C.byref(d), view("q", q, q, H), view("k", k, q, K), view("v", v, q, K), view("o", o, q, H),
-                _flat("lse", lse, torch.float32, device, (H, q.shape[0])), view("d_o", d_o, q, H), cu,
-                view("dq", dq, q, H, True), view("dk", dk, q, K, True), view("dv", dv, q, K, True))
-        need = self.L.pm_attention_packed_workspace_bytes(args[0])
-        _launch(lambda st, ws=None: self.L.pm_attention_packed_backward(*args, ws, need, st), device, stream, need)
+        H, K = self.n_heads, self.n_kv_heads
+        views = self._views(tokens, q.dtype, device, (("q", q, H), ("k", k, K), ("v", v, K), ("o", o, H), ("d_o", d_o, H)),
+                            (("dq", dq, H), ("dk", dk, K), ("dv", dv, K)))
+        p_lse = _flat("lse", lse, torch.float32, device, (H, tokens))
+        at, desc = C.addressof(views), C.byref(d)
+        need = self.L.pm_attention_packed_workspace_bytes(desc)
+        _launch(lambda st, ws=None: self.L.pm_attention_packed_backward(
+            desc, at, at + _VIEW, at + 2 * _VIEW, at + 3 * _VIEW, p_lse, at + 4 * _VIEW, cu, at + 5 * _VIEW, at + 6 * _VIEW, at + 7 * _VIEW, ws, need, st),
+            device, stream, need)
 
     def pm_attention_packed_status(self, device="cuda", stream=None):
         """Raises if a device-side wait of a tensor-core kernel ran out since the last call (a defect); synchronises the stream."""

@@ -150,7 +150,7 @@ def test_overlapping_outputs_are_seen():
     good = [((3, 4, 8), (32, 8, 1)), ((3, 4, 8), (64, 16, 1)), ((3, 4, 8), (8, 24, 1)), ((1, 4, 8), (0, 8, 1))]
     bad = [((3, 4, 8), (0, 8, 1)), ((3, 4, 8), (32, 0, 1)), ((3, 4, 8), (31, 8, 1)), ((3, 4, 8), (8, 23, 1)), ((3, 4, 8), (32, 4, 1))]
     for shape, strides in good:
-        op._view("o", _strided(shape, strides), q[:shape[0]], 4, written=True)
+        op._views(shape[0], q.dtype, q.device, (), (("o", _strided(shape, strides), 4),))
     for shape, strides in bad:
         with pytest.raises(pm.PipeMareError, match="overlaps"):
-            op._view("o", _strided(shape, strides), q[:shape[0]], 4, written=True)
+            op._views(shape[0], q.dtype, q.device, (), (("o", _strided(shape, strides), 4),))
