@@ -129,15 +129,16 @@ __device__ __forceinline__ void pk_store(const HeadView& x, const SeqTile& s, in
     for (int c = 0; c < DP / 16; ++c) if (pk_col<DP>(c) < dim) out[pk_col<DP>(c)] = from_f<T>(acc[i][c] * f[i]);
   }
 }
-__device__ __forceinline__ SeqTile pk_tile(const PackedArgs& a) { return find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x, PK_LOG_T); }
+// tiles are counted from a sequence's end where the last ones see the most keys: the longest blocks start first
+__device__ __forceinline__ int pk_from_end(const SeqTile& s) { return (s.len + PK_T - 1) / PK_T - 1 - s.tile; }
 
 template <typename T, int DP, bool VEC>
 __global__ void __launch_bounds__(PK_THREADS) attn_packed_fwd_kernel(PackedArgs a) {
-  const SeqTile s = pk_tile(a);
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.heads, PK_LOG_T);
   if (s.tile < 0) return;
   extern __shared__ float sm[];
   float *sQ = sm, *sK = sQ + PK_T * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sP = sV + PK_T * kPkLd<DP>;
-  const int h = blockIdx.y, hk = h / a.group, q0 = s.tile * PK_T;
+  const int h = blockIdx.x % a.heads, hk = h / a.group, q0 = pk_from_end(s) * PK_T;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   PkPair<T, DP, VEC> next;
   {
@@ -222,7 +223,7 @@ template <typename T, int DP, bool VEC> __device__ __forceinline__ void pk_dq_bl
   if (s.tile < 0) { pdl_wait(); return; }
   extern __shared__ float sm[];
   float *sQ = sm, *sO = sQ + PK_T * kPkLd<DP>, *sK = sO + PK_T * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sS = sV + PK_T * kPkLd<DP>;
-  const int h = block % a.heads, hk = h / a.group, q0 = s.tile * PK_T;
+  const int h = block % a.heads, hk = h / a.group, q0 = pk_from_end(s) * PK_T;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   PkPair<T, DP, VEC> next;
   {
@@ -356,7 +357,9 @@ template <typename T, int DP, bool VEC> static cudaError_t pk_forward(const Pack
   constexpr int smem = pk_smem<DP>(3, 1);
   const cudaError_t e = pk_allow(attn_packed_fwd_kernel<T, DP, VEC>, smem, done);
   if (e != cudaSuccess) return e;
-  return launch_pdl(attn_packed_fwd_kernel<T, DP, VEC>, dim3((unsigned)most_tiles(a.tokens, a.n_seqs, PK_T), a.heads), dim3(PK_THREADS), smem, st, false, a);
+  const int64_t blocks = most_tiles(a.tokens, a.n_seqs, PK_T) * a.heads;
+  if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  return launch_pdl(attn_packed_fwd_kernel<T, DP, VEC>, dim3((unsigned)blocks), dim3(PK_THREADS), smem, st, false, a);
 }
 template <typename T, int DP, bool VEC> static cudaError_t pk_backward(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
