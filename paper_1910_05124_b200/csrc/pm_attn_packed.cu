@@ -15,21 +15,29 @@
 #include "pm_attn_packed.cuh"
 
 namespace pm {
+#ifndef PK_SMALL
+#define PK_SMALL 296
+#endif
 
-constexpr int PK_T = 64, PK_LOG_T = 6, PK_LDP = PK_T + 4, PK_THREADS = 256;
+constexpr int PK_T = 64, PK_LDP = PK_T + 4;       // rows of a streamed tile
+
+// A block owns R rows, 64 or 32, with 4 R threads.
 
 template <int DP> constexpr int kPkLd = DP + 4;
-template <int DP> constexpr int pk_smem(int tiles, int squares) { return (tiles * PK_T * kPkLd<DP> + squares * PK_T * PK_LDP + 2 * PK_T) * 4; }
+// `own` tiles of R rows, `streamed` ones of 64, `squares` of R x 64, and two values to each streamed row
+template <int DP, int R> constexpr int pk_smem(int own, int streamed, int squares) {
+  return ((own * R + streamed * PK_T) * kPkLd<DP> + squares * R * PK_LDP + 2 * PK_T) * 4;
+}
 
-// Rows row0 .. row0 + 63 of a head, zeros outside the sequence and behind the head's width: four consecutive values to a register
+// ROWS rows of a head from row0 on, zeros outside the sequence and behind the head's width: four consecutive values to a register
 // quadruple, all of a thread's loads in flight before the first is put into the tile.  VEC: one load brings the four.
-template <typename T, int DP, bool VEC> struct PkRows {
-  static constexpr int kN = DP / 16;
+template <typename T, int DP, bool VEC, int ROWS, int THREADS> struct PkRows {
+  static constexpr int kN = ROWS * DP / 4 / THREADS;
   float4 v[kN];
   __device__ __forceinline__ void fetch(const HeadView& x, const SeqTile& s, int row0, int head, int dim) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int at = i * PK_THREADS + threadIdx.x, r = at / (DP / 4), c = at % (DP / 4) * 4;
+      const int at = i * THREADS + threadIdx.x, r = at / (DP / 4), c = at % (DP / 4) * 4;
       v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (row0 + r >= s.len || c >= dim) continue;
       const T* p = head_row<T>(x, s.begin + row0 + r, head) + c;
@@ -49,15 +57,15 @@ template <typename T, int DP, bool VEC> struct PkRows {
   __device__ __forceinline__ void put(float* tile) const {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int at = i * PK_THREADS + threadIdx.x;
+      const int at = i * THREADS + threadIdx.x;
       *reinterpret_cast<float4*>(tile + at / (DP / 4) * kPkLd<DP> + at % (DP / 4) * 4) = v[i];
     }
   }
 };
 // A tile of each of two tensors per step.  The next step's are fetched while this one's are worked on, where registers allow.
-template <typename T, int DP, bool VEC> struct PkPair {
+template <typename T, int DP, bool VEC, int ROWS, int THREADS> struct PkPair {
   static constexpr bool kAhead = DP <= 64;
-  PkRows<T, DP, VEC> x, y;
+  PkRows<T, DP, VEC, ROWS, THREADS> x, y;
   __device__ __forceinline__ void fetch(const HeadView& a, const HeadView& b, const SeqTile& s, int row0, int head, int dim) {
     x.fetch(a, s, row0, head, dim);
     y.fetch(b, s, row0, head, dim);
@@ -130,19 +138,20 @@ __device__ __forceinline__ void pk_store(const HeadView& x, const SeqTile& s, in
   }
 }
 // tiles are counted from a sequence's end where the last ones see the most keys: the longest blocks start first
-__device__ __forceinline__ int pk_from_end(const SeqTile& s) { return (s.len + PK_T - 1) / PK_T - 1 - s.tile; }
+template <int R> __device__ __forceinline__ int pk_from_end(const SeqTile& s) { return (s.len + R - 1) / R - 1 - s.tile; }
+template <int R> constexpr int kLog = R == 64 ? 6 : 5;
 
-template <typename T, int DP, bool VEC>
-__global__ void __launch_bounds__(PK_THREADS) attn_packed_fwd_kernel(PackedArgs a) {
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.heads, PK_LOG_T);
+template <typename T, int DP, bool VEC, int R>
+__global__ void __launch_bounds__(4 * R) attn_packed_fwd_kernel(PackedArgs a) {
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.heads, kLog<R>);
   if (s.tile < 0) return;
   extern __shared__ float sm[];
-  float *sQ = sm, *sK = sQ + PK_T * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sP = sV + PK_T * kPkLd<DP>;
-  const int h = blockIdx.x % a.heads, hk = h / a.group, q0 = pk_from_end(s) * PK_T;
+  float *sQ = sm, *sK = sQ + R * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sP = sV + PK_T * kPkLd<DP>;
+  const int h = blockIdx.x % a.heads, hk = h / a.group, q0 = pk_from_end<R>(s) * R;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  PkPair<T, DP, VEC> next;
+  PkPair<T, DP, VEC, PK_T, 4 * R> next;
   {
-    PkRows<T, DP, VEC> q;
+    PkRows<T, DP, VEC, R, 4 * R> q;
     q.fetch(a.q, s, q0, h, a.dim);
     if (next.kAhead) next.fetch(a.k, a.v, s, 0, hk, a.dim);
     q.put(sQ);
@@ -150,7 +159,7 @@ __global__ void __launch_bounds__(PK_THREADS) attn_packed_fwd_kernel(PackedArgs 
   float o[4][DP / 16] = {}, m[4], l[4] = {};
 #pragma unroll
   for (int i = 0; i < 4; ++i) m[i] = -INFINITY;
-  const int end = a.causal ? min(s.len, q0 + PK_T) : s.len;
+  const int end = a.causal ? min(s.len, q0 + R) : s.len;
   for (int k0 = 0; k0 < end; k0 += PK_T) {
     if (!next.kAhead) next.fetch(a.k, a.v, s, k0, hk, a.dim);
     __syncthreads();
@@ -218,16 +227,16 @@ __global__ void __launch_bounds__(256) attn_packed_delta_kernel(PackedArgs a) {
   }
 }
 
-template <typename T, int DP, bool VEC> __device__ __forceinline__ void pk_dq_block(const PackedArgs& a, int block) {
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.heads, PK_LOG_T);
+template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void pk_dq_block(const PackedArgs& a, int block) {
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.heads, kLog<R>);
   if (s.tile < 0) { pdl_wait(); return; }
   extern __shared__ float sm[];
-  float *sQ = sm, *sO = sQ + PK_T * kPkLd<DP>, *sK = sO + PK_T * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sS = sV + PK_T * kPkLd<DP>;
-  const int h = block % a.heads, hk = h / a.group, q0 = pk_from_end(s) * PK_T;
+  float *sQ = sm, *sO = sQ + R * kPkLd<DP>, *sK = sO + R * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sS = sV + PK_T * kPkLd<DP>;
+  const int h = block % a.heads, hk = h / a.group, q0 = pk_from_end<R>(s) * R;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  PkPair<T, DP, VEC> next;
+  PkPair<T, DP, VEC, PK_T, 4 * R> next;
   {
-    PkPair<T, DP, VEC> own;
+    PkPair<T, DP, VEC, R, 4 * R> own;
     own.fetch(a.q, a.d_o, s, q0, h, a.dim);
     if (next.kAhead) next.fetch(a.k, a.v, s, 0, hk, a.dim);
     own.x.put(sQ);
@@ -242,7 +251,7 @@ template <typename T, int DP, bool VEC> __device__ __forceinline__ void pk_dq_bl
     delta[i] = r < s.len ? a.delta[(int64_t)h * a.tokens + s.begin + r] : 0.f;
   }
   float dq[4][DP / 16] = {};
-  const int end = a.causal ? min(s.len, q0 + PK_T) : s.len;
+  const int end = a.causal ? min(s.len, q0 + R) : s.len;
   for (int k0 = 0; k0 < end; k0 += PK_T) {
     if (!next.kAhead) next.fetch(a.k, a.v, s, k0, hk, a.dim);
     __syncthreads();
@@ -268,13 +277,13 @@ template <typename T, int DP, bool VEC> __device__ __forceinline__ void pk_dq_bl
   pk_store<T, DP>(a.dq, s, q0, h, a.dim, dq, f);
 }
 
-template <typename T, int DP, bool VEC> __device__ __forceinline__ void pk_dkv_block(const PackedArgs& a, int block) {
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.kv_heads, PK_LOG_T);
+template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void pk_dkv_block(const PackedArgs& a, int block) {
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.kv_heads, kLog<R>);
   if (s.tile < 0) { pdl_wait(); return; }
   extern __shared__ float sm[];
-  float *sK = sm, *sV = sK + PK_T * kPkLd<DP>, *sQ = sV + PK_T * kPkLd<DP>, *sO = sQ + PK_T * kPkLd<DP>, *sP = sO + PK_T * kPkLd<DP>,
-        *sS = sP + PK_T * PK_LDP, *sR = sS + PK_T * PK_LDP;
-  const int hk = block % a.kv_heads, k0 = s.tile * PK_T;
+  float *sK = sm, *sV = sK + R * kPkLd<DP>, *sQ = sV + R * kPkLd<DP>, *sO = sQ + PK_T * kPkLd<DP>, *sP = sO + PK_T * kPkLd<DP>,
+        *sS = sP + R * PK_LDP, *sR = sS + R * PK_LDP;
+  const int hk = block % a.kv_heads, k0 = s.tile * R;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int first = a.causal ? k0 : 0, per_head = (s.len - first + PK_T - 1) / PK_T, n_it = per_head * a.group;
   // a query tile's lse (threads 0 .. 63) and delta (64 .. 127) travel with it
@@ -283,9 +292,9 @@ template <typename T, int DP, bool VEC> __device__ __forceinline__ void pk_dkv_b
     if (threadIdx.x >= 128 || r >= s.len) return 0.f;
     return (threadIdx.x < 64 ? a.lse : a.delta)[(int64_t)h * a.tokens + s.begin + r];
   };
-  PkPair<T, DP, VEC> next;
+  PkPair<T, DP, VEC, PK_T, 4 * R> next;
   {
-    PkPair<T, DP, VEC> own;
+    PkPair<T, DP, VEC, R, 4 * R> own;
     own.fetch(a.k, a.v, s, k0, hk, a.dim);
     pdl_wait();                                   // delta
     if (next.kAhead) next.fetch(a.q, a.d_o, s, first, hk * a.group, a.dim);
@@ -335,10 +344,10 @@ template <typename T, int DP, bool VEC> __device__ __forceinline__ void pk_dkv_b
 }
 
 // The blocks of dk and dv, and behind them those of dq.
-template <typename T, int DP, bool VEC>
-__global__ void __launch_bounds__(PK_THREADS) attn_packed_bwd_kernel(PackedArgs a, int dkv_blocks) {
-  if ((int)blockIdx.x < dkv_blocks) pk_dkv_block<T, DP, VEC>(a, blockIdx.x);
-  else pk_dq_block<T, DP, VEC>(a, blockIdx.x - dkv_blocks);
+template <typename T, int DP, bool VEC, int R>
+__global__ void __launch_bounds__(4 * R) attn_packed_bwd_kernel(PackedArgs a, int dkv_blocks) {
+  if ((int)blockIdx.x < dkv_blocks) pk_dkv_block<T, DP, VEC, R>(a, blockIdx.x);
+  else pk_dq_block<T, DP, VEC, R>(a, blockIdx.x - dkv_blocks);
 }
 
 // raises a kernel's shared-memory limit once per device
@@ -352,34 +361,39 @@ template <typename K> static cudaError_t pk_allow(K kernel, int bytes, std::atom
   return e;
 }
 
-template <typename T, int DP, bool VEC> static cudaError_t pk_forward(const PackedArgs& a, cudaStream_t st) {
+template <typename T, int DP, bool VEC, int R> static cudaError_t pk_forward(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
-  constexpr int smem = pk_smem<DP>(3, 1);
-  const cudaError_t e = pk_allow(attn_packed_fwd_kernel<T, DP, VEC>, smem, done);
+  constexpr int smem = pk_smem<DP, R>(1, 2, 1);
+  const cudaError_t e = pk_allow(attn_packed_fwd_kernel<T, DP, VEC, R>, smem, done);
   if (e != cudaSuccess) return e;
-  const int64_t blocks = most_tiles(a.tokens, a.n_seqs, PK_T) * a.heads;
+  const int64_t blocks = most_tiles(a.tokens, a.n_seqs, R) * a.heads;
   if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-  return launch_pdl(attn_packed_fwd_kernel<T, DP, VEC>, dim3((unsigned)blocks), dim3(PK_THREADS), smem, st, false, a);
+  return launch_pdl(attn_packed_fwd_kernel<T, DP, VEC, R>, dim3((unsigned)blocks), dim3(4 * R), smem, st, false, a);
 }
-template <typename T, int DP, bool VEC> static cudaError_t pk_backward(const PackedArgs& a, cudaStream_t st) {
+template <typename T, int DP, bool VEC, int R> static cudaError_t pk_backward(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
-  constexpr int smem = pk_smem<DP>(4, 2);
-  cudaError_t e = pk_allow(attn_packed_bwd_kernel<T, DP, VEC>, smem, done);
-  const int64_t tiles = most_tiles(a.tokens, a.n_seqs, PK_T);
+  constexpr int smem = pk_smem<DP, R>(2, 2, 2);
+  cudaError_t e = pk_allow(attn_packed_bwd_kernel<T, DP, VEC, R>, smem, done);
+  const int64_t tiles = most_tiles(a.tokens, a.n_seqs, R);
   if (tiles * (a.heads + a.kv_heads) > 0x7fffffff) return cudaErrorInvalidConfiguration;
   if (e == cudaSuccess) e = launch_pdl(attn_packed_delta_kernel<T>, dim3((unsigned)((a.tokens * a.heads + 7) / 8)), dim3(256), 0, st, false, a);
   if (e == cudaSuccess)
-    e = launch_pdl(attn_packed_bwd_kernel<T, DP, VEC>, dim3((unsigned)(tiles * (a.heads + a.kv_heads))), dim3(PK_THREADS), smem, st, true, a,
+    e = launch_pdl(attn_packed_bwd_kernel<T, DP, VEC, R>, dim3((unsigned)(tiles * (a.heads + a.kv_heads))), dim3(4 * R), smem, st, true, a,
                    (int)(tiles * a.kv_heads));
   return e;
+}
+template <typename T, int DP, bool VEC> static cudaError_t pk_rows(const PackedArgs& a, bool backward, cudaStream_t st) {
+  // 32 rows to a block where blocks of 64 would leave SMs without one (as a rule on the most tiles that the lengths can make)
+  const bool small = most_tiles(a.tokens, a.n_seqs, PK_T) * (a.heads + (backward ? a.kv_heads : 0)) < PK_SMALL;
+  if (small) return backward ? pk_backward<T, DP, VEC, 32>(a, st) : pk_forward<T, DP, VEC, 32>(a, st);
+  return backward ? pk_backward<T, DP, VEC, 64>(a, st) : pk_forward<T, DP, VEC, 64>(a, st);
 }
 template <typename T, int DP> static cudaError_t pk_width(const PackedArgs& a, bool backward, cudaStream_t st) {
   // four elements at a time where every row of the inputs starts at such a boundary
   const size_t bytes = 4 * sizeof(T);
   bool vec = a.dim % 4 == 0;
   for (const HeadView* x : {&a.q, &a.k, &a.v, backward ? &a.d_o : &a.q}) vec = vec && aligned_to(x->data, bytes) && x->token % 4 == 0 && x->head % 4 == 0;
-  if (vec) return backward ? pk_backward<T, DP, true>(a, st) : pk_forward<T, DP, true>(a, st);
-  return backward ? pk_backward<T, DP, false>(a, st) : pk_forward<T, DP, false>(a, st);
+  return vec ? pk_rows<T, DP, true>(a, backward, st) : pk_rows<T, DP, false>(a, backward, st);
 }
 template <typename T> static cudaError_t pk_run(const PackedArgs& a, bool backward, cudaStream_t st) {
   if (a.dim <= 32) return pk_width<T, 32>(a, backward, st);

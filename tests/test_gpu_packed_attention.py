@@ -80,6 +80,13 @@ def test_shared_heads(cuda_device, H, K, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("D", [30, 32, 61, 64, 100, 128])
+def test_many_heads(cuda_device, D, dtype):
+    """More blocks than run at a time."""
+    check(*make([130, 257, 64], 40, 8, D, dtype, cuda_device, seed=D))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
 def test_many_sequences(cuda_device, dtype):
     lens = [(7 * i) % 23 for i in range(300)]                # more sequences than one round of the tile search takes, empty ones too
     check(*make(lens, 2, 1, 32, dtype, cuda_device, seed=1))
