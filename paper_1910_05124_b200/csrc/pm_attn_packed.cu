@@ -12,12 +12,12 @@
 // scores twice.
 #include <atomic>
 
+#include <cooperative_groups.h>
+
 #include "pm_attn_packed.cuh"
 
 namespace pm {
-#ifndef PK_SMALL
-#define PK_SMALL 296
-#endif
+namespace cg = cooperative_groups;
 
 constexpr int PK_T = 64, PK_LDP = PK_T + 4;       // rows of a streamed tile
 
@@ -140,27 +140,59 @@ __device__ __forceinline__ void pk_store(const HeadView& x, const SeqTile& s, in
 // tiles are counted from a sequence's end where the last ones see the most keys: the longest blocks start first
 template <int R> __device__ __forceinline__ int pk_from_end(const SeqTile& s) { return (s.len + R - 1) / R - 1 - s.tile; }
 template <int R> constexpr int kLog = R == 64 ? 6 : 5;
+template <int R> constexpr bool pk_split = R == 32;  // blocks of 64 rows are launched where there are enough of them: they are not shared
+
+// Where there are few blocks, a cluster of them shares one block's rows: each takes a part of what is streamed, leaves its sums in its
+// shared memory, and finishes a part of the rows from everybody's, added in the order of the parts.
+template <int DP> __device__ __forceinline__ void pk_leave(float* sums, const float (&acc)[4][DP / 16]) {
+  const int ty = threadIdx.x >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) sums[(4 * ty + i) * kPkLd<DP> + pk_col<DP>(c)] = acc[i][c];
+}
+template <typename T, int DP, int R, typename W>
+__device__ __forceinline__ void pk_finish(const HeadView& x, const SeqTile& s, int row0, int head, int dim, float* sums, int part, int parts, W weight) {
+  cg::cluster_group cluster = cg::this_cluster();
+  const int r0 = R * part / parts, r1 = R * (part + 1) / parts;
+  for (int i = threadIdx.x; i < (r1 - r0) * (DP / 4); i += 4 * R) {
+    const int r = r0 + i / (DP / 4), c = i % (DP / 4) * 4;
+    if (row0 + r >= s.len || c >= dim) continue;
+    float v[4] = {};
+    for (int p = 0; p < parts; ++p) {
+      const float4 u = *reinterpret_cast<const float4*>(cluster.map_shared_rank(sums + r * kPkLd<DP> + c, p));
+      const float f = weight(r, p);
+      v[0] += f * u.x; v[1] += f * u.y; v[2] += f * u.z; v[3] += f * u.w;
+    }
+    T* out = head_row_out<T>(x, s.begin + row0 + r, head) + c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) if (c + e < dim) out[e] = from_f<T>(v[e]);
+  }
+}
 
 template <typename T, int DP, bool VEC, int R>
-__global__ void __launch_bounds__(4 * R) attn_packed_fwd_kernel(PackedArgs a) {
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / a.heads, kLog<R>);
+__global__ void __launch_bounds__(4 * R, R == 64 && DP <= 64 ? 2 : 1) attn_packed_fwd_kernel(PackedArgs a) {
+  cg::cluster_group cluster = cg::this_cluster();
+  const int parts = pk_split<R> ? (int)cluster.num_blocks() : 1, part = pk_split<R> ? (int)cluster.block_rank() : 0, block = blockIdx.x / parts;
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.heads, kLog<R>);
   if (s.tile < 0) return;
   extern __shared__ float sm[];
   float *sQ = sm, *sK = sQ + R * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sP = sV + PK_T * kPkLd<DP>;
-  const int h = blockIdx.x % a.heads, hk = h / a.group, q0 = pk_from_end<R>(s) * R;
+  const int h = block % a.heads, hk = h / a.group, q0 = pk_from_end<R>(s) * R;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int all = a.causal ? min(s.len, q0 + R) : s.len, tiles = (all + PK_T - 1) / PK_T;
+  const int begin = tiles * part / parts * PK_T, end = min(all, tiles * (part + 1) / parts * PK_T);
   PkPair<T, DP, VEC, PK_T, 4 * R> next;
   {
     PkRows<T, DP, VEC, R, 4 * R> q;
     q.fetch(a.q, s, q0, h, a.dim);
-    if (next.kAhead) next.fetch(a.k, a.v, s, 0, hk, a.dim);
+    if (next.kAhead) next.fetch(a.k, a.v, s, begin, hk, a.dim);
     q.put(sQ);
   }
   float o[4][DP / 16] = {}, m[4], l[4] = {};
 #pragma unroll
   for (int i = 0; i < 4; ++i) m[i] = -INFINITY;
-  const int end = a.causal ? min(s.len, q0 + R) : s.len;
-  for (int k0 = 0; k0 < end; k0 += PK_T) {
+  for (int k0 = begin; k0 < end; k0 += PK_T) {
     if (!next.kAhead) next.fetch(a.k, a.v, s, k0, hk, a.dim);
     __syncthreads();
     next.x.put(sK);
@@ -181,7 +213,7 @@ __global__ void __launch_bounds__(4 * R) attn_packed_fwd_kernel(PackedArgs a) {
       }
 #pragma unroll
       for (int x = 8; x > 0; x >>= 1) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, x));
-      // the first tile holds key 0, which every row sees: mx is above -infinity unless the scores are
+      // -infinity: no key of this part yet
       const float base = mx == -INFINITY ? 0.f : mx, f = ex2((m[i] - base) * kLog2e);
       float sum = 0.f;
 #pragma unroll
@@ -199,6 +231,34 @@ __global__ void __launch_bounds__(4 * R) attn_packed_fwd_kernel(PackedArgs a) {
     }
     __syncthreads();
     pk_pb<DP>(o, sP, sV);
+  }
+  if (pk_split<R> && parts > 1) {
+    float* stats = sP;                            // maximum, sum [2][R]
+    __syncthreads();
+    pk_leave<DP>(sK, o);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if (tx == 0) { stats[4 * ty + i] = m[i]; stats[R + 4 * ty + i] = l[i]; }
+    cluster.sync();
+    // row r's maximum and 1 / sum over the parts
+    auto total = [&](int r, float& top, float& sum) {
+      top = -INFINITY;
+      for (int p = 0; p < parts; ++p) top = max_nan(top, cluster.map_shared_rank(stats, p)[r]);
+      sum = 0.f;
+      for (int p = 0; p < parts; ++p) sum += ex2((cluster.map_shared_rank(stats, p)[r] - top) * kLog2e) * cluster.map_shared_rank(stats, p)[R + r];
+    };
+    // weights of the parts, once per row of this block's share: [parts][R] behind the statistics
+    float* weights = stats + 2 * R;
+    const int r0 = R * part / parts, r1 = R * (part + 1) / parts;
+    for (int r = r0 + threadIdx.x; r < r1; r += 4 * R) {
+      float top, sum;
+      total(r, top, sum);
+      for (int p = 0; p < parts; ++p) weights[p * R + r] = ex2((cluster.map_shared_rank(stats, p)[r] - top) * kLog2e) / sum;
+      if (a.lse && q0 + r < s.len) a.lse[(int64_t)h * a.tokens + s.begin + q0 + r] = top + logf(sum);
+    }
+    __syncthreads();
+    pk_finish<T, DP, R>(a.o, s, q0, h, a.dim, sK, part, parts, [&](int r, int p) { return weights[p * R + r]; });
+    cluster.sync();                               // the others have read this block's sums
+    return;
   }
   float inv[4];
 #pragma unroll
@@ -227,18 +287,20 @@ __global__ void __launch_bounds__(256) attn_packed_delta_kernel(PackedArgs a) {
   }
 }
 
-template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void pk_dq_block(const PackedArgs& a, int block) {
+template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void pk_dq_block(const PackedArgs& a, int block, int part, int parts) {
   const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.heads, kLog<R>);
   if (s.tile < 0) { pdl_wait(); return; }
   extern __shared__ float sm[];
   float *sQ = sm, *sO = sQ + R * kPkLd<DP>, *sK = sO + R * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sS = sV + PK_T * kPkLd<DP>;
   const int h = block % a.heads, hk = h / a.group, q0 = pk_from_end<R>(s) * R;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int all = a.causal ? min(s.len, q0 + R) : s.len, tiles = (all + PK_T - 1) / PK_T;
+  const int begin = tiles * part / parts * PK_T, end = min(all, tiles * (part + 1) / parts * PK_T);
   PkPair<T, DP, VEC, PK_T, 4 * R> next;
   {
     PkPair<T, DP, VEC, R, 4 * R> own;
     own.fetch(a.q, a.d_o, s, q0, h, a.dim);
-    if (next.kAhead) next.fetch(a.k, a.v, s, 0, hk, a.dim);
+    if (next.kAhead) next.fetch(a.k, a.v, s, begin, hk, a.dim);
     own.x.put(sQ);
     own.y.put(sO);
   }
@@ -251,8 +313,7 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
     delta[i] = r < s.len ? a.delta[(int64_t)h * a.tokens + s.begin + r] : 0.f;
   }
   float dq[4][DP / 16] = {};
-  const int end = a.causal ? min(s.len, q0 + R) : s.len;
-  for (int k0 = 0; k0 < end; k0 += PK_T) {
+  for (int k0 = begin; k0 < end; k0 += PK_T) {
     if (!next.kAhead) next.fetch(a.k, a.v, s, k0, hk, a.dim);
     __syncthreads();
     next.x.put(sK);
@@ -273,11 +334,19 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
     __syncthreads();
     pk_pb<DP>(dq, sS, sK);
   }
+  if (pk_split<R> && parts > 1) {
+    __syncthreads();
+    pk_leave<DP>(sK, dq);
+    cg::this_cluster().sync();
+    pk_finish<T, DP, R>(a.dq, s, q0, h, a.dim, sK, part, parts, [&](int, int) { return a.scale; });
+    cg::this_cluster().sync();                    // the others have read this block's sums
+    return;
+  }
   const float f[4] = {a.scale, a.scale, a.scale, a.scale};
   pk_store<T, DP>(a.dq, s, q0, h, a.dim, dq, f);
 }
 
-template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void pk_dkv_block(const PackedArgs& a, int block) {
+template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void pk_dkv_block(const PackedArgs& a, int block, int part, int parts) {
   const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.kv_heads, kLog<R>);
   if (s.tile < 0) { pdl_wait(); return; }
   extern __shared__ float sm[];
@@ -285,11 +354,13 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
         *sS = sP + R * PK_LDP, *sR = sS + R * PK_LDP;
   const int hk = block % a.kv_heads, k0 = s.tile * R;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int first = a.causal ? k0 : 0, per_head = (s.len - first + PK_T - 1) / PK_T, n_it = per_head * a.group;
+  const int first = a.causal ? k0 : 0, per_head = (s.len - first + PK_T - 1) / PK_T;
+  const int it0 = per_head * a.group * part / parts, it1 = per_head * a.group * (part + 1) / parts;
+  int h = hk * a.group + it0 / per_head, q0 = first + it0 % per_head * PK_T;
   // a query tile's lse (threads 0 .. 63) and delta (64 .. 127) travel with it
   auto row_value = [&](int h, int q0) {
     const int r = q0 + (threadIdx.x & 63);
-    if (threadIdx.x >= 128 || r >= s.len) return 0.f;
+    if (threadIdx.x >= 128 || r >= s.len || it0 >= it1) return 0.f;
     return (threadIdx.x < 64 ? a.lse : a.delta)[(int64_t)h * a.tokens + s.begin + r];
   };
   PkPair<T, DP, VEC, PK_T, 4 * R> next;
@@ -297,14 +368,13 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
     PkPair<T, DP, VEC, R, 4 * R> own;
     own.fetch(a.k, a.v, s, k0, hk, a.dim);
     pdl_wait();                                   // delta
-    if (next.kAhead) next.fetch(a.q, a.d_o, s, first, hk * a.group, a.dim);
+    if (next.kAhead && it0 < it1) next.fetch(a.q, a.d_o, s, q0, h, a.dim);
     own.x.put(sK);
     own.y.put(sV);
   }
-  float next_row = row_value(hk * a.group, first);
+  float next_row = row_value(h, q0);
   float dk[4][DP / 16] = {}, dv[4][DP / 16] = {};
-  int h = hk * a.group, q0 = first;
-  for (int it = 0; it < n_it; ++it) {
+  for (int it = it0; it < it1; ++it) {
     if (!next.kAhead) next.fetch(a.q, a.d_o, s, q0, h, a.dim);
     __syncthreads();
     next.x.put(sQ);
@@ -314,7 +384,7 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
     const int r0 = q0;
     q0 += PK_T;
     if (q0 >= s.len) { q0 = first; ++h; }
-    if (it + 1 < n_it) {
+    if (it + 1 < it1) {
       next_row = row_value(h, q0);
       if (next.kAhead) next.fetch(a.q, a.d_o, s, q0, h, a.dim);
     }
@@ -338,6 +408,17 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
     pk_pb<DP>(dv, sP, sO);
     pk_pb<DP>(dk, sS, sQ);
   }
+  if (pk_split<R> && parts > 1) {
+    float* const other = sQ + R * kPkLd<DP>;
+    __syncthreads();
+    pk_leave<DP>(sQ, dk);
+    pk_leave<DP>(other, dv);
+    cg::this_cluster().sync();
+    pk_finish<T, DP, R>(a.dk, s, k0, hk, a.dim, sQ, part, parts, [&](int, int) { return a.scale; });
+    pk_finish<T, DP, R>(a.dv, s, k0, hk, a.dim, other, part, parts, [&](int, int) { return 1.f; });
+    cg::this_cluster().sync();                    // the others have read this block's sums
+    return;
+  }
   const float f[4] = {a.scale, a.scale, a.scale, a.scale}, one[4] = {1.f, 1.f, 1.f, 1.f};
   pk_store<T, DP>(a.dk, s, k0, hk, a.dim, dk, f);
   pk_store<T, DP>(a.dv, s, k0, hk, a.dim, dv, one);
@@ -346,8 +427,10 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
 // The blocks of dk and dv, and behind them those of dq.
 template <typename T, int DP, bool VEC, int R>
 __global__ void __launch_bounds__(4 * R) attn_packed_bwd_kernel(PackedArgs a, int dkv_blocks) {
-  if ((int)blockIdx.x < dkv_blocks) pk_dkv_block<T, DP, VEC, R>(a, blockIdx.x);
-  else pk_dq_block<T, DP, VEC, R>(a, blockIdx.x - dkv_blocks);
+  const int parts = pk_split<R> ? (int)cg::this_cluster().num_blocks() : 1, part = pk_split<R> ? (int)cg::this_cluster().block_rank() : 0;
+  const int block = blockIdx.x / parts;
+  if (block < dkv_blocks) pk_dkv_block<T, DP, VEC, R>(a, block, part, parts);
+  else pk_dq_block<T, DP, VEC, R>(a, block - dkv_blocks, part, parts);
 }
 
 // raises a kernel's shared-memory limit once per device
@@ -361,30 +444,59 @@ template <typename K> static cudaError_t pk_allow(K kernel, int bytes, std::atom
   return e;
 }
 
+template <typename... K, typename... A>
+static cudaError_t pk_launch(void (*kernel)(K...), int64_t blocks, int threads, int smem, cudaStream_t stream, bool pdl, int parts, A... args) {
+  if (blocks * parts > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(blocks * parts)); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+  cudaLaunchAttribute at[2];
+  int n = 0;
+  if (parts > 1) {
+    at[n].id = cudaLaunchAttributeClusterDimension;
+    at[n].val.clusterDim.x = parts; at[n].val.clusterDim.y = 1; at[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (pdl) {
+    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n].val.programmaticStreamSerializationAllowed = 1;
+    ++n;
+  }
+  cfg.attrs = at;
+  cfg.numAttrs = n;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<K>(args)...);
+}
+// Blocks to a cluster: up to four launched blocks per SM (their number is the most that the lengths can make), as long as each keeps
+// `least` streamed tiles in a sequence of average length.  fp32, both passes, us with clusters / without: 700 + 300 + 13 tokens, 4 heads of 128
+// on 2 XXX; 493 tokens in 7, 4 heads of 32 on 2 XXX.
+static int pk_parts(int64_t blocks, const PackedArgs& a, int heads, int least) {
+  const int64_t average = (a.tokens + a.n_seqs - 1) / a.n_seqs, tiles = (average + PK_T - 1) / PK_T * heads;
+  int parts = 1;
+  while (parts < 8 && blocks * parts * 2 <= 4 * kSms && tiles >= parts * 2 * least) parts *= 2;
+  return parts;
+}
+
 template <typename T, int DP, bool VEC, int R> static cudaError_t pk_forward(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   constexpr int smem = pk_smem<DP, R>(1, 2, 1);
   const cudaError_t e = pk_allow(attn_packed_fwd_kernel<T, DP, VEC, R>, smem, done);
   if (e != cudaSuccess) return e;
   const int64_t blocks = most_tiles(a.tokens, a.n_seqs, R) * a.heads;
-  if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-  return launch_pdl(attn_packed_fwd_kernel<T, DP, VEC, R>, dim3((unsigned)blocks), dim3(4 * R), smem, st, false, a);
+  return pk_launch(attn_packed_fwd_kernel<T, DP, VEC, R>, blocks, 4 * R, smem, st, false, pk_split<R> ? pk_parts(blocks, a, 1, 3) : 1, a);
 }
 template <typename T, int DP, bool VEC, int R> static cudaError_t pk_backward(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   constexpr int smem = pk_smem<DP, R>(2, 2, 2);
   cudaError_t e = pk_allow(attn_packed_bwd_kernel<T, DP, VEC, R>, smem, done);
-  const int64_t tiles = most_tiles(a.tokens, a.n_seqs, R);
-  if (tiles * (a.heads + a.kv_heads) > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  const int64_t tiles = most_tiles(a.tokens, a.n_seqs, R), blocks = tiles * (a.heads + a.kv_heads);
   if (e == cudaSuccess) e = launch_pdl(attn_packed_delta_kernel<T>, dim3((unsigned)((a.tokens * a.heads + 7) / 8)), dim3(256), 0, st, false, a);
   if (e == cudaSuccess)
-    e = launch_pdl(attn_packed_bwd_kernel<T, DP, VEC, R>, dim3((unsigned)(tiles * (a.heads + a.kv_heads))), dim3(4 * R), smem, st, true, a,
-                   (int)(tiles * a.kv_heads));
+    e = pk_launch(attn_packed_bwd_kernel<T, DP, VEC, R>, blocks, 4 * R, smem, st, true, pk_split<R> ? pk_parts(blocks, a, a.group, 2) : 1, a,
+                  (int)(tiles * a.kv_heads));
   return e;
 }
 template <typename T, int DP, bool VEC> static cudaError_t pk_rows(const PackedArgs& a, bool backward, cudaStream_t st) {
   // 32 rows to a block where blocks of 64 would leave SMs without one (as a rule on the most tiles that the lengths can make)
-  const bool small = most_tiles(a.tokens, a.n_seqs, PK_T) * (a.heads + (backward ? a.kv_heads : 0)) < PK_SMALL;
+  const bool small = most_tiles(a.tokens, a.n_seqs, PK_T) * (a.heads + (backward ? a.kv_heads : 0)) < 2 * kSms;
   if (small) return backward ? pk_backward<T, DP, VEC, 32>(a, st) : pk_forward<T, DP, VEC, 32>(a, st);
   return backward ? pk_backward<T, DP, VEC, 64>(a, st) : pk_forward<T, DP, VEC, 64>(a, st);
 }
