@@ -444,44 +444,13 @@ template <typename K> static cudaError_t pk_allow(K kernel, int bytes, std::atom
   return e;
 }
 
-template <typename... K, typename... A>
-static cudaError_t pk_launch(void (*kernel)(K...), int64_t blocks, int threads, int smem, cudaStream_t stream, bool pdl, int parts, A... args) {
-  if (blocks * parts > 0x7fffffff) return cudaErrorInvalidConfiguration;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(blocks * parts)); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
-  cudaLaunchAttribute at[2];
-  int n = 0;
-  if (parts > 1) {
-    at[n].id = cudaLaunchAttributeClusterDimension;
-    at[n].val.clusterDim.x = parts; at[n].val.clusterDim.y = 1; at[n].val.clusterDim.z = 1;
-    ++n;
-  }
-  if (pdl) {
-    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[n].val.programmaticStreamSerializationAllowed = 1;
-    ++n;
-  }
-  cfg.attrs = at;
-  cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<K>(args)...);
-}
-// Blocks to a cluster: up to four launched blocks per SM (their number is the most that the lengths can make), as long as each keeps
-// `least` streamed tiles in a sequence of average length.  fp32, both passes, us with clusters / without: 700 + 300 + 13 tokens, 4 heads of 128
-// on 2 XXX; 493 tokens in 7, 4 heads of 32 on 2 XXX.
-static int pk_parts(int64_t blocks, const PackedArgs& a, int heads, int least) {
-  const int64_t average = (a.tokens + a.n_seqs - 1) / a.n_seqs, tiles = (average + PK_T - 1) / PK_T * heads;
-  int parts = 1;
-  while (parts < 8 && blocks * parts * 2 <= 4 * kSms && tiles >= parts * 2 * least) parts *= 2;
-  return parts;
-}
-
 template <typename T, int DP, bool VEC, int R> static cudaError_t pk_forward(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   constexpr int smem = pk_smem<DP, R>(1, 2, 1);
   const cudaError_t e = pk_allow(attn_packed_fwd_kernel<T, DP, VEC, R>, smem, done);
   if (e != cudaSuccess) return e;
   const int64_t blocks = most_tiles(a.tokens, a.n_seqs, R) * a.heads;
-  return pk_launch(attn_packed_fwd_kernel<T, DP, VEC, R>, blocks, 4 * R, smem, st, false, pk_split<R> ? pk_parts(blocks, a, 1, 3) : 1, a);
+  return launch_clusters(attn_packed_fwd_kernel<T, DP, VEC, R>, blocks, 4 * R, smem, st, false, pk_split<R> ? packed_parts(blocks, a, PK_T, 1, 4 * kSms, 3) : 1, a);
 }
 template <typename T, int DP, bool VEC, int R> static cudaError_t pk_backward(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
@@ -490,7 +459,7 @@ template <typename T, int DP, bool VEC, int R> static cudaError_t pk_backward(co
   const int64_t tiles = most_tiles(a.tokens, a.n_seqs, R), blocks = tiles * (a.heads + a.kv_heads);
   if (e == cudaSuccess) e = launch_pdl(attn_packed_delta_kernel<T>, dim3((unsigned)((a.tokens * a.heads + 7) / 8)), dim3(256), 0, st, false, a);
   if (e == cudaSuccess)
-    e = pk_launch(attn_packed_bwd_kernel<T, DP, VEC, R>, blocks, 4 * R, smem, st, true, pk_split<R> ? pk_parts(blocks, a, a.group, 2) : 1, a,
+    e = launch_clusters(attn_packed_bwd_kernel<T, DP, VEC, R>, blocks, 4 * R, smem, st, true, pk_split<R> ? packed_parts(blocks, a, PK_T, a.group, 4 * kSms, 2) : 1, a,
                   (int)(tiles * a.kv_heads));
   return e;
 }

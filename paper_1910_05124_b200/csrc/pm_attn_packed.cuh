@@ -78,6 +78,38 @@ __device__ __forceinline__ SeqTile find_tile(const int32_t* cu, int n_seqs, int6
 // tiles of `rows` rows that sequences of `tokens` tokens in all can have at most
 inline int64_t most_tiles(int64_t tokens, int n_seqs, int rows) { return tokens / rows + n_seqs; }
 
+// `blocks` clusters of `parts` blocks
+template <typename... K, typename... A>
+inline cudaError_t launch_clusters(void (*kernel)(K...), int64_t blocks, int threads, int smem, cudaStream_t stream, bool pdl, int parts, A... args) {
+  if (blocks * parts > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(blocks * parts)); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+  cudaLaunchAttribute at[2];
+  int n = 0;
+  if (parts > 1) {
+    at[n].id = cudaLaunchAttributeClusterDimension;
+    at[n].val.clusterDim.x = parts; at[n].val.clusterDim.y = 1; at[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (pdl) {
+    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n].val.programmaticStreamSerializationAllowed = 1;
+    ++n;
+  }
+  cfg.attrs = at;
+  cfg.numAttrs = n;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<K>(args)...);
+}
+
+// Blocks that share the work of one: as many as leave no more than `most` in the launch (whose size is the most that the lengths can
+// make), as long as each keeps `least` streamed tiles of `rows` rows of `heads` heads in a sequence of average length.
+inline int packed_parts(int64_t blocks, const PackedArgs& a, int rows, int heads, int most, int least) {
+  const int64_t average = (a.tokens + a.n_seqs - 1) / a.n_seqs, tiles = (average + rows - 1) / rows * heads;
+  int parts = 1;
+  while (parts < 8 && blocks * parts * 2 <= most && tiles >= parts * 2 * least) parts *= 2;
+  return parts;
+}
+
 // launchers of the tensor-core kernels
 bool attn_packed_tc_takes(const PackedArgs& a, int dtype, bool backward);
 cudaError_t attn_packed_tc_forward(const PackedArgs& a, cudaStream_t st);

@@ -13,12 +13,14 @@
 // Where P lies over S, products that read P are issued before the product that overwrites it, and products complete in the order of
 // their issue, so a commit behind S(j + 1) also says that O holds tile j.
 #include <atomic>
-#include <mutex>
+
+#include <cooperative_groups.h>
 
 #include "pm_attn_packed.cuh"
 #include "pm_ptx.cuh"
 
 namespace pm {
+namespace cg = cooperative_groups;
 
 // A bounded wait that ran out (a defect): its code, kept until pm_attention_packed_status reads it.
 __device__ int g_attn_packed_status;
@@ -62,8 +64,12 @@ template <int DT, int NT> struct FwdShape {
 
 struct TcMaps { CUtensorMap q, k, v; };
 
+// What a matrix descriptor takes of a shared-memory address: in a block of a cluster the address carries the block's rank above it.
+__device__ __forceinline__ uint32_t own_address(uint32_t a) { return a & 0x3FFFFu; }
+
 // 128 x N x DT product of two K-major tiles
 template <int DT> __device__ __forceinline__ void mma_abt(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+  a = own_address(a); b = own_address(b);
   const uint64_t base = desc_base(16, 1024);
 #pragma unroll
   for (int k = 0; k < DT / 16; ++k) {
@@ -73,6 +79,7 @@ template <int DT> __device__ __forceinline__ void mma_abt(uint32_t d, uint32_t a
 }
 // 128 x DT x 64 product of half of A in tensor memory and half of a tile whose rows run along the depth
 template <int DT> __device__ __forceinline__ void mma_ab(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate, int half) {
+  b = own_address(b);
   const uint64_t base = desc_base(TC_SUB, 1024);
 #pragma unroll
   for (int k = 0; k < 4; ++k) tc_mma_bf16_ta(d, a + (half * 4 + k) * 8, desc_at(base, b + (half * 4 + k) * 2048), idesc, accumulate || k > 0);
@@ -104,7 +111,7 @@ __device__ __forceinline__ void store_rows(__nv_bfloat16* out, int64_t stride, i
   const int lane = threadIdx.x & 31;
   uint32_t o[32];
   tmem_ld32(taddr + c0, o);
-  tmem_ld_wait();
+  tmem_ld_wait(o);
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     float v[8];
@@ -122,6 +129,39 @@ __device__ __forceinline__ void store_rows(__nv_bfloat16* out, int64_t stride, i
     if (r < rows && c0 + g * 8 < dim) *reinterpret_cast<uint4*>(out + r * stride + c0 + g * 8) = w;
   }
   __syncwarp();
+}
+
+// Where there are few blocks, a cluster of them shares one block's rows: each takes a part of what is streamed, leaves its fp32 sums in its
+// shared memory, and finishes a part of the rows from everybody's, added in the order of the parts.
+template <int DT> constexpr int kSumLd = DT + 4;
+// 32 columns of each lane's row, from the accumulator or, of a block that had nothing to do, zeros
+template <int DT> __device__ __forceinline__ void leave_sums(float* row, uint32_t taddr, int c0, bool any) {
+  uint32_t o[32];
+  tmem_ld32(taddr + c0, o);
+  tmem_ld_wait(o);
+#pragma unroll
+  for (int i = 0; i < 32; i += 4)
+    *reinterpret_cast<uint4*>(row + c0 + i) = any ? make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]) : make_uint4(0u, 0u, 0u, 0u);
+}
+// this block's share of the rows, by its first `threads` threads
+template <int DT, typename W>
+__device__ __forceinline__ void finish_rows(const HeadView& x, const SeqTile& s, int row0, int head, int dim, float* sums, int part, int parts, int threads, W weight) {
+  cg::cluster_group cluster = cg::this_cluster();
+  const int r0 = TC_ROWS * part / parts, r1 = TC_ROWS * (part + 1) / parts;
+  for (int i = threadIdx.x; i < (r1 - r0) * (DT / 8); i += threads) {
+    const int r = r0 + i / (DT / 8), c = i % (DT / 8) * 8;
+    if (row0 + r >= s.len || c >= dim) continue;
+    float v[8] = {};
+    for (int p = 0; p < parts; ++p) {
+      const float4* u = reinterpret_cast<const float4*>(cluster.map_shared_rank(sums + r * kSumLd<DT> + c, p));
+      const float4 lo = u[0], hi = u[1];
+      const float f = weight(r, p);
+      v[0] += f * lo.x; v[1] += f * lo.y; v[2] += f * lo.z; v[3] += f * lo.w;
+      v[4] += f * hi.x; v[5] += f * hi.y; v[6] += f * hi.z; v[7] += f * hi.w;
+    }
+    *reinterpret_cast<uint4*>(head_row_out<__nv_bfloat16>(x, s.begin + row0 + r, head) + c) =
+        make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+  }
 }
 
 // 2^x for two values on the FMA units: x = n + f with n the nearest integer, 2^f by the polynomial of degree 4 with the least relative
@@ -184,8 +224,9 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
     tmem_relinquish();
   }
   const int log_rows = pair_heads ? TC_LOG_ROWS : TC_LOG_ROWS + NT - 1, rows = 1 << log_rows;
-  const int unit = blockIdx.x % units;
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, blockIdx.x / units, log_rows);
+  const int parts = NT == 1 ? (int)cg::this_cluster().num_blocks() : 1, part = NT == 1 ? (int)cg::this_cluster().block_rank() : 0;
+  const int block = blockIdx.x / parts, unit = block % units;
+  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / units, log_rows);
   if (s.tile < 0) {
     __syncthreads();
     if (warp == kIssue) tmem_dealloc(*tmem_slot, S::kCols);
@@ -200,20 +241,22 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
     return q0 >= s.len ? 0 : ((a.causal ? min(s.len, q0 + TC_ROWS) : s.len) + TC_ROWS - 1) / TC_ROWS;
   };
   const int hk = head_of(0) / a.group;
-  int n_keys = keys_of(0);
-  if (NT == 2) n_keys = max(n_keys, keys_of(1));
+  // of the key tiles, this block's share
+  const int j0 = NT == 1 ? keys_of(0) * part / parts : 0;
+  const int n_keys = NT == 1 ? keys_of(0) * (part + 1) / parts - j0 : max(keys_of(0), keys_of(NT - 1));
+  auto count_of = [&](int t) { return NT == 1 ? n_keys : keys_of(t); };
 
   auto copy_keys = [&](int j) {
     const int st = j % S::kStages;
-    if (elect_one()) { mbar_arrive_expect_tx(k_full(st), S::kTile); load_tile<DT>(sK + st * S::kTile, &maps.k, k_full(st), hk, s.begin + j * TC_ROWS); }
+    if (elect_one()) { mbar_arrive_expect_tx(k_full(st), S::kTile); load_tile<DT>(sK + st * S::kTile, &maps.k, k_full(st), hk, s.begin + (j0 + j) * TC_ROWS); }
     __syncwarp();
   };
   auto copy_values = [&](int j) {
     const int st = j % S::kStages;
-    if (elect_one()) { mbar_arrive_expect_tx(v_full(st), S::kTile); load_tile<DT>(sV + st * S::kTile, &maps.v, v_full(st), hk, s.begin + j * TC_ROWS); }
+    if (elect_one()) { mbar_arrive_expect_tx(v_full(st), S::kTile); load_tile<DT>(sV + st * S::kTile, &maps.v, v_full(st), hk, s.begin + (j0 + j) * TC_ROWS); }
     __syncwarp();
   };
-  if (warp == kCopy) {
+  if (warp == kCopy && n_keys > 0) {
     __syncwarp();
     if (elect_one()) {
       int bytes = 0;
@@ -236,7 +279,8 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
 
   if (warp >= S::kWarps) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kOtherRegs));
-  if (warp == kCopy) {                            // ---- copies
+  if (n_keys == 0) {                              // nothing of a shared block's keys
+  } else if (warp == kCopy) {                     // ---- copies
     int armed_k = 1, armed_v = 1;
     bool ok = true;
     for (int j = 1; j < n_keys && ok; ++j) {
@@ -266,7 +310,7 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
       tc_fence_after();
       if (elect_one()) {
         for (int t = 0; t < NT; ++t)
-          if (keys_of(t)) { mma_abt<DT>(col_s(t), sQ + t * S::kTile, sK, id_s); tc_commit(s_full(t)); }
+          if (count_of(t)) { mma_abt<DT>(col_s(t), sQ + t * S::kTile, sK, id_s); tc_commit(s_full(t)); }
         tc_commit(k_empty(0));
       }
       __syncwarp();
@@ -300,7 +344,7 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
           ok = next_keys();
 #pragma unroll
           for (int t = 0; t < NT; ++t)
-            if (ok && j + 1 < keys_of(t)) {
+            if (ok && j + 1 < count_of(t)) {
               ok = wait_for(s_read(t), j & 1, abort_flag, status, 42);
               tc_fence_after();
               if (ok) scores(t, j + 1);
@@ -311,7 +355,7 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
         ok = wait_for(v_full(st), (j / S::kStages) & 1, abort_flag, status, 36);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
-          if (ok && j < keys_of(t)) {
+          if (ok && j < count_of(t)) {
             ok = values(t, j);
             if (ok) done(o_full(t));
           }
@@ -323,7 +367,7 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
         if (ok && more && S::kStages > 1) ok = next_keys();
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          const int n = keys_of(t);
+          const int n = count_of(t);
           if (!ok || j >= n) continue;
           ok = values(t, j);
           if (ok && S::kStages == 1 && j + 1 < n) ok = next_keys();
@@ -338,11 +382,16 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
       }
     }
   }
+  if (NT == 1 && parts > 1) {
+    __syncwarp();
+    cluster_sync_all();
+    cluster_sync_all();
+  }
   } else {                                        // ---- softmax: thread = row
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kSoftmaxRegs));
     const int t = warp >> 2, r = threadIdx.x & 127;
-    const int n = keys_of(t), q0 = first_of(t), row = q0 + r;
-    if (n > 0) {
+    const int n = count_of(t), q0 = first_of(t), row = q0 + r;
+    if (n > 0 || parts > 1) {
       const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
       const uint32_t ts = col_s(t) + lanes, to = col_o(t) + lanes, tp = col_p(t) + lanes;
       const float c = a.scale * kLog2e;
@@ -354,7 +403,7 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after();
-        const int k0 = j * TC_ROWS;
+        const int k0 = (j0 + j) * TC_ROWS;
         const bool edge = k0 + TC_ROWS > s.len || (a.causal && k0 + TC_ROWS > q0 + 1);
         // The rows behind the sequence's end of its last value tile belong to other sequences, or to none: zeros, as p is there, so
         // that nothing that is not finite meets a zero.  The first query tile that reads the tile clears it.
@@ -373,7 +422,8 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
         for (int q = 0; q < 4; ++q) tmem_ld32(ts + q * 32, v[q]);
-        tmem_ld_wait();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_ld_wait(v[q]);
         if (S::kApart) {
           tc_fence_before();
           __syncwarp();
@@ -407,7 +457,7 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
           for (int q = 0; q < DT / 16; ++q) {
             uint32_t o[16];
             tmem_ld16(to + q * 16, o);
-            tmem_ld_wait();
+            tmem_ld_wait(o);
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
             tmem_st16(to + q * 16, o);
@@ -441,17 +491,45 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
         __syncwarp();
         if (lane == 0) mbar_arrive(p_full(t));
       }
-      if (ok) ok = wait_for(o_full(t), S::kApart ? (n - 1) & 1 : 0, abort_flag, status, 41);
+      if (ok && n > 0) ok = wait_for(o_full(t), S::kApart ? (n - 1) & 1 : 0, abort_flag, status, 41);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
-      const float inv = 1.f / l;
       const int h = head_of(t);
+      if (NT == 1 && parts > 1) {                 // the tiles in shared memory have been read
+        float* const sums = reinterpret_cast<float*>(sptr);
+        float* const stats = sums + TC_ROWS * kSumLd<DT>;              // maximum, sum [2][128], then weights [parts][128]
+        float* const weights = stats + 2 * TC_ROWS;
+        static_assert((TC_ROWS * kSumLd<DT> + 10 * TC_ROWS) * 4 <= (NT + 2 * S::kStages) * S::kTile, "sums of a shared block");
+        cg::cluster_group cluster = cg::this_cluster();
+        for (int c0 = 0; c0 < DT; c0 += 32) leave_sums<DT>(sums + r * kSumLd<DT>, to, c0, n > 0);
+        stats[r] = ok ? m : NAN;
+        stats[TC_ROWS + r] = l;
+        __syncwarp();
+        cluster_sync_all();
+        const int r0 = TC_ROWS * part / parts, r1 = TC_ROWS * (part + 1) / parts;
+        if (r >= r0 && r < r1) {
+          float top = -INFINITY, sum = 0.f;
+          for (int p = 0; p < parts; ++p) {
+            const float x = cluster.map_shared_rank(stats, p)[r];
+            top = top != top || x != x ? NAN : fmaxf(top, x);
+          }
+          for (int p = 0; p < parts; ++p) sum += ex2(cluster.map_shared_rank(stats, p)[r] - top) * cluster.map_shared_rank(stats, p)[TC_ROWS + r];
+          for (int p = 0; p < parts; ++p) weights[p * TC_ROWS + r] = ex2(cluster.map_shared_rank(stats, p)[r] - top) / sum;
+          if (a.lse && row < s.len) a.lse[(int64_t)h * a.tokens + s.begin + row] = (top + log2f(sum)) * kLn2;
+        }
+        asm volatile("barrier.cta.sync 1, 128;" ::: "memory");
+        finish_rows<DT>(a.o, s, q0, h, a.dim, sums, part, parts, 128, [&](int at, int p) { return weights[p * TC_ROWS + at]; });
+        __syncwarp();
+        cluster_sync_all();                       // the others have read this block's sums
+      } else {
+      const float inv = 1.f / l;
       if (a.lse && row < s.len) a.lse[(int64_t)h * a.tokens + s.begin + row] = ok ? (m + log2f(l)) * kLn2 : NAN;
       const int first_row = q0 + (warp & 3) * 32;
 #pragma unroll
       for (int q = 0; q < DT / 32; ++q)             // Q's tile has been read
         store_rows(head_row_out<__nv_bfloat16>(a.o, s.begin + first_row, h), a.o.token, s.len - first_row, to, q * 32, a.dim, inv, ok,
                    sptr + t * S::kTile + (warp & 3) * 2048);
+      }
     }
   }
   tc_fence_before();
@@ -504,6 +582,7 @@ template <int DT, int ROWS> __device__ __forceinline__ void copy_rows(uint32_t d
 // 128 x BN x DT product of a resident and a streamed tile
 template <int DT> __device__ __forceinline__ void mma_scores(uint32_t d, uint32_t a, uint32_t b) {
   using S = BwdShape<DT>;
+  a = own_address(a); b = own_address(b);
   const uint64_t base = desc_base(16, 1024);
   const uint32_t idesc = make_idesc_mn(128, S::kCols, 0, 0);
 #pragma unroll
@@ -513,6 +592,7 @@ template <int DT> __device__ __forceinline__ void mma_scores(uint32_t d, uint32_
 // 128 x DT x BN product of factors in tensor memory (16 columns of every 32) and a streamed tile whose rows run along the depth
 template <int DT> __device__ __forceinline__ void mma_gradient(uint32_t d, uint32_t a, uint32_t b, bool accumulate) {
   using S = BwdShape<DT>;
+  b = own_address(b);
   const uint64_t base = desc_base(S::kCols * 128, 1024);
   const uint32_t idesc = make_idesc_mn(128, DT, 0, 1);
 #pragma unroll
@@ -527,7 +607,7 @@ template <int DT> __device__ __forceinline__ void clear_rows(uint8_t* tile, int 
 }
 struct TcBwdMaps { CUtensorMap q, k, v, d_o; };
 
-template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a, const TcBwdMaps& maps, int block) {
+template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a, const TcBwdMaps& maps, int block, int part, int parts) {
   using S = BwdShape<DT>;
   constexpr int BN = S::kCols, kCopy = S::kParts * 4, kIssue = kCopy + 1;        // the warps that copy and issue
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = block % a.kv_heads;
@@ -567,7 +647,9 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
     return;
   }
   const int k0 = s.tile * TC_ROWS, first = a.causal ? k0 : 0;
-  const int per_head = (s.len - first + BN - 1) / BN, n_it = per_head * a.group;
+  // of the query tiles of all heads that share these keys, this block's share
+  const int per_head = (s.len - first + BN - 1) / BN, it0 = per_head * a.group * part / parts, n_it = per_head * a.group * (part + 1) / parts - it0;
+  const int h0 = hk * a.group + it0 / per_head, first_q0 = first + it0 % per_head * BN;
   auto copy_queries = [&](int it, int h, int q0) {
     const int st = it % S::kStages;
     if (elect_one()) {
@@ -577,7 +659,7 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
     }
     __syncwarp();
   };
-  if (warp == kCopy) {
+  if (warp == kCopy && n_it > 0) {
     __syncwarp();
     if (elect_one()) {
       mbar_arrive_expect_tx(kv_full, 2 * S::kTile);
@@ -585,7 +667,7 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
       copy_rows<DT, TC_ROWS>(sV, &maps.v, kv_full, hk, s.begin + k0);
     }
     __syncwarp();
-    copy_queries(0, hk * a.group, first);
+    copy_queries(0, h0, first_q0);
   }
   tc_fence_before();
   __syncthreads();
@@ -593,7 +675,7 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
   const uint32_t tmem = *tmem_slot, col_s = tmem, col_dp = tmem + BN, col_dv = tmem + 2 * BN, col_dk = tmem + 2 * BN + DT;
 
   if (warp == kCopy) {                            // ---- copies
-    int armed = 1, h = hk * a.group, q0 = first;
+    int armed = 1, h = h0, q0 = first_q0;
     bool ok = true;
     pdl_wait();                                   // delta
     for (int it = 0; it < n_it; ++it) {
@@ -625,7 +707,7 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
       q0 += BN;
       if (q0 >= s.len) { q0 = first; ++h; }
     }
-    if (*abort_flag) {                            // nothing may be in flight when the block ends
+    if (*abort_flag && n_it > 0) {                            // nothing may be in flight when the block ends
       volatile int never = 0;
       wait_for(kv_full, 0, &never, status, 53);
       for (int it = max(0, armed - S::kStages); it < armed; ++it) wait_for(full(it % S::kStages), (it / S::kStages) & 1, &never, status, 53);
@@ -635,7 +717,7 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
       const int st = it % S::kStages;
       return wait_for(full(st), (it / S::kStages) & 1, abort_flag, status, 54) && wait_for(row_full(st), (it / S::kStages) & 1, abort_flag, status, 55);
     };
-    bool ok = wait_for(kv_full, 0, abort_flag, status, 56) && ready(0);
+    bool ok = n_it > 0 && wait_for(kv_full, 0, abort_flag, status, 56) && ready(0);
     if (ok) {
       tc_fence_after();
       if (elect_one()) {
@@ -677,7 +759,7 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float c = a.scale * kLog2e;
     bool ok = true;
-    int q0 = first;
+    int q0 = first_q0;
     for (int it = 0; it < n_it; ++it) {
       const int st = it % S::kStages;
       const float* rows = row_values + st * 2 * BN + c0;
@@ -689,7 +771,7 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
       {
         uint32_t v[32], w[16];
         tmem_ld32(col_s + lanes + c0, v);
-        tmem_ld_wait();
+        tmem_ld_wait(v);
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
           const float4 l = *reinterpret_cast<const float4*>(rows + i);
@@ -716,7 +798,7 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
       {
         uint32_t v[32], w[16];
         tmem_ld32(col_dp + lanes + c0, v);
-        tmem_ld_wait();
+        tmem_ld_wait(v);
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
           const float4 d = *reinterpret_cast<const float4*>(rows + BN + i);
@@ -734,15 +816,36 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
       q0 += BN;
       if (q0 >= s.len) q0 = first;
     }
-    if (ok) ok = wait_for(acc_full, 0, abort_flag, status, 62);
+    if (ok && n_it > 0) ok = wait_for(acc_full, 0, abort_flag, status, 62);
     ok = __all_sync(0xffffffffu, ok);
     tc_fence_after();
+    if (parts > 1) {                              // the tiles in shared memory have been read
+      float* const dk = reinterpret_cast<float*>(sptr);
+      float* const dv = dk + TC_ROWS * kSumLd<DT>;
+      static_assert(2 * TC_ROWS * kSumLd<DT> * 4 <= 2 * S::kTile + 2 * S::kStages * S::kStream, "sums of a shared block");
+      const int r = threadIdx.x & 127;
+      leave_sums<DT>(dk + r * kSumLd<DT>, col_dk + lanes, c0, n_it > 0);
+      leave_sums<DT>(dv + r * kSumLd<DT>, col_dv + lanes, c0, n_it > 0);
+      if (!ok) dk[r * kSumLd<DT> + c0] = dv[r * kSumLd<DT> + c0] = NAN;
+      __syncwarp();
+      cluster_sync_all();
+      finish_rows<DT>(a.dk, s, k0, hk, a.dim, dk, part, parts, S::kParts * 128, [&](int, int) { return a.scale; });
+      finish_rows<DT>(a.dv, s, k0, hk, a.dim, dv, part, parts, S::kParts * 128, [&](int, int) { return 1.f; });
+      __syncwarp();
+      cluster_sync_all();                         // the others have read this block's sums
+    } else {
     const int first_row = k0 + (warp & 3) * 32;
     uint8_t* const stage = sptr + (sQ - base) + warp * 2048;           // the streamed tiles have been read
     static_assert(DT == S::kParts * 32, "a part of the threads stores 32 columns of each gradient");
     static_assert(S::kParts * 4 * 2048 <= 2 * S::kStages * S::kStream, "staging");
     store_rows(head_row_out<__nv_bfloat16>(a.dv, s.begin + first_row, hk), a.dv.token, s.len - first_row, col_dv + lanes, c0, a.dim, 1.f, ok, stage);
     store_rows(head_row_out<__nv_bfloat16>(a.dk, s.begin + first_row, hk), a.dk.token, s.len - first_row, col_dk + lanes, c0, a.dim, a.scale, ok, stage);
+    }
+  }
+  if (parts > 1 && warp >= kCopy) {
+    __syncwarp();
+    cluster_sync_all();
+    cluster_sync_all();
   }
   tc_fence_before();
   __syncthreads();
@@ -752,7 +855,7 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
   }
 }
 
-template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, const TcBwdMaps& maps, int block) {
+template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, const TcBwdMaps& maps, int block, int part, int parts) {
   using S = BwdShape<DT>;
   constexpr int BN = S::kCols, kCopy = S::kParts * 4, kIssue = kCopy + 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = block % a.heads, hk = h / a.group;
@@ -789,17 +892,18 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
     return;
   }
   const int tile = (s.len + TC_ROWS - 1) / TC_ROWS - 1 - s.tile;                 // the tiles that see the most keys first
-  const int q0 = tile * TC_ROWS, n_it = ((a.causal ? min(s.len, q0 + TC_ROWS) : s.len) + BN - 1) / BN;
+  const int q0 = tile * TC_ROWS, all = ((a.causal ? min(s.len, q0 + TC_ROWS) : s.len) + BN - 1) / BN;
+  const int it0 = all * part / parts, n_it = all * (part + 1) / parts - it0;     // of the key tiles, this block's share
   auto copy_keys = [&](int it) {
     const int st = it % S::kStages;
     if (elect_one()) {
       mbar_arrive_expect_tx(full(st), 2 * S::kStream);
-      copy_rows<DT, BN>(sK + st * S::kStream, &maps.k, full(st), hk, s.begin + it * BN);
-      copy_rows<DT, BN>(sV + st * S::kStream, &maps.v, full(st), hk, s.begin + it * BN);
+      copy_rows<DT, BN>(sK + st * S::kStream, &maps.k, full(st), hk, s.begin + (it0 + it) * BN);
+      copy_rows<DT, BN>(sV + st * S::kStream, &maps.v, full(st), hk, s.begin + (it0 + it) * BN);
     }
     __syncwarp();
   };
-  if (warp == kCopy) {
+  if (warp == kCopy && n_it > 0) {
     __syncwarp();
     if (elect_one()) {
       mbar_arrive_expect_tx(q_full, 2 * S::kTile);
@@ -818,7 +922,7 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
     int armed = 1;
     bool ok = true;
     for (int it = 0; it < n_it; ++it) {
-      const int st = it % S::kStages, k0 = it * BN;
+      const int st = it % S::kStages, k0 = (it0 + it) * BN;
       if (it >= S::kStages) ok = wait_for(empty(st), (it / S::kStages - 1) & 1, abort_flag, status, 71);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
@@ -835,7 +939,7 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
       }
       mbar_arrive(cleared(st));
     }
-    if (*abort_flag) {                            // nothing may be in flight when the block ends
+    if (*abort_flag && n_it > 0) {                            // nothing may be in flight when the block ends
       volatile int never = 0;
       wait_for(q_full, 0, &never, status, 73);
       for (int it = max(0, armed - S::kStages); it < armed; ++it) wait_for(full(it % S::kStages), (it / S::kStages) & 1, &never, status, 73);
@@ -845,7 +949,7 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
       const int st = it % S::kStages;
       return wait_for(full(st), (it / S::kStages) & 1, abort_flag, status, 74) && wait_for(cleared(st), (it / S::kStages) & 1, abort_flag, status, 75);
     };
-    bool ok = wait_for(q_full, 0, abort_flag, status, 76) && ready(0) && (n_it < 2 || ready(1));
+    bool ok = n_it > 0 && wait_for(q_full, 0, abort_flag, status, 76) && ready(0) && (n_it < 2 || ready(1));
     if (ok) {
       tc_fence_after();
       if (elect_one()) {
@@ -887,7 +991,7 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
     const int limit = a.causal ? min(s.len, row + 1) : s.len;
     bool ok = true;
     for (int it = 0; it < n_it; ++it) {
-      const int k0 = it * BN;
+      const int k0 = (it0 + it) * BN;
       ok = wait_for(s_full + 8 * (it & 1), (it >> 1) & 1, abort_flag, status, 78);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
@@ -895,7 +999,7 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
       float p[32];
       uint32_t v[32], w[16];
       tmem_ld32(col_s + lanes + (it & 1) * BN + c0, v);
-      tmem_ld_wait();
+      tmem_ld_wait(v);
 #pragma unroll
       for (int i = 0; i < 32; i += 2) {
         const float2 x = fma_f32x2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(c, c), make_float2(-lse, -lse));
@@ -906,7 +1010,7 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
       if (!ok) break;
       tc_fence_after();
       tmem_ld32(col_dp + lanes + c0, v);
-      tmem_ld_wait();
+      tmem_ld_wait(v);
 #pragma unroll
       for (int i = 0; i < 32; i += 2) {
         const float2 x = add_f32x2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(-delta, -delta));
@@ -924,12 +1028,29 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
       __syncwarp();
       if (lane == 0) mbar_arrive(ds_full);
     }
-    if (ok) ok = wait_for(acc_full, 0, abort_flag, status, 80);
+    if (ok && n_it > 0) ok = wait_for(acc_full, 0, abort_flag, status, 80);
     ok = __all_sync(0xffffffffu, ok);
     tc_fence_after();
+    if (parts > 1) {                              // the tiles in shared memory have been read
+      float* const sums = reinterpret_cast<float*>(sptr);
+      const int r = threadIdx.x & 127;
+      leave_sums<DT>(sums + r * kSumLd<DT>, col_dq + lanes, c0, n_it > 0);
+      if (!ok) sums[r * kSumLd<DT> + c0] = NAN;
+      __syncwarp();
+      cluster_sync_all();
+      finish_rows<DT>(a.dq, s, q0, h, a.dim, sums, part, parts, S::kParts * 128, [&](int, int) { return a.scale; });
+      __syncwarp();
+      cluster_sync_all();                         // the others have read this block's sums
+    } else {
     const int first_row = q0 + (warp & 3) * 32;
     store_rows(head_row_out<__nv_bfloat16>(a.dq, s.begin + first_row, h), a.dq.token, s.len - first_row, col_dq + lanes, c0, a.dim, a.scale, ok,
                sptr + (sK - base) + warp * 2048);                      // the streamed tiles have been read
+    }
+  }
+  if (parts > 1 && warp >= kCopy) {
+    __syncwarp();
+    cluster_sync_all();
+    cluster_sync_all();
   }
   tc_fence_before();
   __syncthreads();
@@ -943,8 +1064,9 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
 template <int DT>
 __global__ void __launch_bounds__(BwdShape<DT>::kThreads, BwdShape<DT>::kBlocks)
 attn_packed_bwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcBwdMaps maps, int dkv_blocks) {
-  if ((int)blockIdx.x < dkv_blocks) dkv_block<DT>(a, maps, blockIdx.x);
-  else dq_block<DT>(a, maps, blockIdx.x - dkv_blocks);
+  const int parts = (int)cg::this_cluster().num_blocks(), part = (int)cg::this_cluster().block_rank(), block = blockIdx.x / parts;
+  if (block < dkv_blocks) dkv_block<DT>(a, maps, block, part, parts);
+  else dq_block<DT>(a, maps, block - dkv_blocks, part, parts);
 }
 
 
@@ -986,6 +1108,12 @@ __global__ void __launch_bounds__(256) attn_packed_delta_tc_kernel(const __grid_
   }
 }
 
+#ifndef FP_BLOCKS
+#define FP_BLOCKS 296
+#define FP_LEAST 3
+#define BP_BLOCKS 592
+#define BP_LEAST 4
+#endif
 // ---- host side --------------------------------------------------------------------------------------------------
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -1052,14 +1180,17 @@ template <int DT, int NT> static cudaError_t fwd_launch(const PackedArgs& a, cud
   if (e != cudaSuccess) return e;
   const int pair = NT == 2 && a.group % 2 == 0, units = pair ? a.heads / 2 : a.heads;
   const int64_t blocks = most_tiles(a.tokens, a.n_seqs, pair ? TC_ROWS : NT * TC_ROWS) * units;
-  if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-  return launch_pdl(attn_packed_fwd_tc_kernel<DT, NT>, dim3((unsigned)blocks), dim3(S::kThreads), S::kSmem, st, false, a, maps, units, pair);
+  const int parts = NT == 1 ? packed_parts(blocks, a, TC_ROWS, 1, FP_BLOCKS, FP_LEAST) : 1;
+  return launch_clusters(attn_packed_fwd_tc_kernel<DT, NT>, blocks, S::kThreads, S::kSmem, st, false, parts, a, maps, units, pair);
 }
 
+// Two query tiles to a block read keys and values half as often and pay for heads of 128 once every SM has such a block.  8192 tokens,
+// 16 heads of 128, us with two / one: 240 / 252; 4000 tokens, 4 heads of 128: 68 / 63; 8192 tokens, 16 heads of 64: 213 / 205.
 cudaError_t attn_packed_tc_forward(const PackedArgs& a, cudaStream_t st) {
-  const bool two = a.tokens >= (int64_t)512 * a.n_seqs;
-  if (a.dim <= 64) return two ? fwd_launch<64, 2>(a, st) : fwd_launch<64, 1>(a, st);
-  return two ? fwd_launch<128, 2>(a, st) : fwd_launch<128, 1>(a, st);
+  if (a.dim <= 64) return fwd_launch<64, 1>(a, st);
+  const bool pair = a.group % 2 == 0;
+  const int64_t blocks = most_tiles(a.tokens, a.n_seqs, pair ? TC_ROWS : 2 * TC_ROWS) * (pair ? a.heads / 2 : a.heads);
+  return blocks >= kSms ? fwd_launch<128, 2>(a, st) : fwd_launch<128, 1>(a, st);
 }
 
 template <int DT> static cudaError_t bwd_launch(const PackedArgs& a, cudaStream_t st) {
@@ -1072,13 +1203,12 @@ template <int DT> static cudaError_t bwd_launch(const PackedArgs& a, cudaStream_
   if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.tokens, S::kCols);
   if (e == cudaSuccess) e = encode_heads(&maps.d_o, a.d_o, a.dim, a.heads, a.tokens, S::kCols);
   if (e != cudaSuccess) return e;
-  const int64_t tiles = most_tiles(a.tokens, a.n_seqs, TC_ROWS);
-  if (tiles * (a.heads + a.kv_heads) > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  const int64_t tiles = most_tiles(a.tokens, a.n_seqs, TC_ROWS), blocks = tiles * (a.heads + a.kv_heads);
   e = launch_pdl(attn_packed_delta_tc_kernel, dim3((unsigned)((a.tokens + 32 * DELTA_R - 1) / (32 * DELTA_R)), a.heads), dim3(256), 0, st, false, a);
   // starts beside the first's last blocks; its own wait for them before they read delta
   if (e == cudaSuccess)
-    e = launch_pdl(attn_packed_bwd_tc_kernel<DT>, dim3((unsigned)(tiles * (a.heads + a.kv_heads))), dim3(S::kThreads), S::kSmem, st, true, a, maps,
-                   (int)(tiles * a.kv_heads));
+    e = launch_clusters(attn_packed_bwd_tc_kernel<DT>, blocks, S::kThreads, S::kSmem, st, true,
+                        packed_parts(blocks, a, S::kCols, a.group, BP_BLOCKS, BP_LEAST), a, maps, (int)(tiles * a.kv_heads));
   return e;
 }
 cudaError_t attn_packed_tc_backward(const PackedArgs& a, cudaStream_t st) { return a.dim <= 64 ? bwd_launch<64>(a, st) : bwd_launch<128>(a, st); }

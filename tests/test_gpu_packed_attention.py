@@ -86,6 +86,15 @@ def test_many_heads(cuda_device, D, dtype):
     check(*make([130, 257, 64], 40, 8, D, dtype, cuda_device, seed=D))
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("lens,H,K,D", [([2000], 2, 1, 64), ([1500, 3], 1, 1, 64), ([1300], 2, 2, 128), ([1, 900], 4, 1, 120), ([700], 1, 1, 33),
+                                        ([3000], 1, 1, 8)], ids=str)
+def test_few_blocks(cuda_device, lens, H, K, D, dtype, causal):
+    """Long sequences and few heads: blocks share the work of one."""
+    check(*make(lens, H, K, D, dtype, cuda_device, causal=causal, first=3, tail=50, seed=len(lens) + D))
+
+
 @pytest.mark.parametrize("dtype", [BF, F])
 def test_many_sequences(cuda_device, dtype):
     lens = [(7 * i) % 23 for i in range(300)]                # more sequences than one round of the tile search takes, empty ones too
