@@ -501,6 +501,14 @@ static pm_status pk_view(HeadView& out, const pm_head_view* v, const char* name,
   out = HeadView{v->data, v->token_stride, v->head_stride};
   return PM_OK;
 }
+// what is written may not be one of the other tensors
+static pm_status pk_apart(const HeadView* const* written, int n_written, const HeadView* const* read, int n_read) {
+  for (int i = 0; i < n_written; ++i) {
+    for (int j = 0; j < n_read; ++j) if (written[i]->data == read[j]->data) return ops_fail(PM_ERR_INVALID_ARG, "an output is one of the inputs");
+    for (int j = 0; j < i; ++j) if (written[i]->data == written[j]->data) return ops_fail(PM_ERR_INVALID_ARG, "two outputs are the same tensor");
+  }
+  return PM_OK;
+}
 static PackedArgs pk_args(const pm_attention_desc* d, const int32_t* cu, float* lse) {
   PackedArgs a{};
   a.cu = cu; a.lse = lse; a.tokens = d->n_tokens; a.n_seqs = d->n_seqs; a.heads = d->n_heads; a.kv_heads = d->n_kv_heads;
@@ -525,6 +533,8 @@ pm_status pm_attention_packed_forward(const pm_attention_desc* d, const pm_head_
   if (const pm_status s = pk_view(a.k, k, "k", size)) return s;
   if (const pm_status s = pk_view(a.v, v, "v", size)) return s;
   if (const pm_status s = pk_view(a.o, o, "o", size)) return s;
+  const HeadView *written[] = {&a.o}, *read[] = {&a.q, &a.k, &a.v};
+  if (const pm_status s = pk_apart(written, 1, read, 3)) return s;
   const cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t e = attn_packed_tc_takes(a, d->dtype, false) ? attn_packed_tc_forward(a, st)
                         : d->dtype == PM_BF16 ? pk_run<__nv_bfloat16>(a, false, st) : pk_run<float>(a, false, st);
@@ -552,6 +562,8 @@ pm_status pm_attention_packed_backward(const pm_attention_desc* d, const pm_head
   if (const pm_status s = pk_view(a.dq, dq, "dq", size)) return s;
   if (const pm_status s = pk_view(a.dk, dk, "dk", size)) return s;
   if (const pm_status s = pk_view(a.dv, dv, "dv", size)) return s;
+  const HeadView *written[] = {&a.dq, &a.dk, &a.dv}, *read[] = {&a.q, &a.k, &a.v, &a.o, &a.d_o};
+  if (const pm_status s = pk_apart(written, 3, read, 5)) return s;
   const uint64_t need = pm_attention_packed_workspace_bytes(d);
   if (!workspace || workspace_bytes < need) return ops_fail(PM_ERR_NOMEM, "workspace too small: need %llu bytes", (unsigned long long)need);
   if (!aligned_to(workspace, 4)) return ops_fail(PM_ERR_INVALID_ARG, "workspace must be 4-byte aligned");

@@ -102,7 +102,10 @@ inline cudaError_t launch_clusters(void (*kernel)(K...), int64_t blocks, int thr
 }
 
 // Blocks that share the work of one: as many as leave no more than `most` in the launch (whose size is the most that the lengths can
-// make), as long as each keeps `least` streamed tiles of `rows` rows of `heads` heads in a sequence of average length.
+// make), as long as each keeps `least` streamed tiles of `rows` rows of `heads` heads in a sequence of average length.  us shared /
+// not: bf16, 2000 tokens, 2 heads of 64 on 1, forward 18 / 27, backward 35 / 76; 4000 tokens, 4 heads of 128, forward 45 / 63; 2 x 1000
+// tokens, 8 heads of 128 on 2, backward 49 / 70; fp32, 700 + 300 + 13 tokens, 4 heads of 128 on 2, both 205 / 305; 493 tokens in 7, 4
+// heads of 32 on 2, both 27 / 31.  Finer parts lose: the backward pass of the 2 x 1000 tokens in eight parts takes 80.
 inline int packed_parts(int64_t blocks, const PackedArgs& a, int rows, int heads, int most, int least) {
   const int64_t average = (a.tokens + a.n_seqs - 1) / a.n_seqs, tiles = (average + rows - 1) / rows * heads;
   int parts = 1;

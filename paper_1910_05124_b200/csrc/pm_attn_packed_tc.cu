@@ -1108,12 +1108,6 @@ __global__ void __launch_bounds__(256) attn_packed_delta_tc_kernel(const __grid_
   }
 }
 
-#ifndef FP_BLOCKS
-#define FP_BLOCKS 296
-#define FP_LEAST 3
-#define BP_BLOCKS 592
-#define BP_LEAST 4
-#endif
 // ---- host side --------------------------------------------------------------------------------------------------
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -1180,7 +1174,7 @@ template <int DT, int NT> static cudaError_t fwd_launch(const PackedArgs& a, cud
   if (e != cudaSuccess) return e;
   const int pair = NT == 2 && a.group % 2 == 0, units = pair ? a.heads / 2 : a.heads;
   const int64_t blocks = most_tiles(a.tokens, a.n_seqs, pair ? TC_ROWS : NT * TC_ROWS) * units;
-  const int parts = NT == 1 ? packed_parts(blocks, a, TC_ROWS, 1, FP_BLOCKS, FP_LEAST) : 1;
+  const int parts = NT == 1 ? packed_parts(blocks, a, TC_ROWS, 1, 2 * kSms, 3) : 1;
   return launch_clusters(attn_packed_fwd_tc_kernel<DT, NT>, blocks, S::kThreads, S::kSmem, st, false, parts, a, maps, units, pair);
 }
 
@@ -1208,7 +1202,7 @@ template <int DT> static cudaError_t bwd_launch(const PackedArgs& a, cudaStream_
   // starts beside the first's last blocks; its own wait for them before they read delta
   if (e == cudaSuccess)
     e = launch_clusters(attn_packed_bwd_tc_kernel<DT>, blocks, S::kThreads, S::kSmem, st, true,
-                        packed_parts(blocks, a, S::kCols, a.group, BP_BLOCKS, BP_LEAST), a, maps, (int)(tiles * a.kv_heads));
+                        packed_parts(blocks, a, S::kCols, a.group, 4 * kSms, 4), a, maps, (int)(tiles * a.kv_heads));
   return e;
 }
 cudaError_t attn_packed_tc_backward(const PackedArgs& a, cudaStream_t st) { return a.dim <= 64 ? bwd_launch<64>(a, st) : bwd_launch<128>(a, st); }

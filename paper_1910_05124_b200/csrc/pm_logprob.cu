@@ -593,6 +593,10 @@ pm_status pm_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int
   if ((targets == nullptr) != (logprob == nullptr)) return ops_fail(PM_ERR_INVALID_ARG, "targets and logprob are given together or not at all");
   if (top_k < 0 || top_k > kLpMaxK || top_k > vocab) return ops_fail(PM_ERR_INVALID_ARG, "top_k must be 0 to 32 and at most the vocabulary size");
   if (top_k > 0 && (!top_logprob || !top_ids)) return ops_fail(PM_ERR_INVALID_ARG, "top_k without a place for the alternatives");
+  const void* outs[] = {logprob, entropy, lse, top_k > 0 ? top_logprob : nullptr, top_k > 0 ? top_ids : nullptr};
+  for (int i = 0; i < 5; ++i)
+    for (int j = 0; j < i; ++j)
+      if (outs[i] && outs[i] == outs[j]) return ops_fail(PM_ERR_INVALID_ARG, "two results share their memory");
   // A cluster per row once the rows leave SMs without work, as long as each block keeps some vectors per thread.
   const int vectors = vocab / (dtype == PM_BF16 ? 8 : 4);
   int parts = 1;

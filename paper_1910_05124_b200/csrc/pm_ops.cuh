@@ -7,7 +7,9 @@ namespace pm {
 // Sets the message that pm_last_error(NULL) returns to this thread; never throws.
 pm_status ops_fail(pm_status s, const char* format, ...) noexcept;
 inline pm_status ops_cuda(cudaError_t e, const char* what) noexcept {
-  return e == cudaSuccess ? PM_OK : ops_fail(PM_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+  if (e == cudaSuccess) return PM_OK;
+  cudaGetLastError();                             // reported here: not left for whoever asks the runtime next
+  return ops_fail(PM_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 inline bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 

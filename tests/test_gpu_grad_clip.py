@@ -111,6 +111,13 @@ def test_nothing_and_not_finite(cuda_device):
                 assert torch.equal(torch.nan_to_num(out, nan=3.0), torch.nan_to_num(keep, nan=3.0))
 
 
+def test_more_than_32_bits_of_elements(cuda_device):
+    g = torch.zeros(2 ** 32 + 77, dtype=BF, device=cuda_device)
+    g[5], g[2 ** 31 + 1], g[-1] = 2.0, 4.0, 4.0
+    assert run([g], 3.0) == (6.0, 0.5)
+    assert (g[5], g[2 ** 31 + 1], g[-1]) == (1.0, 2.0, 2.0) and int(torch.count_nonzero(g)) == 3
+
+
 def test_same_bits_streams_and_graphs(cuda_device):
     import paper_1910_05124_b200 as pm
     g = make([300000, 7, 123456], [F, BF], cuda_device, seed=4)

@@ -272,6 +272,25 @@ def test_captured_and_on_two_streams(cuda_device, dtype):
     within(o, wo, bo, "o of other lengths")
 
 
+@pytest.mark.parametrize("D", [64, 33])
+def test_offsets_beyond_32_bits(cuda_device, D):
+    """Rows 2^25 elements apart: the last of 130 lies 4.3 billion elements behind the first."""
+    op, q, k, v, d_o, cu = make([130], 1, 1, D, BF, cuda_device, seed=11)
+    far = torch.empty(129 * 2 ** 25 + D, dtype=BF, device=cuda_device).as_strided((130, 1, D), (2 ** 25, D, 1))
+    for name in ("q", "k", "v"):
+        x = dict(q=q, k=k, v=v)
+        far.copy_(x[name])
+        x[name] = far
+        o, lse = forward(op, **x, cu=cu)
+        wo, wl, bo, bl = R.attention_forward(q, k, v, cu, op.scale, True, BF)
+        within(o, wo, bo, "o")
+    g = [torch.zeros_like(x) for x in (q, k, v)]
+    want = R.attention_backward(q, k, v, o, lse, d_o, cu, op.scale, True, BF)
+    op.pm_attention_packed_backward(q, k, v, o, lse, d_o, cu, g[0], g[1], far)
+    within(far, *want["dv"], "dv")
+    op.pm_attention_packed_status()
+
+
 def test_python_refusals(cuda_device):
     import paper_1910_05124_b200 as pm
     op, q, k, v, d_o, cu = make([30, 20], 4, 2, 64, BF, cuda_device)

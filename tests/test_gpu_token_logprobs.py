@@ -170,6 +170,19 @@ def test_strides_and_alignment(cuda_device, dtype):
                 assert (buf[:, :at] == 9.0).all() and (buf[:, at + v:] == 9.0).all()
 
 
+def test_offsets_beyond_32_bits(cuda_device):
+    """Rows 2^28 elements apart, 20 of them, within one tensor."""
+    import paper_1910_05124_b200 as pm
+    x, y, gl, gh = make(20, 700, BF, cuda_device, seed=3)
+    far = torch.empty(19 * 2 ** 28 + 700, dtype=BF, device=cuda_device).as_strided((20, 700), (2 ** 28, 1))
+    far.copy_(x)
+    got = check(far, y, 4)
+    op, ref = pm.TokenLogProbs(700), torch.zeros_like(x)
+    op.pm_token_logprobs_backward(x, y, got["lse"], ref, d_logprob=gl)
+    op.pm_token_logprobs_backward(far, y, got["lse"], far, d_logprob=gl)
+    assert torch.equal(far, ref)
+
+
 def test_optional_results_streams_and_graphs(cuda_device):
     import paper_1910_05124_b200 as pm
     x, y, gl, gh = make(20, 3000, F, cuda_device)

@@ -28,7 +28,7 @@ def view(data=P, token=64, head=8):
 
 def attn(L, desc, *, q=None, cu=P, o=None):
     v = view()
-    return L.pm_attention_packed_forward(C.byref(desc), q or v, v, v, cu, o or v, None, None)
+    return L.pm_attention_packed_forward(C.byref(desc), q or v, v, v, cu, o or view(data=2 * P), None, None)
 
 
 def desc(**kw):
@@ -55,6 +55,8 @@ def test_attention_pointers(L):
     assert status(L, attn(L, desc(), q=view(data=P + 2)))[0] == "PM_ERR_INVALID_ARG"       # fp32 at an odd half-word
     assert status(L, attn(L, desc(), q=view(token=-64)))[0] == "PM_ERR_INVALID_ARG"
     assert status(L, attn(L, desc(), o=view(data=None)))[0] == "PM_ERR_INVALID_ARG"
+    st, msg = status(L, attn(L, desc(), o=view()))
+    assert st == "PM_ERR_INVALID_ARG" and "output" in msg
     # nothing to do: no pointer is looked at
     assert L.pm_attention_packed_forward(C.byref(desc(n_tokens=0)), None, None, None, None, None, None, None) == 0
     assert L.pm_attention_packed_forward(C.byref(desc(n_seqs=0)), None, None, None, None, None, None, None) == 0
@@ -67,8 +69,11 @@ def test_attention_backward_workspace(L):
     assert L.pm_attention_packed_workspace_bytes(None) == 0
     v = [view()] * 4
 
-    def call(lse=P, ws=P, n=need):
-        return status(L, L.pm_attention_packed_backward(C.byref(d), *v, lse, view(), P, view(), view(), view(), ws, n, None))
+    out = [view(data=i * P) for i in (2, 3, 4)]
+
+    def call(lse=P, ws=P, n=need, out=out):
+        return status(L, L.pm_attention_packed_backward(C.byref(d), *v, lse, view(), P, *out, ws, n, None))
+    assert "input" in call(out=[view()] + out[1:])[1] and "same" in call(out=[out[0], out[1], out[0]])[1]
     assert call(lse=None)[0] == "PM_ERR_INVALID_ARG"
     assert call(ws=None)[0] == "PM_ERR_NOMEM"
     st, msg = call(n=need - 1)
@@ -87,7 +92,8 @@ def lp(L, **kw):
     (dict(vocab=(1 << 24) + 1, stride=1 << 25), "PM_ERR_SHAPE"), (dict(rows=(1 << 24) + 1), "PM_ERR_SHAPE"), (dict(stride=9), "PM_ERR_INVALID_ARG"),
     (dict(logits=None), "PM_ERR_INVALID_ARG"), (dict(logits=P + 2), "PM_ERR_INVALID_ARG"), (dict(logprob=None), "PM_ERR_INVALID_ARG"),
     (dict(targets=None), "PM_ERR_INVALID_ARG"), (dict(k=11, top=P, ids=P), "PM_ERR_INVALID_ARG"), (dict(k=-1), "PM_ERR_INVALID_ARG"),
-    (dict(vocab=100, stride=100, k=33, top=P, ids=P), "PM_ERR_INVALID_ARG"), (dict(k=2, ids=P), "PM_ERR_INVALID_ARG"), (dict(rows=0), "PM_OK")])
+    (dict(vocab=100, stride=100, k=33, top=P, ids=P), "PM_ERR_INVALID_ARG"), (dict(k=2, ids=P), "PM_ERR_INVALID_ARG"), (dict(lse=P), "PM_ERR_INVALID_ARG"),
+    (dict(entropy=2 * P, lse=2 * P), "PM_ERR_INVALID_ARG"), (dict(rows=0), "PM_OK")])
 def test_logprob_arguments(L, kw, code):
     assert lp(L, **kw) == code
 
