@@ -81,10 +81,10 @@ __device__ __forceinline__ Sums join(Sums a, Sums b) {
 }
 __device__ __forceinline__ bool beats(float v, int id, float w, int other) { return v > w || (v == w && id < other); }
 
-struct LpShared {
-  Sums warp[kLpWarps];
+template <int THREADS> struct LpShared {
+  Sums warp[THREADS / 32];
   Sums block[kLpMaxCluster];                      // of the cluster's blocks, in its first
-  float lane_max[kLpWarps][32];
+  float lane_max[THREADS / 32][32];
   float threshold;
   int n_list;
   float list_v[kLpList];
@@ -152,8 +152,8 @@ __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // The k best of the block's vectors [j0, j1) in order into sh.top_*: value descending, then index ascending.  `mine` is the largest
-// value of the thread's own vectors j0 + threadIdx.x, + kLpThreads, ...  Missing entries are (-infinity, vocab).
-template <typename T> __device__ void block_top(LpShared& sh, const RowVectors<T>& x, int j0, int j1, int k, float mine) {
+// value of the thread's own vectors j0 + threadIdx.x, + THREADS, ...  Missing entries are (-infinity, vocab).
+template <int THREADS, typename T> __device__ void block_top(LpShared<THREADS>& sh, const RowVectors<T>& x, int j0, int j1, int k, float mine) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   sh.lane_max[warp][lane] = mine;
   if (tid == 0) sh.n_list = 0;
@@ -162,7 +162,7 @@ template <typename T> __device__ void block_top(LpShared& sh, const RowVectors<T
   if (warp == 0) {
     float v = sh.lane_max[0][lane];
 #pragma unroll
-    for (int w = 1; w < kLpWarps; ++w) v = fmaxf(v, sh.lane_max[w][lane]);
+    for (int w = 1; w < THREADS / 32; ++w) v = fmaxf(v, sh.lane_max[w][lane]);
     const float th = __shfl_sync(0xffffffffu, sorted_down(v), k - 1);
     if (lane == 0) sh.threshold = th;
   }
@@ -173,7 +173,7 @@ template <typename T> __device__ void block_top(LpShared& sh, const RowVectors<T
   while (hit) {
     const int who = __ffs(hit) - 1;
     hit &= hit - 1;
-    for (int j = j0 + warp * 32 + who + lane * kLpThreads; j < j1; j += 32 * kLpThreads) {
+    for (int j = j0 + warp * 32 + who + lane * THREADS; j < j1; j += 32 * THREADS) {
       float v[Vec<T>::n];
       x.get(j, v);
 #pragma unroll
@@ -189,7 +189,7 @@ template <typename T> __device__ void block_top(LpShared& sh, const RowVectors<T
   __syncthreads();
   const int n = sh.n_list;
   if (n <= kLpList) {
-    for (int a = tid; a < n; a += kLpThreads) {
+    for (int a = tid; a < n; a += THREADS) {
       const float v = sh.list_v[a];
       const int id = sh.list_id[a];
       int rank = 0;
@@ -204,12 +204,12 @@ template <typename T> __device__ void block_top(LpShared& sh, const RowVectors<T
   for (int r = 0; r < k; ++r) {                    // the best of what comes after the last one found
     float bv = -INFINITY;
     int bid = x.vocab;
-    for (int j = j0 + tid; j < j1; j += kLpThreads) best_after(x, j, last_v, last_id, bv, bid);
+    for (int j = j0 + tid; j < j1; j += THREADS) best_after(x, j, last_v, last_id, bv, bid);
     warp_best(bv, bid);
     if (lane == 0) { sh.list_v[warp] = bv; sh.list_id[warp] = bid; }
     __syncthreads();
     bv = sh.list_v[0]; bid = sh.list_id[0];
-    for (int w = 1; w < kLpWarps; ++w) if (beats(sh.list_v[w], sh.list_id[w], bv, bid)) { bv = sh.list_v[w]; bid = sh.list_id[w]; }
+    for (int w = 1; w < THREADS / 32; ++w) if (beats(sh.list_v[w], sh.list_id[w], bv, bid)) { bv = sh.list_v[w]; bid = sh.list_id[w]; }
     if (tid == 0) { sh.top_v[r] = bv; sh.top_id[r] = bid; }
     last_v = bv; last_id = bid;
     __syncthreads();
@@ -271,11 +271,11 @@ template <typename T, bool ENTROPY, int U> __device__ __forceinline__ void take(
   if (ENTROPY) st.t += t.x + t.y;
 }
 
-// Six blocks to an SM: the end of a row (joining the sums, ranking the alternatives) is a chain of short steps that the other blocks'
+// 1536 threads to an SM, in six blocks or twelve: the end of a row (joining the sums, ranking the alternatives) is a chain of short steps that the other blocks'
 // loads run beside.
-template <typename T, bool TOP, bool ENTROPY>
-__global__ void __launch_bounds__(kLpThreads, 6) logprob_kernel(LogprobArgs a) {
-  __shared__ LpShared sh;
+template <typename T, int THREADS, bool TOP, bool ENTROPY>
+__global__ void __launch_bounds__(THREADS, 1536 / THREADS) logprob_kernel(LogprobArgs a) {
+  __shared__ LpShared<THREADS> sh;
   constexpr int U = 4;
   cg::cluster_group cluster = cg::this_cluster();
   const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
@@ -287,11 +287,11 @@ __global__ void __launch_bounds__(kLpThreads, 6) logprob_kernel(LogprobArgs a) {
 
   Sums st{-INFINITY, 0.f, 0.f};
   const uint32_t none2 = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;   // -infinity, or two of them
-  for (int j = j0 + tid; j < j1; j += U * kLpThreads) {
+  for (int j = j0 + tid; j < j1; j += U * THREADS) {
     uint4 q[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int at = j + u * kLpThreads;
+      const int at = j + u * THREADS;
       q[u] = at < j1 && x.whole(at) ? x.load(at) : make_uint4(none2, none2, none2, none2);
     }
     take<T, ENTROPY>(st, q);
@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(kLpThreads, 6) logprob_kernel(LogprobArgs a) {
   // the vectors that reach over the row's ends, by the threads whose turn they are
   for (int e = 0; e < 2; ++e) {
     const int j = e ? x.count - 1 : 0;
-    if (j < j0 || j >= j1 || (j - j0) % kLpThreads != tid || x.whole(j) || (e && x.count == 1)) continue;
+    if (j < j0 || j >= j1 || (j - j0) % THREADS != tid || x.whole(j) || (e && x.count == 1)) continue;
     float v[Vec<T>::n];
     x.get(j, v);
 #pragma unroll
@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(kLpThreads, 6) logprob_kernel(LogprobArgs a) {
     cluster_wait();                               // all blocks have begun
     if (tid == 0) {
       st = sh.warp[0];
-      for (int w = 1; w < kLpWarps; ++w) st = join(st, sh.warp[w]);
+      for (int w = 1; w < THREADS / 32; ++w) st = join(st, sh.warp[w]);
       *cluster.map_shared_rank(&sh.block[part], 0) = st;
     }
     if (TOP && tid < a.top_k) {
@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(kLpThreads, 6) logprob_kernel(LogprobArgs a) {
     for (int c = 1; c < parts; ++c) st = join(st, sh.block[c]);
   } else {
     st = sh.warp[0];
-    for (int w = 1; w < kLpWarps; ++w) st = join(st, sh.warp[w]);
+    for (int w = 1; w < THREADS / 32; ++w) st = join(st, sh.warp[w]);
   }
   const RowResult r(st);
   if (tid == 0) r.write<T>(a, x, row);
@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(kLpThreads, 6) logprob_kernel(LogprobArgs a) {
     const int k = a.top_k, n = parts * k;
     const float* bv = parts > 1 ? sh.all_v : sh.top_v;
     const int* bid = parts > 1 ? sh.all_id : sh.top_id;
-    for (int i = tid; i < n; i += kLpThreads) {
+    for (int i = tid; i < n; i += THREADS) {
       int rank = i;
       if (parts > 1) {
         // entries of blocks with fewer than k elements are equal among themselves and come behind every element
@@ -552,22 +552,28 @@ __global__ void __launch_bounds__(kLpThreads) logprob_bwd_kernel(LogprobBwdArgs 
   }
 }
 
+template <typename T, int THREADS> static cudaError_t logprob_launch_rows(const LogprobArgs& a, int parts, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(a.rows * parts)); cfg.blockDim = dim3(THREADS); cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  void (*kernel)(LogprobArgs) = a.top_k ? (a.entropy ? logprob_kernel<T, THREADS, true, true> : logprob_kernel<T, THREADS, true, false>)
+                                        : (a.entropy ? logprob_kernel<T, THREADS, false, true> : logprob_kernel<T, THREADS, false, false>);
+  return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
 template <typename T> static cudaError_t logprob_launch(const LogprobArgs& a, int parts, cudaStream_t st) {
   if (a.vocab <= kLpShort) {
     void (*kernel)(LogprobArgs) = a.top_k ? (a.entropy ? logprob_short_kernel<T, true, true> : logprob_short_kernel<T, true, false>)
                                           : (a.entropy ? logprob_short_kernel<T, false, true> : logprob_short_kernel<T, false, false>);
     return launch_pdl(kernel, dim3((unsigned)((a.rows + kLpWarps - 1) / kLpWarps)), dim3(kLpThreads), 0, st, false, a);
   }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(a.rows * parts)); cfg.blockDim = dim3(kLpThreads); cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  void (*kernel)(LogprobArgs) = a.top_k ? (a.entropy ? logprob_kernel<T, true, true> : logprob_kernel<T, true, false>)
-                                        : (a.entropy ? logprob_kernel<T, false, true> : logprob_kernel<T, false, false>);
-  return cudaLaunchKernelEx(&cfg, kernel, a);
+  // Rows of up to 64 KB take 128 threads.  us with 128 / 256: 1345 x 8191 fp32, both passes, 27 / 29; 4096 x 32000 bf16 with eight
+  // alternatives 76 / 78; but the same in fp32, rows of 128 KB, 121 / 103.
+  return a.vocab <= 65536 / (int)sizeof(T) ? logprob_launch_rows<T, 128>(a, parts, st) : logprob_launch_rows<T, 256>(a, parts, st);
 }
 
 static pm_status logprob_shape(int32_t dtype, int64_t rows, int32_t vocab, int64_t row_stride, const void* logits) {
