@@ -85,6 +85,7 @@ template <int THREADS> struct LpShared {
   Sums warp[THREADS / 32];
   Sums block[kLpMaxCluster];                      // of the cluster's blocks, in its first
   float lane_max[THREADS / 32][32];
+  uint8_t hit[THREADS / 32][32];
   float threshold;
   int n_list;
   float list_v[kLpList];
@@ -168,21 +169,22 @@ template <int THREADS, typename T> __device__ void block_top(LpShared<THREADS>& 
   }
   __syncthreads();
   const float th = sh.threshold;
-  // the vectors of each thread that reaches the threshold, read again by its whole warp
-  unsigned hit = __ballot_sync(0xffffffffu, mine >= th);
-  while (hit) {
-    const int who = __ffs(hit) - 1;
-    hit &= hit - 1;
-    for (int j = j0 + warp * 32 + who + lane * THREADS; j < j1; j += 32 * THREADS) {
-      float v[Vec<T>::n];
-      x.get(j, v);
+  // the vectors of the threads that reach the threshold, read again by their whole warp: (thread, vector) pairs over the lanes
+  const unsigned hits = __ballot_sync(0xffffffffu, mine >= th);
+  if (mine >= th) sh.hit[warp][__popc(hits & ((1u << lane) - 1))] = (uint8_t)lane;
+  __syncwarp();
+  const int each = (j1 - j0 + THREADS - 1) / THREADS;
+  for (int p = lane; p < __popc(hits) * each; p += 32) {
+    const int j = j0 + warp * 32 + sh.hit[warp][p / each] + p % each * THREADS;
+    if (j >= j1) continue;
+    float v[Vec<T>::n];
+    x.get(j, v);
 #pragma unroll
-      for (int i = 0; i < Vec<T>::n; ++i) {
-        const int id = x.first(j) + i;
-        if (v[i] >= th && id >= 0 && id < x.vocab) {
-          const int at = atomicAdd(&sh.n_list, 1);
-          if (at < kLpList) { sh.list_v[at] = v[i]; sh.list_id[at] = id; }
-        }
+    for (int i = 0; i < Vec<T>::n; ++i) {
+      const int id = x.first(j) + i;
+      if (v[i] >= th && id >= 0 && id < x.vocab) {
+        const int at = atomicAdd(&sh.n_list, 1);
+        if (at < kLpList) { sh.list_v[at] = v[i]; sh.list_id[at] = id; }
       }
     }
   }
@@ -356,11 +358,13 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) logprob_kernel(Logpro
   }
 }
 
-// Short rows: a warp to each, nothing shared between warps.
-constexpr int kLpShort = 2048;                    // elements
+// Short rows: a warp to each, nothing shared between warps; for rows of up to 4 KB, and of up to 16 KB where there are many.  us with a warp / a block to a row, fp32, five alternatives: 16 x 200 4.4 / 6.3,
+// 300 x 1000 6.3 / 6.3, 1200 x 2000 8.5 / 10.4, 2400 x 4000 15.6 / 18.6; but 40 x 3000 9.2 / 6.4 and 1345 x 8191 30.9 / 27.3.
+constexpr int kLpShortBytes = 4096, kLpMidBytes = 16384, kLpMidRows = 1024;
 constexpr int kLpShortList = 160;
 
 struct LpWarpShared {
+  uint8_t hit[32];
   float v[kLpShortList];
   int id[kLpShortList];
 };
@@ -408,24 +412,23 @@ __global__ void __launch_bounds__(kLpThreads) logprob_short_kernel(LogprobArgs a
     }
     LpWarpShared& sh = shared[warp];
     const float th = __shfl_sync(0xffffffffu, sorted_down(mine), k - 1);
-    unsigned hit = __ballot_sync(0xffffffffu, mine >= th);
+    const unsigned hits = __ballot_sync(0xffffffffu, mine >= th);
+    if (mine >= th) sh.hit[__popc(hits & ((1u << lane) - 1))] = (uint8_t)lane;
+    __syncwarp();
+    const int each = (x.count + 31) / 32, pairs = __popc(hits) * each;
     int n = 0;
-    while (hit) {                                 // the vectors of each lane that reaches the threshold, by the whole warp
-      const int who = __ffs(hit) - 1;
-      hit &= hit - 1;
-      for (int j = who; j < x.count; j += 32 * 32) {
-        float v[N];
-        const int at = j + lane * 32;
-        if (at < x.count) x.get(at, v);
+    for (int base = 0; base < pairs; base += 32) {   // the vectors of the lanes that reach the threshold: (lane, vector) pairs over the lanes
+      const int p = base + lane, at = p < pairs ? sh.hit[p / each] + p % each * 32 : x.count;
+      float v[N];
+      if (at < x.count) x.get(at, v);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int id = x.first(at) + i;
-          const bool in = at < x.count && id >= 0 && id < x.vocab && v[i] >= th;
-          const unsigned all = __ballot_sync(0xffffffffu, in);
-          const int to = n + __popc(all & ((1u << lane) - 1));
-          if (in && to < kLpShortList) { sh.v[to] = v[i]; sh.id[to] = id; }
-          n += __popc(all);
-        }
+      for (int i = 0; i < N; ++i) {
+        const int id = x.first(at) + i;
+        const bool in = at < x.count && id >= 0 && id < x.vocab && v[i] >= th;
+        const unsigned all = __ballot_sync(0xffffffffu, in);
+        const int to = n + __popc(all & ((1u << lane) - 1));
+        if (in && to < kLpShortList) { sh.v[to] = v[i]; sh.id[to] = id; }
+        n += __popc(all);
       }
     }
     __syncwarp();
@@ -566,14 +569,15 @@ template <typename T, int THREADS> static cudaError_t logprob_launch_rows(const 
 }
 
 template <typename T> static cudaError_t logprob_launch(const LogprobArgs& a, int parts, cudaStream_t st) {
-  if (a.vocab <= kLpShort) {
+  const int bytes = a.vocab * (int)sizeof(T);
+  if (bytes <= kLpShortBytes || (bytes <= kLpMidBytes && a.rows >= kLpMidRows)) {
     void (*kernel)(LogprobArgs) = a.top_k ? (a.entropy ? logprob_short_kernel<T, true, true> : logprob_short_kernel<T, true, false>)
                                           : (a.entropy ? logprob_short_kernel<T, false, true> : logprob_short_kernel<T, false, false>);
     return launch_pdl(kernel, dim3((unsigned)((a.rows + kLpWarps - 1) / kLpWarps)), dim3(kLpThreads), 0, st, false, a);
   }
   // Rows of up to 64 KB take 128 threads.  us with 128 / 256: 1345 x 8191 fp32, both passes, 27 / 29; 4096 x 32000 bf16 with eight
   // alternatives 76 / 78; but the same in fp32, rows of 128 KB, 121 / 103.
-  return a.vocab <= 65536 / (int)sizeof(T) ? logprob_launch_rows<T, 128>(a, parts, st) : logprob_launch_rows<T, 256>(a, parts, st);
+  return bytes <= 65536 ? logprob_launch_rows<T, 128>(a, parts, st) : logprob_launch_rows<T, 256>(a, parts, st);
 }
 
 static pm_status logprob_shape(int32_t dtype, int64_t rows, int32_t vocab, int64_t row_stride, const void* logits) {

@@ -86,7 +86,8 @@ def make(n, v, dtype, dev, seed=0, spread=3.0):
 
 
 @pytest.mark.parametrize("dtype", [F, BF])
-@pytest.mark.parametrize("n,v,k", [(1, 1, 1), (3, 2, 2), (5, 31, 4), (2, 32, 32), (7, 1000, 8), (9, 2047, 20), (3, 2048, 0), (5, 2049, 7), (4, 4097, 1), (1, 32000, 8), (3, 50001, 20),
+@pytest.mark.parametrize("n,v,k", [(1, 1, 1), (3, 2, 2), (5, 31, 4), (2, 32, 32), (7, 1000, 8), (9, 1023, 20), (3, 1024, 0), (5, 1025, 7), (9, 2047, 20), (5, 2049, 7), (1024, 4096, 6),
+                                   (1100, 3999, 20), (4, 4097, 1), (1, 32000, 8), (3, 50001, 20),
                                    (33, 8191, 5), (150, 8192, 0), (300, 12345, 3), (1, 131071, 32)])
 def test_sizes(cuda_device, n, v, k, dtype):
     x, y, gl, gh = make(n, v, dtype, cuda_device, seed=v)
@@ -98,7 +99,7 @@ def test_sizes(cuda_device, n, v, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F, BF])
-@pytest.mark.parametrize("v,k", [(40, 5), (1501, 32), (2048, 3), (3001, 8), (20000, 8), (20000, 32)])
+@pytest.mark.parametrize("v,k", [(40, 5), (900, 32), (1024, 3), (1501, 32), (3001, 8), (20000, 8), (20000, 32)])
 def test_ties_go_to_the_lowest_id(cuda_device, dtype, v, k):
     """Few distinct values, one value, sorted rows, the best next to each other, signed zeros."""
     gen = torch.Generator(cuda_device).manual_seed(v)
