@@ -245,30 +245,36 @@ class GradClip:
         self.device = _compute_device("grads[0]", grads[0])
         self.L = lib()
         self.grads, self.outs = grads, outs
-        self.tensors = (pm_tensor_pair * len(grads))()
-        spans = []
+        rows, spans = [], []
         for i, (g, o) in enumerate(zip(grads, outs)):
-            for name, t in ((f"grads[{i}]", g), (f"outs[{i}]", o)):
-                if _compute_device(name, t) != self.device:
-                    _refuse(f"{name} is on {t.device}, expected {self.device}")
-                if not t.is_contiguous():
-                    _refuse(f"{name} must be contiguous")
-            if g.numel() != o.numel():
-                _refuse(f"grads[{i}] has {g.numel()} elements, outs[{i}] {o.numel()}", "PM_ERR_SHAPE")
-            self.tensors[i] = pm_tensor_pair(g.data_ptr(), o.data_ptr(), g.numel(), _DTYPES[g.dtype], _DTYPES[o.dtype])
-            if g.numel() == 0:
-                continue
-            in_place = g.data_ptr() == o.data_ptr() and g.dtype == o.dtype
-            spans.append((o.data_ptr(), o.data_ptr() + o.numel() * o.element_size(), True, f"outs[{i}]"))
-            if not in_place:
-                spans.append((g.data_ptr(), g.data_ptr() + g.numel() * g.element_size(), False, f"grads[{i}]"))
-        end = {True: (0, ""), False: (0, "")}                # the furthest end so far of what is written, and of what is read
-        for a, b, written, name in sorted(spans):
+            if not (self._fits(g) and self._fits(o) and g.numel() == o.numel()):
+                self._mismatch(i, g, o)
+            n, src, dst, src_type, dst_type = g.numel(), g.data_ptr(), o.data_ptr(), _DTYPES[g.dtype], _DTYPES[o.dtype]
+            rows.append((src, dst, n, src_type, dst_type))
+            if n:
+                spans.append((dst, dst + n * o.element_size(), True, i))
+                if src != dst or src_type != dst_type:
+                    spans.append((src, src + n * g.element_size(), False, i))
+        self.tensors = (pm_tensor_pair * len(rows))(*rows)
+        end = {True: (0, 0), False: (0, 0)}                  # the furthest end so far of what is written, and of what is read
+        for start, stop, written, i in sorted(spans):
             for other in (True, False) if written else (True,):
-                if a < end[other][0]:
-                    _refuse(f"{name} overlaps {end[other][1]}")
-            end[written] = max(end[written], (b, name))
+                if start < end[other][0]:
+                    _refuse(f"{'outs' if written else 'grads'}[{i}] overlaps {'outs' if other else 'grads'}[{end[other][1]}]")
+            if stop > end[written][0]:
+                end[written] = (stop, i)
         self.ws_bytes = self.L.pm_clip_gradients_workspace_bytes(len(grads))
+
+    def _fits(self, t):
+        return isinstance(t, torch.Tensor) and t.device == self.device and t.dtype in _DTYPES and t.is_contiguous()
+
+    def _mismatch(self, i, g, o):
+        for name, t in ((f"grads[{i}]", g), (f"outs[{i}]", o)):
+            if _compute_device(name, t) != self.device:
+                _refuse(f"{name} is on {t.device}, expected {self.device}")
+            if not t.is_contiguous():
+                _refuse(f"{name} must be contiguous")
+        _refuse(f"grads[{i}] has {g.numel()} elements, outs[{i}] {o.numel()}", "PM_ERR_SHAPE")
 
     def pm_clip_gradients(self, max_norm, norm, scale, stream=None):
         """Writes outs, the norm before clipping, and the factor (float32 tensors of one element)."""
