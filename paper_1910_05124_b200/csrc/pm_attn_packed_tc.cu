@@ -7,7 +7,7 @@
 //   S = Q K^T (128 x 128 x D, operands in shared memory) -> p = 2^(c s - m) in fp32 -> bf16 P over S's columns in tensor memory
 //   -> O += P V (A = P from tensor memory).
 // While the softmax of one tile runs, the products of the other do.  The running maximum m is raised, and O and the row sum rescaled,
-// only when a row of the warp outgrows it by 2^8: P then reaches at most 256, which bf16 holds as exactly as 1, and most key tiles
+// only when the row outgrows it by 2^8: P then reaches at most 256, which bf16 holds as exactly as 1, and most key tiles
 // leave O alone.
 //
 // Where P lies over S, products that read P are issued before the product that overwrites it, and products complete in the order of
@@ -90,9 +90,9 @@ template <int DT> __device__ __forceinline__ void load_tile(uint32_t dst, const 
   for (int i = 0; i < DT / 64; ++i) tma_load_3d(dst + i * TC_SUB, map, bar, i * 64, head, (int)token);
 }
 
-__device__ __forceinline__ float max3(float a, float b, float c) {
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 // c s - m for two values at a time
@@ -166,7 +166,8 @@ __device__ __forceinline__ void finish_rows(const HeadView& x, const SeqTile& s,
 
 // 2^x for two values on the FMA units: x = n + f with n the nearest integer, 2^f by the polynomial of degree 4 with the least relative
 // error on [-1/2, 1/2] (2.6e-6, a 700th of bf16's half step; found by iteratively reweighted least squares), n added to the exponent.
-// x is at most 8 here; below -126 the result is 2^-126 where the exponential unit gives zero.
+// x is at most 8 here; below -126 the result is 2^-126 where the exponential unit gives zero, and of a NaN it is anything: the row's
+// other exponentials keep it.
 __device__ __forceinline__ float2 ex2_fma(float2 x) {
   const float magic = 12582912.f;                 // 1.5 * 2^23: the sum's low bits are the nearest integer
   x.x = fmaxf(x.x, -126.f); x.y = fmaxf(x.y, -126.f);
@@ -439,8 +440,10 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
 #pragma unroll
         for (int i = 0; i < 32; i += 2)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) mx[q] = max3(mx[q], __uint_as_float(v[q][i]), __uint_as_float(v[q][i + 1]));
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+          for (int q = 0; q < 4; ++q) mx[q] = max3_nan(mx[q], __uint_as_float(v[q][i]), __uint_as_float(v[q][i + 1]));
+        // a NaN or +infinity among the scores: no distribution; the maximum says so to every exponential of the row
+        float top = max3_nan(mx[0], mx[1], max_nan(mx[2], mx[3])) * c;
+        if (top == INFINITY) top = NAN;
         if (S::kApart && j > 0) {                 // P's columns are free, and O holds the tiles before this one
           ok = wait_for(o_full(t), (j - 1) & 1, abort_flag, status, 43);
           ok = __all_sync(0xffffffffu, ok);
@@ -449,8 +452,8 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
         }
         if (j == 0) {
           m = top;
-        } else if (__any_sync(0xffffffffu, top > m + 8.f)) {
-          const float up = fmaxf(m, top), f = ex2(m - up);
+        } else if (__any_sync(0xffffffffu, !(top <= m + 8.f))) {
+          const float up = top <= m + 8.f ? m : max_nan(m, top), f = ex2(m - up);       // rows that need it not keep theirs
           m = up;
           l *= f;
 #pragma unroll

@@ -157,6 +157,29 @@ def test_non_finite_values_keep_to_their_sequence(cuda_device, dtype, causal):
     assert o[120:160].isnan().any()
 
 
+@pytest.mark.parametrize("lens,H,D", [([150, 90], 2, 64), ([400], 1, 128), ([1500], 16, 128), ([300], 2, 33)], ids=str)
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_one_value_that_is_not_finite(cuda_device, dtype, lens, H, D):
+    """A NaN or infinity in one key alone: the rows that see it have no distribution, or do without the key; the others keep their bits."""
+    op, q, k, v, d_o, cu = make(lens, H, H, D, dtype, cuda_device, seed=12)
+    clean, _ = forward(op, q, k, v, cu)
+    for at in (0, 14, 15, 30, 31, 77, 127, 128, 142):
+        for bad in (math.nan, math.inf, -math.inf):
+            if at >= lens[0]:
+                continue
+            k2 = k.clone()
+            k2[at, 0, D // 2] = bad
+            o, lse = forward(op, q, k2, v, cu)
+            s = (q[:lens[0], 0, D // 2].double() * bad)                          # the score's sign, or NaN
+            gone = (torch.arange(lens[0], device=cuda_device) >= at) & ~(s == -math.inf)
+            gone[0] |= at == 0                                                   # its only key
+            assert torch.equal(o[:lens[0], 0].isnan().all(1), gone) and torch.equal(o[:lens[0], 0].isnan().any(1), gone), (at, bad)
+            assert torch.equal(lse[0, :lens[0]].isfinite(), ~gone)
+            same = torch.ones(o.shape[:2], dtype=torch.bool, device=cuda_device)
+            same[at:lens[0], 0] = False
+            assert torch.equal(o[same], clean[same]), (at, bad)
+
+
 @pytest.mark.parametrize("dtype", [BF, F])
 def test_layouts(cuda_device, dtype):
     """Heads first, a token stride that no 16-byte copy can take, tensors that start between two such boundaries, and key heads
