@@ -3,8 +3,8 @@ log probabilities of given tokens, and gradient clipping.  Argument checks and m
 caller, outputs included.
 
 Every call is asynchronous on `stream` (default: the current stream of the tensors' device) and may be captured into a CUDA
-graph.  As with any CUDA call, a tensor that another stream still writes has to be waited for by the caller.  Refused
-arguments raise PipeMareError.
+graph.  As with any CUDA call, a tensor that another stream still writes has to be waited for by the caller, and a tensor
+that belongs to another stream has to be kept until the call has run.  Refused arguments raise PipeMareError.
 """
 import ctypes as C
 
@@ -37,7 +37,7 @@ def _flat(name, t, dtype, device, shape):
     """Data pointer of a contiguous tensor; None for None."""
     if t is None:
         return None
-    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and t.shape == shape and t.is_contiguous()):
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device.index and t.shape == shape and t.is_contiguous()):
         _mismatch(name, t, dtype, device, shape)
     return t.data_ptr()
 
@@ -108,23 +108,21 @@ class PackedAttention:
             _refuse("cu_seqlens must be a one-dimensional tensor of sequences + 1 entries", "PM_ERR_SHAPE")
         cu = _flat("cu_seqlens", cu_seqlens, torch.int32, device, cu_seqlens.shape)
         tokens = q.shape[0]
-        return device, tokens, pm_attention_desc(_DTYPES[q.dtype], self.n_heads, self.n_kv_heads, self.head_dim, cu_seqlens.numel() - 1,
-                                                 self.causal, tokens, self.scale), cu
+        return device, tokens, C.byref(pm_attention_desc(_DTYPES[q.dtype], self.n_heads, self.n_kv_heads, self.head_dim,
+                                                         cu_seqlens.numel() - 1, self.causal, tokens, self.scale)), cu
 
-    def _views(self, tokens, dtype, device, read, written):
-        """One array of pm_head_view for (name, tensor, heads) triples, checked."""
-        d = self.head_dim
-        flat = []
-        for triples, out in ((read, False), (written, True)):
-            for name, t, heads in triples:
-                if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and t.shape == (tokens, heads, d)):
-                    _mismatch(name, t, dtype, device, (tokens, heads, d))
-                token, head, one = t.stride()
-                if one != 1 and d > 1:
-                    _refuse(f"the last dimension of {name} must be contiguous")
-                if out and not (head == d and token >= heads * d):
-                    self._check_apart(name, ((token, tokens), (head, heads)))
-                flat += (t.data_ptr(), token, head)
+    def _views(self, tokens, dtype, device, names, tensors, heads, n_read):
+        """One array of pm_head_view for tensors with `heads` heads each, checked; those behind the first n_read are written."""
+        d, index, flat = self.head_dim, device.index, []
+        for t, h in zip(tensors, heads):
+            if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == index and t.shape == (tokens, h, d)):
+                _mismatch(names[len(flat) // 3], t, dtype, device, (tokens, h, d))
+            token, head, one = t.stride()
+            if one != 1 and d > 1:
+                _refuse(f"the last dimension of {names[len(flat) // 3]} must be contiguous")
+            if (head != d or token < h * d) and len(flat) >= 3 * n_read:
+                self._check_apart(names[len(flat) // 3], ((token, tokens), (head, h)))
+            flat += (t.data_ptr(), token, head)
         return (C.c_int64 * len(flat))(*flat)
 
     def _check_apart(self, name, dims):
@@ -139,23 +137,23 @@ class PackedAttention:
 
     def pm_attention_packed_forward(self, q, k, v, cu_seqlens, o, lse=None, stream=None):
         """Writes o and, for a backward pass, lse."""
-        device, tokens, d, cu = self._desc(q, cu_seqlens)
+        device, tokens, desc, cu = self._desc(q, cu_seqlens)
         H, K = self.n_heads, self.n_kv_heads
-        views = self._views(tokens, q.dtype, device, (("q", q, H), ("k", k, K), ("v", v, K)), (("o", o, H),))
+        views = self._views(tokens, q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), (H, K, K, H), 3)
         p_lse = _flat("lse", lse, torch.float32, device, (H, tokens))
         at = C.addressof(views)
-        _launch(lambda st: self.L.pm_attention_packed_forward(C.byref(d), at, at + _VIEW, at + 2 * _VIEW, cu, at + 3 * _VIEW, p_lse, st), device, stream)
+        _launch(lambda st: self.L.pm_attention_packed_forward(desc, at, at + _VIEW, at + 2 * _VIEW, cu, at + 3 * _VIEW, p_lse, st), device, stream)
 
     def pm_attention_packed_backward(self, q, k, v, o, lse, d_o, cu_seqlens, dq, dk, dv, stream=None):
         """Writes dq, dk and dv from d_o and what the forward call wrote."""
-        device, tokens, d, cu = self._desc(q, cu_seqlens)
+        device, tokens, desc, cu = self._desc(q, cu_seqlens)
         if lse is None:
             _refuse("lse must be a tensor")
         H, K = self.n_heads, self.n_kv_heads
-        views = self._views(tokens, q.dtype, device, (("q", q, H), ("k", k, K), ("v", v, K), ("o", o, H), ("d_o", d_o, H)),
-                            (("dq", dq, H), ("dk", dk, K), ("dv", dv, K)))
+        views = self._views(tokens, q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"), (q, k, v, o, d_o, dq, dk, dv),
+                            (H, K, K, H, H, H, K, K), 5)
         p_lse = _flat("lse", lse, torch.float32, device, (H, tokens))
-        at, desc = C.addressof(views), C.byref(d)
+        at = C.addressof(views)
         need = self.L.pm_attention_packed_workspace_bytes(desc)
         _launch(lambda st, ws=None: self.L.pm_attention_packed_backward(
             desc, at, at + _VIEW, at + 2 * _VIEW, at + 3 * _VIEW, p_lse, at + 4 * _VIEW, cu, at + 5 * _VIEW, at + 6 * _VIEW, at + 7 * _VIEW, ws, need, st),
