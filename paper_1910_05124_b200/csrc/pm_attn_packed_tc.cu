@@ -164,19 +164,20 @@ __device__ __forceinline__ void finish_rows(const HeadView& x, const SeqTile& s,
   }
 }
 
-// 2^x for two values on the FMA units: x = n + f with n the nearest integer, 2^f by the polynomial of degree 4 with the least relative
-// error on [-1/2, 1/2] (2.6e-6, a 700th of bf16's half step; found by iteratively reweighted least squares), n added to the exponent.
-// x is at most 8 here; below -126 the result is 2^-126 where the exponential unit gives zero, and of a NaN it is anything: the row's
+// 2^x for two values on the FMA units: x = n + f with n the nearest integer, 2^f by the polynomial of degree 4 through f(0) = 1 with the
+// least relative error on [-1/2, 1/2] (2.9e-6, a 1300th of bf16's half step; found as a linear program over 4001 points), n added to the
+// exponent.  x is at most 8 here.  At -127 and below, masked scores among them, the result is exactly zero (1.0's exponent less 127):
+// a masked key's value counts for nothing however large.  Between -127 and -126 it is below 2^-126, and of a NaN it is zero: the row's
 // other exponentials keep it.
 __device__ __forceinline__ float2 ex2_fma(float2 x) {
   const float magic = 12582912.f;                 // 1.5 * 2^23: the sum's low bits are the nearest integer
-  x.x = fmaxf(x.x, -126.f); x.y = fmaxf(x.y, -126.f);
+  x.x = fmaxf(x.x, -127.f); x.y = fmaxf(x.y, -127.f);
   const float2 t = add_f32x2(x, make_float2(magic, magic)), n = add_f32x2(t, make_float2(-magic, -magic));
   const float2 f = fma_f32x2(n, make_float2(-1.f, -1.f), x);
-  float2 p = fma_f32x2(make_float2(0.00957010220736f, 0.00957010220736f), f, make_float2(0.0559178628027f, 0.0559178628027f));
-  p = fma_f32x2(p, f, make_float2(0.240247443318f, 0.240247443318f));
-  p = fma_f32x2(p, f, make_float2(0.693121790886f, 0.693121790886f));
-  p = fma_f32x2(p, f, make_float2(0.999999284744f, 0.999999284744f));
+  float2 p = fma_f32x2(make_float2(0.009582852945f, 0.009582852945f), f, make_float2(0.05590642616f, 0.05590642616f));
+  p = fma_f32x2(p, f, make_float2(0.2402409911f, 0.2402409911f));
+  p = fma_f32x2(p, f, make_float2(0.6931241751f, 0.6931241751f));
+  p = fma_f32x2(p, f, make_float2(1.f, 1.f));
   return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)),
                      __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
 }

@@ -180,6 +180,21 @@ def test_one_value_that_is_not_finite(cuda_device, dtype, lens, H, D):
             assert torch.equal(o[same], clean[same]), (at, bad)
 
 
+@pytest.mark.parametrize("lens,H,D", [([150, 90], 2, 64), ([400], 1, 128), ([1500], 16, 128)], ids=str)
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_values_of_masked_keys_count_for_nothing(cuda_device, dtype, lens, H, D):
+    """However large they are: 2^-126 of the type's largest value would already be 4."""
+    op, q, k, v, d_o, cu = make(lens, H, H, D, dtype, cuda_device, seed=13)
+    o0, lse0 = forward(op, q, k, v, cu)
+    dq0 = backward(op, q, k, v, o0, lse0, d_o, cu)["dq"]
+    for n in (1, 15, 100, 140):
+        v2 = v.clone()
+        v2[n:lens[0]] = torch.finfo(dtype).max
+        o, lse = forward(op, q, k, v2, cu)
+        assert torch.equal(o[:n], o0[:n]) and torch.equal(lse, lse0), n
+        assert torch.equal(backward(op, q, k, v2, o, lse, d_o, cu)["dq"][:n], dq0[:n]), n
+
+
 @pytest.mark.parametrize("dtype", [BF, F])
 def test_layouts(cuda_device, dtype):
     """Heads first, a token stride that no 16-byte copy can take, tensors that start between two such boundaries, and key heads
