@@ -46,13 +46,14 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile
 template <int DT, int NT> struct FwdShape {
   static constexpr int kSub = DT / 64;            // sub-tiles of a tile
   static constexpr int kTile = kSub * TC_SUB;
-  static constexpr int kStages = NT == 1 ? (DT == 64 ? 2 : 1) : (DT == 64 ? 4 : 2);
+  static_assert(NT == 1 || DT == 128, "two query tiles to a block are for heads of 128");
+  static constexpr int kStages = NT == 1 && DT == 128 ? 1 : 2;
   static constexpr int kWarps = NT * 4;           // of the softmax: thread = row
   static constexpr int kThreads = kWarps * 32 + 128;
   static constexpr int kBlocks = NT == 1 ? 2 : 1; // per SM
   // Registers: a softmax thread holds a row of 128 scores, the warps that copy and issue need few.  NT = 2: 384 threads are launched
   // with 168, 256 x 224 + 128 x 56 is no more than that; NT = 1: 256 with 128, 128 x 208 + 128 x 48.
-  // (Two threads to a row, 64 scores each, took 332 us where this takes 295, and 229 where it takes 207: see FWD_FMA's sizes.)
+  // (Two threads to a row, 64 scores each, took 332 us where this takes 289: 8192 + 4099 tokens, 16 heads of 128 on 4.)
   static constexpr int kSoftmaxRegs = NT == 1 ? 208 : 224, kOtherRegs = NT == 1 ? 48 : 56;
   // Tensor-memory columns: S (128 for each tile), O (DT), and for heads of 64 P (64) beside S instead of over it, so that the
   // next scores are formed while the exponentials of these are.
@@ -280,115 +281,115 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
   auto col_p = [&](int t) { return S::kApart ? tmem + NT * (128 + DT) + t * 64 : col_s(t); };
 
   if (warp >= S::kWarps) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kOtherRegs));
-  if (n_keys == 0) {                              // nothing of a shared block's keys
-  } else if (warp == kCopy) {                     // ---- copies
-    int armed_k = 1, armed_v = 1;
-    bool ok = true;
-    for (int j = 1; j < n_keys && ok; ++j) {
-      const int st = j % S::kStages;
-      const uint32_t ph = (j / S::kStages - 1) & 1;
-      if (j >= S::kStages) ok = wait_for(k_empty(st), ph, abort_flag, status, 31);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      copy_keys(j);
-      ++armed_k;
-      if (j >= S::kStages) ok = wait_for(v_empty(st), ph, abort_flag, status, 32);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      copy_values(j);
-      ++armed_v;
-    }
-    if (*abort_flag) {                            // nothing may be in flight when the block ends
-      volatile int never = 0;
-      wait_for(bar_q, 0, &never, status, 33);
-      for (int j = max(0, armed_k - S::kStages); j < armed_k; ++j) wait_for(k_full(j % S::kStages), (j / S::kStages) & 1, &never, status, 33);
-      for (int j = max(0, armed_v - S::kStages); j < armed_v; ++j) wait_for(v_full(j % S::kStages), (j / S::kStages) & 1, &never, status, 33);
-    }
-  } else if (warp == kIssue) {                    // ---- products
-    const uint32_t id_s = make_idesc_mn(128, 128, 0, 0), id_o = make_idesc_mn(128, DT, 0, 1);
-    bool ok = wait_for(bar_q, 0, abort_flag, status, 34) && wait_for(k_full(0), 0, abort_flag, status, 35);
-    if (ok) {
-      tc_fence_after();
-      if (elect_one()) {
-        for (int t = 0; t < NT; ++t)
-          if (count_of(t)) { mma_abt<DT>(col_s(t), sQ + t * S::kTile, sK, id_s); tc_commit(s_full(t)); }
-        tc_commit(k_empty(0));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kOtherRegs));
+    if (n_keys == 0) {                              // nothing of a shared block's keys
+    } else if (warp == kCopy) {                     // ---- copies
+      int armed_k = 1, armed_v = 1;
+      bool ok = true;
+      for (int j = 1; j < n_keys && ok; ++j) {
+        const int st = j % S::kStages;
+        const uint32_t ph = (j / S::kStages - 1) & 1;
+        if (j >= S::kStages) ok = wait_for(k_empty(st), ph, abort_flag, status, 31);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        copy_keys(j);
+        ++armed_k;
+        if (j >= S::kStages) ok = wait_for(v_empty(st), ph, abort_flag, status, 32);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        copy_values(j);
+        ++armed_v;
       }
-      __syncwarp();
-    }
-    auto values = [&](int t, int j) {             // O += P V, the first half of the keys as soon as their probabilities are there
-      const uint32_t v = sV + (j % S::kStages) * S::kTile;
-      if (!wait_for(p_half(t), j & 1, abort_flag, status, 38)) return false;
-      tc_fence_after();
-      if (elect_one()) mma_ab<DT>(col_o(t), col_p(t), v, id_o, j > 0, 0);
-      __syncwarp();
-      if (!wait_for(p_full(t), j & 1, abort_flag, status, 38)) return false;
-      tc_fence_after();
-      if (elect_one()) mma_ab<DT>(col_o(t), col_p(t), v, id_o, true, 1);
-      __syncwarp();
-      return true;
-    };
-    auto scores = [&](int t, int j) {
-      if (elect_one()) { mma_abt<DT>(col_s(t), sQ + t * S::kTile, sK + (j % S::kStages) * S::kTile, id_s); tc_commit(s_full(t)); }
-      __syncwarp();
-    };
-    auto done = [&](uint32_t bar) {
-      if (elect_one()) tc_commit(bar);
-      __syncwarp();
-    };
-    for (int j = 0; j < n_keys && ok; ++j) {
-      const int st = j % S::kStages, nx = (j + 1) % S::kStages;
-      const bool more = j + 1 < n_keys;
-      auto next_keys = [&]() { return wait_for(k_full(nx), ((j + 1) / S::kStages) & 1, abort_flag, status, 37); };
-      if constexpr (S::kApart) {
-        if (more) {
-          ok = next_keys();
-#pragma unroll
+      if (*abort_flag) {                            // nothing may be in flight when the block ends
+        volatile int never = 0;
+        wait_for(bar_q, 0, &never, status, 33);
+        for (int j = max(0, armed_k - S::kStages); j < armed_k; ++j) wait_for(k_full(j % S::kStages), (j / S::kStages) & 1, &never, status, 33);
+        for (int j = max(0, armed_v - S::kStages); j < armed_v; ++j) wait_for(v_full(j % S::kStages), (j / S::kStages) & 1, &never, status, 33);
+      }
+    } else if (warp == kIssue) {                    // ---- products
+      const uint32_t id_s = make_idesc_mn(128, 128, 0, 0), id_o = make_idesc_mn(128, DT, 0, 1);
+      bool ok = wait_for(bar_q, 0, abort_flag, status, 34) && wait_for(k_full(0), 0, abort_flag, status, 35);
+      if (ok) {
+        tc_fence_after();
+        if (elect_one()) {
           for (int t = 0; t < NT; ++t)
-            if (ok && j + 1 < count_of(t)) {
-              ok = wait_for(s_read(t), j & 1, abort_flag, status, 42);
-              tc_fence_after();
-              if (ok) scores(t, j + 1);
+            if (count_of(t)) { mma_abt<DT>(col_s(t), sQ + t * S::kTile, sK, id_s); tc_commit(s_full(t)); }
+          tc_commit(k_empty(0));
+        }
+        __syncwarp();
+      }
+      auto values = [&](int t, int j) {             // O += P V, the first half of the keys as soon as their probabilities are there
+        const uint32_t v = sV + (j % S::kStages) * S::kTile;
+        if (!wait_for(p_half(t), j & 1, abort_flag, status, 38)) return false;
+        tc_fence_after();
+        if (elect_one()) mma_ab<DT>(col_o(t), col_p(t), v, id_o, j > 0, 0);
+        __syncwarp();
+        if (!wait_for(p_full(t), j & 1, abort_flag, status, 38)) return false;
+        tc_fence_after();
+        if (elect_one()) mma_ab<DT>(col_o(t), col_p(t), v, id_o, true, 1);
+        __syncwarp();
+        return true;
+      };
+      auto scores = [&](int t, int j) {
+        if (elect_one()) { mma_abt<DT>(col_s(t), sQ + t * S::kTile, sK + (j % S::kStages) * S::kTile, id_s); tc_commit(s_full(t)); }
+        __syncwarp();
+      };
+      auto done = [&](uint32_t bar) {
+        if (elect_one()) tc_commit(bar);
+        __syncwarp();
+      };
+      for (int j = 0; j < n_keys && ok; ++j) {
+        const int st = j % S::kStages, nx = (j + 1) % S::kStages;
+        const bool more = j + 1 < n_keys;
+        auto next_keys = [&]() { return wait_for(k_full(nx), ((j + 1) / S::kStages) & 1, abort_flag, status, 37); };
+        if constexpr (S::kApart) {
+          if (more) {
+            ok = next_keys();
+  #pragma unroll
+            for (int t = 0; t < NT; ++t)
+              if (ok && j + 1 < count_of(t)) {
+                ok = wait_for(s_read(t), j & 1, abort_flag, status, 42);
+                tc_fence_after();
+                if (ok) scores(t, j + 1);
+              }
+            if (!ok) break;
+            done(k_empty(nx));
+          }
+          ok = wait_for(v_full(st), (j / S::kStages) & 1, abort_flag, status, 36);
+  #pragma unroll
+          for (int t = 0; t < NT; ++t)
+            if (ok && j < count_of(t)) {
+              ok = values(t, j);
+              if (ok) done(o_full(t));
             }
           if (!ok) break;
-          done(k_empty(nx));
-        }
-        ok = wait_for(v_full(st), (j / S::kStages) & 1, abort_flag, status, 36);
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-          if (ok && j < count_of(t)) {
+          done(v_empty(st));
+        } else {
+          ok = wait_for(v_full(st), (j / S::kStages) & 1, abort_flag, status, 36);
+          // with one stage the next keys are copied only behind the previous product's commit: waited for below
+          if (ok && more && S::kStages > 1) ok = next_keys();
+  #pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const int n = count_of(t);
+            if (!ok || j >= n) continue;
             ok = values(t, j);
-            if (ok) done(o_full(t));
+            if (ok && S::kStages == 1 && j + 1 < n) ok = next_keys();
+            if (!ok) continue;
+            tc_fence_after();
+            if (j + 1 < n) scores(t, j + 1);
+            else done(o_full(t));
           }
-        if (!ok) break;
-        done(v_empty(st));
-      } else {
-        ok = wait_for(v_full(st), (j / S::kStages) & 1, abort_flag, status, 36);
-        // with one stage the next keys are copied only behind the previous product's commit: waited for below
-        if (ok && more && S::kStages > 1) ok = next_keys();
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const int n = count_of(t);
-          if (!ok || j >= n) continue;
-          ok = values(t, j);
-          if (ok && S::kStages == 1 && j + 1 < n) ok = next_keys();
-          if (!ok) continue;
-          tc_fence_after();
-          if (j + 1 < n) scores(t, j + 1);
-          else done(o_full(t));
+          if (!ok) break;
+          done(v_empty(st));
+          if (more) done(k_empty(nx));
         }
-        if (!ok) break;
-        done(v_empty(st));
-        if (more) done(k_empty(nx));
       }
     }
-  }
-  if (NT == 1 && parts > 1) {
-    __syncwarp();
-    cluster_sync_all();
-    cluster_sync_all();
-  }
+    if (NT == 1 && parts > 1) {
+      __syncwarp();
+      cluster_sync_all();
+      cluster_sync_all();
+    }
   } else {                                        // ---- softmax: thread = row
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kSoftmaxRegs));
     const int t = warp >> 2, r = threadIdx.x & 127;
@@ -526,13 +527,13 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
         __syncwarp();
         cluster_sync_all();                       // the others have read this block's sums
       } else {
-      const float inv = 1.f / l;
-      if (a.lse && row < s.len) a.lse[(int64_t)h * a.tokens + s.begin + row] = ok ? (m + log2f(l)) * kLn2 : NAN;
-      const int first_row = q0 + (warp & 3) * 32;
-#pragma unroll
-      for (int q = 0; q < DT / 32; ++q)             // Q's tile has been read
-        store_rows(head_row_out<__nv_bfloat16>(a.o, s.begin + first_row, h), a.o.token, s.len - first_row, to, q * 32, a.dim, inv, ok,
-                   sptr + t * S::kTile + (warp & 3) * 2048);
+        const float inv = 1.f / l;
+        if (a.lse && row < s.len) a.lse[(int64_t)h * a.tokens + s.begin + row] = ok ? (m + log2f(l)) * kLn2 : NAN;
+        const int first_row = q0 + (warp & 3) * 32;
+  #pragma unroll
+        for (int q = 0; q < DT / 32; ++q)             // Q's tile has been read
+          store_rows(head_row_out<__nv_bfloat16>(a.o, s.begin + first_row, h), a.o.token, s.len - first_row, to, q * 32, a.dim, inv, ok,
+                     sptr + t * S::kTile + (warp & 3) * 2048);
       }
     }
   }
@@ -711,7 +712,7 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
       q0 += BN;
       if (q0 >= s.len) { q0 = first; ++h; }
     }
-    if (*abort_flag && n_it > 0) {                            // nothing may be in flight when the block ends
+    if (*abort_flag && n_it > 0) {                // nothing may be in flight when the block ends
       volatile int never = 0;
       wait_for(kv_full, 0, &never, status, 53);
       for (int it = max(0, armed - S::kStages); it < armed; ++it) wait_for(full(it % S::kStages), (it / S::kStages) & 1, &never, status, 53);
@@ -838,12 +839,12 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
       __syncwarp();
       cluster_sync_all();                         // the others have read this block's sums
     } else {
-    const int first_row = k0 + (warp & 3) * 32;
-    uint8_t* const stage = sptr + (sQ - base) + warp * 2048;           // the streamed tiles have been read
-    static_assert(DT == S::kParts * 32, "a part of the threads stores 32 columns of each gradient");
-    static_assert(S::kParts * 4 * 2048 <= 2 * S::kStages * S::kStream, "staging");
-    store_rows(head_row_out<__nv_bfloat16>(a.dv, s.begin + first_row, hk), a.dv.token, s.len - first_row, col_dv + lanes, c0, a.dim, 1.f, ok, stage);
-    store_rows(head_row_out<__nv_bfloat16>(a.dk, s.begin + first_row, hk), a.dk.token, s.len - first_row, col_dk + lanes, c0, a.dim, a.scale, ok, stage);
+      const int first_row = k0 + (warp & 3) * 32;
+      uint8_t* const stage = sptr + (sQ - base) + warp * 2048;           // the streamed tiles have been read
+      static_assert(DT == S::kParts * 32, "a part of the threads stores 32 columns of each gradient");
+      static_assert(S::kParts * 4 * 2048 <= 2 * S::kStages * S::kStream, "staging");
+      store_rows(head_row_out<__nv_bfloat16>(a.dv, s.begin + first_row, hk), a.dv.token, s.len - first_row, col_dv + lanes, c0, a.dim, 1.f, ok, stage);
+      store_rows(head_row_out<__nv_bfloat16>(a.dk, s.begin + first_row, hk), a.dk.token, s.len - first_row, col_dk + lanes, c0, a.dim, a.scale, ok, stage);
     }
   }
   if (parts > 1 && warp >= kCopy) {
@@ -943,7 +944,7 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
       }
       mbar_arrive(cleared(st));
     }
-    if (*abort_flag && n_it > 0) {                            // nothing may be in flight when the block ends
+    if (*abort_flag && n_it > 0) {                // nothing may be in flight when the block ends
       volatile int never = 0;
       wait_for(q_full, 0, &never, status, 73);
       for (int it = max(0, armed - S::kStages); it < armed; ++it) wait_for(full(it % S::kStages), (it / S::kStages) & 1, &never, status, 73);
@@ -1046,9 +1047,9 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
       __syncwarp();
       cluster_sync_all();                         // the others have read this block's sums
     } else {
-    const int first_row = q0 + (warp & 3) * 32;
-    store_rows(head_row_out<__nv_bfloat16>(a.dq, s.begin + first_row, h), a.dq.token, s.len - first_row, col_dq + lanes, c0, a.dim, a.scale, ok,
-               sptr + (sK - base) + warp * 2048);                      // the streamed tiles have been read
+      const int first_row = q0 + (warp & 3) * 32;
+      store_rows(head_row_out<__nv_bfloat16>(a.dq, s.begin + first_row, h), a.dq.token, s.len - first_row, col_dq + lanes, c0, a.dim, a.scale, ok,
+                 sptr + (sK - base) + warp * 2048);                      // the streamed tiles have been read
     }
   }
   if (parts > 1 && warp >= kCopy) {
@@ -1072,7 +1073,6 @@ attn_packed_bwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
   if (block < dkv_blocks) dkv_block<DT>(a, maps, block, part, parts);
   else dq_block<DT>(a, maps, block - dkv_blocks, part, parts);
 }
-
 
 // delta_i = do_i . o_i: eight lanes a row, two rows to each lane with all loads in flight; blockIdx.y is the head.  Rows outside the
 // sequences get a value that nothing reads.
