@@ -478,7 +478,10 @@ __device__ __forceinline__ float logit_grad(float lp, float gl, float gh, float 
 template <typename T> __device__ __noinline__ void coarse_row(const T* in, T* out, int vocab, int y, float gl, float gh, float h) {
   __shared__ Sums warp_sums[kLpWarps];
   Sums st{-INFINITY, 0.f, 0.f};
-  for (int i = threadIdx.x; i < vocab; i += kLpThreads) st = join(st, Sums{to_f<T>(in[i]), 1.f, 0.f});
+  for (int i = threadIdx.x; i < vocab; i += kLpThreads) {
+    const float v = to_f<T>(in[i]);
+    st = join(st, Sums{v, v == -INFINITY ? 0.f : 1.f, 0.f});
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     const Sums b{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), 0.f};

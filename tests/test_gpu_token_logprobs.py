@@ -146,6 +146,24 @@ def test_infinities_and_nan(cuda_device, dtype, v):
 
 
 @pytest.mark.parametrize("dtype", [F, BF])
+@pytest.mark.parametrize("v", [3, 33, 5000, 40000])
+def test_masked_rows_far_from_zero(cuda_device, dtype, v):
+    """Tokens at -infinity beside logits whose logsumexp lies beyond 4096: they have no part of the sum."""
+    x, y, gl, gh = make(8, v, dtype, cuda_device, seed=v + 1)
+    for row, (far, every) in enumerate([(6000.0, 2), (-6000.0, 2), (1e30, 3), (-1e30, 3), (4200.0, 1), (torch.finfo(dtype).min, 2), (torch.finfo(dtype).max, 2)]):
+        x[row] = (x[row].float() + far).clamp(min=torch.finfo(dtype).min, max=torch.finfo(dtype).max).to(dtype)
+        x[row, 1::every] = -math.inf
+        y[row] = 0 if row % 2 else 1
+    got = forward(x, y, 2)
+    want = R.logprobs(x, y, 2)
+    b = bounds(x[7:])
+    for name in ("entropy", "lse"):
+        assert ((got[name].double() - want[name]).abs() <= b[name] + 2.0 ** -23 * want[name].abs()).all(), name
+    check_backward(x, y, got, gl, gh)
+    check_backward(x, y, got, gl, None, in_place=True)
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
 def test_strides_and_alignment(cuda_device, dtype):
     """Rows of a wider tensor that start at every place within 16 bytes; gradients with the same and with other strides."""
     import paper_1910_05124_b200 as pm
