@@ -56,7 +56,7 @@ template <int DT, int NT> struct FwdShape {
   // (Two threads to a row, 64 scores each, took 332 us where this takes 289: 8192 + 4099 tokens, 16 heads of 128 on 4.)
   static constexpr int kSoftmaxRegs = NT == 1 ? 208 : 224, kOtherRegs = NT == 1 ? 48 : 56;
   // Tensor-memory columns: S (128 for each tile), O (DT), and for heads of 64 P (64) beside S instead of over it, so that the
-  // next scores are formed while the exponentials of these are.
+  // next scores are formed while the exponentials of these are (8192 tokens, 16 heads of 64, causal: 197 us, over S 205).
   static constexpr int kCols = NT * 256;
   static constexpr bool kApart = DT == 64;
   static constexpr int kBars = 1 + 4 * kStages + 5 * NT;
