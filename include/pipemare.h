@@ -418,7 +418,7 @@ typedef struct {
   int32_t n_seqs;
   int32_t causal;
   int64_t n_tokens;              /* rows of every tensor */
-  float scale;                   /* positive; 1 / sqrt(head_dim) as a rule */
+  float scale;                   /* positive, below 2e38; 1 / sqrt(head_dim) as a rule */
 } pm_attention_desc;
 
 /* lse: [n_heads][n_tokens] float, or NULL where no backward pass follows.  o must not overlap q, k or v. */

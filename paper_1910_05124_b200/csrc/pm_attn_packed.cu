@@ -491,7 +491,8 @@ static pm_status pk_check(const pm_attention_desc* d) {
   if (d->n_seqs < 0 || d->n_tokens < 0) return ops_fail(PM_ERR_INVALID_ARG, "negative size");
   if (d->n_tokens > 0x7fffffff - 128 || d->n_seqs > (1 << 24) || d->n_tokens * d->n_heads > ((int64_t)1 << 33))
     return ops_fail(PM_ERR_SHAPE, "too many tokens, sequences or rows");
-  if (!(d->scale > 0) || d->scale > 3e38f) return ops_fail(PM_ERR_INVALID_ARG, "scale must be positive and finite");
+  // the kernels work with scale log2(e), which has to be finite too
+  if (!(d->scale > 0) || d->scale >= 2e38f) return ops_fail(PM_ERR_INVALID_ARG, "scale must be positive and below 2e38");
   return PM_OK;
 }
 static pm_status pk_view(HeadView& out, const pm_head_view* v, const char* name, int size) {

@@ -95,8 +95,8 @@ class PackedAttention:
         if head_dim > 128:
             _refuse("heads wider than 128", "PM_ERR_UNSUPPORTED")
         scale = head_dim ** -0.5 if scale is None else float(scale)
-        if not 0 < scale < 3e38:
-            _refuse("scale must be positive and finite")
+        if not 0 < scale < 2e38:
+            _refuse("scale must be positive and below 2e38")
         self.n_heads, self.n_kv_heads, self.head_dim, self.causal, self.scale = n_heads, n_kv_heads, head_dim, bool(causal), scale
         self.L = lib()
 

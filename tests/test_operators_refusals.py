@@ -42,7 +42,7 @@ def desc(**kw):
     (dict(n_kv_heads=0), "PM_ERR_INVALID_ARG"), (dict(head_dim=0), "PM_ERR_INVALID_ARG"), (dict(head_dim=129), "PM_ERR_UNSUPPORTED"),
     (dict(n_tokens=-1), "PM_ERR_INVALID_ARG"), (dict(n_seqs=-1), "PM_ERR_INVALID_ARG"), (dict(n_tokens=1 << 31), "PM_ERR_SHAPE"),
     (dict(n_heads=1 << 17, n_kv_heads=1), "PM_ERR_SHAPE"), (dict(scale=0.0), "PM_ERR_INVALID_ARG"), (dict(scale=math.nan), "PM_ERR_INVALID_ARG"),
-    (dict(scale=math.inf), "PM_ERR_INVALID_ARG")])
+    (dict(scale=math.inf), "PM_ERR_INVALID_ARG"), (dict(scale=2.5e38), "PM_ERR_INVALID_ARG")])
 def test_attention_descriptions(L, kw, code):
     assert status(L, attn(L, desc(**kw)))[0] == code
 
@@ -129,6 +129,8 @@ def test_python_checks_come_before_the_library(L):
             pm.PackedAttention(*bad)
     with pytest.raises(pm.PipeMareError):
         pm.PackedAttention(4, 2, 8, scale=0.0)
+    with pytest.raises(pm.PipeMareError):
+        pm.PackedAttention(4, 2, 8, scale=2.5e38)
     op = pm.PackedAttention(4, 2, 8)
     with pytest.raises(pm.PipeMareError, match="CUDA"):
         op.pm_attention_packed_forward(torch.zeros(3, 4, 8), torch.zeros(3, 2, 8), torch.zeros(3, 2, 8), torch.zeros(2, dtype=torch.int32),
