@@ -455,7 +455,8 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
         if (j == 0) {
           m = top;
         } else if (__any_sync(0xffffffffu, !(top <= m + 8.f))) {
-          const float up = top <= m + 8.f ? m : max_nan(m, top), f = ex2(m - up);       // rows that need it not keep theirs
+          // rows that need it not keep theirs, those without a finite score so far among them
+          const float up = top <= m + 8.f ? m : max_nan(m, top), f = up == -INFINITY ? 1.f : ex2(m - up);
           m = up;
           l *= f;
 #pragma unroll
@@ -469,7 +470,8 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
           }
         }
         float2 sum = make_float2(0.f, 0.f);
-        const float2 cc = make_float2(c, c), mm = make_float2(-m, -m);
+        const float shift = m == -INFINITY ? 0.f : -m;       // no finite score so far: nothing but zeros
+        const float2 cc = make_float2(c, c), mm = make_float2(shift, shift);
         auto probabilities = [&](const uint32_t (&x)[32], int q) {
           uint32_t p[16];
 #pragma unroll

@@ -180,6 +180,22 @@ def test_one_value_that_is_not_finite(cuda_device, dtype, lens, H, D):
             assert torch.equal(o[same], clean[same]), (at, bad)
 
 
+@pytest.mark.parametrize("lens,H,D", [([450, 90], 2, 64), ([700], 1, 128), ([700], 40, 64), ([1500], 16, 128), ([700], 2, 33)], ids=str)
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_tiles_of_keys_at_minus_infinity(cuda_device, dtype, lens, H, D):
+    """The first keys have scores of -infinity, tiles of them alone: the same bits as with scores whose exponentials are zero."""
+    op, q, k, v, d_o, cu = make(lens, H, H, D, dtype, cuda_device, seed=14)
+    q, k = q.clone(), k.clone()
+    q[:, :, 1] = 1.0
+    for n in (5, 130, 300):
+        out = []
+        for low in (-3e4, -math.inf):
+            k[:n, :, 1] = low
+            out.append(forward(op, q, k, v, cu))
+        (o0, lse0), (o, lse) = out
+        assert not o0.isnan().any() and torch.equal(o[n:], o0[n:]) and torch.equal(lse[:, n:], lse0[:, n:]), n
+
+
 @pytest.mark.parametrize("lens,H,D", [([150, 90], 2, 64), ([400], 1, 128), ([1500], 16, 128)], ids=str)
 @pytest.mark.parametrize("dtype", [BF, F])
 def test_values_of_masked_keys_count_for_nothing(cuda_device, dtype, lens, H, D):
