@@ -408,9 +408,10 @@ typedef struct {
  *   o_i = sum_j exp(s_ij - lse_i) v_j
  * dtype is the type of every tensor but lse (PM_BF16: products of bf16 values with fp32 sums; the probabilities are
  * rounded to bf16 before they multiply v).  head_dim: 1 to 128.  A value that is not finite spreads over the results of
- * its own sequence (in the backward pass, and through v, to positions before it, too) and to no other.  Entries of
- * cu_seqlens outside 0 .. n_tokens are clipped to that range; if they do not ascend, the results of the sequences concerned
- * are undefined, and no tensor is touched outside its rows. */
+ * its own sequence (in the backward pass, and through v, to positions before it, too) and to no other.  A row whose every
+ * score is -infinity has lse -infinity and no distribution: its o is NaN, and so are its dq and the dk and dv of the keys
+ * that it sees.  Entries of cu_seqlens outside 0 .. n_tokens are clipped to that range; if they do not ascend, the results
+ * of the sequences concerned are undefined, and no tensor is touched outside its rows. */
 typedef struct {
   int32_t dtype;                 /* PM_F32 | PM_BF16 */
   int32_t n_heads, n_kv_heads;   /* n_heads a multiple of n_kv_heads */

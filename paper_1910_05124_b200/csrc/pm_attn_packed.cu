@@ -239,20 +239,22 @@ __global__ void __launch_bounds__(4 * R, R == 64 && DP <= 64 ? 2 : 1) attn_packe
 #pragma unroll
     for (int i = 0; i < 4; ++i) if (tx == 0) { stats[4 * ty + i] = m[i]; stats[R + 4 * ty + i] = l[i]; }
     cluster.sync();
-    // row r's maximum and 1 / sum over the parts
-    auto total = [&](int r, float& top, float& sum) {
+    // row r's maximum, what its exponentials are relative to (zero where every score is -infinity: their difference would be NaN, the
+    // sum is zero), and the sum over the parts
+    auto total = [&](int r, float& top, float& base, float& sum) {
       top = -INFINITY;
       for (int p = 0; p < parts; ++p) top = max_nan(top, cluster.map_shared_rank(stats, p)[r]);
+      base = top == -INFINITY ? 0.f : top;
       sum = 0.f;
-      for (int p = 0; p < parts; ++p) sum += ex2((cluster.map_shared_rank(stats, p)[r] - top) * kLog2e) * cluster.map_shared_rank(stats, p)[R + r];
+      for (int p = 0; p < parts; ++p) sum += ex2((cluster.map_shared_rank(stats, p)[r] - base) * kLog2e) * cluster.map_shared_rank(stats, p)[R + r];
     };
     // weights of the parts, once per row of this block's share: [parts][R] behind the statistics
     float* weights = stats + 2 * R;
     const int r0 = R * part / parts, r1 = R * (part + 1) / parts;
     for (int r = r0 + threadIdx.x; r < r1; r += 4 * R) {
-      float top, sum;
-      total(r, top, sum);
-      for (int p = 0; p < parts; ++p) weights[p * R + r] = ex2((cluster.map_shared_rank(stats, p)[r] - top) * kLog2e) / sum;
+      float top, base, sum;
+      total(r, top, base, sum);
+      for (int p = 0; p < parts; ++p) weights[p * R + r] = ex2((cluster.map_shared_rank(stats, p)[r] - base) * kLog2e) / sum;
       if (a.lse && q0 + r < s.len) a.lse[(int64_t)h * a.tokens + s.begin + q0 + r] = top + logf(sum);
     }
     __syncthreads();

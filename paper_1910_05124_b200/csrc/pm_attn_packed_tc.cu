@@ -520,8 +520,9 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
             const float x = cluster.map_shared_rank(stats, p)[r];
             top = top != top || x != x ? NAN : fmaxf(top, x);
           }
-          for (int p = 0; p < parts; ++p) sum += ex2(cluster.map_shared_rank(stats, p)[r] - top) * cluster.map_shared_rank(stats, p)[TC_ROWS + r];
-          for (int p = 0; p < parts; ++p) weights[p * TC_ROWS + r] = ex2(cluster.map_shared_rank(stats, p)[r] - top) / sum;
+          const float base = top == -INFINITY ? 0.f : top;             // every score -infinity: their difference would be NaN, the sum is zero
+          for (int p = 0; p < parts; ++p) sum += ex2(cluster.map_shared_rank(stats, p)[r] - base) * cluster.map_shared_rank(stats, p)[TC_ROWS + r];
+          for (int p = 0; p < parts; ++p) weights[p * TC_ROWS + r] = ex2(cluster.map_shared_rank(stats, p)[r] - base) / sum;
           if (a.lse && row < s.len) a.lse[(int64_t)h * a.tokens + s.begin + row] = (top + log2f(sum)) * kLn2;
         }
         asm volatile("barrier.cta.sync 1, 128;" ::: "memory");
