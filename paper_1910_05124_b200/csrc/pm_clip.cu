@@ -185,8 +185,8 @@ __global__ void __launch_bounds__(kClipThreads, 6) clip_scale_kernel(const __gri
   acc = block_sum(acc, scratch);
   if (threadIdx.x == 0) {
     const double norm = sqrt(acc);
-    // an infinite or undefined norm clips nothing: the caller sees it in norm_out
-    const float scale = (norm > max_norm && isfinite(norm)) ? (float)(max_norm / norm) : 1.f;
+    // an infinite or undefined norm clips nothing: the caller sees it in norm_out (what counts is the norm as reported, in fp32)
+    const float scale = (norm > max_norm && isfinite((float)norm)) ? (float)(max_norm / norm) : 1.f;
     s_scale = scale;
     if (blockIdx.x == 0 && norm_out) { *norm_out = (float)norm; *scale_out = scale; }
   }

@@ -1,0 +1,26 @@
+"""Gradient clipping where the norm or the factor leaves the range of fp32."""
+import math
+
+import pytest
+import torch
+
+import operators_reference as R
+from test_gpu_grad_clip import make, run
+
+pytestmark = pytest.mark.gpu
+BF, F = torch.bfloat16, torch.float32
+PAIRS = [(F, F, True), (BF, BF, True), (F, F, False), (BF, F, False), (F, BF, False), (BF, BF, False)]
+IDS = [f"{str(s)[6:]}-{str(d)[6:]}-{'in_place' if i else 'apart'}" for s, d, i in PAIRS]
+
+
+@pytest.mark.parametrize("src,dst,in_place", PAIRS, ids=IDS)
+@pytest.mark.parametrize("max_norm", [1.0, 1e-6, 1e30, 1e39])
+def test_norm_above_the_range_of_fp32(cuda_device, src, dst, in_place, max_norm):
+    """9000 gradients near 1e38: a norm near 1e40 is reported as infinity, and an infinite norm scales nothing."""
+    g = [(x.double().clamp(-3, 3) * 1e38).to(src) for x in make([9000, 50, 8192], [src], cuda_device, seed=6)]
+    keep = [x.clone() for x in g]
+    outs = None if in_place else [torch.zeros(x.numel(), dtype=dst, device=cuda_device) for x in g]
+    assert R.clip(g, math.inf)[0] > 3.5e38
+    assert run(g, max_norm, outs) == (math.inf, 1.0)
+    for a, b in zip(keep, g if in_place else outs):
+        assert torch.equal(a.to(dst), b)
