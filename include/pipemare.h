@@ -465,7 +465,8 @@ pm_status pm_token_logprobs_backward(const void* logits, int32_t dtype, int64_t 
  * norm and scale: one device float each.  dst may be src itself (clipping in place, same type), or another tensor of
  * either type, such as a slice of the gradient arena; otherwise sources and destinations do not overlap.  The squares are
  * summed in 64 bits, so none leaves the range.  A norm that is infinite in fp32 or NaN is reported as such and scales
- * nothing (scale 1).  tensors: host array, read during the call; empty tensors are allowed.  max_norm: positive, infinity to
+ * nothing (scale 1).  A scale below fp32's normal range is reported with the few bits it has there and applied in 64 bits.
+ * tensors: host array, read during the call; empty tensors are allowed.  max_norm: positive, infinity to
  * measure the norm alone.  workspace: device, at least pm_clip_gradients_workspace_bytes(n_tensors) bytes. */
 typedef struct {
   const void* src;               /* device */

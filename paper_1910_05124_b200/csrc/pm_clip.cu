@@ -10,6 +10,7 @@
 // The list of tensors travels as a kernel parameter (32 bytes a tensor, up to 1000 a launch), so a call copies nothing to the
 // device and can be captured into a graph.  Each tensor is cut into chunks of kChunk elements, a block takes a contiguous range
 // of chunks.
+#include <cfloat>
 #include <cmath>
 
 #include "pm_ops.cuh"
@@ -173,11 +174,18 @@ __device__ __forceinline__ void clip_chunk(const S* src, D* dst, int n, bool vec
   }
 }
 
+// The same with a factor below the normal range of fp32, where its own rounding would be that of a few bits: products in 64 bits,
+// rounded to fp32 as the others.  Out of line: such a norm is above 2^126 max_norm, the other path keeps its registers.
+template <typename S, typename D> __device__ __noinline__ void clip_chunk_tiny(const S* src, D* dst, int n, double factor) {
+  for (int i = threadIdx.x; i < n; i += kClipThreads) dst[i] = from_f<D>((float)((double)to_f<S>(src[i]) * factor));
+}
+
 template <int CAP>
 __global__ void __launch_bounds__(kClipThreads, 6) clip_scale_kernel(const __grid_constant__ ClipTable<CAP> t, const double* partials, int n_partials,
                                                                     double max_norm, float* norm_out, float* scale_out) {
   __shared__ double scratch[kClipThreads / 32];
   __shared__ float s_scale;
+  __shared__ double s_factor;
   pdl_wait();
   pdl_trigger();
   double acc = 0.0;
@@ -186,12 +194,18 @@ __global__ void __launch_bounds__(kClipThreads, 6) clip_scale_kernel(const __gri
   if (threadIdx.x == 0) {
     const double norm = sqrt(acc);
     // an infinite or undefined norm clips nothing: the caller sees it in norm_out (what counts is the norm as reported, in fp32)
-    const float scale = (norm > max_norm && isfinite((float)norm)) ? (float)(max_norm / norm) : 1.f;
+    const double factor = norm > max_norm && isfinite((float)norm) ? max_norm / norm : 1.0;
+    const float scale = (float)factor;
     s_scale = scale;
+    s_factor = factor;
     if (blockIdx.x == 0 && norm_out) { *norm_out = (float)norm; *scale_out = scale; }
   }
   __syncthreads();
   const float scale = s_scale;
+  auto clip = [&](auto* src, auto* dst, int n, bool vec) {
+    if (scale < FLT_MIN) clip_chunk_tiny(src, dst, n, s_factor);
+    else clip_chunk(src, dst, n, vec, scale);
+  };
   const uint32_t c0 = (uint32_t)((uint64_t)t.chunks * blockIdx.x / gridDim.x), c1 = (uint32_t)((uint64_t)t.chunks * (blockIdx.x + 1) / gridDim.x);
   if (c0 >= c1) return;
   uint32_t e = clip_find(t, c1 - 1);
@@ -205,12 +219,12 @@ __global__ void __launch_bounds__(kClipThreads, 6) clip_scale_kernel(const __gri
     const bool sb = flags & CF_SRC_BF16, db = flags & CF_DST_BF16;
     if (sb) {
       const __nv_bfloat16* s = static_cast<const __nv_bfloat16*>(t.e[e].src) + begin;
-      if (db) clip_chunk(s, static_cast<__nv_bfloat16*>(t.e[e].dst) + begin, n, vec, scale);
-      else clip_chunk(s, static_cast<float*>(t.e[e].dst) + begin, n, vec, scale);
+      if (db) clip(s, static_cast<__nv_bfloat16*>(t.e[e].dst) + begin, n, vec);
+      else clip(s, static_cast<float*>(t.e[e].dst) + begin, n, vec);
     } else {
       const float* s = static_cast<const float*>(t.e[e].src) + begin;
-      if (db) clip_chunk(s, static_cast<__nv_bfloat16*>(t.e[e].dst) + begin, n, vec, scale);
-      else clip_chunk(s, static_cast<float*>(t.e[e].dst) + begin, n, vec, scale);
+      if (db) clip(s, static_cast<__nv_bfloat16*>(t.e[e].dst) + begin, n, vec);
+      else clip(s, static_cast<float*>(t.e[e].dst) + begin, n, vec);
     }
   }
 }

@@ -24,3 +24,22 @@ def test_norm_above_the_range_of_fp32(cuda_device, src, dst, in_place, max_norm)
     assert run(g, max_norm, outs) == (math.inf, 1.0)
     for a, b in zip(keep, g if in_place else outs):
         assert torch.equal(a.to(dst), b)
+
+
+@pytest.mark.parametrize("src,dst,in_place", PAIRS, ids=IDS)
+@pytest.mark.parametrize("size,max_norm", [(1e36, 1e-6), (1e36, 1e-10), (1e34, 1e-4), (1e30, 1e-12), (1e36, 1e-30), (1e20, 1e-30), (1.0, 1e-44), (1e36, 1e-50), (1.0, 1e-300)])
+def test_factor_below_the_normal_range_of_fp32(cuda_device, src, dst, in_place, size, max_norm):
+    """The factor itself has few bits there, or none; what it scales has them all."""
+    g = [(x.double().clamp(-3, 3) * size).to(src) for x in make([9000, 50, 8192], [src], cuda_device, seed=7)]
+    want_norm, want_scale = R.clip(g, max_norm)
+    before = [x.clone() for x in g]
+    outs = None if in_place else [torch.zeros(x.numel(), dtype=dst, device=cuda_device) for x in g]
+    norm, scale = run(g, max_norm, outs)
+    assert abs(norm - want_norm) <= 4 * R.U32 * want_norm
+    assert abs(scale - want_scale) <= 5 * R.U32 * want_scale + 2.0 ** -150
+    for a, b in zip(before, g if in_place else outs):
+        want = a.double() * want_scale
+        # the norm's error, the 64-bit factor's, the rounding to fp32 and that to the result's type; below 2^-126 halves of the smallest steps
+        bound = (4 * R.U32 + R.U32 + 2.0 ** -50 + R.u(dst)) * want.abs() + 2.0 ** -150 + torch.finfo(dst).smallest_normal * R.u(dst)
+        off = (b.double() - want).abs() - bound
+        assert float(off.max()) <= 0, float(off.max())
