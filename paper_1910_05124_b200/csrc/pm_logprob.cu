@@ -23,7 +23,10 @@ namespace cg = cooperative_groups;
 constexpr int kLpThreads = 256;
 constexpr int kLpWarps = kLpThreads / 32;
 constexpr int kLpMaxK = 32;
-constexpr int kLpList = 512;                      // candidates; about k (1 + log(32 / (32 - k))) are expected, 130 for k = 32
+// Candidates of a block or warp.  Of independent logits 32 (1/32 + 1/31 + ... + 1/(33 - k)) reach the threshold on average: 9 for k = 8,
+// 31 for 20, 130 for 32, there with a spread of 39; more than n with the chance that 33 - k of 32 parts have a maximum of e^(-n/32) of the
+// elements.  512 are too few in 4 rows of a million at k = 32.
+constexpr int kLpList = 512;
 constexpr int kLpMaxCluster = 8;
 
 struct LogprobArgs {
@@ -361,17 +364,15 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) logprob_kernel(Logpro
 // Short rows: a warp to each, nothing shared between warps; for rows of up to 4 KB, and of up to 16 KB where there are many.  us with a warp / a block to a row, fp32, five alternatives: 16 x 200 4.4 / 6.3,
 // 300 x 1000 6.3 / 6.3, 1200 x 2000 8.5 / 10.4, 2400 x 4000 15.6 / 18.6; but 40 x 3000 9.2 / 6.4 and 1345 x 8191 30.9 / 27.3.
 constexpr int kLpShortBytes = 4096, kLpMidBytes = 16384, kLpMidRows = 1024;
-constexpr int kLpShortList = 160;
-
-struct LpWarpShared {
-  uint8_t hit[32];
-  float v[kLpShortList];
-  int id[kLpShortList];
-};
+// Candidates of a warp: 160 are too few in 3 rows of a million at k = 28, but in 18 of a hundred at k = 32, and the launch waits for such a row's
+// k passes: 2400 x 4000 fp32, k = 32, 350 us with 160, 90 with 512.  Longer lists leave less of L1 to the rows: k = 20, 37 with 512, 33 with 160.
+constexpr int kLpShortList = 160, kLpShortK = 28;
+__host__ __device__ constexpr int lp_short_list(int k) { return k <= kLpShortK ? kLpShortList : kLpList; }
+__host__ __device__ constexpr int lp_short_bytes(int list) { return list * 8 + 32; }       // of a warp
 
 template <typename T, bool TOP, bool ENTROPY>
 __global__ void __launch_bounds__(kLpThreads) logprob_short_kernel(LogprobArgs a) {
-  __shared__ LpWarpShared shared[TOP ? kLpWarps : 1];
+  extern __shared__ float lp_lists[];             // of each warp: the candidates' values, their ids, and the lanes that reach the threshold
   constexpr int U = 4, N = Vec<T>::n;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t row = (int64_t)blockIdx.x * kLpWarps + warp;
@@ -410,15 +411,18 @@ __global__ void __launch_bounds__(kLpThreads) logprob_short_kernel(LogprobArgs a
       if (lane < k) r.write_top(a, row, lane, 0.f, 0);
       return;
     }
-    LpWarpShared& sh = shared[warp];
+    const int list = lp_short_list(k);
+    float* const list_v = lp_lists + warp * (lp_short_bytes(list) / 4);
+    int* const list_id = reinterpret_cast<int*>(list_v + list);
+    uint8_t* const hit = reinterpret_cast<uint8_t*>(list_id + list);
     const float th = __shfl_sync(0xffffffffu, sorted_down(mine), k - 1);
     const unsigned hits = __ballot_sync(0xffffffffu, mine >= th);
-    if (mine >= th) sh.hit[__popc(hits & ((1u << lane) - 1))] = (uint8_t)lane;
+    if (mine >= th) hit[__popc(hits & ((1u << lane) - 1))] = (uint8_t)lane;
     __syncwarp();
     const int each = (x.count + 31) / 32, pairs = __popc(hits) * each;
     int n = 0;
     for (int base = 0; base < pairs; base += 32) {   // the vectors of the lanes that reach the threshold: (lane, vector) pairs over the lanes
-      const int p = base + lane, at = p < pairs ? sh.hit[p / each] + p % each * 32 : x.count;
+      const int p = base + lane, at = p < pairs ? hit[p / each] + p % each * 32 : x.count;
       float v[N];
       if (at < x.count) x.get(at, v);
 #pragma unroll
@@ -427,17 +431,17 @@ __global__ void __launch_bounds__(kLpThreads) logprob_short_kernel(LogprobArgs a
         const bool in = at < x.count && id >= 0 && id < x.vocab && v[i] >= th;
         const unsigned all = __ballot_sync(0xffffffffu, in);
         const int to = n + __popc(all & ((1u << lane) - 1));
-        if (in && to < kLpShortList) { sh.v[to] = v[i]; sh.id[to] = id; }
+        if (in && to < list) { list_v[to] = v[i]; list_id[to] = id; }
         n += __popc(all);
       }
     }
     __syncwarp();
-    if (n <= kLpShortList) {
+    if (n <= list) {
       for (int i = lane; i < n; i += 32) {
-        const float v = sh.v[i];
-        const int id = sh.id[i];
+        const float v = list_v[i];
+        const int id = list_id[i];
         int rank = 0;
-        for (int b = 0; b < n; ++b) rank += beats(sh.v[b], sh.id[b], v, id);
+        for (int b = 0; b < n; ++b) rank += beats(list_v[b], list_id[b], v, id);
         if (rank < k) r.write_top(a, row, rank, v, id);
       }
       return;
@@ -576,7 +580,8 @@ template <typename T> static cudaError_t logprob_launch(const LogprobArgs& a, in
   if (bytes <= kLpShortBytes || (bytes <= kLpMidBytes && a.rows >= kLpMidRows)) {
     void (*kernel)(LogprobArgs) = a.top_k ? (a.entropy ? logprob_short_kernel<T, true, true> : logprob_short_kernel<T, true, false>)
                                           : (a.entropy ? logprob_short_kernel<T, false, true> : logprob_short_kernel<T, false, false>);
-    return launch_pdl(kernel, dim3((unsigned)((a.rows + kLpWarps - 1) / kLpWarps)), dim3(kLpThreads), 0, st, false, a);
+    const int smem = a.top_k ? kLpWarps * lp_short_bytes(lp_short_list(a.top_k)) : 0;
+    return launch_pdl(kernel, dim3((unsigned)((a.rows + kLpWarps - 1) / kLpWarps)), dim3(kLpThreads), smem, st, false, a);
   }
   // Rows of up to 64 KB take 128 threads.  us with 128 / 256: 1345 x 8191 fp32, both passes, 27 / 29; 4096 x 32000 bf16 with eight
   // alternatives 76 / 78; but the same in fp32, rows of 128 KB, 121 / 103.
