@@ -422,12 +422,13 @@ typedef struct {
   float scale;                   /* positive, below 2e38; 1 / sqrt(head_dim) as a rule */
 } pm_attention_desc;
 
-/* lse: [n_heads][n_tokens] float, or NULL where no backward pass follows.  o must not overlap q, k or v. */
+/* lse: [n_heads][n_tokens] float, or NULL where no backward pass follows.  o and lse overlap neither each other nor an input;
+ * such calls are refused (element by element, so slices and interleaved heads of one buffer are allowed). */
 pm_status pm_attention_packed_forward(const pm_attention_desc* desc, const pm_head_view* q, const pm_head_view* k,
                                       const pm_head_view* v, const int32_t* cu_seqlens, const pm_head_view* o, float* lse,
                                       void* stream);
 /* Gradients of q, k, v from d_o and the forward pass's o and lse; dk and dv are summed over the query heads that share
- * them.  dq, dk, dv overlap neither each other nor the inputs.  workspace: at least
+ * them.  dq, dk, dv and the workspace overlap neither each other nor an input (refused, as above).  workspace: at least
  * pm_attention_packed_workspace_bytes(desc) bytes of device memory, 16-byte aligned. */
 uint64_t pm_attention_packed_workspace_bytes(const pm_attention_desc* desc);
 pm_status pm_attention_packed_backward(const pm_attention_desc* desc, const pm_head_view* q, const pm_head_view* k,

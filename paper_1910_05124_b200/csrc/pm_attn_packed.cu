@@ -504,11 +504,14 @@ static pm_status pk_view(HeadView& out, const pm_head_view* v, const char* name,
   out = HeadView{v->data, v->token_stride, v->head_stride};
   return PM_OK;
 }
-// what is written may not be one of the other tensors
-static pm_status pk_apart(const HeadView* const* written, int n_written, const HeadView* const* read, int n_read) {
+static Extent pk_extent(const HeadView& x, int64_t tokens, int heads, int dim, int size) {
+  return Extent{(__int128)reinterpret_cast<uintptr_t>(x.data), (__int128)x.token * size, tokens, (__int128)x.head * size, heads, (__int128)dim * size};
+}
+// what is written shares no memory with the other tensors
+static pm_status pk_apart(const Extent* written, int n_written, const Extent* read, int n_read) {
   for (int i = 0; i < n_written; ++i) {
-    for (int j = 0; j < n_read; ++j) if (written[i]->data == read[j]->data) return ops_fail(PM_ERR_INVALID_ARG, "an output is one of the inputs");
-    for (int j = 0; j < i; ++j) if (written[i]->data == written[j]->data) return ops_fail(PM_ERR_INVALID_ARG, "two outputs are the same tensor");
+    for (int j = 0; j < n_read; ++j) if (extents_share(written[i], read[j])) return ops_fail(PM_ERR_INVALID_ARG, "an output overlaps one of the inputs");
+    for (int j = 0; j < i; ++j) if (extents_share(written[i], written[j])) return ops_fail(PM_ERR_INVALID_ARG, "two outputs overlap or are the same tensor");
   }
   return PM_OK;
 }
@@ -536,8 +539,10 @@ pm_status pm_attention_packed_forward(const pm_attention_desc* d, const pm_head_
   if (const pm_status s = pk_view(a.k, k, "k", size)) return s;
   if (const pm_status s = pk_view(a.v, v, "v", size)) return s;
   if (const pm_status s = pk_view(a.o, o, "o", size)) return s;
-  const HeadView *written[] = {&a.o}, *read[] = {&a.q, &a.k, &a.v};
-  if (const pm_status s = pk_apart(written, 1, read, 3)) return s;
+  auto all = [&](const HeadView& x, int heads) { return pk_extent(x, a.tokens, heads, a.dim, size); };
+  const Extent written[] = {all(a.o, a.heads), dense_extent(lse, 4 * a.tokens * a.heads)};
+  const Extent read[] = {all(a.q, a.heads), all(a.k, a.kv_heads), all(a.v, a.kv_heads), dense_extent(cu_seqlens, 4 * ((int64_t)a.n_seqs + 1))};
+  if (const pm_status s = pk_apart(written, 2, read, 4)) return s;
   const cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t e = attn_packed_tc_takes(a, d->dtype, false) ? attn_packed_tc_forward(a, st)
                         : d->dtype == PM_BF16 ? pk_run<__nv_bfloat16>(a, false, st) : pk_run<float>(a, false, st);
@@ -565,11 +570,15 @@ pm_status pm_attention_packed_backward(const pm_attention_desc* d, const pm_head
   if (const pm_status s = pk_view(a.dq, dq, "dq", size)) return s;
   if (const pm_status s = pk_view(a.dk, dk, "dk", size)) return s;
   if (const pm_status s = pk_view(a.dv, dv, "dv", size)) return s;
-  const HeadView *written[] = {&a.dq, &a.dk, &a.dv}, *read[] = {&a.q, &a.k, &a.v, &a.o, &a.d_o};
-  if (const pm_status s = pk_apart(written, 3, read, 5)) return s;
+  auto all = [&](const HeadView& x, int heads) { return pk_extent(x, a.tokens, heads, a.dim, size); };
+  const Extent others[] = {all(a.dq, a.heads), all(a.dk, a.kv_heads), all(a.dv, a.kv_heads), all(a.q, a.heads), all(a.k, a.kv_heads), all(a.v, a.kv_heads),
+                           all(a.o, a.heads), all(a.d_o, a.heads), dense_extent(lse, 4 * a.tokens * a.heads),
+                           dense_extent(cu_seqlens, 4 * ((int64_t)a.n_seqs + 1))};
+  if (const pm_status s = pk_apart(others, 3, others + 3, 7)) return s;
   const uint64_t need = pm_attention_packed_workspace_bytes(d);
   if (!workspace || workspace_bytes < need) return ops_fail(PM_ERR_NOMEM, "workspace too small: need %llu bytes", (unsigned long long)need);
   if (!aligned_to(workspace, 4)) return ops_fail(PM_ERR_INVALID_ARG, "workspace must be 4-byte aligned");
+  for (const Extent& x : others) if (extents_share(dense_extent(workspace, (int64_t)need), x)) return ops_fail(PM_ERR_INVALID_ARG, "the workspace overlaps a tensor");
   a.delta = static_cast<float*>(workspace);
   const cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t e = attn_packed_tc_takes(a, d->dtype, true) ? attn_packed_tc_backward(a, st)
