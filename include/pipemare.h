@@ -423,7 +423,8 @@ typedef struct {
 } pm_attention_desc;
 
 /* lse: [n_heads][n_tokens] float, or NULL where no backward pass follows.  o and lse overlap neither each other nor an input;
- * such calls are refused (element by element, so slices and interleaved heads of one buffer are allowed). */
+ * such calls are refused (element by element, so slices and interleaved heads of one buffer are allowed; tensors of
+ * different token strides whose spans meet are looked through up to 1024 pairs of rows and left to the caller beyond). */
 pm_status pm_attention_packed_forward(const pm_attention_desc* desc, const pm_head_view* q, const pm_head_view* k,
                                       const pm_head_view* v, const int32_t* cu_seqlens, const pm_head_view* o, float* lse,
                                       void* stream);
@@ -447,7 +448,8 @@ pm_status pm_attention_packed_status(void* stream);
  * targets and logprob [rows] go together (both NULL: not wanted); a target < 0 is padding (logprob 0, no gradient
  * through it), one >= vocab gives NaN.  entropy, lse: [rows] or NULL.  top_logprob, top_ids: [rows, top_k], top_k 0 to 32.
  * Logits of -infinity have probability 0; a row of nothing else has lse and log probabilities -infinity, entropy 0 and no
- * gradient.  A row that holds a NaN or +infinity has no distribution: its float results are NaN, its ids -1. */
+ * gradient.  A row that holds a NaN or +infinity has no distribution: its float results are NaN, its ids -1.  Results that
+ * overlap each other, the logits or the targets are refused. */
 pm_status pm_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t vocab, int64_t row_stride,
                             const int32_t* targets, float* logprob, float* entropy, float* lse, int32_t top_k,
                             float* top_logprob, int32_t* top_ids, void* stream);
@@ -455,7 +457,7 @@ pm_status pm_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int
  * (either may be NULL), with lse and (for d_entropy) entropy as the forward call wrote them:
  *   d_logits_j = d_logprob ([j = y] - p_j) - d_entropy p_j (log p_j + entropy).
  * p_j = exp(x_j - lse); in rows with |lse| > 4096, where a rounded lse no longer resolves p, it is taken from the logits.
- * d_logits may be logits itself (same strides); otherwise the two do not overlap. */
+ * d_logits may be logits itself (same strides); any other overlap of it with an input is refused. */
 pm_status pm_token_logprobs_backward(const void* logits, int32_t dtype, int64_t rows, int32_t vocab, int64_t row_stride,
                                      const int32_t* targets, const float* lse, const float* entropy,
                                      const float* d_logprob, const float* d_entropy, void* d_logits, int64_t grad_stride,

@@ -611,10 +611,13 @@ pm_status pm_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int
   if ((targets == nullptr) != (logprob == nullptr)) return ops_fail(PM_ERR_INVALID_ARG, "targets and logprob are given together or not at all");
   if (top_k < 0 || top_k > kLpMaxK || top_k > vocab) return ops_fail(PM_ERR_INVALID_ARG, "top_k must be 0 to 32 and at most the vocabulary size");
   if (top_k > 0 && (!top_logprob || !top_ids)) return ops_fail(PM_ERR_INVALID_ARG, "top_k without a place for the alternatives");
-  const void* outs[] = {logprob, entropy, lse, top_k > 0 ? top_logprob : nullptr, top_k > 0 ? top_ids : nullptr};
-  for (int i = 0; i < 5; ++i)
-    for (int j = 0; j < i; ++j)
-      if (outs[i] && outs[i] == outs[j]) return ops_fail(PM_ERR_INVALID_ARG, "two results share their memory");
+  const Extent outs[] = {dense_extent(logprob, 4 * rows), dense_extent(entropy, 4 * rows), dense_extent(lse, 4 * rows),
+                         dense_extent(top_k > 0 ? top_logprob : nullptr, 4 * rows * top_k), dense_extent(top_k > 0 ? top_ids : nullptr, 4 * rows * top_k)};
+  const Extent ins[] = {rows_extent(logits, rows, row_stride, vocab, dtype == PM_BF16 ? 2 : 4), dense_extent(targets, 4 * rows)};
+  for (int i = 0; i < 5; ++i) {
+    for (int j = 0; j < i; ++j) if (extents_share(outs[i], outs[j])) return ops_fail(PM_ERR_INVALID_ARG, "two results share their memory");
+    for (const Extent& x : ins) if (extents_share(outs[i], x)) return ops_fail(PM_ERR_INVALID_ARG, "a result overlaps the logits or the targets");
+  }
   // A cluster per row once the rows leave SMs without work, as long as each block keeps some vectors per thread.
   const int vectors = vocab / (dtype == PM_BF16 ? 8 : 4);
   int parts = 1;
@@ -635,6 +638,11 @@ pm_status pm_token_logprobs_backward(const void* logits, int32_t dtype, int64_t 
   if (d_logprob && !targets) return ops_fail(PM_ERR_INVALID_ARG, "a gradient of logprob needs the targets");
   if (d_entropy && !entropy) return ops_fail(PM_ERR_INVALID_ARG, "a gradient of the entropy needs the entropy");
   const int size = dtype == PM_BF16 ? 2 : 4, per_block = kLbVectors * kLpThreads * 16 / size;
+  const Extent out = rows_extent(d_logits, rows, grad_stride, vocab, size);
+  const void* const per_row_inputs[] = {d_logprob ? targets : nullptr, lse, d_entropy ? entropy : nullptr, d_logprob, d_entropy};
+  for (const void* p : per_row_inputs) if (extents_share(out, dense_extent(p, 4 * rows))) return ops_fail(PM_ERR_INVALID_ARG, "d_logits overlaps another input");
+  if ((d_logits != logits || (rows > 1 && grad_stride != row_stride)) && extents_share(out, rows_extent(logits, rows, row_stride, vocab, size)))
+    return ops_fail(PM_ERR_INVALID_ARG, "d_logits overlaps the logits without being them");
   // both rows at the same place within their 16-byte blocks, in every row: vectors; else single elements
   const bool vec = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(d_logits)) & 15) == 0 &&
                    ((row_stride - grad_stride) * size) % 16 == 0;

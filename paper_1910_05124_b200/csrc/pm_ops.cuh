@@ -32,7 +32,7 @@ inline Extent joined(Extent x) {
   return x;
 }
 inline bool joined_share(Extent a, Extent b) {
-  constexpr int kMost = 1 << 16;                  // pairs of pieces that are looked at
+  constexpr int kMost = 1024;                     // pairs of pieces that are looked at: 0.1 ms
   if (a.at >= b.at + b.outer * (b.n_outer - 1) + b.inner * (b.n_inner - 1) + b.bytes) return false;
   if (b.at >= a.at + a.outer * (a.n_outer - 1) + a.inner * (a.n_inner - 1) + a.bytes) return false;
   if (a.n_outer == 1) a.outer = b.outer;          // one piece has any stride

@@ -77,7 +77,9 @@ def test_views_of_one_projection(L):
     # interleaved heads: every second one of a row, then the ones between
     even = (at, 2 * H * D, 2 * D), (at + D * size, 2 * H * D, 2 * D)
     assert call(even[0], even[1], (P + (9 << 26), K * D, D)) == "PM_ERR_NOMEM"
+    T = 16                                                   # of different token strides, as many pairs as are looked at
     assert call(even[0], (even[1][0], 2 * H * D + 1, 2 * D), (P + (9 << 26), K * D, D)) == "PM_ERR_INVALID_ARG"
+    T = 1000
     # an output that reaches into an input's last rows, without starting where it does
     assert call((inputs[3][0] + (T - 1) * H * D * size, H * D, D), (at, K * D, D), (P + (9 << 26), K * D, D)) == "PM_ERR_INVALID_ARG"
 
@@ -103,3 +105,35 @@ def test_attention_forward(L):
                dict(lse=P + (3 << 20) + 4), dict(lse=P + (5 << 20) + 4), dict(o=P + (2 << 20) - 4 * (T * H * D - 1))):
         status, message = call(**kw)
         assert status == "PM_ERR_INVALID_ARG" and "output" in message, (kw, message)
+
+
+def logprobs(L, rows, vocab, stride, logits, targets, logprob, entropy, lse, k, top, ids):
+    st = L.pm_token_logprobs(logits, B.PM_F32, rows, vocab, stride, targets, logprob, entropy, lse, k, top, ids, None)
+    return L.pm_status_string(st).decode(), L.pm_last_error(None).decode()
+
+
+def test_logprob_results(L):
+    rows, vocab, k = 10, 100, 4
+    at = dict(logits=P, targets=P + (1 << 20), logprob=P + (2 << 20), entropy=P + (3 << 20), lse=P + (4 << 20), k=k, top=P + (5 << 20), ids=P + (6 << 20))
+    for stride in (100, 108):
+        for kw in (dict(logprob=P + 36), dict(entropy=P + 4 * 9 * stride + 396), dict(lse=P - 36), dict(top=P + 400 - 4), dict(ids=P + (1 << 20) + 36),
+                   dict(entropy=P + (2 << 20) + 36), dict(lse=P + (5 << 20) + 4 * rows * k - 4), dict(logprob=P + (4 << 20) - 36), dict(ids=P + (5 << 20) + 4)):
+            status, message = logprobs(L, rows, vocab, stride, **dict(at, **kw))
+            assert status == "PM_ERR_INVALID_ARG" and ("share" in message or "overlaps" in message), (stride, kw, message)
+
+
+def test_logprob_gradient(L):
+    rows, vocab = 10, 100
+
+    def call(d_logits, stride=100, grad_stride=100, lse=P + (1 << 20), **kw):
+        a = dict(targets=P + (2 << 20), entropy=P + (3 << 20), d_logprob=P + (4 << 20), d_entropy=P + (5 << 20))
+        a.update(kw)
+        st = L.pm_token_logprobs_backward(P, B.PM_BF16, rows, vocab, stride, a["targets"], lse, a["entropy"], a["d_logprob"], a["d_entropy"], d_logits,
+                                          grad_stride, None)
+        return L.pm_status_string(st).decode(), L.pm_last_error(None).decode()
+    far = P + (8 << 20)
+    for a, kw in (((P + 2,), {}), ((P - 2,), {}), ((P + 2 * 999,), {}), ((P,), dict(grad_stride=108)), ((P + 198, 108, 108), {}), ((P + 200, 108, 100), {}),
+                  ((far,), dict(lse=far + 1998)), ((far,), dict(targets=far - 36)), ((far, 108, 108), dict(d_logprob=far + 216 * 9 - 36)),
+                  ((far,), dict(entropy=far + 400)), ((far,), dict(d_entropy=far + 4))):
+        status, message = call(*a, **kw)
+        assert status == "PM_ERR_INVALID_ARG" and "overlaps" in message, (a, kw, message)
