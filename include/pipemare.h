@@ -439,8 +439,12 @@ pm_status pm_attention_packed_backward(const pm_attention_desc* desc, const pm_h
                                        uint64_t workspace_bytes, void* stream);
 
 /* Every wait inside the tensor-core kernels is bounded (about one second).  One that runs out is a defect: the rows
- * concerned are NaN, and this call, which synchronises the stream, returns PM_ERR_TIMEOUT once. */
+ * concerned are NaN, and this call, which synchronises the stream, returns PM_ERR_TIMEOUT once.  A device keeps one record,
+ * the first since the last call, of all streams and callers; the call of any of them takes it.
+ * The self-test enqueues a one-thread kernel (no tensor memory, no copy in flight) whose wait on a barrier on which nothing
+ * arrives runs out after limit_cycles SM cycles (1 to 10^9; a few million are milliseconds) and is recorded like the others. */
 pm_status pm_attention_packed_status(void* stream);
+pm_status pm_attention_packed_selftest_wait_timeout(int64_t limit_cycles, void* stream);
 
 /* Per row of logits [rows, vocab] (row_stride elements apart, dtype PM_F32 | PM_BF16):
  *   lse = log sum_j exp(x_j);  logprob = x_y - lse for the target y;  entropy = lse - sum_j p_j x_j;  the top_k largest

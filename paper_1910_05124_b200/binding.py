@@ -122,6 +122,7 @@ def lib():
     L.pm_attention_packed_workspace_bytes.restype = u64
     L.pm_attention_packed_backward.argtypes = [desc, view, view, view, view, vp, view, vp, view, view, view, vp, u64, vp]
     L.pm_attention_packed_status.argtypes = [vp]
+    L.pm_attention_packed_selftest_wait_timeout.argtypes = [i64, vp]
     L.pm_token_logprobs.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp, vp, i32, vp, vp, vp]
     L.pm_token_logprobs_backward.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp, vp, vp, vp, i64, vp]
     L.pm_clip_gradients_workspace_bytes.argtypes = [i32]

@@ -586,6 +586,11 @@ pm_status pm_attention_packed_backward(const pm_attention_desc* d, const pm_head
   return ops_cuda(e, "packed attention backward");
 }
 
+pm_status pm_attention_packed_selftest_wait_timeout(int64_t limit_cycles, void* stream) {
+  if (limit_cycles < 1 || limit_cycles > 1000000000) return ops_fail(PM_ERR_INVALID_ARG, "limit_cycles must be 1 to 10^9");
+  return ops_cuda(attn_packed_wait_probe(limit_cycles, (cudaStream_t)stream), "packed attention wait self-test");
+}
+
 pm_status pm_attention_packed_status(void* stream) {
   int code = 0;
   if (const pm_status s = ops_cuda(attn_packed_status(&code, (cudaStream_t)stream), "packed attention status")) return s;

@@ -117,6 +117,8 @@ inline int packed_parts(int64_t blocks, const PackedArgs& a, int rows, int heads
 bool attn_packed_tc_takes(const PackedArgs& a, int dtype, bool backward);
 cudaError_t attn_packed_tc_forward(const PackedArgs& a, cudaStream_t st);
 cudaError_t attn_packed_tc_backward(const PackedArgs& a, cudaStream_t st);
+// a wait of one thread that runs out after so many cycles, recorded as any other
+cudaError_t attn_packed_wait_probe(int64_t limit_cycles, cudaStream_t st);
 // the code of a device-side wait that ran out since the last call (0: none); synchronises the stream
 cudaError_t attn_packed_status(int* code, cudaStream_t st);
 

@@ -13,6 +13,7 @@
 // Where P lies over S, products that read P are issued before the product that overwrites it, and products complete in the order of
 // their issue, so a commit behind S(j + 1) also says that O holds tile j.
 #include <atomic>
+#include <mutex>
 
 #include <cooperative_groups.h>
 
@@ -29,12 +30,13 @@ constexpr int TC_ROWS = 128, TC_LOG_ROWS = 7;     // rows of a tile, of queries 
 constexpr int TC_SUB = TC_ROWS * 128;             // bytes of a [128 x 64] bf16 sub-tile, 128-byte swizzle
 
 // A bounded wait in line: a call from a thread that holds a row of scores would have to put them away.
-__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code,
+                                         long long limit_cycles = WAIT_LIMIT_CYCLES) {
   if (mbar_try_wait(bar, parity)) return true;
   const long long t0 = clock64();
   while (!mbar_try_wait(bar, parity)) {
     if (*abort_flag) return false;
-    if (clock64() - t0 > WAIT_LIMIT_CYCLES) {
+    if (clock64() - t0 > limit_cycles) {
       *abort_flag = 1;
       atomicCAS(status, 0, code);
       return false;
@@ -1214,16 +1216,37 @@ template <int DT> static cudaError_t bwd_launch(const PackedArgs& a, cudaStream_
 }
 cudaError_t attn_packed_tc_backward(const PackedArgs& a, cudaStream_t st) { return a.dim <= 64 ? bwd_launch<64>(a, st) : bwd_launch<128>(a, st); }
 
+// Self-test of the bounded wait: one thread, no tensor memory, no copy in flight, a barrier on which nothing arrives.
+__global__ void attn_packed_wait_probe_kernel(long long limit_cycles) {
+  __shared__ __align__(8) uint64_t bar;
+  __shared__ int abort_flag;
+  const uint32_t b = smem_u32(&bar);
+  mbar_init(b, 1);
+  abort_flag = 0;
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  wait_for(b, 0, &abort_flag, &g_attn_packed_status, 99, limit_cycles);
+}
+cudaError_t attn_packed_wait_probe(int64_t limit_cycles, cudaStream_t st) {
+  return launch_pdl(attn_packed_wait_probe_kernel, dim3(1), dim3(1), 0, st, false, (long long)limit_cycles);
+}
+
+// Reading and clearing are one step on the device, so that no record is lost or reported twice; what was taken passes through a word that
+// one call uses at a time.
+__device__ int g_attn_packed_taken;
+__global__ void attn_packed_take_status_kernel() { g_attn_packed_taken = atomicExch(&g_attn_packed_status, 0); }
+
 cudaError_t attn_packed_status(int* code, cudaStream_t st) {
+  static std::mutex one_at_a_time;
   *code = 0;
-  cudaError_t e = cudaMemcpyFromSymbolAsync(code, g_attn_packed_status, sizeof(int), 0, cudaMemcpyDeviceToHost, st);
-  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-  if (e == cudaSuccess && *code) {
-    const int zero = 0;
-    e = cudaMemcpyToSymbolAsync(g_attn_packed_status, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, st);
+  try {
+    std::lock_guard<std::mutex> lock(one_at_a_time);
+    cudaError_t e = launch_pdl(attn_packed_take_status_kernel, dim3(1), dim3(1), 0, st, false);
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbolAsync(code, g_attn_packed_taken, sizeof(int), 0, cudaMemcpyDeviceToHost, st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    return e;
+  } catch (...) {                                 // from the mutex
+    return cudaErrorOperatingSystem;
   }
-  return e;
 }
 
 }  // namespace pm

@@ -50,6 +50,11 @@ def _compute_device(name, t):
     return t.device
 
 
+def _indexed(device):
+    device = torch.device(device)
+    return device if device.index is not None else torch.device("cuda", torch.cuda.current_device())
+
+
 # the handle of the current stream without the object around it, where this torch has the call
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -160,11 +165,13 @@ class PackedAttention:
             device, stream, need)
 
     def pm_attention_packed_status(self, device="cuda", stream=None):
-        """Raises if a device-side wait of a tensor-core kernel ran out since the last call (a defect); synchronises the stream."""
-        device = torch.device(device)
-        if device.index is None:
-            device = torch.device("cuda", torch.cuda.current_device())
-        _launch(self.L.pm_attention_packed_status, device, stream)
+        """Raises if a device-side wait of a tensor-core kernel ran out since the last call on this device (a defect); synchronises
+        the stream."""
+        _launch(self.L.pm_attention_packed_status, _indexed(device), stream)
+
+    def pm_attention_packed_selftest_wait_timeout(self, limit_cycles, device="cuda", stream=None):
+        """Enqueues a wait that runs out after limit_cycles: the next pm_attention_packed_status on this device raises."""
+        _launch(lambda st: self.L.pm_attention_packed_selftest_wait_timeout(int(limit_cycles), st), _indexed(device), stream)
 
 
 class TokenLogProbs:
