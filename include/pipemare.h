@@ -430,7 +430,7 @@ pm_status pm_attention_packed_forward(const pm_attention_desc* desc, const pm_he
                                       void* stream);
 /* Gradients of q, k, v from d_o and the forward pass's o and lse; dk and dv are summed over the query heads that share
  * them.  dq, dk, dv and the workspace overlap neither each other nor an input (refused, as above).  workspace: at least
- * pm_attention_packed_workspace_bytes(desc) bytes of device memory, 16-byte aligned. */
+ * pm_attention_packed_workspace_bytes(desc) bytes of device memory, 4-byte aligned; it need hold nothing before the call. */
 uint64_t pm_attention_packed_workspace_bytes(const pm_attention_desc* desc);
 pm_status pm_attention_packed_backward(const pm_attention_desc* desc, const pm_head_view* q, const pm_head_view* k,
                                        const pm_head_view* v, const pm_head_view* o, const float* lse,
