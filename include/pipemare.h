@@ -411,7 +411,8 @@ typedef struct {
  * its own sequence (in the backward pass, and through v, to positions before it, too) and to no other.  A row whose every
  * score is -infinity has lse -infinity and no distribution: its o is NaN, and so are its dq and the dk and dv of the keys
  * that it sees.  Entries of cu_seqlens outside 0 .. n_tokens are clipped to that range; if they do not ascend, the results
- * of the sequences concerned are undefined, and no tensor is touched outside its rows. */
+ * of the sequences concerned (of all, where there are more than 256) are undefined, and no tensor is touched outside its
+ * rows.  An empty sequence costs about as much as the launch of a block per head. */
 typedef struct {
   int32_t dtype;                 /* PM_F32 | PM_BF16 */
   int32_t n_heads, n_kv_heads;   /* n_heads a multiple of n_kv_heads */

@@ -29,14 +29,13 @@ struct SeqTile {
   int len, tile;                                  // its length; the tile's index inside it (-1: no such tile)
 };
 
-// Looks for the index-th tile among sequences base .. base + 32 PER - 1, PER consecutive ones to a lane; `before`: tiles in front of
-// them, on return also those among them.
+// The index-th tile of up to 32 PER sequences, PER consecutive ones to a lane: tiles counted through the sequences.
 template <int PER>
-__device__ __forceinline__ bool find_tile_among(SeqTile& out, const int32_t* cu, int n_seqs, int tokens, int index, int log_rows, int base, int& before) {
+__device__ __forceinline__ SeqTile find_counted(const int32_t* cu, int n_seqs, int tokens, int index, int log_rows) {
   const int lane = threadIdx.x & 31;
   int start[PER + 1], tiles[PER], mine = 0;
 #pragma unroll
-  for (int i = 0; i <= PER; ++i) start[i] = min(max(cu[min(base + lane * PER + i, n_seqs)], 0), tokens);
+  for (int i = 0; i <= PER; ++i) start[i] = min(max(cu[min(lane * PER + i, n_seqs)], 0), tokens);
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     tiles[i] = max(start[i + 1] - start[i] + (1 << log_rows) - 1, 0) >> log_rows;
@@ -45,10 +44,9 @@ __device__ __forceinline__ bool find_tile_among(SeqTile& out, const int32_t* cu,
   int upto = mine;
 #pragma unroll
   for (int o = 1; o < 32; o *= 2) { const int v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
-  int at = before + upto - mine;
+  int at = upto - mine;
   const unsigned has = __ballot_sync(0xffffffffu, index >= at && index < at + mine);
-  before += __shfl_sync(0xffffffffu, upto, 31);
-  if (!has) return false;
+  if (!has) return SeqTile{0, 0, -1};
   int tile = 0, len = 0, begin = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
@@ -56,26 +54,46 @@ __device__ __forceinline__ bool find_tile_among(SeqTile& out, const int32_t* cu,
     at += tiles[i];
   }
   const int who = __ffs(has) - 1;
-  out = SeqTile{__shfl_sync(0xffffffffu, begin, who), __shfl_sync(0xffffffffu, len, who), __shfl_sync(0xffffffffu, tile, who)};
-  return true;
+  return SeqTile{__shfl_sync(0xffffffffu, begin, who), __shfl_sync(0xffffffffu, len, who), __shfl_sync(0xffffffffu, tile, who)};
 }
 
-// The index-th tile of 2^log_rows rows, counted through the sequences; called by a whole warp, same result in every lane.  Up to 32
-// sequences, and then every 256, cost one round of loads.  Starts are clipped to 0 .. tokens and a sequence that would end before
-// it starts is empty: whatever the array holds, no tile reaches outside the tensors.
-__device__ __forceinline__ SeqTile find_tile(const int32_t* cu, int n_seqs, int64_t tokens, int index, int log_rows) {
-  SeqTile s{0, 0, -1};
-  int before = 0;
-  if (n_seqs <= 32) {
-    find_tile_among<1>(s, cu, n_seqs, (int)tokens, index, log_rows, 0, before);
-  } else {
-    for (int base = 0; base < n_seqs; base += 256)
-      if (find_tile_among<8>(s, cu, n_seqs, (int)tokens, index, log_rows, base, before)) break;
+// The tile that has a slot: sequence b has the slots from (its start >> log_rows) + b to the next sequence's, at least as many as it has tiles
+// and most_tiles() in all.  They ascend, so a slot's sequence is found by a search of 32 places at a time.  Out of line: it costs the kernels
+// of few sequences nothing.
+static __device__ __noinline__ SeqTile find_slot(const int32_t* cu, int n_seqs, int tokens, int slot, int log_rows) {
+  const int lane = threadIdx.x & 31;
+  auto start = [&](int b) { return min(max(cu[min(b, n_seqs)], 0), tokens); };
+  const SeqTile none{0, 0, -1};
+  int first = 0, n = n_seqs;                      // the sequence is one of n from the first on
+  while (n > 32) {
+    const int step = (n + 31) / 32, b = first + lane * step;
+    const int k = __popc(__ballot_sync(0xffffffffu, lane * step < n && (start(b) >> log_rows) + b <= slot));
+    if (k == 0) return none;
+    first += (k - 1) * step;
+    n = min(step, n - (k - 1) * step);
   }
-  return s;
+  const int mine = start(first + lane);
+  const int k = __popc(__ballot_sync(0xffffffffu, lane < n && (mine >> log_rows) + first + lane <= slot));
+  if (k == 0) return none;
+  const int begin = __shfl_sync(0xffffffffu, mine, k - 1), next = __shfl_sync(0xffffffffu, mine, k & 31), end = k < 32 ? next : start(first + 32);
+  const int len = end - begin, tile = slot - (begin >> log_rows) - (first + k - 1);
+  if (tile < 0 || tile >= (len + (1 << log_rows) - 1) >> log_rows) return none;
+  return SeqTile{begin, len, tile};
 }
 
-// tiles of `rows` rows that sequences of `tokens` tokens in all can have at most
+// The tile of 2^log_rows rows of the index-th block; called by a whole warp, same result in every lane.  Up to 256 sequences are counted in one
+// round of loads, and the blocks without a tile are the last.  Beyond, where counting would make every block walk through all sequences, the
+// search takes two rounds for up to 1024 and a third for up to 32768; its blocks without a tile lie between the others (16 x 256 tokens, 16 heads
+// of 64, forward: 16.6 us counted, 18.6 searched; 1000 x 32: 438 / 356; 4096 x 8: 2460 / 1330; 60000 of which one is not empty, 2 heads: 67800 /
+// 740).  Starts are clipped to 0 .. tokens and a sequence that would end before it starts is empty: whatever the array holds, no tile
+// reaches outside the tensors.
+__device__ __forceinline__ SeqTile find_tile(const int32_t* cu, int n_seqs, int64_t tokens, int index, int log_rows) {
+  if (n_seqs <= 32) return find_counted<1>(cu, n_seqs, (int)tokens, index, log_rows);
+  if (n_seqs <= 256) return find_counted<8>(cu, n_seqs, (int)tokens, index, log_rows);
+  return find_slot(cu, n_seqs, (int)tokens, index, log_rows);
+}
+
+// tiles of `rows` rows that sequences of `tokens` tokens in all can have at most, and their slots
 inline int64_t most_tiles(int64_t tokens, int n_seqs, int rows) { return tokens / rows + n_seqs; }
 
 // `blocks` clusters of `parts` blocks
