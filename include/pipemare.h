@@ -406,13 +406,15 @@ typedef struct {
  * key/value head h / (n_heads / n_kv_heads).
  *   s_ij = scale q_i . k_j for the keys of i's sequence (causal: those with j <= i),  lse_i = log sum_j exp(s_ij),
  *   o_i = sum_j exp(s_ij - lse_i) v_j
- * dtype is the type of every tensor but lse (PM_BF16: products of bf16 values with fp32 sums; the probabilities are
- * rounded to bf16 before they multiply v).  head_dim: 1 to 128.  A value that is not finite spreads over the results of
- * its own sequence (in the backward pass, and through v, to positions before it, too) and to no other.  A row whose every
- * score is -infinity has lse -infinity and no distribution: its o is NaN, and so are its dq and the dk and dv of the keys
- * that it sees.  Entries of cu_seqlens outside 0 .. n_tokens are clipped to that range; if they do not ascend, the results
- * of the sequences concerned (of all, where there are more than 256) are undefined, and no tensor is touched outside its
- * rows.  An empty sequence costs about as much as the launch of a block per head. */
+ * dtype is the type of every tensor but lse (PM_BF16: products of bf16 values with fp32 sums.  On the tensor cores the
+ * probabilities are rounded to bf16 before they multiply v, and in the backward pass also p and p (do_i . v_j - do_i .
+ * o_i) before theirs; an exponential in eight is off by up to 3e-6, the others by 2^-22, and so, before any rounding,
+ * is lse).  head_dim: 1 to 128.  A value that is not finite spreads over the results of its own sequence (in the
+ * backward pass, and through v, to positions before it, too) and to no other.  A row whose every score is -infinity has
+ * lse -infinity and no distribution: its o is NaN, and so are its dq and the dk and dv of the keys that it sees.
+ * Entries of cu_seqlens outside 0 .. n_tokens are clipped to that range; if they do not ascend, the results of the
+ * sequences concerned (of all, where there are more than 256) are undefined, and no tensor is touched outside its rows.
+ * An empty sequence costs about as much as the launch of a block per head. */
 typedef struct {
   int32_t dtype;                 /* PM_F32 | PM_BF16 */
   int32_t n_heads, n_kv_heads;   /* n_heads a multiple of n_kv_heads */
@@ -461,7 +463,8 @@ pm_status pm_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int
 /* d_logits [rows, vocab] (dtype as logits, grad_stride elements apart) from the gradients of logprob and of the entropy
  * (either may be NULL), with lse and (for d_entropy) entropy as the forward call wrote them:
  *   d_logits_j = d_logprob ([j = y] - p_j) - d_entropy p_j (log p_j + entropy).
- * p_j = exp(x_j - lse); in rows with |lse| > 4096, where a rounded lse no longer resolves p, it is taken from the logits.
+ * p_j = exp(x_j - lse), no more exact than the fp32 lse: off by up to 2^-24 |lse| of itself, 1.2e-4 just below 4096; in rows
+ * with |lse| > 4096 it is taken from the logits.
  * d_logits may be logits itself (same strides); any other overlap of it with an input is refused. */
 pm_status pm_token_logprobs_backward(const void* logits, int32_t dtype, int64_t rows, int32_t vocab, int64_t row_stride,
                                      const int32_t* targets, const float* lse, const float* entropy,
@@ -470,12 +473,14 @@ pm_status pm_token_logprobs_backward(const void* logits, int32_t dtype, int64_t 
 
 /* Clipping by the global norm over many tensors:
  *   norm = sqrt(sum of the squares of every src element),  scale = min(1, max_norm / norm),  dst = scale * src
- * norm and scale: one device float each.  dst may be src itself (clipping in place, same type), or another tensor of
- * either type, such as a slice of the gradient arena; otherwise sources and destinations do not overlap.  The squares are
- * summed in 64 bits, so none leaves the range.  A norm that is infinite in fp32 or NaN is reported as such and scales
- * nothing (scale 1).  A scale below fp32's normal range is reported with the few bits it has there and applied in 64 bits.
- * tensors: host array, read during the call; empty tensors are allowed.  max_norm: positive, infinity to
- * measure the norm alone.  workspace: device, at least pm_clip_gradients_workspace_bytes(n_tensors) bytes. */
+ * norm and scale: one device float each, apart from each other and from the tensors.  dst may be src itself (clipping
+ * in place, same type), or another tensor of either type, such as a slice of the gradient arena; otherwise sources and
+ * destinations do not overlap.  Squares are added eight at a time in fp32 where their size allows it, else one by one
+ * in 64 bits, and those sums in 64 bits: none leaves the range, and the norm is off by at most 2^-22 of itself.  A norm
+ * that is infinite in fp32 or NaN is reported as such and scales nothing (scale 1).  A scale below fp32's normal range
+ * is reported with the few bits it has there and applied in 64 bits. tensors: host array, read during the call; empty
+ * tensors are allowed.  max_norm: positive, infinity to measure the norm alone.  workspace: device, at least
+ * pm_clip_gradients_workspace_bytes(n_tensors) bytes. */
 typedef struct {
   const void* src;               /* device */
   void* dst;                     /* device */

@@ -55,7 +55,8 @@ template <int DT, int NT> struct FwdShape {
   static constexpr int kBlocks = NT == 1 ? 2 : 1; // per SM
   // Registers: a softmax thread holds a row of 128 scores, the warps that copy and issue need few.  NT = 2: 384 threads are launched
   // with 168, 256 x 224 + 128 x 56 is no more than that; NT = 1: 256 with 128, 128 x 208 + 128 x 48.
-  // (Two threads to a row, 64 scores each, took 332 us where this takes 289: 8192 + 4099 tokens, 16 heads of 128 on 4.)
+  // What does not fit while a row is held goes to local memory: 100 to 132 bytes of stores, 176 to 184 of loads.
+  // (Two threads to a row, 64 scores each, took 332 us where this took 295: 8192 + 4099 tokens, 16 heads of 128 on 4.)
   static constexpr int kSoftmaxRegs = NT == 1 ? 208 : 224, kOtherRegs = NT == 1 ? 48 : 56;
   // Tensor-memory columns: S (128 for each tile), O (DT), and for heads of 64 P (64) beside S instead of over it, so that the
   // next scores are formed while the exponentials of these are (8192 tokens, 16 heads of 64, causal: 197 us, over S 205).
@@ -169,7 +170,7 @@ __device__ __forceinline__ void finish_rows(const HeadView& x, const SeqTile& s,
 
 // 2^x for two values on the FMA units: x = n + f with n the nearest integer, 2^f by the polynomial of degree 4 through f(0) = 1 with the
 // least relative error on [-1/2, 1/2] (2.9e-6, a 1300th of bf16's half step; found as a linear program over 4001 points), n added to the
-// exponent.  x is at most 8 here.  At -127 and below, masked scores among them, the result is exactly zero (1.0's exponent less 127):
+// exponent.  The row sum takes the same values in fp32, so that o stays their weighted mean; lse carries their error, at most 2.9e-6 absolute.  x is at most 8 here.  At -127 and below, masked scores among them, the result is exactly zero (1.0's exponent less 127):
 // a masked key's value counts for nothing however large.  Between -127 and -126 it is below 2^-126, and of a NaN it is zero: the row's
 // other exponentials keep it.
 __device__ __forceinline__ float2 ex2_fma(float2 x) {
@@ -347,7 +348,7 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
         if constexpr (S::kApart) {
           if (more) {
             ok = next_keys();
-  #pragma unroll
+#pragma unroll
             for (int t = 0; t < NT; ++t)
               if (ok && j + 1 < count_of(t)) {
                 ok = wait_for(s_read(t), j & 1, abort_flag, status, 42);
@@ -358,7 +359,7 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
             done(k_empty(nx));
           }
           ok = wait_for(v_full(st), (j / S::kStages) & 1, abort_flag, status, 36);
-  #pragma unroll
+#pragma unroll
           for (int t = 0; t < NT; ++t)
             if (ok && j < count_of(t)) {
               ok = values(t, j);
@@ -370,7 +371,7 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
           ok = wait_for(v_full(st), (j / S::kStages) & 1, abort_flag, status, 36);
           // with one stage the next keys are copied only behind the previous product's commit: waited for below
           if (ok && more && S::kStages > 1) ok = next_keys();
-  #pragma unroll
+#pragma unroll
           for (int t = 0; t < NT; ++t) {
             const int n = count_of(t);
             if (!ok || j >= n) continue;
@@ -535,7 +536,7 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
         const float inv = 1.f / l;
         if (a.lse && row < s.len) a.lse[(int64_t)h * a.tokens + s.begin + row] = ok ? (m + log2f(l)) * kLn2 : NAN;
         const int first_row = q0 + (warp & 3) * 32;
-  #pragma unroll
+#pragma unroll
         for (int q = 0; q < DT / 32; ++q)             // Q's tile has been read
           store_rows(head_row_out<__nv_bfloat16>(a.o, s.begin + first_row, h), a.o.token, s.len - first_row, to, q * 32, a.dim, inv, ok,
                      sptr + t * S::kTile + (warp & 3) * 2048);

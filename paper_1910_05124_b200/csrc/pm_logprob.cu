@@ -276,8 +276,8 @@ template <typename T, bool ENTROPY, int U> __device__ __forceinline__ void take(
   if (ENTROPY) st.t += t.x + t.y;
 }
 
-// 1536 threads to an SM, in six blocks or twelve: the end of a row (joining the sums, ranking the alternatives) is a chain of short steps that the other blocks'
-// loads run beside.
+// 1536 threads to an SM, in six blocks or twelve: the end of a row (joining the sums, ranking the alternatives) is a chain of short steps that
+// the other blocks' loads run beside.
 template <typename T, int THREADS, bool TOP, bool ENTROPY>
 __global__ void __launch_bounds__(THREADS, 1536 / THREADS) logprob_kernel(LogprobArgs a) {
   __shared__ LpShared<THREADS> sh;
@@ -361,8 +361,8 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) logprob_kernel(Logpro
   }
 }
 
-// Short rows: a warp to each, nothing shared between warps; for rows of up to 4 KB, and of up to 16 KB where there are many.  us with a warp / a block to a row, fp32, five alternatives: 16 x 200 4.4 / 6.3,
-// 300 x 1000 6.3 / 6.3, 1200 x 2000 8.5 / 10.4, 2400 x 4000 15.6 / 18.6; but 40 x 3000 9.2 / 6.4 and 1345 x 8191 30.9 / 27.3.
+// Short rows: a warp to each, nothing shared between warps; for rows of up to 4 KB, and of up to 16 KB where there are many.  us with a warp / a
+// block to a row, fp32, five alternatives: 16 x 200 4.4 / 6.3, 300 x 1000 6.3 / 6.3, 1200 x 2000 8.5 / 10.4, 2400 x 4000 15.6 / 18.6; but 40 x 3000 9.2 / 6.4 and 1345 x 8191 30.9 / 27.3.
 constexpr int kLpShortBytes = 4096, kLpMidBytes = 16384, kLpMidRows = 1024;
 // Candidates of a warp: 160 are too few in 3 rows of a million at k = 28, but in 18 of a hundred at k = 32, and the launch waits for such a row's
 // k passes: 2400 x 4000 fp32, k = 32, 350 us with 160, 90 with 512.  Longer lists leave less of L1 to the rows: k = 20, 37 with 512, 33 with 160.
@@ -470,8 +470,9 @@ struct LogprobBwdArgs {
 
 constexpr int kLbVectors = 4;                     // 16-byte vectors per thread
 
-// An lse beyond this magnitude no longer resolves log p (its rounding alone is 2^-13 and more), as in a row whose every logit is a
-// mask's lowest value.  Such a row is left to one block, which takes the maximum and the sum from the logits again.
+// An lse beyond this magnitude no longer resolves log p (its rounding alone reaches 2^-12 there), as in a row whose every logit is a
+// mask's lowest value.  Such a row is left to one block, which takes the maximum and the sum from the logits again.  Below, p is off by up to
+// 2^-24 |lse| of itself: 6e-7 at an lse of 10, 1.2e-4 just below the limit.
 constexpr float kLseCoarse = 4096.f;
 
 __device__ __forceinline__ float logit_grad(float lp, float gl, float gh, float h) {
