@@ -449,16 +449,18 @@ template <typename K> static cudaError_t pk_allow(K kernel, int bytes, std::atom
 template <typename T, int DP, bool VEC, int R> static cudaError_t pk_forward(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   constexpr int smem = pk_smem<DP, R>(1, 2, 1);
+  const int64_t blocks = most_tiles(a.tokens, a.n_seqs, R) * a.heads;
+  if (!launchable(blocks)) return cudaErrorInvalidConfiguration;
   const cudaError_t e = pk_allow(attn_packed_fwd_kernel<T, DP, VEC, R>, smem, done);
   if (e != cudaSuccess) return e;
-  const int64_t blocks = most_tiles(a.tokens, a.n_seqs, R) * a.heads;
   return launch_clusters(attn_packed_fwd_kernel<T, DP, VEC, R>, blocks, 4 * R, smem, st, false, pk_split<R> ? packed_parts(blocks, a, PK_T, 1, 4 * kSms, 3) : 1, a);
 }
 template <typename T, int DP, bool VEC, int R> static cudaError_t pk_backward(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   constexpr int smem = pk_smem<DP, R>(2, 2, 2);
-  cudaError_t e = pk_allow(attn_packed_bwd_kernel<T, DP, VEC, R>, smem, done);
   const int64_t tiles = most_tiles(a.tokens, a.n_seqs, R), blocks = tiles * (a.heads + a.kv_heads);
+  if (!launchable(blocks)) return cudaErrorInvalidConfiguration;
+  cudaError_t e = pk_allow(attn_packed_bwd_kernel<T, DP, VEC, R>, smem, done);
   if (e == cudaSuccess) e = launch_pdl(attn_packed_delta_kernel<T>, dim3((unsigned)((a.tokens * a.heads + 7) / 8)), dim3(256), 0, st, false, a);
   if (e == cudaSuccess)
     e = launch_clusters(attn_packed_bwd_kernel<T, DP, VEC, R>, blocks, 4 * R, smem, st, true, pk_split<R> ? packed_parts(blocks, a, PK_T, a.group, 4 * kSms, 2) : 1, a,
@@ -515,6 +517,11 @@ static pm_status pk_apart(const Extent* written, int n_written, const Extent* re
   }
   return PM_OK;
 }
+static pm_status pk_result(cudaError_t e, const char* what) {
+  if (e != cudaErrorInvalidConfiguration) return ops_cuda(e, what);
+  cudaGetLastError();                             // as ops_cuda does
+  return ops_fail(PM_ERR_SHAPE, "%s: more blocks than a launch has: too many sequences for so many heads", what);
+}
 static PackedArgs pk_args(const pm_attention_desc* d, const int32_t* cu, float* lse) {
   PackedArgs a{};
   a.cu = cu; a.lse = lse; a.tokens = d->n_tokens; a.n_seqs = d->n_seqs; a.heads = d->n_heads; a.kv_heads = d->n_kv_heads;
@@ -546,7 +553,7 @@ pm_status pm_attention_packed_forward(const pm_attention_desc* d, const pm_head_
   const cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t e = attn_packed_tc_takes(a, d->dtype, false) ? attn_packed_tc_forward(a, st)
                         : d->dtype == PM_BF16 ? pk_run<__nv_bfloat16>(a, false, st) : pk_run<float>(a, false, st);
-  return ops_cuda(e, "packed attention");
+  return pk_result(e, "packed attention");
 }
 
 uint64_t pm_attention_packed_workspace_bytes(const pm_attention_desc* d) {
@@ -583,7 +590,7 @@ pm_status pm_attention_packed_backward(const pm_attention_desc* d, const pm_head
   const cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t e = attn_packed_tc_takes(a, d->dtype, true) ? attn_packed_tc_backward(a, st)
                         : d->dtype == PM_BF16 ? pk_run<__nv_bfloat16>(a, true, st) : pk_run<float>(a, true, st);
-  return ops_cuda(e, "packed attention backward");
+  return pk_result(e, "packed attention backward");
 }
 
 pm_status pm_attention_packed_selftest_wait_timeout(int64_t limit_cycles, void* stream) {

@@ -96,10 +96,12 @@ __device__ __forceinline__ SeqTile find_tile(const int32_t* cu, int n_seqs, int6
 // tiles of `rows` rows that sequences of `tokens` tokens in all can have at most, and their slots
 inline int64_t most_tiles(int64_t tokens, int n_seqs, int rows) { return tokens / rows + n_seqs; }
 
+// Whether one launch can have so many blocks; asked before anything is launched.
+inline bool launchable(int64_t blocks) { return blocks <= 0x7fffffff; }
+
 // `blocks` clusters of `parts` blocks
 template <typename... K, typename... A>
 inline cudaError_t launch_clusters(void (*kernel)(K...), int64_t blocks, int threads, int smem, cudaStream_t stream, bool pdl, int parts, A... args) {
-  if (blocks * parts > 0x7fffffff) return cudaErrorInvalidConfiguration;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(blocks * parts)); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
   cudaLaunchAttribute at[2];

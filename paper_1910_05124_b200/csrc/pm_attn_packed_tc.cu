@@ -1177,13 +1177,14 @@ template <int DT, int NT> static cudaError_t fwd_launch(const PackedArgs& a, cud
   static std::atomic<uint64_t> done{0};
   using S = FwdShape<DT, NT>;
   TcMaps maps;
+  const int pair = NT == 2 && a.group % 2 == 0, units = pair ? a.heads / 2 : a.heads;
+  const int64_t blocks = most_tiles(a.tokens, a.n_seqs, pair ? TC_ROWS : NT * TC_ROWS) * units;
+  if (!launchable(blocks)) return cudaErrorInvalidConfiguration;
   cudaError_t e = allow_smem(attn_packed_fwd_tc_kernel<DT, NT>, S::kSmem, done);
   if (e == cudaSuccess) e = encode_heads(&maps.q, a.q, a.dim, a.heads, a.tokens, TC_ROWS);
   if (e == cudaSuccess) e = encode_heads(&maps.k, a.k, a.dim, a.kv_heads, a.tokens, TC_ROWS);
   if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.tokens, TC_ROWS);
   if (e != cudaSuccess) return e;
-  const int pair = NT == 2 && a.group % 2 == 0, units = pair ? a.heads / 2 : a.heads;
-  const int64_t blocks = most_tiles(a.tokens, a.n_seqs, pair ? TC_ROWS : NT * TC_ROWS) * units;
   const int parts = NT == 1 ? packed_parts(blocks, a, TC_ROWS, 1, 2 * kSms, 3) : 1;
   return launch_clusters(attn_packed_fwd_tc_kernel<DT, NT>, blocks, S::kThreads, S::kSmem, st, false, parts, a, maps, units, pair);
 }
@@ -1201,13 +1202,14 @@ template <int DT> static cudaError_t bwd_launch(const PackedArgs& a, cudaStream_
   static std::atomic<uint64_t> done{0};
   using S = BwdShape<DT>;
   TcBwdMaps maps;
+  const int64_t tiles = most_tiles(a.tokens, a.n_seqs, TC_ROWS), blocks = tiles * (a.heads + a.kv_heads);
+  if (!launchable(blocks)) return cudaErrorInvalidConfiguration;
   cudaError_t e = allow_smem(attn_packed_bwd_tc_kernel<DT>, S::kSmem, done);
   if (e == cudaSuccess) e = encode_heads(&maps.q, a.q, a.dim, a.heads, a.tokens, S::kCols);
   if (e == cudaSuccess) e = encode_heads(&maps.k, a.k, a.dim, a.kv_heads, a.tokens, S::kCols);
   if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.tokens, S::kCols);
   if (e == cudaSuccess) e = encode_heads(&maps.d_o, a.d_o, a.dim, a.heads, a.tokens, S::kCols);
   if (e != cudaSuccess) return e;
-  const int64_t tiles = most_tiles(a.tokens, a.n_seqs, TC_ROWS), blocks = tiles * (a.heads + a.kv_heads);
   e = launch_pdl(attn_packed_delta_tc_kernel, dim3((unsigned)((a.tokens + 32 * DELTA_R - 1) / (32 * DELTA_R)), a.heads), dim3(256), 0, st, false, a);
   // starts beside the first's last blocks; its own wait for them before they read delta
   if (e == cudaSuccess)
