@@ -7,6 +7,7 @@ graph.  As with any CUDA call, a tensor that another stream still writes has to 
 that belongs to another stream has to be kept until the call has run.  Refused arguments raise PipeMareError.
 """
 import ctypes as C
+from bisect import bisect_left
 
 import torch
 
@@ -262,12 +263,15 @@ class GradClip:
                     spans.append((src, src + n * g.element_size(), False, i))
         self.tensors = (pm_tensor_pair * len(rows))(*rows)
         end = {True: (0, 0), False: (0, 0)}                  # the furthest end so far of what is written, and of what is read
+        self.starts, self.stops = starts, stops = [], []     # of what the tensors cover, ascending
         for start, stop, written, i in sorted(spans):
             for other in (True, False) if written else (True,):
                 if start < end[other][0]:
                     _refuse(f"{'outs' if written else 'grads'}[{i}] overlaps {'outs' if other else 'grads'}[{end[other][1]}]")
             if stop > end[written][0]:
                 end[written] = (stop, i)
+            starts.append(start)
+            stops.append(max(stop, stops[-1]) if stops else stop)
         self.ws_bytes = self.L.pm_clip_gradients_workspace_bytes(len(grads))
 
     def _fits(self, t):
@@ -292,5 +296,8 @@ class GradClip:
             _refuse("norm and scale must be tensors")
         if p_norm == p_scale:
             _refuse("norm and scale share their memory")
+        i, j = bisect_left(self.starts, p_norm + 4), bisect_left(self.starts, p_scale + 4)     # the spans that start in front of their ends
+        if i and self.stops[i - 1] > p_norm or j and self.stops[j - 1] > p_scale:
+            _refuse(f"{'norm' if i and self.stops[i - 1] > p_norm else 'scale'} lies in one of the tensors")
         _launch(lambda st, ws: self.L.pm_clip_gradients(self.tensors, len(self.tensors), max_norm, p_norm, p_scale, ws, self.ws_bytes, st),
                 self.device, stream, self.ws_bytes)

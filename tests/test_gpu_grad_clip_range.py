@@ -43,3 +43,23 @@ def test_factor_below_the_normal_range_of_fp32(cuda_device, src, dst, in_place, 
         bound = (4 * R.U32 + R.U32 + 2.0 ** -50 + R.u(dst)) * want.abs() + 2.0 ** -150 + torch.finfo(dst).smallest_normal * R.u(dst)
         off = (b.double() - want).abs() - bound
         assert float(off.max()) <= 0, float(off.max())
+
+
+def test_norm_and_scale_lie_apart_from_the_tensors(cuda_device):
+    """Within the arena, but between its slices, they may lie."""
+    import paper_1910_05124_b200 as pm
+    arena, g = torch.zeros(1000, device=cuda_device), make([100, 0, 200], [F, BF], cuda_device, seed=8)
+    outs = [arena[0:100], arena[128:128], arena[128:328]]
+    op, one = pm.GradClip(g, outs), torch.zeros(1, device=cuda_device)
+    for bad in (arena[0:1], arena[99:100], arena[327:328], g[0][50:51], g[2].view(F)[40:41] if g[2].dtype == BF else g[2][40:41]):
+        with pytest.raises(pm.PipeMareError, match="norm lies in"):
+            op.pm_clip_gradients(1.0, bad, one)
+        with pytest.raises(pm.PipeMareError, match="scale lies in"):
+            op.pm_clip_gradients(1.0, one, bad)
+    assert (arena == 0).all()
+    op.pm_clip_gradients(1.0, arena[100:101], arena[328:329])
+    want = R.clip(g, 1.0)
+    assert abs(float(arena[100]) - want[0]) <= 4 * R.U32 * want[0] and abs(float(arena[328]) - want[1]) <= 5 * R.U32 * want[1]
+    empty = pm.GradClip([torch.zeros(0, device=cuda_device)])
+    empty.pm_clip_gradients(1.0, one, arena[500:501])
+    assert float(one) == 0.0 and float(arena[500]) == 1.0
