@@ -441,6 +441,33 @@ pm_status pm_attention_packed_backward(const pm_attention_desc* desc, const pm_h
                                        const pm_head_view* dk, const pm_head_view* dv, void* workspace,
                                        uint64_t workspace_bytes, void* stream);
 
+/* Attention of packed sequences over the sequences of another tensor (a decoder's tokens over an encoder's states, of another
+ * length each): q, o [n_tokens, n_heads, head_dim] with cu_seqlens; k, v [n_kv_tokens, n_kv_heads, head_dim] with
+ * cu_seqlens_kv; both arrays are of n_seqs + 1 entries, and sequence b of q attends to every row of sequence b of k, v.
+ * Formulas, types, layouts, treatment of tokens outside the sequences, of cu_seqlens that are out of range and of values that
+ * are not finite as above, without `causal` (a value that is not finite reaches the results of its sequence).  A sequence without
+ * keys has o zero, lse -infinity and dq zero; one without queries has dk and dv zero.  A tensor of no rows may have a NULL pointer.
+ * A decoding step is a call with a token, or the few of a beam, to each sequence: with few query rows the keys of a sequence are
+ * shared out among blocks, whose sums are joined in a fixed order. */
+typedef struct {
+  int32_t dtype;                 /* PM_F32 | PM_BF16 */
+  int32_t n_heads, n_kv_heads;   /* n_heads a multiple of n_kv_heads */
+  int32_t head_dim;
+  int32_t n_seqs;
+  int64_t n_tokens;              /* rows of q, o, d_o and dq */
+  int64_t n_kv_tokens;           /* rows of k, v, dk and dv */
+  float scale;                   /* positive, below 2e38; 1 / sqrt(head_dim) as a rule */
+} pm_cross_attention_desc;
+pm_status pm_attention_cross_forward(const pm_cross_attention_desc* desc, const pm_head_view* q, const pm_head_view* k,
+                                     const pm_head_view* v, const int32_t* cu_seqlens, const int32_t* cu_seqlens_kv,
+                                     const pm_head_view* o, float* lse, void* stream);
+uint64_t pm_attention_cross_workspace_bytes(const pm_cross_attention_desc* desc);
+pm_status pm_attention_cross_backward(const pm_cross_attention_desc* desc, const pm_head_view* q, const pm_head_view* k,
+                                      const pm_head_view* v, const pm_head_view* o, const float* lse, const pm_head_view* d_o,
+                                      const int32_t* cu_seqlens, const int32_t* cu_seqlens_kv, const pm_head_view* dq,
+                                      const pm_head_view* dk, const pm_head_view* dv, void* workspace,
+                                      uint64_t workspace_bytes, void* stream);
+
 /* Every wait inside the tensor-core kernels is bounded (about one second).  One that runs out is a defect: the rows
  * concerned are NaN, and this call, which synchronises the stream, returns PM_ERR_TIMEOUT once.  A device keeps one record,
  * the first since the last call, of all streams and callers; the call of any of them takes it.

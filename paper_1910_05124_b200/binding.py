@@ -60,6 +60,11 @@ class pm_attention_desc(C.Structure):
                 ("n_seqs", C.c_int32), ("causal", C.c_int32), ("n_tokens", C.c_int64), ("scale", C.c_float)]
 
 
+class pm_cross_attention_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("n_seqs", C.c_int32),
+                ("n_tokens", C.c_int64), ("n_kv_tokens", C.c_int64), ("scale", C.c_float)]
+
+
 class pm_tensor_pair(C.Structure):
     _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("count", C.c_uint64), ("src_dtype", C.c_int32), ("dst_dtype", C.c_int32)]
 
@@ -121,6 +126,11 @@ def lib():
     L.pm_attention_packed_workspace_bytes.argtypes = [desc]
     L.pm_attention_packed_workspace_bytes.restype = u64
     L.pm_attention_packed_backward.argtypes = [desc, view, view, view, view, vp, view, vp, view, view, view, vp, u64, vp]
+    cross = C.POINTER(pm_cross_attention_desc)
+    L.pm_attention_cross_forward.argtypes = [cross, view, view, view, vp, vp, view, vp, vp]
+    L.pm_attention_cross_workspace_bytes.argtypes = [cross]
+    L.pm_attention_cross_workspace_bytes.restype = u64
+    L.pm_attention_cross_backward.argtypes = [cross, view, view, view, view, vp, view, vp, vp, view, view, view, vp, u64, vp]
     L.pm_attention_packed_status.argtypes = [vp]
     L.pm_attention_packed_selftest_wait_timeout.argtypes = [i64, vp]
     L.pm_token_logprobs.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp, vp, i32, vp, vp, vp]

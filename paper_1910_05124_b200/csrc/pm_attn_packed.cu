@@ -176,29 +176,30 @@ __global__ void __launch_bounds__(4 * R, R == 64 && DP <= 64 ? 2 : 1) attn_packe
   const int parts = pk_split<R> ? (int)cluster.num_blocks() : 1, part = pk_split<R> ? (int)cluster.block_rank() : 0, block = blockIdx.x / parts;
   const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.heads, kLog<R>);
   if (s.tile < 0) return;
+  const SeqTile ks = other_side(a.cross, s, a.cu_kv, a.kv_tokens);
   extern __shared__ float sm[];
   float *sQ = sm, *sK = sQ + R * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sP = sV + PK_T * kPkLd<DP>;
   const int h = block % a.heads, hk = h / a.group, q0 = pk_from_end<R>(s) * R;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int all = a.causal ? min(s.len, q0 + R) : s.len, tiles = (all + PK_T - 1) / PK_T;
+  const int all = a.causal ? min(s.len, q0 + R) : ks.len, tiles = (all + PK_T - 1) / PK_T;
   const int begin = tiles * part / parts * PK_T, end = min(all, tiles * (part + 1) / parts * PK_T);
   PkPair<T, DP, VEC, PK_T, 4 * R> next;
   {
     PkRows<T, DP, VEC, R, 4 * R> q;
     q.fetch(a.q, s, q0, h, a.dim);
-    if (next.kAhead) next.fetch(a.k, a.v, s, begin, hk, a.dim);
+    if (next.kAhead) next.fetch(a.k, a.v, ks, begin, hk, a.dim);
     q.put(sQ);
   }
   float o[4][DP / 16] = {}, m[4], l[4] = {};
 #pragma unroll
   for (int i = 0; i < 4; ++i) m[i] = -INFINITY;
   for (int k0 = begin; k0 < end; k0 += PK_T) {
-    if (!next.kAhead) next.fetch(a.k, a.v, s, k0, hk, a.dim);
+    if (!next.kAhead) next.fetch(a.k, a.v, ks, k0, hk, a.dim);
     __syncthreads();
     next.x.put(sK);
     next.y.put(sV);
     __syncthreads();
-    if (next.kAhead && k0 + PK_T < end) next.fetch(a.k, a.v, s, k0 + PK_T, hk, a.dim);
+    if (next.kAhead && k0 + PK_T < end) next.fetch(a.k, a.v, ks, k0 + PK_T, hk, a.dim);
     float acc[4][4] = {};
     pk_abt<DP>(acc, sQ, sK);
 #pragma unroll
@@ -208,7 +209,7 @@ __global__ void __launch_bounds__(4 * R, R == 64 && DP <= 64 ? 2 : 1) attn_packe
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int c = k0 + tx + 16 * j;
-        acc[i][j] = c < s.len && (!a.causal || c <= r) ? acc[i][j] * a.scale : -INFINITY;
+        acc[i][j] = c < ks.len && (!a.causal || c <= r) ? acc[i][j] * a.scale : -INFINITY;
         mx = max_nan(mx, acc[i][j]);
       }
 #pragma unroll
@@ -254,7 +255,7 @@ __global__ void __launch_bounds__(4 * R, R == 64 && DP <= 64 ? 2 : 1) attn_packe
     for (int r = r0 + threadIdx.x; r < r1; r += 4 * R) {
       float top, base, sum;
       total(r, top, base, sum);
-      for (int p = 0; p < parts; ++p) weights[p * R + r] = ex2((cluster.map_shared_rank(stats, p)[r] - base) * kLog2e) / sum;
+      for (int p = 0; p < parts; ++p) weights[p * R + r] = ks.len ? ex2((cluster.map_shared_rank(stats, p)[r] - base) * kLog2e) / sum : 0.f;
       if (a.lse && q0 + r < s.len) a.lse[(int64_t)h * a.tokens + s.begin + q0 + r] = top + logf(sum);
     }
     __syncthreads();
@@ -265,7 +266,7 @@ __global__ void __launch_bounds__(4 * R, R == 64 && DP <= 64 ? 2 : 1) attn_packe
   float inv[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    inv[i] = 1.f / l[i];
+    inv[i] = ks.len ? 1.f / l[i] : 0.f;           // no keys: zeros
     const int r = q0 + 4 * ty + i;
     if (a.lse && tx == 0 && r < s.len) a.lse[(int64_t)h * a.tokens + s.begin + r] = m[i] + logf(l[i]);
   }
@@ -292,17 +293,18 @@ __global__ void __launch_bounds__(256) attn_packed_delta_kernel(PackedArgs a) {
 template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void pk_dq_block(const PackedArgs& a, int block, int part, int parts) {
   const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.heads, kLog<R>);
   if (s.tile < 0) { pdl_wait(); return; }
+  const SeqTile ks = other_side(a.cross, s, a.cu_kv, a.kv_tokens);
   extern __shared__ float sm[];
   float *sQ = sm, *sO = sQ + R * kPkLd<DP>, *sK = sO + R * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sS = sV + PK_T * kPkLd<DP>;
   const int h = block % a.heads, hk = h / a.group, q0 = pk_from_end<R>(s) * R;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int all = a.causal ? min(s.len, q0 + R) : s.len, tiles = (all + PK_T - 1) / PK_T;
+  const int all = a.causal ? min(s.len, q0 + R) : ks.len, tiles = (all + PK_T - 1) / PK_T;
   const int begin = tiles * part / parts * PK_T, end = min(all, tiles * (part + 1) / parts * PK_T);
   PkPair<T, DP, VEC, PK_T, 4 * R> next;
   {
     PkPair<T, DP, VEC, R, 4 * R> own;
     own.fetch(a.q, a.d_o, s, q0, h, a.dim);
-    if (next.kAhead) next.fetch(a.k, a.v, s, begin, hk, a.dim);
+    if (next.kAhead) next.fetch(a.k, a.v, ks, begin, hk, a.dim);
     own.x.put(sQ);
     own.y.put(sO);
   }
@@ -316,12 +318,12 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
   }
   float dq[4][DP / 16] = {};
   for (int k0 = begin; k0 < end; k0 += PK_T) {
-    if (!next.kAhead) next.fetch(a.k, a.v, s, k0, hk, a.dim);
+    if (!next.kAhead) next.fetch(a.k, a.v, ks, k0, hk, a.dim);
     __syncthreads();
     next.x.put(sK);
     next.y.put(sV);
     __syncthreads();
-    if (next.kAhead && k0 + PK_T < end) next.fetch(a.k, a.v, s, k0 + PK_T, hk, a.dim);
+    if (next.kAhead && k0 + PK_T < end) next.fetch(a.k, a.v, ks, k0 + PK_T, hk, a.dim);
     float acc[4][4] = {}, dp[4][4] = {};
     pk_abt<DP>(acc, sQ, sK);
     pk_abt<DP>(dp, sO, sV);
@@ -331,7 +333,7 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
       for (int j = 0; j < 4; ++j) {
         const int c = k0 + tx + 16 * j, r = q0 + 4 * ty + i;
         const float p = ex2((acc[i][j] * a.scale - lse[i]) * kLog2e);
-        sS[(4 * ty + i) * PK_LDP + tx + 16 * j] = c < s.len && r < s.len && (!a.causal || c <= r) ? p * (dp[i][j] - delta[i]) : 0.f;
+        sS[(4 * ty + i) * PK_LDP + tx + 16 * j] = c < ks.len && r < s.len && (!a.causal || c <= r) ? p * (dp[i][j] - delta[i]) : 0.f;
       }
     __syncthreads();
     pk_pb<DP>(dq, sS, sK);
@@ -349,35 +351,36 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
 }
 
 template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void pk_dkv_block(const PackedArgs& a, int block, int part, int parts) {
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.kv_heads, kLog<R>);
+  const SeqTile s = find_tile(a.cu_kv, a.n_seqs, a.kv_tokens, block / a.kv_heads, kLog<R>);
   if (s.tile < 0) { pdl_wait(); return; }
+  const SeqTile qs = other_side(a.cross, s, a.cu, a.tokens);
   extern __shared__ float sm[];
   float *sK = sm, *sV = sK + R * kPkLd<DP>, *sQ = sV + R * kPkLd<DP>, *sO = sQ + PK_T * kPkLd<DP>, *sP = sO + PK_T * kPkLd<DP>,
         *sS = sP + R * PK_LDP, *sR = sS + R * PK_LDP;
   const int hk = block % a.kv_heads, k0 = s.tile * R;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int first = a.causal ? k0 : 0, per_head = (s.len - first + PK_T - 1) / PK_T;
+  const int first = a.causal ? k0 : 0, per_head = (qs.len - first + PK_T - 1) / PK_T;
   const int it0 = per_head * a.group * part / parts, it1 = per_head * a.group * (part + 1) / parts;
-  int h = hk * a.group + it0 / per_head, q0 = first + it0 % per_head * PK_T;
+  int h = hk * a.group + it0 / max(per_head, 1), q0 = first + it0 % max(per_head, 1) * PK_T;
   // a query tile's lse (threads 0 .. 63) and delta (64 .. 127) travel with it
   auto row_value = [&](int h, int q0) {
     const int r = q0 + (threadIdx.x & 63);
-    if (threadIdx.x >= 128 || r >= s.len || it0 >= it1) return 0.f;
-    return (threadIdx.x < 64 ? a.lse : a.delta)[(int64_t)h * a.tokens + s.begin + r];
+    if (threadIdx.x >= 128 || r >= qs.len || it0 >= it1) return 0.f;
+    return (threadIdx.x < 64 ? a.lse : a.delta)[(int64_t)h * a.tokens + qs.begin + r];
   };
   PkPair<T, DP, VEC, PK_T, 4 * R> next;
   {
     PkPair<T, DP, VEC, R, 4 * R> own;
     own.fetch(a.k, a.v, s, k0, hk, a.dim);
     pdl_wait();                                   // delta
-    if (next.kAhead && it0 < it1) next.fetch(a.q, a.d_o, s, q0, h, a.dim);
+    if (next.kAhead && it0 < it1) next.fetch(a.q, a.d_o, qs, q0, h, a.dim);
     own.x.put(sK);
     own.y.put(sV);
   }
   float next_row = row_value(h, q0);
   float dk[4][DP / 16] = {}, dv[4][DP / 16] = {};
   for (int it = it0; it < it1; ++it) {
-    if (!next.kAhead) next.fetch(a.q, a.d_o, s, q0, h, a.dim);
+    if (!next.kAhead) next.fetch(a.q, a.d_o, qs, q0, h, a.dim);
     __syncthreads();
     next.x.put(sQ);
     next.y.put(sO);
@@ -385,10 +388,10 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
     __syncthreads();
     const int r0 = q0;
     q0 += PK_T;
-    if (q0 >= s.len) { q0 = first; ++h; }
+    if (q0 >= qs.len) { q0 = first; ++h; }
     if (it + 1 < it1) {
       next_row = row_value(h, q0);
-      if (next.kAhead) next.fetch(a.q, a.d_o, s, q0, h, a.dim);
+      if (next.kAhead) next.fetch(a.q, a.d_o, qs, q0, h, a.dim);
     }
     float acc[4][4] = {}, dp[4][4] = {};
     pk_abt<DP>(acc, sK, sQ);                      // rows: keys, columns: queries
@@ -400,7 +403,7 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int c = k0 + 4 * ty + i;
-        const bool in = c < s.len && r < s.len && (!a.causal || c <= r);
+        const bool in = c < s.len && r < qs.len && (!a.causal || c <= r);
         const float p = in ? ex2((acc[i][j] * a.scale - lse) * kLog2e) : 0.f;
         sP[(4 * ty + i) * PK_LDP + tx + 16 * j] = p;
         sS[(4 * ty + i) * PK_LDP + tx + 16 * j] = in ? p * (dp[i][j] - delta) : 0.f;
@@ -458,18 +461,18 @@ template <typename T, int DP, bool VEC, int R> static cudaError_t pk_forward(con
 template <typename T, int DP, bool VEC, int R> static cudaError_t pk_backward(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   constexpr int smem = pk_smem<DP, R>(2, 2, 2);
-  const int64_t tiles = most_tiles(a.tokens, a.n_seqs, R), blocks = tiles * (a.heads + a.kv_heads);
+  const int64_t dkv = most_tiles(a.kv_tokens, a.n_seqs, R) * a.kv_heads, blocks = most_tiles(a.tokens, a.n_seqs, R) * a.heads + dkv;
   if (!launchable(blocks)) return cudaErrorInvalidConfiguration;
   cudaError_t e = pk_allow(attn_packed_bwd_kernel<T, DP, VEC, R>, smem, done);
   if (e == cudaSuccess) e = launch_pdl(attn_packed_delta_kernel<T>, dim3((unsigned)((a.tokens * a.heads + 7) / 8)), dim3(256), 0, st, false, a);
   if (e == cudaSuccess)
     e = launch_clusters(attn_packed_bwd_kernel<T, DP, VEC, R>, blocks, 4 * R, smem, st, true, pk_split<R> ? packed_parts(blocks, a, PK_T, a.group, 4 * kSms, 2) : 1, a,
-                  (int)(tiles * a.kv_heads));
+                  (int)dkv);
   return e;
 }
 template <typename T, int DP, bool VEC> static cudaError_t pk_rows(const PackedArgs& a, bool backward, cudaStream_t st) {
   // 32 rows to a block where blocks of 64 would leave SMs without one (as a rule on the most tiles that the lengths can make)
-  const bool small = most_tiles(a.tokens, a.n_seqs, PK_T) * (a.heads + (backward ? a.kv_heads : 0)) < 2 * kSms;
+  const bool small = most_tiles(a.tokens, a.n_seqs, PK_T) * a.heads + (backward ? most_tiles(a.kv_tokens, a.n_seqs, PK_T) * a.kv_heads : 0) < 2 * kSms;
   if (small) return backward ? pk_backward<T, DP, VEC, 32>(a, st) : pk_forward<T, DP, VEC, 32>(a, st);
   return backward ? pk_backward<T, DP, VEC, 64>(a, st) : pk_forward<T, DP, VEC, 64>(a, st);
 }
@@ -524,9 +527,96 @@ static pm_status pk_result(cudaError_t e, const char* what) {
 }
 static PackedArgs pk_args(const pm_attention_desc* d, const int32_t* cu, float* lse) {
   PackedArgs a{};
-  a.cu = cu; a.lse = lse; a.tokens = d->n_tokens; a.n_seqs = d->n_seqs; a.heads = d->n_heads; a.kv_heads = d->n_kv_heads;
+  a.cu = a.cu_kv = cu; a.lse = lse; a.tokens = a.kv_tokens = d->n_tokens; a.n_seqs = d->n_seqs; a.heads = d->n_heads; a.kv_heads = d->n_kv_heads;
   a.group = d->n_heads / d->n_kv_heads; a.dim = d->head_dim; a.causal = d->causal != 0; a.scale = d->scale;
   return a;
+}
+static Extent pk_starts(const int32_t* cu, int n_seqs) { return dense_extent(cu, 4 * ((int64_t)n_seqs + 1)); }
+
+// Rows of the sequences of x: zeros, and -infinity in lse (either may be absent).  For calls of cross attention whose other side has no rows at all.
+template <typename T>
+__global__ void __launch_bounds__(256) attn_cross_clear_kernel(HeadView x, const int32_t* cu, int n_seqs, int64_t tokens, int heads, int dim, float* lse) {
+  const int64_t first = min(max((int64_t)cu[0], (int64_t)0), tokens), last = min(max((int64_t)cu[n_seqs], (int64_t)0), tokens);
+  for (int64_t i = (first * heads * 32 + (int64_t)blockIdx.x * 256 + threadIdx.x) >> 5; i < last * heads; i += (int64_t)gridDim.x * 8) {
+    const int64_t token = i / heads;
+    const int h = (int)(i - token * heads), lane = threadIdx.x & 31;
+    if (x.data) for (int c = lane; c < dim; c += 32) head_row_out<T>(x, token, h)[c] = from_f<T>(0.f);
+    if (lse && lane == 0) lse[(int64_t)h * tokens + token] = -INFINITY;
+  }
+}
+static cudaError_t pk_clear(const HeadView& x, const int32_t* cu, int n_seqs, int64_t tokens, int heads, int dim, float* lse, int dtype, cudaStream_t st) {
+  const dim3 grid((unsigned)std::min<int64_t>((tokens * heads + 7) / 8, 8 * kSms));
+  return dtype == PM_BF16 ? launch_pdl(attn_cross_clear_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, false, x, cu, n_seqs, tokens, heads, dim, lse)
+                          : launch_pdl(attn_cross_clear_kernel<float>, grid, dim3(256), 0, st, false, x, cu, n_seqs, tokens, heads, dim, lse);
+}
+
+// The checks and launches that both kinds of calls share, behind those of their descriptions.
+static pm_status pk_forward_call(PackedArgs& a, int dtype, const pm_head_view* q, const pm_head_view* k, const pm_head_view* v, const pm_head_view* o,
+                                 cudaStream_t st) {
+  const int size = dtype == PM_BF16 ? 2 : 4;
+  if (const pm_status s = pk_view(a.q, q, "q", size)) return s;
+  if (a.kv_tokens) {
+    if (const pm_status s = pk_view(a.k, k, "k", size)) return s;
+    if (const pm_status s = pk_view(a.v, v, "v", size)) return s;
+  }
+  if (const pm_status s = pk_view(a.o, o, "o", size)) return s;
+  auto all = [&](const HeadView& x, int64_t tokens, int heads) { return pk_extent(x, tokens, heads, a.dim, size); };
+  const Extent written[] = {all(a.o, a.tokens, a.heads), dense_extent(a.lse, 4 * a.tokens * a.heads)};
+  const Extent read[] = {all(a.q, a.tokens, a.heads), all(a.k, a.kv_tokens, a.kv_heads), all(a.v, a.kv_tokens, a.kv_heads), pk_starts(a.cu, a.n_seqs),
+                         pk_starts(a.cu_kv, a.n_seqs)};
+  if (const pm_status s = pk_apart(written, 2, read, a.cross ? 5 : 4)) return s;
+  const cudaError_t e = a.kv_tokens == 0 ? pk_clear(a.o, a.cu, a.n_seqs, a.tokens, a.heads, a.dim, a.lse, dtype, st)
+                        : attn_packed_tc_takes(a, dtype, false) ? attn_packed_tc_forward(a, st)
+                        : dtype == PM_BF16 ? pk_run<__nv_bfloat16>(a, false, st) : pk_run<float>(a, false, st);
+  return pk_result(e, a.cross ? "cross attention" : "packed attention");
+}
+static pm_status pk_backward_call(PackedArgs& a, int dtype, const pm_head_view* q, const pm_head_view* k, const pm_head_view* v, const pm_head_view* o,
+                                  const pm_head_view* d_o, const pm_head_view* dq, const pm_head_view* dk, const pm_head_view* dv, void* workspace,
+                                  uint64_t workspace_bytes, uint64_t need, cudaStream_t st) {
+  const int size = dtype == PM_BF16 ? 2 : 4;
+  const struct { HeadView& to; const pm_head_view* from; const char* name; bool keys; } views[] = {
+      {a.q, q, "q", false}, {a.k, k, "k", true}, {a.v, v, "v", true}, {a.o, o, "o", false}, {a.d_o, d_o, "d_o", false},
+      {a.dq, dq, "dq", false}, {a.dk, dk, "dk", true}, {a.dv, dv, "dv", true}};
+  for (const auto& x : views)
+    if (x.keys ? a.kv_tokens : a.tokens)
+      if (const pm_status s = pk_view(x.to, x.from, x.name, size)) return s;
+  auto all = [&](const HeadView& x, int64_t tokens, int heads) { return pk_extent(x, tokens, heads, a.dim, size); };
+  const Extent others[] = {all(a.dq, a.tokens, a.heads), all(a.dk, a.kv_tokens, a.kv_heads), all(a.dv, a.kv_tokens, a.kv_heads),
+                           all(a.q, a.tokens, a.heads), all(a.k, a.kv_tokens, a.kv_heads), all(a.v, a.kv_tokens, a.kv_heads),
+                           all(a.o, a.tokens, a.heads), all(a.d_o, a.tokens, a.heads), dense_extent(a.lse, 4 * a.tokens * a.heads),
+                           pk_starts(a.cu, a.n_seqs), pk_starts(a.cu_kv, a.n_seqs)};
+  if (const pm_status s = pk_apart(others, 3, others + 3, a.cross ? 8 : 7)) return s;
+  if (need) {
+    if (!workspace || workspace_bytes < need) return ops_fail(PM_ERR_NOMEM, "workspace too small: need %llu bytes", (unsigned long long)need);
+    if (!aligned_to(workspace, 4)) return ops_fail(PM_ERR_INVALID_ARG, "workspace must be 4-byte aligned");
+    for (const Extent& x : others) if (extents_share(dense_extent(workspace, (int64_t)need), x)) return ops_fail(PM_ERR_INVALID_ARG, "the workspace overlaps a tensor");
+  }
+  a.delta = static_cast<float*>(workspace);
+  cudaError_t e;
+  if (a.tokens == 0) {
+    e = pk_clear(a.dk, a.cu_kv, a.n_seqs, a.kv_tokens, a.kv_heads, a.dim, nullptr, dtype, st);
+    if (e == cudaSuccess) e = pk_clear(a.dv, a.cu_kv, a.n_seqs, a.kv_tokens, a.kv_heads, a.dim, nullptr, dtype, st);
+  } else if (a.kv_tokens == 0) {
+    e = pk_clear(a.dq, a.cu, a.n_seqs, a.tokens, a.heads, a.dim, nullptr, dtype, st);
+  } else {
+    e = attn_packed_tc_takes(a, dtype, true) ? attn_packed_tc_backward(a, st)
+        : dtype == PM_BF16 ? pk_run<__nv_bfloat16>(a, true, st) : pk_run<float>(a, true, st);
+  }
+  return pk_result(e, a.cross ? "cross attention backward" : "packed attention backward");
+}
+static pm_attention_desc pk_side(const pm_cross_attention_desc& d, int64_t tokens) {
+  return pm_attention_desc{d.dtype, d.n_heads, d.n_kv_heads, d.head_dim, d.n_seqs, 0, tokens, d.scale};
+}
+static pm_status pk_cross_args(PackedArgs& a, const pm_cross_attention_desc* d, const int32_t* cu, const int32_t* cu_kv, float* lse) {
+  if (!d) return ops_fail(PM_ERR_INVALID_ARG, "null argument");
+  const pm_attention_desc queries = pk_side(*d, d->n_tokens), keys = pk_side(*d, d->n_kv_tokens);
+  if (const pm_status s = pk_check(&queries)) return s;
+  if (const pm_status s = pk_check(&keys)) return s;
+  a = pk_args(&queries, cu, lse);
+  a.cu_kv = cu_kv;
+  a.kv_tokens = d->n_kv_tokens;
+  a.cross = 1;
+  return PM_OK;
 }
 
 }  // namespace pm
@@ -541,19 +631,7 @@ pm_status pm_attention_packed_forward(const pm_attention_desc* d, const pm_head_
   if (d->n_tokens == 0 || d->n_seqs == 0) return PM_OK;
   if (!cu_seqlens) return ops_fail(PM_ERR_INVALID_ARG, "null cu_seqlens");
   PackedArgs a = pk_args(d, cu_seqlens, lse);
-  const int size = d->dtype == PM_BF16 ? 2 : 4;
-  if (const pm_status s = pk_view(a.q, q, "q", size)) return s;
-  if (const pm_status s = pk_view(a.k, k, "k", size)) return s;
-  if (const pm_status s = pk_view(a.v, v, "v", size)) return s;
-  if (const pm_status s = pk_view(a.o, o, "o", size)) return s;
-  auto all = [&](const HeadView& x, int heads) { return pk_extent(x, a.tokens, heads, a.dim, size); };
-  const Extent written[] = {all(a.o, a.heads), dense_extent(lse, 4 * a.tokens * a.heads)};
-  const Extent read[] = {all(a.q, a.heads), all(a.k, a.kv_heads), all(a.v, a.kv_heads), dense_extent(cu_seqlens, 4 * ((int64_t)a.n_seqs + 1))};
-  if (const pm_status s = pk_apart(written, 2, read, 4)) return s;
-  const cudaStream_t st = (cudaStream_t)stream;
-  const cudaError_t e = attn_packed_tc_takes(a, d->dtype, false) ? attn_packed_tc_forward(a, st)
-                        : d->dtype == PM_BF16 ? pk_run<__nv_bfloat16>(a, false, st) : pk_run<float>(a, false, st);
-  return pk_result(e, "packed attention");
+  return pk_forward_call(a, d->dtype, q, k, v, o, (cudaStream_t)stream);
 }
 
 uint64_t pm_attention_packed_workspace_bytes(const pm_attention_desc* d) {
@@ -568,29 +646,33 @@ pm_status pm_attention_packed_backward(const pm_attention_desc* d, const pm_head
   if (d->n_tokens == 0 || d->n_seqs == 0) return PM_OK;
   if (!cu_seqlens || !lse) return ops_fail(PM_ERR_INVALID_ARG, "null cu_seqlens or lse");
   PackedArgs a = pk_args(d, cu_seqlens, const_cast<float*>(lse));
-  const int size = d->dtype == PM_BF16 ? 2 : 4;
-  if (const pm_status s = pk_view(a.q, q, "q", size)) return s;
-  if (const pm_status s = pk_view(a.k, k, "k", size)) return s;
-  if (const pm_status s = pk_view(a.v, v, "v", size)) return s;
-  if (const pm_status s = pk_view(a.o, o, "o", size)) return s;
-  if (const pm_status s = pk_view(a.d_o, d_o, "d_o", size)) return s;
-  if (const pm_status s = pk_view(a.dq, dq, "dq", size)) return s;
-  if (const pm_status s = pk_view(a.dk, dk, "dk", size)) return s;
-  if (const pm_status s = pk_view(a.dv, dv, "dv", size)) return s;
-  auto all = [&](const HeadView& x, int heads) { return pk_extent(x, a.tokens, heads, a.dim, size); };
-  const Extent others[] = {all(a.dq, a.heads), all(a.dk, a.kv_heads), all(a.dv, a.kv_heads), all(a.q, a.heads), all(a.k, a.kv_heads), all(a.v, a.kv_heads),
-                           all(a.o, a.heads), all(a.d_o, a.heads), dense_extent(lse, 4 * a.tokens * a.heads),
-                           dense_extent(cu_seqlens, 4 * ((int64_t)a.n_seqs + 1))};
-  if (const pm_status s = pk_apart(others, 3, others + 3, 7)) return s;
-  const uint64_t need = pm_attention_packed_workspace_bytes(d);
-  if (!workspace || workspace_bytes < need) return ops_fail(PM_ERR_NOMEM, "workspace too small: need %llu bytes", (unsigned long long)need);
-  if (!aligned_to(workspace, 4)) return ops_fail(PM_ERR_INVALID_ARG, "workspace must be 4-byte aligned");
-  for (const Extent& x : others) if (extents_share(dense_extent(workspace, (int64_t)need), x)) return ops_fail(PM_ERR_INVALID_ARG, "the workspace overlaps a tensor");
-  a.delta = static_cast<float*>(workspace);
-  const cudaStream_t st = (cudaStream_t)stream;
-  const cudaError_t e = attn_packed_tc_takes(a, d->dtype, true) ? attn_packed_tc_backward(a, st)
-                        : d->dtype == PM_BF16 ? pk_run<__nv_bfloat16>(a, true, st) : pk_run<float>(a, true, st);
-  return pk_result(e, "packed attention backward");
+  return pk_backward_call(a, d->dtype, q, k, v, o, d_o, dq, dk, dv, workspace, workspace_bytes, pm_attention_packed_workspace_bytes(d), (cudaStream_t)stream);
+}
+
+pm_status pm_attention_cross_forward(const pm_cross_attention_desc* d, const pm_head_view* q, const pm_head_view* k, const pm_head_view* v,
+                                     const int32_t* cu_seqlens, const int32_t* cu_seqlens_kv, const pm_head_view* o, float* lse, void* stream) {
+  PackedArgs a;
+  if (const pm_status s = pk_cross_args(a, d, cu_seqlens, cu_seqlens_kv, lse)) return s;
+  if (d->n_tokens == 0 || d->n_seqs == 0) return PM_OK;
+  if (!cu_seqlens || !cu_seqlens_kv) return ops_fail(PM_ERR_INVALID_ARG, "null cu_seqlens or cu_seqlens_kv");
+  return pk_forward_call(a, d->dtype, q, k, v, o, (cudaStream_t)stream);
+}
+
+uint64_t pm_attention_cross_workspace_bytes(const pm_cross_attention_desc* d) {
+  if (!d) return 0;
+  const pm_attention_desc queries = pk_side(*d, d->n_tokens);
+  return pm_attention_packed_workspace_bytes(&queries);
+}
+
+pm_status pm_attention_cross_backward(const pm_cross_attention_desc* d, const pm_head_view* q, const pm_head_view* k, const pm_head_view* v,
+                                      const pm_head_view* o, const float* lse, const pm_head_view* d_o, const int32_t* cu_seqlens,
+                                      const int32_t* cu_seqlens_kv, const pm_head_view* dq, const pm_head_view* dk, const pm_head_view* dv,
+                                      void* workspace, uint64_t workspace_bytes, void* stream) {
+  PackedArgs a;
+  if (const pm_status s = pk_cross_args(a, d, cu_seqlens, cu_seqlens_kv, const_cast<float*>(lse))) return s;
+  if ((d->n_tokens == 0 && d->n_kv_tokens == 0) || d->n_seqs == 0) return PM_OK;
+  if (!cu_seqlens || !cu_seqlens_kv || (!lse && d->n_tokens)) return ops_fail(PM_ERR_INVALID_ARG, "null cu_seqlens, cu_seqlens_kv or lse");
+  return pk_backward_call(a, d->dtype, q, k, v, o, d_o, dq, dk, dv, workspace, workspace_bytes, pm_attention_cross_workspace_bytes(d), (cudaStream_t)stream);
 }
 
 pm_status pm_attention_packed_selftest_wait_timeout(int64_t limit_cycles, void* stream) {

@@ -1,4 +1,5 @@
-// Attention over packed sequences: arguments and the map from a block to its tile of a sequence.
+// Attention over packed sequences, of their own tokens or (cross attention) of the sequences of another tensor: arguments and the map
+// from a block to its tile of a sequence.
 #pragma once
 #include "pm_ops.cuh"
 
@@ -10,10 +11,10 @@ struct HeadView {
 };
 struct PackedArgs {
   HeadView q, k, v, o, d_o, dq, dk, dv;           // o is written by the forward pass, dq, dk, dv by the backward pass
-  const int32_t* cu;                              // [n_seqs + 1]
+  const int32_t *cu, *cu_kv;                      // [n_seqs + 1], of the queries and of the keys: the same array without `cross`
   float *lse, *delta;                             // [heads][tokens]
-  int64_t tokens;
-  int n_seqs, heads, kv_heads, group, dim, causal;
+  int64_t tokens, kv_tokens;                      // rows of q, o and of k, v
+  int n_seqs, heads, kv_heads, group, dim, causal, cross;
   float scale;
 };
 
@@ -27,6 +28,7 @@ template <typename T> __device__ __forceinline__ T* head_row_out(const HeadView&
 struct SeqTile {
   int64_t begin;                                  // first token of the sequence
   int len, tile;                                  // its length; the tile's index inside it (-1: no such tile)
+  int seq;                                        // which sequence it is
 };
 
 // The index-th tile of up to 32 PER sequences, PER consecutive ones to a lane: tiles counted through the sequences.
@@ -46,15 +48,16 @@ __device__ __forceinline__ SeqTile find_counted(const int32_t* cu, int n_seqs, i
   for (int o = 1; o < 32; o *= 2) { const int v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
   int at = upto - mine;
   const unsigned has = __ballot_sync(0xffffffffu, index >= at && index < at + mine);
-  if (!has) return SeqTile{0, 0, -1};
-  int tile = 0, len = 0, begin = 0;
+  if (!has) return SeqTile{0, 0, -1, 0};
+  int tile = 0, len = 0, begin = 0, seq = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    if (index >= at && index < at + tiles[i]) { tile = index - at; begin = start[i]; len = start[i + 1] - start[i]; }
+    if (index >= at && index < at + tiles[i]) { tile = index - at; begin = start[i]; len = start[i + 1] - start[i]; seq = lane * PER + i; }
     at += tiles[i];
   }
   const int who = __ffs(has) - 1;
-  return SeqTile{__shfl_sync(0xffffffffu, begin, who), __shfl_sync(0xffffffffu, len, who), __shfl_sync(0xffffffffu, tile, who)};
+  return SeqTile{__shfl_sync(0xffffffffu, begin, who), __shfl_sync(0xffffffffu, len, who), __shfl_sync(0xffffffffu, tile, who),
+                 __shfl_sync(0xffffffffu, seq, who)};
 }
 
 // The tile that has a slot: sequence b has the slots from (its start >> log_rows) + b to the next sequence's, at least as many as it has tiles
@@ -63,7 +66,7 @@ __device__ __forceinline__ SeqTile find_counted(const int32_t* cu, int n_seqs, i
 static __device__ __noinline__ SeqTile find_slot(const int32_t* cu, int n_seqs, int tokens, int slot, int log_rows) {
   const int lane = threadIdx.x & 31;
   auto start = [&](int b) { return min(max(cu[min(b, n_seqs)], 0), tokens); };
-  const SeqTile none{0, 0, -1};
+  const SeqTile none{0, 0, -1, 0};
   int first = 0, n = n_seqs;                      // the sequence is one of n from the first on
   while (n > 32) {
     const int step = (n + 31) / 32, b = first + lane * step;
@@ -78,7 +81,7 @@ static __device__ __noinline__ SeqTile find_slot(const int32_t* cu, int n_seqs, 
   const int begin = __shfl_sync(0xffffffffu, mine, k - 1), next = __shfl_sync(0xffffffffu, mine, k & 31), end = k < 32 ? next : start(first + 32);
   const int len = end - begin, tile = slot - (begin >> log_rows) - (first + k - 1);
   if (tile < 0 || tile >= (len + (1 << log_rows) - 1) >> log_rows) return none;
-  return SeqTile{begin, len, tile};
+  return SeqTile{begin, len, tile, first + k - 1};
 }
 
 // The tile of 2^log_rows rows of the index-th block; called by a whole warp, same result in every lane.  Up to 256 sequences are counted in one
@@ -91,6 +94,13 @@ __device__ __forceinline__ SeqTile find_tile(const int32_t* cu, int n_seqs, int6
   if (n_seqs <= 32) return find_counted<1>(cu, n_seqs, (int)tokens, index, log_rows);
   if (n_seqs <= 256) return find_counted<8>(cu, n_seqs, (int)tokens, index, log_rows);
   return find_slot(cu, n_seqs, (int)tokens, index, log_rows);
+}
+
+// The rows of the other side that a tile's sequence meets: of an encoder's states with `cross`, else its own tokens.  Clipped as above.
+__device__ __forceinline__ SeqTile other_side(bool cross, const SeqTile& s, const int32_t* cu, int64_t tokens) {
+  if (!cross) return s;
+  const int begin = min(max(cu[s.seq], 0), (int)tokens), end = min(max(cu[s.seq + 1], 0), (int)tokens);
+  return SeqTile{begin, max(end - begin, 0), 0, s.seq};
 }
 
 // tiles of `rows` rows that sequences of `tokens` tokens in all can have at most, and their slots
@@ -126,8 +136,11 @@ inline cudaError_t launch_clusters(void (*kernel)(K...), int64_t blocks, int thr
 // not: bf16, 2000 tokens, 2 heads of 64 on 1, forward 18 / 27, backward 35 / 76; 4000 tokens, 4 heads of 128, forward 45 / 63; 2 x 1000
 // tokens, 8 heads of 128 on 2, backward 49 / 70; fp32, 700 + 300 + 13 tokens, 4 heads of 128 on 2, both 205 / 305; 493 tokens in 7, 4
 // heads of 32 on 2, both 27 / 31.  Finer parts lose: the backward pass of the 2 x 1000 tokens in eight parts takes 80.
+// Blocks that stream keys and blocks that stream the queries of `heads` heads share alike: by the longer of the two, and a part
+// that gets nothing of the shorter adds zeros.
 inline int packed_parts(int64_t blocks, const PackedArgs& a, int rows, int heads, int most, int least) {
-  const int64_t average = (a.tokens + a.n_seqs - 1) / a.n_seqs, tiles = (average + rows - 1) / rows * heads;
+  auto streamed = [&](int64_t tokens) { return ((tokens + a.n_seqs - 1) / a.n_seqs + rows - 1) / rows; };
+  const int64_t tiles = std::max(streamed(a.tokens) * heads, a.cross ? streamed(a.kv_tokens) : 0);
   int parts = 1;
   while (parts < 8 && blocks * parts * 2 <= most && tiles >= parts * 2 * least) parts *= 2;
   return parts;

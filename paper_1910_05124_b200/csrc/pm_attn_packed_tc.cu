@@ -190,7 +190,9 @@ __device__ __forceinline__ float2 ex2_fma(float2 x) {
 // none / 1/8 / 1/4 / 3/8 / 1/2: heads of 128 230 / 231 / 229 / 235 / 244, heads of 64 211 / 191 / 200 / 198 / 206.
 constexpr uint32_t FWD_FMA = 0x8080;
 
-template <int DT, int NT>
+// X: the keys are those of other sequences (cross attention), which may have none; a template, so that the registers of a row of scores
+// are as many as they are without.
+template <int DT, int NT, bool X>
 __global__ void __launch_bounds__(FwdShape<DT, NT>::kThreads, FwdShape<DT, NT>::kBlocks)
 attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcMaps maps, int units, int pair_heads) {
   using S = FwdShape<DT, NT>;
@@ -238,13 +240,14 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
     if (warp == kIssue) tmem_dealloc(*tmem_slot, S::kCols);
     return;
   }
+  const SeqTile ks = other_side(X, s, a.cu_kv, a.kv_tokens);
   // the last tiles of a sequence see the most keys: they come first
   const int tile = ((s.len + rows - 1) >> log_rows) - 1 - s.tile;
   auto head_of = [&](int t) { return pair_heads ? unit * 2 + t : unit; };
   auto first_of = [&](int t) { return pair_heads ? tile * TC_ROWS : (tile * NT + t) * TC_ROWS; };
   auto keys_of = [&](int t) {                     // key tiles that query tile t sees
     const int q0 = first_of(t);
-    return q0 >= s.len ? 0 : ((a.causal ? min(s.len, q0 + TC_ROWS) : s.len) + TC_ROWS - 1) / TC_ROWS;
+    return q0 >= s.len ? 0 : ((!X && a.causal ? min(s.len, q0 + TC_ROWS) : ks.len) + TC_ROWS - 1) / TC_ROWS;
   };
   const int hk = head_of(0) / a.group;
   // of the key tiles, this block's share
@@ -254,12 +257,12 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
 
   auto copy_keys = [&](int j) {
     const int st = j % S::kStages;
-    if (elect_one()) { mbar_arrive_expect_tx(k_full(st), S::kTile); load_tile<DT>(sK + st * S::kTile, &maps.k, k_full(st), hk, s.begin + (j0 + j) * TC_ROWS); }
+    if (elect_one()) { mbar_arrive_expect_tx(k_full(st), S::kTile); load_tile<DT>(sK + st * S::kTile, &maps.k, k_full(st), hk, ks.begin + (j0 + j) * TC_ROWS); }
     __syncwarp();
   };
   auto copy_values = [&](int j) {
     const int st = j % S::kStages;
-    if (elect_one()) { mbar_arrive_expect_tx(v_full(st), S::kTile); load_tile<DT>(sV + st * S::kTile, &maps.v, v_full(st), hk, s.begin + (j0 + j) * TC_ROWS); }
+    if (elect_one()) { mbar_arrive_expect_tx(v_full(st), S::kTile); load_tile<DT>(sV + st * S::kTile, &maps.v, v_full(st), hk, ks.begin + (j0 + j) * TC_ROWS); }
     __syncwarp();
   };
   if (warp == kCopy && n_keys > 0) {
@@ -397,11 +400,23 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kSoftmaxRegs));
     const int t = warp >> 2, r = threadIdx.x & 127;
     const int n = count_of(t), q0 = first_of(t), row = q0 + r;
-    if (n > 0 || parts > 1) {
+    if (X && ks.len == 0) {                       // no keys: zeros
+      if (parts > 1) {                            // as the other warps do
+        __syncwarp();
+        cluster_sync_all();
+        cluster_sync_all();
+      }
+      if (part == 0 && row < s.len) {
+        const int h = head_of(t);
+        uint4* const out = reinterpret_cast<uint4*>(head_row_out<__nv_bfloat16>(a.o, s.begin + row, h));
+        for (int i = 0; i < a.dim / 8; ++i) out[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (a.lse) a.lse[(int64_t)h * a.tokens + s.begin + row] = -INFINITY;
+      }
+    } else if (n > 0 || parts > 1) {
       const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
       const uint32_t ts = col_s(t) + lanes, to = col_o(t) + lanes, tp = col_p(t) + lanes;
       const float c = a.scale * kLog2e;
-      const int limit = a.causal ? min(s.len, row + 1) : s.len;      // keys this row sees
+      const int limit = !X && a.causal ? min(s.len, row + 1) : ks.len;      // keys this row sees
       float m = -INFINITY, l = 0.f;               // m: the maximum in use, times c
       bool ok = true;
       for (int j = 0; j < n; ++j) {
@@ -410,11 +425,11 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
         if (!ok) break;
         tc_fence_after();
         const int k0 = (j0 + j) * TC_ROWS;
-        const bool edge = k0 + TC_ROWS > s.len || (a.causal && k0 + TC_ROWS > q0 + 1);
+        const bool edge = k0 + TC_ROWS > ks.len || (!X && a.causal && k0 + TC_ROWS > q0 + 1);
         // The rows behind the sequence's end of its last value tile belong to other sequences, or to none: zeros, as p is there, so
         // that nothing that is not finite meets a zero.  The first query tile that reads the tile clears it.
-        if (k0 + TC_ROWS > s.len && (t == 0 || keys_of(0) <= j)) {
-          const int st = j % S::kStages, valid = s.len - k0;
+        if (k0 + TC_ROWS > ks.len && (t == 0 || keys_of(0) <= j)) {
+          const int st = j % S::kStages, valid = ks.len - k0;
           ok = wait_for(v_full(st), (j / S::kStages) & 1, abort_flag, status, 40);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
@@ -618,7 +633,13 @@ template <int DT> __device__ __forceinline__ void clear_rows(uint8_t* tile, int 
 }
 struct TcBwdMaps { CUtensorMap q, k, v, d_o; };
 
-template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a, const TcBwdMaps& maps, int block, int part, int parts) {
+// 32 columns of a row
+__device__ __forceinline__ void zero_columns(__nv_bfloat16* row, int c0, int dim) {
+#pragma unroll
+  for (int c = c0; c < c0 + 32; c += 8) if (c < dim) *reinterpret_cast<uint4*>(row + c) = make_uint4(0u, 0u, 0u, 0u);
+}
+
+template <int DT, bool X> __device__ __forceinline__ void dkv_block(const PackedArgs& a, const TcBwdMaps& maps, int block, int part, int parts) {
   using S = BwdShape<DT>;
   constexpr int BN = S::kCols, kCopy = S::kParts * 4, kIssue = kCopy + 1;        // the warps that copy and issue
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = block % a.kv_heads;
@@ -650,23 +671,24 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
     tmem_alloc(smem_u32(tmem_slot), S::kTmem);
     tmem_relinquish();
   }
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.kv_heads, TC_LOG_ROWS);
+  const SeqTile s = find_tile(a.cu_kv, a.n_seqs, a.kv_tokens, block / a.kv_heads, TC_LOG_ROWS);
   if (s.tile < 0) {
     __syncthreads();
     if (warp == kIssue) tmem_dealloc(*tmem_slot, S::kTmem);
     pdl_wait();
     return;
   }
-  const int k0 = s.tile * TC_ROWS, first = a.causal ? k0 : 0;
+  const SeqTile qs = other_side(X, s, a.cu, a.tokens);
+  const int k0 = s.tile * TC_ROWS, first = !X && a.causal ? k0 : 0;
   // of the query tiles of all heads that share these keys, this block's share
-  const int per_head = (s.len - first + BN - 1) / BN, it0 = per_head * a.group * part / parts, n_it = per_head * a.group * (part + 1) / parts - it0;
-  const int h0 = hk * a.group + it0 / per_head, first_q0 = first + it0 % per_head * BN;
+  const int per_head = (qs.len - first + BN - 1) / BN, it0 = per_head * a.group * part / parts, n_it = per_head * a.group * (part + 1) / parts - it0;
+  const int some = X ? max(per_head, 1) : per_head, h0 = hk * a.group + it0 / some, first_q0 = first + it0 % some * BN;
   auto copy_queries = [&](int it, int h, int q0) {
     const int st = it % S::kStages;
     if (elect_one()) {
       mbar_arrive_expect_tx(full(st), 2 * S::kStream);
-      copy_rows<DT, BN>(sQ + st * S::kStream, &maps.q, full(st), h, s.begin + q0);
-      copy_rows<DT, BN>(sO + st * S::kStream, &maps.d_o, full(st), h, s.begin + q0);
+      copy_rows<DT, BN>(sQ + st * S::kStream, &maps.q, full(st), h, qs.begin + q0);
+      copy_rows<DT, BN>(sO + st * S::kStream, &maps.d_o, full(st), h, qs.begin + q0);
     }
     __syncwarp();
   };
@@ -702,21 +724,21 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
 #pragma unroll
       for (int i = 0; i < BN; i += 32) {
         const int r = q0 + i + lane;
-        const int64_t at = (int64_t)h * a.tokens + s.begin + r;
-        rows[i + lane] = r < s.len ? a.lse[at] * kLog2e : INFINITY;              // no row: probability zero
-        rows[BN + i + lane] = r < s.len ? a.delta[at] : 0.f;
+        const int64_t at = (int64_t)h * a.tokens + qs.begin + r;
+        rows[i + lane] = r < qs.len ? a.lse[at] * kLog2e : INFINITY;              // no row: probability zero
+        rows[BN + i + lane] = r < qs.len ? a.delta[at] : 0.f;
       }
-      if (q0 + BN > s.len) {                      // rows of other sequences, or of none: zeros, where P and dS are zero
+      if (q0 + BN > qs.len) {                      // rows of other sequences, or of none: zeros, where P and dS are zero
         ok = wait_for(full(st), (it / S::kStages) & 1, abort_flag, status, 52);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        clear_rows<DT>(sptr + (sQ - base) + st * S::kStream, s.len - q0);
-        clear_rows<DT>(sptr + (sO - base) + st * S::kStream, s.len - q0);
+        clear_rows<DT>(sptr + (sQ - base) + st * S::kStream, qs.len - q0);
+        clear_rows<DT>(sptr + (sO - base) + st * S::kStream, qs.len - q0);
         fence_async_smem();
       }
       mbar_arrive(row_full(st));
       q0 += BN;
-      if (q0 >= s.len) { q0 = first; ++h; }
+      if (q0 >= qs.len) { q0 = first; ++h; }
     }
     if (*abort_flag && n_it > 0) {                // nothing may be in flight when the block ends
       volatile int never = 0;
@@ -790,7 +812,7 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
           const float2 y = fma_f32x2(make_float2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), make_float2(c, c), make_float2(-l.z, -l.w));
           p[i] = ex2(x.x); p[i + 1] = ex2(x.y); p[i + 2] = ex2(y.x); p[i + 3] = ex2(y.y);
         }
-        if (a.causal && q0 < k0 + TC_ROWS)
+        if (!X && a.causal && q0 < k0 + TC_ROWS)
 #pragma unroll
           for (int i = 0; i < 32; ++i)
             if (q0 + c0 + i < key) p[i] = 0.f;
@@ -825,7 +847,7 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
       __syncwarp();
       if (lane == 0) mbar_arrive(ds_full);
       q0 += BN;
-      if (q0 >= s.len) q0 = first;
+      if (q0 >= qs.len) q0 = first;
     }
     if (ok && n_it > 0) ok = wait_for(acc_full, 0, abort_flag, status, 62);
     ok = __all_sync(0xffffffffu, ok);
@@ -844,6 +866,11 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
       finish_rows<DT>(a.dv, s, k0, hk, a.dim, dv, part, parts, S::kParts * 128, [&](int, int) { return 1.f; });
       __syncwarp();
       cluster_sync_all();                         // the others have read this block's sums
+    } else if (X && n_it == 0) {                  // no queries: zeros
+      if (key < s.len) {
+        zero_columns(head_row_out<__nv_bfloat16>(a.dv, s.begin + key, hk), c0, a.dim);
+        zero_columns(head_row_out<__nv_bfloat16>(a.dk, s.begin + key, hk), c0, a.dim);
+      }
     } else {
       const int first_row = k0 + (warp & 3) * 32;
       uint8_t* const stage = sptr + (sQ - base) + warp * 2048;           // the streamed tiles have been read
@@ -866,7 +893,7 @@ template <int DT> __device__ __forceinline__ void dkv_block(const PackedArgs& a,
   }
 }
 
-template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, const TcBwdMaps& maps, int block, int part, int parts) {
+template <int DT, bool X> __device__ __forceinline__ void dq_block(const PackedArgs& a, const TcBwdMaps& maps, int block, int part, int parts) {
   using S = BwdShape<DT>;
   constexpr int BN = S::kCols, kCopy = S::kParts * 4, kIssue = kCopy + 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = block % a.heads, hk = h / a.group;
@@ -902,15 +929,16 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
     pdl_wait();
     return;
   }
+  const SeqTile ks = other_side(X, s, a.cu_kv, a.kv_tokens);
   const int tile = (s.len + TC_ROWS - 1) / TC_ROWS - 1 - s.tile;                 // the tiles that see the most keys first
-  const int q0 = tile * TC_ROWS, all = ((a.causal ? min(s.len, q0 + TC_ROWS) : s.len) + BN - 1) / BN;
+  const int q0 = tile * TC_ROWS, all = ((!X && a.causal ? min(s.len, q0 + TC_ROWS) : ks.len) + BN - 1) / BN;
   const int it0 = all * part / parts, n_it = all * (part + 1) / parts - it0;     // of the key tiles, this block's share
   auto copy_keys = [&](int it) {
     const int st = it % S::kStages;
     if (elect_one()) {
       mbar_arrive_expect_tx(full(st), 2 * S::kStream);
-      copy_rows<DT, BN>(sK + st * S::kStream, &maps.k, full(st), hk, s.begin + (it0 + it) * BN);
-      copy_rows<DT, BN>(sV + st * S::kStream, &maps.v, full(st), hk, s.begin + (it0 + it) * BN);
+      copy_rows<DT, BN>(sK + st * S::kStream, &maps.k, full(st), hk, ks.begin + (it0 + it) * BN);
+      copy_rows<DT, BN>(sV + st * S::kStream, &maps.v, full(st), hk, ks.begin + (it0 + it) * BN);
     }
     __syncwarp();
   };
@@ -941,11 +969,11 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
         copy_keys(it);
         ++armed;
       }
-      if (k0 + BN > s.len) {                      // keys of other sequences, or of none: zeros, where dS is zero
+      if (k0 + BN > ks.len) {                      // keys of other sequences, or of none: zeros, where dS is zero
         ok = wait_for(full(st), (it / S::kStages) & 1, abort_flag, status, 72);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        clear_rows<DT>(sptr + (sK - base) + st * S::kStream, s.len - k0);
+        clear_rows<DT>(sptr + (sK - base) + st * S::kStream, ks.len - k0);
         fence_async_smem();
       }
       mbar_arrive(cleared(st));
@@ -999,7 +1027,7 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
     const int64_t at = (int64_t)h * a.tokens + s.begin + row;
     pdl_wait();                                   // delta
     const float lse = row < s.len ? a.lse[at] * kLog2e : INFINITY, delta = row < s.len ? a.delta[at] : 0.f;
-    const int limit = a.causal ? min(s.len, row + 1) : s.len;
+    const int limit = !X && a.causal ? min(s.len, row + 1) : ks.len;
     bool ok = true;
     for (int it = 0; it < n_it; ++it) {
       const int k0 = (it0 + it) * BN;
@@ -1027,7 +1055,7 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
         const float2 x = add_f32x2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(-delta, -delta));
         p[i] *= x.x; p[i + 1] *= x.y;
       }
-      if (k0 + BN > s.len || (a.causal && k0 + BN > q0 + 1))
+      if (k0 + BN > ks.len || (!X && a.causal && k0 + BN > q0 + 1))
 #pragma unroll
         for (int i = 0; i < 32; ++i)
           if (k0 + c0 + i >= limit) p[i] = 0.f;
@@ -1052,6 +1080,8 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
       finish_rows<DT>(a.dq, s, q0, h, a.dim, sums, part, parts, S::kParts * 128, [&](int, int) { return a.scale; });
       __syncwarp();
       cluster_sync_all();                         // the others have read this block's sums
+    } else if (X && n_it == 0) {                  // no keys: zeros
+      if (row < s.len) zero_columns(head_row_out<__nv_bfloat16>(a.dq, s.begin + row, h), c0, a.dim);
     } else {
       const int first_row = q0 + (warp & 3) * 32;
       store_rows(head_row_out<__nv_bfloat16>(a.dq, s.begin + first_row, h), a.dq.token, s.len - first_row, col_dq + lanes, c0, a.dim, a.scale, ok,
@@ -1072,12 +1102,12 @@ template <int DT> __device__ __forceinline__ void dq_block(const PackedArgs& a, 
 }
 
 // The blocks of dk and dv, and behind them, on the SMs that the longest of those leave free, the blocks of dq.
-template <int DT>
+template <int DT, bool X>
 __global__ void __launch_bounds__(BwdShape<DT>::kThreads, BwdShape<DT>::kBlocks)
 attn_packed_bwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcBwdMaps maps, int dkv_blocks) {
   const int parts = (int)cg::this_cluster().num_blocks(), part = (int)cg::this_cluster().block_rank(), block = blockIdx.x / parts;
-  if (block < dkv_blocks) dkv_block<DT>(a, maps, block, part, parts);
-  else dq_block<DT>(a, maps, block - dkv_blocks, part, parts);
+  if (block < dkv_blocks) dkv_block<DT, X>(a, maps, block, part, parts);
+  else dq_block<DT, X>(a, maps, block - dkv_blocks, part, parts);
 }
 
 // delta_i = do_i . o_i: eight lanes a row, two rows to each lane with all loads in flight; blockIdx.y is the head.  Rows outside the
@@ -1156,11 +1186,11 @@ static bool tc_view(const HeadView& x, int heads, int64_t tokens) {
 }
 
 bool attn_packed_tc_takes(const PackedArgs& a, int dtype, bool backward) {
-  const bool inputs = dtype == PM_BF16 && a.dim % 8 == 0 && tc_view(a.q, a.heads, a.tokens) && tc_view(a.k, a.kv_heads, a.tokens) &&
-                      tc_view(a.v, a.kv_heads, a.tokens) && tc_view(a.o, a.heads, a.tokens);
+  const bool inputs = dtype == PM_BF16 && a.dim % 8 == 0 && tc_view(a.q, a.heads, a.tokens) && tc_view(a.k, a.kv_heads, a.kv_tokens) &&
+                      tc_view(a.v, a.kv_heads, a.kv_tokens) && tc_view(a.o, a.heads, a.tokens);
   if (!inputs || !backward) return inputs;
-  return tc_view(a.d_o, a.heads, a.tokens) && tc_view(a.dq, a.heads, a.tokens) && tc_view(a.dk, a.kv_heads, a.tokens) &&
-         tc_view(a.dv, a.kv_heads, a.tokens);
+  return tc_view(a.d_o, a.heads, a.tokens) && tc_view(a.dq, a.heads, a.tokens) && tc_view(a.dk, a.kv_heads, a.kv_tokens) &&
+         tc_view(a.dv, a.kv_heads, a.kv_tokens);
 }
 
 template <typename K> static cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>& done) {
@@ -1173,51 +1203,55 @@ template <typename K> static cudaError_t allow_smem(K kernel, int bytes, std::at
   return e;
 }
 
-template <int DT, int NT> static cudaError_t fwd_launch(const PackedArgs& a, cudaStream_t st) {
+template <int DT, int NT, bool X> static cudaError_t fwd_launch(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   using S = FwdShape<DT, NT>;
   TcMaps maps;
   const int pair = NT == 2 && a.group % 2 == 0, units = pair ? a.heads / 2 : a.heads;
   const int64_t blocks = most_tiles(a.tokens, a.n_seqs, pair ? TC_ROWS : NT * TC_ROWS) * units;
   if (!launchable(blocks)) return cudaErrorInvalidConfiguration;
-  cudaError_t e = allow_smem(attn_packed_fwd_tc_kernel<DT, NT>, S::kSmem, done);
+  cudaError_t e = allow_smem(attn_packed_fwd_tc_kernel<DT, NT, X>, S::kSmem, done);
   if (e == cudaSuccess) e = encode_heads(&maps.q, a.q, a.dim, a.heads, a.tokens, TC_ROWS);
-  if (e == cudaSuccess) e = encode_heads(&maps.k, a.k, a.dim, a.kv_heads, a.tokens, TC_ROWS);
-  if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.tokens, TC_ROWS);
+  if (e == cudaSuccess) e = encode_heads(&maps.k, a.k, a.dim, a.kv_heads, a.kv_tokens, TC_ROWS);
+  if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.kv_tokens, TC_ROWS);
   if (e != cudaSuccess) return e;
   const int parts = NT == 1 ? packed_parts(blocks, a, TC_ROWS, 1, 2 * kSms, 3) : 1;
-  return launch_clusters(attn_packed_fwd_tc_kernel<DT, NT>, blocks, S::kThreads, S::kSmem, st, false, parts, a, maps, units, pair);
+  return launch_clusters(attn_packed_fwd_tc_kernel<DT, NT, X>, blocks, S::kThreads, S::kSmem, st, false, parts, a, maps, units, pair);
 }
 
 // Two query tiles to a block read keys and values half as often and pay for heads of 128 once every SM has such a block.  8192 tokens,
 // 16 heads of 128, us with two / one: 240 / 252; 4000 tokens, 4 heads of 128: 68 / 63; 8192 tokens, 16 heads of 64: 213 / 205.
-cudaError_t attn_packed_tc_forward(const PackedArgs& a, cudaStream_t st) {
-  if (a.dim <= 64) return fwd_launch<64, 1>(a, st);
+template <bool X> static cudaError_t tc_forward(const PackedArgs& a, cudaStream_t st) {
+  if (a.dim <= 64) return fwd_launch<64, 1, X>(a, st);
   const bool pair = a.group % 2 == 0;
   const int64_t blocks = most_tiles(a.tokens, a.n_seqs, pair ? TC_ROWS : 2 * TC_ROWS) * (pair ? a.heads / 2 : a.heads);
-  return blocks >= kSms ? fwd_launch<128, 2>(a, st) : fwd_launch<128, 1>(a, st);
+  return blocks >= kSms ? fwd_launch<128, 2, X>(a, st) : fwd_launch<128, 1, X>(a, st);
 }
+cudaError_t attn_packed_tc_forward(const PackedArgs& a, cudaStream_t st) { return a.cross ? tc_forward<true>(a, st) : tc_forward<false>(a, st); }
 
-template <int DT> static cudaError_t bwd_launch(const PackedArgs& a, cudaStream_t st) {
+template <int DT, bool X> static cudaError_t bwd_launch(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   using S = BwdShape<DT>;
   TcBwdMaps maps;
-  const int64_t tiles = most_tiles(a.tokens, a.n_seqs, TC_ROWS), blocks = tiles * (a.heads + a.kv_heads);
+  const int64_t dkv = most_tiles(a.kv_tokens, a.n_seqs, TC_ROWS) * a.kv_heads, blocks = most_tiles(a.tokens, a.n_seqs, TC_ROWS) * a.heads + dkv;
   if (!launchable(blocks)) return cudaErrorInvalidConfiguration;
-  cudaError_t e = allow_smem(attn_packed_bwd_tc_kernel<DT>, S::kSmem, done);
+  cudaError_t e = allow_smem(attn_packed_bwd_tc_kernel<DT, X>, S::kSmem, done);
   if (e == cudaSuccess) e = encode_heads(&maps.q, a.q, a.dim, a.heads, a.tokens, S::kCols);
-  if (e == cudaSuccess) e = encode_heads(&maps.k, a.k, a.dim, a.kv_heads, a.tokens, S::kCols);
-  if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.tokens, S::kCols);
+  if (e == cudaSuccess) e = encode_heads(&maps.k, a.k, a.dim, a.kv_heads, a.kv_tokens, S::kCols);
+  if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.kv_tokens, S::kCols);
   if (e == cudaSuccess) e = encode_heads(&maps.d_o, a.d_o, a.dim, a.heads, a.tokens, S::kCols);
   if (e != cudaSuccess) return e;
   e = launch_pdl(attn_packed_delta_tc_kernel, dim3((unsigned)((a.tokens + 32 * DELTA_R - 1) / (32 * DELTA_R)), a.heads), dim3(256), 0, st, false, a);
   // starts beside the first's last blocks; its own wait for them before they read delta
   if (e == cudaSuccess)
-    e = launch_clusters(attn_packed_bwd_tc_kernel<DT>, blocks, S::kThreads, S::kSmem, st, true,
-                        packed_parts(blocks, a, S::kCols, a.group, 4 * kSms, 4), a, maps, (int)(tiles * a.kv_heads));
+    e = launch_clusters(attn_packed_bwd_tc_kernel<DT, X>, blocks, S::kThreads, S::kSmem, st, true,
+                        packed_parts(blocks, a, S::kCols, a.group, 4 * kSms, 4), a, maps, (int)dkv);
   return e;
 }
-cudaError_t attn_packed_tc_backward(const PackedArgs& a, cudaStream_t st) { return a.dim <= 64 ? bwd_launch<64>(a, st) : bwd_launch<128>(a, st); }
+cudaError_t attn_packed_tc_backward(const PackedArgs& a, cudaStream_t st) {
+  if (a.cross) return a.dim <= 64 ? bwd_launch<64, true>(a, st) : bwd_launch<128, true>(a, st);
+  return a.dim <= 64 ? bwd_launch<64, false>(a, st) : bwd_launch<128, false>(a, st);
+}
 
 // Self-test of the bounded wait: one thread, no tensor memory, no copy in flight, a barrier on which nothing arrives.
 __global__ void attn_packed_wait_probe_kernel(long long limit_cycles) {

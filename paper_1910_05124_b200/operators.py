@@ -11,7 +11,8 @@ from bisect import bisect_left
 
 import torch
 
-from .binding import (PM_BF16, PM_F32, PipeMareError, _check, lib, pm_attention_desc, pm_head_view, pm_tensor_pair)
+from .binding import (PM_BF16, PM_F32, PipeMareError, _check, lib, pm_attention_desc, pm_cross_attention_desc, pm_head_view,
+                      pm_tensor_pair)
 
 _DTYPES = {torch.float32: PM_F32, torch.bfloat16: PM_BF16}
 _VIEW = C.sizeof(pm_head_view)
@@ -84,16 +85,10 @@ def _launch(call, device, stream, workspace=0):
     return _check(call(handle, scratch.data_ptr()))
 
 
-class PackedAttention:
-    """Attention over sequences of different lengths laid end to end, with shared key/value heads.
+class _HeadAttention:
+    """What the attention classes share: heads, scale, and views of [tokens, heads, head_dim] tensors."""
 
-    q, o: [tokens, n_heads, head_dim]; k, v: [tokens, n_kv_heads, head_dim]; all float32 or all bfloat16, the last dimension
-    contiguous, the others at any stride (q, k and v may be views of one projection's output).  cu_seqlens: int32
-    [sequences + 1] on the device, ascending; sequence b is tokens cu_seqlens[b] to cu_seqlens[b + 1] - 1, and tokens outside
-    all sequences are neither used nor written.  lse: float32 [n_heads, tokens].  head_dim up to 128.
-    """
-
-    def __init__(self, n_heads, n_kv_heads, head_dim, *, causal=True, scale=None):
+    def __init__(self, n_heads, n_kv_heads, head_dim, scale):
         if n_heads < 1 or n_kv_heads < 1 or n_heads % n_kv_heads:
             _refuse("n_heads must be a positive multiple of n_kv_heads")
         if head_dim < 1:
@@ -103,26 +98,28 @@ class PackedAttention:
         scale = head_dim ** -0.5 if scale is None else float(scale)
         if not 0 < scale < 2e38:
             _refuse("scale must be positive and below 2e38")
-        self.n_heads, self.n_kv_heads, self.head_dim, self.causal, self.scale = n_heads, n_kv_heads, head_dim, bool(causal), scale
+        self.n_heads, self.n_kv_heads, self.head_dim, self.scale = n_heads, n_kv_heads, head_dim, scale
         self.L = lib()
 
-    def _desc(self, q, cu_seqlens):
-        device = _compute_device("q", q)
-        if q.dim() != 3:
-            _refuse(f"q has shape {tuple(q.shape)}, expected [tokens, {self.n_heads}, {self.head_dim}]", "PM_ERR_SHAPE")
-        if not isinstance(cu_seqlens, torch.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.numel() < 1:
-            _refuse("cu_seqlens must be a one-dimensional tensor of sequences + 1 entries", "PM_ERR_SHAPE")
-        cu = _flat("cu_seqlens", cu_seqlens, torch.int32, device, cu_seqlens.shape)
-        tokens = q.shape[0]
-        return device, tokens, C.byref(pm_attention_desc(_DTYPES[q.dtype], self.n_heads, self.n_kv_heads, self.head_dim,
-                                                         cu_seqlens.numel() - 1, self.causal, tokens, self.scale)), cu
+    def _starts(self, name, cu, device):
+        """Pointer and number of sequences of an array of starts."""
+        if not isinstance(cu, torch.Tensor) or cu.dim() != 1 or cu.numel() < 1:
+            _refuse(f"{name} must be a one-dimensional tensor of sequences + 1 entries", "PM_ERR_SHAPE")
+        return _flat(name, cu, torch.int32, device, cu.shape), cu.numel() - 1
 
-    def _views(self, tokens, dtype, device, names, tensors, heads, n_read):
-        """One array of pm_head_view for tensors with `heads` heads each, checked; those behind the first n_read are written."""
-        d, index, flat = self.head_dim, device.index, []
-        for t, h in zip(tensors, heads):
-            if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == index and t.shape == (tokens, h, d)):
-                _mismatch(names[len(flat) // 3], t, dtype, device, (tokens, h, d))
+    def _rows(self, name, t, heads):
+        device = _compute_device(name, t)
+        if t.dim() != 3:
+            _refuse(f"{name} has shape {tuple(t.shape)}, expected [tokens, {heads}, {self.head_dim}]", "PM_ERR_SHAPE")
+        return device, t.shape[0]
+
+    def _views(self, shapes, dtype, device, names, tensors, n_read):
+        """One array of pm_head_view for tensors of these shapes, checked; those behind the first n_read are written."""
+        index, flat = device.index, []
+        for t, shape in zip(tensors, shapes):
+            if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == index and t.shape == shape):
+                _mismatch(names[len(flat) // 3], t, dtype, device, shape)
+            tokens, h, d = shape
             token, head, one = t.stride()
             if one != 1 and d > 1:
                 _refuse(f"the last dimension of {names[len(flat) // 3]} must be contiguous")
@@ -141,30 +138,6 @@ class PackedAttention:
                 _refuse(f"{name} overlaps itself")
             end += stride * (n - 1)
 
-    def pm_attention_packed_forward(self, q, k, v, cu_seqlens, o, lse=None, stream=None):
-        """Writes o and, for a backward pass, lse."""
-        device, tokens, desc, cu = self._desc(q, cu_seqlens)
-        H, K = self.n_heads, self.n_kv_heads
-        views = self._views(tokens, q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), (H, K, K, H), 3)
-        p_lse = _flat("lse", lse, torch.float32, device, (H, tokens))
-        at = C.addressof(views)
-        _launch(lambda st: self.L.pm_attention_packed_forward(desc, at, at + _VIEW, at + 2 * _VIEW, cu, at + 3 * _VIEW, p_lse, st), device, stream)
-
-    def pm_attention_packed_backward(self, q, k, v, o, lse, d_o, cu_seqlens, dq, dk, dv, stream=None):
-        """Writes dq, dk and dv from d_o and what the forward call wrote."""
-        device, tokens, desc, cu = self._desc(q, cu_seqlens)
-        if lse is None:
-            _refuse("lse must be a tensor")
-        H, K = self.n_heads, self.n_kv_heads
-        views = self._views(tokens, q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"), (q, k, v, o, d_o, dq, dk, dv),
-                            (H, K, K, H, H, H, K, K), 5)
-        p_lse = _flat("lse", lse, torch.float32, device, (H, tokens))
-        at = C.addressof(views)
-        need = self.L.pm_attention_packed_workspace_bytes(desc)
-        _launch(lambda st, ws=None: self.L.pm_attention_packed_backward(
-            desc, at, at + _VIEW, at + 2 * _VIEW, at + 3 * _VIEW, p_lse, at + 4 * _VIEW, cu, at + 5 * _VIEW, at + 6 * _VIEW, at + 7 * _VIEW, ws, need, st),
-            device, stream, need)
-
     def pm_attention_packed_status(self, device="cuda", stream=None):
         """Raises if a device-side wait of a tensor-core kernel ran out since the last call on this device (a defect); synchronises
         the stream."""
@@ -173,6 +146,95 @@ class PackedAttention:
     def pm_attention_packed_selftest_wait_timeout(self, limit_cycles, device="cuda", stream=None):
         """Enqueues a wait that runs out after limit_cycles: the next pm_attention_packed_status on this device raises."""
         _launch(lambda st: self.L.pm_attention_packed_selftest_wait_timeout(int(limit_cycles), st), _indexed(device), stream)
+
+
+class PackedAttention(_HeadAttention):
+    """Attention over sequences of different lengths laid end to end, with shared key/value heads.
+
+    q, o: [tokens, n_heads, head_dim]; k, v: [tokens, n_kv_heads, head_dim]; all float32 or all bfloat16, the last dimension
+    contiguous, the others at any stride (q, k and v may be views of one projection's output).  cu_seqlens: int32
+    [sequences + 1] on the device, ascending; sequence b is tokens cu_seqlens[b] to cu_seqlens[b + 1] - 1, and tokens outside
+    all sequences are neither used nor written.  lse: float32 [n_heads, tokens].  head_dim up to 128.
+    """
+
+    def __init__(self, n_heads, n_kv_heads, head_dim, *, causal=True, scale=None):
+        super().__init__(n_heads, n_kv_heads, head_dim, scale)
+        self.causal = bool(causal)
+
+    def _desc(self, q, cu_seqlens):
+        device, tokens = self._rows("q", q, self.n_heads)
+        cu, n_seqs = self._starts("cu_seqlens", cu_seqlens, device)
+        return device, tokens, C.byref(pm_attention_desc(_DTYPES[q.dtype], self.n_heads, self.n_kv_heads, self.head_dim, n_seqs, self.causal, tokens,
+                                                         self.scale)), cu
+
+    def pm_attention_packed_forward(self, q, k, v, cu_seqlens, o, lse=None, stream=None):
+        """Writes o and, for a backward pass, lse."""
+        device, tokens, desc, cu = self._desc(q, cu_seqlens)
+        Q, K = (tokens, self.n_heads, self.head_dim), (tokens, self.n_kv_heads, self.head_dim)
+        views = self._views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
+        p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, tokens))
+        at = C.addressof(views)
+        _launch(lambda st: self.L.pm_attention_packed_forward(desc, at, at + _VIEW, at + 2 * _VIEW, cu, at + 3 * _VIEW, p_lse, st), device, stream)
+
+    def pm_attention_packed_backward(self, q, k, v, o, lse, d_o, cu_seqlens, dq, dk, dv, stream=None):
+        """Writes dq, dk and dv from d_o and what the forward call wrote."""
+        device, tokens, desc, cu = self._desc(q, cu_seqlens)
+        if lse is None:
+            _refuse("lse must be a tensor")
+        Q, K = (tokens, self.n_heads, self.head_dim), (tokens, self.n_kv_heads, self.head_dim)
+        views = self._views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
+                            (q, k, v, o, d_o, dq, dk, dv), 5)
+        p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, tokens))
+        at = C.addressof(views)
+        need = self.L.pm_attention_packed_workspace_bytes(desc)
+        _launch(lambda st, ws=None: self.L.pm_attention_packed_backward(
+            desc, at, at + _VIEW, at + 2 * _VIEW, at + 3 * _VIEW, p_lse, at + 4 * _VIEW, cu, at + 5 * _VIEW, at + 6 * _VIEW, at + 7 * _VIEW, ws, need, st),
+            device, stream, need)
+
+
+class CrossAttention(_HeadAttention):
+    """Attention of packed sequences over the sequences of another tensor, such as a decoder's tokens over an encoder's states.
+
+    q, o: [tokens, n_heads, head_dim] with cu_seqlens; k, v: [kv_tokens, n_kv_heads, head_dim] with cu_seqlens_kv; the rest as in
+    PackedAttention, without a causal mask.  Sequence b of q attends to every row of sequence b of k and v; without keys its o is
+    zero and its lse -infinity.  A decoding step is a call with one token, or the few of a beam, to each sequence.
+    """
+
+    def __init__(self, n_heads, n_kv_heads, head_dim, *, scale=None):
+        super().__init__(n_heads, n_kv_heads, head_dim, scale)
+
+    def _desc(self, q, k, cu_seqlens, cu_seqlens_kv):
+        device, tokens = self._rows("q", q, self.n_heads)
+        _, kv_tokens = self._rows("k", k, self.n_kv_heads)
+        cu, n_seqs = self._starts("cu_seqlens", cu_seqlens, device)
+        cu_kv, n_kv_seqs = self._starts("cu_seqlens_kv", cu_seqlens_kv, device)
+        if n_seqs != n_kv_seqs:
+            _refuse(f"cu_seqlens has {n_seqs} sequences, cu_seqlens_kv {n_kv_seqs}", "PM_ERR_SHAPE")
+        Q, K = (tokens, self.n_heads, self.head_dim), (kv_tokens, self.n_kv_heads, self.head_dim)
+        return device, Q, K, C.byref(pm_cross_attention_desc(_DTYPES[q.dtype], self.n_heads, self.n_kv_heads, self.head_dim, n_seqs, tokens, kv_tokens,
+                                                             self.scale)), cu, cu_kv
+
+    def pm_attention_cross_forward(self, q, k, v, cu_seqlens, cu_seqlens_kv, o, lse=None, stream=None):
+        """Writes o and, for a backward pass, lse."""
+        device, Q, K, desc, cu, cu_kv = self._desc(q, k, cu_seqlens, cu_seqlens_kv)
+        views = self._views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
+        p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, Q[0]))
+        at = C.addressof(views)
+        _launch(lambda st: self.L.pm_attention_cross_forward(desc, at, at + _VIEW, at + 2 * _VIEW, cu, cu_kv, at + 3 * _VIEW, p_lse, st), device, stream)
+
+    def pm_attention_cross_backward(self, q, k, v, o, lse, d_o, cu_seqlens, cu_seqlens_kv, dq, dk, dv, stream=None):
+        """Writes dq, dk and dv from d_o and what the forward call wrote."""
+        device, Q, K, desc, cu, cu_kv = self._desc(q, k, cu_seqlens, cu_seqlens_kv)
+        if lse is None:
+            _refuse("lse must be a tensor")
+        views = self._views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
+                            (q, k, v, o, d_o, dq, dk, dv), 5)
+        p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, Q[0]))
+        at = C.addressof(views)
+        need = self.L.pm_attention_cross_workspace_bytes(desc)
+        _launch(lambda st, ws=None: self.L.pm_attention_cross_backward(
+            desc, at, at + _VIEW, at + 2 * _VIEW, at + 3 * _VIEW, p_lse, at + 4 * _VIEW, cu, cu_kv, at + 5 * _VIEW, at + 6 * _VIEW, at + 7 * _VIEW, ws, need, st),
+            device, stream, need)
 
 
 class TokenLogProbs:
