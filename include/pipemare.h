@@ -476,6 +476,54 @@ pm_status pm_attention_cross_backward(const pm_cross_attention_desc* desc, const
 pm_status pm_attention_packed_status(void* stream);
 pm_status pm_attention_packed_selftest_wait_timeout(int64_t limit_cycles, void* stream);
 
+/* Norms of queries and keys for each head, and the rotation by their positions, in one pass: what attention reads from what the
+ * projection wrote.  For every row x of head_dim values, with the gains g [head_dim] of queries or of keys:
+ *   n_i = g_i x_i (mean_j x_j^2 + eps)^(-1/2);   y = n, but for the first rotary_dim dimensions, whose pairs (a, b) turn by the
+ *   angle phi_i = position f_i:   y_a = n_a cos - n_b sin,  y_b = n_b cos + n_a sin
+ * Pair i is (i, i + rotary_dim / 2), with `interleaved` (2 i, 2 i + 1).  turns: host array of rotary_dim / 2 frequencies in units
+ * of 2^-64 turns per position, read during the call, as pm_rotation_turns fills it for f_i = base^(-2 i / rotary_dim) (base at
+ * least 1); angles are exact to 2^-33 turns at every position, negative ones among them.  positions: int32 [n_tokens] on the
+ * device, not looked at with rotary_dim 0.  Gains are floats whatever dtype is.  Squares are summed in fp32: a row whose mean square
+ * leaves its range (values beyond 1e18) gives zeros; eps may be 0, a row of zeros is then NaN.  A value that is not finite reaches
+ * the results of its row (and, in the backward pass, the gains' gradients) alone.
+ * n_heads or n_kv_heads may be 0, the arguments of that side then count for nothing (queries of cross attention, whose keys
+ * were normed when the encoder ran). */
+typedef struct {
+  int32_t dtype;                 /* PM_F32 | PM_BF16, of every tensor with heads */
+  int32_t n_heads, n_kv_heads;   /* of q and of k */
+  int32_t head_dim;              /* 1 to 128 */
+  int32_t rotary_dim;            /* even, 0 to head_dim */
+  int32_t interleaved;
+  int64_t n_tokens;
+  float eps;
+  const uint64_t* turns;         /* host, rotary_dim / 2 entries */
+} pm_head_norm_desc;
+pm_status pm_rotation_turns(int32_t rotary_dim, double base, uint64_t* turns);
+/* q_out and k_out may be q and k themselves (same strides); any other overlap with an input, or of each other, is refused. */
+pm_status pm_head_norm_rotate(const pm_head_norm_desc* desc, const pm_head_view* q, const pm_head_view* k, const int32_t* positions,
+                              const float* q_gain, const float* k_gain, const pm_head_view* q_out, const pm_head_view* k_out,
+                              void* stream);
+/* Gradients of q, k and (unless NULL) of the gains, summed over tokens and heads in a fixed order, from those of q_out and k_out.
+ * dq and dk may be d_q_out and d_k_out themselves (same strides).  workspace: needed with a gain's gradient, at least
+ * pm_head_norm_rotate_workspace_bytes(desc) bytes of device memory, 4-byte aligned. */
+uint64_t pm_head_norm_rotate_workspace_bytes(const pm_head_norm_desc* desc);
+pm_status pm_head_norm_rotate_backward(const pm_head_norm_desc* desc, const pm_head_view* q, const pm_head_view* k,
+                                       const int32_t* positions, const float* q_gain, const float* k_gain,
+                                       const pm_head_view* d_q_out, const pm_head_view* d_k_out, const pm_head_view* dq,
+                                       const pm_head_view* dk, float* d_q_gain, float* d_k_gain, void* workspace,
+                                       uint64_t workspace_bytes, void* stream);
+
+/* Dropout of n elements with a mask that is never stored, added to a residual stream (NULL: not added):
+ *   y_i = residual_i + (kept_i ? x_i 2^16 / (2^16 - T) : 0),   kept_i = bits_i >= T,   T = p 2^16 to the nearest whole number
+ * so p is taken to the nearest 2^-16 (0 to below 1 - 2^-17) and the scale is that of the p taken.  bits_i: 16 bits of
+ * Philox4x32-10 with the key rng[0] (its lower 32 bits first) and the 128-bit counter rng[1] + i / 8: of its four words, word
+ * (i mod 8) / 2, the lower half for even i.  rng: two int64 on the device, read when the call runs, so a captured graph draws
+ * anew when the program moves rng[1] on by (n + 7) / 8 or more between replays; the backward call takes the rng of its forward
+ * call.  What is dropped may be NaN or infinite.  One rounding, of the result.  y may be x or the residual itself; any other
+ * overlap is refused.  The backward pass of the residual is the identity. */
+pm_status pm_dropout(const void* x, const void* residual, int32_t dtype, int64_t n, double p, const int64_t* rng, void* y, void* stream);
+pm_status pm_dropout_backward(const void* d_y, int32_t dtype, int64_t n, double p, const int64_t* rng, void* d_x, void* stream);
+
 /* Per row of logits [rows, vocab] (row_stride elements apart, dtype PM_F32 | PM_BF16):
  *   lse = log sum_j exp(x_j);  logprob = x_y - lse for the target y;  entropy = lse - sum_j p_j x_j;  the top_k largest
  *   logits' ids, in descending order (equal logits: the lower id first), and their log probabilities.
@@ -497,6 +545,30 @@ pm_status pm_token_logprobs_backward(const void* logits, int32_t dtype, int64_t 
                                      const int32_t* targets, const float* lse, const float* entropy,
                                      const float* d_logprob, const float* d_entropy, void* d_logits, int64_t grad_stride,
                                      void* stream);
+
+/* The clipped policy loss of n sampled tokens with a KL term and an entropy bonus, and its gradients, from the log probabilities
+ * and entropies of pm_token_logprobs:
+ *   ratio = exp(logprob - old_logprob);   policy = -min(ratio A, clip(ratio, 1 - clip_low, 1 + clip_high) A), A the advantage
+ *   kl = exp(d) - d - 1 with d = ref_logprob - logprob
+ *   loss = sum_i share_i (policy_i + kl_coef kl_i - entropy_coef entropy_i)
+ * share is the token's weight (NULL: 1), with `mean` divided by the sum of the weights; weights are not negative, and if all are
+ * zero so is everything.  A token of weight 0 is padding: its values may be NaN or infinite.  An advantage of 0 has no policy
+ * term whatever the ratio is; other values that are not finite give what the formulas give.
+ * stats: five floats on the device, the loss and the weighted sums of policy, kl, entropy and [clipped].  ref_logprob and entropy
+ * may be NULL if their coefficients are 0 (their sums are then 0).  d_logprob, d_entropy: gradients of the loss, or NULL; they go
+ * to pm_token_logprobs_backward.  At a border the ratio is not clipped; which side a token is on is decided in 64 bits.  Outputs
+ * overlap neither each other nor an input (refused).  workspace: at least pm_policy_loss_workspace_bytes(n) bytes of device
+ * memory (0 for short lists), 8-byte aligned. */
+typedef struct {
+  double clip_low, clip_high;    /* 0 to 1; not negative, infinity for none */
+  double kl_coef, entropy_coef;
+  int32_t mean;
+} pm_policy_desc;
+uint64_t pm_policy_loss_workspace_bytes(int64_t n);
+pm_status pm_policy_loss(const pm_policy_desc* desc, int64_t n, const float* logprob, const float* old_logprob,
+                         const float* advantage, const float* ref_logprob, const float* entropy, const float* weight,
+                         float* stats, float* d_logprob, float* d_entropy, void* workspace, uint64_t workspace_bytes,
+                         void* stream);
 
 /* Clipping by the global norm over many tensors:
  *   norm = sqrt(sum of the squares of every src element),  scale = min(1, max_norm / norm),  dst = scale * src

@@ -13,7 +13,7 @@ from .binding import (  # noqa: F401
 
 def __getattr__(name):
     """The operators work on torch tensors; torch is imported with the first of them."""
-    if name in ("CrossAttention", "GradClip", "PackedAttention", "TokenLogProbs"):
+    if name in ("CrossAttention", "Dropout", "GradClip", "HeadNormRotate", "PackedAttention", "PolicyLoss", "TokenLogProbs"):
         from . import operators
         return getattr(operators, name)
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

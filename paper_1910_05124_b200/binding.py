@@ -65,6 +65,15 @@ class pm_cross_attention_desc(C.Structure):
                 ("n_tokens", C.c_int64), ("n_kv_tokens", C.c_int64), ("scale", C.c_float)]
 
 
+class pm_head_norm_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("rotary_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("n_tokens", C.c_int64), ("eps", C.c_float), ("turns", C.POINTER(C.c_uint64))]
+
+
+class pm_policy_desc(C.Structure):
+    _fields_ = [("clip_low", C.c_double), ("clip_high", C.c_double), ("kl_coef", C.c_double), ("entropy_coef", C.c_double), ("mean", C.c_int32)]
+
+
 class pm_tensor_pair(C.Structure):
     _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("count", C.c_uint64), ("src_dtype", C.c_int32), ("dst_dtype", C.c_int32)]
 
@@ -133,6 +142,17 @@ def lib():
     L.pm_attention_cross_backward.argtypes = [cross, view, view, view, view, vp, view, vp, vp, view, view, view, vp, u64, vp]
     L.pm_attention_packed_status.argtypes = [vp]
     L.pm_attention_packed_selftest_wait_timeout.argtypes = [i64, vp]
+    norm, f64 = C.POINTER(pm_head_norm_desc), C.c_double
+    L.pm_rotation_turns.argtypes = [i32, f64, u64p]
+    L.pm_head_norm_rotate.argtypes = [norm, view, view, vp, vp, vp, view, view, vp]
+    L.pm_head_norm_rotate_workspace_bytes.argtypes = [norm]
+    L.pm_head_norm_rotate_workspace_bytes.restype = u64
+    L.pm_head_norm_rotate_backward.argtypes = [norm, view, view, vp, vp, vp, view, view, view, view, vp, vp, vp, u64, vp]
+    L.pm_dropout.argtypes = [vp, vp, i32, i64, f64, vp, vp, vp]
+    L.pm_dropout_backward.argtypes = [vp, i32, i64, f64, vp, vp, vp]
+    L.pm_policy_loss_workspace_bytes.argtypes = [i64]
+    L.pm_policy_loss_workspace_bytes.restype = u64
+    L.pm_policy_loss.argtypes = [C.POINTER(pm_policy_desc), i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, u64, vp]
     L.pm_token_logprobs.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp, vp, i32, vp, vp, vp]
     L.pm_token_logprobs_backward.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp, vp, vp, vp, i64, vp]
     L.pm_clip_gradients_workspace_bytes.argtypes = [i32]

@@ -1,0 +1,115 @@
+// Dropout whose mask is formed from a counter-based generator wherever it is needed, with the sum into a residual stream.
+//
+//   bits_i = 16 bits of Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011) with the key
+//            `seed` and the counter `first + i / 8`: eight elements to a counter, the lower half of a word before its upper half
+//   kept_i = bits_i >= T,  T = p 2^16 to the nearest whole number;   y_i = residual_i + (kept_i ? x_i 2^16 / (2^16 - T) : 0)
+//
+// Bound by memory: x (and the residual) read, y written, nothing stored for the backward pass, which is the same call on the gradient.
+// 16 bits to an element, so a counter's ten rounds serve a whole 16-byte vector of bf16: 32 bits to an element would take twice the
+// multiplications, which are then as long as the memory takes.
+#include "pm_ops.cuh"
+
+namespace pm {
+
+constexpr int kDropThreads = 256, kDropVectors = 2;                  // vectors of eight elements to a thread
+
+__device__ __forceinline__ uint4 philox(uint4 c, uint2 key) {
+#pragma unroll
+  for (int i = 0; i < 10; ++i) {
+    const uint64_t a = (uint64_t)0xD2511F53u * c.x, b = (uint64_t)0xCD9E8D57u * c.z;
+    c = make_uint4((uint32_t)(b >> 32) ^ c.y ^ key.x, (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ key.y, (uint32_t)a);
+    key.x += 0x9E3779B9u;
+    key.y += 0xBB67AE85u;
+  }
+  return c;
+}
+
+// VEC: every tensor starts at a 16-byte boundary.  x and y may be one tensor, so nothing is declared read-only.
+template <typename T, bool VEC, bool RES>
+__global__ void __launch_bounds__(kDropThreads) dropout_kernel(const T* x, const T* residual, T* y, int64_t n, const uint64_t* rng, uint32_t dropped, float scale) {
+  constexpr int U = kDropVectors;
+  const int64_t first = (int64_t)blockIdx.x * kDropThreads * U + threadIdx.x;
+  float v[U][8], r[U][8];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t at = (first + u * kDropThreads) * 8;
+    if (VEC && at + 8 <= n) {
+      load8<T>(x + at, v[u]);
+      if (RES) load8<T>(residual + at, r[u]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[u][e] = at + e < n ? to_f<T>(x[at + e]) : 0.f;
+        if (RES) r[u][e] = at + e < n ? to_f<T>(residual[at + e]) : 0.f;
+      }
+    }
+  }
+  const uint64_t key = rng[0], counter = rng[1];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t vector = first + u * kDropThreads, at = vector * 8;
+    if (at >= n) break;
+    const uint64_t c = counter + (uint64_t)vector;
+    const uint4 w = philox(make_uint4((uint32_t)c, (uint32_t)(c >> 32), 0u, 0u), make_uint2((uint32_t)key, (uint32_t)(key >> 32)));
+    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+    float out[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t bits = e & 1 ? words[e / 2] >> 16 : words[e / 2] & 0xFFFFu;
+      const float kept = bits >= dropped ? v[u][e] * scale : 0.f;    // chosen, not multiplied: what is dropped may be anything
+      out[e] = RES ? r[u][e] + kept : kept;
+    }
+    if (VEC && at + 8 <= n) {
+      store8<T>(y + at, out);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (at + e < n) y[at + e] = from_f<T>(out[e]);
+    }
+  }
+}
+
+template <typename T> static cudaError_t dropout_run(const void* x, const void* residual, void* y, int64_t n, const int64_t* rng, uint32_t dropped, cudaStream_t st) {
+  const bool vec = aligned_to(x, 16) && aligned_to(residual, 16) && aligned_to(y, 16);
+  const int64_t blocks = (n + 8 * kDropThreads * kDropVectors - 1) / (8 * kDropThreads * kDropVectors);
+  const float scale = 65536.f / (float)(65536u - dropped);
+  auto go = [&](auto kernel) {
+    return launch_pdl(kernel, dim3((unsigned)blocks), dim3(kDropThreads), 0, st, false, static_cast<const T*>(x), static_cast<const T*>(residual), static_cast<T*>(y), n,
+                      reinterpret_cast<const uint64_t*>(rng), dropped, scale);
+  };
+  if (residual) return vec ? go(dropout_kernel<T, true, true>) : go(dropout_kernel<T, false, true>);
+  return vec ? go(dropout_kernel<T, true, false>) : go(dropout_kernel<T, false, false>);
+}
+
+static pm_status dropout_call(const void* x, const void* residual, int32_t dtype, int64_t n, double p, const int64_t* rng, void* y, const char* what, void* stream) {
+  if (dtype != PM_F32 && dtype != PM_BF16) return ops_fail(PM_ERR_INVALID_ARG, "unknown element type");
+  if (n < 0) return ops_fail(PM_ERR_INVALID_ARG, "negative size");
+  if (n > (int64_t)1 << 42) return ops_fail(PM_ERR_SHAPE, "too many elements");
+  if (!(p >= 0.0) || p >= 1.0 - 1.0 / 131072) return ops_fail(PM_ERR_INVALID_ARG, "p must be 0 to below 1 - 2^-17");
+  if (n == 0) return PM_OK;
+  const int size = dtype == PM_BF16 ? 2 : 4;
+  if (!x || !y || !rng) return ops_fail(PM_ERR_INVALID_ARG, "null pointer");
+  if (!aligned_to(x, size) || !aligned_to(residual, size) || !aligned_to(y, size)) return ops_fail(PM_ERR_INVALID_ARG, "pointer not aligned to its element type");
+  if (!aligned_to(rng, 8)) return ops_fail(PM_ERR_INVALID_ARG, "rng must be 8-byte aligned");
+  auto apart = [&](const void* in, int64_t bytes) { return in == y && bytes == n * size ? true : !extents_share(dense_extent(y, n * size), dense_extent(in, bytes)); };
+  if (!apart(x, n * size) || !apart(residual, n * size) || extents_share(dense_extent(y, n * size), dense_extent(rng, 16)))
+    return ops_fail(PM_ERR_INVALID_ARG, "the output overlaps an input without being the same tensor");
+  const uint32_t dropped = (uint32_t)(p * 65536.0 + 0.5);
+  const cudaStream_t st = (cudaStream_t)stream;
+  return ops_cuda(dtype == PM_BF16 ? dropout_run<__nv_bfloat16>(x, residual, y, n, rng, dropped, st) : dropout_run<float>(x, residual, y, n, rng, dropped, st), what);
+}
+
+}  // namespace pm
+
+using namespace pm;
+
+extern "C" {
+
+pm_status pm_dropout(const void* x, const void* residual, int32_t dtype, int64_t n, double p, const int64_t* rng, void* y, void* stream) {
+  return dropout_call(x, residual, dtype, n, p, rng, y, "dropout", stream);
+}
+
+pm_status pm_dropout_backward(const void* d_y, int32_t dtype, int64_t n, double p, const int64_t* rng, void* d_x, void* stream) {
+  return dropout_call(d_y, nullptr, dtype, n, p, rng, d_x, "dropout backward", stream);
+}
+
+}  // extern "C"

@@ -1,18 +1,20 @@
-"""Operators for programs with their own forward and backward pass, next to `FlatUpdate`: attention over packed sequences,
-log probabilities of given tokens, and gradient clipping.  Argument checks and marshalling only; the tensors belong to the
-caller, outputs included.
+"""Operators for programs with their own forward and backward pass, next to `FlatUpdate`: attention over packed sequences and over
+those of another tensor, norms and rotation of queries and keys, dropout into a residual stream, log probabilities of given tokens,
+the policy loss of sampled ones, and gradient clipping.  Argument checks and marshalling only; the tensors belong to the caller,
+outputs included.
 
 Every call is asynchronous on `stream` (default: the current stream of the tensors' device) and may be captured into a CUDA
 graph.  As with any CUDA call, a tensor that another stream still writes has to be waited for by the caller, and a tensor
 that belongs to another stream has to be kept until the call has run.  Refused arguments raise PipeMareError.
 """
 import ctypes as C
+import math
 from bisect import bisect_left
 
 import torch
 
-from .binding import (PM_BF16, PM_F32, PipeMareError, _check, lib, pm_attention_desc, pm_cross_attention_desc, pm_head_view,
-                      pm_tensor_pair)
+from .binding import (PM_BF16, PM_F32, PipeMareError, _check, lib, pm_attention_desc, pm_cross_attention_desc, pm_head_norm_desc,
+                      pm_head_view, pm_policy_desc, pm_tensor_pair)
 
 _DTYPES = {torch.float32: PM_F32, torch.bfloat16: PM_BF16}
 _VIEW = C.sizeof(pm_head_view)
@@ -85,8 +87,47 @@ def _launch(call, device, stream, workspace=0):
     return _check(call(handle, scratch.data_ptr()))
 
 
+def _head_views(shapes, dtype, device, names, tensors, n_read):
+    """One array of pm_head_view for tensors of these shapes ([tokens, heads, head_dim]), checked; those behind the first n_read are
+    written.  None gives a null view."""
+    index, flat = device.index, []
+    for t, shape in zip(tensors, shapes):
+        if shape is None:
+            flat += (0, 0, 0)
+            continue
+        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == index and t.shape == shape):
+            _mismatch(names[len(flat) // 3], t, dtype, device, shape)
+        tokens, h, d = shape
+        token, head, one = t.stride()
+        if one != 1 and d > 1:
+            _refuse(f"the last dimension of {names[len(flat) // 3]} must be contiguous")
+        if (head != d or token < h * d) and len(flat) >= 3 * n_read:
+            _check_apart(names[len(flat) // 3], d, ((token, tokens), (head, h)))
+        flat += (t.data_ptr(), token, head)
+    return (C.c_int64 * len(flat))(*flat)
+
+
+def _check_apart(name, head_dim, dims):
+    """Rows of one head, or heads of one row, of a tensor that is written must not share elements."""
+    if min(n for _, n in dims) < 1:
+        return
+    end = head_dim
+    for stride, n in sorted((s, n) for s, n in dims if n > 1):
+        if stride < end:
+            _refuse(f"{name} overlaps itself")
+        end += stride * (n - 1)
+
+
+def _head_rows(name, t, heads, head_dim):
+    """Device and number of tokens of a [tokens, heads, head_dim] tensor."""
+    device = _compute_device(name, t)
+    if t.dim() != 3:
+        _refuse(f"{name} has shape {tuple(t.shape)}, expected [tokens, {heads}, {head_dim}]", "PM_ERR_SHAPE")
+    return device, t.shape[0]
+
+
 class _HeadAttention:
-    """What the attention classes share: heads, scale, and views of [tokens, heads, head_dim] tensors."""
+    """What the attention classes share."""
 
     def __init__(self, n_heads, n_kv_heads, head_dim, scale):
         if n_heads < 1 or n_kv_heads < 1 or n_heads % n_kv_heads:
@@ -107,36 +148,8 @@ class _HeadAttention:
             _refuse(f"{name} must be a one-dimensional tensor of sequences + 1 entries", "PM_ERR_SHAPE")
         return _flat(name, cu, torch.int32, device, cu.shape), cu.numel() - 1
 
-    def _rows(self, name, t, heads):
-        device = _compute_device(name, t)
-        if t.dim() != 3:
-            _refuse(f"{name} has shape {tuple(t.shape)}, expected [tokens, {heads}, {self.head_dim}]", "PM_ERR_SHAPE")
-        return device, t.shape[0]
-
-    def _views(self, shapes, dtype, device, names, tensors, n_read):
-        """One array of pm_head_view for tensors of these shapes, checked; those behind the first n_read are written."""
-        index, flat = device.index, []
-        for t, shape in zip(tensors, shapes):
-            if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == index and t.shape == shape):
-                _mismatch(names[len(flat) // 3], t, dtype, device, shape)
-            tokens, h, d = shape
-            token, head, one = t.stride()
-            if one != 1 and d > 1:
-                _refuse(f"the last dimension of {names[len(flat) // 3]} must be contiguous")
-            if (head != d or token < h * d) and len(flat) >= 3 * n_read:
-                self._check_apart(names[len(flat) // 3], ((token, tokens), (head, h)))
-            flat += (t.data_ptr(), token, head)
-        return (C.c_int64 * len(flat))(*flat)
-
     def _check_apart(self, name, dims):
-        """Rows of one head, or heads of one row, of a tensor that is written must not share elements."""
-        if min(n for _, n in dims) < 1:
-            return
-        end = self.head_dim
-        for stride, n in sorted((s, n) for s, n in dims if n > 1):
-            if stride < end:
-                _refuse(f"{name} overlaps itself")
-            end += stride * (n - 1)
+        _check_apart(name, self.head_dim, dims)
 
     def pm_attention_packed_status(self, device="cuda", stream=None):
         """Raises if a device-side wait of a tensor-core kernel ran out since the last call on this device (a defect); synchronises
@@ -162,7 +175,7 @@ class PackedAttention(_HeadAttention):
         self.causal = bool(causal)
 
     def _desc(self, q, cu_seqlens):
-        device, tokens = self._rows("q", q, self.n_heads)
+        device, tokens = _head_rows("q", q, self.n_heads, self.head_dim)
         cu, n_seqs = self._starts("cu_seqlens", cu_seqlens, device)
         return device, tokens, C.byref(pm_attention_desc(_DTYPES[q.dtype], self.n_heads, self.n_kv_heads, self.head_dim, n_seqs, self.causal, tokens,
                                                          self.scale)), cu
@@ -171,7 +184,7 @@ class PackedAttention(_HeadAttention):
         """Writes o and, for a backward pass, lse."""
         device, tokens, desc, cu = self._desc(q, cu_seqlens)
         Q, K = (tokens, self.n_heads, self.head_dim), (tokens, self.n_kv_heads, self.head_dim)
-        views = self._views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
+        views = _head_views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
         p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, tokens))
         at = C.addressof(views)
         _launch(lambda st: self.L.pm_attention_packed_forward(desc, at, at + _VIEW, at + 2 * _VIEW, cu, at + 3 * _VIEW, p_lse, st), device, stream)
@@ -182,7 +195,7 @@ class PackedAttention(_HeadAttention):
         if lse is None:
             _refuse("lse must be a tensor")
         Q, K = (tokens, self.n_heads, self.head_dim), (tokens, self.n_kv_heads, self.head_dim)
-        views = self._views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
+        views = _head_views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
                             (q, k, v, o, d_o, dq, dk, dv), 5)
         p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, tokens))
         at = C.addressof(views)
@@ -204,8 +217,8 @@ class CrossAttention(_HeadAttention):
         super().__init__(n_heads, n_kv_heads, head_dim, scale)
 
     def _desc(self, q, k, cu_seqlens, cu_seqlens_kv):
-        device, tokens = self._rows("q", q, self.n_heads)
-        _, kv_tokens = self._rows("k", k, self.n_kv_heads)
+        device, tokens = _head_rows("q", q, self.n_heads, self.head_dim)
+        _, kv_tokens = _head_rows("k", k, self.n_kv_heads, self.head_dim)
         cu, n_seqs = self._starts("cu_seqlens", cu_seqlens, device)
         cu_kv, n_kv_seqs = self._starts("cu_seqlens_kv", cu_seqlens_kv, device)
         if n_seqs != n_kv_seqs:
@@ -217,7 +230,7 @@ class CrossAttention(_HeadAttention):
     def pm_attention_cross_forward(self, q, k, v, cu_seqlens, cu_seqlens_kv, o, lse=None, stream=None):
         """Writes o and, for a backward pass, lse."""
         device, Q, K, desc, cu, cu_kv = self._desc(q, k, cu_seqlens, cu_seqlens_kv)
-        views = self._views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
+        views = _head_views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
         p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, Q[0]))
         at = C.addressof(views)
         _launch(lambda st: self.L.pm_attention_cross_forward(desc, at, at + _VIEW, at + 2 * _VIEW, cu, cu_kv, at + 3 * _VIEW, p_lse, st), device, stream)
@@ -227,7 +240,7 @@ class CrossAttention(_HeadAttention):
         device, Q, K, desc, cu, cu_kv = self._desc(q, k, cu_seqlens, cu_seqlens_kv)
         if lse is None:
             _refuse("lse must be a tensor")
-        views = self._views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
+        views = _head_views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
                             (q, k, v, o, d_o, dq, dk, dv), 5)
         p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, Q[0]))
         at = C.addressof(views)
@@ -235,6 +248,123 @@ class CrossAttention(_HeadAttention):
         _launch(lambda st, ws=None: self.L.pm_attention_cross_backward(
             desc, at, at + _VIEW, at + 2 * _VIEW, at + 3 * _VIEW, p_lse, at + 4 * _VIEW, cu, cu_kv, at + 5 * _VIEW, at + 6 * _VIEW, at + 7 * _VIEW, ws, need, st),
             device, stream, need)
+
+
+class HeadNormRotate:
+    """Root-mean-square norms of queries and keys for each head, with a gain, and the rotation of their first rotary_dim dimensions (None:
+    all, 0: none) by the positions, in one pass.
+
+    q, q_out: [tokens, n_heads, head_dim]; k, k_out: [tokens, n_kv_heads, head_dim]; all float32 or all bfloat16, at any strides with the
+    last dimension contiguous; either side may be None with its gain and output.  positions: int32 [tokens] on the device (None
+    without rotation).  gains: float32 [head_dim].  Pairs are (i, i + rotary_dim / 2) or, interleaved, (2 i, 2 i + 1); pair i turns by
+    base^(-2 i / rotary_dim) a position, exactly at every position.
+    """
+
+    def __init__(self, head_dim, *, rotary_dim=None, base=10000.0, interleaved=False, eps=1e-6):
+        rotary_dim = head_dim if rotary_dim is None else rotary_dim
+        if head_dim < 1:
+            _refuse("head_dim must be positive")
+        if head_dim > 128:
+            _refuse("heads wider than 128", "PM_ERR_UNSUPPORTED")
+        if not 0 <= rotary_dim <= head_dim or rotary_dim % 2:
+            _refuse("rotary_dim must be even and at most head_dim")
+        if not 0 <= float(eps) <= 1e30:
+            _refuse("eps must not be negative")
+        self.head_dim, self.rotary_dim, self.base, self.interleaved, self.eps = head_dim, rotary_dim, float(base), bool(interleaved), float(eps)
+        self.L = lib()
+        self.turns = (C.c_uint64 * max(1, rotary_dim // 2))()
+        _check(self.L.pm_rotation_turns(rotary_dim, self.base, self.turns))
+
+    def _sides(self, q, k, positions, q_gain, k_gain):
+        """Device, dtype, shapes of both sides (None: absent), description, and pointers of positions and gains."""
+        d = self.head_dim
+        if q is None and k is None:
+            _refuse("neither queries nor keys")
+        lead, name = (q, "q") if q is not None else (k, "k")
+        device, tokens = _head_rows(name, lead, "heads", d)
+        shapes = []
+        for name, t in (("q", q), ("k", k)):
+            if t is None:
+                shapes.append(None)
+                continue
+            if not isinstance(t, torch.Tensor) or t.dim() != 3:
+                _refuse(f"{name} must be a tensor of [tokens, heads, {d}]", "PM_ERR_SHAPE")
+            if t.shape[1] < 1:
+                _refuse(f"{name} has no heads", "PM_ERR_SHAPE")
+            shapes.append((tokens, t.shape[1], d))
+        Q, K = shapes
+        if self.rotary_dim and positions is None:
+            _refuse("positions must be a tensor")
+        at = _flat("positions", positions, torch.int32, device, (tokens,)) if self.rotary_dim else None
+        gains = []
+        for name, shape, g in (("q_gain", Q, q_gain), ("k_gain", K, k_gain)):
+            if shape is not None and g is None:
+                _refuse(f"{name} must be a tensor")
+            gains.append(None if shape is None else _flat(name, g, torch.float32, device, (d,)))
+        desc = C.byref(pm_head_norm_desc(_DTYPES[lead.dtype], Q[1] if Q else 0, K[1] if K else 0, d, self.rotary_dim, self.interleaved, tokens, self.eps,
+                                         self.turns))
+        return device, lead.dtype, Q, K, desc, at, gains
+
+    def pm_head_norm_rotate(self, q, k, positions, q_gain, k_gain, q_out, k_out, stream=None):
+        """Writes q_out and k_out, which may be q and k."""
+        device, dtype, Q, K, desc, pos, gains = self._sides(q, k, positions, q_gain, k_gain)
+        views = _head_views((Q, K, Q, K), dtype, device, ("q", "k", "q_out", "k_out"), (q, k, q_out, k_out), 2)
+        at = C.addressof(views)
+        _launch(lambda st: self.L.pm_head_norm_rotate(desc, at, at + _VIEW, pos, *gains, at + 2 * _VIEW, at + 3 * _VIEW, st), device, stream)
+
+    def pm_head_norm_rotate_backward(self, q, k, positions, q_gain, k_gain, d_q_out, d_k_out, dq, dk, d_q_gain=None, d_k_gain=None, stream=None):
+        """Writes dq and dk (which may be d_q_out and d_k_out) and the gains' gradients that are given."""
+        device, dtype, Q, K, desc, pos, gains = self._sides(q, k, positions, q_gain, k_gain)
+        views = _head_views((Q, K, Q, K, Q, K), dtype, device, ("q", "k", "d_q_out", "d_k_out", "dq", "dk"), (q, k, d_q_out, d_k_out, dq, dk), 4)
+        grads = [_flat(n, g, torch.float32, device, (self.head_dim,)) for n, g in (("d_q_gain", d_q_gain), ("d_k_gain", d_k_gain))]
+        at = C.addressof(views)
+        need = self.L.pm_head_norm_rotate_workspace_bytes(desc) if grads != [None, None] else 0
+        _launch(lambda st, ws=None: self.L.pm_head_norm_rotate_backward(
+            desc, at, at + _VIEW, pos, *gains, at + 2 * _VIEW, at + 3 * _VIEW, at + 4 * _VIEW, at + 5 * _VIEW, *grads, ws, need, st), device, stream, need)
+
+
+class Dropout:
+    """Dropout with a mask that is never stored: formed from a counter-based generator in the forward and in the backward call.
+
+    x, y, residual: tensors of one shape, contiguous, all float32 or all bfloat16.  rng: int64 [2] on the device, the generator's key and
+    the first counter of this call, which uses counters(x.numel()) of them; the backward call takes the same two numbers.  They are
+    read when the call runs: between replays of a captured graph the program moves the counter on.  p is taken to the nearest
+    2^-16; what is kept is scaled by 1 / (1 - p).
+    """
+
+    def __init__(self, p):
+        p = float(p)
+        if not 0 <= p < 1 - 2.0 ** -17:
+            _refuse("p must be 0 to below 1 - 2^-17")
+        self.p = p
+        self.L = lib()
+
+    @staticmethod
+    def counters(n):
+        """How many counters a call on n elements uses."""
+        return (n + 7) // 8
+
+    def _tensors(self, names, tensors, rng):
+        lead = tensors[0]
+        device = _compute_device(names[0], lead)
+        pointers = [_flat(n, t, lead.dtype, device, lead.shape) for n, t in zip(names, tensors)]
+        if rng is None:
+            _refuse("rng must be a tensor")
+        return device, _DTYPES[lead.dtype], lead.numel(), pointers, _flat("rng", rng, torch.int64, device, (2,))
+
+    def pm_dropout(self, x, rng, y, residual=None, stream=None):
+        """Writes y (which may be x or the residual): what is kept of x, scaled, added to the residual."""
+        device, dtype, n, (p_x, p_y, p_res), p_rng = self._tensors(("x", "y", "residual"), (x, y, residual), rng)
+        if y is None:
+            _refuse("y must be a tensor")
+        _launch(lambda st: self.L.pm_dropout(p_x, p_res, dtype, n, self.p, p_rng, p_y, st), device, stream)
+
+    def pm_dropout_backward(self, d_y, rng, d_x, stream=None):
+        """Writes d_x (which may be d_y); the residual's gradient is d_y itself."""
+        device, dtype, n, (p_y, p_x), p_rng = self._tensors(("d_y", "d_x"), (d_y, d_x), rng)
+        if d_x is None:
+            _refuse("d_x must be a tensor")
+        _launch(lambda st: self.L.pm_dropout_backward(p_y, dtype, n, self.p, p_rng, p_x, st), device, stream)
 
 
 class TokenLogProbs:
@@ -293,6 +423,45 @@ class TokenLogProbs:
                 _flat("d_logprob", d_logprob, f32, device, (n,)), _flat("d_entropy", d_entropy, f32, device, (n,)),
                 d_logits.data_ptr(), grad_stride)
         _launch(lambda st: self.L.pm_token_logprobs_backward(*args, st), device, stream)
+
+
+class PolicyLoss:
+    """Clipped policy loss of sampled tokens with a KL term to a reference and an entropy bonus, with its gradients, between
+    TokenLogProbs' forward and backward call.
+
+    All tensors float32 [tokens], contiguous: logprob, old_logprob, advantage; ref_logprob (needed with kl_coef) and entropy (needed with
+    entropy_coef); weight (None: 1), 0 for padding, whose values count for nothing.  With mean the weights are divided by their sum, else
+    they are taken as they are (1 / the tokens of all microbatches, say).  stats: float32 [5], the loss and the weighted sums of its
+    policy term, of the KL term, of the entropy, and of the clipped tokens.
+    """
+
+    def __init__(self, *, clip_low=0.2, clip_high=0.2, kl_coef=0.0, entropy_coef=0.0, mean=True):
+        clip_low, clip_high, kl_coef, entropy_coef = float(clip_low), float(clip_high), float(kl_coef), float(entropy_coef)
+        if not 0 <= clip_low <= 1:
+            _refuse("clip_low must be 0 to 1")
+        if not clip_high >= 0:
+            _refuse("clip_high must not be negative")
+        if not (math.isfinite(kl_coef) and math.isfinite(entropy_coef)):
+            _refuse("coefficients must be finite")
+        self.kl_coef, self.entropy_coef = kl_coef, entropy_coef
+        self.desc = pm_policy_desc(clip_low, clip_high, kl_coef, entropy_coef, bool(mean))
+        self.L = lib()
+
+    def pm_policy_loss(self, logprob, old_logprob, advantage, stats, d_logprob=None, ref_logprob=None, entropy=None, d_entropy=None, weight=None,
+                       stream=None):
+        """Writes stats and the gradients that are given."""
+        if not (isinstance(logprob, torch.Tensor) and logprob.is_cuda):
+            _refuse("logprob must be a CUDA tensor")
+        device, f32, n = logprob.device, torch.float32, logprob.numel()
+        if old_logprob is None or advantage is None or stats is None:
+            _refuse("old_logprob, advantage and stats must be tensors")
+        if self.kl_coef and ref_logprob is None or self.entropy_coef and entropy is None:
+            _refuse("kl_coef without ref_logprob" if self.kl_coef and ref_logprob is None else "entropy_coef without entropy")
+        names = ("logprob", "old_logprob", "advantage", "ref_logprob", "entropy", "weight")
+        ins = [_flat(name, t, f32, device, (n,)) for name, t in zip(names, (logprob, old_logprob, advantage, ref_logprob, entropy, weight))]
+        outs = [_flat("stats", stats, f32, device, (5,)), _flat("d_logprob", d_logprob, f32, device, (n,)), _flat("d_entropy", d_entropy, f32, device, (n,))]
+        need = self.L.pm_policy_loss_workspace_bytes(n)
+        _launch(lambda st, ws=None: self.L.pm_policy_loss(C.byref(self.desc), n, *ins, *outs, ws, need, st), device, stream, need)
 
 
 class GradClip:
