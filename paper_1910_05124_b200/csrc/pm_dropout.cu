@@ -13,13 +13,21 @@ namespace pm {
 
 constexpr int kDropThreads = 256, kDropVectors = 2;                  // vectors of eight elements to a thread
 
-__device__ __forceinline__ uint4 philox(uint4 c, uint2 key) {
+// The keys of the ten rounds, formed once for a thread's counters.
+struct RoundKeys {
+  uint2 k[10];
+  __device__ __forceinline__ explicit RoundKeys(uint64_t key) {
+    k[0] = make_uint2((uint32_t)key, (uint32_t)(key >> 32));
+#pragma unroll
+    for (int i = 1; i < 10; ++i) k[i] = make_uint2(k[i - 1].x + 0x9E3779B9u, k[i - 1].y + 0xBB67AE85u);
+  }
+};
+__device__ __forceinline__ uint4 philox(uint64_t counter, const RoundKeys& keys) {
+  uint4 c = make_uint4((uint32_t)counter, (uint32_t)(counter >> 32), 0u, 0u);
 #pragma unroll
   for (int i = 0; i < 10; ++i) {
     const uint64_t a = (uint64_t)0xD2511F53u * c.x, b = (uint64_t)0xCD9E8D57u * c.z;
-    c = make_uint4((uint32_t)(b >> 32) ^ c.y ^ key.x, (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ key.y, (uint32_t)a);
-    key.x += 0x9E3779B9u;
-    key.y += 0xBB67AE85u;
+    c = make_uint4((uint32_t)(b >> 32) ^ c.y ^ keys.k[i].x, (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ keys.k[i].y, (uint32_t)a);
   }
   return c;
 }
@@ -29,6 +37,8 @@ template <typename T, bool VEC, bool RES>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const T* x, const T* residual, T* y, int64_t n, const uint64_t* rng, uint32_t dropped, float scale) {
   constexpr int U = kDropVectors;
   const int64_t first = (int64_t)blockIdx.x * kDropThreads * U + threadIdx.x;
+  const uint64_t counter = rng[1];
+  const RoundKeys keys(rng[0]);
   float v[U][8], r[U][8];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -44,20 +54,18 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const T* x, const
       }
     }
   }
-  const uint64_t key = rng[0], counter = rng[1];
+  const uint32_t border = dropped << 16;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int64_t vector = first + u * kDropThreads, at = vector * 8;
     if (at >= n) break;
-    const uint64_t c = counter + (uint64_t)vector;
-    const uint4 w = philox(make_uint4((uint32_t)c, (uint32_t)(c >> 32), 0u, 0u), make_uint2((uint32_t)key, (uint32_t)(key >> 32)));
+    const uint4 w = philox(counter + (uint64_t)vector, keys);
     const uint32_t words[4] = {w.x, w.y, w.z, w.w};
     float out[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t bits = e & 1 ? words[e / 2] >> 16 : words[e / 2] & 0xFFFFu;
-      const float kept = bits >= dropped ? v[u][e] * scale : 0.f;    // chosen, not multiplied: what is dropped may be anything
-      out[e] = RES ? r[u][e] + kept : kept;
+    for (int e = 0; e < 8; ++e) {                 // chosen, not multiplied: what is dropped may be anything
+      const bool kept = (e & 1 ? words[e / 2] : words[e / 2] << 16) >= border;   // the half as the upper one: the lower bits decide nothing
+      out[e] = kept ? (RES ? fmaf(v[u][e], scale, r[u][e]) : v[u][e] * scale) : (RES ? r[u][e] : 0.f);
     }
     if (VEC && at + 8 <= n) {
       store8<T>(y + at, out);

@@ -26,9 +26,10 @@ struct NormSide {
 struct NormArgs {
   NormSide side[2];                               // queries, keys
   const int32_t* positions;
-  float* partials;                                // [block][side][dim], of the gains' gradients
+  float* partials;                                // [block][dim] of the gains' gradients, the keys' blocks behind the queries'
   int64_t tokens;
   int dim, rotary, parts;                         // parts: groups to a token
+  int blocks[2], side_parts[2];                   // backward pass: blocks of each side, groups to a token there
   float eps;
   uint64_t turns[kNormMostPairs];                 // frequency of each pair, 2^-64 turns per position
 };
@@ -107,6 +108,14 @@ template <typename T, bool INTER> struct NormLane {
     unpack<T>(*reinterpret_cast<const uint4*>(row + a), v);
     unpack<T>(*reinterpret_cast<const uint4*>(row + b), v + V);
   }
+  __device__ __forceinline__ void fetch(uint4 (&v)[2], const T* row) const {
+    v[0] = *reinterpret_cast<const uint4*>(row + a);
+    v[1] = *reinterpret_cast<const uint4*>(row + b);
+  }
+  static __device__ __forceinline__ void spread(float (&v)[2 * V], const uint4 (&raw)[2]) {
+    unpack<T>(raw[0], v);
+    unpack<T>(raw[1], v + V);
+  }
   __device__ __forceinline__ void gains(float (&g)[2 * V], const float* gain) const {
 #pragma unroll
     for (int e = 0; e < V; ++e) { g[e] = gain[a + e]; g[V + e] = gain[b + e]; }
@@ -170,9 +179,9 @@ __global__ void __launch_bounds__(kNormThreads) head_norm_kernel(const __grid_co
   }
 }
 
-// The block's sums of the gains' gradients, over its groups in a fixed order.
+// The block's sums of the gains' gradients, over its groups in a fixed order, to row `block` of the partial sums.
 template <int L, int N, typename COL>
-__device__ __forceinline__ void leave_gains(const NormArgs& p, int side, const float (&acc)[N], bool on, COL col) {
+__device__ __forceinline__ void leave_gains(const NormArgs& p, int block, const float (&acc)[N], bool on, COL col) {
   __shared__ float sums[kNormThreads / 32][128];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   __syncthreads();
@@ -188,56 +197,62 @@ __device__ __forceinline__ void leave_gains(const NormArgs& p, int side, const f
     float v = 0.f;
 #pragma unroll
     for (int w = 0; w < kNormThreads / 32; ++w) v += sums[w][i];
-    p.partials[((int64_t)blockIdx.x * 2 + side) * p.dim + i] = v;
+    p.partials[(int64_t)block * p.dim + i] = v;
   }
 }
 
+// A block has rows of queries or rows of keys alone, so that it needs the sums of one gain; the next head's rows are fetched while this
+// one's are worked on.
 template <typename T, int L, bool INTER>
-__global__ void __launch_bounds__(kNormThreads) head_norm_bwd_kernel(const __grid_constant__ NormArgs p) {
+__global__ void __launch_bounds__(kNormThreads, 2) head_norm_bwd_kernel(const __grid_constant__ NormArgs p) {
   constexpr int V = kVec<T>;
-  const int64_t groups = p.tokens * p.parts, step = (int64_t)gridDim.x * (kNormThreads / L);
+  pdl_trigger();
+  const int side = blockIdx.x >= p.blocks[0], block = blockIdx.x - (side ? p.blocks[0] : 0), parts = p.side_parts[side];
+  const NormSide& s = p.side[side];
+  const int64_t groups = p.tokens * parts, step = (int64_t)p.blocks[side] * (kNormThreads / L);
   const NormLane<T, INTER> at(threadIdx.x % L, p.dim, p.rotary);
   const float per = 1.f / p.dim;
-  float acc[2][2 * V] = {};
-  for (int64_t group = ((int64_t)blockIdx.x * kNormThreads + threadIdx.x) / L; group < groups; group += step) {
-    const int64_t token = group / p.parts;
+  float acc[2 * V] = {}, g[2 * V];
+  at.gains(g, s.gain);
+  for (int64_t group = ((int64_t)block * kNormThreads + threadIdx.x) / L; group < groups; group += step) {
+    const int64_t token = group / parts;
+    const int part = (int)(group - token * parts), h0 = s.heads * part / parts, h1 = s.heads * (part + 1) / parts;
+    const T *x_row = head_row<T>(s.x, token, h0), *u_row = head_row<T>(s.y, token, h0);
+    T* out = head_row_out<T>(s.dx, token, h0);
+    uint4 next_x[2], next_u[2];
+    at.fetch(next_x, x_row);
+    at.fetch(next_u, u_row);
     float2 cs[V];
     at.angles(cs, p, p.rotary ? p.positions[token] : 0);
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
-      const NormSide& s = p.side[side];
-      int h0, h1;
-      heads_of(p, side, (int)(group - token * p.parts), h0, h1);
-      if (h0 >= h1) continue;
-      float g[2 * V];
-      at.gains(g, s.gain);
-      for (int h = h0; h < h1; ++h) {
-        float x[2 * V], u[2 * V];
-        at.load(x, head_row<T>(s.x, token, h));
-        at.load(u, head_row<T>(s.y, token, h));
-        at.template turn<true>(u, cs);
-        float square = 0.f, dot = 0.f;
-#pragma unroll
-        for (int e = 0; e < 2 * V; ++e) { square = fmaf(x[e], x[e], square); dot = fmaf(x[e], u[e] * g[e], dot); }
-        const float r = rsqrtf(group_sum<L>(at.on ? square : 0.f) * per + p.eps);
-        const float f = group_sum<L>(at.on ? dot : 0.f) * per * r * r;
-#pragma unroll
-        for (int e = 0; e < 2 * V; ++e) {
-          acc[side][e] = fmaf(u[e], x[e] * r, acc[side][e]);
-          x[e] = r * (g[e] * u[e] - x[e] * f);
-        }
-        T* out = head_row_out<T>(s.dx, token, h);
-        if (at.on) {
-          *reinterpret_cast<uint4*>(out + at.a) = packed<T>(x);
-          *reinterpret_cast<uint4*>(out + at.b) = packed<T>(x + V);
-        }
+    for (int h = h0; h < h1; ++h) {
+      float x[2 * V], u[2 * V];
+      at.spread(x, next_x);
+      at.spread(u, next_u);
+      if (h + 1 < h1) {
+        x_row += s.x.head;
+        u_row += s.y.head;
+        at.fetch(next_x, x_row);
+        at.fetch(next_u, u_row);
       }
+      at.template turn<true>(u, cs);
+      float square = 0.f, dot = 0.f;
+#pragma unroll
+      for (int e = 0; e < 2 * V; ++e) { square = fmaf(x[e], x[e], square); dot = fmaf(x[e], u[e] * g[e], dot); }
+      const float r = rsqrtf(group_sum<L>(at.on ? square : 0.f) * per + p.eps);
+      const float f = group_sum<L>(at.on ? dot : 0.f) * per * r * r;
+#pragma unroll
+      for (int e = 0; e < 2 * V; ++e) {
+        acc[e] = fmaf(u[e], x[e] * r, acc[e]);
+        x[e] = r * (g[e] * u[e] - x[e] * f);
+      }
+      if (at.on) {
+        *reinterpret_cast<uint4*>(out + at.a) = packed<T>(x);
+        *reinterpret_cast<uint4*>(out + at.b) = packed<T>(x + V);
+      }
+      out += s.dx.head;
     }
   }
-  if (!p.partials) return;
-#pragma unroll
-  for (int side = 0; side < 2; ++side)
-    if (p.side[side].heads) leave_gains<L>(p, side, acc[side], at.on, [&](int e) { return e < V ? at.a + e : at.b + e - V; });
+  if (p.partials) leave_gains<L>(p, blockIdx.x, acc, at.on, [&](int e) { return e < V ? at.a + e : at.b + e - V; });
 }
 
 // Rows of any width, alignment and pairing: a warp to a row, an element to a lane, the other of a pair through shared memory.
@@ -246,11 +261,13 @@ __global__ void __launch_bounds__(kNormThreads) head_norm_any_kernel(const __gri
   __shared__ float rows[kNormThreads / 32][128];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = p.rotary / 2;
   float* const row = rows[warp];
-  const int64_t groups = p.tokens * p.parts, step = (int64_t)gridDim.x * (kNormThreads / 32);
+  const int only = BACKWARD && blockIdx.x >= p.blocks[0], block = blockIdx.x - (only ? p.blocks[0] : 0), parts = BACKWARD ? p.side_parts[only] : p.parts;
+  const int64_t groups = p.tokens * parts, step = (int64_t)(BACKWARD ? p.blocks[only] : (int)gridDim.x) * (kNormThreads / 32);
   const float per = 1.f / p.dim;
-  float acc[2][4] = {};
-  for (int64_t group = (int64_t)blockIdx.x * (kNormThreads / 32) + warp; group < groups; group += step) {
-    const int64_t token = group / p.parts;
+  float acc[4] = {};
+  if (BACKWARD) pdl_trigger();
+  for (int64_t group = (int64_t)block * (kNormThreads / 32) + warp; group < groups; group += step) {
+    const int64_t token = group / parts;
     const int32_t position = p.rotary ? p.positions[token] : 0;
     float c[4], sn[4];
     int other[4];
@@ -272,11 +289,12 @@ __global__ void __launch_bounds__(kNormThreads) head_norm_any_kernel(const __gri
 #pragma unroll
       for (int j = 0; j < 4; ++j) if (lane + 32 * j < p.rotary) v[j] = v[j] * c[j] + row[other[j]] * sn[j];
     };
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
+    const int part = (int)(group - token * parts);
+    for (int side = only; side < (BACKWARD ? only + 1 : 2); ++side) {
       const NormSide& s = p.side[side];
       int h0, h1;
-      heads_of(p, side, (int)(group - token * p.parts), h0, h1);
+      if (BACKWARD) { h0 = s.heads * part / parts; h1 = s.heads * (part + 1) / parts; }
+      else heads_of(p, side, part, h0, h1);
       for (int h = h0; h < h1; ++h) {
         float x[4], g[4], u[4];
         float square = 0.f, dot = 0.f;
@@ -297,7 +315,7 @@ __global__ void __launch_bounds__(kNormThreads) head_norm_any_kernel(const __gri
           T* out = head_row_out<T>(s.dx, token, h);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            acc[side][j] = fmaf(u[j], x[j] * r, acc[side][j]);
+            acc[j] = fmaf(u[j], x[j] * r, acc[j]);
             if (lane + 32 * j < p.dim) out[lane + 32 * j] = from_f<T>(r * (g[j] * u[j] - x[j] * f));
           }
         } else {
@@ -311,23 +329,21 @@ __global__ void __launch_bounds__(kNormThreads) head_norm_any_kernel(const __gri
       }
     }
   }
-  if (!BACKWARD || !p.partials) return;
-#pragma unroll
-  for (int side = 0; side < 2; ++side)
-    if (p.side[side].heads) leave_gains<32>(p, side, acc[side], true, [&](int e) { return lane + 32 * e; });
+  if (BACKWARD && p.partials) leave_gains<32>(p, blockIdx.x, acc, true, [&](int e) { return lane + 32 * e; });
 }
 
 // Sums of the blocks' parts in a fixed order, in 64 bits: 32 columns of a side to a block, 32 rows at a time.
-__global__ void __launch_bounds__(1024) head_norm_gains_kernel(const float* partials, int blocks, int dim, float* d_gain_q, float* d_gain_k) {
+__global__ void __launch_bounds__(1024) head_norm_gains_kernel(const float* partials, int blocks_q, int blocks_k, int dim, float* d_gain_q, float* d_gain_k) {
   __shared__ double sums[32][33];
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, side = blockIdx.y, col = blockIdx.x * 32 + x;
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, side = blockIdx.y, col = blockIdx.x * 32 + x, blocks = side ? blocks_k : blocks_q;
   float* const out = side ? d_gain_k : d_gain_q;
   pdl_wait();
   if (!out) return;
+  if (side) partials += (int64_t)blocks_q * dim;
   double v = 0.0;
   if (col < dim)
 #pragma unroll 4
-    for (int b = y; b < blocks; b += 32) v += partials[((int64_t)b * 2 + side) * dim + col];
+    for (int b = y; b < blocks; b += 32) v += partials[(int64_t)b * dim + col];
   sums[y][x] = v;
   __syncthreads();
   v = sums[x][y];                                 // a warp to a column
@@ -336,7 +352,7 @@ __global__ void __launch_bounds__(1024) head_norm_gains_kernel(const float* part
   if (x == 0 && blockIdx.x * 32 + y < dim) out[blockIdx.x * 32 + y] = (float)v;
 }
 
-constexpr int kNormBwdBlocks = 4 * kSms;
+constexpr int kNormBwdBlocks = 2 * kSms;          // as many as run at a time; the two sides share them
 
 // lanes to a row: the vectors of half a row, rounded up to a power of two
 static int norm_lanes(int dim, int vec) {
@@ -377,9 +393,23 @@ template <typename T> static cudaError_t norm_run(NormArgs& p, bool interleaved,
       if (backward) whole(s.dx);
     }
   const int lanes = vec ? norm_lanes(p.dim, V) : 32, heads = p.side[0].heads + p.side[1].heads;
-  p.parts = norm_parts(p.tokens, heads, lanes);
-  const int64_t per_block = kNormThreads / lanes, all = (p.tokens * p.parts + per_block - 1) / per_block;
-  const int64_t blocks = backward ? std::min<int64_t>(all, kNormBwdBlocks) : all;
+  const int64_t per_block = kNormThreads / lanes;
+  int64_t blocks;
+  if (backward) {
+    // both sides' groups, and the blocks, by their heads
+    blocks = 0;
+    for (int i = 0; i < 2; ++i) {
+      const int n = p.side[i].heads;
+      if (!n) continue;
+      const int share = std::max(1, (int)((int64_t)kNormBwdBlocks * n / heads));
+      p.side_parts[i] = norm_parts(p.tokens, n, lanes);
+      p.blocks[i] = (int)std::min<int64_t>((p.tokens * p.side_parts[i] + per_block - 1) / per_block, share);
+      blocks += p.blocks[i];
+    }
+  } else {
+    p.parts = norm_parts(p.tokens, heads, lanes);
+    blocks = (p.tokens * p.parts + per_block - 1) / per_block;
+  }
   if (!launchable(blocks)) return cudaErrorInvalidConfiguration;
   cudaError_t e;
   if (!vec)
@@ -388,7 +418,8 @@ template <typename T> static cudaError_t norm_run(NormArgs& p, bool interleaved,
   else
     e = interleaved ? norm_width<T, true>(p, lanes, backward, blocks, st) : norm_width<T, false>(p, lanes, backward, blocks, st);
   if (e == cudaSuccess && p.partials)
-    e = launch_pdl(head_norm_gains_kernel, dim3((p.dim + 31) / 32, 2), dim3(1024), 0, st, true, (const float*)p.partials, (int)blocks, p.dim, d_gain_q, d_gain_k);
+    e = launch_pdl(head_norm_gains_kernel, dim3((p.dim + 31) / 32, 2), dim3(1024), 0, st, true, (const float*)p.partials, p.blocks[0], p.blocks[1], p.dim,
+                   d_gain_q, d_gain_k);
   return e;
 }
 
@@ -470,7 +501,7 @@ pm_status pm_head_norm_rotate(const pm_head_norm_desc* d, const pm_head_view* q,
 }
 
 uint64_t pm_head_norm_rotate_workspace_bytes(const pm_head_norm_desc* d) {
-  return !d || d->head_dim < 1 || d->head_dim > 128 ? 0 : (uint64_t)kNormBwdBlocks * 2 * d->head_dim * sizeof(float);
+  return !d || d->head_dim < 1 || d->head_dim > 128 ? 0 : (uint64_t)(kNormBwdBlocks + 1) * d->head_dim * sizeof(float);
 }
 
 pm_status pm_head_norm_rotate_backward(const pm_head_norm_desc* d, const pm_head_view* q, const pm_head_view* k, const int32_t* positions,

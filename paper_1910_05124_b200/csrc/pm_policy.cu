@@ -22,12 +22,13 @@ namespace cg = cooperative_groups;
 constexpr int kPolicySums = 5;                    // of the weights, policy, kl, entropy and clipped terms
 constexpr int kPolicyThreads = 512, kPolicyHeld = 4, kPolicyCluster = 8;         // short lists: tokens to a thread, blocks
 constexpr int64_t kPolicyShort = (int64_t)kPolicyThreads * kPolicyHeld * kPolicyCluster;
-constexpr int kPolicyBlocks = 4 * kSms;           // long lists
+// Long lists: blocks of the launch that adds the weights; threads, consecutive tokens to a thread and most blocks of the one that does the rest.
+constexpr int kWeightBlocks = kSms, kPolicyLong = 256, kPolicyRun = 4, kPolicyBlocks = 4096;
 
 struct PolicyArgs {
   const float *logprob, *old_logprob, *advantage, *ref_logprob, *entropy, *weight;
   float *stats, *d_logprob, *d_entropy;
-  double* sums;                                   // long lists: of the weights [blocks], then of the terms [blocks][4]
+  double* sums;                                   // long lists: of the weights [kWeightBlocks], then of the terms [blocks][4]
   unsigned* ended;
   int64_t n;
   double log_low, log_high;                       // borders of delta
@@ -46,6 +47,16 @@ struct PolicyToken {
     adv = in ? a.advantage[i] : 0.f;
     ref = in && a.ref_logprob ? a.ref_logprob[i] : 0.f;
     ent = in && a.entropy ? a.entropy[i] : 0.f;
+  }
+  // four tokens from 16-byte loads
+  static __device__ __forceinline__ void load4(PolicyToken (&t)[4], const PolicyArgs& a, int64_t i) {
+    auto four = [&](const float* p, float other) { return p ? *reinterpret_cast<const float4*>(p + i) : make_float4(other, other, other, other); };
+    const float4 w = four(a.weight, 1.f), lp = four(a.logprob, 0.f), old = four(a.old_logprob, 0.f), adv = four(a.advantage, 0.f), ref = four(a.ref_logprob, 0.f),
+                 ent = four(a.entropy, 0.f);
+    t[0] = PolicyToken{lp.x, old.x, adv.x, ref.x, ent.x, w.x};
+    t[1] = PolicyToken{lp.y, old.y, adv.y, ref.y, ent.y, w.y};
+    t[2] = PolicyToken{lp.z, old.z, adv.z, ref.z, ent.z, w.z};
+    t[3] = PolicyToken{lp.w, old.w, adv.w, ref.w, ent.w, w.w};
   }
   // adds the token's terms; returns its gradient but for the share
   __device__ __forceinline__ float terms(const PolicyArgs& a, double (&sums)[kPolicySums]) const {
@@ -82,11 +93,14 @@ struct PolicyToken {
     if (a.entropy) sums[3] += (double)w * ent;
     return grad;
   }
+  __device__ __forceinline__ float lp_gradient(float grad, double share) const { return w == 0.f ? 0.f : (float)((double)w * share) * grad; }
+  __device__ __forceinline__ float entropy_gradient(const PolicyArgs& a, double share) const {
+    return w == 0.f ? 0.f : (float)(-a.entropy_coef * ((double)w * share));
+  }
   __device__ __forceinline__ void store(const PolicyArgs& a, int64_t i, float grad, double share) const {
     if (i >= a.n) return;
-    const float s = w == 0.f ? 0.f : (float)((double)w * share);
-    if (a.d_logprob) a.d_logprob[i] = w == 0.f ? 0.f : s * grad;
-    if (a.d_entropy) a.d_entropy[i] = w == 0.f ? 0.f : (float)(-a.entropy_coef * ((double)w * share));
+    if (a.d_logprob) a.d_logprob[i] = lp_gradient(grad, share);
+    if (a.d_entropy) a.d_entropy[i] = entropy_gradient(a, share);
   }
 };
 
@@ -147,40 +161,74 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_short_kernel(const __gr
 }
 
 // Sum of the weights, a part to a block, and the counter of the next launch.
-__global__ void __launch_bounds__(kPolicyThreads) policy_weights_kernel(const __grid_constant__ PolicyArgs a) {
+template <bool VEC> __global__ void __launch_bounds__(kPolicyThreads) policy_weights_kernel(const __grid_constant__ PolicyArgs a) {
   __shared__ double scratch[kPolicyThreads / 32][1];
   pdl_trigger();
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.ended = 0;
+  if (!a.weight || !a.mean) return;
   double sum[1] = {};
-  if (a.weight && a.mean)
-    for (int64_t i = (int64_t)blockIdx.x * kPolicyThreads + threadIdx.x; i < a.n; i += (int64_t)gridDim.x * kPolicyThreads) sum[0] += a.weight[i];
+  const int64_t first = (int64_t)blockIdx.x * kPolicyThreads + threadIdx.x, step = (int64_t)gridDim.x * kPolicyThreads, whole = VEC ? a.n / 4 : 0;
+  if (VEC)
+#pragma unroll 4
+    for (int64_t i = first; i < whole; i += step) {
+      const float4 w = reinterpret_cast<const float4*>(a.weight)[i];
+      sum[0] += ((double)w.x + w.y) + ((double)w.z + w.w);
+    }
+  for (int64_t i = whole * 4 + first; i < a.n; i += step) sum[0] += a.weight[i];
   const double v = policy_block_sum(sum, scratch);
   if (threadIdx.x == 0) a.sums[blockIdx.x] = v;
 }
 
-__global__ void __launch_bounds__(kPolicyThreads) policy_long_kernel(const __grid_constant__ PolicyArgs a) {
-  __shared__ double scratch[kPolicyThreads / 32][kPolicySums];
+// VEC: every tensor starts at a 16-byte boundary.
+template <bool VEC> __global__ void __launch_bounds__(kPolicyLong, 4) policy_long_kernel(const __grid_constant__ PolicyArgs a) {
+  __shared__ double scratch[kPolicyLong / 32][kPolicySums];
   __shared__ double total[kPolicySums];
   __shared__ bool last;
+  constexpr int R = kPolicyRun;
+  const int64_t step = (int64_t)gridDim.x * kPolicyLong * R;
+  int64_t i = ((int64_t)blockIdx.x * kPolicyLong + threadIdx.x) * R;
+  PolicyToken t[R];
+  auto load = [&]() {
+    if (VEC && i + R <= a.n) {
+      PolicyToken::load4(t, a, i);
+    } else {
+#pragma unroll
+      for (int e = 0; e < R; ++e) t[e].load(a, i + e);
+    }
+  };
+  load();                                         // the first tokens while the weights are added
+  double sums[kPolicySums] = {};
+  float grad[R];
+#pragma unroll
+  for (int e = 0; e < R; ++e) grad[e] = t[e].terms(a, sums);
   pdl_wait();
   if (threadIdx.x < 32) {
     double v = 0.0;
     if (a.weight && a.mean)
-      for (int b = threadIdx.x; b < (int)gridDim.x; b += 32) v += a.sums[b];
+      for (int b = threadIdx.x; b < kWeightBlocks; b += 32) v += a.sums[b];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     if (threadIdx.x == 0) total[0] = a.weight && a.mean ? v : (double)a.n;
   }
   __syncthreads();
   const double weights = total[0], share = policy_share(a, weights);
-  double sums[kPolicySums] = {};
-  for (int64_t i = (int64_t)blockIdx.x * kPolicyThreads + threadIdx.x; i < a.n; i += (int64_t)gridDim.x * kPolicyThreads) {
-    PolicyToken t;
-    t.load(a, i);
-    t.store(a, i, t.terms(a, sums), share);
+  for (;;) {
+    if (VEC && i + R <= a.n) {
+      auto four = [&](auto value) { return make_float4(value(0), value(1), value(2), value(3)); };
+      if (a.d_logprob) *reinterpret_cast<float4*>(a.d_logprob + i) = four([&](int e) { return t[e].lp_gradient(grad[e], share); });
+      if (a.d_entropy) *reinterpret_cast<float4*>(a.d_entropy + i) = four([&](int e) { return t[e].entropy_gradient(a, share); });
+    } else {
+#pragma unroll
+      for (int e = 0; e < R; ++e) t[e].store(a, i + e, grad[e], share);
+    }
+    i += step;
+    if (i >= a.n) break;
+    load();
+#pragma unroll
+    for (int e = 0; e < R; ++e) grad[e] = t[e].terms(a, sums);
   }
   const double sum = policy_block_sum(sums, scratch);
-  double* const terms = a.sums + gridDim.x;
+  double* const terms = a.sums + kWeightBlocks;
   if (threadIdx.x > 0 && threadIdx.x < kPolicySums) __stcg(terms + (int64_t)blockIdx.x * 4 + threadIdx.x - 1, sum);
   __threadfence();
   __syncthreads();
@@ -188,13 +236,20 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_long_kernel(const __gri
   __syncthreads();
   if (!last) return;
   __threadfence();
-  if (threadIdx.x < 128) {                        // a warp to a term
-    const int k = threadIdx.x >> 5;
+  {                                               // a lane in four to a term
+    const int k = threadIdx.x & 3;
     double v = 0.0;
-    for (int b = threadIdx.x & 31; b < (int)gridDim.x; b += 32) v += __ldcg(terms + (int64_t)b * 4 + k);
+#pragma unroll 8
+    for (int b = threadIdx.x >> 2; b < (int)gridDim.x; b += kPolicyLong / 4) v += __ldcg(terms + (int64_t)b * 4 + k);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if ((threadIdx.x & 31) == 0) total[k + 1] = v;
+    for (int o = 16; o >= 4; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) < 4) scratch[threadIdx.x >> 5][k] = v;
+  }
+  __syncthreads();
+  if (threadIdx.x < 4) {
+    double v = 0.0;
+    for (int w = 0; w < kPolicyLong / 32; ++w) v += scratch[w][threadIdx.x];
+    total[threadIdx.x + 1] = v;
   }
   __syncthreads();
   if (threadIdx.x == 0) policy_stats(a, total, share);
@@ -207,7 +262,7 @@ using namespace pm;
 extern "C" {
 
 uint64_t pm_policy_loss_workspace_bytes(int64_t n) {
-  return n <= kPolicyShort ? 0 : (uint64_t)kPolicyBlocks * 5 * sizeof(double) + 16;
+  return n <= kPolicyShort ? 0 : (uint64_t)(kWeightBlocks + kPolicyBlocks * 4 + 1) * sizeof(double);
 }
 
 pm_status pm_policy_loss(const pm_policy_desc* d, int64_t n, const float* logprob, const float* old_logprob, const float* advantage, const float* ref_logprob,
@@ -259,9 +314,14 @@ pm_status pm_policy_loss(const pm_policy_desc* d, int64_t n, const float* logpro
     return ops_cuda(cudaLaunchKernelEx(&cfg, policy_short_kernel, a), "policy loss");
   }
   a.sums = static_cast<double*>(workspace);
-  a.ended = reinterpret_cast<unsigned*>(a.sums + kPolicyBlocks * 5);
-  cudaError_t e = launch_pdl(policy_weights_kernel, dim3(weight && a.mean ? kPolicyBlocks : 1), dim3(kPolicyThreads), 0, st, false, a);
-  if (e == cudaSuccess) e = launch_pdl(policy_long_kernel, dim3(kPolicyBlocks), dim3(kPolicyThreads), 0, st, true, a);
+  a.ended = reinterpret_cast<unsigned*>(a.sums + kWeightBlocks + kPolicyBlocks * 4);
+  bool vec = true;
+  for (const void* p : {(const void*)logprob, (const void*)old_logprob, (const void*)advantage, (const void*)ref_logprob, (const void*)entropy, (const void*)weight,
+                        (const void*)d_logprob, (const void*)d_entropy})
+    vec = vec && aligned_to(p, 16);
+  const dim3 first(weight && a.mean ? kWeightBlocks : 1), rest((unsigned)std::min<int64_t>((n + kPolicyLong * kPolicyRun - 1) / (kPolicyLong * kPolicyRun), kPolicyBlocks));
+  cudaError_t e = launch_pdl(vec ? policy_weights_kernel<true> : policy_weights_kernel<false>, first, dim3(kPolicyThreads), 0, st, false, a);
+  if (e == cudaSuccess) e = launch_pdl(vec ? policy_long_kernel<true> : policy_long_kernel<false>, rest, dim3(kPolicyLong), 0, st, true, a);
   return ops_cuda(e, "policy loss");
 }
 
