@@ -11,7 +11,7 @@
 
 namespace pm {
 
-constexpr int kDropThreads = 256, kDropVectors = 2;                  // vectors of eight elements to a thread
+constexpr int kDropThreads = 256, kDropVectors = 2, kDropBlocks = 4;  // vectors of eight elements to a thread, blocks to an SM
 
 // The keys of the ten rounds, formed once for a thread's counters.
 struct RoundKeys {
@@ -32,53 +32,75 @@ __device__ __forceinline__ uint4 philox(uint64_t counter, const RoundKeys& keys)
   return c;
 }
 
-// VEC: every tensor starts at a 16-byte boundary.  x and y may be one tensor, so nothing is declared read-only.
+// Eight values as they lie in memory.
+template <typename T> struct Eight {
+  uint4 w[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
+  }
+  __device__ __forceinline__ void load(const T* p, int64_t n) {                  // of which n exist; any alignment
+    T v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e] : from_f<T>(0.f);
+    memcpy(w, v, sizeof(w));
+  }
+  __device__ __forceinline__ void spread(float (&v)[8]) const {
+    const T* p = reinterpret_cast<const T*>(w);
+    load8<T>(p, v);
+  }
+};
+
+// VEC: every tensor starts at a 16-byte boundary.  x and y may be one tensor, so nothing is declared read-only.  The generator works while
+// the loads are under way; as many blocks as run at a time, whose threads form the round keys once.
 template <typename T, bool VEC, bool RES>
-__global__ void __launch_bounds__(kDropThreads) dropout_kernel(const T* x, const T* residual, T* y, int64_t n, const uint64_t* rng, uint32_t dropped, float scale) {
+__global__ void __launch_bounds__(kDropThreads, kDropBlocks) dropout_kernel(const T* x, const T* residual, T* y, int64_t n, const uint64_t* rng, uint32_t dropped, float scale) {
   constexpr int U = kDropVectors;
-  const int64_t first = (int64_t)blockIdx.x * kDropThreads * U + threadIdx.x;
   const uint64_t counter = rng[1];
   const RoundKeys keys(rng[0]);
-  float v[U][8], r[U][8];
+  const uint32_t border = dropped << 16;
+  for (int64_t first = (int64_t)blockIdx.x * kDropThreads * U + threadIdx.x; first * 8 < n; first += (int64_t)gridDim.x * kDropThreads * U) {
+    Eight<T> a[U], b[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int64_t at = (first + u * kDropThreads) * 8;
-    if (VEC && at + 8 <= n) {
-      load8<T>(x + at, v[u]);
-      if (RES) load8<T>(residual + at, r[u]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[u][e] = at + e < n ? to_f<T>(x[at + e]) : 0.f;
-        if (RES) r[u][e] = at + e < n ? to_f<T>(residual[at + e]) : 0.f;
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = (first + u * kDropThreads) * 8;
+      if (VEC && at + 8 <= n) {
+        a[u].load(x + at);
+        if (RES) b[u].load(residual + at);
+      } else {
+        a[u].load(x + at, n - at);
+        if (RES) b[u].load(residual + at, n - at);
       }
     }
-  }
-  const uint32_t border = dropped << 16;
+    uint4 words[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int64_t vector = first + u * kDropThreads, at = vector * 8;
-    if (at >= n) break;
-    const uint4 w = philox(counter + (uint64_t)vector, keys);
-    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-    float out[8];
+    for (int u = 0; u < U; ++u) words[u] = philox(counter + (uint64_t)(first + u * kDropThreads), keys);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {                 // chosen, not multiplied: what is dropped may be anything
-      const bool kept = (e & 1 ? words[e / 2] : words[e / 2] << 16) >= border;   // the half as the upper one: the lower bits decide nothing
-      out[e] = kept ? (RES ? fmaf(v[u][e], scale, r[u][e]) : v[u][e] * scale) : (RES ? r[u][e] : 0.f);
-    }
-    if (VEC && at + 8 <= n) {
-      store8<T>(y + at, out);
-    } else {
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = (first + u * kDropThreads) * 8;
+      if (at >= n) break;
+      const uint32_t w[4] = {words[u].x, words[u].y, words[u].z, words[u].w};
+      float v[8], r[8];
+      a[u].spread(v);
+      if (RES) b[u].spread(r);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) if (at + e < n) y[at + e] = from_f<T>(out[e]);
+      for (int e = 0; e < 8; ++e) {               // chosen, not multiplied: what is dropped may be anything
+        const bool kept = (e & 1 ? w[e / 2] : w[e / 2] << 16) >= border;         // the half as the upper one: the lower bits decide nothing
+        v[e] = kept ? (RES ? fmaf(v[e], scale, r[e]) : v[e] * scale) : (RES ? r[e] : 0.f);
+      }
+      if (VEC && at + 8 <= n) {
+        store8<T>(y + at, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (at + e < n) y[at + e] = from_f<T>(v[e]);
+      }
     }
   }
 }
 
 template <typename T> static cudaError_t dropout_run(const void* x, const void* residual, void* y, int64_t n, const int64_t* rng, uint32_t dropped, cudaStream_t st) {
   const bool vec = aligned_to(x, 16) && aligned_to(residual, 16) && aligned_to(y, 16);
-  const int64_t blocks = (n + 8 * kDropThreads * kDropVectors - 1) / (8 * kDropThreads * kDropVectors);
+  const int64_t blocks = std::min<int64_t>((n + 8 * kDropThreads * kDropVectors - 1) / (8 * kDropThreads * kDropVectors), kDropBlocks * kSms);
   const float scale = 65536.f / (float)(65536u - dropped);
   auto go = [&](auto kernel) {
     return launch_pdl(kernel, dim3((unsigned)blocks), dim3(kDropThreads), 0, st, false, static_cast<const T*>(x), static_cast<const T*>(residual), static_cast<T*>(y), n,

@@ -4,15 +4,20 @@
 //   (y_a, y_b) = (n_a cos - n_b sin, n_b cos + n_a sin) for pair i of the first rotary_dim dimensions at the angle position f_i
 //   u = R^T dy,  dg = sum u x r,  dx = r (g u - x r^2 mean_i(g_i u_i x_i))
 //
-// Bound by memory: each row is read once and written once.  A group of lanes takes all heads of a token in turn, so the sines and cosines
-// of a token are formed once, in registers, by the lanes whose dimensions they turn; both dimensions of a pair lie in one lane, and
-// only the sum of squares crosses lanes.  Where there are few tokens, several groups share a token's heads.
+// Bound by memory: each row is read once and written once.  A group of lanes takes a row, and the groups of a warp take the same head of
+// consecutive tokens, then the next head: the sines and cosines of a token are formed once or twice, in registers, by the lanes whose
+// dimensions they turn, at the same time in the whole warp.  Both dimensions of a pair lie in one lane, and only the sum of squares
+// crosses lanes.  A lane's constants and values fill 100 registers, so few warps run at a time: what is under way is kept in shared
+// memory, each lane copying its own part of the next rows there.
 //
 // The angle is a fraction of a turn in 64 bits: position times the frequency in units of 2^-64 turns wraps as angles do, so it is exact
 // to 2^-33 turns at every position; the nearest quarter turn is taken off it before it becomes a float (at most an eighth of a turn, rounded
-// by 2.4e-8 radians).
-#include "pm_ops.cuh"
+// by 7e-8 radians), and sine and cosine of that are their series.
+#include <atomic>
+#include <cmath>
+
 #include "pm_attn_packed.cuh"
+#include "pm_ptx.cuh"
 
 namespace pm {
 
@@ -28,53 +33,57 @@ struct NormArgs {
   const int32_t* positions;
   float* partials;                                // [block][dim] of the gains' gradients, the keys' blocks behind the queries'
   int64_t tokens;
-  int dim, rotary, parts;                         // parts: groups to a token
-  int blocks[2], side_parts[2];                   // backward pass: blocks of each side, groups to a token there
+  int dim, rotary;
+  int blocks[2];                                  // of each side
   float eps;
   uint64_t turns[kNormMostPairs];                 // frequency of each pair, 2^-64 turns per position
 };
 
-// cos and sin of position times a frequency
-__device__ __forceinline__ float2 turn_of(int32_t position, uint64_t turns) {
+// What is left of position times a frequency beside its nearest quarter turn, in radians, and that quarter.
+__device__ __forceinline__ float rest_of(int32_t position, uint64_t turns, int& quarter) {
   const uint64_t a = (uint64_t)(int64_t)position * turns + (1ull << 61);         // an eighth of a turn on: the quarter is the nearest one
-  const int quarter = (int)(a >> 62);
-  const int32_t rest = (int32_t)((int64_t)((a & ((1ull << 62) - 1)) - (1ull << 61)) >> 30);   // 2^-34 turns
-  float s, c;
-  sincospif((float)rest * 1.1641532182693481e-10f, &s, &c);          // half turns: 2^-33
+  quarter = (int)(a >> 62);
+  const int32_t rest = (int32_t)((uint32_t)(a >> 30) - (1u << 31));              // 2^-34 turns
+  return (float)rest * 3.6572951e-10f;                                           // 2 pi 2^-34
+}
+// cosines (x) and sines of two angles of at most pi / 4: the series up to x^10 and x^9, whose next terms are below 2e-10 and 2e-9
+__device__ __forceinline__ void series(float2 x, float2& c, float2& s) {
+  auto k = [](float v) { return make_float2(v, v); };
+  const float2 q = mul_f32x2(x, x);
+  c = fma_f32x2(q, k(-1.f / 3628800.f), k(1.f / 40320.f));
+  s = fma_f32x2(q, k(1.f / 362880.f), k(-1.f / 5040.f));
+  c = fma_f32x2(c, q, k(-1.f / 720.f));
+  s = fma_f32x2(s, q, k(1.f / 120.f));
+  c = fma_f32x2(c, q, k(1.f / 24.f));
+  s = fma_f32x2(s, q, k(-1.f / 6.f));
+  c = fma_f32x2(c, q, k(-0.5f));
+  s = mul_f32x2(s, q);
+  c = fma_f32x2(c, q, k(1.f));
+  s = fma_f32x2(s, x, x);
+}
+// cos and sin from those of the rest
+__device__ __forceinline__ void turn_quarters(float& c, float& s, int quarter) {
   const float x = quarter & 1 ? -s : c, y = quarter & 1 ? c : s;
-  return quarter & 2 ? make_float2(-x, -y) : make_float2(x, y);
+  c = quarter & 2 ? -x : x;
+  s = quarter & 2 ? -y : y;
+}
+__device__ __forceinline__ float2 turn_of(int32_t position, uint64_t turns) {
+  int quarter;
+  float2 x = make_float2(rest_of(position, turns, quarter), 0.f), c, s;
+  series(x, c, s);
+  turn_quarters(c.x, s.x, quarter);
+  return make_float2(c.x, s.x);
 }
 
 template <typename T> constexpr int kVec = 16 / sizeof(T);           // elements of a 16-byte vector
 
-template <typename T> __device__ __forceinline__ void unpack(const uint4& w, float* v) {
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(T) == 4) {
-      v[i] = __uint_as_float(u[i]);
-    } else {
-      v[2 * i] = __uint_as_float(u[i] << 16);
-      v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-    }
-  }
-}
-template <typename T> __device__ __forceinline__ uint4 packed(const float* v) {
-  if constexpr (sizeof(T) == 4) {
-    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-  } else {
-    uint32_t u[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-      u[i] = *reinterpret_cast<const uint32_t*>(&b);
-    }
-    return make_uint4(u[0], u[1], u[2], u[3]);
-  }
-}
+// V pairs: the first elements and the second ones, two pairs to a register pair of the packed arithmetic.
+template <int V> struct Pairs {
+  float2 f[V / 2], s[V / 2];
+};
 
-// What a lane of a group holds of every row: two vectors, at columns a and b.  Without INTER a pair is an element of each, with INTER
-// it is two neighbours; behind the rotated dimensions the angle is zero.
+// What a lane of a group holds of every row: two vectors, at columns a and b, which are V pairs.  Without INTER a pair is an element of
+// each, with INTER it is two neighbours; behind the rotated dimensions the angle is zero.
 template <typename T, bool INTER> struct NormLane {
   static constexpr int V = kVec<T>;
   int a, b;
@@ -85,99 +94,109 @@ template <typename T, bool INTER> struct NormLane {
     if (INTER || c * 2 * V >= rotary) { a = 2 * c * V; b = a + V; }
     else { a = c * V; b = rotary / 2 + c * V; }
   }
-  // pair of the e-th angle
-  __device__ __forceinline__ int pair(int e) const {
-    if (INTER) return e < V / 2 ? a / 2 + e : b / 2 + e - V / 2;
-    return a + e;
-  }
-  __device__ __forceinline__ void angles(float2 (&cs)[V], const NormArgs& p, int32_t position) const {
+  // columns of the e-th pair
+  __device__ __forceinline__ int first(int e) const { return INTER ? (e < V / 2 ? a + 2 * e : b + 2 * e - V) : a + e; }
+  __device__ __forceinline__ int second(int e) const { return INTER ? first(e) + 1 : b + e; }
+  // cos in f, sin in s
+  __device__ __forceinline__ void angles(Pairs<V>& cs, const NormArgs& p, int32_t position) const {
+    if (a >= p.rotary) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) cs[e] = a < p.rotary ? turn_of(position, p.turns[pair(e)]) : make_float2(1.f, 0.f);
-  }
-  // v (both vectors one behind the other) turned forth or (BACK) back
-  template <bool BACK> static __device__ __forceinline__ void turn(float (&v)[2 * V], const float2 (&cs)[V]) {
+      for (int i = 0; i < V / 2; ++i) { cs.f[i] = make_float2(1.f, 1.f); cs.s[i] = make_float2(0.f, 0.f); }
+      return;
+    }
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const int i = INTER ? 2 * e : e, j = INTER ? 2 * e + 1 : V + e;
-      const float c = cs[e].x, s = BACK ? -cs[e].y : cs[e].y, x = v[i], y = v[j];
-      v[i] = x * c - y * s;
-      v[j] = y * c + x * s;
+    for (int i = 0; i < V / 2; ++i) {
+      const int pair = INTER ? first(2 * i) / 2 : a + 2 * i;       // of which the next one is the lane's next one, too
+      int qx, qy;
+      float2 x;
+      x.x = rest_of(position, p.turns[pair], qx);
+      x.y = rest_of(position, p.turns[pair + 1], qy);
+      series(x, cs.f[i], cs.s[i]);
+      turn_quarters(cs.f[i].x, cs.s[i].x, qx);
+      turn_quarters(cs.f[i].y, cs.s[i].y, qy);
     }
   }
-  __device__ __forceinline__ void load(float (&v)[2 * V], const T* row) const {
-    unpack<T>(*reinterpret_cast<const uint4*>(row + a), v);
-    unpack<T>(*reinterpret_cast<const uint4*>(row + b), v + V);
+  __device__ __forceinline__ void gains(Pairs<V>& g, const float* gain) const {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      (e & 1 ? g.f[e / 2].y : g.f[e / 2].x) = gain[first(e)];
+      (e & 1 ? g.s[e / 2].y : g.s[e / 2].x) = gain[second(e)];
+    }
   }
-  __device__ __forceinline__ void fetch(uint4 (&v)[2], const T* row) const {
-    v[0] = *reinterpret_cast<const uint4*>(row + a);
-    v[1] = *reinterpret_cast<const uint4*>(row + b);
-  }
-  static __device__ __forceinline__ void spread(float (&v)[2 * V], const uint4 (&raw)[2]) {
-    unpack<T>(raw[0], v);
-    unpack<T>(raw[1], v + V);
-  }
-  __device__ __forceinline__ void gains(float (&g)[2 * V], const float* gain) const {
+  static __device__ __forceinline__ void spread(Pairs<V>& v, const uint4* slot) {
+    const uint4 lo = slot[0], hi = slot[kNormThreads];
+    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) { g[e] = gain[a + e]; g[V + e] = gain[b + e]; }
-  }
-};
-
-template <int L> __device__ __forceinline__ uint32_t group_mask() {
-  return L == 32 ? 0xffffffffu : ((1u << (L & 31)) - 1) << (threadIdx.x & 31 & ~(L - 1));
-}
-template <int L> __device__ __forceinline__ float group_sum(float v) {
+      for (int i = 0; i < 2; ++i) {
+        v.f[i] = INTER ? make_float2(__uint_as_float(w[4 * i]), __uint_as_float(w[4 * i + 2])) : make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+        v.s[i] = INTER ? make_float2(__uint_as_float(w[4 * i + 1]), __uint_as_float(w[4 * i + 3]))
+                       : make_float2(__uint_as_float(w[4 + 2 * i]), __uint_as_float(w[5 + 2 * i]));
+      }
+    } else {
+      auto low = [](uint32_t u) { return __uint_as_float(u << 16); };
+      auto high = [](uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); };
 #pragma unroll
-  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(group_mask<L>(), v, o);
-  return v;
-}
-
-// The heads of `side` that part `part` of `parts` takes, of both sides' heads in a row.
-__device__ __forceinline__ void heads_of(const NormArgs& p, int side, int part, int& h0, int& h1) {
-  const int n = p.side[0].heads, all = n + p.side[1].heads;
-  const int first = (int)((int64_t)all * part / p.parts), last = (int)((int64_t)all * (part + 1) / p.parts);
-  h0 = side ? max(first - n, 0) : min(first, n);
-  h1 = side ? max(last - n, 0) : min(last, n);
-}
-
-template <typename T, int L, bool INTER>
-__global__ void __launch_bounds__(kNormThreads) head_norm_kernel(const __grid_constant__ NormArgs p) {
-  constexpr int V = kVec<T>, U = 2;               // heads in flight
-  const int64_t group = ((int64_t)blockIdx.x * kNormThreads + threadIdx.x) / L, token = group / p.parts;
-  if (token >= p.tokens) return;
-  const NormLane<T, INTER> at(threadIdx.x % L, p.dim, p.rotary);
-  float2 cs[V];
-  at.angles(cs, p, p.rotary ? p.positions[token] : 0);
-  const float per = 1.f / p.dim;
-  for (int side = 0; side < 2; ++side) {
-    const NormSide& s = p.side[side];
-    int h0, h1;
-    heads_of(p, side, (int)(group - token * p.parts), h0, h1);
-    if (h0 >= h1) continue;
-    float g[2 * V];
-    at.gains(g, s.gain);
-    for (int h = h0; h < h1; h += U) {
-      float x[U][2 * V];
-#pragma unroll
-      for (int i = 0; i < U; ++i) at.load(x[i], head_row<T>(s.x, token, min(h + i, h1 - 1)));
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        if (h + i >= h1) break;
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 2 * V; ++e) sum = fmaf(x[i][e], x[i][e], sum);
-        const float r = rsqrtf(group_sum<L>(at.on ? sum : 0.f) * per + p.eps);
-#pragma unroll
-        for (int e = 0; e < 2 * V; ++e) x[i][e] *= r * g[e];
-        at.template turn<false>(x[i], cs);
-        T* out = head_row_out<T>(s.y, token, h + i);
-        if (at.on) {
-          *reinterpret_cast<uint4*>(out + at.a) = packed<T>(x[i]);
-          *reinterpret_cast<uint4*>(out + at.b) = packed<T>(x[i] + V);
-        }
+      for (int i = 0; i < 4; ++i) {
+        v.f[i] = INTER ? make_float2(low(w[2 * i]), low(w[2 * i + 1])) : make_float2(low(w[i]), high(w[i]));
+        v.s[i] = INTER ? make_float2(high(w[2 * i]), high(w[2 * i + 1])) : make_float2(low(w[4 + i]), high(w[4 + i]));
       }
     }
   }
+  // to the lane's columns, of which `row` is the first; the other vector is `apart` elements on
+  static __device__ __forceinline__ void store(T* row, int apart, const Pairs<V>& v) {
+    uint32_t w[8];
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float x[4] = {v.f[i].x, v.f[i].y, v.s[i].x, v.s[i].y};
+        w[INTER ? 4 * i : 2 * i] = __float_as_uint(x[0]);
+        w[INTER ? 4 * i + 2 : 2 * i + 1] = __float_as_uint(x[1]);
+        w[INTER ? 4 * i + 1 : 4 + 2 * i] = __float_as_uint(x[2]);
+        w[INTER ? 4 * i + 3 : 5 + 2 * i] = __float_as_uint(x[3]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        w[INTER ? 2 * i : i] = INTER ? pack_bf16(v.f[i].x, v.s[i].x) : pack_bf16(v.f[i].x, v.f[i].y);
+        w[INTER ? 2 * i + 1 : 4 + i] = INTER ? pack_bf16(v.f[i].y, v.s[i].y) : pack_bf16(v.s[i].x, v.s[i].y);
+      }
+    }
+    *reinterpret_cast<uint4*>(row) = make_uint4(w[0], w[1], w[2], w[3]);
+    *reinterpret_cast<uint4*>(row + apart) = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+};
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 minus(float2 x) { return make_float2(-x.x, -x.y); }
+
+// over the L lanes of a group; the whole warp takes part
+template <int L> __device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
 }
+
+// The rows that a warp takes in turn, those of `tokens` consecutive tokens at a time: its share of one side's, heads within tokens.
+struct NormWalk {
+  int64_t token, left;
+  int h, heads, tokens;
+  __device__ __forceinline__ NormWalk(const NormArgs& p, int side, int block, int tokens) : heads(p.side[side].heads), tokens(tokens) {
+    const int64_t all = (p.tokens + tokens - 1) / tokens * heads, warps = (int64_t)p.blocks[side] * (kNormThreads / 32);
+    const int64_t at = (int64_t)block * (kNormThreads / 32) + (threadIdx.x >> 5), first = all * at / warps;
+    left = all * (at + 1) / warps - first;
+    token = first / heads;
+    h = (int)(first - token * heads);
+    token = token * tokens + (threadIdx.x & 31) / (32 / tokens);
+  }
+  // whether the next row is another token's
+  __device__ __forceinline__ bool next() {
+    --left;
+    if (++h < heads) return false;
+    h = 0;
+    token += tokens;
+    return true;
+  }
+};
 
 // The block's sums of the gains' gradients, over its groups in a fixed order, to row `block` of the partial sums.
 template <int L, int N, typename COL>
@@ -201,58 +220,122 @@ __device__ __forceinline__ void leave_gains(const NormArgs& p, int block, const 
   }
 }
 
-// A block has rows of queries or rows of keys alone, so that it needs the sums of one gain; the next head's rows are fetched while this
-// one's are worked on.
-template <typename T, int L, bool INTER>
-__global__ void __launch_bounds__(kNormThreads, 2) head_norm_bwd_kernel(const __grid_constant__ NormArgs p) {
-  constexpr int V = kVec<T>;
-  pdl_trigger();
-  const int side = blockIdx.x >= p.blocks[0], block = blockIdx.x - (side ? p.blocks[0] : 0), parts = p.side_parts[side];
+// Rows ahead of the one that is worked on, of 32 bytes a lane or, with their gradients, 64.
+template <bool BACKWARD> constexpr int kNormAhead = BACKWARD ? 3 : 5;
+template <bool BACKWARD> constexpr int kNormSmem = (kNormAhead<BACKWARD> + 1) * (BACKWARD ? 4 : 2) * kNormThreads * 16;
+
+// A block has rows of queries or rows of keys alone: one gain, and the sums of one.
+template <typename T, int L, bool INTER, bool BACKWARD>
+__global__ void __launch_bounds__(kNormThreads, BACKWARD ? 2 : 3) head_norm_kernel(const __grid_constant__ NormArgs p) {
+  constexpr int V = kVec<T>, A = kNormAhead<BACKWARD>, W = BACKWARD ? 4 : 2;     // W: vectors of a row in shared memory
+  extern __shared__ uint4 ring[];
+  if (BACKWARD) pdl_trigger();
+  const int side = blockIdx.x >= p.blocks[0], block = blockIdx.x - (side ? p.blocks[0] : 0);
   const NormSide& s = p.side[side];
-  const int64_t groups = p.tokens * parts, step = (int64_t)p.blocks[side] * (kNormThreads / L);
   const NormLane<T, INTER> at(threadIdx.x % L, p.dim, p.rotary);
   const float per = 1.f / p.dim;
-  float acc[2 * V] = {}, g[2 * V];
-  at.gains(g, s.gain);
-  for (int64_t group = ((int64_t)block * kNormThreads + threadIdx.x) / L; group < groups; group += step) {
-    const int64_t token = group / parts;
-    const int part = (int)(group - token * parts), h0 = s.heads * part / parts, h1 = s.heads * (part + 1) / parts;
-    const T *x_row = head_row<T>(s.x, token, h0), *u_row = head_row<T>(s.y, token, h0);
-    T* out = head_row_out<T>(s.dx, token, h0);
-    uint4 next_x[2], next_u[2];
-    at.fetch(next_x, x_row);
-    at.fetch(next_u, u_row);
-    float2 cs[V];
-    at.angles(cs, p, p.rotary ? p.positions[token] : 0);
-    for (int h = h0; h < h1; ++h) {
-      float x[2 * V], u[2 * V];
-      at.spread(x, next_x);
-      at.spread(u, next_u);
-      if (h + 1 < h1) {
-        x_row += s.x.head;
+  NormWalk now(p, side, block, 32 / L), ahead = now;
+  // a group behind the last token takes that one's rows and writes nothing
+  auto row_of = [&](const HeadView& v, const NormWalk& w) { return head_row<T>(v, min(w.token, p.tokens - 1), w.h) + at.a; };
+  const T *x_row = row_of(s.x, ahead), *u_row = BACKWARD ? row_of(s.y, ahead) : nullptr;
+  const HeadView& result = BACKWARD ? s.dx : s.y;
+  T* out = nullptr;
+  const int apart = at.b - at.a;
+  uint4* const mine = ring + threadIdx.x;
+  int put = 0, get = 0;                           // places in the ring, in vectors
+  constexpr int kPlace = W * kNormThreads, kPlaces = (A + 1) * kPlace;
+  auto copy_next = [&]() {                        // a group of copies even where there is no row left: they are counted
+    if (ahead.left > 0) {
+      cp_async16(mine + put, x_row);
+      cp_async16(mine + put + kNormThreads, x_row + apart);
+      x_row += s.x.head;
+      if (BACKWARD) {
+        cp_async16(mine + put + 2 * kNormThreads, u_row);
+        cp_async16(mine + put + 3 * kNormThreads, u_row + apart);
         u_row += s.y.head;
-        at.fetch(next_x, x_row);
-        at.fetch(next_u, u_row);
       }
-      at.template turn<true>(u, cs);
-      float square = 0.f, dot = 0.f;
-#pragma unroll
-      for (int e = 0; e < 2 * V; ++e) { square = fmaf(x[e], x[e], square); dot = fmaf(x[e], u[e] * g[e], dot); }
-      const float r = rsqrtf(group_sum<L>(at.on ? square : 0.f) * per + p.eps);
-      const float f = group_sum<L>(at.on ? dot : 0.f) * per * r * r;
-#pragma unroll
-      for (int e = 0; e < 2 * V; ++e) {
-        acc[e] = fmaf(u[e], x[e] * r, acc[e]);
-        x[e] = r * (g[e] * u[e] - x[e] * f);
+      if (ahead.next()) {
+        x_row = row_of(s.x, ahead);
+        if (BACKWARD) u_row = row_of(s.y, ahead);
       }
-      if (at.on) {
-        *reinterpret_cast<uint4*>(out + at.a) = packed<T>(x);
-        *reinterpret_cast<uint4*>(out + at.b) = packed<T>(x + V);
-      }
-      out += s.dx.head;
     }
+    cp_async_commit();
+    put = put + kPlace == kPlaces ? 0 : put + kPlace;
+  };
+#pragma unroll
+  for (int i = 0; i < A; ++i) copy_next();
+  Pairs<V> g, acc = {}, cs, gs;
+  if (BACKWARD) at.gains(g, s.gain);
+  for (bool fresh = true; now.left > 0; fresh = now.next()) {
+    const bool on = at.on && now.token < p.tokens;
+    if (fresh) {
+      out = const_cast<T*>(row_of(result, now));
+      at.angles(cs, p, p.rotary && on ? p.positions[now.token] : 0);
+      if (!BACKWARD) {                            // gains times cosines (in cs, first and second element) and sines
+        at.gains(g, s.gain);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+          gs.f[i] = mul_f32x2(g.f[i], cs.s[i]);
+          gs.s[i] = mul_f32x2(g.s[i], minus(cs.s[i]));
+          cs.s[i] = mul_f32x2(g.s[i], cs.f[i]);
+          cs.f[i] = mul_f32x2(g.f[i], cs.f[i]);
+        }
+      }
+    }
+    copy_next();
+    cp_async_wait<A>();                           // this row's copies, the oldest
+    const uint4* const slot = mine + get;
+    get = get + kPlace == kPlaces ? 0 : get + kPlace;
+    Pairs<V> x;
+    at.spread(x, slot);
+    float2 square = both(0.f);
+    if constexpr (!BACKWARD) {
+#pragma unroll
+      for (int e = 0; e < V / 2; ++e) square = fma_f32x2(x.s[e], x.s[e], fma_f32x2(x.f[e], x.f[e], square));
+      const float2 r = both(rsqrtf(group_sum<L>(on ? square.x + square.y : 0.f) * per + p.eps));
+#pragma unroll
+      for (int e = 0; e < V / 2; ++e) {           // y_a = r (x_a g_a cos - x_b g_b sin), y_b = r (x_b g_b cos + x_a g_a sin)
+        const float2 f = mul_f32x2(r, fma_f32x2(x.f[e], cs.f[e], mul_f32x2(x.s[e], gs.s[e])));
+        x.s[e] = mul_f32x2(r, fma_f32x2(x.s[e], cs.s[e], mul_f32x2(x.f[e], gs.f[e])));
+        x.f[e] = f;
+      }
+      if (on) at.store(out, apart, x);
+    } else {
+      Pairs<V> u;
+      at.spread(u, slot + 2 * kNormThreads);
+      float2 dot = both(0.f);
+#pragma unroll
+      for (int e = 0; e < V / 2; ++e) {
+        const float2 f = fma_f32x2(u.f[e], cs.f[e], mul_f32x2(u.s[e], cs.s[e]));
+        u.s[e] = fma_f32x2(u.s[e], cs.f[e], mul_f32x2(u.f[e], minus(cs.s[e])));
+        u.f[e] = f;
+        square = fma_f32x2(x.s[e], x.s[e], fma_f32x2(x.f[e], x.f[e], square));
+        dot = fma_f32x2(mul_f32x2(x.s[e], u.s[e]), g.s[e], fma_f32x2(mul_f32x2(x.f[e], u.f[e]), g.f[e], dot));
+      }
+      const float r = rsqrtf(group_sum<L>(on ? square.x + square.y : 0.f) * per + p.eps);
+      const float2 rr = both(on ? r : 0.f), f = both(group_sum<L>(on ? dot.x + dot.y : 0.f) * per * r * r * -r);
+#pragma unroll
+      for (int e = 0; e < V / 2; ++e) {
+        u.f[e] = mul_f32x2(u.f[e], rr);
+        u.s[e] = mul_f32x2(u.s[e], rr);
+        acc.f[e] = fma_f32x2(u.f[e], x.f[e], acc.f[e]);
+        acc.s[e] = fma_f32x2(u.s[e], x.s[e], acc.s[e]);
+        u.f[e] = fma_f32x2(x.f[e], f, mul_f32x2(u.f[e], g.f[e]));
+        u.s[e] = fma_f32x2(x.s[e], f, mul_f32x2(u.s[e], g.s[e]));
+      }
+      if (on) at.store(out, apart, u);
+    }
+    out += result.head;
   }
-  if (p.partials) leave_gains<L>(p, blockIdx.x, acc, at.on, [&](int e) { return e < V ? at.a + e : at.b + e - V; });
+  cp_async_wait<0>();
+  if (!BACKWARD || !p.partials) return;
+  float sums[2 * V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    sums[e] = e & 1 ? acc.f[e / 2].y : acc.f[e / 2].x;
+    sums[V + e] = e & 1 ? acc.s[e / 2].y : acc.s[e / 2].x;
+  }
+  leave_gains<L>(p, blockIdx.x, sums, at.on, [&](int e) { return e < V ? at.first(e) : at.second(e - V); });
 }
 
 // Rows of any width, alignment and pairing: a warp to a row, an element to a lane, the other of a pair through shared memory.
@@ -261,72 +344,65 @@ __global__ void __launch_bounds__(kNormThreads) head_norm_any_kernel(const __gri
   __shared__ float rows[kNormThreads / 32][128];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = p.rotary / 2;
   float* const row = rows[warp];
-  const int only = BACKWARD && blockIdx.x >= p.blocks[0], block = blockIdx.x - (only ? p.blocks[0] : 0), parts = BACKWARD ? p.side_parts[only] : p.parts;
-  const int64_t groups = p.tokens * parts, step = (int64_t)(BACKWARD ? p.blocks[only] : (int)gridDim.x) * (kNormThreads / 32);
+  const int side = blockIdx.x >= p.blocks[0], block = blockIdx.x - (side ? p.blocks[0] : 0);
+  const NormSide& s = p.side[side];
   const float per = 1.f / p.dim;
   float acc[4] = {};
   if (BACKWARD) pdl_trigger();
-  for (int64_t group = (int64_t)block * (kNormThreads / 32) + warp; group < groups; group += step) {
-    const int64_t token = group / parts;
-    const int32_t position = p.rotary ? p.positions[token] : 0;
-    float c[4], sn[4];
-    int other[4];
+  NormWalk now(p, side, block, 1);
+  float c[4], sn[4];
+  int other[4];
+  auto turn = [&](float (&v)[4]) {
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) row[lane + 32 * j] = v[j];
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) if (lane + 32 * j < p.rotary) v[j] = v[j] * c[j] + row[other[j]] * sn[j];
+  };
+  for (bool fresh = true; now.left > 0; fresh = now.next()) {
+    if (fresh) {
+      const int32_t position = p.rotary ? p.positions[now.token] : 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = lane + 32 * j;
+        const bool turned = i < p.rotary, second = interleaved ? i & 1 : i >= half;
+        const int pair = interleaved ? i / 2 : second ? i - half : i;
+        const float2 t = turned ? turn_of(position, p.turns[pair]) : make_float2(1.f, 0.f);
+        other[j] = turned ? (interleaved ? i ^ 1 : second ? i - half : i + half) : 0;
+        c[j] = t.x;
+        sn[j] = second != BACKWARD ? t.y : -t.y;  // what the other element of the pair is multiplied with
+      }
+    }
+    float x[4], g[4], u[4];
+    float square = 0.f, dot = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int i = lane + 32 * j;
-      const bool turned = i < p.rotary, second = interleaved ? i & 1 : i >= half;
-      const int pair = interleaved ? i / 2 : second ? i - half : i;
-      const float2 t = turned ? turn_of(position, p.turns[pair]) : make_float2(1.f, 0.f);
-      other[j] = turned ? (interleaved ? i ^ 1 : second ? i - half : i + half) : 0;
-      c[j] = t.x;
-      sn[j] = second != BACKWARD ? t.y : -t.y;    // what the other element of the pair is multiplied with
+      x[j] = i < p.dim ? to_f<T>(head_row<T>(s.x, now.token, now.h)[i]) : 0.f;
+      u[j] = BACKWARD && i < p.dim ? to_f<T>(head_row<T>(s.y, now.token, now.h)[i]) : 0.f;
+      g[j] = i < p.dim ? s.gain[i] : 0.f;
+      square = fmaf(x[j], x[j], square);
     }
-    auto turn = [&](float (&v)[4]) {
-      __syncwarp();
+    const float r = rsqrtf(group_sum<32>(square) * per + p.eps);
+    if constexpr (BACKWARD) {
+      turn(u);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) row[lane + 32 * j] = v[j];
-      __syncwarp();
+      for (int j = 0; j < 4; ++j) dot = fmaf(x[j], u[j] * g[j], dot);
+      const float f = group_sum<32>(dot) * per * r * r;
+      T* out = head_row_out<T>(s.dx, now.token, now.h);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) if (lane + 32 * j < p.rotary) v[j] = v[j] * c[j] + row[other[j]] * sn[j];
-    };
-    const int part = (int)(group - token * parts);
-    for (int side = only; side < (BACKWARD ? only + 1 : 2); ++side) {
-      const NormSide& s = p.side[side];
-      int h0, h1;
-      if (BACKWARD) { h0 = s.heads * part / parts; h1 = s.heads * (part + 1) / parts; }
-      else heads_of(p, side, part, h0, h1);
-      for (int h = h0; h < h1; ++h) {
-        float x[4], g[4], u[4];
-        float square = 0.f, dot = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int i = lane + 32 * j;
-          x[j] = i < p.dim ? to_f<T>(head_row<T>(s.x, token, h)[i]) : 0.f;
-          u[j] = BACKWARD && i < p.dim ? to_f<T>(head_row<T>(s.y, token, h)[i]) : 0.f;
-          g[j] = i < p.dim ? s.gain[i] : 0.f;
-          square = fmaf(x[j], x[j], square);
-        }
-        const float r = rsqrtf(group_sum<32>(square) * per + p.eps);
-        if constexpr (BACKWARD) {
-          turn(u);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) dot = fmaf(x[j], u[j] * g[j], dot);
-          const float f = group_sum<32>(dot) * per * r * r;
-          T* out = head_row_out<T>(s.dx, token, h);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            acc[j] = fmaf(u[j], x[j] * r, acc[j]);
-            if (lane + 32 * j < p.dim) out[lane + 32 * j] = from_f<T>(r * (g[j] * u[j] - x[j] * f));
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] *= r * g[j];
-          turn(x);
-          T* out = head_row_out<T>(s.y, token, h);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) if (lane + 32 * j < p.dim) out[lane + 32 * j] = from_f<T>(x[j]);
-        }
+      for (int j = 0; j < 4; ++j) {
+        acc[j] = fmaf(u[j], x[j] * r, acc[j]);
+        if (lane + 32 * j < p.dim) out[lane + 32 * j] = from_f<T>(r * (g[j] * u[j] - x[j] * f));
       }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] *= r * g[j];
+      turn(x);
+      T* out = head_row_out<T>(s.y, now.token, now.h);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) if (lane + 32 * j < p.dim) out[lane + 32 * j] = from_f<T>(x[j]);
     }
   }
   if (BACKWARD && p.partials) leave_gains<32>(p, blockIdx.x, acc, true, [&](int e) { return lane + 32 * e; });
@@ -352,7 +428,8 @@ __global__ void __launch_bounds__(1024) head_norm_gains_kernel(const float* part
   if (x == 0 && blockIdx.x * 32 + y < dim) out[blockIdx.x * 32 + y] = (float)v;
 }
 
-constexpr int kNormBwdBlocks = 2 * kSms;          // as many as run at a time; the two sides share them
+// As many blocks as run at a time; the two sides share them.
+template <bool BACKWARD> constexpr int kNormBlocks = (BACKWARD ? 2 : 3) * kSms;
 
 // lanes to a row: the vectors of half a row, rounded up to a power of two
 static int norm_lanes(int dim, int vec) {
@@ -360,25 +437,36 @@ static int norm_lanes(int dim, int vec) {
   while (lanes * 2 * vec < dim) lanes *= 2;
   return lanes;
 }
-// Groups to a token: one where tokens alone fill the SMs with 512 threads each, else as many as that takes and there are heads.
-static int norm_parts(int64_t tokens, int heads, int lanes) {
-  const int64_t want = (int64_t)512 * kSms / lanes;
-  return (int)std::min<int64_t>(heads, std::max<int64_t>(1, (want + tokens - 1) / tokens));
-}
 
-template <typename T, int L, bool INTER> static cudaError_t norm_vec(const NormArgs& p, bool backward, int64_t blocks, cudaStream_t st) {
-  return backward ? launch_pdl(head_norm_bwd_kernel<T, L, INTER>, dim3((unsigned)blocks), dim3(kNormThreads), 0, st, false, p)
-                  : launch_pdl(head_norm_kernel<T, L, INTER>, dim3((unsigned)blocks), dim3(kNormThreads), 0, st, false, p);
+// raises a kernel's shared-memory limit once per device
+template <typename K> static cudaError_t norm_allow(K kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev > 63 || !(done.load(std::memory_order_relaxed) >> dev & 1))) {
+    e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev <= 63) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  return e;
 }
-template <typename T, bool INTER> static cudaError_t norm_width(const NormArgs& p, int lanes, bool backward, int64_t blocks, cudaStream_t st) {
+template <typename T, int L, bool INTER, bool BACKWARD> static cudaError_t norm_launch(const NormArgs& p, cudaStream_t st) {
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = norm_allow(head_norm_kernel<T, L, INTER, BACKWARD>, kNormSmem<BACKWARD>, done);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(head_norm_kernel<T, L, INTER, BACKWARD>, dim3(p.blocks[0] + p.blocks[1]), dim3(kNormThreads), kNormSmem<BACKWARD>, st, false, p);
+}
+template <typename T, int L> static cudaError_t norm_vec(const NormArgs& p, bool interleaved, bool backward, cudaStream_t st) {
+  if (interleaved) return backward ? norm_launch<T, L, true, true>(p, st) : norm_launch<T, L, true, false>(p, st);
+  return backward ? norm_launch<T, L, false, true>(p, st) : norm_launch<T, L, false, false>(p, st);
+}
+template <typename T> static cudaError_t norm_width(const NormArgs& p, int lanes, bool interleaved, bool backward, cudaStream_t st) {
   switch (lanes) {
-    case 1: return norm_vec<T, 1, INTER>(p, backward, blocks, st);
-    case 2: return norm_vec<T, 2, INTER>(p, backward, blocks, st);
-    case 4: return norm_vec<T, 4, INTER>(p, backward, blocks, st);
-    case 8: return norm_vec<T, 8, INTER>(p, backward, blocks, st);
+    case 1: return norm_vec<T, 1>(p, interleaved, backward, st);
+    case 2: return norm_vec<T, 2>(p, interleaved, backward, st);
+    case 4: return norm_vec<T, 4>(p, interleaved, backward, st);
+    case 8: return norm_vec<T, 8>(p, interleaved, backward, st);
     default: break;
   }
-  if constexpr (sizeof(T) == 4) return norm_vec<T, 16, INTER>(p, backward, blocks, st);
+  if constexpr (sizeof(T) == 4) return norm_vec<T, 16>(p, interleaved, backward, st);
   return cudaErrorInvalidValue;
 }
 
@@ -394,29 +482,21 @@ template <typename T> static cudaError_t norm_run(NormArgs& p, bool interleaved,
     }
   const int lanes = vec ? norm_lanes(p.dim, V) : 32, heads = p.side[0].heads + p.side[1].heads;
   const int64_t per_block = kNormThreads / lanes;
-  int64_t blocks;
-  if (backward) {
-    // both sides' groups, and the blocks, by their heads
-    blocks = 0;
-    for (int i = 0; i < 2; ++i) {
-      const int n = p.side[i].heads;
-      if (!n) continue;
-      const int share = std::max(1, (int)((int64_t)kNormBwdBlocks * n / heads));
-      p.side_parts[i] = norm_parts(p.tokens, n, lanes);
-      p.blocks[i] = (int)std::min<int64_t>((p.tokens * p.side_parts[i] + per_block - 1) / per_block, share);
-      blocks += p.blocks[i];
-    }
-  } else {
-    p.parts = norm_parts(p.tokens, heads, lanes);
-    blocks = (p.tokens * p.parts + per_block - 1) / per_block;
+  for (int i = 0; i < 2; ++i) {
+    const int n = p.side[i].heads;
+    if (!n) continue;
+    // the blocks that run at a time go to the sides by their heads
+    const int64_t rows = (p.tokens + 32 / lanes - 1) / (32 / lanes) * (32 / lanes) * n;
+    p.blocks[i] = (int)std::min<int64_t>((rows + per_block - 1) / per_block, std::max(1, (int)((int64_t)(backward ? kNormBlocks<true> : kNormBlocks<false>) * n / heads)));
   }
-  if (!launchable(blocks)) return cudaErrorInvalidConfiguration;
   cudaError_t e;
-  if (!vec)
-    e = backward ? launch_pdl(head_norm_any_kernel<T, true>, dim3((unsigned)blocks), dim3(kNormThreads), 0, st, false, p, (int)interleaved)
-                 : launch_pdl(head_norm_any_kernel<T, false>, dim3((unsigned)blocks), dim3(kNormThreads), 0, st, false, p, (int)interleaved);
-  else
-    e = interleaved ? norm_width<T, true>(p, lanes, backward, blocks, st) : norm_width<T, false>(p, lanes, backward, blocks, st);
+  if (vec) {
+    e = norm_width<T>(p, lanes, interleaved, backward, st);
+  } else {
+    const dim3 grid(p.blocks[0] + p.blocks[1]);
+    e = backward ? launch_pdl(head_norm_any_kernel<T, true>, grid, dim3(kNormThreads), 0, st, false, p, (int)interleaved)
+                 : launch_pdl(head_norm_any_kernel<T, false>, grid, dim3(kNormThreads), 0, st, false, p, (int)interleaved);
+  }
   if (e == cudaSuccess && p.partials)
     e = launch_pdl(head_norm_gains_kernel, dim3((p.dim + 31) / 32, 2), dim3(1024), 0, st, true, (const float*)p.partials, p.blocks[0], p.blocks[1], p.dim,
                    d_gain_q, d_gain_k);
@@ -501,7 +581,7 @@ pm_status pm_head_norm_rotate(const pm_head_norm_desc* d, const pm_head_view* q,
 }
 
 uint64_t pm_head_norm_rotate_workspace_bytes(const pm_head_norm_desc* d) {
-  return !d || d->head_dim < 1 || d->head_dim > 128 ? 0 : (uint64_t)(kNormBwdBlocks + 1) * d->head_dim * sizeof(float);
+  return !d || d->head_dim < 1 || d->head_dim > 128 ? 0 : (uint64_t)(kNormBlocks<true> + 1) * d->head_dim * sizeof(float);
 }
 
 pm_status pm_head_norm_rotate_backward(const pm_head_norm_desc* d, const pm_head_view* q, const pm_head_view* k, const int32_t* positions,
