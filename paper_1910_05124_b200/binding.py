@@ -129,20 +129,20 @@ def lib():
                                         C.c_int32, C.POINTER(pm_config), C.c_int64, vp]
     L.pm_update_flat_static_max_stages.restype = C.c_int32
     L.pm_update_flat_static_last_error.restype = C.c_char_p
-    # views by address: a call's views are one array
-    i32, i64, u64, view, desc = C.c_int32, C.c_int64, C.c_uint64, vp, C.POINTER(pm_attention_desc)
+    # views and descriptions by address, or as their bytes
+    i32, i64, u64, view, desc = C.c_int32, C.c_int64, C.c_uint64, vp, vp
     L.pm_attention_packed_forward.argtypes = [desc, view, view, view, vp, view, vp, vp]
     L.pm_attention_packed_workspace_bytes.argtypes = [desc]
     L.pm_attention_packed_workspace_bytes.restype = u64
     L.pm_attention_packed_backward.argtypes = [desc, view, view, view, view, vp, view, vp, view, view, view, vp, u64, vp]
-    cross = C.POINTER(pm_cross_attention_desc)
+    cross = vp
     L.pm_attention_cross_forward.argtypes = [cross, view, view, view, vp, vp, view, vp, vp]
     L.pm_attention_cross_workspace_bytes.argtypes = [cross]
     L.pm_attention_cross_workspace_bytes.restype = u64
     L.pm_attention_cross_backward.argtypes = [cross, view, view, view, view, vp, view, vp, vp, view, view, view, vp, u64, vp]
     L.pm_attention_packed_status.argtypes = [vp]
     L.pm_attention_packed_selftest_wait_timeout.argtypes = [i64, vp]
-    norm, f64 = C.POINTER(pm_head_norm_desc), C.c_double
+    norm, f64 = vp, C.c_double
     L.pm_rotation_turns.argtypes = [i32, f64, u64p]
     L.pm_head_norm_rotate.argtypes = [norm, view, view, vp, vp, vp, view, view, vp]
     L.pm_head_norm_rotate_workspace_bytes.argtypes = [norm]

@@ -120,8 +120,8 @@ static pm_status dropout_call(const void* x, const void* residual, int32_t dtype
   if (!x || !y || !rng) return ops_fail(PM_ERR_INVALID_ARG, "null pointer");
   if (!aligned_to(x, size) || !aligned_to(residual, size) || !aligned_to(y, size)) return ops_fail(PM_ERR_INVALID_ARG, "pointer not aligned to its element type");
   if (!aligned_to(rng, 8)) return ops_fail(PM_ERR_INVALID_ARG, "rng must be 8-byte aligned");
-  auto apart = [&](const void* in, int64_t bytes) { return in == y && bytes == n * size ? true : !extents_share(dense_extent(y, n * size), dense_extent(in, bytes)); };
-  if (!apart(x, n * size) || !apart(residual, n * size) || extents_share(dense_extent(y, n * size), dense_extent(rng, 16)))
+  auto apart = [&](const void* in) { return in == y || !dense_share(y, n * size, in, n * size); };
+  if (!apart(x) || !apart(residual) || dense_share(y, n * size, rng, 16))
     return ops_fail(PM_ERR_INVALID_ARG, "the output overlaps an input without being the same tensor");
   const uint32_t dropped = (uint32_t)(p * 65536.0 + 0.5);
   const cudaStream_t st = (cudaStream_t)stream;

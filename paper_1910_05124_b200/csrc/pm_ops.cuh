@@ -24,6 +24,12 @@ inline Extent dense_extent(const void* p, int64_t bytes) { return Extent{(__int1
 inline Extent rows_extent(const void* p, int64_t rows, int64_t row_stride, int64_t columns, int size) {
   return Extent{(__int128)reinterpret_cast<uintptr_t>(p), (__int128)row_stride * size, rows, 0, 1, (__int128)columns * size};
 }
+// Whether two runs of bytes, of non-null pointers, have one in common.
+inline bool dense_share(const void* p, int64_t p_bytes, const void* q, int64_t q_bytes) {
+  if (!p || !q || p_bytes < 1 || q_bytes < 1) return false;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return a < b ? b - a < (uintptr_t)p_bytes : a - b < (uintptr_t)q_bytes;
+}
 // The same bytes in as few pieces as possible, the larger stride outside.
 inline Extent joined(Extent x) {
   if (x.n_inner > 1 && (x.outer < x.inner || x.n_outer == 1)) { std::swap(x.outer, x.inner); std::swap(x.n_outer, x.n_inner); }

@@ -284,14 +284,14 @@ pm_status pm_policy_loss(const pm_policy_desc* d, int64_t n, const float* logpro
   for (const auto& x : all) if (!aligned_to(x.p, 4)) return ops_fail(PM_ERR_INVALID_ARG, "pointer not aligned to its element type");
   for (int i = 0; i < 3; ++i)
     for (int j = 0; j < 9; ++j)
-      if (i != j && extents_share(dense_extent(all[i].p, all[i].bytes), dense_extent(all[j].p, all[j].bytes)))
+      if (i != j && dense_share(all[i].p, all[i].bytes, all[j].p, all[j].bytes))
         return ops_fail(PM_ERR_INVALID_ARG, j < 3 ? "two outputs overlap" : "an output overlaps one of the inputs");
   const uint64_t need = pm_policy_loss_workspace_bytes(n);
   if (need) {
     if (!workspace || workspace_bytes < need) return ops_fail(PM_ERR_NOMEM, "workspace too small: need %llu bytes", (unsigned long long)need);
     if (!aligned_to(workspace, 8)) return ops_fail(PM_ERR_INVALID_ARG, "workspace must be 8-byte aligned");
     for (const auto& x : all)
-      if (extents_share(dense_extent(workspace, (int64_t)need), dense_extent(x.p, x.bytes))) return ops_fail(PM_ERR_INVALID_ARG, "the workspace overlaps a tensor");
+      if (dense_share(workspace, (int64_t)need, x.p, x.bytes)) return ops_fail(PM_ERR_INVALID_ARG, "the workspace overlaps a tensor");
   }
   PolicyArgs a{};
   a.logprob = logprob; a.old_logprob = old_logprob; a.advantage = advantage; a.ref_logprob = ref_logprob; a.entropy = entropy; a.weight = weight;

@@ -7,17 +7,19 @@ Every call is asynchronous on `stream` (default: the current stream of the tenso
 graph.  As with any CUDA call, a tensor that another stream still writes has to be waited for by the caller, and a tensor
 that belongs to another stream has to be kept until the call has run.  Refused arguments raise PipeMareError.
 """
-import ctypes as C
 import math
+import struct
 from bisect import bisect_left
+from ctypes import addressof, byref, c_uint64
 
 import torch
 
-from .binding import (PM_BF16, PM_F32, PipeMareError, _check, lib, pm_attention_desc, pm_cross_attention_desc, pm_head_norm_desc,
-                      pm_head_view, pm_policy_desc, pm_tensor_pair)
+from .binding import PM_BF16, PM_F32, PipeMareError, _check, lib, pm_policy_desc, pm_tensor_pair
 
 _DTYPES = {torch.float32: PM_F32, torch.bfloat16: PM_BF16}
-_VIEW = C.sizeof(pm_head_view)
+_Tensor = torch.Tensor
+# pm_head_view and the descriptions as they lie in memory: what a call passes for a moment costs less as bytes than as ctypes objects
+_VIEW, _ATTENTION, _CROSS, _HEAD_NORM = (struct.Struct(f).pack for f in ("@Pqq", "@6iqf4x", "@5iqqf4x", "@6iqfP"))
 
 
 def _refuse(message, status="PM_ERR_INVALID_ARG"):
@@ -41,9 +43,22 @@ def _flat(name, t, dtype, device, shape):
     """Data pointer of a contiguous tensor; None for None."""
     if t is None:
         return None
-    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device.index and t.shape == shape and t.is_contiguous()):
+    if not (isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == device.index and t.shape == shape and t.is_contiguous()):
         _mismatch(name, t, dtype, device, shape)
     return t.data_ptr()
+
+
+def _flats(names, tensors, dtype, device, shape):
+    """_flat of several tensors of one type and shape."""
+    index, out = device.index, []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+        elif isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == index and t.shape == shape and t.is_contiguous():
+            out.append(t.data_ptr())
+        else:
+            _mismatch(names[len(out)], t, dtype, device, shape)
+    return out
 
 
 def _compute_device(name, t):
@@ -61,50 +76,63 @@ def _indexed(device):
 
 # the handle of the current stream without the object around it, where this torch has the call
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _launch(call, device, stream, workspace=0):
-    """call(stream handle[, workspace pointer]) with the tensors' device current, and its status checked.
-
-    The workspace is device scratch of this call alone: it comes from the allocator's pool of the launching stream, so the
-    memory is reused only by work queued behind the call (under capture it stays with the graph)."""
-    if device.index != torch.cuda.current_device():
+def _launch(call, args, device, stream):
+    """call(*args, stream handle) with the tensors' device current, and its status checked."""
+    index = device.index
+    if index != _current_device():
         with torch.cuda.device(device):
-            return _launch(call, device, stream, workspace)
+            return _launch(call, args, device, stream)
     if stream is None:
-        handle = _raw_stream(device.index)
+        status = call(*args, _raw_stream(index))
     else:
         if stream.device != device:
             _refuse(f"the stream belongs to {stream.device}, the tensors to {device}")
-        handle = stream.cuda_stream
+        status = call(*args, stream.cuda_stream)
+    if status:
+        _check(status)
+
+
+def _launch_with(workspace, call, args, device, stream):
+    """_launch of call(*args, workspace pointer, its bytes, stream handle).
+
+    The workspace is device scratch of this call alone: it comes from the allocator's pool of the launching stream, so the
+    memory is reused only by work queued behind the call (under capture it stays with the graph)."""
     if not workspace:
-        return _check(call(handle))
-    if stream is None or handle == _raw_stream(device.index):
+        return _launch(call, (*args, None, 0), device, stream)
+    if device.index != _current_device():
+        with torch.cuda.device(device):
+            return _launch_with(workspace, call, args, device, stream)
+    if stream is None or stream.cuda_stream == _raw_stream(device.index):
         scratch = torch.empty(workspace, dtype=torch.uint8, device=device)
     else:
+        if stream.device != device:
+            _refuse(f"the stream belongs to {stream.device}, the tensors to {device}")
         with torch.cuda.stream(stream):
             scratch = torch.empty(workspace, dtype=torch.uint8, device=device)
-    return _check(call(handle, scratch.data_ptr()))
+    _launch(call, (*args, scratch.data_ptr(), workspace), device, stream)
 
 
 def _head_views(shapes, dtype, device, names, tensors, n_read):
-    """One array of pm_head_view for tensors of these shapes ([tokens, heads, head_dim]), checked; those behind the first n_read are
-    written.  None gives a null view."""
-    index, flat = device.index, []
+    """A pm_head_view for each of the tensors, of these shapes ([tokens, heads, head_dim]), checked; those behind the first n_read are
+    written.  A shape of None gives None."""
+    index, views = device.index, []
     for t, shape in zip(tensors, shapes):
         if shape is None:
-            flat += (0, 0, 0)
+            views.append(None)
             continue
-        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == index and t.shape == shape):
-            _mismatch(names[len(flat) // 3], t, dtype, device, shape)
+        if not (isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == index and t.shape == shape):
+            _mismatch(names[len(views)], t, dtype, device, shape)
         tokens, h, d = shape
         token, head, one = t.stride()
         if one != 1 and d > 1:
-            _refuse(f"the last dimension of {names[len(flat) // 3]} must be contiguous")
-        if (head != d or token < h * d) and len(flat) >= 3 * n_read:
-            _check_apart(names[len(flat) // 3], d, ((token, tokens), (head, h)))
-        flat += (t.data_ptr(), token, head)
-    return (C.c_int64 * len(flat))(*flat)
+            _refuse(f"the last dimension of {names[len(views)]} must be contiguous")
+        if (head != d or token < h * d) and len(views) >= n_read:
+            _check_apart(names[len(views)], d, ((token, tokens), (head, h)))
+        views.append(_VIEW(t.data_ptr(), token, head))
+    return views
 
 
 def _check_apart(name, head_dim, dims):
@@ -154,11 +182,11 @@ class _HeadAttention:
     def pm_attention_packed_status(self, device="cuda", stream=None):
         """Raises if a device-side wait of a tensor-core kernel ran out since the last call on this device (a defect); synchronises
         the stream."""
-        _launch(self.L.pm_attention_packed_status, _indexed(device), stream)
+        _launch(self.L.pm_attention_packed_status, (), _indexed(device), stream)
 
     def pm_attention_packed_selftest_wait_timeout(self, limit_cycles, device="cuda", stream=None):
         """Enqueues a wait that runs out after limit_cycles: the next pm_attention_packed_status on this device raises."""
-        _launch(lambda st: self.L.pm_attention_packed_selftest_wait_timeout(int(limit_cycles), st), _indexed(device), stream)
+        _launch(self.L.pm_attention_packed_selftest_wait_timeout, (int(limit_cycles),), _indexed(device), stream)
 
 
 class PackedAttention(_HeadAttention):
@@ -177,32 +205,25 @@ class PackedAttention(_HeadAttention):
     def _desc(self, q, cu_seqlens):
         device, tokens = _head_rows("q", q, self.n_heads, self.head_dim)
         cu, n_seqs = self._starts("cu_seqlens", cu_seqlens, device)
-        return device, tokens, C.byref(pm_attention_desc(_DTYPES[q.dtype], self.n_heads, self.n_kv_heads, self.head_dim, n_seqs, self.causal, tokens,
-                                                         self.scale)), cu
+        return device, (tokens, self.n_heads, self.head_dim), (tokens, self.n_kv_heads, self.head_dim), _ATTENTION(
+            _DTYPES[q.dtype], self.n_heads, self.n_kv_heads, self.head_dim, n_seqs, self.causal, tokens, self.scale), cu
 
     def pm_attention_packed_forward(self, q, k, v, cu_seqlens, o, lse=None, stream=None):
         """Writes o and, for a backward pass, lse."""
-        device, tokens, desc, cu = self._desc(q, cu_seqlens)
-        Q, K = (tokens, self.n_heads, self.head_dim), (tokens, self.n_kv_heads, self.head_dim)
-        views = _head_views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
-        p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, tokens))
-        at = C.addressof(views)
-        _launch(lambda st: self.L.pm_attention_packed_forward(desc, at, at + _VIEW, at + 2 * _VIEW, cu, at + 3 * _VIEW, p_lse, st), device, stream)
+        device, Q, K, desc, cu = self._desc(q, cu_seqlens)
+        vq, vk, vv, vo = _head_views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
+        p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, Q[0]))
+        _launch(self.L.pm_attention_packed_forward, (desc, vq, vk, vv, cu, vo, p_lse), device, stream)
 
     def pm_attention_packed_backward(self, q, k, v, o, lse, d_o, cu_seqlens, dq, dk, dv, stream=None):
         """Writes dq, dk and dv from d_o and what the forward call wrote."""
-        device, tokens, desc, cu = self._desc(q, cu_seqlens)
+        device, Q, K, desc, cu = self._desc(q, cu_seqlens)
         if lse is None:
             _refuse("lse must be a tensor")
-        Q, K = (tokens, self.n_heads, self.head_dim), (tokens, self.n_kv_heads, self.head_dim)
-        views = _head_views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
-                            (q, k, v, o, d_o, dq, dk, dv), 5)
-        p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, tokens))
-        at = C.addressof(views)
-        need = self.L.pm_attention_packed_workspace_bytes(desc)
-        _launch(lambda st, ws=None: self.L.pm_attention_packed_backward(
-            desc, at, at + _VIEW, at + 2 * _VIEW, at + 3 * _VIEW, p_lse, at + 4 * _VIEW, cu, at + 5 * _VIEW, at + 6 * _VIEW, at + 7 * _VIEW, ws, need, st),
-            device, stream, need)
+        vq, vk, vv, vo, vdo, *grads = _head_views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
+                                                  (q, k, v, o, d_o, dq, dk, dv), 5)
+        p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, Q[0]))
+        _launch_with(4 * self.n_heads * Q[0], self.L.pm_attention_packed_backward, (desc, vq, vk, vv, vo, p_lse, vdo, cu, *grads), device, stream)
 
 
 class CrossAttention(_HeadAttention):
@@ -223,31 +244,25 @@ class CrossAttention(_HeadAttention):
         cu_kv, n_kv_seqs = self._starts("cu_seqlens_kv", cu_seqlens_kv, device)
         if n_seqs != n_kv_seqs:
             _refuse(f"cu_seqlens has {n_seqs} sequences, cu_seqlens_kv {n_kv_seqs}", "PM_ERR_SHAPE")
-        Q, K = (tokens, self.n_heads, self.head_dim), (kv_tokens, self.n_kv_heads, self.head_dim)
-        return device, Q, K, C.byref(pm_cross_attention_desc(_DTYPES[q.dtype], self.n_heads, self.n_kv_heads, self.head_dim, n_seqs, tokens, kv_tokens,
-                                                             self.scale)), cu, cu_kv
+        return device, (tokens, self.n_heads, self.head_dim), (kv_tokens, self.n_kv_heads, self.head_dim), _CROSS(
+            _DTYPES[q.dtype], self.n_heads, self.n_kv_heads, self.head_dim, n_seqs, tokens, kv_tokens, self.scale), cu, cu_kv
 
     def pm_attention_cross_forward(self, q, k, v, cu_seqlens, cu_seqlens_kv, o, lse=None, stream=None):
         """Writes o and, for a backward pass, lse."""
         device, Q, K, desc, cu, cu_kv = self._desc(q, k, cu_seqlens, cu_seqlens_kv)
-        views = _head_views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
+        vq, vk, vv, vo = _head_views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
         p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, Q[0]))
-        at = C.addressof(views)
-        _launch(lambda st: self.L.pm_attention_cross_forward(desc, at, at + _VIEW, at + 2 * _VIEW, cu, cu_kv, at + 3 * _VIEW, p_lse, st), device, stream)
+        _launch(self.L.pm_attention_cross_forward, (desc, vq, vk, vv, cu, cu_kv, vo, p_lse), device, stream)
 
     def pm_attention_cross_backward(self, q, k, v, o, lse, d_o, cu_seqlens, cu_seqlens_kv, dq, dk, dv, stream=None):
         """Writes dq, dk and dv from d_o and what the forward call wrote."""
         device, Q, K, desc, cu, cu_kv = self._desc(q, k, cu_seqlens, cu_seqlens_kv)
         if lse is None:
             _refuse("lse must be a tensor")
-        views = _head_views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
-                            (q, k, v, o, d_o, dq, dk, dv), 5)
+        vq, vk, vv, vo, vdo, *grads = _head_views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
+                                                  (q, k, v, o, d_o, dq, dk, dv), 5)
         p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, Q[0]))
-        at = C.addressof(views)
-        need = self.L.pm_attention_cross_workspace_bytes(desc)
-        _launch(lambda st, ws=None: self.L.pm_attention_cross_backward(
-            desc, at, at + _VIEW, at + 2 * _VIEW, at + 3 * _VIEW, p_lse, at + 4 * _VIEW, cu, cu_kv, at + 5 * _VIEW, at + 6 * _VIEW, at + 7 * _VIEW, ws, need, st),
-            device, stream, need)
+        _launch_with(4 * self.n_heads * Q[0], self.L.pm_attention_cross_backward, (desc, vq, vk, vv, vo, p_lse, vdo, cu, cu_kv, *grads), device, stream)
 
 
 class HeadNormRotate:
@@ -272,8 +287,10 @@ class HeadNormRotate:
             _refuse("eps must not be negative")
         self.head_dim, self.rotary_dim, self.base, self.interleaved, self.eps = head_dim, rotary_dim, float(base), bool(interleaved), float(eps)
         self.L = lib()
-        self.turns = (C.c_uint64 * max(1, rotary_dim // 2))()
+        self.turns = (c_uint64 * max(1, rotary_dim // 2))()
         _check(self.L.pm_rotation_turns(rotary_dim, self.base, self.turns))
+        self.p_turns = addressof(self.turns)
+        self.ws_bytes = self.L.pm_head_norm_rotate_workspace_bytes(_HEAD_NORM(PM_F32, 1, 1, head_dim, rotary_dim, 0, 0, 0.0, self.p_turns))
 
     def _sides(self, q, k, positions, q_gain, k_gain):
         """Device, dtype, shapes of both sides (None: absent), description, and pointers of positions and gains."""
@@ -301,26 +318,22 @@ class HeadNormRotate:
             if shape is not None and g is None:
                 _refuse(f"{name} must be a tensor")
             gains.append(None if shape is None else _flat(name, g, torch.float32, device, (d,)))
-        desc = C.byref(pm_head_norm_desc(_DTYPES[lead.dtype], Q[1] if Q else 0, K[1] if K else 0, d, self.rotary_dim, self.interleaved, tokens, self.eps,
-                                         self.turns))
+        desc = _HEAD_NORM(_DTYPES[lead.dtype], Q[1] if Q else 0, K[1] if K else 0, d, self.rotary_dim, self.interleaved, tokens, self.eps, self.p_turns)
         return device, lead.dtype, Q, K, desc, at, gains
 
     def pm_head_norm_rotate(self, q, k, positions, q_gain, k_gain, q_out, k_out, stream=None):
         """Writes q_out and k_out, which may be q and k."""
         device, dtype, Q, K, desc, pos, gains = self._sides(q, k, positions, q_gain, k_gain)
-        views = _head_views((Q, K, Q, K), dtype, device, ("q", "k", "q_out", "k_out"), (q, k, q_out, k_out), 2)
-        at = C.addressof(views)
-        _launch(lambda st: self.L.pm_head_norm_rotate(desc, at, at + _VIEW, pos, *gains, at + 2 * _VIEW, at + 3 * _VIEW, st), device, stream)
+        vq, vk, *outs = _head_views((Q, K, Q, K), dtype, device, ("q", "k", "q_out", "k_out"), (q, k, q_out, k_out), 2)
+        _launch(self.L.pm_head_norm_rotate, (desc, vq, vk, pos, *gains, *outs), device, stream)
 
     def pm_head_norm_rotate_backward(self, q, k, positions, q_gain, k_gain, d_q_out, d_k_out, dq, dk, d_q_gain=None, d_k_gain=None, stream=None):
         """Writes dq and dk (which may be d_q_out and d_k_out) and the gains' gradients that are given."""
         device, dtype, Q, K, desc, pos, gains = self._sides(q, k, positions, q_gain, k_gain)
-        views = _head_views((Q, K, Q, K, Q, K), dtype, device, ("q", "k", "d_q_out", "d_k_out", "dq", "dk"), (q, k, d_q_out, d_k_out, dq, dk), 4)
-        grads = [_flat(n, g, torch.float32, device, (self.head_dim,)) for n, g in (("d_q_gain", d_q_gain), ("d_k_gain", d_k_gain))]
-        at = C.addressof(views)
-        need = self.L.pm_head_norm_rotate_workspace_bytes(desc) if grads != [None, None] else 0
-        _launch(lambda st, ws=None: self.L.pm_head_norm_rotate_backward(
-            desc, at, at + _VIEW, pos, *gains, at + 2 * _VIEW, at + 3 * _VIEW, at + 4 * _VIEW, at + 5 * _VIEW, *grads, ws, need, st), device, stream, need)
+        vq, vk, *views = _head_views((Q, K, Q, K, Q, K), dtype, device, ("q", "k", "d_q_out", "d_k_out", "dq", "dk"), (q, k, d_q_out, d_k_out, dq, dk), 4)
+        grads = _flats(("d_q_gain", "d_k_gain"), (d_q_gain, d_k_gain), torch.float32, device, (self.head_dim,))
+        _launch_with(0 if d_q_gain is None and d_k_gain is None else self.ws_bytes, self.L.pm_head_norm_rotate_backward,
+                     (desc, vq, vk, pos, *gains, *views, *grads), device, stream)
 
 
 class Dropout:
@@ -347,7 +360,7 @@ class Dropout:
     def _tensors(self, names, tensors, rng):
         lead = tensors[0]
         device = _compute_device(names[0], lead)
-        pointers = [_flat(n, t, lead.dtype, device, lead.shape) for n, t in zip(names, tensors)]
+        pointers = _flats(names, tensors, lead.dtype, device, lead.shape)
         if rng is None:
             _refuse("rng must be a tensor")
         return device, _DTYPES[lead.dtype], lead.numel(), pointers, _flat("rng", rng, torch.int64, device, (2,))
@@ -357,14 +370,14 @@ class Dropout:
         device, dtype, n, (p_x, p_y, p_res), p_rng = self._tensors(("x", "y", "residual"), (x, y, residual), rng)
         if y is None:
             _refuse("y must be a tensor")
-        _launch(lambda st: self.L.pm_dropout(p_x, p_res, dtype, n, self.p, p_rng, p_y, st), device, stream)
+        _launch(self.L.pm_dropout, (p_x, p_res, dtype, n, self.p, p_rng, p_y), device, stream)
 
     def pm_dropout_backward(self, d_y, rng, d_x, stream=None):
         """Writes d_x (which may be d_y); the residual's gradient is d_y itself."""
         device, dtype, n, (p_y, p_x), p_rng = self._tensors(("d_y", "d_x"), (d_y, d_x), rng)
         if d_x is None:
             _refuse("d_x must be a tensor")
-        _launch(lambda st: self.L.pm_dropout_backward(p_y, dtype, n, self.p, p_rng, p_x, st), device, stream)
+        _launch(self.L.pm_dropout_backward, (p_y, dtype, n, self.p, p_rng, p_x), device, stream)
 
 
 class TokenLogProbs:
@@ -407,7 +420,7 @@ class TokenLogProbs:
         args = (logits.data_ptr(), _DTYPES[logits.dtype], n, self.vocab, stride, _flat("targets", targets, i32, device, (n,)),
                 _flat("logprob", logprob, f32, device, (n,)), _flat("entropy", entropy, f32, device, (n,)), _flat("lse", lse, f32, device, (n,)),
                 k, _flat("top_logprob", top_logprob, f32, device, (n, k)), _flat("top_ids", top_ids, i32, device, (n, k)))
-        _launch(lambda st: self.L.pm_token_logprobs(*args, st), device, stream)
+        _launch(self.L.pm_token_logprobs, args, device, stream)
 
     def pm_token_logprobs_backward(self, logits, targets, lse, d_logits, d_logprob=None, entropy=None, d_entropy=None, stream=None):
         """Writes d_logits (logits itself is allowed) from the gradients of logprob and / or of the entropy."""
@@ -422,7 +435,7 @@ class TokenLogProbs:
                 _flat("lse", lse, f32, device, (n,)), _flat("entropy", entropy, f32, device, (n,)),
                 _flat("d_logprob", d_logprob, f32, device, (n,)), _flat("d_entropy", d_entropy, f32, device, (n,)),
                 d_logits.data_ptr(), grad_stride)
-        _launch(lambda st: self.L.pm_token_logprobs_backward(*args, st), device, stream)
+        _launch(self.L.pm_token_logprobs_backward, args, device, stream)
 
 
 class PolicyLoss:
@@ -444,7 +457,7 @@ class PolicyLoss:
         if not (math.isfinite(kl_coef) and math.isfinite(entropy_coef)):
             _refuse("coefficients must be finite")
         self.kl_coef, self.entropy_coef = kl_coef, entropy_coef
-        self.desc = pm_policy_desc(clip_low, clip_high, kl_coef, entropy_coef, bool(mean))
+        self.desc = byref(pm_policy_desc(clip_low, clip_high, kl_coef, entropy_coef, bool(mean)))
         self.L = lib()
 
     def pm_policy_loss(self, logprob, old_logprob, advantage, stats, d_logprob=None, ref_logprob=None, entropy=None, d_entropy=None, weight=None,
@@ -457,11 +470,10 @@ class PolicyLoss:
             _refuse("old_logprob, advantage and stats must be tensors")
         if self.kl_coef and ref_logprob is None or self.entropy_coef and entropy is None:
             _refuse("kl_coef without ref_logprob" if self.kl_coef and ref_logprob is None else "entropy_coef without entropy")
-        names = ("logprob", "old_logprob", "advantage", "ref_logprob", "entropy", "weight")
-        ins = [_flat(name, t, f32, device, (n,)) for name, t in zip(names, (logprob, old_logprob, advantage, ref_logprob, entropy, weight))]
-        outs = [_flat("stats", stats, f32, device, (5,)), _flat("d_logprob", d_logprob, f32, device, (n,)), _flat("d_entropy", d_entropy, f32, device, (n,))]
-        need = self.L.pm_policy_loss_workspace_bytes(n)
-        _launch(lambda st, ws=None: self.L.pm_policy_loss(C.byref(self.desc), n, *ins, *outs, ws, need, st), device, stream, need)
+        *ins, p_lp, p_ent = _flats(("logprob", "old_logprob", "advantage", "ref_logprob", "entropy", "weight", "d_logprob", "d_entropy"),
+                                   (logprob, old_logprob, advantage, ref_logprob, entropy, weight, d_logprob, d_entropy), f32, device, (n,))
+        _launch_with(self.L.pm_policy_loss_workspace_bytes(n), self.L.pm_policy_loss,
+                     (self.desc, n, *ins, _flat("stats", stats, f32, device, (5,)), p_lp, p_ent), device, stream)
 
 
 class GradClip:
@@ -530,5 +542,4 @@ class GradClip:
         i, j = bisect_left(self.starts, p_norm + 4), bisect_left(self.starts, p_scale + 4)     # the spans that start in front of their ends
         if i and self.stops[i - 1] > p_norm or j and self.stops[j - 1] > p_scale:
             _refuse(f"{'norm' if i and self.stops[i - 1] > p_norm else 'scale'} lies in one of the tensors")
-        _launch(lambda st, ws: self.L.pm_clip_gradients(self.tensors, len(self.tensors), max_norm, p_norm, p_scale, ws, self.ws_bytes, st),
-                self.device, stream, self.ws_bytes)
+        _launch_with(self.ws_bytes, self.L.pm_clip_gradients, (self.tensors, len(self.tensors), max_norm, p_norm, p_scale), self.device, stream)
