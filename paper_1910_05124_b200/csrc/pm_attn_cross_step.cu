@@ -290,9 +290,9 @@ __global__ void __launch_bounds__(StepShape<DT, TEAM>::kWarps * 32, StepShape<DT
   extern __shared__ __align__(128) uint8_t step_smem[];
   const int parts = TEAM == 1 ? 1 : (int)cg::this_cluster().num_blocks(), part = TEAM == 1 ? 0 : (int)cg::this_cluster().block_rank();
   const int team = threadIdx.x / (TEAM * 32), unit = blockIdx.x / parts * S::kTeams + team, hk = unit % a.kv_heads;
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, unit / a.kv_heads, log_tokens);
+  SeqTile ks;
+  const SeqTile s = find_pair(a.cu, a.cu_kv, a.n_seqs, a.tokens, a.kv_tokens, unit / a.kv_heads, log_tokens, ks);
   if (s.tile < 0) return;
-  const SeqTile ks = other_side(true, s, a.cu_kv, a.kv_tokens);
   const int token0 = s.tile << log_tokens, rows = min(s.len - token0, 1 << log_tokens) * a.group;
   if (ks.len == 0) {                              // no keys: zeros
     if (part == 0)

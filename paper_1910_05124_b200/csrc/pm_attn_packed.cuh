@@ -32,12 +32,17 @@ struct SeqTile {
 };
 
 // The index-th tile of up to 32 PER sequences, PER consecutive ones to a lane: tiles counted through the sequences.
+// With `other` the starts of the other side are loaded in the same round, and *there becomes its rows.
 template <int PER>
-__device__ __forceinline__ SeqTile find_counted(const int32_t* cu, int n_seqs, int tokens, int index, int log_rows) {
+__device__ __forceinline__ SeqTile find_counted(const int32_t* cu, int n_seqs, int tokens, int index, int log_rows, const int32_t* other = nullptr,
+                                                int other_tokens = 0, SeqTile* there = nullptr) {
   const int lane = threadIdx.x & 31;
-  int start[PER + 1], tiles[PER], mine = 0;
+  int start[PER + 1], far[PER + 1], tiles[PER], mine = 0;
 #pragma unroll
-  for (int i = 0; i <= PER; ++i) start[i] = min(max(cu[min(lane * PER + i, n_seqs)], 0), tokens);
+  for (int i = 0; i <= PER; ++i) {
+    start[i] = min(max(cu[min(lane * PER + i, n_seqs)], 0), tokens);
+    if (other) far[i] = min(max(other[min(lane * PER + i, n_seqs)], 0), other_tokens);
+  }
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     tiles[i] = max(start[i + 1] - start[i] + (1 << log_rows) - 1, 0) >> log_rows;
@@ -49,13 +54,21 @@ __device__ __forceinline__ SeqTile find_counted(const int32_t* cu, int n_seqs, i
   int at = upto - mine;
   const unsigned has = __ballot_sync(0xffffffffu, index >= at && index < at + mine);
   if (!has) return SeqTile{0, 0, -1, 0};
-  int tile = 0, len = 0, begin = 0, seq = 0;
+  int tile = 0, len = 0, begin = 0, seq = 0, far_begin = 0, far_end = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    if (index >= at && index < at + tiles[i]) { tile = index - at; begin = start[i]; len = start[i + 1] - start[i]; seq = lane * PER + i; }
+    if (index >= at && index < at + tiles[i]) {
+      tile = index - at; begin = start[i]; len = start[i + 1] - start[i]; seq = lane * PER + i;
+      if (other) { far_begin = far[i]; far_end = far[i + 1]; }
+    }
     at += tiles[i];
   }
   const int who = __ffs(has) - 1;
+  if (other) {
+    far_begin = __shfl_sync(0xffffffffu, far_begin, who);
+    far_end = __shfl_sync(0xffffffffu, far_end, who);
+    *there = SeqTile{far_begin, max(far_end - far_begin, 0), 0, 0};
+  }
   return SeqTile{__shfl_sync(0xffffffffu, begin, who), __shfl_sync(0xffffffffu, len, who), __shfl_sync(0xffffffffu, tile, who),
                  __shfl_sync(0xffffffffu, seq, who)};
 }
@@ -101,6 +114,15 @@ __device__ __forceinline__ SeqTile other_side(bool cross, const SeqTile& s, cons
   if (!cross) return s;
   const int begin = min(max(cu[s.seq], 0), (int)tokens), end = min(max(cu[s.seq + 1], 0), (int)tokens);
   return SeqTile{begin, max(end - begin, 0), 0, s.seq};
+}
+// find_tile and other_side of cross attention in one round of loads, where the sequences are counted
+__device__ __forceinline__ SeqTile find_pair(const int32_t* cu, const int32_t* cu_other, int n_seqs, int64_t tokens, int64_t other_tokens, int index, int log_rows,
+                                             SeqTile& there) {
+  if (n_seqs <= 32) return find_counted<1>(cu, n_seqs, (int)tokens, index, log_rows, cu_other, (int)other_tokens, &there);
+  if (n_seqs <= 256) return find_counted<8>(cu, n_seqs, (int)tokens, index, log_rows, cu_other, (int)other_tokens, &there);
+  const SeqTile s = find_slot(cu, n_seqs, (int)tokens, index, log_rows);
+  if (s.tile >= 0) there = other_side(true, s, cu_other, other_tokens);
+  return s;
 }
 
 // tiles of `rows` rows that sequences of `tokens` tokens in all can have at most, and their slots

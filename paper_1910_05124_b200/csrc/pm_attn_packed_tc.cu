@@ -226,13 +226,15 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
   const int log_rows = pair_heads ? TC_LOG_ROWS : TC_LOG_ROWS + NT - 1, rows = 1 << log_rows;
   const int parts = NT == 1 ? (int)cg::this_cluster().num_blocks() : 1, part = NT == 1 ? (int)cg::this_cluster().block_rank() : 0;
   const int block = blockIdx.x / parts, unit = block % units;
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / units, log_rows);
+  SeqTile ks;
+  SeqTile s;
+  if constexpr (X) s = find_pair(a.cu, a.cu_kv, a.n_seqs, a.tokens, a.kv_tokens, block / units, log_rows, ks);
+  else ks = s = find_tile(a.cu, a.n_seqs, a.tokens, block / units, log_rows);
   if (s.tile < 0) {
     __syncthreads();
     if (warp == kIssue) tmem_dealloc(*tmem_slot, S::kCols);
     return;
   }
-  const SeqTile ks = other_side(X, s, a.cu_kv, a.kv_tokens);
   // the last tiles of a sequence see the most keys: they come first
   const int tile = ((s.len + rows - 1) >> log_rows) - 1 - s.tile;
   auto head_of = [&](int t) { return pair_heads ? unit * 2 + t : unit; };
@@ -663,14 +665,16 @@ template <int DT, bool X> __device__ __forceinline__ void dkv_block(const Packed
     tmem_alloc(smem_u32(tmem_slot), S::kTmem);
     tmem_relinquish();
   }
-  const SeqTile s = find_tile(a.cu_kv, a.n_seqs, a.kv_tokens, block / a.kv_heads, TC_LOG_ROWS);
+  SeqTile qs;
+  SeqTile s;
+  if constexpr (X) s = find_pair(a.cu_kv, a.cu, a.n_seqs, a.kv_tokens, a.tokens, block / a.kv_heads, TC_LOG_ROWS, qs);
+  else qs = s = find_tile(a.cu_kv, a.n_seqs, a.kv_tokens, block / a.kv_heads, TC_LOG_ROWS);
   if (s.tile < 0) {
     __syncthreads();
     if (warp == kIssue) tmem_dealloc(*tmem_slot, S::kTmem);
     pdl_wait();
     return;
   }
-  const SeqTile qs = other_side(X, s, a.cu, a.tokens);
   const int k0 = s.tile * TC_ROWS, first = !X && a.causal ? k0 : 0;
   // of the query tiles of all heads that share these keys, this block's share
   const int per_head = (qs.len - first + BN - 1) / BN, it0 = per_head * a.group * part / parts, n_it = per_head * a.group * (part + 1) / parts - it0;
@@ -914,14 +918,16 @@ template <int DT, bool X> __device__ __forceinline__ void dq_block(const PackedA
     tmem_alloc(smem_u32(tmem_slot), S::kTmem);
     tmem_relinquish();
   }
-  const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.heads, TC_LOG_ROWS);
+  SeqTile ks;
+  SeqTile s;
+  if constexpr (X) s = find_pair(a.cu, a.cu_kv, a.n_seqs, a.tokens, a.kv_tokens, block / a.heads, TC_LOG_ROWS, ks);
+  else ks = s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.heads, TC_LOG_ROWS);
   if (s.tile < 0) {
     __syncthreads();
     if (warp == kIssue) tmem_dealloc(*tmem_slot, S::kTmem);
     pdl_wait();
     return;
   }
-  const SeqTile ks = other_side(X, s, a.cu_kv, a.kv_tokens);
   const int tile = (s.len + TC_ROWS - 1) / TC_ROWS - 1 - s.tile;                 // the tiles that see the most keys first
   const int q0 = tile * TC_ROWS, all = ((!X && a.causal ? min(s.len, q0 + TC_ROWS) : ks.len) + BN - 1) / BN;
   const int it0 = all * part / parts, n_it = all * (part + 1) / parts - it0;     // of the key tiles, this block's share

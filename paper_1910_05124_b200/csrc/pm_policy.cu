@@ -23,7 +23,7 @@ constexpr int kPolicySums = 5;                    // of the weights, policy, kl,
 constexpr int kPolicyThreads = 512, kPolicyHeld = 4, kPolicyCluster = 8;         // short lists: tokens to a thread, blocks
 constexpr int64_t kPolicyShort = (int64_t)kPolicyThreads * kPolicyHeld * kPolicyCluster;
 // Long lists: blocks of the launch that adds the weights; threads, consecutive tokens to a thread and most blocks of the one that does the rest.
-constexpr int kWeightBlocks = kSms, kPolicyLong = 256, kPolicyRun = 4, kPolicyBlocks = 4096;
+constexpr int kWeightBlocks = kSms, kPolicyLong = 256, kPolicyRun = 4, kPolicyBlocks = 4 * kSms;
 
 struct PolicyArgs {
   const float *logprob, *old_logprob, *advantage, *ref_logprob, *entropy, *weight;
@@ -72,23 +72,20 @@ struct PolicyToken {
     if (clipped) sums[4] += w;
     if (a.ref_logprob) {
       const float d = ref - lp;
-      // e^d - 1 - d loses its bits for small d: there its series d^2 (1/2 + d/6 + ...), the next term below 2^-28 of the sum
-      float kl;
-      if (fabsf(d) < 0.5f) {
-        float s = 1.f / 362880.f;
-        s = fmaf(s, d, 1.f / 40320.f);
-        s = fmaf(s, d, 1.f / 5040.f);
-        s = fmaf(s, d, 1.f / 720.f);
-        s = fmaf(s, d, 1.f / 120.f);
-        s = fmaf(s, d, 1.f / 24.f);
-        s = fmaf(s, d, 1.f / 6.f);
-        s = fmaf(s, d, 0.5f);
-        kl = d * d * s;
-      } else {
-        kl = expm1f(d) - d;
-      }
+      // e^d - 1 and e^d - 1 - d.  The second loses its bits for small d: there its series d^2 (1/2 + d/6 + ...), the next term below 2^-28 of
+      // the sum; from 1/2 on the exponential's own error is at most two and a half times as large in either.
+      float s = 1.f / 362880.f;
+      s = fmaf(s, d, 1.f / 40320.f);
+      s = fmaf(s, d, 1.f / 5040.f);
+      s = fmaf(s, d, 1.f / 720.f);
+      s = fmaf(s, d, 1.f / 120.f);
+      s = fmaf(s, d, 1.f / 24.f);
+      s = fmaf(s, d, 1.f / 6.f);
+      s = fmaf(s, d, 0.5f);
+      const bool near = fabsf(d) < 0.5f;
+      const float far = expf(d) - 1.f, kl = near ? d * d * s : far - d, slope = near ? d + kl : far;
       sums[2] += (double)w * kl;
-      grad -= (float)a.kl_coef * expm1f(d);
+      grad -= (float)a.kl_coef * slope;
     }
     if (a.entropy) sums[3] += (double)w * ent;
     return grad;
