@@ -125,6 +125,28 @@ __device__ __forceinline__ SeqTile find_pair(const int32_t* cu, const int32_t* c
   return s;
 }
 
+// find_pair with the tiles of the sequence that has the longest other side first, where a warp holds all sequences.
+__device__ __forceinline__ SeqTile find_longest(const int32_t* cu, const int32_t* cu_other, int n_seqs, int64_t tokens, int64_t other_tokens, int index, int log_rows,
+                                                SeqTile& there) {
+  if (n_seqs > 32) return find_pair(cu, cu_other, n_seqs, tokens, other_tokens, index, log_rows, there);
+  const int lane = threadIdx.x & 31;
+  auto start = [&](const int32_t* c, int64_t most, int b) { return min(max(c[min(b, n_seqs)], 0), (int)most); };
+  const int begin = start(cu, tokens, lane), far = start(cu_other, other_tokens, lane);
+  const int len = max(start(cu, tokens, lane + 1) - begin, 0), far_len = max(start(cu_other, other_tokens, lane + 1) - far, 0);
+  const int tiles = (len + (1 << log_rows) - 1) >> log_rows;
+  int at = 0;                                     // tiles of the sequences before this one
+#pragma unroll 8
+  for (int j = 0; j < 32; ++j) {
+    const int n = __shfl_sync(0xffffffffu, tiles, j), f = __shfl_sync(0xffffffffu, far_len, j);
+    if (f > far_len || (f == far_len && j < lane)) at += n;
+  }
+  const unsigned has = __ballot_sync(0xffffffffu, index >= at && index < at + tiles);
+  if (!has) return SeqTile{0, 0, -1, 0};
+  const int who = __ffs(has) - 1;
+  there = SeqTile{__shfl_sync(0xffffffffu, far, who), __shfl_sync(0xffffffffu, far_len, who), 0, 0};
+  return SeqTile{__shfl_sync(0xffffffffu, begin, who), __shfl_sync(0xffffffffu, len, who), __shfl_sync(0xffffffffu, index - at, who), who};
+}
+
 // tiles of `rows` rows that sequences of `tokens` tokens in all can have at most, and their slots
 inline int64_t most_tiles(int64_t tokens, int n_seqs, int rows) { return tokens / rows + n_seqs; }
 

@@ -560,6 +560,328 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
   }
 }
 
+// ---- forward, cross attention of heads of up to 64, more tiles than blocks run at a time -----------------------------
+//
+// The same work by blocks that stay: a block takes query tiles in turn, and the copies and products of the next tile run while the
+// softmax warps bring the last one's rows out; in short sequences the ends of a tile (its place, the first copies, the barriers between
+// the first products and the last rows) are most of its time.  16 x 256 tokens over 100 to 475 keys, 16 heads of 64: 20.1 us with a block to
+// a tile, 17.1 with these; 100 x 100 over 300, 64 and 46; 4096 over 8192, 211 and 204.
+//
+// Key tiles are counted through all tiles of a block: g-th of all, in stage g mod 2, its barriers' phases by g.  The places of a block's
+// tiles, 32 at most, are found at the start by all its warps.
+
+struct StreamTile {
+  int64_t row, key;                               // first rows of the sequence, in q and o and in k and v
+  int len, q0, head, n_keys, key_len;             // rows of the sequence, the tile's first; key tiles and keys; -1 key tiles: no such tile
+};
+struct StreamShape {
+  static constexpr int kTile = TC_SUB;            // [128 x 64]
+  static constexpr int kStages = 2, kMost = 32;
+  static constexpr int kCols = 256;               // S 128, O 64, P 64
+  static constexpr int kThreads = 256;
+  static constexpr int kStaging = 4 * 2048;
+  static constexpr int kBars = 2 + 2 + 4 * kStages + 6;
+  static constexpr int kSmem = 2 * kTile + 2 * kStages * kTile + kStaging + 1024 + kBars * 8 + kMost * (int)sizeof(StreamTile) + 16;
+  static constexpr int kSoftmaxRegs = 208, kOtherRegs = 48;          // of 256 x 128 that are launched
+};
+
+// the block's i-th unit: forth through one round of blocks, back through the next, so that longer tiles and shorter ones behind them even out
+__device__ __forceinline__ int64_t stream_unit(int i) { return (int64_t)i * gridDim.x + (i & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x); }
+
+__global__ void __launch_bounds__(StreamShape::kThreads, 2)
+attn_cross_stream_kernel(const __grid_constant__ PackedArgs a, const __grid_constant__ TcMaps maps, int units) {
+  using S = StreamShape;
+  constexpr int DT = 64, kCopy = 4, kIssue = 5;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  uint8_t* const sptr = smem_raw + (base - raw);
+  const uint32_t sQ = base, sK = sQ + 2 * S::kTile, sV = sK + S::kStages * S::kTile, staging = sV + S::kStages * S::kTile, bars = staging + S::kStaging;
+  auto q_full = [&](int i) { return bars + 8 * i; };
+  auto q_empty = [&](int i) { return bars + 8 * (2 + i); };
+  auto k_full = [&](int i) { return bars + 8 * (4 + i); };
+  auto k_empty = [&](int i) { return bars + 8 * (6 + i); };
+  auto v_full = [&](int i) { return bars + 8 * (8 + i); };
+  auto v_empty = [&](int i) { return bars + 8 * (10 + i); };
+  const uint32_t s_full = bars + 8 * 12, s_read = s_full + 8, p_half = s_full + 16, p_full = s_full + 24, o_full = s_full + 32, o_read = s_full + 40;
+  static_assert(S::kBars == 18);
+  StreamTile* const tiles = reinterpret_cast<StreamTile*>(sptr + (bars - base) + 8 * S::kBars);
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(tiles + S::kMost);
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* const status = &g_attn_packed_status;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (warp == kCopy && lane == 0) {
+    for (int i = 0; i < 2; ++i) { mbar_init(q_full(i), 1); mbar_init(q_empty(i), 1); mbar_init(k_full(i), 1); mbar_init(k_empty(i), 1); mbar_init(v_full(i), 1); mbar_init(v_empty(i), 1); }
+    mbar_init(s_full, 1); mbar_init(s_read, 4); mbar_init(p_half, 4); mbar_init(p_full, 4); mbar_init(o_full, 1); mbar_init(o_read, 4);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    tma_prefetch_desc(&maps.q);
+    tma_prefetch_desc(&maps.k);
+    tma_prefetch_desc(&maps.v);
+  }
+  if (warp == kIssue) {
+    tmem_alloc(smem_u32(tmem_slot), S::kCols);
+    tmem_relinquish();
+  }
+  const int64_t all = (a.tokens / TC_ROWS + a.n_seqs) * units;       // as most_tiles counts them
+  int n_tiles = 0;
+  while (n_tiles < S::kMost && stream_unit(n_tiles) < all) ++n_tiles;
+  for (int i = warp; i < n_tiles; i += S::kThreads / 32) {
+    const int64_t unit = stream_unit(i);
+    SeqTile ks;
+    const SeqTile s = find_longest(a.cu, a.cu_kv, a.n_seqs, a.tokens, a.kv_tokens, (int)(unit / units), TC_LOG_ROWS, ks);
+    if (lane == 0)
+      tiles[i] = s.tile < 0 ? StreamTile{0, 0, 0, 0, 0, -1, 0}
+                            : StreamTile{s.begin, ks.begin, s.len, s.tile * TC_ROWS, (int)(unit % units), (ks.len + TC_ROWS - 1) / TC_ROWS, ks.len};
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot, col_s = tmem, col_o = tmem + 128, col_p = tmem + 192;
+
+  if (warp >= 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kOtherRegs));
+    if (warp == kCopy) {                          // ---- places and copies
+      int r = 0, g = 0;                           // tiles with keys, key tiles
+      bool ok = true;
+      for (int i = 0; i < n_tiles && ok; ++i) {
+        const int n_keys = tiles[i].n_keys, hk = tiles[i].head / a.group;
+        const int64_t key = tiles[i].key;
+        if (n_keys <= 0) continue;
+        if (r >= 2) ok = wait_for(q_empty(r & 1), (r / 2 - 1) & 1, abort_flag, status, 131);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        if (elect_one()) {
+          mbar_arrive_expect_tx(q_full(r & 1), S::kTile);
+          load_tile<DT>(sQ + (r & 1) * S::kTile, &maps.q, q_full(r & 1), tiles[i].head, tiles[i].row + tiles[i].q0);
+        }
+        __syncwarp();
+        ++r;
+        for (int j = 0; j < n_keys; ++j, ++g) {
+          const int st = g & 1;
+          const uint32_t ph = (g / 2 - 1) & 1;
+          if (g >= 2) ok = wait_for(k_empty(st), ph, abort_flag, status, 132);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          if (elect_one()) { mbar_arrive_expect_tx(k_full(st), S::kTile); load_tile<DT>(sK + st * S::kTile, &maps.k, k_full(st), hk, key + j * TC_ROWS); }
+          __syncwarp();
+          if (g >= 2) ok = wait_for(v_empty(st), ph, abort_flag, status, 133);
+          ok = __all_sync(0xffffffffu, ok);
+          if (elect_one()) {                      // armed even when the wait ran out: as many values as keys have to be waited for
+            mbar_arrive_expect_tx(v_full(st), ok ? S::kTile : 0);
+            if (ok) load_tile<DT>(sV + st * S::kTile, &maps.v, v_full(st), hk, key + j * TC_ROWS);
+          }
+          __syncwarp();
+          if (!ok) { ++g; break; }
+        }
+      }
+      if (*abort_flag) {                          // nothing may be in flight when the block ends
+        volatile int never = 0;
+        for (int i = max(0, r - 2); i < r; ++i) wait_for(q_full(i & 1), (i / 2) & 1, &never, status, 134);
+        for (int i = max(0, g - 2); i < g; ++i) {
+          wait_for(k_full(i & 1), (i / 2) & 1, &never, status, 134);
+          wait_for(v_full(i & 1), (i / 2) & 1, &never, status, 134);
+        }
+      }
+    } else if (warp == kIssue) {                  // ---- products
+      const uint32_t id_s = make_idesc_mn(128, 128, 0, 0);
+      int n = 0, left = 0;                        // tiles so far; key tiles of the last of them without scores
+      int r = -1, g_s = 0;                        // its number among those with keys; key tiles with scores
+      // S of the next key tile of all, if there is one
+      auto scores = [&](bool& any) {
+        any = false;
+        while (left == 0) {
+          if (n == n_tiles) return true;
+          left = max(tiles[n++].n_keys, 0);
+          if (left == 0) continue;
+          ++r;
+          if (!wait_for(q_full(r & 1), (r / 2) & 1, abort_flag, status, 136)) return false;
+        }
+        if (!wait_for(k_full(g_s & 1), (g_s / 2) & 1, abort_flag, status, 137)) return false;
+        if (g_s > 0 && !wait_for(s_read, (g_s - 1) & 1, abort_flag, status, 138)) return false;
+        tc_fence_after();
+        if (elect_one()) {
+          mma_abt<DT>(col_s, sQ + (r & 1) * S::kTile, sK + (g_s & 1) * S::kTile, id_s);
+          tc_commit(s_full);
+          tc_commit(k_empty(g_s & 1));
+          if (left == 1) tc_commit(q_empty(r & 1));
+        }
+        __syncwarp();
+        --left;
+        ++g_s;
+        any = true;
+        return true;
+      };
+      const uint32_t id_o = make_idesc_mn(128, DT, 0, 1);
+      bool more;
+      bool ok = scores(more);
+      int first = 0, tile = 0;                    // key tiles before this tile's first; tiles whose values have begun
+      int next_first = ok && more ? left + 1 : 0; // key tiles up to the end of the tile with the last scores
+      for (int g = 0; ok && more; ++g) {
+        const int end = next_first;               // of the tile that g belongs to, as its scores were the last
+        ok = scores(more);
+        if (!ok) break;
+        if (more && g + 1 == end) next_first = end + left + 1;
+        const uint32_t v = sV + (g & 1) * S::kTile;
+        ok = wait_for(v_full(g & 1), (g / 2) & 1, abort_flag, status, 139) && wait_for(p_half, g & 1, abort_flag, status, 140);
+        if (ok && g == first && tile > 0) ok = wait_for(o_read, (tile - 1) & 1, abort_flag, status, 141);      // the last tile's rows have left O
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) mma_ab<DT>(col_o, col_p, v, id_o, g > first, 0);
+        __syncwarp();
+        ok = wait_for(p_full, g & 1, abort_flag, status, 142);
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) {
+          mma_ab<DT>(col_o, col_p, v, id_o, true, 1);
+          tc_commit(o_full);
+          tc_commit(v_empty(g & 1));
+        }
+        __syncwarp();
+        if (g + 1 == end) { first = end; ++tile; }
+      }
+    }
+  } else {                                        // ---- softmax: thread = row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kSoftmaxRegs));
+    const int row_in = threadIdx.x & 127;
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16, ts = col_s + lanes, to = col_o + lanes, tp = col_p + lanes;
+    const float c = a.scale * kLog2e;
+    int g = 0, n = 0;                             // key tiles, tiles
+    bool ok = true;
+    for (; n < n_tiles; ++n) {
+      const StreamTile& t = tiles[n];
+      const int n_keys = t.n_keys;
+      if (n_keys < 0) continue;
+      if (n_keys == 0) {                          // no keys: zeros
+        const int row = t.q0 + row_in;
+        if (row < t.len) {
+          uint4* const out = reinterpret_cast<uint4*>(head_row_out<__nv_bfloat16>(a.o, t.row + row, t.head));
+          for (int i = 0; i < a.dim / 8; ++i) out[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (a.lse) a.lse[(int64_t)t.head * a.tokens + t.row + row] = -INFINITY;
+        }
+        continue;
+      }
+      float m = -INFINITY, l = 0.f;               // m: the maximum in use, times c
+      for (int j = 0; j < n_keys; ++j, ++g) {
+        ok = wait_for(s_full, g & 1, abort_flag, status, 144);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        const int valid = t.key_len - j * TC_ROWS;
+        if (valid < TC_ROWS) {                    // rows behind the last key: zeros, as p is there
+          ok = wait_for(v_full(g & 1), (g / 2) & 1, abort_flag, status, 145);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          for (int i = valid * 8 + row_in; i < TC_ROWS * 8; i += 128)
+            *reinterpret_cast<uint4*>(sptr + (sV - base) + (g & 1) * S::kTile + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+          fence_async_smem();
+        }
+        uint32_t v[4][32];
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_ld32(ts + q * 32, v[q]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_ld_wait(v[q]);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(s_read);
+        if (valid < TC_ROWS) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (q * 32 + i >= valid) v[q][i] = 0xFF800000u;
+        }
+#pragma unroll
+        for (int i = 0; i < 32; i += 2)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) mx[q] = max3_nan(mx[q], __uint_as_float(v[q][i]), __uint_as_float(v[q][i + 1]));
+        // a NaN or +infinity among the scores: no distribution; the maximum says so to every exponential of the row
+        float top = max3_nan(mx[0], mx[1], max_nan(mx[2], mx[3])) * c;
+        if (top == INFINITY) top = NAN;
+        if (j > 0) {                              // P's columns are free, and O holds the tiles before this one
+          ok = wait_for(o_full, (g - 1) & 1, abort_flag, status, 146);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+        }
+        if (j == 0) {
+          m = top;
+        } else if (__any_sync(0xffffffffu, !(top <= m + 8.f))) {
+          const float up = top <= m + 8.f ? m : max_nan(m, top), f = up == -INFINITY ? 1.f : ex2(m - up);
+          m = up;
+          l *= f;
+#pragma unroll
+          for (int q = 0; q < DT / 16; ++q) {
+            uint32_t o[16];
+            tmem_ld16(to + q * 16, o);
+            tmem_ld_wait(o);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_st16(to + q * 16, o);
+          }
+        }
+        float2 sum = make_float2(0.f, 0.f);
+        const float shift = m == -INFINITY ? 0.f : -m;       // no finite score so far: nothing but zeros
+        const float2 cc = make_float2(c, c), mm = make_float2(shift, shift);
+        auto probabilities = [&](const uint32_t (&x)[32], int q) {
+          uint32_t p[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float2 e = fma_f32x2(make_float2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), cc, mm);
+            if (FWD_FMA >> i & 1) e = ex2_fma(e);
+            else { e.x = ex2(e.x); e.y = ex2(e.y); }
+            sum = add_f32x2(sum, e);
+            p[i] = pack_bf16(e.x, e.y);
+          }
+          tmem_st16(tp + q * 16, p);
+        };
+        probabilities(v[0], 0);
+        probabilities(v[1], 1);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_half);
+        probabilities(v[2], 2);
+        probabilities(v[3], 3);
+        l += sum.x + sum.y;
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full);
+      }
+      if (ok) ok = wait_for(o_full, (g - 1) & 1, abort_flag, status, 147);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      const int row = t.q0 + row_in, first_row = t.q0 + warp * 32, h = t.head;
+      if (a.lse && row < t.len) a.lse[(int64_t)h * a.tokens + t.row + row] = (m + log2f(l)) * kLn2;
+      const float inv = 1.f / l;
+#pragma unroll
+      for (int q = 0; q < DT / 32; ++q)
+        store_rows(head_row_out<__nv_bfloat16>(a.o, t.row + first_row, h), a.o.token, t.len - first_row, to, q * 32, a.dim, inv, true,
+                   sptr + (staging - base) + warp * 2048);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(o_read);
+    }
+    for (; n < n_tiles; ++n) {                    // where a wait ran out, the rows that are left: NaN
+      const StreamTile& t = tiles[n];
+      const int row = t.q0 + row_in;
+      if (t.n_keys < 0 || row >= t.len) continue;
+      uint4* const out = reinterpret_cast<uint4*>(head_row_out<__nv_bfloat16>(a.o, t.row + row, t.head));
+      for (int q = 0; q < a.dim / 8; ++q) out[q] = make_uint4(0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u);
+      if (a.lse) a.lse[(int64_t)t.head * a.tokens + t.row + row] = NAN;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kIssue) {
+    tc_fence_after();
+    tmem_dealloc(tmem, S::kCols);
+  }
+}
+
 // ---- backward ---------------------------------------------------------------------------------------------------
 //
 // Two kinds of blocks, as on the CUDA cores: one owns 128 key rows (dk, dv), one 128 query rows (dq); every gradient is summed by one
@@ -1219,7 +1541,23 @@ template <int DT, int NT, bool X> static cudaError_t fwd_launch(const PackedArgs
 
 // Two query tiles to a block read keys and values half as often and pay for heads of 128 once every SM has such a block.  8192 tokens,
 // 16 heads of 128, us with two / one: 240 / 252; 4000 tokens, 4 heads of 128: 68 / 63; 8192 tokens, 16 heads of 64: 213 / 205.
+static cudaError_t stream_launch(const PackedArgs& a, cudaStream_t st) {
+  static std::atomic<uint64_t> done{0};
+  using S = StreamShape;
+  TcMaps maps;
+  cudaError_t e = allow_smem(attn_cross_stream_kernel, S::kSmem, done);
+  if (e == cudaSuccess) e = encode_heads(&maps.q, a.q, a.dim, a.heads, a.tokens, TC_ROWS);
+  if (e == cudaSuccess) e = encode_heads(&maps.k, a.k, a.dim, a.kv_heads, a.kv_tokens, TC_ROWS);
+  if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.kv_tokens, TC_ROWS);
+  if (e != cudaSuccess) return e;
+  const int64_t all = most_tiles(a.tokens, a.n_seqs, TC_ROWS) * a.heads, blocks = std::max<int64_t>(2 * kSms, (all + S::kMost - 1) / S::kMost);
+  if (!launchable(all)) return cudaErrorInvalidConfiguration;
+  return launch_pdl(attn_cross_stream_kernel, dim3((unsigned)blocks), dim3(S::kThreads), S::kSmem, st, false, a, maps, a.heads);
+}
+
 template <bool X> static cudaError_t tc_forward(const PackedArgs& a, cudaStream_t st) {
+  // blocks that stay where there are more tiles than run at a time
+  if (X && a.dim <= 64 && most_tiles(a.tokens, a.n_seqs, TC_ROWS) * a.heads > 2 * kSms) return stream_launch(a, st);
   if (a.dim <= 64) return fwd_launch<64, 1, X>(a, st);
   const bool pair = a.group % 2 == 0;
   const int64_t blocks = most_tiles(a.tokens, a.n_seqs, pair ? TC_ROWS : 2 * TC_ROWS) * (pair ? a.heads / 2 : a.heads);

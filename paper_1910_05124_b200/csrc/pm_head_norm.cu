@@ -328,14 +328,16 @@ __global__ void __launch_bounds__(kNormThreads, BACKWARD ? 2 : 3) head_norm_kern
     out += result.head;
   }
   cp_async_wait<0>();
-  if (!BACKWARD || !p.partials) return;
-  float sums[2 * V];
+  if constexpr (BACKWARD) {
+    if (!p.partials) return;
+    float sums[2 * V];
 #pragma unroll
-  for (int e = 0; e < V; ++e) {
-    sums[e] = e & 1 ? acc.f[e / 2].y : acc.f[e / 2].x;
-    sums[V + e] = e & 1 ? acc.s[e / 2].y : acc.s[e / 2].x;
+    for (int e = 0; e < V; ++e) {
+      sums[e] = e & 1 ? acc.f[e / 2].y : acc.f[e / 2].x;
+      sums[V + e] = e & 1 ? acc.s[e / 2].y : acc.s[e / 2].x;
+    }
+    leave_gains<L>(p, blockIdx.x, sums, at.on, [&](int e) { return e < V ? at.first(e) : at.second(e - V); });
   }
-  leave_gains<L>(p, blockIdx.x, sums, at.on, [&](int e) { return e < V ? at.first(e) : at.second(e - V); });
 }
 
 // Rows of any width, alignment and pairing: a warp to a row, an element to a lane, the other of a pair through shared memory.

@@ -110,6 +110,14 @@ def test_many_sequences(cuda_device, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("lens,kv_lens,H,K,D", [
+    ([256] * 6, [100, 475, 128, 1, 257, 0], 32, 32, 64), ([130, 257, 64, 0, 300, 33], [64, 130, 300, 40, 0, 700], 64, 16, 48), ([700], [1300], 96, 2, 64),
+    ([100] * 40, [(i * 37) % 200 for i in range(40)], 8, 8, 32), ([20] * 200, [20 * (i % 7) for i in range(200)], 48, 48, 64)], ids=str)
+def test_more_tiles_than_run_at_a_time(cuda_device, lens, kv_lens, H, K, D, dtype):
+    check(*make(lens, kv_lens, H, K, D, dtype, cuda_device, first=2, tail=6, seed=D, spread=2.0), gradients=len(lens) < 100)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("lens", [[100], [1]])
 @pytest.mark.parametrize("spread,scale", [(6.0, None), (0.01, None), (1.0, 2.0)])
 def test_peaked_and_flat_scores(cuda_device, dtype, spread, scale, lens):
