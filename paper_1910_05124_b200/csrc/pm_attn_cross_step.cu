@@ -330,12 +330,12 @@ template <int DT, int TEAM> static cudaError_t step_launch(const PackedArgs& a, 
   }
   if (e != cudaSuccess) return e;
   const int64_t blocks = (units + S::kTeams - 1) / S::kTeams;
-  if (!launchable(blocks * parts)) return cudaErrorInvalidConfiguration;
   return launch_clusters(attn_cross_step_kernel<DT, TEAM>, blocks, S::kWarps * 32, S::kSmem, st, false, parts, a, log_tokens);
 }
 template <int DT> static cudaError_t step_width(const PackedArgs& a, cudaStream_t st) {
   const int log_tokens = step_log_tokens(a);
   const int64_t units = most_tiles(a.tokens, a.n_seqs, 1 << log_tokens) * a.kv_heads, average = (a.kv_tokens + a.n_seqs - 1) / a.n_seqs;
+  if (!launchable(units)) return cudaErrorInvalidConfiguration;      // parts are for launches of few
   // Many short sequences: a warp to a tile and nothing to join.  us with one / four warps to a tile: 256 tokens over 50 keys each, 16 heads
   // of 64, 16.2 / 37.1; 600 over 100, 8 heads, 29.0 / 48.0; 64 over 512, 16 heads, 25.1 / 26.4.
   if (units >= 4 * kSms && average <= 512) return step_launch<DT, 1>(a, units, 1, log_tokens, st);
