@@ -566,7 +566,8 @@ static pm_status pk_forward_call(PackedArgs& a, int dtype, const pm_head_view* q
                          pk_starts(a.cu_kv, a.n_seqs)};
   if (const pm_status s = pk_apart(written, 2, read, a.cross ? 5 : 4)) return s;
   const cudaError_t e = a.kv_tokens == 0 ? pk_clear(a.o, a.cu, a.n_seqs, a.tokens, a.heads, a.dim, a.lse, dtype, st)
-                        : attn_packed_tc_takes(a, dtype, false) ? (attn_cross_step_takes(a) ? attn_cross_step(a, st) : attn_packed_tc_forward(a, st))
+                        : attn_cross_step_takes(a, dtype) ? attn_cross_step(a, dtype, st)
+                        : attn_packed_tc_takes(a, dtype, false) ? attn_packed_tc_forward(a, st)
                         : dtype == PM_BF16 ? pk_run<__nv_bfloat16>(a, false, st) : pk_run<float>(a, false, st);
   return pk_result(e, a.cross ? "cross attention" : "packed attention");
 }

@@ -194,9 +194,9 @@ inline int packed_parts(int64_t blocks, const PackedArgs& a, int rows, int heads
 bool attn_packed_tc_takes(const PackedArgs& a, int dtype, bool backward);
 cudaError_t attn_packed_tc_forward(const PackedArgs& a, cudaStream_t st);
 cudaError_t attn_packed_tc_backward(const PackedArgs& a, cudaStream_t st);
-// the kernel of cross attention with few query rows, for what attn_packed_tc_takes (forward)
-bool attn_cross_step_takes(const PackedArgs& a);
-cudaError_t attn_cross_step(const PackedArgs& a, cudaStream_t st);
+// the kernel of cross attention with few query rows, forward
+bool attn_cross_step_takes(const PackedArgs& a, int dtype);
+cudaError_t attn_cross_step(const PackedArgs& a, int dtype, cudaStream_t st);
 // a wait of one thread that runs out after so many cycles, recorded as any other
 cudaError_t attn_packed_wait_probe(int64_t limit_cycles, cudaStream_t st);
 // the code of a device-side wait that ran out since the last call (0: none); synchronises the stream
