@@ -58,9 +58,8 @@ template <typename T> struct Eight {
 
 // VEC: every tensor starts at a 16-byte boundary.  x and y may be one tensor, so nothing is declared read-only.  The generator works while
 // the loads are under way; as many blocks as run at a time, whose threads form the round keys once.
-template <typename T, bool VEC, bool RES>
+template <typename T, bool VEC, bool RES, int U>
 __global__ void __launch_bounds__(kDropThreads, kDropBlocks<T, RES>) dropout_kernel(const T* x, const T* residual, T* y, int64_t n, const uint64_t* rng, uint32_t dropped, float scale) {
-  constexpr int U = kDropVectors;
   const uint64_t counter = rng[1];
   const RoundKeys keys(rng[0]);
   const uint32_t border = dropped << 16;
@@ -106,15 +105,17 @@ __global__ void __launch_bounds__(kDropThreads, kDropBlocks<T, RES>) dropout_ker
 template <typename T> static cudaError_t dropout_run(const void* x, const void* residual, void* y, int64_t n, const int64_t* rng, uint32_t dropped, cudaStream_t st) {
   const bool vec = aligned_to(x, 16) && aligned_to(residual, 16) && aligned_to(y, 16);
   const float scale = 65536.f / (float)(65536u - dropped);
-  auto go = [&](auto kernel, int blocks) {
-    constexpr int64_t kEach = 8 * kDropThreads * kDropVectors;
-    const int64_t all = (n + kEach - 1) / kEach;
-    return launch_pdl(kernel, dim3((unsigned)std::min<int64_t>(all, blocks * kSms)), dim3(kDropThreads), 0, st, false, static_cast<const T*>(x), static_cast<const T*>(residual),
-                      static_cast<T*>(y), n, reinterpret_cast<const uint64_t*>(rng), dropped, scale);
+  const int64_t groups = (n + 8 * kDropThreads - 1) / (8 * kDropThreads);        // blocks with one vector to a thread
+  auto go = [&](auto kernel, int64_t blocks) {
+    return launch_pdl(kernel, dim3((unsigned)blocks), dim3(kDropThreads), 0, st, false, static_cast<const T*>(x), static_cast<const T*>(residual), static_cast<T*>(y), n,
+                      reinterpret_cast<const uint64_t*>(rng), dropped, scale);
   };
   auto with = [&](auto res) {
     constexpr bool RES = decltype(res)::value;
-    return go(vec ? dropout_kernel<T, true, RES> : dropout_kernel<T, false, RES>, kDropBlocks<T, RES>);
+    constexpr int kMost = kDropBlocks<T, RES> * kSms, V = kDropVectors;
+    // tensors whose vectors all have a thread at the same time take one each
+    if (groups <= kMost) return go(vec ? dropout_kernel<T, true, RES, 1> : dropout_kernel<T, false, RES, 1>, groups);
+    return go(vec ? dropout_kernel<T, true, RES, V> : dropout_kernel<T, false, RES, V>, std::min<int64_t>((groups + V - 1) / V, kMost));
   };
   return residual ? with(std::true_type{}) : with(std::false_type{});
 }

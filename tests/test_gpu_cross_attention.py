@@ -228,6 +228,33 @@ def test_strides(cuda_device, dtype, lens, kv_lens):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("lens,kv_lens,H,K,D", [([1, 2], [300, 40], 4, 2, 64), ([100, 30], [50, 400], 4, 2, 128), ([700, 300, 0, 4], [200, 100, 5, 0], 64, 64, 64), ([60], [90], 3, 1, 33)], ids=str)
+def test_without_lse_on_another_stream(cuda_device, lens, kv_lens, H, K, D, dtype):
+    """An evaluation needs no statistics; the call goes to the stream that is given."""
+    op, q, k, v, _, cu, cu_kv = make(lens, kv_lens, H, K, D, dtype, cuda_device, seed=17)
+    want, _ = forward(op, q, k, v, cu, cu_kv)
+    o, stream = torch.zeros_like(q), torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    op.pm_attention_cross_forward(q, k, v, cu, cu_kv, o, stream=stream)
+    stream.synchronize()
+    assert torch.equal(o, want)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("lens,H,K,D", [([3, 5], 2, 1, 64), ([200, 90], 4, 2, 128), ([70] * 12, 48, 48, 64), ([9] * 300, 2, 1, 32)], ids=str)
+def test_starts_out_of_range(cuda_device, lens, H, K, D, dtype):
+    """Starts before the first and behind the last row are clipped to the tensors, on either side."""
+    op, q, k, v, d_o, cu, cu_kv = make(lens, [2 * n for n in lens], H, K, D, dtype, cuda_device, seed=18)
+    far, far_kv = cu.clone(), cu_kv.clone()
+    far[0], far[-1], far_kv[0], far_kv[-1] = -7, q.shape[0] + 1000, -2 ** 31, 2 ** 31 - 1
+    o, lse = forward(op, q, k, v, cu, cu_kv)
+    o2, lse2 = forward(op, q, k, v, far, far_kv)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    a, b = backward(op, q, k, v, o, lse, d_o, cu, cu_kv), backward(op, q, k, v, o, lse, d_o, far, far_kv)
+    assert all(torch.equal(a[n], b[n]) for n in a)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
 def test_no_rows_on_one_side(cuda_device, dtype):
     op, q, k, v, d_o, cu, cu_kv = make([3, 4], [5, 6], 2, 1, 64, dtype, cuda_device, first=1, tail=2)
     none, none_q = k[:0], q[:0]
