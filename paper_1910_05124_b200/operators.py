@@ -17,7 +17,7 @@ import torch
 from .binding import PM_BF16, PM_F32, PipeMareError, _check, lib, pm_policy_desc, pm_tensor_pair
 
 _DTYPES = {torch.float32: PM_F32, torch.bfloat16: PM_BF16}
-_Tensor = torch.Tensor
+_Tensor, _I32, _F32 = torch.Tensor, torch.int32, torch.float32
 # pm_head_view and the descriptions as they lie in memory: what a call passes for a moment costs less as bytes than as ctypes objects
 _VIEW, _ATTENTION, _CROSS, _HEAD_NORM = (struct.Struct(f).pack for f in ("@Pqq", "@6iqf4x", "@5iqqf4x", "@6iqfP"))
 
@@ -172,9 +172,11 @@ class _HeadAttention:
 
     def _starts(self, name, cu, device):
         """Pointer and number of sequences of an array of starts."""
-        if not isinstance(cu, torch.Tensor) or cu.dim() != 1 or cu.numel() < 1:
+        if not isinstance(cu, _Tensor) or cu.dim() != 1 or not (n := cu.numel()):
             _refuse(f"{name} must be a one-dimensional tensor of sequences + 1 entries", "PM_ERR_SHAPE")
-        return _flat(name, cu, torch.int32, device, cu.shape), cu.numel() - 1
+        if not (cu.dtype is _I32 and cu.get_device() == device.index and cu.is_contiguous()):
+            _mismatch(name, cu, _I32, device, (n,))
+        return cu.data_ptr(), n - 1
 
     def _check_apart(self, name, dims):
         _check_apart(name, self.head_dim, dims)
@@ -212,7 +214,7 @@ class PackedAttention(_HeadAttention):
         """Writes o and, for a backward pass, lse."""
         device, Q, K, desc, cu = self._desc(q, cu_seqlens)
         vq, vk, vv, vo = _head_views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
-        p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, Q[0]))
+        p_lse = _flat("lse", lse, _F32, device, (self.n_heads, Q[0]))
         _launch(self.L.pm_attention_packed_forward, (desc, vq, vk, vv, cu, vo, p_lse), device, stream)
 
     def pm_attention_packed_backward(self, q, k, v, o, lse, d_o, cu_seqlens, dq, dk, dv, stream=None):
@@ -222,7 +224,7 @@ class PackedAttention(_HeadAttention):
             _refuse("lse must be a tensor")
         vq, vk, vv, vo, vdo, *grads = _head_views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
                                                   (q, k, v, o, d_o, dq, dk, dv), 5)
-        p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, Q[0]))
+        p_lse = _flat("lse", lse, _F32, device, (self.n_heads, Q[0]))
         _launch_with(4 * self.n_heads * Q[0], self.L.pm_attention_packed_backward, (desc, vq, vk, vv, vo, p_lse, vdo, cu, *grads), device, stream)
 
 
@@ -239,7 +241,7 @@ class CrossAttention(_HeadAttention):
 
     def _desc(self, q, k, cu_seqlens, cu_seqlens_kv):
         device, tokens = _head_rows("q", q, self.n_heads, self.head_dim)
-        _, kv_tokens = _head_rows("k", k, self.n_kv_heads, self.head_dim)
+        kv_tokens = k.shape[0] if isinstance(k, _Tensor) and k.dim() else 0           # k's type and shape: with the others
         cu, n_seqs = self._starts("cu_seqlens", cu_seqlens, device)
         cu_kv, n_kv_seqs = self._starts("cu_seqlens_kv", cu_seqlens_kv, device)
         if n_seqs != n_kv_seqs:
@@ -251,7 +253,7 @@ class CrossAttention(_HeadAttention):
         """Writes o and, for a backward pass, lse."""
         device, Q, K, desc, cu, cu_kv = self._desc(q, k, cu_seqlens, cu_seqlens_kv)
         vq, vk, vv, vo = _head_views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
-        p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, Q[0]))
+        p_lse = _flat("lse", lse, _F32, device, (self.n_heads, Q[0]))
         _launch(self.L.pm_attention_cross_forward, (desc, vq, vk, vv, cu, cu_kv, vo, p_lse), device, stream)
 
     def pm_attention_cross_backward(self, q, k, v, o, lse, d_o, cu_seqlens, cu_seqlens_kv, dq, dk, dv, stream=None):
@@ -261,7 +263,7 @@ class CrossAttention(_HeadAttention):
             _refuse("lse must be a tensor")
         vq, vk, vv, vo, vdo, *grads = _head_views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
                                                   (q, k, v, o, d_o, dq, dk, dv), 5)
-        p_lse = _flat("lse", lse, torch.float32, device, (self.n_heads, Q[0]))
+        p_lse = _flat("lse", lse, _F32, device, (self.n_heads, Q[0]))
         _launch_with(4 * self.n_heads * Q[0], self.L.pm_attention_cross_backward, (desc, vq, vk, vv, vo, p_lse, vdo, cu, cu_kv, *grads), device, stream)
 
 
@@ -294,32 +296,26 @@ class HeadNormRotate:
 
     def _sides(self, q, k, positions, q_gain, k_gain):
         """Device, dtype, shapes of both sides (None: absent), description, and pointers of positions and gains."""
-        d = self.head_dim
-        if q is None and k is None:
-            _refuse("neither queries nor keys")
+        d, Q, K, p_q, p_k = self.head_dim, None, None, None, None
         lead, name = (q, "q") if q is not None else (k, "k")
+        if lead is None:
+            _refuse("neither queries nor keys")
         device, tokens = _head_rows(name, lead, "heads", d)
-        shapes = []
-        for name, t in (("q", q), ("k", k)):
-            if t is None:
-                shapes.append(None)
-                continue
-            if not isinstance(t, torch.Tensor) or t.dim() != 3:
-                _refuse(f"{name} must be a tensor of [tokens, heads, {d}]", "PM_ERR_SHAPE")
-            if t.shape[1] < 1:
-                _refuse(f"{name} has no heads", "PM_ERR_SHAPE")
-            shapes.append((tokens, t.shape[1], d))
-        Q, K = shapes
-        if self.rotary_dim and positions is None:
-            _refuse("positions must be a tensor")
-        at = _flat("positions", positions, torch.int32, device, (tokens,)) if self.rotary_dim else None
-        gains = []
-        for name, shape, g in (("q_gain", Q, q_gain), ("k_gain", K, k_gain)):
-            if shape is not None and g is None:
-                _refuse(f"{name} must be a tensor")
-            gains.append(None if shape is None else _flat(name, g, torch.float32, device, (d,)))
+        if q is not None:
+            if q.shape[1] < 1:
+                _refuse("q has no heads", "PM_ERR_SHAPE")
+            Q = tokens, q.shape[1], d
+            p_q = _flat("q_gain", q_gain, _F32, device, (d,))
+        if k is not None:
+            if not isinstance(k, _Tensor) or k.dim() != 3 or k.shape[1] < 1:
+                _refuse(f"k must be a tensor of [tokens, heads, {d}]", "PM_ERR_SHAPE")
+            K = tokens, k.shape[1], d
+            p_k = _flat("k_gain", k_gain, _F32, device, (d,))
+        at = _flat("positions", positions, _I32, device, (tokens,)) if self.rotary_dim else None
+        if self.rotary_dim and positions is None or Q and q_gain is None or K and k_gain is None:
+            _refuse("positions must be a tensor" if self.rotary_dim and positions is None else "the gains must be tensors")
         desc = _HEAD_NORM(_DTYPES[lead.dtype], Q[1] if Q else 0, K[1] if K else 0, d, self.rotary_dim, self.interleaved, tokens, self.eps, self.p_turns)
-        return device, lead.dtype, Q, K, desc, at, gains
+        return device, lead.dtype, Q, K, desc, at, (p_q, p_k)
 
     def pm_head_norm_rotate(self, q, k, positions, q_gain, k_gain, q_out, k_out, stream=None):
         """Writes q_out and k_out, which may be q and k."""
