@@ -482,7 +482,7 @@ pm_status pm_attention_packed_selftest_wait_timeout(int64_t limit_cycles, void* 
  *   angle phi_i = position f_i:   y_a = n_a cos - n_b sin,  y_b = n_b cos + n_a sin
  * Pair i is (i, i + rotary_dim / 2), with `interleaved` (2 i, 2 i + 1).  turns: host array of rotary_dim / 2 frequencies in units
  * of 2^-64 turns per position, read during the call, as pm_rotation_turns fills it for f_i = base^(-2 i / rotary_dim) (base at
- * least 1); angles are exact to 2^-33 turns at every position, negative ones among them.  positions: int32 [n_tokens] on the
+ * least 1); angles are exact to 2^-33 turns at every position, negative ones among them, their sines and cosines to 2.4e-7.  positions: int32 [n_tokens] on the
  * device, not looked at with rotary_dim 0.  Gains are floats whatever dtype is.  Squares are summed in fp32: a row whose mean square
  * leaves its range (values beyond 1e18) gives zeros; eps may be 0, a row of zeros is then NaN.  A value that is not finite reaches
  * the results of its row (and, in the backward pass, the gains' gradients) alone.
@@ -516,8 +516,8 @@ pm_status pm_head_norm_rotate_backward(const pm_head_norm_desc* desc, const pm_h
 /* Dropout of n elements with a mask that is never stored, added to a residual stream (NULL: not added):
  *   y_i = residual_i + (kept_i ? x_i 2^16 / (2^16 - T) : 0),   kept_i = bits_i >= T,   T = p 2^16 to the nearest whole number
  * so p is taken to the nearest 2^-16 (0 to below 1 - 2^-17) and the scale is that of the p taken.  bits_i: 16 bits of
- * Philox4x32-10 with the key rng[0] (its lower 32 bits first) and the 128-bit counter rng[1] + i / 8: of its four words, word
- * (i mod 8) / 2, the lower half for even i.  rng: two int64 on the device, read when the call runs, so a captured graph draws
+ * Philox4x32-10 with the key rng[0] (its lower 32 bits first) and the counter rng[1] + i / 8 modulo 2^64 (lower word first, the two
+ * upper words zero): of its four words, word (i mod 8) / 2, the lower half for even i.  rng: two int64 on the device, read when the call runs, so a captured graph draws
  * anew when the program moves rng[1] on by (n + 7) / 8 or more between replays; the backward call takes the rng of its forward
  * call.  What is dropped may be NaN or infinite.  One rounding, of the result.  y may be x or the residual itself; any other
  * overlap is refused.  The backward pass of the residual is the identity. */
@@ -555,7 +555,8 @@ pm_status pm_token_logprobs_backward(const void* logits, int32_t dtype, int64_t 
  * zero so is everything.  A token of weight 0 is padding: its values may be NaN or infinite.  An advantage of 0 has no policy
  * term whatever the ratio is; other values that are not finite give what the formulas give.
  * stats: five floats on the device, the loss and the weighted sums of policy, kl, entropy and [clipped].  ref_logprob and entropy
- * may be NULL if their coefficients are 0 (their sums are then 0).  d_logprob, d_entropy: gradients of the loss, or NULL; they go
+ * may be NULL if their coefficients are 0 (their sums are then 0); a term whose coefficient is 0 is measured and counts for nothing
+ * else, whatever its values.  d_logprob, d_entropy: gradients of the loss, or NULL; they go
  * to pm_token_logprobs_backward.  At a border the ratio is not clipped; which side a token is on is decided in 64 bits.  Outputs
  * overlap neither each other nor an input (refused).  workspace: at least pm_policy_loss_workspace_bytes(n) bytes of device
  * memory (0 for short lists), 8-byte aligned. */

@@ -85,7 +85,7 @@ struct PolicyToken {
       const bool near = fabsf(d) < 0.5f;
       const float far = expf(d) - 1.f, kl = near ? d * d * s : far - d, slope = near ? d + kl : far;
       sums[2] += (double)w * kl;
-      grad -= (float)a.kl_coef * slope;
+      if (a.kl_coef != 0.0) grad -= (float)a.kl_coef * slope;        // measured alone: an infinite slope has no part of the gradient
     }
     if (a.entropy) sums[3] += (double)w * ent;
     return grad;
@@ -106,7 +106,7 @@ __device__ __forceinline__ double policy_share(const PolicyArgs& a, double weigh
 
 __device__ __forceinline__ void policy_stats(const PolicyArgs& a, const double (&sums)[kPolicySums], double share) {
   const double policy = sums[1] * share, kl = sums[2] * share, entropy = sums[3] * share;
-  a.stats[0] = (float)(policy + a.kl_coef * kl - a.entropy_coef * entropy);
+  a.stats[0] = (float)(policy + (a.kl_coef != 0.0 ? a.kl_coef * kl : 0.0) - (a.entropy_coef != 0.0 ? a.entropy_coef * entropy : 0.0));
   a.stats[1] = (float)policy;
   a.stats[2] = (float)kl;
   a.stats[3] = (float)entropy;

@@ -133,6 +133,19 @@ def test_values_that_are_not_finite(cuda_device, n):
 
 
 @pytest.mark.parametrize("n", [300, 20000])
+def test_terms_that_are_measured_alone(cuda_device, n):
+    """A term whose coefficient is zero has no part of the loss and the gradient, even where it is infinite."""
+    t = make(n, cuda_device, seed=18)
+    del t["w"]
+    plain = call({k: v for k, v in t.items() if k not in ("ref", "ent")}, kl=0.0, ent=0.0)
+    t["ref"], t["ent"] = t["ref"].clone(), t["ent"].clone()
+    t["ref"][0], t["ent"][1] = 200.0, math.inf
+    stats, d_lp, d_ent = call(t, kl=0.0, ent=0.0)
+    assert stats[0] == plain[0][0] and torch.equal(d_lp, plain[1]) and (d_ent == 0).all()
+    assert stats[2] == math.inf and stats[3] == math.inf and torch.equal(stats[[1, 4]], plain[0][[1, 4]])
+
+
+@pytest.mark.parametrize("n", [300, 20000])
 def test_statistics_alone(cuda_device, n):
     t = make(n, cuda_device, seed=8)
     want = check(t)[0]
