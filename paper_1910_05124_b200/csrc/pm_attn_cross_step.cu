@@ -492,7 +492,7 @@ __global__ void __launch_bounds__(StepShape<E, TEAM>::kWarps * 32, StepShape<E, 
   const int parts = TEAM == 1 ? 1 : (int)cg::this_cluster().num_blocks(), part = TEAM == 1 ? 0 : (int)cg::this_cluster().block_rank();
   const int team = threadIdx.x / (TEAM * 32), unit = blockIdx.x / parts * S::kTeams + team, hk = unit % a.kv_heads;
   SeqTile ks;
-  const SeqTile s = find_pair(a.cu, a.cu_kv, a.n_seqs, a.tokens, a.kv_tokens, unit / a.kv_heads, log_tokens, ks);
+  const SeqTile s = find_longest(a.cu, a.cu_kv, a.n_seqs, a.tokens, a.kv_tokens, unit / a.kv_heads, log_tokens, ks);
   if (s.tile < 0) return;
   const int token0 = s.tile << log_tokens, rows = min(s.len - token0, 1 << log_tokens) * a.group;
   if (ks.len == 0) {                              // no keys: zeros

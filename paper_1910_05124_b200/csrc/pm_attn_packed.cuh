@@ -135,8 +135,8 @@ __device__ __forceinline__ SeqTile find_longest(const int32_t* cu, const int32_t
   const int len = max(start(cu, tokens, lane + 1) - begin, 0), far_len = max(start(cu_other, other_tokens, lane + 1) - far, 0);
   const int tiles = (len + (1 << log_rows) - 1) >> log_rows;
   int at = 0;                                     // tiles of the sequences before this one
-#pragma unroll 8
-  for (int j = 0; j < 32; ++j) {
+#pragma unroll 4
+  for (int j = 0; j < n_seqs; ++j) {
     const int n = __shfl_sync(0xffffffffu, tiles, j), f = __shfl_sync(0xffffffffu, far_len, j);
     if (f > far_len || (f == far_len && j < lane)) at += n;
   }

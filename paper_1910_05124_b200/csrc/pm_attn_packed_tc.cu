@@ -228,7 +228,7 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
   const int block = blockIdx.x / parts, unit = block % units;
   SeqTile ks;
   SeqTile s;
-  if constexpr (X) s = find_pair(a.cu, a.cu_kv, a.n_seqs, a.tokens, a.kv_tokens, block / units, log_rows, ks);
+  if constexpr (X) s = find_longest(a.cu, a.cu_kv, a.n_seqs, a.tokens, a.kv_tokens, block / units, log_rows, ks);
   else ks = s = find_tile(a.cu, a.n_seqs, a.tokens, block / units, log_rows);
   if (s.tile < 0) {
     __syncthreads();
@@ -989,7 +989,7 @@ template <int DT, bool X> __device__ __forceinline__ void dkv_block(const Packed
   }
   SeqTile qs;
   SeqTile s;
-  if constexpr (X) s = find_pair(a.cu_kv, a.cu, a.n_seqs, a.kv_tokens, a.tokens, block / a.kv_heads, TC_LOG_ROWS, qs);
+  if constexpr (X) s = find_longest(a.cu_kv, a.cu, a.n_seqs, a.kv_tokens, a.tokens, block / a.kv_heads, TC_LOG_ROWS, qs);
   else qs = s = find_tile(a.cu_kv, a.n_seqs, a.kv_tokens, block / a.kv_heads, TC_LOG_ROWS);
   if (s.tile < 0) {
     __syncthreads();
@@ -1242,7 +1242,7 @@ template <int DT, bool X> __device__ __forceinline__ void dq_block(const PackedA
   }
   SeqTile ks;
   SeqTile s;
-  if constexpr (X) s = find_pair(a.cu, a.cu_kv, a.n_seqs, a.tokens, a.kv_tokens, block / a.heads, TC_LOG_ROWS, ks);
+  if constexpr (X) s = find_longest(a.cu, a.cu_kv, a.n_seqs, a.tokens, a.kv_tokens, block / a.heads, TC_LOG_ROWS, ks);
   else ks = s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.heads, TC_LOG_ROWS);
   if (s.tile < 0) {
     __syncthreads();
