@@ -1539,8 +1539,6 @@ template <int DT, int NT, bool X> static cudaError_t fwd_launch(const PackedArgs
   return launch_clusters(attn_packed_fwd_tc_kernel<DT, NT, X>, blocks, S::kThreads, S::kSmem, st, false, parts, a, maps, units, pair);
 }
 
-// Two query tiles to a block read keys and values half as often and pay for heads of 128 once every SM has such a block.  8192 tokens,
-// 16 heads of 128, us with two / one: 240 / 252; 4000 tokens, 4 heads of 128: 68 / 63; 8192 tokens, 16 heads of 64: 213 / 205.
 static cudaError_t stream_launch(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   using S = StreamShape;
@@ -1555,6 +1553,8 @@ static cudaError_t stream_launch(const PackedArgs& a, cudaStream_t st) {
   return launch_pdl(attn_cross_stream_kernel, dim3((unsigned)blocks), dim3(S::kThreads), S::kSmem, st, false, a, maps, a.heads);
 }
 
+// Two query tiles to a block read keys and values half as often and pay for heads of 128 once every SM has such a block.  8192 tokens,
+// 16 heads of 128, us with two / one: 240 / 252; 4000 tokens, 4 heads of 128: 68 / 63; 8192 tokens, 16 heads of 64: 213 / 205.
 template <bool X> static cudaError_t tc_forward(const PackedArgs& a, cudaStream_t st) {
   // blocks that stay where there are more tiles than run at a time
   if (X && a.dim <= 64 && most_tiles(a.tokens, a.n_seqs, TC_ROWS) * a.heads > 2 * kSms) return stream_launch(a, st);
