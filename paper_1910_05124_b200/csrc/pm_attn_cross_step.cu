@@ -1,6 +1,6 @@
 // Cross attention of few query rows: a decoding step, with a token or the few of a beam to each sequence.  bf16 and fp32.
 //
-// Bound by memory: every key and value is read once and meets at most 16 query rows (tokens times the heads that share it), far too few
+// Bound by memory: every key and value is read once for 16 query rows (tokens times the heads that share it), most often for all, far too few
 // for a tile of the other kernels, whose chain of waits would set the pace.  Here every warp has a pipeline of its own and no barrier in it: it
 // copies runs of keys and values into its part of shared memory (cp.async, zeros behind the sequence's end), forms S = Q K^T and
 // O += P V, and keeps its own running maximum and sum.  bf16: 16-row products from registers (mma m16n8k16; Q in registers throughout, P
@@ -518,9 +518,15 @@ static int step_log_tokens(const PackedArgs& a, int rows) {
   return log;
 }
 
-// Sequences of no more rows on average than a tile has; bf16 in what the tensor-core kernels take.
+// Rows (tokens times the heads that share a key) on average of a sequence that these kernels are the faster ones for; bf16 in what the tensor-core
+// kernels take.  us with these / the others: bf16, 16 x 8 tokens over 1000 keys, 16 heads of 128 on 4 (32 rows) 15.5 / 22.8; 64 x 20 over 60, 8 heads
+// of 64 (20) 8.0 / 11.7; 16 x 32 over 1000, 16 heads of 64 (32) 19.8 / 19.4; 16 x 64 (64) 34.7 / 19.7.  fp32, 16 x 8 over 1000, 16 heads of 128 on 4 121 / 160; 16 x 5
+// over 3000, 32 heads of 128 on 8 (20) 496 / 1720; but 16 x 20 over 1000, 16 heads of 64 177 / 148: heads that share keys are what the others repeat.
 bool attn_cross_step_takes(const PackedArgs& a, int dtype) {
-  return a.cross && a.tokens * a.group <= (int64_t)CS_ROWS * a.n_seqs && (dtype == PM_F32 || attn_packed_tc_takes(a, dtype, false));
+  const int64_t rows = a.tokens * a.group;
+  if (!a.cross || rows > (int64_t)32 * a.n_seqs) return false;
+  if (dtype == PM_F32) return rows <= (int64_t)16 * a.n_seqs || a.tokens <= (int64_t)8 * a.n_seqs;
+  return attn_packed_tc_takes(a, dtype, false);
 }
 
 template <typename E, int TEAM> static cudaError_t step_launch(const PackedArgs& a, int64_t units, int parts, int log_tokens, cudaStream_t st) {

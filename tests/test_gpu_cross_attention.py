@@ -88,7 +88,8 @@ def test_shared_heads(cuda_device, H, K, dtype):
 @pytest.mark.parametrize("lens,kv_lens,H,K,D", [
     ([1] * 16, [37 * (i + 1) for i in range(16)], 4, 4, 64), ([1], [5000], 2, 1, 64), ([1, 1, 1], [2, 3001, 0], 8, 2, 128), ([4] * 5, [600, 1, 64, 65, 129], 4, 2, 64),
     ([1, 40, 1, 1, 1, 1, 1, 1, 1], [70] * 9, 2, 2, 64), ([3] * 70, [11 * (i % 9) for i in range(70)], 2, 1, 96), ([1] * 300, [i % 40 for i in range(300)], 1, 1, 64),
-    ([16] * 3, [90, 900, 9], 1, 1, 128), ([17] * 3, [90, 900, 9], 2, 2, 80)], ids=str)
+    ([16] * 3, [90, 900, 9], 1, 1, 128), ([17] * 3, [90, 900, 9], 2, 2, 80), ([32] * 4, [90, 300, 9, 0], 2, 2, 64), ([8, 9, 3, 0], [90, 300, 9, 5], 8, 2, 128),
+    ([5] * 40, [60] * 40, 24, 4, 64), ([1, 60], [700, 300], 4, 2, 48)], ids=str)
 def test_few_queries(cuda_device, lens, kv_lens, H, K, D, dtype):
     """Decoding steps: a token or a few to each sequence, one sequence with more among them."""
     check(*make(lens, kv_lens, H, K, D, dtype, cuda_device, first=2, tail=5, seed=len(lens)))
