@@ -8,8 +8,9 @@
 // Short lists: one cluster of blocks, whose threads hold their tokens while the sum of the weights and the sums of the terms cross the
 // cluster's shared memory; one launch, bound by its latency.  Long lists: a launch that adds the weights, and one that does the rest, in
 // which the block that ends last adds the blocks' sums, in their order.  Bound by memory: each input once, the weights twice (the second
-// time from L2).  4096 tokens 3.9 us, 1048576 12.4 us (33 MB: 5.2 at the rate of a copy; the ends of two launches are the rest).  Sums in 64 bits; which side of a border a ratio is on is decided by delta in 64 bits, where the difference of two fp32
-// numbers is all but exact, so that no rounding of an exponential moves a gradient across the border.
+// time from L2).  4096 tokens 3.9 us, 1048576 12.4 us (33 MB: 5.2 at the rate of a copy; the ends of two launches are the rest).  Sums in
+// 64 bits; which side of a border a ratio is on is decided by delta in 64 bits, where the difference of two fp32 numbers is all but
+// exact, so that no rounding of an exponential moves a gradient across the border.
 #include <cmath>
 
 #include <cooperative_groups.h>
