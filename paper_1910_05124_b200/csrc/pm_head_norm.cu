@@ -77,6 +77,12 @@ __device__ __forceinline__ float2 turn_of(int32_t position, uint64_t turns) {
 }
 
 template <typename T> constexpr int kVec = 16 / sizeof(T);           // elements of a 16-byte vector
+// V elements: 16 bytes, or 8 where that is what divides rows and their rotated part
+template <typename T, int V> using NormVector = std::conditional_t<V * sizeof(T) == 16, uint4, uint2>;
+template <int BYTES> __device__ __forceinline__ void norm_copy(void* dst, const void* src) {
+  if constexpr (BYTES == 16) cp_async16(dst, src);
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
 
 // V pairs: the first elements and the second ones, two pairs to a register pair of the packed arithmetic.
 template <int V> struct Pairs {
@@ -85,8 +91,9 @@ template <int V> struct Pairs {
 
 // What a lane of a group holds of every row: two vectors, at columns a and b, which are V pairs.  Without INTER a pair is an element of
 // each, with INTER it is two neighbours; behind the rotated dimensions the angle is zero.
-template <typename T, bool INTER> struct NormLane {
-  static constexpr int V = kVec<T>;
+template <typename T, int V, bool INTER> struct NormLane {
+  using Vector = NormVector<T, V>;
+  static constexpr int kWords = sizeof(Vector) / 4;
   int a, b;
   bool on;                                        // a group may have more lanes than a row has vectors
   __device__ __forceinline__ NormLane(int c, int dim, int rotary) {
@@ -124,9 +131,11 @@ template <typename T, bool INTER> struct NormLane {
       (e & 1 ? g.s[e / 2].y : g.s[e / 2].x) = gain[second(e)];
     }
   }
-  static __device__ __forceinline__ void spread(Pairs<V>& v, const uint4* slot) {
-    const uint4 lo = slot[0], hi = slot[kNormThreads];
-    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  static __device__ __forceinline__ void spread(Pairs<V>& v, const Vector* slot) {
+    const Vector lo = slot[0], hi = slot[kNormThreads];
+    uint32_t w[2 * kWords];
+    memcpy(w, &lo, sizeof(lo));
+    memcpy(w + kWords, &hi, sizeof(hi));
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -138,15 +147,15 @@ template <typename T, bool INTER> struct NormLane {
       auto low = [](uint32_t u) { return __uint_as_float(u << 16); };
       auto high = [](uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); };
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < kWords; ++i) {
         v.f[i] = INTER ? make_float2(low(w[2 * i]), low(w[2 * i + 1])) : make_float2(low(w[i]), high(w[i]));
-        v.s[i] = INTER ? make_float2(high(w[2 * i]), high(w[2 * i + 1])) : make_float2(low(w[4 + i]), high(w[4 + i]));
+        v.s[i] = INTER ? make_float2(high(w[2 * i]), high(w[2 * i + 1])) : make_float2(low(w[kWords + i]), high(w[kWords + i]));
       }
     }
   }
   // to the lane's columns, of which `row` is the first; the other vector is `apart` elements on
   static __device__ __forceinline__ void store(T* row, int apart, const Pairs<V>& v) {
-    uint32_t w[8];
+    uint32_t w[2 * kWords];
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -158,13 +167,16 @@ template <typename T, bool INTER> struct NormLane {
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < kWords; ++i) {
         w[INTER ? 2 * i : i] = INTER ? pack_bf16(v.f[i].x, v.s[i].x) : pack_bf16(v.f[i].x, v.f[i].y);
-        w[INTER ? 2 * i + 1 : 4 + i] = INTER ? pack_bf16(v.f[i].y, v.s[i].y) : pack_bf16(v.s[i].x, v.s[i].y);
+        w[INTER ? 2 * i + 1 : kWords + i] = INTER ? pack_bf16(v.f[i].y, v.s[i].y) : pack_bf16(v.s[i].x, v.s[i].y);
       }
     }
-    *reinterpret_cast<uint4*>(row) = make_uint4(w[0], w[1], w[2], w[3]);
-    *reinterpret_cast<uint4*>(row + apart) = make_uint4(w[4], w[5], w[6], w[7]);
+    Vector lo, hi;
+    memcpy(&lo, w, sizeof(lo));
+    memcpy(&hi, w + kWords, sizeof(hi));
+    *reinterpret_cast<Vector*>(row) = lo;
+    *reinterpret_cast<Vector*>(row + apart) = hi;
   }
 };
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
@@ -221,19 +233,20 @@ __device__ __forceinline__ void leave_gains(const NormArgs& p, int block, const 
   }
 }
 
-// Rows ahead of the one that is worked on, of 32 bytes a lane or, with their gradients, 64.
-template <bool BACKWARD> constexpr int kNormAhead = BACKWARD ? 3 : 5;
-template <bool BACKWARD> constexpr int kNormSmem = (kNormAhead<BACKWARD> + 1) * (BACKWARD ? 4 : 2) * kNormThreads * 16;
+// Rows ahead of the one that is worked on, of two vectors of BYTES a lane or, with their gradients, four.
+template <bool BACKWARD, int BYTES> constexpr int kNormAhead = (BACKWARD ? 4 : 6) * 16 / BYTES - 1;
+template <bool BACKWARD> constexpr int kNormSmem = (kNormAhead<BACKWARD, 16> + 1) * (BACKWARD ? 4 : 2) * kNormThreads * 16;
 
 // A block has rows of queries or rows of keys alone: one gain, and the sums of one.
-template <typename T, int L, bool INTER, bool BACKWARD>
+template <typename T, int V, int L, bool INTER, bool BACKWARD>
 __global__ void __launch_bounds__(kNormThreads, BACKWARD ? 2 : 3) head_norm_kernel(const __grid_constant__ NormArgs p) {
-  constexpr int V = kVec<T>, A = kNormAhead<BACKWARD>, W = BACKWARD ? 4 : 2;     // W: vectors of a row in shared memory
-  extern __shared__ uint4 ring[];
+  constexpr int kBytes = V * sizeof(T), A = kNormAhead<BACKWARD, kBytes>, W = BACKWARD ? 4 : 2;  // W: vectors of a row in shared memory
+  using Vector = NormVector<T, V>;
+  extern __shared__ uint4 norm_ring[];
   if (BACKWARD) pdl_trigger();
   const int side = blockIdx.x >= p.blocks[0], block = blockIdx.x - (side ? p.blocks[0] : 0);
   const NormSide& s = p.side[side];
-  const NormLane<T, INTER> at(threadIdx.x % L, p.dim, p.rotary);
+  const NormLane<T, V, INTER> at(threadIdx.x % L, p.dim, p.rotary);
   const float per = 1.f / p.dim;
   NormWalk now(p, side, block, 32 / L), ahead = now;
   // a group behind the last token takes that one's rows and writes nothing
@@ -242,17 +255,17 @@ __global__ void __launch_bounds__(kNormThreads, BACKWARD ? 2 : 3) head_norm_kern
   const HeadView& result = BACKWARD ? s.dx : s.y;
   T* out = nullptr;
   const int apart = at.b - at.a;
-  uint4* const mine = ring + threadIdx.x;
+  Vector* const mine = reinterpret_cast<Vector*>(norm_ring) + threadIdx.x;
   int put = 0, get = 0;                           // places in the ring, in vectors
   constexpr int kPlace = W * kNormThreads, kPlaces = (A + 1) * kPlace;
   auto copy_next = [&]() {                        // a group of copies even where there is no row left: they are counted
     if (ahead.left > 0) {
-      cp_async16(mine + put, x_row);
-      cp_async16(mine + put + kNormThreads, x_row + apart);
+      norm_copy<kBytes>(mine + put, x_row);
+      norm_copy<kBytes>(mine + put + kNormThreads, x_row + apart);
       x_row += s.x.head;
       if (BACKWARD) {
-        cp_async16(mine + put + 2 * kNormThreads, u_row);
-        cp_async16(mine + put + 3 * kNormThreads, u_row + apart);
+        norm_copy<kBytes>(mine + put + 2 * kNormThreads, u_row);
+        norm_copy<kBytes>(mine + put + 3 * kNormThreads, u_row + apart);
         u_row += s.y.head;
       }
       if (ahead.next()) {
@@ -285,7 +298,7 @@ __global__ void __launch_bounds__(kNormThreads, BACKWARD ? 2 : 3) head_norm_kern
     }
     copy_next();
     cp_async_wait<A>();                           // this row's copies, the oldest
-    const uint4* const slot = mine + get;
+    const Vector* const slot = mine + get;
     get = get + kPlace == kPlaces ? 0 : get + kPlace;
     Pairs<V> x;
     at.spread(x, slot);
@@ -451,39 +464,43 @@ template <typename K> static cudaError_t norm_allow(K kernel, int bytes, std::at
   }
   return e;
 }
-template <typename T, int L, bool INTER, bool BACKWARD> static cudaError_t norm_launch(const NormArgs& p, cudaStream_t st) {
+template <typename T, int V, int L, bool INTER, bool BACKWARD> static cudaError_t norm_launch(const NormArgs& p, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
-  const cudaError_t e = norm_allow(head_norm_kernel<T, L, INTER, BACKWARD>, kNormSmem<BACKWARD>, done);
+  const cudaError_t e = norm_allow(head_norm_kernel<T, V, L, INTER, BACKWARD>, kNormSmem<BACKWARD>, done);
   if (e != cudaSuccess) return e;
-  return launch_pdl(head_norm_kernel<T, L, INTER, BACKWARD>, dim3(p.blocks[0] + p.blocks[1]), dim3(kNormThreads), kNormSmem<BACKWARD>, st, false, p);
+  return launch_pdl(head_norm_kernel<T, V, L, INTER, BACKWARD>, dim3(p.blocks[0] + p.blocks[1]), dim3(kNormThreads), kNormSmem<BACKWARD>, st, false, p);
 }
-template <typename T, int L> static cudaError_t norm_vec(const NormArgs& p, bool interleaved, bool backward, cudaStream_t st) {
-  if (interleaved) return backward ? norm_launch<T, L, true, true>(p, st) : norm_launch<T, L, true, false>(p, st);
-  return backward ? norm_launch<T, L, false, true>(p, st) : norm_launch<T, L, false, false>(p, st);
+template <typename T, int V, int L> static cudaError_t norm_vec(const NormArgs& p, bool interleaved, bool backward, cudaStream_t st) {
+  if (interleaved) return backward ? norm_launch<T, V, L, true, true>(p, st) : norm_launch<T, V, L, true, false>(p, st);
+  return backward ? norm_launch<T, V, L, false, true>(p, st) : norm_launch<T, V, L, false, false>(p, st);
 }
-template <typename T> static cudaError_t norm_width(const NormArgs& p, int lanes, bool interleaved, bool backward, cudaStream_t st) {
+template <typename T, int V> static cudaError_t norm_width(const NormArgs& p, int lanes, bool interleaved, bool backward, cudaStream_t st) {
   switch (lanes) {
-    case 1: return norm_vec<T, 1>(p, interleaved, backward, st);
-    case 2: return norm_vec<T, 2>(p, interleaved, backward, st);
-    case 4: return norm_vec<T, 4>(p, interleaved, backward, st);
-    case 8: return norm_vec<T, 8>(p, interleaved, backward, st);
+    case 1: return norm_vec<T, V, 1>(p, interleaved, backward, st);
+    case 2: return norm_vec<T, V, 2>(p, interleaved, backward, st);
+    case 4: return norm_vec<T, V, 4>(p, interleaved, backward, st);
+    case 8: return norm_vec<T, V, 8>(p, interleaved, backward, st);
     default: break;
   }
-  if constexpr (sizeof(T) == 4) return norm_vec<T, 16>(p, interleaved, backward, st);
+  if constexpr (V == 4) return norm_vec<T, V, 16>(p, interleaved, backward, st);
   return cudaErrorInvalidValue;
 }
 
 template <typename T> static cudaError_t norm_run(NormArgs& p, bool interleaved, bool backward, float* d_gain_q, float* d_gain_k, cudaStream_t st) {
-  constexpr int V = kVec<T>;
-  bool vec = p.dim % (2 * V) == 0 && p.rotary % (2 * V) == 0;
-  auto whole = [&](const HeadView& x) { vec = vec && aligned_to(x.data, 16) && x.token % V == 0 && x.head % V == 0; };
-  for (const NormSide& s : p.side)
-    if (s.heads) {
-      whole(s.x);
-      whole(s.y);
-      if (backward) whole(s.dx);
-    }
-  const int lanes = vec ? norm_lanes(p.dim, V) : 32;
+  // the longest vectors that divide rows, their rotated part and strides
+  auto divides = [&](int v) {
+    bool all = p.dim % (2 * v) == 0 && p.rotary % (2 * v) == 0;
+    auto whole = [&](const HeadView& x) { all = all && aligned_to(x.data, v * (int)sizeof(T)) && x.token % v == 0 && x.head % v == 0; };
+    for (const NormSide& s : p.side)
+      if (s.heads) {
+        whole(s.x);
+        whole(s.y);
+        if (backward) whole(s.dx);
+      }
+    return all;
+  };
+  const int vec = divides(kVec<T>) ? kVec<T> : divides(4) ? 4 : 1;
+  const int lanes = vec > 1 ? norm_lanes(p.dim, vec) : 32;
   // the blocks that run at a time go to the sides by their work: heads, and a token's angles, which take about as long as two rows (12291 tokens,
   // 16 + 2 heads of 128: 22 us forward and 33 backward, by heads alone 25 and 38)
   auto weight = [&](int n) { return n ? n + (p.rotary ? 2 : 0) : 0; };
@@ -495,8 +512,10 @@ template <typename T> static cudaError_t norm_run(NormArgs& p, bool interleaved,
     p.blocks[i] = (int)std::min<int64_t>((rows + per_block - 1) / per_block, std::max(1, (int)((int64_t)(backward ? kNormBlocks<true> : kNormBlocks<false>) * weight(n) / (weight(p.side[0].heads) + weight(p.side[1].heads)))));
   }
   cudaError_t e;
-  if (vec) {
-    e = norm_width<T>(p, lanes, interleaved, backward, st);
+  if (vec == kVec<T>) {
+    e = norm_width<T, kVec<T>>(p, lanes, interleaved, backward, st);
+  } else if (vec == 4) {
+    e = norm_width<T, 4>(p, lanes, interleaved, backward, st);
   } else {
     const dim3 grid(p.blocks[0] + p.blocks[1]);
     e = backward ? launch_pdl(head_norm_any_kernel<T, true>, grid, dim3(kNormThreads), 0, st, false, p, (int)interleaved)

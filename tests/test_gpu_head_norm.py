@@ -61,6 +61,18 @@ def test_sizes(cuda_device, tokens, H, K, dtype):
         check(pm.HeadNormRotate(D), *make(tokens, H, K, D, dtype, cuda_device, seed=tokens))
 
 
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("D,rotary", [(40, 40), (80, 40), (24, 8), (56, 56), (120, 0), (104, 24), (64, 8)])
+def test_short_vectors(cuda_device, D, rotary, inter):
+    """bf16 rows that vectors of 8 bytes divide and those of 16 do not, or whose strides and starts they do not."""
+    import paper_1910_05124_b200 as pm
+    op = pm.HeadNormRotate(D, rotary_dim=rotary, interleaved=inter)
+    for tokens in (1, 301):
+        check(op, *make(tokens, 5, 1, D, BF, cuda_device, seed=D + tokens))
+    q, k, d_q, d_k, gains, positions = make(70, 3, 2, 64, BF, cuda_device, seed=D)
+    check(pm.HeadNormRotate(64, interleaved=inter), torch.cat([q.new_zeros(70, 3, 4), q], 2)[..., 4:], k, d_q, d_k, gains, positions)
+
+
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("base", [1.0, 100.0, 10000.0, 5e6])
 def test_positions(cuda_device, base, dtype):
