@@ -456,7 +456,7 @@ template <typename T, int DP, bool VEC, int R> static cudaError_t pk_forward(con
   if (!launchable(blocks)) return cudaErrorInvalidConfiguration;
   const cudaError_t e = pk_allow(attn_packed_fwd_kernel<T, DP, VEC, R>, smem, done);
   if (e != cudaSuccess) return e;
-  return launch_clusters(attn_packed_fwd_kernel<T, DP, VEC, R>, blocks, 4 * R, smem, st, false, pk_split<R> ? packed_parts(blocks, a, PK_T, 1, 4 * kSms, 3) : 1, a);
+  return launch_clusters(attn_packed_fwd_kernel<T, DP, VEC, R>, blocks, 4 * R, smem, st, false, pk_split<R> ? forward_parts(blocks, a, PK_T, 4 * kSms, 3) : 1, a);
 }
 template <typename T, int DP, bool VEC, int R> static cudaError_t pk_backward(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
@@ -466,7 +466,7 @@ template <typename T, int DP, bool VEC, int R> static cudaError_t pk_backward(co
   cudaError_t e = pk_allow(attn_packed_bwd_kernel<T, DP, VEC, R>, smem, done);
   if (e == cudaSuccess) e = launch_pdl(attn_packed_delta_kernel<T>, dim3((unsigned)((a.tokens * a.heads + 7) / 8)), dim3(256), 0, st, false, a);
   if (e == cudaSuccess)
-    e = launch_clusters(attn_packed_bwd_kernel<T, DP, VEC, R>, blocks, 4 * R, smem, st, true, pk_split<R> ? packed_parts(blocks, a, PK_T, a.group, 4 * kSms, 2) : 1, a,
+    e = launch_clusters(attn_packed_bwd_kernel<T, DP, VEC, R>, blocks, 4 * R, smem, st, true, pk_split<R> ? backward_parts(blocks, a, PK_T, 4 * kSms, 2) : 1, a,
                   (int)dkv);
   return e;
 }

@@ -176,18 +176,26 @@ inline cudaError_t launch_clusters(void (*kernel)(K...), int64_t blocks, int thr
 }
 
 // Blocks that share the work of one: as many as leave no more than `most` in the launch (whose size is the most that the lengths can
-// make), as long as each keeps `least` streamed tiles of `rows` rows of `heads` heads in a sequence of average length.  us shared /
+// make), as long as each keeps `least` of the `streamed` tiles of a sequence of average length.  us shared /
 // not: bf16, 2000 tokens, 2 heads of 64 on 1, forward 18 / 27, backward 35 / 76; 4000 tokens, 4 heads of 128, forward 45 / 63; 2 x 1000
 // tokens, 8 heads of 128 on 2, backward 49 / 70; fp32, 700 + 300 + 13 tokens, 4 heads of 128 on 2, both 205 / 305; 493 tokens in 7, 4
 // heads of 32 on 2, both 27 / 31.  Finer parts lose: the backward pass of the 2 x 1000 tokens in eight parts takes 80.
-// Blocks that stream keys and blocks that stream the queries of `heads` heads share alike: by the longer of the two, and a part
-// that gets nothing of the shorter adds zeros.
-inline int packed_parts(int64_t blocks, const PackedArgs& a, int rows, int heads, int most, int least) {
-  auto streamed = [&](int64_t tokens) { return ((tokens + a.n_seqs - 1) / a.n_seqs + rows - 1) / rows; };
-  const int64_t tiles = std::max(streamed(a.tokens) * heads, a.cross ? streamed(a.kv_tokens) : 0);
+inline int packed_parts(int64_t blocks, int64_t streamed, int most, int least) {
   int parts = 1;
-  while (parts < 8 && blocks * parts * 2 <= most && tiles >= parts * 2 * least) parts *= 2;
+  while (parts < 8 && blocks * parts * 2 <= most && streamed >= parts * 2 * least) parts *= 2;
   return parts;
+}
+// tiles of `rows` rows of a sequence of average length
+inline int64_t average_tiles(int64_t tokens, int n_seqs, int rows) { return ((tokens + n_seqs - 1) / n_seqs + rows - 1) / rows; }
+// The forward pass streams keys alone, however many the queries (cross attention, us shared by the longer side / by the keys: 4000 tokens over
+// 100, a head of 64 in bf16, 16.0 / 5.9; 2000 over 40, 2 heads of 64, bf16 10.5 / 5.9, fp32 21.6 / 6.2; 4000 over 600, 2 heads of 128, 19.2 / 13.9).
+inline int forward_parts(int64_t blocks, const PackedArgs& a, int rows, int most, int least) {
+  return packed_parts(blocks, average_tiles(a.kv_tokens, a.n_seqs, rows), most, least);
+}
+// The backward pass has blocks that stream keys and blocks that stream the queries of all heads that share them.  They share alike, by the
+// longer of the two: a part that gets nothing of the shorter adds zeros.
+inline int backward_parts(int64_t blocks, const PackedArgs& a, int rows, int most, int least) {
+  return packed_parts(blocks, std::max(average_tiles(a.tokens, a.n_seqs, rows) * a.group, average_tiles(a.kv_tokens, a.n_seqs, rows)), most, least);
 }
 
 // launchers of the tensor-core kernels

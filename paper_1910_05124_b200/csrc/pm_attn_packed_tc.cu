@@ -1535,7 +1535,7 @@ template <int DT, int NT, bool X> static cudaError_t fwd_launch(const PackedArgs
   if (e == cudaSuccess) e = encode_heads(&maps.k, a.k, a.dim, a.kv_heads, a.kv_tokens, TC_ROWS);
   if (e == cudaSuccess) e = encode_heads(&maps.v, a.v, a.dim, a.kv_heads, a.kv_tokens, TC_ROWS);
   if (e != cudaSuccess) return e;
-  const int parts = NT == 1 ? packed_parts(blocks, a, TC_ROWS, 1, 2 * kSms, 3) : 1;
+  const int parts = NT == 1 ? forward_parts(blocks, a, TC_ROWS, 2 * kSms, 3) : 1;
   return launch_clusters(attn_packed_fwd_tc_kernel<DT, NT, X>, blocks, S::kThreads, S::kSmem, st, false, parts, a, maps, units, pair);
 }
 
@@ -1581,7 +1581,7 @@ template <int DT, bool X> static cudaError_t bwd_launch(const PackedArgs& a, cud
   // starts beside the first's last blocks; its own wait for them before they read delta
   if (e == cudaSuccess)
     e = launch_clusters(attn_packed_bwd_tc_kernel<DT, X>, blocks, S::kThreads, S::kSmem, st, true,
-                        packed_parts(blocks, a, S::kCols, a.group, 4 * kSms, 4), a, maps, (int)dkv);
+                        backward_parts(blocks, a, S::kCols, 4 * kSms, 4), a, maps, (int)dkv);
   return e;
 }
 cudaError_t attn_packed_tc_backward(const PackedArgs& a, cudaStream_t st) {
