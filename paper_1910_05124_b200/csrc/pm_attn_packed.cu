@@ -170,18 +170,20 @@ __device__ __forceinline__ void pk_finish(const HeadView& x, const SeqTile& s, i
   }
 }
 
-template <typename T, int DP, bool VEC, int R>
+// X: the keys are those of other sequences (cross attention), which may have none; a template, so that a sequence's own keys cost no registers
+// for it (2 x 1024 tokens, 16 heads of 64, unaligned bf16: forward 150 us, backward 565; with a branch 153 and 570).
+template <typename T, int DP, bool VEC, int R, bool X>
 __global__ void __launch_bounds__(4 * R, R == 64 && DP <= 64 ? 2 : 1) attn_packed_fwd_kernel(PackedArgs a) {
   cg::cluster_group cluster = cg::this_cluster();
   const int parts = pk_split<R> ? (int)cluster.num_blocks() : 1, part = pk_split<R> ? (int)cluster.block_rank() : 0, block = blockIdx.x / parts;
   const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.heads, kLog<R>);
   if (s.tile < 0) return;
-  const SeqTile ks = other_side(a.cross, s, a.cu_kv, a.kv_tokens);
+  const SeqTile ks = X ? other_side(s, a.cu_kv, a.kv_tokens) : s;
   extern __shared__ float sm[];
   float *sQ = sm, *sK = sQ + R * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sP = sV + PK_T * kPkLd<DP>;
   const int h = block % a.heads, hk = h / a.group, q0 = pk_from_end<R>(s) * R;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int all = a.causal ? min(s.len, q0 + R) : ks.len, tiles = (all + PK_T - 1) / PK_T;
+  const int all = !X && a.causal ? min(s.len, q0 + R) : ks.len, tiles = (all + PK_T - 1) / PK_T;
   const int begin = tiles * part / parts * PK_T, end = min(all, tiles * (part + 1) / parts * PK_T);
   PkPair<T, DP, VEC, PK_T, 4 * R> next;
   {
@@ -209,7 +211,7 @@ __global__ void __launch_bounds__(4 * R, R == 64 && DP <= 64 ? 2 : 1) attn_packe
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int c = k0 + tx + 16 * j;
-        acc[i][j] = c < ks.len && (!a.causal || c <= r) ? acc[i][j] * a.scale : -INFINITY;
+        acc[i][j] = c < ks.len && (X || !a.causal || c <= r) ? acc[i][j] * a.scale : -INFINITY;
         mx = max_nan(mx, acc[i][j]);
       }
 #pragma unroll
@@ -255,7 +257,7 @@ __global__ void __launch_bounds__(4 * R, R == 64 && DP <= 64 ? 2 : 1) attn_packe
     for (int r = r0 + threadIdx.x; r < r1; r += 4 * R) {
       float top, base, sum;
       total(r, top, base, sum);
-      for (int p = 0; p < parts; ++p) weights[p * R + r] = ks.len ? ex2((cluster.map_shared_rank(stats, p)[r] - base) * kLog2e) / sum : 0.f;
+      for (int p = 0; p < parts; ++p) weights[p * R + r] = !X || ks.len ? ex2((cluster.map_shared_rank(stats, p)[r] - base) * kLog2e) / sum : 0.f;
       if (a.lse && q0 + r < s.len) a.lse[(int64_t)h * a.tokens + s.begin + q0 + r] = top + logf(sum);
     }
     __syncthreads();
@@ -266,7 +268,7 @@ __global__ void __launch_bounds__(4 * R, R == 64 && DP <= 64 ? 2 : 1) attn_packe
   float inv[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    inv[i] = ks.len ? 1.f / l[i] : 0.f;           // no keys: zeros
+    inv[i] = !X || ks.len ? 1.f / l[i] : 0.f;           // no keys: zeros
     const int r = q0 + 4 * ty + i;
     if (a.lse && tx == 0 && r < s.len) a.lse[(int64_t)h * a.tokens + s.begin + r] = m[i] + logf(l[i]);
   }
@@ -290,15 +292,15 @@ __global__ void __launch_bounds__(256) attn_packed_delta_kernel(PackedArgs a) {
   }
 }
 
-template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void pk_dq_block(const PackedArgs& a, int block, int part, int parts) {
+template <typename T, int DP, bool VEC, int R, bool X> __device__ __forceinline__ void pk_dq_block(const PackedArgs& a, int block, int part, int parts) {
   const SeqTile s = find_tile(a.cu, a.n_seqs, a.tokens, block / a.heads, kLog<R>);
   if (s.tile < 0) { pdl_wait(); return; }
-  const SeqTile ks = other_side(a.cross, s, a.cu_kv, a.kv_tokens);
+  const SeqTile ks = X ? other_side(s, a.cu_kv, a.kv_tokens) : s;
   extern __shared__ float sm[];
   float *sQ = sm, *sO = sQ + R * kPkLd<DP>, *sK = sO + R * kPkLd<DP>, *sV = sK + PK_T * kPkLd<DP>, *sS = sV + PK_T * kPkLd<DP>;
   const int h = block % a.heads, hk = h / a.group, q0 = pk_from_end<R>(s) * R;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int all = a.causal ? min(s.len, q0 + R) : ks.len, tiles = (all + PK_T - 1) / PK_T;
+  const int all = !X && a.causal ? min(s.len, q0 + R) : ks.len, tiles = (all + PK_T - 1) / PK_T;
   const int begin = tiles * part / parts * PK_T, end = min(all, tiles * (part + 1) / parts * PK_T);
   PkPair<T, DP, VEC, PK_T, 4 * R> next;
   {
@@ -333,7 +335,7 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
       for (int j = 0; j < 4; ++j) {
         const int c = k0 + tx + 16 * j, r = q0 + 4 * ty + i;
         const float p = ex2((acc[i][j] * a.scale - lse[i]) * kLog2e);
-        sS[(4 * ty + i) * PK_LDP + tx + 16 * j] = c < ks.len && r < s.len && (!a.causal || c <= r) ? p * (dp[i][j] - delta[i]) : 0.f;
+        sS[(4 * ty + i) * PK_LDP + tx + 16 * j] = c < ks.len && r < s.len && (X || !a.causal || c <= r) ? p * (dp[i][j] - delta[i]) : 0.f;
       }
     __syncthreads();
     pk_pb<DP>(dq, sS, sK);
@@ -350,18 +352,18 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
   pk_store<T, DP>(a.dq, s, q0, h, a.dim, dq, f);
 }
 
-template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void pk_dkv_block(const PackedArgs& a, int block, int part, int parts) {
-  const SeqTile s = find_tile(a.cu_kv, a.n_seqs, a.kv_tokens, block / a.kv_heads, kLog<R>);
+template <typename T, int DP, bool VEC, int R, bool X> __device__ __forceinline__ void pk_dkv_block(const PackedArgs& a, int block, int part, int parts) {
+  const SeqTile s = find_tile(X ? a.cu_kv : a.cu, a.n_seqs, X ? a.kv_tokens : a.tokens, block / a.kv_heads, kLog<R>);
   if (s.tile < 0) { pdl_wait(); return; }
-  const SeqTile qs = other_side(a.cross, s, a.cu, a.tokens);
+  const SeqTile qs = X ? other_side(s, a.cu, a.tokens) : s;
   extern __shared__ float sm[];
   float *sK = sm, *sV = sK + R * kPkLd<DP>, *sQ = sV + R * kPkLd<DP>, *sO = sQ + PK_T * kPkLd<DP>, *sP = sO + PK_T * kPkLd<DP>,
         *sS = sP + R * PK_LDP, *sR = sS + R * PK_LDP;
   const int hk = block % a.kv_heads, k0 = s.tile * R;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int first = a.causal ? k0 : 0, per_head = (qs.len - first + PK_T - 1) / PK_T;
+  const int first = !X && a.causal ? k0 : 0, per_head = (qs.len - first + PK_T - 1) / PK_T, some = X ? max(per_head, 1) : per_head;
   const int it0 = per_head * a.group * part / parts, it1 = per_head * a.group * (part + 1) / parts;
-  int h = hk * a.group + it0 / max(per_head, 1), q0 = first + it0 % max(per_head, 1) * PK_T;
+  int h = hk * a.group + it0 / some, q0 = first + it0 % some * PK_T;
   // a query tile's lse (threads 0 .. 63) and delta (64 .. 127) travel with it
   auto row_value = [&](int h, int q0) {
     const int r = q0 + (threadIdx.x & 63);
@@ -403,7 +405,7 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int c = k0 + 4 * ty + i;
-        const bool in = c < s.len && r < qs.len && (!a.causal || c <= r);
+        const bool in = c < s.len && r < qs.len && (X || !a.causal || c <= r);
         const float p = in ? ex2((acc[i][j] * a.scale - lse) * kLog2e) : 0.f;
         sP[(4 * ty + i) * PK_LDP + tx + 16 * j] = p;
         sS[(4 * ty + i) * PK_LDP + tx + 16 * j] = in ? p * (dp[i][j] - delta) : 0.f;
@@ -429,13 +431,14 @@ template <typename T, int DP, bool VEC, int R> __device__ __forceinline__ void p
   pk_store<T, DP>(a.dv, s, k0, hk, a.dim, dv, one);
 }
 
-// The blocks of dk and dv, and behind them those of dq.
-template <typename T, int DP, bool VEC, int R>
-__global__ void __launch_bounds__(4 * R) attn_packed_bwd_kernel(PackedArgs a, int dkv_blocks) {
+// The blocks of dk and dv, and behind them those of dq.  Two blocks to an SM for heads of 32, which the compiler may else give up for a
+// few registers more (2 x 1024 tokens, 16 heads, unaligned: 282 us; with 150 registers 305 in fp32, 334 in bf16).
+template <typename T, int DP, bool VEC, int R, bool X>
+__global__ void __launch_bounds__(4 * R, R == 64 && DP == 32 ? 2 : 0) attn_packed_bwd_kernel(PackedArgs a, int dkv_blocks) {
   const int parts = pk_split<R> ? (int)cg::this_cluster().num_blocks() : 1, part = pk_split<R> ? (int)cg::this_cluster().block_rank() : 0;
   const int block = blockIdx.x / parts;
-  if (block < dkv_blocks) pk_dkv_block<T, DP, VEC, R>(a, block, part, parts);
-  else pk_dq_block<T, DP, VEC, R>(a, block - dkv_blocks, part, parts);
+  if (block < dkv_blocks) pk_dkv_block<T, DP, VEC, R, X>(a, block, part, parts);
+  else pk_dq_block<T, DP, VEC, R, X>(a, block - dkv_blocks, part, parts);
 }
 
 // raises a kernel's shared-memory limit once per device
@@ -449,43 +452,46 @@ template <typename K> static cudaError_t pk_allow(K kernel, int bytes, std::atom
   return e;
 }
 
-template <typename T, int DP, bool VEC, int R> static cudaError_t pk_forward(const PackedArgs& a, cudaStream_t st) {
+template <typename T, int DP, bool VEC, int R, bool X> static cudaError_t pk_forward(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   constexpr int smem = pk_smem<DP, R>(1, 2, 1);
   const int64_t blocks = most_tiles(a.tokens, a.n_seqs, R) * a.heads;
   if (!launchable(blocks)) return cudaErrorInvalidConfiguration;
-  const cudaError_t e = pk_allow(attn_packed_fwd_kernel<T, DP, VEC, R>, smem, done);
+  const cudaError_t e = pk_allow(attn_packed_fwd_kernel<T, DP, VEC, R, X>, smem, done);
   if (e != cudaSuccess) return e;
-  return launch_clusters(attn_packed_fwd_kernel<T, DP, VEC, R>, blocks, 4 * R, smem, st, false, pk_split<R> ? forward_parts(blocks, a, PK_T, 4 * kSms, 3) : 1, a);
+  return launch_clusters(attn_packed_fwd_kernel<T, DP, VEC, R, X>, blocks, 4 * R, smem, st, false, pk_split<R> ? forward_parts(blocks, a, PK_T, 4 * kSms, 3) : 1, a);
 }
-template <typename T, int DP, bool VEC, int R> static cudaError_t pk_backward(const PackedArgs& a, cudaStream_t st) {
+template <typename T, int DP, bool VEC, int R, bool X> static cudaError_t pk_backward(const PackedArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   constexpr int smem = pk_smem<DP, R>(2, 2, 2);
   const int64_t dkv = most_tiles(a.kv_tokens, a.n_seqs, R) * a.kv_heads, blocks = most_tiles(a.tokens, a.n_seqs, R) * a.heads + dkv;
   if (!launchable(blocks)) return cudaErrorInvalidConfiguration;
-  cudaError_t e = pk_allow(attn_packed_bwd_kernel<T, DP, VEC, R>, smem, done);
+  cudaError_t e = pk_allow(attn_packed_bwd_kernel<T, DP, VEC, R, X>, smem, done);
   if (e == cudaSuccess) e = launch_pdl(attn_packed_delta_kernel<T>, dim3((unsigned)((a.tokens * a.heads + 7) / 8)), dim3(256), 0, st, false, a);
   if (e == cudaSuccess)
-    e = launch_clusters(attn_packed_bwd_kernel<T, DP, VEC, R>, blocks, 4 * R, smem, st, true, pk_split<R> ? backward_parts(blocks, a, PK_T, 4 * kSms, 2) : 1, a,
+    e = launch_clusters(attn_packed_bwd_kernel<T, DP, VEC, R, X>, blocks, 4 * R, smem, st, true, pk_split<R> ? backward_parts(blocks, a, PK_T, 4 * kSms, 2) : 1, a,
                   (int)dkv);
   return e;
 }
-template <typename T, int DP, bool VEC> static cudaError_t pk_rows(const PackedArgs& a, bool backward, cudaStream_t st) {
+template <typename T, int DP, bool VEC, bool X> static cudaError_t pk_rows(const PackedArgs& a, bool backward, cudaStream_t st) {
   // 32 rows to a block where blocks of 64 would leave SMs without one (as a rule on the most tiles that the lengths can make)
   const bool small = most_tiles(a.tokens, a.n_seqs, PK_T) * a.heads + (backward ? most_tiles(a.kv_tokens, a.n_seqs, PK_T) * a.kv_heads : 0) < 2 * kSms;
-  if (small) return backward ? pk_backward<T, DP, VEC, 32>(a, st) : pk_forward<T, DP, VEC, 32>(a, st);
-  return backward ? pk_backward<T, DP, VEC, 64>(a, st) : pk_forward<T, DP, VEC, 64>(a, st);
+  if (small) return backward ? pk_backward<T, DP, VEC, 32, X>(a, st) : pk_forward<T, DP, VEC, 32, X>(a, st);
+  return backward ? pk_backward<T, DP, VEC, 64, X>(a, st) : pk_forward<T, DP, VEC, 64, X>(a, st);
 }
-template <typename T, int DP> static cudaError_t pk_width(const PackedArgs& a, bool backward, cudaStream_t st) {
+template <typename T, int DP, bool X> static cudaError_t pk_width(const PackedArgs& a, bool backward, cudaStream_t st) {
   // four elements at a time where every row of the inputs starts at such a boundary
   const size_t bytes = 4 * sizeof(T);
   bool vec = a.dim % 4 == 0;
   for (const HeadView* x : {&a.q, &a.k, &a.v, backward ? &a.d_o : &a.q}) vec = vec && aligned_to(x->data, bytes) && x->token % 4 == 0 && x->head % 4 == 0;
-  return vec ? pk_rows<T, DP, true>(a, backward, st) : pk_rows<T, DP, false>(a, backward, st);
+  return vec ? pk_rows<T, DP, true, X>(a, backward, st) : pk_rows<T, DP, false, X>(a, backward, st);
+}
+template <typename T, bool X> static cudaError_t pk_kind(const PackedArgs& a, bool backward, cudaStream_t st) {
+  if (a.dim <= 32) return pk_width<T, 32, X>(a, backward, st);
+  return a.dim <= 64 ? pk_width<T, 64, X>(a, backward, st) : pk_width<T, 128, X>(a, backward, st);
 }
 template <typename T> static cudaError_t pk_run(const PackedArgs& a, bool backward, cudaStream_t st) {
-  if (a.dim <= 32) return pk_width<T, 32>(a, backward, st);
-  return a.dim <= 64 ? pk_width<T, 64>(a, backward, st) : pk_width<T, 128>(a, backward, st);
+  return a.cross ? pk_kind<T, true>(a, backward, st) : pk_kind<T, false>(a, backward, st);
 }
 
 static pm_status pk_check(const pm_attention_desc* d) {

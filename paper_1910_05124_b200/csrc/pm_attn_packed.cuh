@@ -109,9 +109,8 @@ __device__ __forceinline__ SeqTile find_tile(const int32_t* cu, int n_seqs, int6
   return find_slot(cu, n_seqs, (int)tokens, index, log_rows);
 }
 
-// The rows of the other side that a tile's sequence meets: of an encoder's states with `cross`, else its own tokens.  Clipped as above.
-__device__ __forceinline__ SeqTile other_side(bool cross, const SeqTile& s, const int32_t* cu, int64_t tokens) {
-  if (!cross) return s;
+// The rows of cross attention's other side that a tile's sequence meets.  Clipped as above.
+__device__ __forceinline__ SeqTile other_side(const SeqTile& s, const int32_t* cu, int64_t tokens) {
   const int begin = min(max(cu[s.seq], 0), (int)tokens), end = min(max(cu[s.seq + 1], 0), (int)tokens);
   return SeqTile{begin, max(end - begin, 0), 0, s.seq};
 }
@@ -121,7 +120,7 @@ __device__ __forceinline__ SeqTile find_pair(const int32_t* cu, const int32_t* c
   if (n_seqs <= 32) return find_counted<1>(cu, n_seqs, (int)tokens, index, log_rows, cu_other, (int)other_tokens, &there);
   if (n_seqs <= 256) return find_counted<8>(cu, n_seqs, (int)tokens, index, log_rows, cu_other, (int)other_tokens, &there);
   const SeqTile s = find_slot(cu, n_seqs, (int)tokens, index, log_rows);
-  if (s.tile >= 0) there = other_side(true, s, cu_other, other_tokens);
+  if (s.tile >= 0) there = other_side(s, cu_other, other_tokens);
   return s;
 }
 
