@@ -73,9 +73,12 @@ struct PolicyToken {
     if (clipped) sums[4] += w;
     if (a.ref_logprob) {
       const float d = ref - lp;
-      // e^d - 1 and e^d - 1 - d.  The second loses its bits for small d: there its series d^2 (1/2 + d/6 + ...), the next term below 2^-28 of
-      // the sum; from 1/2 on the exponential's own error is at most two and a half times as large in either.
-      float s = 1.f / 362880.f;
+      // e^d - 1 and e^d - 1 - d.  The second loses its bits for small d: there its series d^2 (1/2 + d/6 + ...), the next term below 2^-27 of
+      // the sum.  From 1 on it has the exponential's own error e^d / (e^d - 1 - d) times, at most 3.8, and the first 1.6 times; behind -1
+      // neither has more than the exponential.  (From 1/2 on it would be 11 times.)
+      float s = 1.f / 39916800.f;
+      s = fmaf(s, d, 1.f / 3628800.f);
+      s = fmaf(s, d, 1.f / 362880.f);
       s = fmaf(s, d, 1.f / 40320.f);
       s = fmaf(s, d, 1.f / 5040.f);
       s = fmaf(s, d, 1.f / 720.f);
@@ -83,7 +86,7 @@ struct PolicyToken {
       s = fmaf(s, d, 1.f / 24.f);
       s = fmaf(s, d, 1.f / 6.f);
       s = fmaf(s, d, 0.5f);
-      const bool near = fabsf(d) < 0.5f;
+      const bool near = fabsf(d) < 1.f;
       const float far = expf(d) - 1.f, kl = near ? d * d * s : far - d, slope = near ? d + kl : far;
       sums[2] += (double)w * kl;
       if (a.kl_coef != 0.0) grad -= (float)a.kl_coef * slope;        // measured alone: an infinite slope has no part of the gradient
