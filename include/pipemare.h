@@ -519,8 +519,9 @@ pm_status pm_head_norm_rotate_backward(const pm_head_norm_desc* desc, const pm_h
  * Philox4x32-10 with the key rng[0] (its lower 32 bits first) and the counter rng[1] + i / 8 modulo 2^64 (lower word first, the two
  * upper words zero): of its four words, word (i mod 8) / 2, the lower half for even i.  rng: two int64 on the device, read when the call runs, so a captured graph draws
  * anew when the program moves rng[1] on by (n + 7) / 8 or more between replays; the backward call takes the rng of its forward
- * call.  What is dropped may be NaN or infinite.  One rounding, of the result.  y may be x or the residual itself; any other
- * overlap is refused.  The backward pass of the residual is the identity. */
+ * call.  What is dropped may be NaN or infinite.  The scale is rounded to fp32; product and sum (or the product alone) are
+ * one operation with one rounding to fp32, and a bf16 result is rounded once more, from that.  y may be x or the residual itself; any
+ * other overlap is refused.  The backward pass of the residual is the identity. */
 pm_status pm_dropout(const void* x, const void* residual, int32_t dtype, int64_t n, double p, const int64_t* rng, void* y, void* stream);
 pm_status pm_dropout_backward(const void* d_y, int32_t dtype, int64_t n, double p, const int64_t* rng, void* d_x, void* stream);
 

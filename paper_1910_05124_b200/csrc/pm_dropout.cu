@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kDropThreads, kDropBlocks<T, RES>) dropout_ker
 
 template <typename T> static cudaError_t dropout_run(const void* x, const void* residual, void* y, int64_t n, const int64_t* rng, uint32_t dropped, cudaStream_t st) {
   const bool vec = aligned_to(x, 16) && aligned_to(residual, 16) && aligned_to(y, 16);
-  const float scale = 65536.f / (float)(65536u - dropped);
+  const float scale = 65536.f / (float)(65536u - dropped);                       // rounded: off by 2^-24 of itself at most, all elements alike
   const int64_t groups = (n + 8 * kDropThreads - 1) / (8 * kDropThreads);        // blocks with one vector to a thread
   auto go = [&](auto kernel, int64_t blocks) {
     return launch_pdl(kernel, dim3((unsigned)blocks), dim3(kDropThreads), 0, st, false, static_cast<const T*>(x), static_cast<const T*>(residual), static_cast<T*>(y), n,
