@@ -484,7 +484,8 @@ pm_status pm_attention_packed_selftest_wait_timeout(int64_t limit_cycles, void* 
  * of 2^-64 turns per position, read during the call, as pm_rotation_turns fills it for f_i = base^(-2 i / rotary_dim) (base at
  * least 1); angles are exact to 2^-33 turns at every position, negative ones among them, their sines and cosines to 2.4e-7.  positions: int32 [n_tokens] on the
  * device, not looked at with rotary_dim 0.  Gains are floats whatever dtype is.  Squares are summed in fp32: a row whose mean square
- * leaves its range (values beyond 1e18) gives zeros; eps may be 0, a row of zeros is then NaN.  A value that is not finite reaches
+ * leaves its range (values beyond 1e18) gives zeros, and zero gradients; eps may be 0, a row whose mean square is below 1e-36 then gives
+ * results that are off, infinite or NaN.  A value that is not finite reaches
  * the results of its row (and, in the backward pass, the gains' gradients) alone.
  * n_heads or n_kv_heads may be 0, the arguments of that side then count for nothing (queries of cross attention, whose keys
  * were normed when the encoder ran). */

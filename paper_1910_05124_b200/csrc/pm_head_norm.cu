@@ -310,6 +310,9 @@ __global__ void __launch_bounds__(kNormThreads, BACKWARD ? 2 : 3) head_norm_kern
 #pragma unroll
       for (int e = 0; e < V / 2; ++e) square = fma_f32x2(x.s[e], x.s[e], fma_f32x2(x.f[e], x.f[e], square));
       const float2 r = both(rsqrtf(group_sum<L>(on ? square.x + square.y : 0.f) * per + p.eps));
+      if (r.x == 0.f)                             // the squares left the range of fp32, and a product might before r makes it zero
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) { x.f[e] = mul_f32x2(x.f[e], r); x.s[e] = mul_f32x2(x.s[e], r); }
 #pragma unroll
       for (int e = 0; e < V / 2; ++e) {           // y_a = r (x_a g_a cos - x_b g_b sin), y_b = r (x_b g_b cos + x_a g_a sin)
         const float2 f = mul_f32x2(r, fma_f32x2(x.f[e], cs.f[e], mul_f32x2(x.s[e], gs.s[e])));
@@ -330,7 +333,8 @@ __global__ void __launch_bounds__(kNormThreads, BACKWARD ? 2 : 3) head_norm_kern
         dot = fma_f32x2(mul_f32x2(x.s[e], u.s[e]), g.s[e], fma_f32x2(mul_f32x2(x.f[e], u.f[e]), g.f[e], dot));
       }
       const float r = rsqrtf(group_sum<L>(on ? square.x + square.y : 0.f) * per + p.eps);
-      const float2 rr = both(on ? r : 0.f), f = both(group_sum<L>(on ? dot.x + dot.y : 0.f) * per * r * r * -r);
+      const float mean = group_sum<L>(on ? dot.x + dot.y : 0.f) * per;
+      const float2 rr = both(on ? r : 0.f), f = both(r == 0.f ? 0.f : mean * r * r * -r);      // with r the sum of products may have left the range, too
 #pragma unroll
       for (int e = 0; e < V / 2; ++e) {
         u.f[e] = mul_f32x2(u.f[e], rr);
@@ -408,7 +412,7 @@ __global__ void __launch_bounds__(kNormThreads) head_norm_any_kernel(const __gri
       turn(u);
 #pragma unroll
       for (int j = 0; j < 4; ++j) dot = fmaf(x[j], u[j] * g[j], dot);
-      const float f = group_sum<32>(dot) * per * r * r;
+      const float mean = group_sum<32>(dot) * per, f = r == 0.f ? 0.f : mean * r * r;         // with r the sum of products may have left the range, too
       T* out = head_row_out<T>(s.dx, now.token, now.h);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
