@@ -114,20 +114,16 @@ __device__ __forceinline__ SeqTile other_side(const SeqTile& s, const int32_t* c
   const int begin = min(max(cu[s.seq], 0), (int)tokens), end = min(max(cu[s.seq + 1], 0), (int)tokens);
   return SeqTile{begin, max(end - begin, 0), 0, s.seq};
 }
-// find_tile and other_side of cross attention in one round of loads, where the sequences are counted
-__device__ __forceinline__ SeqTile find_pair(const int32_t* cu, const int32_t* cu_other, int n_seqs, int64_t tokens, int64_t other_tokens, int index, int log_rows,
-                                             SeqTile& there) {
-  if (n_seqs <= 32) return find_counted<1>(cu, n_seqs, (int)tokens, index, log_rows, cu_other, (int)other_tokens, &there);
-  if (n_seqs <= 256) return find_counted<8>(cu, n_seqs, (int)tokens, index, log_rows, cu_other, (int)other_tokens, &there);
-  const SeqTile s = find_slot(cu, n_seqs, (int)tokens, index, log_rows);
-  if (s.tile >= 0) there = other_side(s, cu_other, other_tokens);
-  return s;
-}
-
-// find_pair with the tiles of the sequence that has the longest other side first, where a warp holds all sequences.
+// find_tile and other_side of cross attention, in one round of loads where the sequences are counted.  Where a warp holds all sequences the tiles
+// of the one that has the longest other side come first.
 __device__ __forceinline__ SeqTile find_longest(const int32_t* cu, const int32_t* cu_other, int n_seqs, int64_t tokens, int64_t other_tokens, int index, int log_rows,
                                                 SeqTile& there) {
-  if (n_seqs > 32) return find_pair(cu, cu_other, n_seqs, tokens, other_tokens, index, log_rows, there);
+  if (n_seqs > 256) {
+    const SeqTile s = find_slot(cu, n_seqs, (int)tokens, index, log_rows);
+    if (s.tile >= 0) there = other_side(s, cu_other, other_tokens);
+    return s;
+  }
+  if (n_seqs > 32) return find_counted<8>(cu, n_seqs, (int)tokens, index, log_rows, cu_other, (int)other_tokens, &there);
   const int lane = threadIdx.x & 31;
   auto start = [&](const int32_t* c, int64_t most, int b) { return min(max(c[min(b, n_seqs)], 0), (int)most); };
   const int begin = start(cu, tokens, lane), far = start(cu_other, other_tokens, lane);
