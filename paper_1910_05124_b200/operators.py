@@ -115,37 +115,6 @@ def _launch_with(workspace, call, args, device, stream):
     _launch(call, (*args, scratch.data_ptr(), workspace), device, stream)
 
 
-def _head_views(shapes, dtype, device, names, tensors, n_read):
-    """A pm_head_view for each of the tensors, of these shapes ([tokens, heads, head_dim]), checked; those behind the first n_read are
-    written.  A shape of None gives None."""
-    index, views = device.index, []
-    for t, shape in zip(tensors, shapes):
-        if shape is None:
-            views.append(None)
-            continue
-        if not (isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == index and t.shape == shape):
-            _mismatch(names[len(views)], t, dtype, device, shape)
-        tokens, h, d = shape
-        token, head, one = t.stride()
-        if one != 1 and d > 1:
-            _refuse(f"the last dimension of {names[len(views)]} must be contiguous")
-        if (head != d or token < h * d) and len(views) >= n_read:
-            _check_apart(names[len(views)], d, ((token, tokens), (head, h)))
-        views.append(_VIEW(t.data_ptr(), token, head))
-    return views
-
-
-def _check_apart(name, head_dim, dims):
-    """Rows of one head, or heads of one row, of a tensor that is written must not share elements."""
-    if min(n for _, n in dims) < 1:
-        return
-    end = head_dim
-    for stride, n in sorted((s, n) for s, n in dims if n > 1):
-        if stride < end:
-            _refuse(f"{name} overlaps itself")
-        end += stride * (n - 1)
-
-
 def _head_rows(name, t, heads, head_dim):
     """Device and number of tokens of a [tokens, heads, head_dim] tensor."""
     device = _compute_device(name, t)
@@ -154,7 +123,40 @@ def _head_rows(name, t, heads, head_dim):
     return device, t.shape[0]
 
 
-class _HeadAttention:
+class _HeadTensors:
+    """Views of [tokens, heads, head_dim] tensors, for classes with a head_dim."""
+
+    def _views(self, shapes, dtype, device, names, tensors, n_read):
+        """A pm_head_view for each of the tensors, of these shapes, checked; those behind the first n_read are written.  A shape of None gives
+        None."""
+        index, views = device.index, []
+        for t, shape in zip(tensors, shapes):
+            if shape is None:
+                views.append(None)
+                continue
+            if not (isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == index and t.shape == shape):
+                _mismatch(names[len(views)], t, dtype, device, shape)
+            tokens, h, d = shape
+            token, head, one = t.stride()
+            if one != 1 and d > 1:
+                _refuse(f"the last dimension of {names[len(views)]} must be contiguous")
+            if (head != d or token < h * d) and len(views) >= n_read:
+                self._check_apart(names[len(views)], ((token, tokens), (head, h)))
+            views.append(_VIEW(t.data_ptr(), token, head))
+        return views
+
+    def _check_apart(self, name, dims):
+        """Rows of one head, or heads of one row, of a tensor that is written must not share elements."""
+        if min(n for _, n in dims) < 1:
+            return
+        end = self.head_dim
+        for stride, n in sorted((s, n) for s, n in dims if n > 1):
+            if stride < end:
+                _refuse(f"{name} overlaps itself")
+            end += stride * (n - 1)
+
+
+class _HeadAttention(_HeadTensors):
     """What the attention classes share."""
 
     def __init__(self, n_heads, n_kv_heads, head_dim, scale):
@@ -177,9 +179,6 @@ class _HeadAttention:
         if not (cu.dtype is _I32 and cu.get_device() == device.index and cu.is_contiguous()):
             _mismatch(name, cu, _I32, device, (n,))
         return cu.data_ptr(), n - 1
-
-    def _check_apart(self, name, dims):
-        _check_apart(name, self.head_dim, dims)
 
     def pm_attention_packed_status(self, device="cuda", stream=None):
         """Raises if a device-side wait of a tensor-core kernel ran out since the last call on this device (a defect); synchronises
@@ -213,7 +212,7 @@ class PackedAttention(_HeadAttention):
     def pm_attention_packed_forward(self, q, k, v, cu_seqlens, o, lse=None, stream=None):
         """Writes o and, for a backward pass, lse."""
         device, Q, K, desc, cu = self._desc(q, cu_seqlens)
-        vq, vk, vv, vo = _head_views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
+        vq, vk, vv, vo = self._views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
         p_lse = _flat("lse", lse, _F32, device, (self.n_heads, Q[0]))
         _launch(self.L.pm_attention_packed_forward, (desc, vq, vk, vv, cu, vo, p_lse), device, stream)
 
@@ -222,7 +221,7 @@ class PackedAttention(_HeadAttention):
         device, Q, K, desc, cu = self._desc(q, cu_seqlens)
         if lse is None:
             _refuse("lse must be a tensor")
-        vq, vk, vv, vo, vdo, *grads = _head_views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
+        vq, vk, vv, vo, vdo, *grads = self._views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
                                                   (q, k, v, o, d_o, dq, dk, dv), 5)
         p_lse = _flat("lse", lse, _F32, device, (self.n_heads, Q[0]))
         _launch_with(4 * self.n_heads * Q[0], self.L.pm_attention_packed_backward, (desc, vq, vk, vv, vo, p_lse, vdo, cu, *grads), device, stream)
@@ -252,7 +251,7 @@ class CrossAttention(_HeadAttention):
     def pm_attention_cross_forward(self, q, k, v, cu_seqlens, cu_seqlens_kv, o, lse=None, stream=None):
         """Writes o and, for a backward pass, lse."""
         device, Q, K, desc, cu, cu_kv = self._desc(q, k, cu_seqlens, cu_seqlens_kv)
-        vq, vk, vv, vo = _head_views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
+        vq, vk, vv, vo = self._views((Q, K, K, Q), q.dtype, device, ("q", "k", "v", "o"), (q, k, v, o), 3)
         p_lse = _flat("lse", lse, _F32, device, (self.n_heads, Q[0]))
         _launch(self.L.pm_attention_cross_forward, (desc, vq, vk, vv, cu, cu_kv, vo, p_lse), device, stream)
 
@@ -261,13 +260,13 @@ class CrossAttention(_HeadAttention):
         device, Q, K, desc, cu, cu_kv = self._desc(q, k, cu_seqlens, cu_seqlens_kv)
         if lse is None:
             _refuse("lse must be a tensor")
-        vq, vk, vv, vo, vdo, *grads = _head_views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
+        vq, vk, vv, vo, vdo, *grads = self._views((Q, K, K, Q, Q, Q, K, K), q.dtype, device, ("q", "k", "v", "o", "d_o", "dq", "dk", "dv"),
                                                   (q, k, v, o, d_o, dq, dk, dv), 5)
         p_lse = _flat("lse", lse, _F32, device, (self.n_heads, Q[0]))
         _launch_with(4 * self.n_heads * Q[0], self.L.pm_attention_cross_backward, (desc, vq, vk, vv, vo, p_lse, vdo, cu, cu_kv, *grads), device, stream)
 
 
-class HeadNormRotate:
+class HeadNormRotate(_HeadTensors):
     """Root-mean-square norms of queries and keys for each head, with a gain, and the rotation of their first rotary_dim dimensions (None:
     all, 0: none) by the positions, in one pass.
 
@@ -320,13 +319,13 @@ class HeadNormRotate:
     def pm_head_norm_rotate(self, q, k, positions, q_gain, k_gain, q_out, k_out, stream=None):
         """Writes q_out and k_out, which may be q and k."""
         device, dtype, Q, K, desc, pos, gains = self._sides(q, k, positions, q_gain, k_gain)
-        vq, vk, *outs = _head_views((Q, K, Q, K), dtype, device, ("q", "k", "q_out", "k_out"), (q, k, q_out, k_out), 2)
+        vq, vk, *outs = self._views((Q, K, Q, K), dtype, device, ("q", "k", "q_out", "k_out"), (q, k, q_out, k_out), 2)
         _launch(self.L.pm_head_norm_rotate, (desc, vq, vk, pos, *gains, *outs), device, stream)
 
     def pm_head_norm_rotate_backward(self, q, k, positions, q_gain, k_gain, d_q_out, d_k_out, dq, dk, d_q_gain=None, d_k_gain=None, stream=None):
         """Writes dq and dk (which may be d_q_out and d_k_out) and the gains' gradients that are given."""
         device, dtype, Q, K, desc, pos, gains = self._sides(q, k, positions, q_gain, k_gain)
-        vq, vk, *views = _head_views((Q, K, Q, K, Q, K), dtype, device, ("q", "k", "d_q_out", "d_k_out", "dq", "dk"), (q, k, d_q_out, d_k_out, dq, dk), 4)
+        vq, vk, *views = self._views((Q, K, Q, K, Q, K), dtype, device, ("q", "k", "d_q_out", "d_k_out", "dq", "dk"), (q, k, d_q_out, d_k_out, dq, dk), 4)
         grads = _flats(("d_q_gain", "d_k_gain"), (d_q_gain, d_k_gain), torch.float32, device, (self.head_dim,))
         _launch_with(0 if d_q_gain is None and d_k_gain is None else self.ws_bytes, self.L.pm_head_norm_rotate_backward,
                      (desc, vq, vk, pos, *gains, *views, *grads), device, stream)
