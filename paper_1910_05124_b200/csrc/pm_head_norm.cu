@@ -508,8 +508,10 @@ template <typename T> static cudaError_t norm_run(NormArgs& p, bool interleaved,
   };
   const int vec = divides(kVec<T>) ? kVec<T> : divides(4) ? 4 : 1;
   const int lanes = vec > 1 ? norm_lanes(p.dim, vec) : 32;
-  // the blocks that run at a time go to the sides by their work: heads, and a token's angles, which take about as long as two rows (12291 tokens,
-  // 16 + 2 heads of 128: 22 us forward and 33 backward, by heads alone 25 and 38)
+  // the blocks that run at a time go to the sides by their work: heads, and a token's angles, which take about as long as two rows.  By heads alone
+  // the smaller side's blocks are the last by far, one to four rows are alike (12291 tokens, us forward / backward with none, one, two, four, bf16: 16 + 2
+  // heads of 128 25 / 38, 22 / 33, 22 / 33, 23 / 33; 40 + 1 of 64 35 / 51, 26 / 38, 26 / 38, 26 / 38; 32 + 8 of 128 52 / 73, 51 / 72, 51 / 72, 50 / 71; fp32, 8 + 1 of
+  // 128, 64 rotated, 23 / 36, 18 / 31, 18 / 31, 19 / 31)
   auto weight = [&](int n) { return n ? n + (p.rotary ? 2 : 0) : 0; };
   const int64_t per_block = kNormThreads / lanes;
   for (int i = 0; i < 2; ++i) {
