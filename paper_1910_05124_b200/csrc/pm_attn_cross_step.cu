@@ -7,8 +7,8 @@
 // handed from one product's accumulator to the other's operand).  fp32: a few lanes to a key for the scores, a few columns to a lane
 // for O.  The warps of a block and the blocks of a cluster that share a sequence's keys join their fp32 sums at the end in a fixed order.
 //
-// 16 sequences of 251 to 4016 keys, 16 heads of 64, a token each, bf16 (143 MB): 28 us, 5.0 TB/s; 55 with the 128-row tiles.  128 of 4096 keys,
-// 32 heads of 128 on 8 (2.1 GB): 299 us, 7.2 TB/s with what the 126 MB L2 keeps from call to call.
+// 16 sequences of 251 to 4016 keys, 16 heads of 64, a token each, bf16 (143 MB): 28 us, 5.0 TB/s; 48 with the 128-row tiles.  128 of 4096 keys,
+// 32 heads of 128 on 8 (2.1 GB): 296 us, 7.3 TB/s with what the 126 MB L2 keeps from call to call.
 #include <algorithm>
 #include <atomic>
 
@@ -519,9 +519,9 @@ static int step_log_tokens(const PackedArgs& a, int rows) {
 }
 
 // Rows (tokens times the heads that share a key) on average of a sequence that these kernels are the faster ones for; bf16 in what the tensor-core
-// kernels take.  us with these / the others: bf16, 16 x 8 tokens over 1000 keys, 16 heads of 128 on 4 (32 rows) 15.5 / 22.8; 64 x 20 over 60, 8 heads
-// of 64 (20) 8.0 / 11.7; 16 x 32 over 1000, 16 heads of 64 (32) 19.8 / 19.4; 16 x 64 (64) 34.7 / 19.7.  fp32, 16 x 8 over 1000, 16 heads of 128 on 4 121 / 160; 16 x 5
-// over 3000, 32 heads of 128 on 8 (20) 496 / 1720; but 16 x 20 over 1000, 16 heads of 64 177 / 148: heads that share keys are what the others repeat.
+// kernels take.  us with these / the others: bf16, 16 x 8 tokens over 1000 keys, 16 heads of 128 on 4 (32 rows) 15.1 / 22.4; 64 x 20 over 60, 8 heads
+// of 64 (20) 8.0 / 11.6; 16 x 32 over 1000, 16 heads of 64 (32) 20.0 / 19.7; 16 x 64 (64) 34.7 / 19.6.  fp32, 16 x 8 over 1000, 16 heads of 128 on 4 125 / 164; 16 x 5
+// over 3000, 32 heads of 128 on 8 (20) 490 / 1714; but 16 x 20 over 1000, 16 heads of 64 175 / 147: heads that share keys are what the others repeat.
 bool attn_cross_step_takes(const PackedArgs& a, int dtype) {
   const int64_t rows = a.tokens * a.group;
   if (!a.cross || rows > (int64_t)32 * a.n_seqs) return false;
@@ -547,18 +547,18 @@ template <typename E> static cudaError_t step_run(const PackedArgs& a, cudaStrea
   const int64_t units = most_tiles(a.tokens, a.n_seqs, 1 << log_tokens) * a.kv_heads, average = (a.kv_tokens + a.n_seqs - 1) / a.n_seqs;
   if (!launchable(units)) return cudaErrorInvalidConfiguration;      // parts are for launches of few
   // Many short sequences: a warp to a tile and nothing to join.  us with one / four warps to a tile, bf16: 256 tokens over 50 keys each, 16 heads
-  // of 64, 13 / 37; 600 over 100, 8 heads, 26 / 48; 64 over 512, 16 heads, 24.4 / 26.4.  fp32: 25 / 42, 51 / 55, 52 / 44.
+  // of 64, 14 / 33; 600 over 100, 8 heads, 27 / 39; 64 over 512, 16 heads, 24.3 / 25.7.  fp32: 25 / 42, 50 / 55, 51 / 44.
   if (units >= 4 * kSms && average <= E::kShort) return step_launch<E, 1>(a, units, 1, log_tokens, st);
   // Parts of at least four runs to a warp on average, as long as the launch has no more than four blocks to an SM: clusters cost what finer
-  // parts would gain (bf16, 16 sequences of 2133 keys, 16 heads of 64: 26 us with 272 blocks in two parts, 31 in four, 46 in eight; 8
-  // sequences of 300 keys: 6.9 whole, 8.8 in two).  Blocks without a tile, of which there may be many, do not count.
+  // parts would gain (bf16, 16 sequences of 2133 keys, 16 heads of 64: 25 us whole, 26 with 272 blocks in two parts, 31 in four, 46 in eight; 8
+  // sequences of 300 keys: 5.6 whole, 7.4 in two).  Blocks without a tile, of which there may be many, do not count.
   const int64_t tokens = (a.tokens + a.n_seqs - 1) / a.n_seqs, filled = std::min(units, (int64_t)a.n_seqs * ((tokens + (1 << log_tokens) - 1) >> log_tokens) * a.kv_heads);
   auto parts_of = [&](int team, int64_t most_blocks) {
     int parts = 1;
     while (parts < StepShape<E, 4>::kParts && filled * parts * 2 <= most_blocks && average >= (int64_t)parts * 2 * team * 4 * E::kKeys) parts *= 2;
     return parts;
   };
-  // Few tiles: eight warps to a block (one of 100000 keys, 8 heads of 128: 80 us, with four 112; one of 30000, 4 heads of 64 on 1: 22 / 30).
+  // Few tiles: eight warps to a block (one of 100000 keys, 8 heads of 128: 70 us, with four 100; one of 30000, 4 heads of 64 on 1: 19 / 30).
   if (filled * 8 <= kSms) return step_launch<E, 8>(a, units, parts_of(8, kSms), log_tokens, st);
   return step_launch<E, 4>(a, units, parts_of(4, 4 * kSms), log_tokens, st);
 }

@@ -564,8 +564,8 @@ attn_packed_fwd_tc_kernel(const __grid_constant__ PackedArgs a, const __grid_con
 //
 // The same work by blocks that stay: a block takes query tiles in turn, and the copies and products of the next tile run while the
 // softmax warps bring the last one's rows out; in short sequences the ends of a tile (its place, the first copies, the barriers between
-// the first products and the last rows) are most of its time.  16 x 256 tokens over 100 to 475 keys, 16 heads of 64: 20.1 us with a block to
-// a tile, 17.1 with these; 100 x 100 over 300, 64 and 46; 4096 over 8192, 211 and 204.
+// the first products and the last rows) are most of its time.  16 x 256 tokens over 100 to 475 keys, 16 heads of 64: 19.1 us with a block to
+// a tile, 17.0 with these; 100 x 100 over 300, 64 and 46; 4096 over 8192, 213 and 205.
 //
 // Key tiles are counted through all tiles of a block: g-th of all, in stage g mod 2, its barriers' phases by g.  The places of a block's
 // tiles, 32 at most, are found at the start by all its warps.
