@@ -333,16 +333,18 @@ __global__ void __launch_bounds__(kNormThreads, BACKWARD ? 2 : 3) head_norm_kern
         dot = fma_f32x2(mul_f32x2(x.s[e], u.s[e]), g.s[e], fma_f32x2(mul_f32x2(x.f[e], u.f[e]), g.f[e], dot));
       }
       const float r = rsqrtf(group_sum<L>(on ? square.x + square.y : 0.f) * per + p.eps);
+      // x r before it meets anything else: r^2 mean by itself leaves the normal range of fp32 where rows are large and gradients small (1e17 and
+      // 1e-6).  With r = 0 the sum of products may have left it, too.
       const float mean = group_sum<L>(on ? dot.x + dot.y : 0.f) * per;
-      const float2 rr = both(on ? r : 0.f), f = both(r == 0.f ? 0.f : mean * r * r * -r);      // with r the sum of products may have left the range, too
+      const float2 rr = both(on ? r : 0.f), f = both(r == 0.f ? 0.f : mean * -r);
 #pragma unroll
       for (int e = 0; e < V / 2; ++e) {
-        u.f[e] = mul_f32x2(u.f[e], rr);
-        u.s[e] = mul_f32x2(u.s[e], rr);
+        x.f[e] = mul_f32x2(x.f[e], rr);
+        x.s[e] = mul_f32x2(x.s[e], rr);
         acc.f[e] = fma_f32x2(u.f[e], x.f[e], acc.f[e]);
         acc.s[e] = fma_f32x2(u.s[e], x.s[e], acc.s[e]);
-        u.f[e] = fma_f32x2(x.f[e], f, mul_f32x2(u.f[e], g.f[e]));
-        u.s[e] = fma_f32x2(x.s[e], f, mul_f32x2(u.s[e], g.s[e]));
+        u.f[e] = mul_f32x2(fma_f32x2(x.f[e], f, mul_f32x2(u.f[e], g.f[e])), rr);
+        u.s[e] = mul_f32x2(fma_f32x2(x.s[e], f, mul_f32x2(u.s[e], g.s[e])), rr);
       }
       if (on) at.store(out, apart, u);
     }

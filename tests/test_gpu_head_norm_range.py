@@ -36,3 +36,13 @@ def test_rows_within_the_range(cuda_device, dtype, spread):
     import paper_1910_05124_b200 as pm
     for D in (64, 40, 36):
         check(pm.HeadNormRotate(D, eps=0.0), *make(20, 2, 2, D, dtype, cuda_device, spread=spread, seed=4))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("spread,small", [(1e17, 1e-6), (1e15, 1e-9), (1e-17, 1e6), (1e17, 1e6), (1e-17, 1e-12)])
+def test_rows_and_gradients_of_other_sizes(cuda_device, dtype, spread, small):
+    """Every product of the formula that has to be formed lies within the range."""
+    import paper_1910_05124_b200 as pm
+    for D in (64, 40, 36):
+        q, k, d_q, d_k, gains, positions = make(20, 2, 2, D, dtype, cuda_device, spread=spread, seed=5)
+        check(pm.HeadNormRotate(D, eps=0.0), q, k, d_q * small, d_k * small, gains, positions)
