@@ -412,7 +412,7 @@ typedef struct {
  * is lse).  head_dim: 1 to 128.  A value that is not finite spreads over the results of its own sequence (in the
  * backward pass, and through v, to positions before it, too) and to no other.  A row whose every score is -infinity has
  * lse -infinity and no distribution: its o is NaN, and so are its dq and the dk and dv of the keys that it sees.
- * Scores are to lie within 1e9 in size: beyond, where their products with log2(e) are more than 64 apart, a row may be NaN.  The backward
+ * Scores are to lie within 1e9 in size: beyond, where fp32 has steps of more than 64, a row may be NaN.  The backward
  * pass forms e^(s - lse), no more exact than the fp32 lse: off by up to 2^-22 |lse| of itself.
  * Entries of cu_seqlens outside 0 .. n_tokens are clipped to that range; if they do not ascend, the results of the
  * sequences concerned (of all, where there are more than 256) are undefined, and no tensor is touched outside its rows.
